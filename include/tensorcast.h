@@ -440,6 +440,134 @@ TC_API int tc_plan_destroy(tc_plan_t *plan);
 TC_API int tc_kv_pack_noalloc(const tc_plan_spec_t *spec, const void *const *src_bases, size_t n_src,
                               void *const *dst_bases, size_t n_dst, void *stream);
 
+/* ---- operators on one layer of a paged pool ----------------------------------------------
+ *
+ * The plans above move a pool's bytes.  The calls below fill a pool with numbers, read them back
+ * and answer queries from it, one layer per call, in the same block layouts:
+ *   tc_kv_append    new tokens' K and V (and Q) with rotary positions, quantised as they are written
+ *   tc_kv_gather    pages of a pool, quantised or not, back into contiguous rows
+ *   tc_attn_decode  attention of one query token per request over a prefix that the whole batch
+ *                   shares, read once for all of it, and over the request's own pages
+ *
+ * Quantised pools hold one byte per element, code, and one fp32 scale per (token, head) of K and
+ * of V: the value is code * scale.  The scales are a paged pool of their own, addressed by the
+ * formulas at the top of this file with D = 1 and E = 4 - so a TC_KV_* plan of shape (L, B, H, 1, 4)
+ * packs, unpacks and migrates them beside the codes.  A row y of D numbers is written as
+ *     a = max |y_i|,  scale = a / Q  (Q = 448 for TC_E4M3, 127 for TC_INT8),  code_i = round(y_i / scale)
+ * in fp32, to nearest even.  A scale below 2^-126 is written as 0 with codes 0; a row that holds
+ * an infinity or a NaN gets scale NaN and codes 0, so that all of it reads back as NaN.
+ *
+ * The structs are HOST memory, read before the call returns; every pointer inside them is DEVICE-
+ * addressable (device memory of the current device, or pinned and mapped host memory) and belongs
+ * to the caller.  Block tables, lengths, slots and positions are DEVICE arrays, so that a captured
+ * call can be replayed with new ones; only the sizes that the structs hold are fixed by a capture.
+ * What the host cannot see is checked by the kernels: a block id, slot, position or length out of
+ * its range sets TC_DEVICE_BAD_INDEX in the device status word (tc_device_status) and the row or
+ * key that it would have named is neither read nor written.  Nothing is allocated, nothing is
+ * kept from call to call, and calls on different streams may run at once on different outputs
+ * (and workspaces).  Strides are in BYTES; the D elements of a row are contiguous everywhere.
+ * Every address and stride is a multiple of its element's size; where all are multiples of 16
+ * bytes (and D of 8) rows move as 16-byte vectors, elsewhere tc_kv_append and tc_kv_gather fall
+ * back to single elements.  A request for nothing (no tokens, no rows) returns TC_OK at once. */
+typedef enum {
+    TC_BF16 = 1,
+    TC_FP16 = 2,
+    TC_FP32 = 3,
+    TC_E4M3 = 4, /* pools only: 8-bit float, 4 exponent and 3 mantissa bits, no infinities */
+    TC_INT8 = 5  /* pools only */
+} tc_dtype;
+
+/* One layer of a paged pool. */
+typedef struct {
+    uint32_t struct_size;    /* sizeof(tc_kv_layer_t) */
+    int32_t dtype;           /* tc_dtype of the pool's elements */
+    int64_t B, H, D;         /* tokens per block, KV heads, head dim */
+    tc_kv_pool_t pool;       /* layout, num_blocks and block_stride are used (0 = tight) */
+    tc_kv_pool_t scale_pool; /* quantised pools: the same of the scale pool (its num_blocks >= pool's) */
+    void *k, *v;             /* planes (l,0) and (l,1) of the pool */
+    void *k_scale, *v_scale; /* quantised pools: planes (l,0) and (l,1) of the scale pool; else NULL */
+} tc_kv_layer_t;
+
+/* Token i's heads go to slot slots[i] = block * B + (position in the block); negative: the token is
+ * padding, neither its pool rows nor its q_out row are written.  A slot may appear once per call
+ * (twice: one of the two tokens' rows is left there, possibly parts of both).
+ * With rot_dim > 0 the first rot_dim elements of every K and Q row are rotated by row positions[i]
+ * of the cos / sin tables first:
+ *   pairs (x_j, x_{j + rot_dim/2}), or (x_2j, x_{2j+1}) with TC_ROPE_INTERLEAVED,
+ *   become (x cos_j - x' sin_j, x' cos_j + x sin_j), each product and sum rounded to fp32.
+ * How positions are scaled for long contexts is in the tables.  V is never rotated. */
+typedef struct {
+    uint32_t struct_size; /* sizeof(tc_kv_append_t) */
+    uint32_t flags;       /* TC_ROPE_INTERLEAVED or 0 */
+    int64_t n_tokens;
+    int64_t Hq;           /* query heads (q != NULL) */
+    int32_t dtype;        /* TC_BF16, TC_FP16 or TC_FP32: of q, k, v and q_out */
+    int32_t rot_dim;      /* even, 0..D; 0 = no rotation */
+    const void *q;        /* [n_tokens][Hq][D] or NULL */
+    void *q_out;          /* the rotated queries; may be q itself (same strides) */
+    const void *k, *v;    /* [n_tokens][H][D] */
+    int64_t q_stride[2], q_out_stride[2], k_stride[2], v_stride[2]; /* token, head */
+    const int64_t *slots;     /* [n_tokens] */
+    const int64_t *positions; /* [n_tokens] (rot_dim > 0) */
+    const float *cos, *sin;   /* [n_positions][rot_dim / 2] */
+    int64_t n_positions, table_stride; /* rows of the tables, and bytes from row to row */
+} tc_kv_append_t;
+#define TC_ROPE_INTERLEAVED 1u
+
+TC_API int tc_kv_append(const tc_kv_layer_t *layer, const tc_kv_append_t *args, void *stream);
+
+/* Row offsets[r] + i of k_out and v_out <- token first[r] + i of request r, for i in
+ * [0, offsets[r+1] - offsets[r]); token t lives in block tables[r][t / B], slot t % B.  Rows at and
+ * past offsets[R] are left as they were. */
+typedef struct {
+    uint32_t struct_size;   /* sizeof(tc_kv_gather_t) */
+    int32_t dtype;          /* TC_BF16, TC_FP16 or TC_FP32: of k_out and v_out */
+    int64_t R;              /* requests */
+    int64_t n_rows;         /* rows of k_out and v_out: offsets past it are out of range */
+    const int32_t *tables;  /* [R][table_width] block ids */
+    int64_t table_width, table_stride; /* entries per request, bytes from request to request */
+    const int64_t *offsets; /* [R + 1], from 0, not decreasing */
+    const int64_t *first;   /* [R] first token of each request, or NULL = 0 */
+    void *k_out, *v_out;    /* [n_rows][H][D]; either may be NULL */
+    int64_t k_stride[2], v_stride[2]; /* row, head */
+} tc_kv_gather_t;
+
+TC_API int tc_kv_gather(const tc_kv_layer_t *layer, const tc_kv_gather_t *args, void *stream);
+
+/* For every request r and query head h, with KV head h / (Hq / H) and keys j = the *prefix_len tokens of
+ * the prefix followed by the lens[r] tokens of the request's own table:
+ *   s_j = scale * (q . k_j),  out[r][h] = sum_j exp(s_j) v_j / sum_j exp(s_j),  lse[r][h] = log sum_j exp(s_j)
+ * A request without keys (and one whose every s_j is -infinity) gets out 0 and lse -infinity;
+ * lens[r] < 0: the request is padding, its rows of out and lse are left as they were.
+ * Pages are read once per call for the prefix (per 256 rows of queries and KV head) and once for
+ * each request's own; slots past a length are never read.
+ * D is a multiple of 16 up to 256, every address and stride a multiple of 16 bytes (tables, lens,
+ * prefix_len, lse and the scales: of 4).  An unquantised pool has the queries' type. */
+typedef struct {
+    uint32_t struct_size; /* sizeof(tc_attn_decode_t) */
+    int32_t dtype;        /* TC_BF16 or TC_FP16: of q and out */
+    int64_t R, Hq;        /* requests, query heads (a multiple of H) */
+    const void *q;        /* [R][Hq][D] */
+    void *out;            /* [R][Hq][D]; not q */
+    int64_t q_stride[2], out_stride[2]; /* request, head */
+    float *lse;           /* [R][Hq], tight, natural logarithm; or NULL */
+    float scale;          /* of the scores; 0 = 1 / sqrt(D) */
+    int32_t reserved;     /* 0 */
+    const int32_t *tables; /* [R][table_width] block ids of each request's own tokens */
+    int64_t table_width, table_stride; /* entries per request, bytes from request to request */
+    const int32_t *lens;   /* [R] own tokens */
+    int64_t max_len;       /* no lens[r] is larger */
+    const int32_t *prefix_table; /* block ids of the prefix (max_prefix > 0) */
+    const int32_t *prefix_len;   /* one number: tokens of the prefix (max_prefix > 0) */
+    int64_t max_prefix;          /* it is at most this; 0 = no prefix */
+    void *workspace;             /* 16-byte aligned, >= tc_attn_workspace bytes, not shared by calls that */
+    int64_t workspace_bytes;     /*   may run at once; its contents before and after mean nothing */
+} tc_attn_decode_t;
+
+/* Bytes of workspace that the call needs: by R, Hq, max_len, max_prefix and the layer's geometry alone. */
+TC_API int tc_attn_workspace(const tc_kv_layer_t *layer, const tc_attn_decode_t *args, int64_t *bytes);
+TC_API int tc_attn_decode(const tc_kv_layer_t *layer, const tc_attn_decode_t *args, void *stream);
+
 /* ---- off the data path: inspection and diagnostics -------------------------------------- */
 
 typedef struct {
@@ -525,6 +653,8 @@ TC_API int tc_trim(void);
 #define TC_DEVICE_OUT_OF_BOUNDS 2u /* the bounds checker of a TC_PLAN_DEBUG_BOUNDS plan found a descriptor that
                                       reaches outside its table slot; copy kernels of such plans return
                                       without copying while the flag is set (read it to clear it) */
+#define TC_DEVICE_BAD_INDEX 4u /* tc_kv_append, tc_kv_gather or tc_attn_decode met a block id, slot, position or
+                                  length out of its range and left out what it named */
 TC_API int tc_device_status(uint32_t *flags);
 
 /* Run only the device-side bounds checker of a TC_PLAN_DEBUG_BOUNDS plan on `stream`: every

@@ -7,5 +7,7 @@ from .binding import (  # noqa: F401
     TC_MAX_TABLE_SLOTS, TC_NHD, TC_OK, TC_REQUEST_MAJOR, TC_LAYER_MAJOR, TC_PLAN_HOST_ONLY, TC_PLAN_STAGED, TC_PLAN_CHECKSUM, TC_PLAN_SAME_POOL, tc_weights_materialize_checksum, tc_trim, TC_WEIGHTS, EXPORTS, Plan,
     TensorCastError, kv_spec, load_library, pool, tc_kv_pack, tc_kv_unpack, tc_plan_create,
     tc_plan_descriptors, tc_plan_destroy, tc_plan_stats, tc_device_status, tc_selftest_wait_timeout, tc_plan_check_device, TC_PLAN_DEBUG_BOUNDS, TC_DEVICE_OUT_OF_BOUNDS, TC_DEVICE_BULK_WAIT_TIMEOUT, tc_weights_materialize, weights_spec,
+    TC_BF16, TC_FP16, TC_FP32, TC_E4M3, TC_INT8, TC_ROPE_INTERLEAVED, TC_DEVICE_BAD_INDEX, KVLayer, kv_layer, tc_kv_append, tc_kv_gather, tc_attn_decode,
+    tc_attn_workspace_bytes,
 )
 from .build import build_library  # noqa: F401

@@ -32,6 +32,9 @@ TC_PLAN_DEBUG_BOUNDS = 128
 TC_MAX_TABLE_SLOTS = 4000
 TC_DEVICE_BULK_WAIT_TIMEOUT = 1
 TC_DEVICE_OUT_OF_BOUNDS = 2
+TC_DEVICE_BAD_INDEX = 4
+TC_BF16, TC_FP16, TC_FP32, TC_E4M3, TC_INT8 = 1, 2, 3, 4, 5
+TC_ROPE_INTERLEAVED = 1
 
 
 class tc_kv_pool_t(C.Structure):
@@ -102,10 +105,42 @@ class tc_segment_t(C.Structure):
                 ("desc0", C.c_uint32), ("n_descs", C.c_uint32), ("outer0", C.c_uint32), ("n_outer", C.c_uint32)]
 
 
+class tc_kv_layer_t(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("dtype", C.c_int32), ("B", C.c_int64), ("H", C.c_int64), ("D", C.c_int64),
+                ("pool", tc_kv_pool_t), ("scale_pool", tc_kv_pool_t), ("k", C.c_void_p), ("v", C.c_void_p),
+                ("k_scale", C.c_void_p), ("v_scale", C.c_void_p)]
+
+
+_Stride = C.c_int64 * 2
+
+
+class tc_kv_append_t(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("flags", C.c_uint32), ("n_tokens", C.c_int64), ("Hq", C.c_int64),
+                ("dtype", C.c_int32), ("rot_dim", C.c_int32), ("q", C.c_void_p), ("q_out", C.c_void_p), ("k", C.c_void_p), ("v", C.c_void_p),
+                ("q_stride", _Stride), ("q_out_stride", _Stride), ("k_stride", _Stride), ("v_stride", _Stride),
+                ("slots", C.c_void_p), ("positions", C.c_void_p), ("cos", C.c_void_p), ("sin", C.c_void_p),
+                ("n_positions", C.c_int64), ("table_stride", C.c_int64)]
+
+
+class tc_kv_gather_t(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("dtype", C.c_int32), ("R", C.c_int64), ("n_rows", C.c_int64),
+                ("tables", C.c_void_p), ("table_width", C.c_int64), ("table_stride", C.c_int64), ("offsets", C.c_void_p), ("first", C.c_void_p),
+                ("k_out", C.c_void_p), ("v_out", C.c_void_p), ("k_stride", _Stride), ("v_stride", _Stride)]
+
+
+class tc_attn_decode_t(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("dtype", C.c_int32), ("R", C.c_int64), ("Hq", C.c_int64), ("q", C.c_void_p), ("out", C.c_void_p),
+                ("q_stride", _Stride), ("out_stride", _Stride), ("lse", C.c_void_p), ("scale", C.c_float), ("reserved", C.c_int32),
+                ("tables", C.c_void_p), ("table_width", C.c_int64), ("table_stride", C.c_int64), ("lens", C.c_void_p), ("max_len", C.c_int64),
+                ("prefix_table", C.c_void_p), ("prefix_len", C.c_void_p), ("max_prefix", C.c_int64),
+                ("workspace", C.c_void_p), ("workspace_bytes", C.c_int64)]
+
+
 EXPORTS = ("tc_plan_create", "tc_kv_pack", "tc_kv_unpack", "tc_weights_materialize",
            "tc_plan_destroy", "tc_plan_stats", "tc_plan_descriptors", "tc_strerror", "tc_last_error",
            "tc_kv_pack_noalloc", "tc_weights_materialize_checksum", "tc_trim",
-           "tc_weights_materialize_file", "tc_plan_segments", "tc_device_status", "tc_selftest_wait_timeout", "tc_plan_check_device")
+           "tc_weights_materialize_file", "tc_plan_segments", "tc_device_status", "tc_selftest_wait_timeout", "tc_plan_check_device",
+           "tc_kv_append", "tc_kv_gather", "tc_attn_decode", "tc_attn_workspace")
 
 _lib = None
 
@@ -141,6 +176,11 @@ def load_library(path: str | None = None):
     lib.tc_plan_check_device.restype = C.c_int
     lib.tc_selftest_wait_timeout.argtypes = [vp]
     lib.tc_selftest_wait_timeout.restype = C.c_int
+    for name, args in (("tc_kv_append", tc_kv_append_t), ("tc_kv_gather", tc_kv_gather_t), ("tc_attn_decode", tc_attn_decode_t)):
+        getattr(lib, name).argtypes = [C.POINTER(tc_kv_layer_t), C.POINTER(args), vp]
+        getattr(lib, name).restype = C.c_int
+    lib.tc_attn_workspace.argtypes = [C.POINTER(tc_kv_layer_t), C.POINTER(tc_attn_decode_t), C.POINTER(C.c_int64)]
+    lib.tc_attn_workspace.restype = C.c_int
     lib.tc_trim.argtypes = []
     lib.tc_trim.restype = C.c_int
     lib.tc_strerror.argtypes = [C.c_int]
@@ -406,3 +446,153 @@ def tc_plan_descriptors(plan: Plan, group: int = 0):
     arr = (tc_descriptor_t * max(n.value, 1))()
     _check(lib.tc_plan_descriptors(plan.handle, group, arr, n.value, C.byref(n)))
     return [arr[i] for i in range(n.value)]
+
+
+# ---- operators on one layer of a paged pool ------------------------------------------------
+class KVLayer:
+    """One layer of a paged pool as the operators see it.  Keeps the tensors it was made from alive."""
+
+    def __init__(self, struct: tc_kv_layer_t, refs):
+        self.struct, self.refs = struct, refs
+        self.ref = C.byref(struct)
+        self.B, self.H, self.D = int(struct.B), int(struct.H), int(struct.D)
+
+
+def kv_layer(pool: tc_kv_pool_t, shape, dtype, bases, *, layer=0, scale_pool=None, scale_bases=None) -> KVLayer:
+    """Describe layer `layer` of the pool that `bases` (the table the execute calls take) holds.
+    shape = (B, H, D); dtype a TC_* number.  Quantised pools name their scales' pool - the same
+    geometry with D = 1, E = 4 - and its table."""
+    def planes(p, table, what):
+        table = [table] if hasattr(table, "data_ptr") or isinstance(table, int) else list(table)
+        if p.n_slots == 1 and len(table) == 1:
+            return [_addr(table[0]) + (2 * layer + c) * p.plane_stride for c in (0, 1)]
+        if len(table) != p.n_slots or p.n_slots < 2 * layer + 2:
+            raise ValueError(f"{what} table has {len(table)} entries; its pool says {p.n_slots}, layer {layer} needs {2 * layer + 2} (or one)")
+        return [_addr(table[2 * layer + c]) for c in (0, 1)]
+
+    B, H, D = shape
+    k, v = planes(pool, bases, "pool")
+    ks, vs = planes(scale_pool, scale_bases, "scale pool") if scale_pool is not None else (None, None)
+    struct = tc_kv_layer_t(C.sizeof(tc_kv_layer_t), dtype, B, H, D, pool, scale_pool or tc_kv_pool_t(), k, v, ks, vs)
+    return KVLayer(struct, (bases, scale_bases))
+
+
+_dtypes = {}
+
+
+def _dtype(t) -> int:
+    """TC_* number of a torch tensor's element type."""
+    if not _dtypes:
+        import torch
+        _dtypes.update({torch.bfloat16: TC_BF16, torch.float16: TC_FP16, torch.float32: TC_FP32})
+    try:
+        return _dtypes[t.dtype]
+    except KeyError:
+        raise ValueError(f"tensors of type {t.dtype} are not taken here") from None
+
+
+def _rows(name, t, n, heads, D):
+    """Byte strides of a [n, heads, D] tensor with contiguous rows."""
+    if tuple(t.shape) != (n, heads, D):
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {(n, heads, D)}")
+    s0, s1, s2 = t.stride()
+    if s2 != 1 and D > 1:
+        raise ValueError(f"{name}: the elements of a row must be contiguous (stride {s2})")
+    e = t.element_size()
+    return _Stride(s0 * e, s1 * e)
+
+
+def _vector(name, t, n, size):
+    """Address of a contiguous device vector of n elements of `size` bytes."""
+    if t is None:
+        return None
+    if t.numel() < n or t.element_size() != size or t.is_floating_point() or not t.is_contiguous():
+        raise ValueError(f"{name} must hold {n} contiguous integers of {8 * size} bits")
+    return t.data_ptr()
+
+
+def _matrix(name, t, rows):
+    """(address, width, byte stride) of an int32 [rows, width] table."""
+    if t.dim() != 2 or t.shape[0] < rows or t.element_size() != 4 or t.is_floating_point() or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError(f"{name} must be a matrix of {rows} rows of contiguous 32-bit integers")
+    return t.data_ptr(), t.shape[1], t.stride(0) * 4
+
+
+def tc_kv_append(layer: KVLayer, k, v, slots, *, q=None, q_out=None, positions=None, cos=None, sin=None, interleaved=False, stream=None) -> None:
+    """Write tokens' K and V, [n, H, D], into the pool at `slots` (int64, negative = padding), quantised if the
+    pool is.  cos, sin ([positions, rot_dim / 2], fp32): rotate K, and q ([n, Hq, D]) into q_out, by row positions[i]."""
+    n = k.shape[0]
+    a = tc_kv_append_t(C.sizeof(tc_kv_append_t), TC_ROPE_INTERLEAVED if interleaved else 0, n, 0, _dtype(k))
+    a.k, a.k_stride = k.data_ptr(), _rows("k", k, n, layer.H, layer.D)
+    a.v, a.v_stride = v.data_ptr(), _rows("v", v, n, layer.H, layer.D)
+    if v.dtype != k.dtype:
+        raise ValueError("k and v differ in type")
+    if q is not None:
+        if q_out is None or q.dtype != k.dtype or q_out.dtype != k.dtype:
+            raise ValueError("q needs a q_out, and both k's type")
+        a.Hq = q.shape[1]
+        a.q, a.q_stride = q.data_ptr(), _rows("q", q, n, a.Hq, layer.D)
+        a.q_out, a.q_out_stride = q_out.data_ptr(), _rows("q_out", q_out, n, a.Hq, layer.D)
+    a.slots = _vector("slots", slots, n, 8)
+    if cos is not None:
+        if sin is None or cos.shape != sin.shape or cos.dim() != 2 or cos.element_size() != 4 or sin.element_size() != 4 or cos.stride() != sin.stride() or (cos.shape[1] > 1 and cos.stride(1) != 1):
+            raise ValueError("cos and sin must be fp32 matrices of the same shape and strides, with contiguous rows")
+        a.rot_dim = 2 * cos.shape[1]
+        if a.rot_dim:
+            a.positions = _vector("positions", positions, n, 8)
+            a.cos, a.sin, a.n_positions, a.table_stride = cos.data_ptr(), sin.data_ptr(), cos.shape[0], cos.stride(0) * 4
+    _check(load_library().tc_kv_append(layer.ref, C.byref(a), _stream(stream)))
+
+
+def tc_kv_gather(layer: KVLayer, tables, offsets, k_out=None, v_out=None, *, first=None, stream=None) -> None:
+    """Rows offsets[r] .. offsets[r + 1] of k_out and v_out ([rows, H, D]) <- the tokens of request r from first[r]
+    (default 0) on, by tables (int32, [R, width]).  offsets: int64 [R + 1]."""
+    R = offsets.shape[0] - 1
+    a = tc_kv_gather_t(C.sizeof(tc_kv_gather_t))
+    for name, t in (("k", k_out), ("v", v_out)):
+        if t is None:
+            continue
+        if a.dtype and (a.dtype != _dtype(t) or a.n_rows != t.shape[0]):
+            raise ValueError("k_out and v_out differ in type or rows")
+        a.dtype, a.n_rows = _dtype(t), t.shape[0]
+        setattr(a, name + "_out", t.data_ptr())
+        setattr(a, name + "_stride", _rows(name + "_out", t, a.n_rows, layer.H, layer.D))
+    a.R = R
+    a.tables, a.table_width, a.table_stride = _matrix("tables", tables, R)
+    a.offsets, a.first = _vector("offsets", offsets, R + 1, 8), _vector("first", first, R, 8)
+    _check(load_library().tc_kv_gather(layer.ref, C.byref(a), _stream(stream)))
+
+
+def _decode_args(q, max_len, max_prefix):
+    return tc_attn_decode_t(C.sizeof(tc_attn_decode_t), _dtype(q), q.shape[0], q.shape[1], max_len=max_len, max_prefix=max_prefix)
+
+
+def tc_attn_workspace_bytes(layer: KVLayer, q, *, max_len, max_prefix=0) -> int:
+    """Bytes of workspace that tc_attn_decode needs for queries of this shape and these bounds."""
+    out = C.c_int64()
+    _check(load_library().tc_attn_workspace(layer.ref, C.byref(_decode_args(q, max_len, max_prefix)), C.byref(out)))
+    return out.value
+
+
+def tc_attn_decode(layer: KVLayer, q, out, tables, lens, *, max_len, workspace, prefix_table=None, prefix_len=None, max_prefix=0, scale=0.0, lse=None, stream=None) -> None:
+    """out[r, h] <- attention of q[r, h] ([R, Hq, D]) over the prefix (prefix_len tokens of prefix_table, read once for
+    all requests) and the lens[r] tokens (int32; negative = padding) of tables[r].  lse: fp32 [R, Hq] or None."""
+    R, Hq = q.shape[0], q.shape[1]
+    a = _decode_args(q, max_len, max_prefix)
+    a.q, a.q_stride = q.data_ptr(), _rows("q", q, R, Hq, layer.D)
+    if out.dtype != q.dtype:
+        raise ValueError("out must have q's type")
+    a.out, a.out_stride = out.data_ptr(), _rows("out", out, R, Hq, layer.D)
+    a.scale = scale
+    if lse is not None:
+        if tuple(lse.shape) != (R, Hq) or lse.element_size() != 4 or not lse.is_contiguous():
+            raise ValueError("lse must be a contiguous fp32 [R, Hq]")
+        a.lse = lse.data_ptr()
+    if max_len:
+        a.tables, a.table_width, a.table_stride = _matrix("tables", tables, R)
+    a.lens = _vector("lens", lens, R, 4)
+    if max_prefix:
+        a.prefix_table = _vector("prefix_table", prefix_table, -(-max_prefix // layer.B), 4)
+        a.prefix_len = _vector("prefix_len", prefix_len, 1, 4)
+    a.workspace, a.workspace_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    _check(load_library().tc_attn_decode(layer.ref, C.byref(a), _stream(stream)))

@@ -4,15 +4,17 @@ from __future__ import annotations
 import os
 import subprocess
 import sys
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libtensorcast_b200.so")
-SOURCES = ["exec.cu", "launch.cu", "staging.cu", "noalloc.cu", "plan_build.cpp"]
+SOURCES = ["exec.cu", "launch.cu", "staging.cu", "noalloc.cu", "plan_build.cpp", "ops_check.cpp", "kv_append.cu", "kv_gather.cu", "attn_decode.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-              "-Xcompiler", "-fPIC,-Wall,-Wextra,-fvisibility=hidden", "-shared", "-cudart", "static"]
+              "-Xcompiler", "-fPIC,-Wall,-Wextra,-fvisibility=hidden"]
 
 
 def _inputs():
@@ -34,11 +36,18 @@ def build_library(force: bool = False, verbose: bool = False) -> str:
         return LIB
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
     tmp = LIB + f".{os.getpid()}.tmp"
-    cmd = [nvcc, *NVCC_FLAGS, "-I", INCLUDE, "-I", CSRC, "-o", tmp] + [os.path.join(CSRC, s) for s in SOURCES]
-    if verbose:
-        cmd.insert(1, "-Xptxas=-v")
-        print(" ".join(cmd), file=sys.stderr)
-    subprocess.check_call(cmd)
+
+    def run(cmd):
+        if verbose:
+            print(" ".join(cmd), file=sys.stderr)
+        subprocess.check_call(cmd)
+
+    with tempfile.TemporaryDirectory() as objects:
+        made = [os.path.join(objects, s + ".o") for s in SOURCES]
+        compile_ = [nvcc, *(["-Xptxas=-v"] if verbose else []), *NVCC_FLAGS, "-I", INCLUDE, "-I", CSRC, "-c"]
+        with ThreadPoolExecutor(os.cpu_count() or 1) as workers:
+            list(workers.map(lambda s, o: run([*compile_, "-o", o, os.path.join(CSRC, s)]), SOURCES, made))
+        run([nvcc, *NVCC_FLAGS, "-shared", "-cudart", "static", "-o", tmp, *made])
     os.replace(tmp, LIB)
     return LIB
 

@@ -1,0 +1,44 @@
+// How tc_attn_decode cuts its work: shared by the entry points and the kernels' launchers.
+#pragma once
+
+#include "ops.h"
+
+namespace tc {
+
+// The keys of a row of queries are cut into parts; every part leaves a normalised output and the base-2
+// logarithm of its sum in the workspace, and a last kernel joins them.
+struct AttnSplit {
+    int32_t group;             // query heads per KV head
+    int32_t prefix_rows;       // rows of queries one prefix CTA takes
+    int32_t prefix_blocks;     // such blocks of the R * group rows of one KV head
+    int32_t own_blocks;        // blocks of 16 of a request's group rows
+    int64_t prefix_chunk, own_chunk;  // keys per part
+    int32_t prefix_parts, own_parts;
+    int64_t rows;              // R * Hq
+    int64_t sum_bytes;         // workspace: [parts][rows] logarithms, then [parts][rows][D] outputs
+    int64_t workspace;
+};
+
+struct AttnParams {
+    Layer layer;
+    const char *q;
+    int64_t q_req, q_head;
+    char *out;
+    int64_t out_req, out_head;
+    float *lse;
+    const char *tables;
+    int64_t table_width, table_stride;
+    const int32_t *lens, *prefix_table, *prefix_len;
+    int64_t R, max_len, max_prefix;
+    int32_t Hq;
+    float scale_log2;  // scale * log2(e)
+    FastDiv div_block, div_group;
+    AttnSplit split;
+    float *sums, *parts;
+    unsigned int *status;
+};
+
+// attn_decode.cu
+void split_attn(int64_t R, int64_t Hq, int64_t H, int64_t D, int64_t max_len, int64_t max_prefix, AttnSplit *out);
+
+}  // namespace tc

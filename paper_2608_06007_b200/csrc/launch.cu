@@ -7,6 +7,7 @@
 
 #include "copy_kernel.cuh"
 #include "exec.h"
+#include "ops.h"
 
 namespace tc {
 
@@ -203,6 +204,35 @@ int read_device_status(unsigned int *out)
     if (e == cudaSuccess) e = cudaMemcpyFromSymbol(out, g_device_status, sizeof *out);
     if (e == cudaSuccess && *out) e = cudaMemcpyToSymbol(g_device_status, &zero, sizeof zero);
     return e == cudaSuccess ? TC_OK : cuda_fail(e, "reading the device status word");
+}
+
+int op_device(int *device, unsigned int **status, int *sm_count)
+{
+    struct Known {
+        unsigned int *status;
+        int sms;
+    };
+    static Known known[kMaxDevices];
+    static pthread_mutex_t mu = PTHREAD_MUTEX_INITIALIZER;
+    cudaError_t e = cudaGetDevice(device);
+    if (e != cudaSuccess) return cuda_fail(e, "querying the current device");
+    if (*device < 0 || *device >= kMaxDevices) return fail(TC_ERR_INVALID_ARG, "device ordinal %d is not supported", *device);
+    pthread_mutex_lock(&mu);
+    Known &k = known[*device];
+    if (!k.status) {
+        // the lookup may load the library's module, which a capturing thread would not be allowed to
+        cudaStreamCaptureMode mode = cudaStreamCaptureModeRelaxed;
+        cudaThreadExchangeStreamCaptureMode(&mode);
+        void *p = nullptr;
+        e = cudaGetSymbolAddress(&p, g_device_status);
+        if (e == cudaSuccess) e = cudaDeviceGetAttribute(&k.sms, cudaDevAttrMultiProcessorCount, *device);
+        if (e == cudaSuccess) k.status = static_cast<unsigned int *>(p);
+        cudaThreadExchangeStreamCaptureMode(&mode);
+    }
+    *status = k.status;
+    *sm_count = k.sms;
+    pthread_mutex_unlock(&mu);
+    return e == cudaSuccess ? TC_OK : cuda_fail(e, "resolving the device status word");
 }
 
 int launch_bounds_check(const Group &g, int64_t shrink, cudaStream_t s)

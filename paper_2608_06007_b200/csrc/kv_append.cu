@@ -28,16 +28,23 @@ struct AppendParams {
     int32_t log2_lanes;        // lanes of a row (vector kernel)
     int32_t threads_per_token; // a power of two, 32..256
     unsigned int *status;
+    float minus_zero;
 };
 
 struct RowPlace {
-    const char *src;
     char *dst;
     float *scale;
     bool turn, pool;
 };
 
 // Row `row` of a token: H rows of K, H of V, Hq of Q.
+__device__ __forceinline__ const char *row_source(const AppendParams &p, int row, int64_t token)
+{
+    const int H = p.layer.H;
+    if (row < H) return p.k + token * p.k_tok + row * p.k_head;
+    if (row < 2 * H) return p.v + token * p.v_tok + (row - H) * p.v_head;
+    return p.q + token * p.q_tok + (row - 2 * H) * p.q_head;
+}
 __device__ __forceinline__ RowPlace row_place(const AppendParams &p, int row, int64_t token, int64_t block, int32_t n)
 {
     RowPlace r;
@@ -45,14 +52,12 @@ __device__ __forceinline__ RowPlace row_place(const AppendParams &p, int row, in
     if (row < 2 * H) {
         const bool is_v = row >= H;
         const int h = is_v ? row - H : row;
-        r.src = is_v ? p.v + token * p.v_tok + h * p.v_head : p.k + token * p.k_tok + h * p.k_head;
         r.dst = (is_v ? p.layer.v : p.layer.k) + p.layer.geo.at(block, n, h);
         r.scale = p.layer.k_scale ? reinterpret_cast<float *>(reinterpret_cast<char *>(is_v ? p.layer.v_scale : p.layer.k_scale) + p.layer.scale_geo.at(block, n, h)) : nullptr;
         r.turn = !is_v;
         r.pool = true;
     } else {
         const int h = row - 2 * H;
-        r.src = p.q + token * p.q_tok + h * p.q_head;
         r.dst = p.q_out + token * p.o_tok + h * p.o_head;
         r.scale = nullptr;
         r.turn = true;
@@ -61,13 +66,11 @@ __device__ __forceinline__ RowPlace row_place(const AppendParams &p, int row, in
     return r;
 }
 
-// The token's slot and position; false: nothing of it is written.
-__device__ __forceinline__ bool token_target(const AppendParams &p, int64_t token, int64_t *block, int32_t *n, int64_t *pos)
+// Where the token goes; false: nothing of it is written.
+__device__ __forceinline__ bool token_target(const AppendParams &p, int64_t slot, int64_t pos, int64_t *block, int32_t *n)
 {
-    const int64_t slot = p.slots[token];
-    *pos = p.rot ? p.positions[token] : 0;
     if (slot < 0) return false;
-    if (!slot_place(slot, p.layer.B, p.layer.num_blocks, block, n) || (p.rot && (*pos < 0 || *pos >= p.n_positions))) {
+    if (!slot_place(slot, p.layer.B, p.layer.num_blocks, block, n) || (p.rot && (pos < 0 || pos >= p.n_positions))) {
         atomicOr(p.status, kStatusBadIndex);
         return false;
     }
@@ -91,89 +94,216 @@ __device__ __forceinline__ float row_scale(uint32_t most, int dtype)
     return s < 1.17549435e-38f ? 0.f : s;
 }
 
-template <typename T>
-__device__ __forceinline__ void store_chunk(const AppendParams &p, const RowPlace &r, int at, const float *x, float scale)
+// Two fp32 operations at once, each rounded by itself.  The assembler contracts a packed product and a
+// packed sum into one FMA (measured: a fifth of the rotated numbers differed), so products that a sum
+// follows are FMAs already: x * y + (-0), the same number, with a -0 that is known at run time only.
+__device__ __forceinline__ float2 add2(float2 a, float2 b)
 {
-    if (!r.pool) return store_floats<T, 8>(r.dst + at * static_cast<int>(sizeof(T)), x);
-    switch (p.layer.dtype) {
-    case TC_BF16: return store_floats<__nv_bfloat16, 8>(r.dst + at * 2, x);
-    case TC_FP16: return store_floats<__half, 8>(r.dst + at * 2, x);
-    case TC_FP32: return store_floats<float, 8>(r.dst + at * 4, x);
-    default: break;
-    }
-    uint32_t w[4];
-    const bool some = scale > 0.f;
+    float2 r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(reinterpret_cast<uint64_t &>(r)) : "l"(reinterpret_cast<uint64_t &>(a)), "l"(reinterpret_cast<uint64_t &>(b)));
+    return r;
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c)
+{
+    float2 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;"
+        : "=l"(reinterpret_cast<uint64_t &>(r)) : "l"(reinterpret_cast<uint64_t &>(a)), "l"(reinterpret_cast<uint64_t &>(b)), "l"(reinterpret_cast<uint64_t &>(c)));
+    return r;
+}
+
+// x / scale for two numbers, correctly rounded, by Markstein's method: with y the rounded reciprocal, one
+// step q + (x - q scale) y brings q within an ulp, a second one rounds it correctly, as long as the
+// remainders are exact.  They are where scale >= 2^-80: a quotient below 2^-11 becomes code 0 however
+// it is rounded, and above that the remainder's last bit is above 2^-149.
+__device__ __forceinline__ float2 divide2(float2 x, float minus_scale, float y)
+{
+    const float2 ms = make_float2(minus_scale, minus_scale), y2 = make_float2(y, y);
+    float2 q = fma2(x, y2, make_float2(-0.f, -0.f));
+    q = fma2(fma2(q, ms, x), y2, q);
+    return fma2(fma2(q, ms, x), y2, q);
+}
+constexpr float kDividable = 8.27180613e-25f;  // 2^-80
+
+// The larger magnitude; a NaN wins.
+__device__ __forceinline__ float larger(float a, float b)
+{
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
+
+// A thread's 16 elements of a row: two chunks of 8, held as pairs of rotation partners - lo[i] and hi[i] hold
+// elements 2i, 2i + 1 of chunks a and b (half layout), or the even and the odd ones of four neighbours.
+struct Pairs {
+    float2 lo[4], hi[4];
+};
+// Chunks of 8 elements of T as they are loaded.
+template <typename T> struct Chunk { uint4 v[sizeof(T) / 2]; };
+
+template <typename T>
+__device__ __forceinline__ void load_chunk(const char *p, Chunk<T> &c)
+{
+    c.v[0] = *reinterpret_cast<const uint4 *>(p);
+    if constexpr (sizeof(T) == 4) c.v[1] = *reinterpret_cast<const uint4 *>(p + 16);
+}
+template <typename T, bool INTERLEAVED>
+__device__ __forceinline__ void widen_chunks(const Chunk<T> (&c)[2], Pairs &x)
+{
+    const uint32_t *w[2] = {reinterpret_cast<const uint32_t *>(&c[0]), reinterpret_cast<const uint32_t *>(&c[1])};
+#pragma unroll
+    for (int half = 0; half < 2; half++)
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            float2 f;  // elements 2i, 2i + 1 of the chunk
+            if constexpr (sizeof(T) == 4) f = make_float2(__uint_as_float(w[half][2 * i]), __uint_as_float(w[half][2 * i + 1]));
+            else f = unpack2<T>(w[half][i]);
+            if constexpr (INTERLEAVED) {
+                const int j = 2 * half + i / 2;
+                if (i % 2 == 0) x.lo[j].x = f.x, x.hi[j].x = f.y;
+                else x.lo[j].y = f.x, x.hi[j].y = f.y;
+            } else {
+                (half ? x.hi : x.lo)[i] = f;
+            }
+        }
+}
+// Elements 2i, 2i + 1 of chunk `half`.
+template <bool INTERLEAVED>
+__device__ __forceinline__ float2 element2(const Pairs &x, int half, int i)
+{
+    if constexpr (!INTERLEAVED) return half ? x.hi[i] : x.lo[i];
+    const int j = 2 * half + i / 2;
+    return i % 2 == 0 ? make_float2(x.lo[j].x, x.hi[j].x) : make_float2(x.lo[j].y, x.hi[j].y);
+}
+template <typename T, bool INTERLEAVED>
+__device__ __forceinline__ void store_chunk(char *p, const Pairs &x, int half)
+{
+    float f[8];
 #pragma unroll
     for (int i = 0; i < 4; i++) {
-        const float a = some ? __fdiv_rn(x[2 * i], scale) : 0.f, b = some ? __fdiv_rn(x[2 * i + 1], scale) : 0.f;
-        w[i] = p.layer.dtype == TC_E4M3 ? e4m3_pair(a, b) : int8_pair(a, b);
+        const float2 e = element2<INTERLEAVED>(x, half, i);
+        f[2 * i] = e.x, f[2 * i + 1] = e.y;
     }
-    *reinterpret_cast<uint2 *>(r.dst + at) = make_uint2(w[0] | (w[1] << 16), w[2] | (w[3] << 16));
+    store_floats<T, 8>(p, f);
 }
 
 // Rows whose D is a multiple of 8 and whose addresses are multiples of 16 bytes; rot_dim a multiple of 16.
-template <typename T>
-__global__ void __launch_bounds__(256) append_vector_kernel(const __grid_constant__ AppendParams p)
+template <typename T, bool INTERLEAVED, bool QUANTISED>
+__global__ void __launch_bounds__(256, sizeof(T) == 4 ? 2 : 3) append_vector_kernel(const __grid_constant__ AppendParams p)
 {
-    constexpr int kRows = 2;  // rows in flight per thread: loads of both before the work on either
+    constexpr int kRows = 3;  // rows in flight
     const int tpt = p.threads_per_token, lt = threadIdx.x & (tpt - 1);
-    const int64_t token = static_cast<int64_t>(blockIdx.x) * (256 / tpt) + threadIdx.x / tpt;
+    const int64_t token = static_cast<int64_t>(blockIdx.x) * (blockDim.x / tpt) + threadIdx.x / tpt;
     if (token >= p.n_tokens) return;
-    int64_t block, pos;
-    int32_t n;
-    if (!token_target(p, token, &block, &n, &pos)) return;  // one token's threads are whole warps
+    const int64_t slot = p.slots[token], pos = p.rot ? p.positions[token] : 0;
 
-    const int lanes = 1 << p.log2_lanes, pair = lt & (lanes - 1), D = p.layer.D;
+    const int lanes = 1 << p.log2_lanes, pair = lt & (lanes - 1), D = p.layer.D, H = p.layer.H;
     const int turned = p.rot >> 4;  // pairs that are rotated
     int a, b;
-    if (pair < turned && !p.interleaved) a = 8 * pair, b = a + p.rot / 2;
+    if (!INTERLEAVED && pair < turned) a = 8 * pair, b = a + p.rot / 2;
     else a = 16 * pair, b = a + 8;
     const bool has_a = a < D, has_b = b < D;
-    float c[8], s[8];
-    if (pair < turned) {
-        load_floats<float, 8>(p.cos + pos * p.table_stride + 32 * pair, c);
-        load_floats<float, 8>(p.sin + pos * p.table_stride + 32 * pair, s);
-    }
-    const int rows = 2 * p.layer.H + p.Hq, step = tpt >> p.log2_lanes;
-    for (int row0 = lt >> p.log2_lanes; row0 - (lt >> p.log2_lanes) < rows; row0 += kRows * step) {
-        float x[kRows][16];
-        RowPlace place[kRows];
+    const int rows = 2 * H + p.Hq, step = tpt >> p.log2_lanes, first = lt >> p.log2_lanes;
+    using Rows = Chunk<T>[kRows][2];
+    auto load_rows = [&](int base, Rows &in) {  // waits for neither slot nor position
 #pragma unroll
         for (int u = 0; u < kRows; u++) {
-            const int row = row0 + u * step;
-#pragma unroll
-            for (int i = 0; i < 16; i++) x[u][i] = 0.f;
-            if (row < rows) {
-                place[u] = row_place(p, row, token, block, n);
-                if (has_a) load_floats<T, 8>(place[u].src + a * static_cast<int>(sizeof(T)), x[u]);
-                if (has_b) load_floats<T, 8>(place[u].src + b * static_cast<int>(sizeof(T)), x[u] + 8);
-            }
+            const int row = base + first + u * step;
+            in[u][0] = Chunk<T>{}, in[u][1] = Chunk<T>{};
+            if (row >= rows) continue;
+            const char *src = row_source(p, row, token);
+            if (has_a) load_chunk<T>(src + a * static_cast<int>(sizeof(T)), in[u][0]);
+            if (has_b) load_chunk<T>(src + b * static_cast<int>(sizeof(T)), in[u][1]);
         }
+    };
+    Rows in;
+    load_rows(0, in);
+    int64_t block;
+    int32_t n;
+    if (!token_target(p, slot, pos, &block, &n)) return;  // one token's threads are whole warps
+    float2 c[4], s[4];
+    if (pair < turned) {
+        load_floats<float, 8>(p.cos + pos * p.table_stride + 32 * pair, reinterpret_cast<float *>(c));
+        load_floats<float, 8>(p.sin + pos * p.table_stride + 32 * pair, reinterpret_cast<float *>(s));
+    }
+    const int64_t place = p.layer.geo.at(block, n, 0), scale_place = QUANTISED ? p.layer.scale_geo.at(block, n, 0) : 0;
+    const float2 zero = make_float2(p.minus_zero, p.minus_zero);
+    auto work = [&](int base) {
 #pragma unroll
         for (int u = 0; u < kRows; u++) {
-            const bool here = row0 + u * step < rows;
-            if (here && pair < turned && place[u].turn) {
-                if (p.interleaved) {
+            const int row = base + first + u * step;
+            if (base + (first & ~(32 / lanes - 1)) + u * step >= rows) break;  // nothing for the whole warp
+            Pairs x;
+            widen_chunks<T, INTERLEAVED>(in[u], x);
+            if (pair < turned && (row < H || row >= 2 * H)) {
 #pragma unroll
-                    for (int i = 0; i < 8; i++) turn(x[u][2 * i], x[u][2 * i + 1], c[i], s[i]);
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 8; i++) turn(x[u][i], x[u][8 + i], c[i], s[i]);
+                for (int i = 0; i < 4; i++) {
+                    const float2 xs = fma2(x.lo[i], s[i], zero), ys = fma2(x.hi[i], s[i], zero);
+                    x.lo[i] = add2(fma2(x.lo[i], c[i], zero), make_float2(-ys.x, -ys.y));
+                    x.hi[i] = add2(fma2(x.hi[i], c[i], zero), xs);
                 }
             }
             float scale = 0.f;
-            if (p.layer.k_scale) {
-                uint32_t most = 0;
+            if constexpr (QUANTISED) {
+                // lanes of K or V rows need their partners; a warp of query rows alone skips this
+                if (__any_sync(0xffffffffu, row < 2 * H)) {
+                    float most = 0.f;
 #pragma unroll
-                for (int i = 0; i < 16; i++) most = max(most, __float_as_uint(x[u][i]) & 0x7fffffffu);
-                for (int m = 1; m < lanes; m <<= 1) most = max(most, __shfl_xor_sync(0xffffffffu, most, m));
-                scale = row_scale(most, p.layer.dtype);
+                    for (int i = 0; i < 4; i++)
+                        most = larger(larger(larger(most, fabsf(x.lo[i].x)), fabsf(x.lo[i].y)), larger(fabsf(x.hi[i].x), fabsf(x.hi[i].y)));
+                    for (int m = 1; m < lanes; m <<= 1) most = larger(most, __shfl_xor_sync(0xffffffffu, most, m));
+                    scale = row_scale(__float_as_uint(most), p.layer.dtype);
+                }
             }
-            if (!here) continue;
-            if (place[u].pool && place[u].scale && pair == 0) *place[u].scale = scale;
-            if (has_a) store_chunk<T>(p, place[u], a, x[u], scale);
-            if (has_b) store_chunk<T>(p, place[u], b, x[u] + 8, scale);
+            if (row >= rows) continue;
+            if (row >= 2 * H) {
+                char *dst = p.q_out + token * p.o_tok + (row - 2 * H) * p.o_head;
+                if (has_a) store_chunk<T, INTERLEAVED>(dst + a * static_cast<int>(sizeof(T)), x, 0);
+                if (has_b) store_chunk<T, INTERLEAVED>(dst + b * static_cast<int>(sizeof(T)), x, 1);
+                continue;
+            }
+            const bool is_v = row >= H;
+            const int h = is_v ? row - H : row;
+            char *dst = (is_v ? p.layer.v : p.layer.k) + place + static_cast<int64_t>(h) * p.layer.geo.head;
+            if constexpr (!QUANTISED) {
+                auto put = [&](auto type) {
+                    using P = decltype(type);
+                    if (has_a) store_chunk<P, INTERLEAVED>(dst + a * static_cast<int>(sizeof(P)), x, 0);
+                    if (has_b) store_chunk<P, INTERLEAVED>(dst + b * static_cast<int>(sizeof(P)), x, 1);
+                };
+                if (p.layer.dtype == TC_BF16) put(__nv_bfloat16{});
+                else if (p.layer.dtype == TC_FP16) put(__half{});
+                else put(float{});
+            } else {
+                if (pair == 0) *reinterpret_cast<float *>(reinterpret_cast<char *>(is_v ? p.layer.v_scale : p.layer.k_scale) + scale_place + static_cast<int64_t>(h) * p.layer.scale_geo.head) = scale;
+                if (scale >= kDividable) {
+                    const float y = __fdiv_rn(1.f, scale);
+#pragma unroll
+                    for (int i = 0; i < 4; i++) x.lo[i] = divide2(x.lo[i], -scale, y), x.hi[i] = divide2(x.hi[i], -scale, y);
+                } else {
+                    const bool some = scale > 0.f;  // rows tinier than divide2 takes; and rows whose codes are 0
+#pragma unroll
+                    for (int i = 0; i < 4; i++) {
+                        x.lo[i] = some ? make_float2(__fdiv_rn(x.lo[i].x, scale), __fdiv_rn(x.lo[i].y, scale)) : make_float2(0.f, 0.f);
+                        x.hi[i] = some ? make_float2(__fdiv_rn(x.hi[i].x, scale), __fdiv_rn(x.hi[i].y, scale)) : make_float2(0.f, 0.f);
+                    }
+                }
+#pragma unroll
+                for (int half = 0; half < 2; half++) {
+                    uint32_t w[4];
+#pragma unroll
+                    for (int i = 0; i < 4; i++) {
+                        const float2 e = element2<INTERLEAVED>(x, half, i);
+                        w[i] = p.layer.dtype == TC_E4M3 ? e4m3_pair(e.x, e.y) : int8_pair(e.x, e.y);
+                    }
+                    if (half ? has_b : has_a) *reinterpret_cast<uint2 *>(dst + (half ? b : a)) = make_uint2(w[0] | (w[1] << 16), w[2] | (w[3] << 16));
+                }
+            }
         }
+    };
+    for (int base = 0;;) {
+        work(base);
+        if ((base += kRows * step) >= rows) break;
+        load_rows(base, in);
     }
 }
 
@@ -185,11 +315,13 @@ __global__ void __launch_bounds__(256) append_scalar_kernel(const __grid_constan
     const int64_t item = static_cast<int64_t>(blockIdx.x) * 8 + (threadIdx.x >> 5);
     const int64_t token = item / rows;
     if (token >= p.n_tokens) return;
-    int64_t block, pos;
+    const int row = static_cast<int>(item - token * rows);
+    const int64_t pos = p.rot ? p.positions[token] : 0;
+    int64_t block;
     int32_t n;
-    if (!token_target(p, token, &block, &n, &pos)) return;
-    const RowPlace r = row_place(p, static_cast<int>(item - token * rows), token, block, n);
-    const T *src = reinterpret_cast<const T *>(r.src);
+    if (!token_target(p, p.slots[token], pos, &block, &n)) return;
+    const RowPlace r = row_place(p, row, token, block, n);
+    const T *src = reinterpret_cast<const T *>(row_source(p, row, token));
     float x[16];
     uint32_t most = 0;
 #pragma unroll
@@ -246,13 +378,21 @@ static int launch_append(AppendParams &p, bool vector, cudaStream_t s)
     if (vector) {
         int log2_lanes = 0;
         while ((16 << log2_lanes) < p.layer.D) log2_lanes++;
+        const int64_t wanted = rows << log2_lanes;
         int tpt = 32;
-        while (tpt < 256 && tpt < (rows << log2_lanes)) tpt *= 2;
+        while (tpt < 256 && tpt < wanted) tpt *= 2;
         p.log2_lanes = log2_lanes;
         p.threads_per_token = tpt;
         const int64_t grid = (p.n_tokens + 256 / tpt - 1) / (256 / tpt);
         if (grid > INT32_MAX) return fail(TC_ERR_TOO_LARGE, "n_tokens %lld: too many for one call", (long long)p.n_tokens);
-        append_vector_kernel<T><<<static_cast<unsigned>(grid), 256, 0, s>>>(p);
+        const unsigned g = static_cast<unsigned>(grid);
+        if (p.layer.quantised()) {
+            if (p.interleaved) append_vector_kernel<T, true, true><<<g, 256, 0, s>>>(p);
+            else append_vector_kernel<T, false, true><<<g, 256, 0, s>>>(p);
+        } else {
+            if (p.interleaved) append_vector_kernel<T, true, false><<<g, 256, 0, s>>>(p);
+            else append_vector_kernel<T, false, false><<<g, 256, 0, s>>>(p);
+        }
     } else {
         if (static_cast<__int128>(p.n_tokens) * rows > static_cast<__int128>(INT32_MAX) * 8) return fail(TC_ERR_TOO_LARGE, "n_tokens %lld: too many for one call", (long long)p.n_tokens);
         append_scalar_kernel<T><<<static_cast<unsigned>((p.n_tokens * rows + 7) / 8), 256, 0, s>>>(p);
@@ -322,6 +462,7 @@ extern "C" int tc_kv_append(const tc_kv_layer_t *layer, const tc_kv_append_t *a,
     p.n_tokens = a->n_tokens;
     p.Hq = a->q ? static_cast<int32_t>(a->Hq) : 0;
     p.rot = a->rot_dim;
+    p.minus_zero = -0.f;
     p.interleaved = (a->flags & TC_ROPE_INTERLEAVED) != 0;
     const bool vector = align >= 16 && D % 8 == 0 && a->rot_dim % 16 == 0;
     cudaStream_t s = static_cast<cudaStream_t>(stream);

@@ -1,8 +1,8 @@
 // tc_kv_gather: pages of a paged layer, quantised or not, into contiguous rows.
 //
 // A CTA takes a few consecutive output rows: one thread per row finds its request (bisection of
-// the offsets) and its block, then all threads walk the rows' units of 16 output bytes, in output
-// order, each read as the 4 to 16 bytes of the pool that hold the same elements.  Bound by HBM.
+// the offsets) and its block, then every thread keeps one place (plane, head, unit of 32 output
+// bytes) and steps from token to token, eight loads in flight.  Bound by HBM.
 #include "ops_device.cuh"
 
 #include <algorithm>
@@ -19,8 +19,9 @@ struct GatherParams {
     int64_t R, n_rows;
     char *out[2];
     int64_t row_stride[2], head_stride[2];
-    int32_t rows_per_cta, units;   // units of one (token, head) row
-    FastDiv div_units, div_heads, div_token;  // by units, H, and planes * H * units
+    uint32_t rows_per_cta, units, per_token;  // units of one (token, head) row, and of a token: planes * H * units
+    uint32_t tokens_per_pass;                 // tokens that 256 threads cover at once
+    FastDiv div_units, div_heads, div_token;  // by units, H and per_token
     int32_t planes, plane0;        // outputs asked for: 2, or 1 of which the first is plane0
     unsigned int *status;
 };
@@ -30,41 +31,53 @@ template <> struct PoolType<TC_BF16> { using type = __nv_bfloat16; };
 template <> struct PoolType<TC_FP16> { using type = __half; };
 template <> struct PoolType<TC_FP32> { using type = float; };
 
-// N elements of the pool at p as floats (codes: before their scale).
-template <int POOL, int N>
-__device__ __forceinline__ void load_codes(const char *p, float *x)
+// N elements of the pool as floats (codes: before their scale).
+template <int POOL, int N, int W>
+__device__ __forceinline__ void widen_words(const Words<W> &v, float *x)
 {
-    if constexpr (POOL == TC_E4M3 || POOL == TC_INT8) {
-        uint32_t w[N / 4];
-        if constexpr (N == 8) {
-            const uint2 v = *reinterpret_cast<const uint2 *>(p);
-            w[0] = v.x, w[1] = v.y;
-        } else {
-            w[0] = *reinterpret_cast<const uint32_t *>(p);
-        }
+    if constexpr (POOL == TC_E4M3) {
 #pragma unroll
-        for (int i = 0; i < N / 4; i++) {
-            if constexpr (POOL == TC_E4M3) {
-                const float2 a = unpack2<__half>(e4m3_to_half2(w[i])), b = unpack2<__half>(e4m3_to_half2(w[i] >> 16));
-                x[4 * i] = a.x, x[4 * i + 1] = a.y, x[4 * i + 2] = b.x, x[4 * i + 3] = b.y;
-            } else {
-#pragma unroll
-                for (int j = 0; j < 4; j++) x[4 * i + j] = static_cast<float>(static_cast<int8_t>(w[i] >> (8 * j)));
-            }
+        for (int i = 0; i < W; i++) {
+            const float2 a = unpack2<__half>(e4m3_to_half2(v.w[i])), b = unpack2<__half>(e4m3_to_half2(v.w[i] >> 16));
+            x[4 * i] = a.x, x[4 * i + 1] = a.y, x[4 * i + 2] = b.x, x[4 * i + 3] = b.y;
         }
+    } else if constexpr (POOL == TC_INT8) {
+#pragma unroll
+        for (int i = 0; i < N; i++) x[i] = static_cast<float>(static_cast<int8_t>(v.w[i / 4] >> (8 * (i % 4))));
+    } else if constexpr (POOL == TC_FP32) {
+#pragma unroll
+        for (int i = 0; i < N; i++) x[i] = __uint_as_float(v.w[i]);
     } else {
-        load_floats<typename PoolType<POOL>::type, N>(p, x);
+#pragma unroll
+        for (int i = 0; i < W; i++) {
+            const float2 f = unpack2<typename PoolType<POOL>::type>(v.w[i]);
+            x[2 * i] = f.x, x[2 * i + 1] = f.y;
+        }
     }
 }
+template <typename T, int N>
+__device__ __forceinline__ Words<N * static_cast<int>(sizeof(T)) / 4> narrow_words(const float *x)
+{
+    Words<N * static_cast<int>(sizeof(T)) / 4> r;
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int i = 0; i < N; i++) r.w[i] = __float_as_uint(x[i]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < N / 2; i++) r.w[i] = pack2<T>(x[2 * i], x[2 * i + 1]);
+    }
+    return r;
+}
 
-// VEC: units of 16 output bytes.  Otherwise a unit is one element, at any alignment of the element.
-template <int POOL, typename T, bool VEC>
+// A unit is UNIT output bytes: 32 or 16, or (0) one element at any alignment of the element.
+template <int POOL, typename T, int UNIT>
 __global__ void __launch_bounds__(256) gather_kernel(const __grid_constant__ GatherParams p)
 {
-    constexpr int N = VEC ? 16 / static_cast<int>(sizeof(T)) : 1;
-    constexpr int kUnroll = 4;
     constexpr bool quantised = POOL == TC_E4M3 || POOL == TC_INT8;
     constexpr int esize = POOL == TC_FP32 ? 4 : quantised ? 1 : 2;
+    constexpr int N = UNIT ? UNIT / static_cast<int>(sizeof(T)) : 1;
+    constexpr int W = UNIT ? N * esize / 4 : 1;
+    constexpr int kUnroll = W <= 4 ? 8 : 4;  // 128 bytes in flight per thread
     __shared__ int64_t place[kGatherRows], scale_place[kGatherRows];
     const int64_t row0 = static_cast<int64_t>(blockIdx.x) * p.rows_per_cta;
     if (threadIdx.x < p.rows_per_cta) {
@@ -92,76 +105,83 @@ __global__ void __launch_bounds__(256) gather_kernel(const __grid_constant__ Gat
         scale_place[threadIdx.x] = scale_at;
     }
     __syncthreads();
-    const uint32_t per_token = p.planes * p.layer.H * p.units, total = p.rows_per_cta * per_token;
-    for (uint32_t i0 = threadIdx.x; i0 < total; i0 += 256 * kUnroll) {
-        float x[kUnroll][N];
-        float scale[kUnroll];
-        char *dst[kUnroll];
+    // A thread keeps its place inside a token (plane, head, unit) and steps from token to token.
+    const uint32_t ty = p.tokens_per_pass > 1 ? quick_div(threadIdx.x, p.div_token) : 0;
+    if (ty >= p.tokens_per_pass) return;
+    for (uint32_t x = threadIdx.x - ty * p.per_token; x < p.per_token; x += 256) {
+        const uint32_t row = quick_div(x, p.div_units), unit = x - row * p.units;
+        const uint32_t plane = quick_div(row, p.div_heads), h = row - plane * p.layer.H;
+        const int c = p.plane0 + plane;
+        const char *src = (c ? p.layer.v : p.layer.k) + static_cast<int64_t>(h) * p.layer.geo.head + unit * N * esize;
+        const char *scales = reinterpret_cast<const char *>(c ? p.layer.v_scale : p.layer.k_scale) + static_cast<int64_t>(h) * p.layer.scale_geo.head;
+        const int64_t stride = c ? p.row_stride[1] : p.row_stride[0];
+        char *dst = (c ? p.out[1] : p.out[0]) + row0 * stride + h * (c ? p.head_stride[1] : p.head_stride[0]) + unit * N * static_cast<int>(sizeof(T));
+        for (uint32_t t0 = ty; t0 < p.rows_per_cta; t0 += p.tokens_per_pass * kUnroll) {
+            Words<W> v[kUnroll];
+            float scale[kUnroll];
+            bool there[kUnroll];
 #pragma unroll
-        for (int u = 0; u < kUnroll; u++) {
-            const uint32_t i = i0 + 256 * u;
-            dst[u] = nullptr;
-            if (i >= total) continue;
-            const uint32_t token = quick_div(i, p.div_token), rest = i - token * per_token;
-            const uint32_t row = quick_div(rest, p.div_units), unit = rest - row * p.units;
-            const uint32_t plane = quick_div(row, p.div_heads), h = row - plane * p.layer.H;
-            const int64_t at = place[token];
-            if (at < 0) continue;
-            const int c = p.plane0 + plane;
-            const char *src = (c ? p.layer.v : p.layer.k) + at + static_cast<int64_t>(h) * p.layer.geo.head + unit * N * esize;
-            if constexpr (VEC) {
-                load_codes<POOL, N>(src, x[u]);
-            } else if constexpr (POOL == TC_E4M3) {
-                x[u][0] = unpack2<__half>(e4m3_to_half2(*reinterpret_cast<const uint8_t *>(src))).x;
-            } else if constexpr (POOL == TC_INT8) {
-                x[u][0] = static_cast<float>(*reinterpret_cast<const int8_t *>(src));
-            } else {
-                x[u][0] = to_float(*reinterpret_cast<const typename PoolType<POOL>::type *>(src));
+            for (int u = 0; u < kUnroll; u++) {
+                const uint32_t t = t0 + u * p.tokens_per_pass;
+                const int64_t at = t < p.rows_per_cta ? place[t] : -1;
+                there[u] = at >= 0;
+                scale[u] = 1.f;
+                if (!there[u]) continue;
+                if constexpr (UNIT != 0) v[u] = load_words<W>(src + at);
+                else if constexpr (esize == 1) v[u].w[0] = *reinterpret_cast<const uint8_t *>(src + at);
+                else if constexpr (esize == 2) v[u].w[0] = *reinterpret_cast<const uint16_t *>(src + at);
+                else v[u].w[0] = *reinterpret_cast<const uint32_t *>(src + at);
+                if constexpr (quantised) scale[u] = *reinterpret_cast<const float *>(scales + scale_place[t]);
             }
-            if constexpr (quantised)
-                scale[u] = *reinterpret_cast<const float *>(reinterpret_cast<const char *>(c ? p.layer.v_scale : p.layer.k_scale) + scale_place[token] + static_cast<int64_t>(h) * p.layer.scale_geo.head);
-            dst[u] = (c ? p.out[1] : p.out[0]) + (row0 + token) * (c ? p.row_stride[1] : p.row_stride[0]) + h * (c ? p.head_stride[1] : p.head_stride[0]) + unit * N * static_cast<int>(sizeof(T));
-        }
 #pragma unroll
-        for (int u = 0; u < kUnroll; u++) {
-            if (!dst[u]) continue;
-            if constexpr (quantised)
+            for (int u = 0; u < kUnroll; u++) {
+                if (!there[u]) continue;
+                float f[4 * W > N ? 4 * W : N];
+                widen_words<POOL, N, W>(v[u], f);
+                if constexpr (quantised)
 #pragma unroll
-                for (int j = 0; j < N; j++) x[u][j] = __fmul_rn(x[u][j], scale[u]);
-            if constexpr (VEC) store_floats<T, N>(dst[u], x[u]);
-            else *reinterpret_cast<T *>(dst[u]) = from_float<T>(x[u][0]);
+                    for (int j = 0; j < N; j++) f[j] = __fmul_rn(f[j], scale[u]);
+                char *to = dst + (t0 + u * p.tokens_per_pass) * stride;
+                if constexpr (UNIT != 0) store_words(to, narrow_words<T, N>(f));
+                else *reinterpret_cast<T *>(to) = from_float<T>(f[0]);
+            }
         }
     }
 }
 
 template <int POOL, typename T>
-static int launch_gather(GatherParams &p, bool vector, int sms, cudaStream_t s)
+static int launch_gather(GatherParams &p, int unit, int sms, cudaStream_t s)
 {
-    p.units = vector ? p.layer.D * static_cast<int>(sizeof(T)) / 16 : p.layer.D;
+    constexpr int widest = POOL == TC_FP32 && sizeof(T) == 2 ? 16 : 32;  // a unit reads at most 32 bytes of the pool
+    unit = std::min(unit, widest);
+    p.units = unit ? p.layer.D * static_cast<uint32_t>(sizeof(T)) / unit : p.layer.D;
     const int64_t per_token = static_cast<int64_t>(p.planes) * p.layer.H * p.units;
-    if (per_token * kGatherRows > INT32_MAX) return fail(TC_ERR_TOO_LARGE, "H * D = %lld * %lld: a token's row is too large", (long long)p.layer.H, (long long)p.layer.D);
-    // eight units a thread, fewer where that would leave SMs without a CTA
-    int64_t rows = std::max<int64_t>(1, std::min<int64_t>(kGatherRows, 2048 / std::max<int64_t>(per_token, 1)));
-    rows = std::max<int64_t>(1, std::min(rows, p.n_rows / (2 * sms)));
-    p.rows_per_cta = static_cast<int32_t>(rows);
-    p.div_units = make_fastdiv(static_cast<uint32_t>(p.units));
+    if (per_token > INT32_MAX / 2) return fail(TC_ERR_TOO_LARGE, "H * D = %lld * %lld: a token's row is too large", (long long)p.layer.H, (long long)p.layer.D);
+    // 32 rows a CTA, fewer where that would leave SMs without two CTAs
+    const int64_t rows = std::max<int64_t>(1, std::min<int64_t>(kGatherRows, p.n_rows / (2 * sms)));
+    p.rows_per_cta = static_cast<uint32_t>(rows);
+    p.per_token = static_cast<uint32_t>(per_token);
+    p.tokens_per_pass = std::max<uint32_t>(1, 256 / p.per_token);
+    p.div_units = make_fastdiv(p.units);
     p.div_heads = make_fastdiv(static_cast<uint32_t>(p.layer.H));
-    p.div_token = make_fastdiv(static_cast<uint32_t>(per_token));
+    p.div_token = make_fastdiv(p.per_token);
     const int64_t grid = (p.n_rows + rows - 1) / rows;
     if (grid > INT32_MAX) return fail(TC_ERR_TOO_LARGE, "n_rows %lld: too many for one call", (long long)p.n_rows);
-    if (vector) gather_kernel<POOL, T, true><<<static_cast<unsigned>(grid), 256, 0, s>>>(p);
-    else gather_kernel<POOL, T, false><<<static_cast<unsigned>(grid), 256, 0, s>>>(p);
+    if constexpr (widest == 32)
+        if (unit == 32) gather_kernel<POOL, T, 32><<<static_cast<unsigned>(grid), 256, 0, s>>>(p);
+    if (unit == 16) gather_kernel<POOL, T, 16><<<static_cast<unsigned>(grid), 256, 0, s>>>(p);
+    if (unit == 0) gather_kernel<POOL, T, 0><<<static_cast<unsigned>(grid), 256, 0, s>>>(p);
     const cudaError_t e = cudaGetLastError();
     return e == cudaSuccess ? TC_OK : cuda_fail(e, "kernel launch");
 }
 
 template <int POOL>
-static int launch_gather_to(GatherParams &p, int dtype, bool vector, int sms, cudaStream_t s)
+static int launch_gather_to(GatherParams &p, int dtype, int unit, int sms, cudaStream_t s)
 {
     switch (dtype) {
-    case TC_BF16: return launch_gather<POOL, __nv_bfloat16>(p, vector, sms, s);
-    case TC_FP16: return launch_gather<POOL, __half>(p, vector, sms, s);
-    default: return launch_gather<POOL, float>(p, vector, sms, s);
+    case TC_BF16: return launch_gather<POOL, __nv_bfloat16>(p, unit, sms, s);
+    case TC_FP16: return launch_gather<POOL, __half>(p, unit, sms, s);
+    default: return launch_gather<POOL, float>(p, unit, sms, s);
     }
 }
 
@@ -181,7 +201,7 @@ extern "C" int tc_kv_gather(const tc_kv_layer_t *layer, const tc_kv_gather_t *a,
     if (a->R < 0 || a->n_rows < 0) return fail(TC_ERR_SHAPE, "R %lld and n_rows %lld must be >= 0", (long long)a->R, (long long)a->n_rows);
     if (a->R == 0 || a->n_rows == 0) return TC_OK;
     const int e = dtype_size(a->dtype), D = p.layer.D;
-    uint32_t align = 16;
+    uint32_t align = 32;
     if (!a->k_out && !a->v_out) return fail(TC_ERR_INVALID_ARG, "k_out or v_out is required");
     if (a->k_out && (rc = check_rows("k_out", a->k_out, a->k_stride, a->n_rows, p.layer.H, int64_t(D) * e, e, true, &align)) != TC_OK) return rc;
     if (a->v_out && (rc = check_rows("v_out", a->v_out, a->v_stride, a->n_rows, p.layer.H, int64_t(D) * e, e, true, &align)) != TC_OK) return rc;
@@ -209,14 +229,16 @@ extern "C" int tc_kv_gather(const tc_kv_layer_t *layer, const tc_kv_gather_t *a,
     }
     p.planes = (a->k_out != nullptr) + (a->v_out != nullptr);
     p.plane0 = a->k_out ? 0 : 1;
-    // a unit's 16 output bytes come from 16 / e elements of the pool
-    const bool vector = align >= 16 && D % (16 / e) == 0 && p.layer.align >= std::min<uint32_t>(16, 16u / e * p.layer.esize);
+    // Units of 32 output bytes where both sides are aligned to what one unit reads and writes in one
+    // access, else of 16, else single elements.
+    auto fits = [&](int unit) { return align >= static_cast<uint32_t>(unit) && D * e % unit == 0 && p.layer.align >= static_cast<uint32_t>(std::min(32, unit / e * p.layer.esize)); };
+    const int unit = fits(32) ? 32 : fits(16) ? 16 : 0;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     switch (p.layer.dtype) {
-    case TC_BF16: return launch_gather_to<TC_BF16>(p, a->dtype, vector, sms, s);
-    case TC_FP16: return launch_gather_to<TC_FP16>(p, a->dtype, vector, sms, s);
-    case TC_FP32: return launch_gather_to<TC_FP32>(p, a->dtype, vector, sms, s);
-    case TC_E4M3: return launch_gather_to<TC_E4M3>(p, a->dtype, vector, sms, s);
-    default: return launch_gather_to<TC_INT8>(p, a->dtype, vector, sms, s);
+    case TC_BF16: return launch_gather_to<TC_BF16>(p, a->dtype, unit, sms, s);
+    case TC_FP16: return launch_gather_to<TC_FP16>(p, a->dtype, unit, sms, s);
+    case TC_FP32: return launch_gather_to<TC_FP32>(p, a->dtype, unit, sms, s);
+    case TC_E4M3: return launch_gather_to<TC_E4M3>(p, a->dtype, unit, sms, s);
+    default: return launch_gather_to<TC_INT8>(p, a->dtype, unit, sms, s);
     }
 }

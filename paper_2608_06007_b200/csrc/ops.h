@@ -19,7 +19,7 @@ struct Layer {
     int32_t H, D, dtype, esize;
     char *k, *v;
     float *k_scale, *v_scale;
-    uint32_t align;  // of its planes and strides together, up to 16
+    uint32_t align;  // of its planes and strides together, up to 32
     bool quantised() const { return dtype == TC_E4M3 || dtype == TC_INT8; }
 };
 

@@ -16,7 +16,7 @@ int dtype_size(int dtype)
     }
 }
 
-static uint32_t low_bit(uint64_t v) { return v ? static_cast<uint32_t>(std::min<uint64_t>(v & -v, 16)) : 16u; }
+static uint32_t low_bit(uint64_t v) { return v ? static_cast<uint32_t>(std::min<uint64_t>(v & -v, 32)) : 32u; }
 
 // One plane's strides for rows of `row` bytes; block_stride 0 = tight.
 static int plane_geo(const char *name, const tc_kv_pool_t &p, int64_t B, int64_t H, int64_t row, PlaneGeo *out)

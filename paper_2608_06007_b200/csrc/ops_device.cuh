@@ -56,6 +56,31 @@ __device__ __forceinline__ uint32_t int8_pair(float a, float b)
     return (static_cast<uint32_t>(__float2int_rn(a)) & 0xffu) | ((static_cast<uint32_t>(__float2int_rn(b)) & 0xffu) << 8);
 }
 
+// W words at p, in one access: 16-byte accesses are aligned to 16 bytes, 32-byte ones to 32.
+template <int W> struct Words { uint32_t w[W]; };
+template <int W>
+__device__ __forceinline__ Words<W> load_words(const void *p)
+{
+    Words<W> r;
+    static_assert(W == 1 || W == 2 || W == 4 || W == 8);
+    if constexpr (W == 1) r.w[0] = *static_cast<const uint32_t *>(p);
+    if constexpr (W == 2) asm volatile("ld.global.v2.b32 {%0,%1}, [%2];" : "=r"(r.w[0]), "=r"(r.w[1]) : "l"(p));
+    if constexpr (W == 4) asm volatile("ld.global.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(r.w[0]), "=r"(r.w[1]), "=r"(r.w[2]), "=r"(r.w[3]) : "l"(p));
+    if constexpr (W == 8)
+        asm volatile("ld.global.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                     : "=r"(r.w[0]), "=r"(r.w[1]), "=r"(r.w[2]), "=r"(r.w[3]), "=r"(r.w[4]), "=r"(r.w[5]), "=r"(r.w[6]), "=r"(r.w[7]) : "l"(p));
+    return r;
+}
+template <int W>
+__device__ __forceinline__ void store_words(void *p, const Words<W> &r)
+{
+    static_assert(W == 4 || W == 8);
+    if constexpr (W == 4) asm volatile("st.global.v4.b32 [%0], {%1,%2,%3,%4};" ::"l"(p), "r"(r.w[0]), "r"(r.w[1]), "r"(r.w[2]), "r"(r.w[3]) : "memory");
+    if constexpr (W == 8)
+        asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(r.w[0]), "r"(r.w[1]), "r"(r.w[2]), "r"(r.w[3]), "r"(r.w[4]), "r"(r.w[5]), "r"(r.w[6]), "r"(r.w[7])
+                     : "memory");
+}
+
 // N numbers of type T at p (aligned to min(16, N * sizeof(T)) bytes) as floats.
 template <typename T, int N>
 __device__ __forceinline__ void load_floats(const void *p, float *x)

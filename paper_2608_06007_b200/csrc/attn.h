@@ -9,7 +9,8 @@ namespace tc {
 // logarithm of its sum in the workspace, and a last kernel joins them.
 struct AttnSplit {
     int32_t group;             // query heads per KV head
-    int32_t prefix_rows;       // rows of queries one prefix CTA takes
+    int32_t prefix_rows;       // rows of queries one prefix CTA takes: 16 (parts_kernel), 128 or 256 (prefix_kernel;
+                               // 128: two parts per chunk of keys, one a slot)
     int32_t prefix_blocks;     // such blocks of the R * group rows of one KV head
     int32_t own_blocks;        // blocks of 16 of a request's group rows
     int64_t prefix_chunk, own_chunk;  // keys per part
@@ -39,6 +40,9 @@ struct AttnParams {
 };
 
 // attn_decode.cu
-void split_attn(int64_t R, int64_t Hq, int64_t H, int64_t D, int64_t max_len, int64_t max_prefix, AttnSplit *out);
+void split_attn(int64_t R, int64_t Hq, int64_t H, int64_t D, int64_t max_len, int64_t max_prefix, bool quantised, AttnSplit *out);
+
+// attn_prefix.cu: the prefix parts of splits whose prefix_rows is 128 or 256
+int launch_prefix(const AttnParams &p, int dtype, int device, cudaStream_t s);
 
 }  // namespace tc

@@ -9,13 +9,13 @@
 #include <cmath>
 
 #include "attn.h"
-#include "ops_device.cuh"
+#include "attn_device.cuh"
 
 namespace tc {
 
 constexpr int kSms = 148;  // B200; the workspace must not depend on the device that happens to be current
 
-void split_attn(int64_t R, int64_t Hq, int64_t H, int64_t D, int64_t max_len, int64_t max_prefix, AttnSplit *s)
+void split_attn(int64_t R, int64_t Hq, int64_t H, int64_t D, int64_t max_len, int64_t max_prefix, bool quantised, AttnSplit *s)
 {
     *s = AttnSplit{};
     s->group = static_cast<int32_t>(Hq / H);
@@ -37,27 +37,30 @@ void split_attn(int64_t R, int64_t Hq, int64_t H, int64_t D, int64_t max_len, in
     // Own tokens: about six CTAs per SM where there are few requests; at most 1024 keys a part, so that
     // one long request among short ones is not one CTA's work.
     cut(max_len, R * H * s->own_blocks, 6 * kSms, 1024, &s->own_chunk, &s->own_parts);
-    s->prefix_rows = 16;
-    s->prefix_blocks = static_cast<int32_t>((R * s->group + s->prefix_rows - 1) / s->prefix_rows);
-    cut(max_prefix, H * s->prefix_blocks, 6 * kSms, 1 << 20, &s->prefix_chunk, &s->prefix_parts);
+    const int64_t rows = R * s->group;  // of one KV head
+    s->prefix_rows = max_prefix == 0 || rows <= 16 || D > 128 || quantised ? 16 : rows <= 128 ? 128 : 256;
+    s->prefix_blocks = static_cast<int32_t>((rows + s->prefix_rows - 1) / s->prefix_rows);
+    if (s->prefix_rows == 16) {
+        cut(max_prefix, H * s->prefix_blocks, 6 * kSms, 1 << 20, &s->prefix_chunk, &s->prefix_parts);
+    } else {
+        // One CTA per SM: the number of parts that leaves the fewest tiles to the busiest SM, a part costing
+        // about two tiles to start and end.
+        const int64_t tiles = (max_prefix + 127) / 128, ctas = H * s->prefix_blocks;
+        int64_t best = 1, best_cost = INT64_MAX;
+        for (int64_t n = 1; n <= std::min<int64_t>(tiles, 64); n++) {
+            const int64_t per = (tiles + n - 1) / n, cost = (ctas * ((tiles + per - 1) / per) + kSms - 1) / kSms * (per + 2);
+            if (cost < best_cost) best = n, best_cost = cost;
+        }
+        const int64_t per = (tiles + best - 1) / best;
+        s->prefix_chunk = per * 128;
+        s->prefix_parts = static_cast<int32_t>((tiles + per - 1) / per) * (s->prefix_rows == 128 ? 2 : 1);
+    }
     const int64_t parts = static_cast<int64_t>(s->own_parts) + s->prefix_parts;
     s->sum_bytes = (parts * s->rows * 4 + 255) / 256 * 256;
     s->workspace = s->sum_bytes + parts * s->rows * D * 4;
 }
 
 // ------------------------------------------------------------------------------- device helpers
-__device__ __forceinline__ void copy_async16(uint32_t dst, const void *src, bool there)
-{
-    // nothing is read where `there` is false: 16 zero bytes are written
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
-}
-__device__ __forceinline__ void copy_async4(uint32_t dst, const void *src, bool there)
-{
-    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(there ? 4 : 0) : "memory");
-}
-__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N> __device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
-
 template <bool TRANS>
 __device__ __forceinline__ void load_matrix4(uint32_t addr, uint32_t (&r)[4])
 {
@@ -94,13 +97,6 @@ template <> __device__ __forceinline__ void mma16816<__nv_bfloat16>(float (&c)[4
 {
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
-
-__device__ __forceinline__ float exp2_approx(float x)
-{
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
 }
 
 // ------------------------------------------------------------------------------ the parts' kernel
@@ -191,7 +187,7 @@ __global__ void __launch_bounds__(128) parts_kernel(const __grid_constant__ Attn
     const int H = p.layer.H, group = p.split.group;
 
     // Which part: [begin, end) of the keys behind `table`, for rows row0 .. of KV head h.
-    const int64_t prefix_ctas = static_cast<int64_t>(p.split.prefix_parts) * H * p.split.prefix_blocks;
+    const int64_t prefix_ctas = p.split.prefix_rows == 16 ? static_cast<int64_t>(p.split.prefix_parts) * H * p.split.prefix_blocks : 0;
     int64_t id = blockIdx.x, begin, end, row0, row_end, part, table_width;
     int h;
     const int32_t *table;
@@ -485,7 +481,7 @@ __global__ void __launch_bounds__(128) join_kernel(const __grid_constant__ AttnP
     if (len < 0) return;
     len = min(len, p.max_len);
     const int64_t shared_len = p.split.prefix_parts ? min(max(static_cast<int64_t>(*p.prefix_len), int64_t(0)), p.max_prefix) : 0;
-    const int front = static_cast<int>((shared_len + p.split.prefix_chunk - 1) / p.split.prefix_chunk);
+    const int front = static_cast<int>((shared_len + p.split.prefix_chunk - 1) / p.split.prefix_chunk) * (p.split.prefix_rows == 128 ? 2 : 1);
     const int back = static_cast<int>((len + p.split.own_chunk - 1) / p.split.own_chunk);
     const int n = front + back;
     auto index = [&](int i) -> int64_t { return static_cast<int64_t>(i < front ? i : p.split.prefix_parts + i - front) * p.split.rows + row; };
@@ -498,6 +494,7 @@ __global__ void __launch_bounds__(128) join_kernel(const __grid_constant__ AttnP
     for (int i = 0; i < n; i++) {
         const int64_t at = index(i);
         const float w = exp2f(p.sums[at] - base);
+        if (w == 0.f) continue;  // also a part that has no keys: its outputs were not written
         total += w;
         const float *src = p.parts + at * D + lane * 4;
 #pragma unroll
@@ -543,9 +540,10 @@ static int launch_parts_for(const AttnParams &p, unsigned grid, int device, cuda
 template <typename T>
 static int launch_decode(const AttnParams &p, int device, cudaStream_t s)
 {
-    const int64_t ctas = static_cast<int64_t>(p.split.prefix_parts) * p.layer.H * p.split.prefix_blocks + static_cast<int64_t>(p.split.own_parts) * p.R * p.layer.H * p.split.own_blocks;
-    if (ctas > INT32_MAX) return fail(TC_ERR_TOO_LARGE, "%lld parts: too many for one call", (long long)ctas);
     int rc = TC_OK;
+    if (p.split.prefix_rows > 16 && (rc = launch_prefix(p, std::is_same<T, __half>::value ? TC_FP16 : TC_BF16, device, s)) != TC_OK) return rc;
+    const int64_t ctas = (p.split.prefix_rows == 16 ? static_cast<int64_t>(p.split.prefix_parts) * p.layer.H * p.split.prefix_blocks : 0) + static_cast<int64_t>(p.split.own_parts) * p.R * p.layer.H * p.split.own_blocks;
+    if (ctas > INT32_MAX) return fail(TC_ERR_TOO_LARGE, "%lld parts: too many for one call", (long long)ctas);
     if (ctas) {
         const unsigned grid = static_cast<unsigned>(ctas);
         switch (p.layer.dtype) {
@@ -578,7 +576,7 @@ static int check_decode(const tc_kv_layer_t *layer, const tc_attn_decode_t *a, A
     if (a->max_len < 0 || a->max_len > INT32_MAX - 4096 || a->max_prefix < 0 || a->max_prefix > INT32_MAX - 4096)
         return fail(TC_ERR_SHAPE, "max_len %lld and max_prefix %lld must be in [0, 2^31 - 4096)", (long long)a->max_len, (long long)a->max_prefix);
     if (!(a->scale == a->scale) || std::isinf(a->scale)) return fail(TC_ERR_INVALID_ARG, "scale is not a finite number");
-    split_attn(a->R, a->Hq, p->layer.H, D, a->max_len, a->max_prefix, &p->split);
+    split_attn(a->R, a->Hq, p->layer.H, D, a->max_len, a->max_prefix, p->layer.quantised(), &p->split);
     return TC_OK;
 }
 

@@ -1,0 +1,387 @@
+// The shared prefix of tc_attn_decode on the fifth-generation tensor cores.
+//
+// All rows of queries of one KV head - R requests x Hq / H heads - meet every key of the prefix, so
+// this is a dense attention over pages.  A CTA has two slots of 128 rows in tensor memory, each with its scores S (128
+// columns) and its outputs O.  With more than 128 rows the slots hold different rows and both take
+// every tile of 128 keys, so a tile is read once for 256 rows; with fewer, both hold the same rows and
+// take the tiles in turn.  Either way the tensor cores work on one slot while the other is in its softmax.
+//
+//   warps 0-3, 4-7   softmax of slot 0 and 1: a thread owns one row, so no shuffle is needed.  Two passes
+//                    over S: the maximum, then the probabilities, rounded to 16 bits and written over
+//                    S, where the second product takes them from tensor memory.  The running maximum
+//                    moves only when a tile exceeds it by more than 2^8 (then O is rescaled).
+//   warps 8-11       fill a ring of K and V tiles from the pages: 16-byte asynchronous copies into the
+//                    swizzled layout, whatever the page size; one lane looks a key's block up.
+//   warp 12          one thread issues the matrix products in the order
+//                    O0 += P0 V, S0 = Q0 K', O1 += P1 V, S1 = Q1 K', ...
+//
+// Every wait is bounded; one that runs out sets TC_DEVICE_BULK_WAIT_TIMEOUT and the CTA leaves.
+#include <algorithm>
+
+#include "attn.h"
+#include "attn_device.cuh"
+
+namespace tc {
+
+constexpr int kTile = 128;       // keys of a tile, and rows of a slot
+constexpr int kPrefixThreads = 416;
+
+template <int DP, bool TWO>
+struct PrefixShape {
+    static constexpr int halves = DP / 64;
+    static constexpr int tile = kTile * DP * 2;        // bytes of a K or V tile, and of a slot's queries
+    static constexpr int queries = (TWO ? 2 : 1) * tile;
+    static constexpr int stages = TWO && DP == 128 ? 4 : DP == 128 ? 5 : 8;
+    static constexpr int infos = 8;                    // tiles whose validity masks are kept
+    static constexpr int bytes = queries + stages * tile + infos * 16 + 512 + 1024;  // + slack for the alignment
+};
+
+__device__ __forceinline__ void barrier_init(uint32_t bar, uint32_t count) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory"); }
+__device__ __forceinline__ void barrier_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
+// Waits for the phase of that parity to end; false when it does not within about a second.
+__device__ __forceinline__ bool barrier_wait(uint32_t bar, uint32_t parity)
+{
+    for (uint32_t spin = 0; spin < (1u << 20); spin++) {
+        uint32_t done;
+        asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+                     : "=r"(done) : "r"(bar), "r"(parity), "r"(1000u) : "memory");
+        if (done) return true;
+        if (spin > 64) __nanosleep(500);
+    }
+    return false;
+}
+
+// Shared-memory operand descriptor: 128-byte swizzle, 8-row atoms of 1024 bytes `sbo` apart; lbo: from one
+// 64-element column of atoms to the next (only where the 64 elements run along M or N).
+__device__ __forceinline__ uint64_t operand(uint32_t addr, uint32_t lbo)
+{
+    return static_cast<uint64_t>((addr >> 4) & 0x3fff) | static_cast<uint64_t>(lbo >> 4) << 16 | static_cast<uint64_t>(1024 >> 4) << 32 | 1ull << 46 | 2ull << 61;
+}
+// Instruction descriptor: fp32 sums of 16-bit products, M = 128.
+template <typename A> __device__ constexpr uint32_t instruction(int n, bool b_rows_along_n)
+{
+    const uint32_t type = sizeof(A) && std::is_same<A, __nv_bfloat16>::value ? 1 : 0;
+    return 1u << 4 | type << 7 | type << 10 | (b_rows_along_n ? 1u << 16 : 0u) | static_cast<uint32_t>(n / 8) << 17 | (128u / 16) << 24;
+}
+__device__ __forceinline__ void mma_shared(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add)
+{
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(static_cast<uint32_t>(add)) : "memory");
+}
+__device__ __forceinline__ void mma_tensor(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool add)
+{
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(static_cast<uint32_t>(add)) : "memory");
+}
+// Arrives at the barrier when all products issued so far by this thread are done.
+__device__ __forceinline__ void commit_to(uint32_t bar) { asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory"); }
+
+#define TC_R8(r, o) "=r"(r[o]), "=r"(r[o + 1]), "=r"(r[o + 2]), "=r"(r[o + 3]), "=r"(r[o + 4]), "=r"(r[o + 5]), "=r"(r[o + 6]), "=r"(r[o + 7])
+#define TC_W8(r, o) "r"(r[o]), "r"(r[o + 1]), "r"(r[o + 2]), "r"(r[o + 3]), "r"(r[o + 4]), "r"(r[o + 5]), "r"(r[o + 6]), "r"(r[o + 7])
+// 32 columns of this thread's lane.  The registers hold them after tensor_loaded().
+__device__ __forceinline__ void tensor_load32(uint32_t addr, uint32_t (&r)[32])
+{
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+                 : TC_R8(r, 0), TC_R8(r, 8), TC_R8(r, 16), TC_R8(r, 24) : "r"(addr));
+}
+__device__ __forceinline__ void tensor_store32(uint32_t addr, const uint32_t (&r)[32])
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31};" ::TC_W8(r, 0), TC_W8(r, 8),
+                 TC_W8(r, 16), TC_W8(r, 24), "r"(addr) : "memory");
+}
+__device__ __forceinline__ void tensor_store16(uint32_t addr, const uint32_t (&r)[16])
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15};" ::TC_W8(r, 0), TC_W8(r, 8), "r"(addr) : "memory");
+}
+__device__ __forceinline__ void tensor_loaded() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tensor_stored() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void fence_shared_to_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+
+// Byte of element d of row r in a swizzled tile of 128 rows: columns of 64 elements, 128 bytes a row, the
+// 16-byte chunks of a row permuted by its place in its group of eight.
+__device__ __forceinline__ uint32_t swizzled(int r, int chunk) { return (chunk >> 3) * (kTile * 128) + r * 128 + (((chunk & 7) ^ (r & 7)) << 4); }
+
+template <typename T, int DP, bool TWO>
+__global__ void __launch_bounds__(kPrefixThreads, 1) prefix_kernel(const __grid_constant__ AttnParams p)
+{
+    using Shape = PrefixShape<DP, TWO>;
+    extern __shared__ unsigned char raw[];
+    const uint32_t base = (static_cast<uint32_t>(__cvta_generic_to_shared(raw)) + 1023) & ~1023u;
+    unsigned char *const gen = raw + (base - static_cast<uint32_t>(__cvta_generic_to_shared(raw)));
+    const uint32_t ring = base + Shape::queries, info = ring + Shape::stages * Shape::tile, bars = info + Shape::infos * 16;
+    const uint32_t full = bars, empty = full + 8 * Shape::stages, s_full = empty + 8 * Shape::stages, p_ready = s_full + 16, o_done = p_ready + 16, tensor_at = o_done + 16;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, H = p.layer.H, group = p.split.group, D = p.layer.D;
+
+    // Which rows, which keys.
+    int64_t id = blockIdx.x;
+    const int64_t block = id % p.split.prefix_blocks;
+    id /= p.split.prefix_blocks;
+    const int h = static_cast<int>(id % H);
+    const int64_t part = id / H;
+    int64_t len = *p.prefix_len;
+    if (len > p.max_prefix || len < 0) {
+        if (threadIdx.x == 0) atomicOr(p.status, kStatusBadIndex);
+        len = len < 0 ? 0 : p.max_prefix;
+    }
+    const int begin = static_cast<int>(part * p.split.prefix_chunk);
+    const int end = static_cast<int>(min(static_cast<int64_t>(begin) + p.split.prefix_chunk, len));
+    if (begin >= end) return;
+    const int tiles = (end - begin + kTile - 1) / kTile;
+    const int64_t row0 = block * (TWO ? 256 : 128), row_end = p.R * group;
+    const int steps = TWO ? 2 * tiles : tiles;  // step t: slot t & 1, tile t / 2 (TWO) or t
+
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < Shape::stages; i++) barrier_init(full + 8 * i, 128), barrier_init(empty + 8 * i, 1);
+        for (int i = 0; i < 2; i++) barrier_init(s_full + 8 * i, 1), barrier_init(p_ready + 8 * i, 128), barrier_init(o_done + 8 * i, 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 12) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(tensor_at) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    // Queries: zero past the last row and past D; a negative scale is taken into their sign.
+    const uint32_t flip = p.scale_log2 < 0.f ? 0x80008000u : 0u;
+    for (int i = threadIdx.x; i < (TWO ? 256 : 128) * (DP / 8); i += kPrefixThreads) {
+        const int r = i / (DP / 8), chunk = i % (DP / 8);
+        const int64_t row = row0 + r;
+        uint4 v = make_uint4(0, 0, 0, 0);
+        if (row < row_end && chunk * 8 < D) {
+            const int64_t req = quick_div(static_cast<uint32_t>(row), p.div_group);
+            v = *reinterpret_cast<const uint4 *>(p.q + req * p.q_req + (h * group + (row - req * group)) * p.q_head + chunk * 16);
+            v.x ^= flip, v.y ^= flip, v.z ^= flip, v.w ^= flip;
+        }
+        *reinterpret_cast<uint4 *>(gen + (r >> 7) * Shape::tile + swizzled(r & 127, chunk)) = v;
+    }
+    fence_shared_to_async();
+    fence_before();
+    __syncthreads();
+    fence_after();
+    uint32_t tensor;
+    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(tensor) : "r"(tensor_at));
+    bool fine = true;  // no wait of this thread has run out
+
+    if (warp < 8) {
+        // ---------------------------------------------------------------------------- softmax
+        const int slot = warp >> 2, r = (warp & 3) * 32 + lane;
+        const uint32_t lanes = tensor + (static_cast<uint32_t>((warp & 3) * 32) << 16), s_at = lanes + slot * 128, o_at = lanes + 256 + slot * 128;
+        const float scale = fabsf(p.scale_log2);
+        float top = -INFINITY, sum = 0.f;
+        int mine = 0;
+        for (int t = slot; t < steps && fine; t += 2, mine++) {
+            fine = __all_sync(0xffffffffu, barrier_wait(s_full + 8 * slot, mine & 1));
+            if (!fine) break;
+            fence_after();
+            const int tile = TWO ? t >> 1 : t;
+            uint32_t mask[4];
+            asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(mask[0]), "=r"(mask[1]), "=r"(mask[2]), "=r"(mask[3]) : "r"(info + (tile % Shape::infos) * 16));
+            const bool whole = (mask[0] & mask[1] & mask[2] & mask[3]) == 0xffffffffu;
+            float most = -INFINITY;
+#pragma unroll
+            for (int c = 0; c < 4; c++) {
+                uint32_t v[32];
+                tensor_load32(s_at + 32 * c, v);
+                tensor_loaded();
+                if (whole) {
+#pragma unroll
+                    for (int i = 0; i < 32; i += 2) most = fmaxf(most, fmaxf(__uint_as_float(v[i]), __uint_as_float(v[i + 1])));
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 32; i++)
+                        if (mask[c] >> i & 1) most = fmaxf(most, __uint_as_float(v[i]));
+                }
+            }
+            most *= scale;
+            if (__any_sync(0xffffffffu, most > top + 8.f)) {
+                const float m = fmaxf(top, most), f = m == top ? 1.f : exp2_approx(top - m);
+                top = m;
+                sum *= f;
+                if (mine) {
+#pragma unroll
+                    for (int c = 0; c < DP / 32; c++) {
+                        uint32_t v[32];
+                        tensor_load32(o_at + 32 * c, v);
+                        tensor_loaded();
+#pragma unroll
+                        for (int i = 0; i < 32; i++) v[i] = __float_as_uint(__uint_as_float(v[i]) * f);
+                        tensor_store32(o_at + 32 * c, v);
+                    }
+                }
+            }
+            const float m = top == -INFINITY ? 0.f : top;
+            float add[2] = {0.f, 0.f};
+#pragma unroll
+            for (int c = 0; c < 4; c++) {
+                uint32_t v[32], w[16];
+                tensor_load32(s_at + 32 * c, v);
+                tensor_loaded();
+#pragma unroll
+                for (int i = 0; i < 16; i++) {
+                    float a = fmaf(__uint_as_float(v[2 * i]), scale, -m), b = fmaf(__uint_as_float(v[2 * i + 1]), scale, -m);
+                    if (!whole) {
+                        if (!(mask[c] >> (2 * i) & 1)) a = -INFINITY;
+                        if (!(mask[c] >> (2 * i + 1) & 1)) b = -INFINITY;
+                    }
+                    a = exp2_approx(a), b = exp2_approx(b);
+                    add[0] += a, add[1] += b;
+                    w[i] = pack2<T>(a, b);
+                }
+                tensor_store16(s_at + 16 * c, w);
+            }
+            sum += add[0] + add[1];
+            tensor_stored();
+            fence_before();
+            barrier_arrive(p_ready + 8 * slot);
+        }
+        // The part: outputs by the sum, and its logarithm.  A slot without a tile says -infinity.
+        const int64_t row = row0 + (TWO ? slot * 128 : 0) + r;
+        const int64_t out_part = TWO ? part : 2 * part + slot;
+        const bool store = row < row_end;
+        const int64_t req = store ? quick_div(static_cast<uint32_t>(row), p.div_group) : 0;
+        const int64_t at = out_part * p.split.rows + req * p.Hq + h * group + (row - req * group);
+        if (mine && fine) fine = __all_sync(0xffffffffu, barrier_wait(o_done + 8 * slot, 0));
+        if (mine && fine) {
+            fence_after();
+            const float inv = sum == 0.f ? 0.f : 1.f / sum;
+#pragma unroll
+            for (int c = 0; c < DP / 32; c++) {
+                uint32_t v[32];
+                tensor_load32(o_at + 32 * c, v);
+                tensor_loaded();
+#pragma unroll
+                for (int i = 0; i < 32; i += 4)
+                    if (store && 32 * c + i < D)
+                        *reinterpret_cast<float4 *>(p.parts + at * D + 32 * c + i) =
+                            make_float4(__uint_as_float(v[i]) * inv, __uint_as_float(v[i + 1]) * inv, __uint_as_float(v[i + 2]) * inv, __uint_as_float(v[i + 3]) * inv);
+            }
+        }
+        if (store) p.sums[at] = !mine || sum == 0.f ? -INFINITY : (top == -INFINITY ? 0.f : top) + log2f(sum);
+    } else if (warp < 12) {
+        // --------------------------------------------------------------------------- the pages
+        const int w = warp - 8;
+        auto look_up = [&](int tile) -> int32_t {
+            const int t = begin + tile * kTile + w * 32 + lane;
+            if (tile >= tiles || t >= end) return -1;
+            const int32_t b = p.prefix_table[quick_div(static_cast<uint32_t>(t), p.div_block)];
+            if (b < 0 || b >= p.layer.num_blocks) {
+                atomicOr(p.status, kStatusBadIndex);
+                return -1;
+            }
+            return b;
+        };
+        int32_t ahead = look_up(0);
+        int told = 0;  // copies whose arrival has been passed on
+        // Copy u (K of tile u / 2, then V) goes to stage u % stages; three copies are in flight.
+        auto pass_on = [&](int u) {
+            fence_shared_to_async();
+            barrier_arrive(full + 8 * (u % Shape::stages));
+        };
+        for (int tile = 0; tile < tiles && fine; tile++) {
+            const int32_t blk = ahead;
+            ahead = look_up(tile + 1);
+            const int t = begin + tile * kTile + w * 32 + lane;
+            const int n = t - static_cast<int>(quick_div(static_cast<uint32_t>(t), p.div_block)) * static_cast<int>(p.layer.B);
+            const int64_t off = blk >= 0 ? p.layer.geo.at(blk, n, h) : -1;
+            const uint32_t mask = __ballot_sync(0xffffffffu, blk >= 0);
+            for (int kv = 0; kv < 2; kv++) {
+                const int u = 2 * tile + kv, stage = u % Shape::stages;
+                if (u >= Shape::stages) fine = __all_sync(0xffffffffu, barrier_wait(empty + 8 * stage, (u / Shape::stages - 1) & 1));
+                if (!fine) break;
+                // an older tile's mask is past its last use when this tile's K stage is free
+                if (kv == 0 && lane == 0) asm volatile("st.shared.u32 [%0], %1;" ::"r"(info + (tile % Shape::infos) * 16 + 4 * w), "r"(mask) : "memory");
+                const char *plane = kv ? p.layer.v : p.layer.k;
+                const uint32_t to = ring + stage * Shape::tile;
+                constexpr int chunks = DP / 8;
+#pragma unroll
+                for (int i = 0; i < chunks; i++) {
+                    const int idx = i * 32 + lane, rr = idx / chunks, ch = idx % chunks;
+                    const int64_t src = __shfl_sync(0xffffffffu, off, rr);
+                    const bool there = src >= 0 && ch * 8 < D;
+                    copy_async16(to + swizzled(w * 32 + rr, ch), plane + (there ? src + ch * 16 : 0), there);
+                }
+                copy_commit();
+                if (u >= 2) {
+                    copy_wait<2>();
+                    pass_on(told++);
+                }
+            }
+        }
+        copy_wait<0>();
+        if (fine)
+            while (told < 2 * tiles) pass_on(told++);
+    } else if (lane == 0) {
+        // --------------------------------------------------------------------- matrix products
+        const uint32_t qk = instruction<T>(kTile, false), pv = instruction<T>(DP, true);
+        auto scores = [&](int t) {
+            const int slot = t & 1, tile = TWO ? t >> 1 : t, u = 2 * tile, stage = u % Shape::stages;
+            if (!TWO || slot == 0) {
+                if (!barrier_wait(full + 8 * stage, (u / Shape::stages) & 1)) return false;
+                fence_after();
+            }
+            const uint32_t q = base + (TWO ? slot * Shape::tile : 0), k = ring + stage * Shape::tile;
+#pragma unroll
+            for (int i = 0; i < DP / 16; i++) {
+                const uint32_t at = (i >> 2) * (kTile * 128) + (i & 3) * 32;
+                mma_shared(tensor + slot * 128, operand(q + at, 16), operand(k + at, 16), qk, i > 0);
+            }
+            commit_to(s_full + 8 * slot);
+            if (!TWO || slot == 1) commit_to(empty + 8 * stage);
+            return true;
+        };
+        for (int t = 0; t < 2 && t < steps && fine; t++) fine = scores(t);
+        for (int t = 0; t < steps && fine; t++) {
+            const int slot = t & 1, tile = TWO ? t >> 1 : t, u = 2 * tile + 1, stage = u % Shape::stages;
+            if (!TWO || slot == 0) fine = barrier_wait(full + 8 * stage, (u / Shape::stages) & 1);
+            if (fine) fine = barrier_wait(p_ready + 8 * slot, (t >> 1) & 1);
+            if (!fine) break;
+            fence_after();
+            const uint32_t v = ring + stage * Shape::tile;
+#pragma unroll
+            for (int i = 0; i < kTile / 16; i++) mma_tensor(tensor + 256 + slot * 128, tensor + slot * 128 + 8 * i, operand(v + i * 2048, kTile * 128), pv, t > 1 || i > 0);
+            if (!TWO || slot == 1) commit_to(empty + 8 * stage);
+            if (t + 2 >= steps) commit_to(o_done + 8 * slot);
+            else fine = scores(t + 2);
+        }
+        if (!fine) {
+            // products may be in flight: let them end before the tensor memory is given back
+            commit_to(o_done);
+            barrier_wait(o_done, 0);
+        }
+    }
+    if (!fine) atomicOr(p.status, static_cast<unsigned int>(TC_DEVICE_BULK_WAIT_TIMEOUT));
+    fence_before();
+    __syncthreads();
+    if (warp == 12) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tensor) : "memory");
+}
+
+template <typename T, int DP, bool TWO>
+static int launch_prefix_shape(const AttnParams &p, unsigned grid, int device, cudaStream_t s)
+{
+    static bool raised[kMaxDevices];
+    if (!raised[device]) {
+        const cudaError_t e = cudaFuncSetAttribute(prefix_kernel<T, DP, TWO>, cudaFuncAttributeMaxDynamicSharedMemorySize, PrefixShape<DP, TWO>::bytes);
+        if (e != cudaSuccess) return cuda_fail(e, "cudaFuncSetAttribute(dynamic shared memory)");
+        raised[device] = true;
+    }
+    prefix_kernel<T, DP, TWO><<<grid, kPrefixThreads, PrefixShape<DP, TWO>::bytes, s>>>(p);
+    const cudaError_t e = cudaGetLastError();
+    return e == cudaSuccess ? TC_OK : cuda_fail(e, "kernel launch");
+}
+
+template <typename T>
+static int launch_prefix_type(const AttnParams &p, unsigned grid, int device, cudaStream_t s)
+{
+    const bool two = p.split.prefix_rows == 256;
+    if (p.layer.D <= 64) return two ? launch_prefix_shape<T, 64, true>(p, grid, device, s) : launch_prefix_shape<T, 64, false>(p, grid, device, s);
+    return two ? launch_prefix_shape<T, 128, true>(p, grid, device, s) : launch_prefix_shape<T, 128, false>(p, grid, device, s);
+}
+
+int launch_prefix(const AttnParams &p, int dtype, int device, cudaStream_t s)
+{
+    const int64_t chunks = p.split.prefix_rows == 256 ? p.split.prefix_parts : p.split.prefix_parts / 2;
+    const int64_t ctas = chunks * p.layer.H * p.split.prefix_blocks;
+    if (ctas > INT32_MAX) return fail(TC_ERR_TOO_LARGE, "%lld parts: too many for one call", (long long)ctas);
+    const unsigned grid = static_cast<unsigned>(ctas);
+    return dtype == TC_BF16 ? launch_prefix_type<__nv_bfloat16>(p, grid, device, s) : launch_prefix_type<__half>(p, grid, device, s);
+}
+
+}  // namespace tc

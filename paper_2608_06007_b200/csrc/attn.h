@@ -9,10 +9,11 @@ namespace tc {
 // logarithm of its sum in the workspace, and a last kernel joins them.
 struct AttnSplit {
     int32_t group;             // query heads per KV head
-    int32_t prefix_rows;       // rows of queries one prefix CTA takes: 16 (parts_kernel), 128 or 256 (prefix_kernel;
+    int32_t prefix_rows;       // rows of queries one prefix CTA takes: 16 (parts_kernel, `columns`), 128 or 256 (prefix_kernel;
                                // 128: two parts per chunk of keys, one a slot)
     int32_t prefix_blocks;     // such blocks of the R * group rows of one KV head
-    int32_t own_blocks;        // blocks of 16 of a request's group rows
+    int32_t columns;           // rows a CTA of parts_kernel takes: 8, or 16 for groups of more than 8
+    int32_t own_blocks;        // blocks of `columns` of a request's group rows
     int64_t prefix_chunk, own_chunk;  // keys per part
     int32_t prefix_parts, own_parts;
     int64_t rows;              // R * Hq
@@ -31,7 +32,7 @@ struct AttnParams {
     int64_t table_width, table_stride;
     const int32_t *lens, *prefix_table, *prefix_len;
     int64_t R, max_len, max_prefix;
-    int32_t Hq;
+    int32_t Hq, q_bf16;
     float scale_log2;  // scale * log2(e)
     FastDiv div_block, div_group;
     AttnSplit split;

@@ -20,7 +20,8 @@ void split_attn(int64_t R, int64_t Hq, int64_t H, int64_t D, int64_t max_len, in
     *s = AttnSplit{};
     s->group = static_cast<int32_t>(Hq / H);
     s->rows = R * Hq;
-    s->own_blocks = (s->group + 15) / 16;
+    s->columns = s->group <= 8 ? 8 : 16;
+    s->own_blocks = (s->group + s->columns - 1) / s->columns;
     auto cut = [&](int64_t keys, int64_t ctas, int64_t want, int64_t longest, int64_t *chunk, int32_t *parts) {
         if (keys <= 0) {
             *chunk = 64, *parts = 0;
@@ -39,7 +40,8 @@ void split_attn(int64_t R, int64_t Hq, int64_t H, int64_t D, int64_t max_len, in
     cut(max_len, R * H * s->own_blocks, 6 * kSms, 1024, &s->own_chunk, &s->own_parts);
     const int64_t rows = R * s->group;  // of one KV head
     s->prefix_rows = max_prefix == 0 || rows <= 16 || D > 128 || quantised ? 16 : rows <= 128 ? 128 : 256;
-    s->prefix_blocks = static_cast<int32_t>((rows + s->prefix_rows - 1) / s->prefix_rows);
+    const int64_t block = s->prefix_rows == 16 ? s->columns : s->prefix_rows;
+    s->prefix_blocks = static_cast<int32_t>((rows + block - 1) / block);
     if (s->prefix_rows == 16) {
         cut(max_prefix, H * s->prefix_blocks, 6 * kSms, 1 << 20, &s->prefix_chunk, &s->prefix_parts);
     } else {
@@ -101,26 +103,31 @@ template <> __device__ __forceinline__ void mma16816<__nv_bfloat16>(float (&c)[4
 
 // ------------------------------------------------------------------------------ the parts' kernel
 // One warp works alone on tiles of 16 keys; four warps of a CTA share a part and join at its end.
-// S = Q K^T and O = P V run on m16n8k16: 16 rows are the query heads of one KV head (or 16 rows of
-// the batch for the prefix), so each staged byte of K and V is used once per row block and the
-// kernel is bound by HBM.  A warp has its own ring of stages, filled by 16-byte asynchronous copies
-// whatever the size of the pages, and waits for no other warp until the end.
+// The keys are the rows of the matrix products, S' = K Q' and O' = V' P' on m16n8k16: the columns are
+// the query heads of one KV head (or rows of the batch, for a prefix with few of them), 8 or 16 at
+// a time, so few heads leave little of a product idle, and every staged byte of K and V is used once
+// per block of columns.  Bound by HBM.  S' comes out with a key's scores along a lane quad; packed
+// to 16 bits its 8 x 8 blocks are transposed into the second product's operand by movmatrix.
+// A warp has its own ring of stages, filled by 16-byte asynchronous copies whatever the size of
+// the pages, and waits for no other warp until the end.
 //
-// Codes of a quantised pool are staged as they are.  They become 16-bit numbers on the way into the
-// fragments, exactly (both formats fit bf16 and fp16); the scales multiply the scores and the
-// probabilities.  A lane reads 16 consecutive codes at once, so the order of the d's inside the two
-// products is a permutation: the queries' fragments use the same one, the outputs undo it.
+// Codes of a quantised pool are staged as they are and become 16-bit numbers on the way into the
+// fragments, exactly: K in fp16, V in bf16.  The scales multiply the scores and the probabilities; a
+// probability times a scale needs bf16's range.  Queries of such a pool are fp16 with a power of two
+// per row taken out, so that the row's largest is in [2^14, 2^15): what is then below fp16's smallest
+// step is below 2^-38 of that largest.  A lane reads 16 consecutive codes at once, so the order of the d's
+// inside the products is a permutation: the queries use the same one, the outputs undo it.
 enum { kPlain = 0, kE4m3 = 1, kInt8 = 2 };
 
-template <int KIND, int DP>
+template <int KIND, int DP, int NB>
 struct Ring {
     static constexpr int esize = KIND == kPlain ? 2 : 1;
     static constexpr int row = DP * esize, chunks = row / 16;  // bytes and 16-byte chunks of a key
     static constexpr int plane = 16 * row;
     static constexpr int scale_at = 2 * plane, mask_at = scale_at + (KIND == kPlain ? 0 : 128);
     static constexpr int stage = mask_at + 16;
-    static constexpr int stages = stage > 6144 ? 3 : 4;
-    static constexpr int join = 4 * 16 * (DP + 2) * 4;  // the warps' outputs and statistics at the end
+    static constexpr int stages = 3;  // D = 128: two CTAs an SM for 16-bit pools, four for codes
+    static constexpr int join = 4 * 8 * NB * (DP + 2) * 4;  // the warps' outputs and statistics at the end
     static constexpr int bytes = 4 * stages * stage > join ? 4 * stages * stage : join;
 };
 
@@ -130,58 +137,63 @@ struct Ring {
 template <int KIND, int DP>
 __device__ __forceinline__ int place_of(int r, int c)
 {
-    if constexpr (KIND == kPlain) return r * Ring<KIND, DP>::row + ((c ^ (r & 7)) << 4);
-    else if constexpr (DP >= 128) return r * Ring<KIND, DP>::row + ((c ^ ((((r ^ (r >> 2)) & 1) << 2) | (r & 2))) << 4);
-    else return r * Ring<KIND, DP>::row + ((c ^ ((r >> 1) & 2)) << 4);
+    constexpr int row = DP * (KIND == kPlain ? 2 : 1);
+    if constexpr (KIND == kPlain) return r * row + ((c ^ (r & 7)) << 4);
+    else if constexpr (DP >= 128) return r * row + ((c ^ ((((r ^ (r >> 2)) & 1) << 2) | (r & 2))) << 4);
+    else return r * row + ((c ^ ((r >> 1) & 2)) << 4);
 }
 
-// Two codes, bytes 0 and 2 of w (the others may hold anything), as two 16-bit numbers.
-template <int KIND, typename T> __device__ __forceinline__ uint32_t widen(uint32_t w);
-// e4m3 -> bf16: sign, exponent and fraction bits in place are the value times 2^-120 (subnormals too);
-// the product with 2^120 is exact.  The two codes 0x7f and 0xff (NaN) are not made by tc_kv_append.
-template <> __device__ __forceinline__ uint32_t widen<kE4m3, __nv_bfloat16>(uint32_t w)
+// Four codes w as two pairs of fp16 numbers, exactly.
+template <int KIND>
+__device__ __forceinline__ void widen_half(uint32_t w, uint32_t &lo, uint32_t &hi)
 {
-    const uint32_t v = ((w & 0x00800080u) << 8) | ((w & 0x007f007fu) << 4);
-    const uint32_t big = 0x7b807b80u;  // 2^120
-    const __nv_bfloat162 r = __hmul2(*reinterpret_cast<const __nv_bfloat162 *>(&v), *reinterpret_cast<const __nv_bfloat162 *>(&big));
-    return *reinterpret_cast<const uint32_t *>(&r);
-}
-template <> __device__ __forceinline__ uint32_t widen<kE4m3, __half>(uint32_t w) { return e4m3_to_half2((w & 0xffu) | ((w >> 8) & 0xff00u)); }
-// int8 -> bf16: 128 + the low seven bits, less 128 or (sign bit set) 256; both are bf16 numbers.
-template <> __device__ __forceinline__ uint32_t widen<kInt8, __nv_bfloat16>(uint32_t w)
-{
-    const uint32_t a = (w & 0x007f007fu) | 0x43004300u, b = (w & 0x00800080u) | 0x43004300u;
-    const __nv_bfloat162 r = __hsub2(*reinterpret_cast<const __nv_bfloat162 *>(&a), *reinterpret_cast<const __nv_bfloat162 *>(&b));
-    return *reinterpret_cast<const uint32_t *>(&r);
-}
-// int8 -> fp16: 1024 + (code + 128), less 1152.
-template <> __device__ __forceinline__ uint32_t widen<kInt8, __half>(uint32_t w)
-{
-    const uint32_t a = ((w & 0x00ff00ffu) ^ 0x00800080u) | 0x64006400u, b = 0x64806480u;
-    const __half2 r = __hsub2(*reinterpret_cast<const __half2 *>(&a), *reinterpret_cast<const __half2 *>(&b));
-    return *reinterpret_cast<const uint32_t *>(&r);
-}
-
-// Probabilities meet V in bf16 when V is codes: p * v_scale keeps fp32's range there.
-template <int KIND, typename T> struct ValueType { using type = T; };
-template <typename T> struct ValueType<kE4m3, T> { using type = __nv_bfloat16; };
-template <typename T> struct ValueType<kInt8, T> { using type = __nv_bfloat16; };
-
-// A length read from the device, cut to what the caller promised.
-__device__ __forceinline__ int64_t checked_length(int64_t len, int64_t most, unsigned int *status)
-{
-    if (len > most) {
-        atomicOr(status, kStatusBadIndex);
-        return most;
+    if constexpr (KIND == kE4m3) {
+        lo = e4m3_to_half2(w), hi = e4m3_to_half2(w >> 16);
+    } else {
+        // int8: the bytes of 1024 + (code + 128), less 1152
+        const uint32_t u = w ^ 0x80808080u, less = 0x64806480u;
+        const uint32_t a = __byte_perm(u, 0x64646464u, 0x4140), b = __byte_perm(u, 0x64646464u, 0x4342);
+        const __half2 x = __hsub2(*reinterpret_cast<const __half2 *>(&a), *reinterpret_cast<const __half2 *>(&less));
+        const __half2 y = __hsub2(*reinterpret_cast<const __half2 *>(&b), *reinterpret_cast<const __half2 *>(&less));
+        lo = *reinterpret_cast<const uint32_t *>(&x), hi = *reinterpret_cast<const uint32_t *>(&y);
     }
-    return len;
+}
+// The codes in byte t of v and w as a pair of bf16 numbers, exactly.
+template <int KIND>
+__device__ __forceinline__ uint32_t widen_bf16(uint32_t v, uint32_t w, int t)
+{
+    __nv_bfloat162 r;
+    if constexpr (KIND == kE4m3) {
+        // Sign, exponent and fraction bits in place are the value times 2^-120 (subnormals too); the product
+        // with 2^120 is exact.  (Codes 0x7f and 0xff, e4m3's NaN, would be +-480; a quantised row has none.)
+        const uint32_t x = __byte_perm(v, w, (t << 4) | ((4 + t) << 12));
+        const uint32_t y = (x & 0x80008000u) | ((x >> 4) & 0x07f007f0u), big = 0x7b807b80u;
+        r = __hmul2(*reinterpret_cast<const __nv_bfloat162 *>(&y), *reinterpret_cast<const __nv_bfloat162 *>(&big));
+    } else {
+        // 128 + the low seven bits, less 128 or (sign bit set) 256: all bf16 numbers
+        const uint32_t x = __byte_perm(v, w, t | ((4 + t) << 8));
+        const uint32_t a = (x & 0x007f007fu) | 0x43004300u, b = (x & 0x00800080u) | 0x43004300u;
+        r = __hsub2(*reinterpret_cast<const __nv_bfloat162 *>(&a), *reinterpret_cast<const __nv_bfloat162 *>(&b));
+    }
+    return *reinterpret_cast<const uint32_t *>(&r);
 }
 
-template <typename T, int KIND, int DP>
+__device__ __forceinline__ uint32_t transposed(uint32_t v)
+{
+    uint32_t r;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+    return r;
+}
+
+// T: the type of the products - the queries' for a plain pool; quantised pools have one kernel (fp16 scores,
+// bf16 values) and look at p.q_bf16.
+template <typename T, int KIND, int DP, int NB>
 __global__ void __launch_bounds__(128) parts_kernel(const __grid_constant__ AttnParams p)
 {
-    using R = Ring<KIND, DP>;
-    using VT = typename ValueType<KIND, T>::type;
+    using R = Ring<KIND, DP, NB>;
+    using ST = std::conditional_t<KIND == kPlain, T, __half>;
+    using VT = std::conditional_t<KIND == kPlain, T, __nv_bfloat16>;
+    constexpr int kCols = 8 * NB;
     extern __shared__ __align__(128) unsigned char shared[];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int H = p.layer.H, group = p.split.group;
@@ -206,7 +218,7 @@ __global__ void __launch_bounds__(128) parts_kernel(const __grid_constant__ Attn
         end = min(begin + p.split.prefix_chunk, len);
         table = p.prefix_table;
         table_width = INT32_MAX;
-        row0 = block * 16;
+        row0 = block * kCols;
         row_end = p.R * group;
     } else {
         id -= prefix_ctas;
@@ -226,39 +238,17 @@ __global__ void __launch_bounds__(128) parts_kernel(const __grid_constant__ Attn
         part += p.split.prefix_parts;
         table = reinterpret_cast<const int32_t *>(p.tables + r * p.table_stride);
         table_width = p.table_width;
-        row0 = r * group + block * 16;
+        row0 = r * group + block * kCols;
         row_end = (r + 1) * group;
     }
     if (begin >= end) return;
 
-    // Queries as A fragments.  Plain: element pairs 2c and 2c + 8 of every 16.  Codes: the lane's share
-    // of every 64 is 16c .. 16c + 15, four to a step.
     const int c = lane & 3, g = lane >> 2, D = p.layer.D;
-    uint32_t qf[DP / 16][4];
-#pragma unroll
-    for (int half = 0; half < 2; half++) {
-        const int64_t row = row0 + g + 8 * half;
-        const bool there = row < row_end;
-        const int64_t r = there ? quick_div(static_cast<uint32_t>(row), p.div_group) : 0;
-        const char *q = p.q + r * p.q_req + (h * group + (there ? row - r * group : 0)) * p.q_head;
-#pragma unroll
-        for (int ks = 0; ks < DP / 16; ks++) {
-            const int d0 = KIND == kPlain ? 16 * ks + 2 * c : 64 * (ks / 4) + 16 * c + 4 * (ks % 4);
-            const int d1 = KIND == kPlain ? d0 + 8 : d0 + 2;
-            qf[ks][half] = there && d0 < D ? *reinterpret_cast<const uint32_t *>(q + d0 * 2) : 0u;
-            qf[ks][half + 2] = there && d1 < D ? *reinterpret_cast<const uint32_t *>(q + d1 * 2) : 0u;
-        }
-    }
-
-    float o[DP / 8][4];
-#pragma unroll
-    for (int i = 0; i < DP / 8; i++) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
-    float top[2] = {-INFINITY, -INFINITY}, sum[2] = {0.f, 0.f};
-
     const uint32_t ring = static_cast<uint32_t>(__cvta_generic_to_shared(shared)) + warp * R::stages * R::stage;
     const int first = static_cast<int>(begin) + 16 * warp, last = static_cast<int>(end);
     const int tiles = first < last ? (last - first + 63) / 64 : 0;
 
+    const bool one_block = p.layer.B % 16 == 0;  // parts begin at multiples of 64 keys
     // the block that holds key `first + 64 * tile + (lane & 15)`; -1: not a key
     auto look_up = [&](int tile) -> int32_t {
         const int t = first + 64 * tile + (lane & 15);
@@ -279,15 +269,30 @@ __global__ void __launch_bounds__(128) parts_kernel(const __grid_constant__ Attn
         const int64_t off = block >= 0 ? p.layer.geo.at(block, n, h) : -1;
         const uint32_t mask = __ballot_sync(0xffffffffu, block >= 0);
         if (lane == 0) asm volatile("st.shared.u32 [%0], %1;" ::"r"(at + R::mask_at), "r"(mask) : "memory");
+        if (one_block) {
+            // 16 keys of one block: a fixed step from row to row
+            const int64_t base = __shfl_sync(0xffffffffu, off, 0);
+            const char *k = p.layer.k + base, *v = p.layer.v + base;
 #pragma unroll
-        for (int i = 0; i < 16 * R::chunks / 32; i++) {
-            const int idx = i * 32 + lane, r = idx / R::chunks, ch = idx % R::chunks;
-            const int64_t src = __shfl_sync(0xffffffffu, off, r);
-            const bool there = src >= 0 && ch * 16 < D * R::esize;
-            const int64_t from = there ? src + ch * 16 : 0;
-            const uint32_t to = at + place_of<KIND, DP>(r, ch);
-            copy_async16(to, p.layer.k + from, there);
-            copy_async16(to + R::plane, p.layer.v + from, there);
+            for (int i = 0; i < 16 * R::chunks / 32; i++) {
+                const int idx = i * 32 + lane, r = idx / R::chunks, ch = idx % R::chunks;
+                const bool there = mask >> r & 1 && ch * 16 < D * R::esize;
+                const int from = there ? r * p.layer.geo.token + ch * 16 : 0;
+                const uint32_t to = at + place_of<KIND, DP>(r, ch);
+                copy_async16(to, k + from, there);
+                copy_async16(to + R::plane, v + from, there);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 16 * R::chunks / 32; i++) {
+                const int idx = i * 32 + lane, r = idx / R::chunks, ch = idx % R::chunks;
+                const int64_t src = __shfl_sync(0xffffffffu, off, r);
+                const bool there = src >= 0 && ch * 16 < D * R::esize;
+                const int64_t from = there ? src + ch * 16 : 0;
+                const uint32_t to = at + place_of<KIND, DP>(r, ch);
+                copy_async16(to, p.layer.k + from, there);
+                copy_async16(to + R::plane, p.layer.v + from, there);
+            }
         }
         if constexpr (KIND != kPlain) {
             const int64_t from = block >= 0 ? p.layer.scale_geo.at(block, n, h) : 0;
@@ -303,6 +308,59 @@ __global__ void __launch_bounds__(128) parts_kernel(const __grid_constant__ Attn
         if (i < tiles) fill(i, b);
         copy_commit();
     }
+
+    // Queries as B fragments: column g, element pairs 2c and 2c + 8 of every 16; for codes the lane's share of every
+    // 64 is 16c .. 16c + 15, four to a step.  factor: of the scores of columns 2c and 2c + 1.
+    uint32_t qf[NB][DP / 16][2];
+    float factor[NB][2];
+#pragma unroll
+    for (int nb = 0; nb < NB; nb++) {
+        const int64_t row = row0 + 8 * nb + g;
+        const bool there = row < row_end;
+        const int64_t r = there ? quick_div(static_cast<uint32_t>(row), p.div_group) : 0;
+        const char *q = p.q + r * p.q_req + (h * group + (there ? row - r * group : 0)) * p.q_head;
+#pragma unroll
+        for (int ks = 0; ks < DP / 16; ks++) {
+            const int d0 = KIND == kPlain ? 16 * ks + 2 * c : 64 * (ks / 4) + 16 * c + 4 * (ks % 4);
+            const int d1 = KIND == kPlain ? d0 + 8 : d0 + 2;
+            qf[nb][ks][0] = there && d0 < D ? *reinterpret_cast<const uint32_t *>(q + d0 * 2) : 0u;
+            qf[nb][ks][1] = there && d1 < D ? *reinterpret_cast<const uint32_t *>(q + d1 * 2) : 0u;
+        }
+        factor[nb][0] = factor[nb][1] = p.scale_log2;
+        if constexpr (KIND != kPlain) {
+            float most = 0.f;  // of the finite ones
+#pragma unroll
+            for (int ks = 0; ks < DP / 16; ks++)
+#pragma unroll
+                for (int j = 0; j < 2; j++) {
+                    const float2 f = p.q_bf16 ? unpack2<__nv_bfloat16>(qf[nb][ks][j]) : unpack2<__half>(qf[nb][ks][j]);
+                    if (fabsf(f.x) < INFINITY) most = fmaxf(most, fabsf(f.x));
+                    if (fabsf(f.y) < INFINITY) most = fmaxf(most, fabsf(f.y));
+                }
+            most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 1));
+            most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 2));
+            const int e = most > 0.f ? max(static_cast<int>(__float_as_uint(most) >> 23) - 127, -100) : 14;
+            const float up = __uint_as_float(static_cast<uint32_t>(14 - e + 127) << 23), down = __uint_as_float(static_cast<uint32_t>(e - 14 + 127) << 23);
+#pragma unroll
+            for (int ks = 0; ks < DP / 16; ks++)
+#pragma unroll
+                for (int j = 0; j < 2; j++) {
+                    const float2 f = p.q_bf16 ? unpack2<__nv_bfloat16>(qf[nb][ks][j]) : unpack2<__half>(qf[nb][ks][j]);
+                    qf[nb][ks][j] = pack2<__half>(f.x * up, f.y * up);
+                }
+            factor[nb][0] = p.scale_log2 * __shfl_sync(0xffffffffu, down, 8 * c);
+            factor[nb][1] = p.scale_log2 * __shfl_sync(0xffffffffu, down, 8 * c + 4);
+        }
+    }
+
+    float o[NB][DP / 16][4], top[NB][2], sum[NB][2];
+#pragma unroll
+    for (int nb = 0; nb < NB; nb++) {
+#pragma unroll
+        for (int i = 0; i < DP / 16; i++) o[nb][i][0] = o[nb][i][1] = o[nb][i][2] = o[nb][i][3] = 0.f;
+        top[nb][0] = top[nb][1] = -INFINITY, sum[nb][0] = sum[nb][1] = 0.f;
+    }
+
     for (int i = 0; i < tiles; i++) {
         copy_wait<R::stages - 2>();
         __syncwarp();
@@ -310,86 +368,88 @@ __global__ void __launch_bounds__(128) parts_kernel(const __grid_constant__ Attn
         uint32_t mask;
         asm volatile("ld.shared.u32 %0, [%1];" : "=r"(mask) : "r"(at + R::mask_at));
 
-        float s[2][4] = {};
+        // s: keys g (0, 1) and g + 8 (2, 3) x columns 2c, 2c + 1
+        float s[NB][4] = {};
         if constexpr (KIND == kPlain) {
 #pragma unroll
             for (int ks = 0; ks < DP / 16; ks++) {
-                uint32_t b[4];
-                load_matrix4<false>(at + place_of<KIND, DP>(((lane >> 4) << 3) + (lane & 7), 2 * ks + ((lane >> 3) & 1)), b);
-                mma16816<T>(s[0], qf[ks], b[0], b[1]);
-                mma16816<T>(s[1], qf[ks], b[2], b[3]);
+                uint32_t a[4];
+                load_matrix4<false>(at + place_of<KIND, DP>(lane & 15, 2 * ks + (lane >> 4)), a);
+#pragma unroll
+                for (int nb = 0; nb < NB; nb++) mma16816<ST>(s[nb], a, qf[nb][ks][0], qf[nb][ks][1]);
             }
         } else {
 #pragma unroll
-            for (int k64 = 0; k64 < DP / 64; k64++)
+            for (int k64 = 0; k64 < DP / 64; k64++) {
+                const uint4 v = load_shared16(at + place_of<KIND, DP>(g, 4 * k64 + c)), w = load_shared16(at + place_of<KIND, DP>(g + 8, 4 * k64 + c));
+                const uint32_t lo[4] = {v.x, v.y, v.z, v.w}, hi[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
-                for (int nt = 0; nt < 2; nt++) {
-                    const uint4 v = load_shared16(at + place_of<KIND, DP>(8 * nt + g, 4 * k64 + c));
-                    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+                for (int j = 0; j < 4; j++) {
+                    uint32_t a[4];
+                    widen_half<KIND>(lo[j], a[0], a[2]);
+                    widen_half<KIND>(hi[j], a[1], a[3]);
 #pragma unroll
-                    for (int j = 0; j < 4; j++)
-                        mma16816<T>(s[nt], qf[4 * k64 + j], widen<KIND, T>(__byte_perm(w[j], 0, 0x4140)), widen<KIND, T>(__byte_perm(w[j], 0, 0x4342)));
+                    for (int nb = 0; nb < NB; nb++) mma16816<ST>(s[nb], a, qf[nb][4 * k64 + j][0], qf[nb][4 * k64 + j][1]);
                 }
+            }
         }
 
-        float2 vs[2];
-        float most[2] = {-INFINITY, -INFINITY};
+        float k_scale[2] = {1.f, 1.f}, v_scale[2] = {1.f, 1.f};
+        if constexpr (KIND != kPlain) {
 #pragma unroll
-        for (int nt = 0; nt < 2; nt++) {
-            float f0 = p.scale_log2, f1 = p.scale_log2;
-            if constexpr (KIND != kPlain) {
-                const float2 ks = load_shared_f2(at + R::scale_at + (8 * nt + 2 * c) * 4);
-                f0 *= ks.x, f1 *= ks.y;
-                vs[nt] = load_shared_f2(at + R::scale_at + 64 + (8 * nt + 2 * c) * 4);
-            }
-            const bool k0 = mask >> (8 * nt + 2 * c) & 1, k1 = mask >> (8 * nt + 2 * c + 1) & 1;
-#pragma unroll
-            for (int half = 0; half < 2; half++) {
-                s[nt][2 * half] = k0 ? s[nt][2 * half] * f0 : -INFINITY;
-                s[nt][2 * half + 1] = k1 ? s[nt][2 * half + 1] * f1 : -INFINITY;
-                most[half] = fmaxf(most[half], fmaxf(s[nt][2 * half], s[nt][2 * half + 1]));
+            for (int j = 0; j < 2; j++) {
+                asm volatile("ld.shared.f32 %0, [%1];" : "=f"(k_scale[j]) : "r"(at + R::scale_at + (g + 8 * j) * 4));
+                asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v_scale[j]) : "r"(at + R::scale_at + 64 + (g + 8 * j) * 4));
             }
         }
+        float most[NB][2];
+        bool move = false;
+        const bool key[2] = {(mask >> g & 1) != 0, (mask >> (g + 8) & 1) != 0};
 #pragma unroll
-        for (int half = 0; half < 2; half++) {
-            most[half] = fmaxf(most[half], __shfl_xor_sync(0xffffffffu, most[half], 1));
-            most[half] = fmaxf(most[half], __shfl_xor_sync(0xffffffffu, most[half], 2));
-        }
-        // The running maximum moves only when a tile exceeds it by more than 2^8: up to there the
-        // probabilities stay small enough for either 16-bit type, and the outputs need no rescaling.
-        const bool move = most[0] > top[0] + 8.f || most[1] > top[1] + 8.f;
+        for (int nb = 0; nb < NB; nb++)
+#pragma unroll
+            for (int j = 0; j < 2; j++) {
+                s[nb][j] = key[0] ? s[nb][j] * (KIND == kPlain ? factor[nb][j] : factor[nb][j] * k_scale[0]) : -INFINITY;
+                s[nb][j + 2] = key[1] ? s[nb][j + 2] * (KIND == kPlain ? factor[nb][j] : factor[nb][j] * k_scale[1]) : -INFINITY;
+                most[nb][j] = fmaxf(s[nb][j], s[nb][j + 2]);
+                move = move || most[nb][j] > top[nb][j] + 8.f;
+            }
+        // A running maximum moves only when a score exceeds it by more than 8 (2^8 in probabilities): up
+        // to there they stay small enough for either 16-bit type and the outputs need no rescaling.
         if (__any_sync(0xffffffffu, move)) {
-            float f[2];
 #pragma unroll
-            for (int half = 0; half < 2; half++) {
-                const float m = fmaxf(top[half], most[half]);
-                f[half] = m == top[half] ? 1.f : exp2_approx(top[half] - m);
-                top[half] = m;
-                sum[half] *= f[half];
+            for (int nb = 0; nb < NB; nb++) {
+                float f[2];
+#pragma unroll
+                for (int j = 0; j < 2; j++) {
+#pragma unroll
+                    for (int x = 4; x < 32; x <<= 1) most[nb][j] = fmaxf(most[nb][j], __shfl_xor_sync(0xffffffffu, most[nb][j], x));
+                    const float m = fmaxf(top[nb][j], most[nb][j]);
+                    f[j] = m == top[nb][j] ? 1.f : exp2_approx(top[nb][j] - m);
+                    top[nb][j] = m;
+                    sum[nb][j] *= f[j];
+                }
+#pragma unroll
+                for (int k = 0; k < DP / 16; k++) o[nb][k][0] *= f[0], o[nb][k][1] *= f[1], o[nb][k][2] *= f[0], o[nb][k][3] *= f[1];
             }
-#pragma unroll
-            for (int k = 0; k < DP / 8; k++) o[k][0] *= f[0], o[k][1] *= f[0], o[k][2] *= f[1], o[k][3] *= f[1];
         }
-        uint32_t pf[4];
+        uint32_t pf[NB][2];
 #pragma unroll
-        for (int half = 0; half < 2; half++) {
-            const float m = top[half] == -INFINITY ? 0.f : top[half];
-#pragma unroll
-            for (int nt = 0; nt < 2; nt++) {
-                float a = exp2_approx(s[nt][2 * half] - m), b = exp2_approx(s[nt][2 * half + 1] - m);
-                sum[half] += a + b;
-                if constexpr (KIND != kPlain) a *= vs[nt].x, b *= vs[nt].y;
-                pf[half + 2 * nt] = pack2<VT>(a, b);
-            }
+        for (int nb = 0; nb < NB; nb++) {
+            const float m0 = top[nb][0] == -INFINITY ? 0.f : top[nb][0], m1 = top[nb][1] == -INFINITY ? 0.f : top[nb][1];
+            const float e0 = exp2_approx(s[nb][0] - m0), e1 = exp2_approx(s[nb][1] - m1), e2 = exp2_approx(s[nb][2] - m0), e3 = exp2_approx(s[nb][3] - m1);
+            sum[nb][0] += e0 + e2, sum[nb][1] += e1 + e3;
+            pf[nb][0] = transposed(KIND == kPlain ? pack2<VT>(e0, e1) : pack2<VT>(e0 * v_scale[0], e1 * v_scale[0]));
+            pf[nb][1] = transposed(KIND == kPlain ? pack2<VT>(e2, e3) : pack2<VT>(e2 * v_scale[1], e3 * v_scale[1]));
         }
 
         if constexpr (KIND == kPlain) {
 #pragma unroll
             for (int k = 0; k < DP / 16; k++) {
-                uint32_t b[4];
-                load_matrix4<true>(at + R::plane + place_of<KIND, DP>((((lane >> 3) & 1) << 3) + (lane & 7), 2 * k + (lane >> 4)), b);
-                mma16816<VT>(o[2 * k], pf, b[0], b[1]);
-                mma16816<VT>(o[2 * k + 1], pf, b[2], b[3]);
+                uint32_t a[4];  // d's 16k .. + 7 and + 8 .., keys 0-7 and 8-15
+                load_matrix4<true>(at + R::plane + place_of<KIND, DP>((lane & 7) + ((lane >> 4) << 3), 2 * k + ((lane >> 3) & 1)), a);
+#pragma unroll
+                for (int nb = 0; nb < NB; nb++) mma16816<VT>(o[nb][k], a, pf[nb][0], pf[nb][1]);
             }
         } else {
             constexpr int bytes = DP >= 128 ? 16 : 8;  // codes a lane reads of each of its four keys
@@ -398,21 +458,21 @@ __global__ void __launch_bounds__(128) parts_kernel(const __grid_constant__ Attn
                 uint32_t w[4][bytes / 4];
 #pragma unroll
                 for (int k = 0; k < 4; k++) {
-                    const int key = 2 * c + (k & 1) + 8 * (k >> 1);
+                    const int kk = 2 * c + (k & 1) + 8 * (k >> 1);
                     if constexpr (bytes == 16) {
-                        const uint4 v = load_shared16(at + R::plane + place_of<KIND, DP>(key, 8 * u + g));
+                        const uint4 v = load_shared16(at + R::plane + place_of<KIND, DP>(kk, 8 * u + g));
                         w[k][0] = v.x, w[k][1] = v.y, w[k][2] = v.z, w[k][3] = v.w;
                     } else {
-                        const uint2 v = load_shared8(at + R::plane + place_of<KIND, DP>(key, g >> 1) + (g & 1) * 8);
+                        const uint2 v = load_shared8(at + R::plane + place_of<KIND, DP>(kk, g >> 1) + (g & 1) * 8);
                         w[k][0] = v.x, w[k][1] = v.y;
                     }
                 }
 #pragma unroll
-                for (int t = 0; t < bytes; t++) {
-                    // byte t of two keys, to bytes 0 and 2
-                    const uint32_t pick = (t & 3) | (4 + (t & 3)) << 8;
-                    mma16816<VT>(o[bytes * u + t], pf, widen<KIND, VT>(__byte_perm(w[0][t / 4], w[1][t / 4], pick)),
-                                 widen<KIND, VT>(__byte_perm(w[2][t / 4], w[3][t / 4], pick)));
+                for (int t = 0; t < bytes; t += 2) {
+                    const uint32_t a[4] = {widen_bf16<KIND>(w[0][t / 4], w[1][t / 4], t & 3), widen_bf16<KIND>(w[0][t / 4], w[1][t / 4], (t & 3) + 1),
+                                           widen_bf16<KIND>(w[2][t / 4], w[3][t / 4], t & 3), widen_bf16<KIND>(w[2][t / 4], w[3][t / 4], (t & 3) + 1)};
+#pragma unroll
+                    for (int nb = 0; nb < NB; nb++) mma16816<VT>(o[nb][(bytes * u + t) / 2], a, pf[nb][0], pf[nb][1]);
                 }
             }
         }
@@ -423,37 +483,36 @@ __global__ void __launch_bounds__(128) parts_kernel(const __grid_constant__ Attn
         copy_commit();
     }
     copy_wait<0>();
-#pragma unroll
-    for (int half = 0; half < 2; half++) {
-        sum[half] += __shfl_xor_sync(0xffffffffu, sum[half], 1);
-        sum[half] += __shfl_xor_sync(0xffffffffu, sum[half], 2);
-    }
 
     // Join the four warps: outputs and (maximum, sum) of each in shared memory.
     __syncthreads();
-    float *mine = reinterpret_cast<float *>(shared) + warp * 16 * (DP + 2);
+    float *mine = reinterpret_cast<float *>(shared) + warp * kCols * (DP + 2);
 #pragma unroll
-    for (int half = 0; half < 2; half++) {
-        float *row = mine + (g + 8 * half) * (DP + 2);
+    for (int nb = 0; nb < NB; nb++)
 #pragma unroll
-        for (int k = 0; k < DP / 8; k++)
+        for (int j = 0; j < 2; j++) {
 #pragma unroll
-            for (int j = 0; j < 2; j++) {
-                constexpr int bytes = DP >= 128 ? 16 : 8;
-                const int d = KIND == kPlain ? 8 * k + 2 * c + j : 8 * bytes * (k / bytes) + (2 * c + j) * bytes + k % bytes;
-                row[d] = o[k][2 * half + j];
-            }
-        if (c == 0) row[DP] = top[half], row[DP + 1] = sum[half];
-    }
+            for (int x = 4; x < 32; x <<= 1) sum[nb][j] += __shfl_xor_sync(0xffffffffu, sum[nb][j], x);
+            float *col = mine + (8 * nb + 2 * c + j) * (DP + 2);
+#pragma unroll
+            for (int k = 0; k < DP / 16; k++)
+#pragma unroll
+                for (int half = 0; half < 2; half++) {
+                    constexpr int bytes = DP >= 128 ? 16 : 8;
+                    const int d = KIND == kPlain ? 16 * k + g + 8 * half : 8 * bytes * (2 * k / bytes) + g * bytes + 2 * k % bytes + half;
+                    col[d] = o[nb][k][2 * half + j];
+                }
+            if (g == 0) col[DP] = top[nb][j], col[DP + 1] = sum[nb][j];
+        }
     __syncthreads();
-    for (int i = warp; i < 16; i += 4) {
+    for (int i = warp; i < kCols; i += 4) {
         const int64_t row = row0 + i;
         if (row >= row_end) break;
         const float *w[4];
         float m = -INFINITY, f[4], total = 0.f;
 #pragma unroll
         for (int k = 0; k < 4; k++) {
-            w[k] = reinterpret_cast<const float *>(shared) + (k * 16 + i) * (DP + 2);
+            w[k] = reinterpret_cast<const float *>(shared) + (k * kCols + i) * (DP + 2);
             m = fmaxf(m, w[k][DP]);
         }
 #pragma unroll
@@ -469,13 +528,16 @@ __global__ void __launch_bounds__(128) parts_kernel(const __grid_constant__ Attn
     }
 }
 
-// A warp per row: the parts' outputs, each by its share of the whole sum.
-template <typename T>
+// The parts' outputs, each by its share of the whole sum.  WARPS warps of a CTA take a row, each some of its
+// parts: one where there are few parts, four where one warp's chain of loads would be long.
+template <typename T, int WARPS>
 __global__ void __launch_bounds__(128) join_kernel(const __grid_constant__ AttnParams p)
 {
-    const int lane = threadIdx.x & 31, D = p.layer.D;
-    const int64_t row = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 5);
-    if (row >= p.split.rows) return;
+    constexpr int kAhead = 4;  // parts loaded at once
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, D = p.layer.D, share = warp % WARPS;
+    __shared__ float others[WARPS == 1 ? 1 : 4][WARPS == 1 ? 1 : 32 * 8 + 1];
+    const int64_t row = static_cast<int64_t>(blockIdx.x) * (4 / WARPS) + warp / WARPS;
+    if (row >= p.split.rows) return;  // WARPS > 1: a CTA is one row
     const int64_t r = row / p.Hq, head = row - r * p.Hq;
     int64_t len = p.lens[r];
     if (len < 0) return;
@@ -491,18 +553,44 @@ __global__ void __launch_bounds__(128) join_kernel(const __grid_constant__ AttnP
     for (int x = 16; x; x >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, x));
     const float base = m == -INFINITY ? 0.f : m;
     float acc[8] = {}, total = 0.f;
-    for (int i = 0; i < n; i++) {
-        const int64_t at = index(i);
-        const float w = exp2f(p.sums[at] - base);
-        if (w == 0.f) continue;  // also a part that has no keys: its outputs were not written
-        total += w;
-        const float *src = p.parts + at * D + lane * 4;
+    const int from = n * share / WARPS, to = n * (share + 1) / WARPS;
+    for (int i0 = from; i0 < to; i0 += 32) {
+        const int mine = i0 + lane;
+        const float weight = mine < to ? exp2f(p.sums[index(mine)] - base) : 0.f;
+        total += weight;
+        for (int j0 = 0; j0 < min(32, to - i0); j0 += kAhead) {
+            float w[kAhead];
+            float4 v[kAhead][2];
 #pragma unroll
-        for (int k = 0; k < 2; k++)
-            if (lane * 4 + 128 * k < D) {
-                const float4 v = *reinterpret_cast<const float4 *>(src + 128 * k);
-                acc[4 * k] += w * v.x, acc[4 * k + 1] += w * v.y, acc[4 * k + 2] += w * v.z, acc[4 * k + 3] += w * v.w;
+            for (int j = 0; j < kAhead; j++) {
+                w[j] = __shfl_sync(0xffffffffu, weight, j0 + j);  // 0 past the end and for a part without keys, whose outputs were not written
+#pragma unroll
+                for (int k = 0; k < 2; k++) {
+                    v[j][k] = make_float4(0.f, 0.f, 0.f, 0.f);
+                    if (w[j] != 0.f && lane * 4 + 128 * k < D) v[j][k] = *reinterpret_cast<const float4 *>(p.parts + index(i0 + j0 + j) * D + lane * 4 + 128 * k);
+                }
             }
+#pragma unroll
+            for (int j = 0; j < kAhead; j++)
+#pragma unroll
+                for (int k = 0; k < 2; k++)
+                    if (w[j] != 0.f) acc[4 * k] += w[j] * v[j][k].x, acc[4 * k + 1] += w[j] * v[j][k].y, acc[4 * k + 2] += w[j] * v[j][k].z, acc[4 * k + 3] += w[j] * v[j][k].w;
+        }
+    }
+#pragma unroll
+    for (int x = 16; x; x >>= 1) total += __shfl_xor_sync(0xffffffffu, total, x);
+    if constexpr (WARPS > 1) {
+#pragma unroll
+        for (int k = 0; k < 8; k++) others[warp][k * 32 + lane] = acc[k];
+        if (lane == 0) others[warp][256] = total;
+        __syncthreads();
+        if (warp) return;
+#pragma unroll
+        for (int w = 1; w < WARPS; w++) {
+#pragma unroll
+            for (int k = 0; k < 8; k++) acc[k] += others[w][k * 32 + lane];
+            total += others[w][256];
+        }
     }
     const float inv = total == 0.f ? 0.f : 1.f / total;
     char *dst = p.out + r * p.out_req + head * p.out_head;
@@ -514,27 +602,33 @@ __global__ void __launch_bounds__(128) join_kernel(const __grid_constant__ AttnP
 }
 
 // --------------------------------------------------------------------------------------- launching
-template <typename T, int KIND, int DP>
+template <typename T, int KIND, int DP, int NB>
 static int launch_parts(const AttnParams &p, unsigned grid, int device, cudaStream_t s)
 {
-    using R = Ring<KIND, DP>;
+    using R = Ring<KIND, DP, NB>;
     static bool raised[kMaxDevices];  // set once per device; setting it twice does no harm
     if (!raised[device]) {
-        const cudaError_t e = cudaFuncSetAttribute(parts_kernel<T, KIND, DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, R::bytes);
+        const cudaError_t e = cudaFuncSetAttribute(parts_kernel<T, KIND, DP, NB>, cudaFuncAttributeMaxDynamicSharedMemorySize, R::bytes);
         if (e != cudaSuccess) return cuda_fail(e, "cudaFuncSetAttribute(dynamic shared memory)");
         raised[device] = true;
     }
-    parts_kernel<T, KIND, DP><<<grid, 128, R::bytes, s>>>(p);
+    parts_kernel<T, KIND, DP, NB><<<grid, 128, R::bytes, s>>>(p);
     const cudaError_t e = cudaGetLastError();
     return e == cudaSuccess ? TC_OK : cuda_fail(e, "kernel launch");
 }
 
-template <typename T, int KIND>
+template <typename T, int KIND, int NB>
 static int launch_parts_for(const AttnParams &p, unsigned grid, int device, cudaStream_t s)
 {
-    if (p.layer.D <= 64) return launch_parts<T, KIND, 64>(p, grid, device, s);
-    if (p.layer.D <= 128) return launch_parts<T, KIND, 128>(p, grid, device, s);
-    return launch_parts<T, KIND, 256>(p, grid, device, s);
+    if (p.layer.D <= 64) return launch_parts<T, KIND, 64, NB>(p, grid, device, s);
+    if (p.layer.D <= 128) return launch_parts<T, KIND, 128, NB>(p, grid, device, s);
+    return launch_parts<T, KIND, 256, NB>(p, grid, device, s);
+}
+
+template <typename T, int KIND>
+static int launch_parts_columns(const AttnParams &p, unsigned grid, int device, cudaStream_t s)
+{
+    return p.split.columns == 8 ? launch_parts_for<T, KIND, 1>(p, grid, device, s) : launch_parts_for<T, KIND, 2>(p, grid, device, s);
 }
 
 template <typename T>
@@ -547,13 +641,14 @@ static int launch_decode(const AttnParams &p, int device, cudaStream_t s)
     if (ctas) {
         const unsigned grid = static_cast<unsigned>(ctas);
         switch (p.layer.dtype) {
-        case TC_E4M3: rc = launch_parts_for<T, kE4m3>(p, grid, device, s); break;
-        case TC_INT8: rc = launch_parts_for<T, kInt8>(p, grid, device, s); break;
-        default: rc = launch_parts_for<T, kPlain>(p, grid, device, s); break;
+        case TC_E4M3: rc = launch_parts_columns<__half, kE4m3>(p, grid, device, s); break;
+        case TC_INT8: rc = launch_parts_columns<__half, kInt8>(p, grid, device, s); break;
+        default: rc = launch_parts_columns<T, kPlain>(p, grid, device, s); break;
         }
         if (rc != TC_OK) return rc;
     }
-    join_kernel<T><<<static_cast<unsigned>((p.split.rows + 3) / 4), 128, 0, s>>>(p);
+    if (p.split.prefix_parts + p.split.own_parts > 8) join_kernel<T, 4><<<static_cast<unsigned>(p.split.rows), 128, 0, s>>>(p);
+    else join_kernel<T, 1><<<static_cast<unsigned>((p.split.rows + 3) / 4), 128, 0, s>>>(p);
     const cudaError_t e = cudaGetLastError();
     return e == cudaSuccess ? TC_OK : cuda_fail(e, "kernel launch");
 }
@@ -642,6 +737,7 @@ extern "C" int tc_attn_decode(const tc_kv_layer_t *layer, const tc_attn_decode_t
     p.lens = a->lens, p.prefix_table = a->prefix_table, p.prefix_len = a->prefix_len;
     p.R = a->R, p.max_len = a->max_len, p.max_prefix = a->max_prefix;
     p.Hq = static_cast<int32_t>(a->Hq);
+    p.q_bf16 = a->dtype == TC_BF16;
     p.scale_log2 = static_cast<float>((a->scale != 0.f ? static_cast<double>(a->scale) : 1.0 / std::sqrt(static_cast<double>(p.layer.D))) * 1.4426950408889634);
     p.div_block = make_fastdiv(p.layer.B);
     p.div_group = make_fastdiv(static_cast<uint32_t>(p.split.group));

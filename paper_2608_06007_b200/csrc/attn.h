@@ -5,20 +5,22 @@
 
 namespace tc {
 
-// The keys of a row of queries are cut into parts; every part leaves a normalised output and the base-2
-// logarithm of its sum in the workspace, and a last kernel joins them.
+// Every part of a row's keys leaves a normalised output and the base-2 logarithm of its sum in the workspace; a
+// last kernel joins them.
 struct AttnSplit {
     int32_t group;             // query heads per KV head
-    int32_t prefix_rows;       // rows of queries one prefix CTA takes: 16 (parts_kernel, `columns`), 128 or 256 (prefix_kernel;
-                               // 128: two parts per chunk of keys, one a slot)
-    int32_t prefix_blocks;     // such blocks of the R * group rows of one KV head
-    int32_t columns;           // rows a CTA of parts_kernel takes: 8, or 16 for groups of more than 8
+    int32_t columns;           // rows an item of the stream has: 8, or 16 for groups of more than 8
     int32_t own_blocks;        // blocks of `columns` of a request's group rows
-    int64_t prefix_chunk, own_chunk;  // keys per part
-    int32_t prefix_parts, own_parts;
+    int32_t prefix_rows;       // rows of queries one prefix CTA takes: 128 (two parts per chunk of keys, one a slot) or
+                               // 256; 16: the prefix is part of the stream
+    int32_t prefix_blocks;     // blocks of that many (of `columns`) of the R * group rows of one KV head
+    int32_t prefix_parts;      // parts that prefix_kernel leaves of every row
+    int32_t stream_ctas;       // of four warps each
+    int32_t whole_parts;       // prefix_parts, the own keys' part, and that of a prefix in the stream
+    int64_t prefix_chunk;      // keys per part of prefix_kernel
     int64_t rows;              // R * Hq
-    int64_t sum_bytes;         // workspace: [parts][rows] logarithms, then [parts][rows][D] outputs
-    int64_t workspace;
+    int64_t workspace;         // bytes; in it: [whole_parts][rows] sums and [..][D] outputs, [warps][2][columns] sums
+    int64_t sums_at, parts_at, piece_sums_at, pieces_at, before_at;  // and [..][D] outputs of pieces, [R + 2] tiles before a request
 };
 
 struct AttnParams {
@@ -36,7 +38,8 @@ struct AttnParams {
     float scale_log2;  // scale * log2(e)
     FastDiv div_block, div_group;
     AttnSplit split;
-    float *sums, *parts;
+    float *sums, *parts, *piece_sums, *pieces;
+    int64_t *before;
     unsigned int *status;
 };
 

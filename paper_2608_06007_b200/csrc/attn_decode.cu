@@ -1,8 +1,8 @@
 // tc_attn_decode: one query token per request over a shared prefix and the request's own pages.
 //
-// The keys are cut into parts.  A part's kernel leaves, for each of its rows (request, head), the
-// softmax-weighted mean of its values and log2 of its sum; join_kernel weighs the parts against one
-// another.  Softmax statistics, scores and outputs are fp32 throughout; only the probabilities are
+// The keys of a row (request, head) are cut into parts, each of which leaves the softmax-weighted mean of its
+// values and log2 of its sum in the workspace; join_kernel weighs the parts against one another.
+// prefix_kernel (attn_prefix.cu) takes a prefix that many rows share, stream_kernel all other keys.  Softmax statistics, scores and outputs are fp32 throughout; only the probabilities are
 // rounded, to 16 bits, to enter the second matrix product (half a step of 2^-8 or 2^-11 relative to
 // each, no worse than the rounding of the values and of the output to those types).
 #include <algorithm>
@@ -13,7 +13,16 @@
 
 namespace tc {
 
+constexpr int kLeastShare = 4;  // tiles of 16 keys that a warp of the stream takes at least
 constexpr int kSms = 148;  // B200; the workspace must not depend on the device that happens to be current
+
+// CTAs of stream_kernel that one SM holds: by shared memory (three stages a warp) and registers.
+static int stream_ctas(bool quantised, int64_t D, int columns)
+{
+    if (D > 128) return 1 + (quantised && columns == 8);
+    if (D > 64) return quantised && columns == 8 ? 4 : 2;
+    return 4;
+}
 
 void split_attn(int64_t R, int64_t Hq, int64_t H, int64_t D, int64_t max_len, int64_t max_prefix, bool quantised, AttnSplit *s)
 {
@@ -22,34 +31,17 @@ void split_attn(int64_t R, int64_t Hq, int64_t H, int64_t D, int64_t max_len, in
     s->rows = R * Hq;
     s->columns = s->group <= 8 ? 8 : 16;
     s->own_blocks = (s->group + s->columns - 1) / s->columns;
-    auto cut = [&](int64_t keys, int64_t ctas, int64_t want, int64_t longest, int64_t *chunk, int32_t *parts) {
-        if (keys <= 0) {
-            *chunk = 64, *parts = 0;
-            return;
-        }
-        const int64_t tiles = (keys + 63) / 64;
-        const int64_t n = std::max<int64_t>(1, std::min<int64_t>(tiles, want / std::max<int64_t>(ctas, 1)));
-        int64_t c = std::min((tiles + n - 1) / n * 64, longest);
-        // at most 256 MB of parts
-        while (c < tiles * 64 && ((keys + c - 1) / c) * s->rows * (D + 1) * 4 > (256ll << 20)) c *= 2;
-        *chunk = c;
-        *parts = static_cast<int32_t>((keys + c - 1) / c);
-    };
-    // Own tokens: about six CTAs per SM where there are few requests; at most 1024 keys a part, so that
-    // one long request among short ones is not one CTA's work.
-    cut(max_len, R * H * s->own_blocks, 6 * kSms, 1024, &s->own_chunk, &s->own_parts);
     const int64_t rows = R * s->group;  // of one KV head
     s->prefix_rows = max_prefix == 0 || rows <= 16 || D > 128 || quantised ? 16 : rows <= 128 ? 128 : 256;
     const int64_t block = s->prefix_rows == 16 ? s->columns : s->prefix_rows;
     s->prefix_blocks = static_cast<int32_t>((rows + block - 1) / block);
-    if (s->prefix_rows == 16) {
-        cut(max_prefix, H * s->prefix_blocks, 6 * kSms, 1 << 20, &s->prefix_chunk, &s->prefix_parts);
-    } else {
+    s->prefix_chunk = 128;
+    if (s->prefix_rows > 16) {
         // One CTA per SM: the number of parts that leaves the fewest tiles to the busiest SM, a part costing
-        // about two tiles to start and end.
-        const int64_t tiles = (max_prefix + 127) / 128, ctas = H * s->prefix_blocks;
+        // about two tiles to start and end.  At most 64 parts, and 256 MB of them.
+        const int64_t tiles = (max_prefix + 127) / 128, ctas = H * s->prefix_blocks, most = std::max<int64_t>(1, (128ll << 20) / (s->rows * (D + 1) * 4));
         int64_t best = 1, best_cost = INT64_MAX;
-        for (int64_t n = 1; n <= std::min<int64_t>(tiles, 64); n++) {
+        for (int64_t n = 1; n <= std::min<int64_t>({tiles, 64, most}); n++) {
             const int64_t per = (tiles + n - 1) / n, cost = (ctas * ((tiles + per - 1) / per) + kSms - 1) / kSms * (per + 2);
             if (cost < best_cost) best = n, best_cost = cost;
         }
@@ -57,9 +49,23 @@ void split_attn(int64_t R, int64_t Hq, int64_t H, int64_t D, int64_t max_len, in
         s->prefix_chunk = per * 128;
         s->prefix_parts = static_cast<int32_t>((tiles + per - 1) / per) * (s->prefix_rows == 128 ? 2 : 1);
     }
-    const int64_t parts = static_cast<int64_t>(s->own_parts) + s->prefix_parts;
-    s->sum_bytes = (parts * s->rows * 4 + 255) / 256 * 256;
-    s->workspace = s->sum_bytes + parts * s->rows * D * 4;
+    // The stream's warps: what the GPU holds at once, fewer where not even the longest batch would
+    // give each its least share.
+    const int64_t stream_tiles = R * H * s->own_blocks * ((max_len + 15) / 16) + (s->prefix_rows == 16 ? H * s->prefix_blocks * ((max_prefix + 15) / 16) : 0);
+    const int64_t ctas = std::min<int64_t>(static_cast<int64_t>(kSms) * stream_ctas(quantised, D, s->columns), (stream_tiles + kLeastShare - 1) / kLeastShare);
+    s->stream_ctas = static_cast<int32_t>(ctas);
+    const int64_t whole = s->prefix_parts + (max_len > 0) + (max_prefix > 0 && s->prefix_rows == 16), pieces = ctas * 4 * 2 * s->columns;
+    auto place = [&](int64_t bytes) {
+        const int64_t at = s->workspace;
+        s->workspace += (bytes + 255) / 256 * 256;
+        return at;
+    };
+    s->whole_parts = static_cast<int32_t>(whole);
+    s->sums_at = place(whole * s->rows * 4);
+    s->parts_at = place(whole * s->rows * D * 4);
+    s->piece_sums_at = place(pieces * 4);
+    s->pieces_at = place(pieces * D * 4);
+    s->before_at = place(ctas ? (R + 2) * 8 : 0);
 }
 
 // ------------------------------------------------------------------------------- device helpers
@@ -68,24 +74,6 @@ __device__ __forceinline__ void load_matrix4(uint32_t addr, uint32_t (&r)[4])
 {
     if constexpr (TRANS) asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr));
     else asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr));
-}
-__device__ __forceinline__ uint4 load_shared16(uint32_t addr)
-{
-    uint4 v;
-    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr));
-    return v;
-}
-__device__ __forceinline__ uint2 load_shared8(uint32_t addr)
-{
-    uint2 v;
-    asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(addr));
-    return v;
-}
-__device__ __forceinline__ float2 load_shared_f2(uint32_t addr)
-{
-    float2 v;
-    asm volatile("ld.shared.v2.f32 {%0,%1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(addr));
-    return v;
 }
 
 // c (16 x 8) += a (16 x 16) * b (16 x 8), fp32 sums
@@ -101,51 +89,55 @@ template <> __device__ __forceinline__ void mma16816<__nv_bfloat16>(float (&c)[4
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-// ------------------------------------------------------------------------------ the parts' kernel
-// One warp works alone on tiles of 16 keys; four warps of a CTA share a part and join at its end.
-// The keys are the rows of the matrix products, S' = K Q' and O' = V' P' on m16n8k16: the columns are
-// the query heads of one KV head (or rows of the batch, for a prefix with few of them), 8 or 16 at
-// a time, so few heads leave little of a product idle, and every staged byte of K and V is used once
-// per block of columns.  Bound by HBM.  S' comes out with a key's scores along a lane quad; packed
-// to 16 bits its 8 x 8 blocks are transposed into the second product's operand by movmatrix.
-// A warp has its own ring of stages, filled by 16-byte asynchronous copies whatever the size of
-// the pages, and waits for no other warp until the end.
+// ---------------------------------------------------------------------------------- the stream
+// All tiles of 16 keys - of every request, KV head and block of columns in turn, then of a prefix that
+// few rows share - are one sequence, of which every warp of the grid takes an equal stretch, whatever
+// the lengths.  It has its own ring of stages, filled by 16-byte asynchronous copies whatever the size
+// of the pages, and works alone: the copies run ahead across the ends of items, so that short
+// requests cost no gaps.  An item that is one warp's leaves a whole part, one that is cut leaves pieces,
+// at most two a warp.  Bound by HBM.
 //
-// Codes of a quantised pool are staged as they are and become 16-bit numbers on the way into the
-// fragments, exactly: K in fp16, V in bf16.  The scales multiply the scores and the probabilities; a
-// probability times a scale needs bf16's range.  Queries of such a pool are fp16 with a power of two
+// The keys are the rows of the matrix products, S' = K Q' and O' = V' P' on m16n8k16: the columns are
+// the query heads of one KV head (or rows of the batch, for the prefix), 8 or 16 at a time, so few
+// heads leave little of a product idle, and every staged byte of K and V is used once per block of
+// columns.  S' comes out with a key's scores along a lane quad; packed to 16 bits its 8 x 8 blocks are
+// transposed into the second product's operand by movmatrix.
+//
+// Codes of a quantised pool are staged as they are and become fp16 on the way into the fragments,
+// exactly.  ldmatrix hands a lane four codes of one key's row (K), its 8-bit transpose four keys' codes of
+// one d (V); which key is which row of S' is chosen so that both products agree on the order of the keys.
+// The key's scale multiplies the scores.  The value's goes into the exponent, w = exp2(s + log2 v_scale
+// - top), so that fp16 probabilities have the largest contribution as their reference whatever the scales
+// are; the sum takes w / v_scale, which is exp2(s - top).  Queries of such a pool are fp16 with a power of two
 // per row taken out, so that the row's largest is in [2^14, 2^15): what is then below fp16's smallest
-// step is below 2^-38 of that largest.  A lane reads 16 consecutive codes at once, so the order of the d's
-// inside the products is a permutation: the queries use the same one, the outputs undo it.
+// step is below 2^-38 of that largest.
 enum { kPlain = 0, kE4m3 = 1, kInt8 = 2 };
 
-template <int KIND, int DP, int NB>
+template <int KIND, int DP>
 struct Ring {
     static constexpr int esize = KIND == kPlain ? 2 : 1;
     static constexpr int row = DP * esize, chunks = row / 16;  // bytes and 16-byte chunks of a key
-    static constexpr int plane = 16 * row;
-    static constexpr int scale_at = 2 * plane, mask_at = scale_at + (KIND == kPlain ? 0 : 128);
-    static constexpr int stage = mask_at + 16;
+    static constexpr int plane = 16 * row, tile = 2 * plane;   // K, then V
+    static constexpr int head = KIND == kPlain ? 16 : 144;     // {mask and flags, request, item}, then 16 scales of K and of V
     static constexpr int stages = 3;  // D = 128: two CTAs an SM for 16-bit pools, four for codes
-    static constexpr int join = 4 * 8 * NB * (DP + 2) * 4;  // the warps' outputs and statistics at the end
-    static constexpr int bytes = 4 * stages * stage > join ? 4 * stages * stage : join;
+    static constexpr int bytes = 4 * stages * (tile + head);
+    static constexpr int copies = 16 * chunks / 32, rows_per_copy = 32 / chunks;  // of a plane, by a warp
 };
 
-// Where chunk c of key r of a tile is staged: no two of the lanes that one shared-memory pass serves
-// meet in a bank, for ldmatrix (eight keys, one chunk) and for the code reads (two keys x four chunks of
-// K; keys 0 2 4 6 or their successors x two chunks of V).
+// Where chunk c of key r of a tile is staged: no two of the rows that one shared-memory pass serves meet in a
+// bank - eight keys in order (16-bit), keys 0 1 4 5 8 9 12 13 or their successors but one (codes).
 template <int KIND, int DP>
 __device__ __forceinline__ int place_of(int r, int c)
 {
     constexpr int row = DP * (KIND == kPlain ? 2 : 1);
     if constexpr (KIND == kPlain) return r * row + ((c ^ (r & 7)) << 4);
-    else if constexpr (DP >= 128) return r * row + ((c ^ ((((r ^ (r >> 2)) & 1) << 2) | (r & 2))) << 4);
-    else return r * row + ((c ^ ((r >> 1) & 2)) << 4);
+    else if constexpr (DP >= 128) return r * row + ((c ^ (((r >> 2) << 1 | (r & 1)) & 7)) << 4);
+    else return r * row + ((c ^ (r >> 2 & 3)) << 4);
 }
 
-// Four codes w as two pairs of fp16 numbers, exactly.
+// Four codes as two pairs of fp16 numbers, exactly.
 template <int KIND>
-__device__ __forceinline__ void widen_half(uint32_t w, uint32_t &lo, uint32_t &hi)
+__device__ __forceinline__ void widen(uint32_t w, uint32_t &lo, uint32_t &hi)
 {
     if constexpr (KIND == kE4m3) {
         lo = e4m3_to_half2(w), hi = e4m3_to_half2(w >> 16);
@@ -158,24 +150,10 @@ __device__ __forceinline__ void widen_half(uint32_t w, uint32_t &lo, uint32_t &h
         lo = *reinterpret_cast<const uint32_t *>(&x), hi = *reinterpret_cast<const uint32_t *>(&y);
     }
 }
-// The codes in byte t of v and w as a pair of bf16 numbers, exactly.
-template <int KIND>
-__device__ __forceinline__ uint32_t widen_bf16(uint32_t v, uint32_t w, int t)
+// 16 keys x 32 d's of 8 bits, transposed: r[0], r[1]: d's g and g + 8, keys 4c .. 4c + 3; r[2], r[3]: 16 d's on.
+__device__ __forceinline__ void load_codes_transposed(uint32_t addr, uint32_t (&r)[4])
 {
-    __nv_bfloat162 r;
-    if constexpr (KIND == kE4m3) {
-        // Sign, exponent and fraction bits in place are the value times 2^-120 (subnormals too); the product
-        // with 2^120 is exact.  (Codes 0x7f and 0xff, e4m3's NaN, would be +-480; a quantised row has none.)
-        const uint32_t x = __byte_perm(v, w, (t << 4) | ((4 + t) << 12));
-        const uint32_t y = (x & 0x80008000u) | ((x >> 4) & 0x07f007f0u), big = 0x7b807b80u;
-        r = __hmul2(*reinterpret_cast<const __nv_bfloat162 *>(&y), *reinterpret_cast<const __nv_bfloat162 *>(&big));
-    } else {
-        // 128 + the low seven bits, less 128 or (sign bit set) 256: all bf16 numbers
-        const uint32_t x = __byte_perm(v, w, t | ((4 + t) << 8));
-        const uint32_t a = (x & 0x007f007fu) | 0x43004300u, b = (x & 0x00800080u) | 0x43004300u;
-        r = __hsub2(*reinterpret_cast<const __nv_bfloat162 *>(&a), *reinterpret_cast<const __nv_bfloat162 *>(&b));
-    }
-    return *reinterpret_cast<const uint32_t *>(&r);
+    asm volatile("ldmatrix.sync.aligned.m16n16.x2.trans.shared.b8 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr));
 }
 
 __device__ __forceinline__ uint32_t transposed(uint32_t v)
@@ -185,188 +163,277 @@ __device__ __forceinline__ uint32_t transposed(uint32_t v)
     return r;
 }
 
-// T: the type of the products - the queries' for a plain pool; quantised pools have one kernel (fp16 scores,
-// bf16 values) and look at p.q_bf16.
-template <typename T, int KIND, int DP, int NB>
-__global__ void __launch_bounds__(128) parts_kernel(const __grid_constant__ AttnParams p)
+// Length of a request (r < R) or of the prefix (r == R; 0 where prefix_kernel takes it), in keys.
+__device__ __forceinline__ int stream_length(const AttnParams &p, int64_t r, bool tell)
 {
-    using R = Ring<KIND, DP, NB>;
+    const int64_t most = r < p.R ? p.max_len : p.max_prefix;
+    if (most == 0 || (r == p.R && p.split.prefix_rows != 16)) return 0;
+    int64_t len = r < p.R ? p.lens[r] : *p.prefix_len;
+    if (tell && (len > most || (r == p.R && len < 0))) atomicOr(p.status, kStatusBadIndex);
+    return static_cast<int>(min(max(len, int64_t(0)), most));
+}
+__device__ __forceinline__ int stream_items(const AttnParams &p, int64_t r) { return p.layer.H * (r < p.R ? p.split.own_blocks : p.split.prefix_blocks); }
+// Warps that share `total` tiles, and the first tile of warp w.
+__device__ __forceinline__ int64_t stream_warps(const AttnParams &p, int64_t total) { return min(static_cast<int64_t>(p.split.stream_ctas) * 4, (total + kLeastShare - 1) / kLeastShare); }
+__device__ __forceinline__ int64_t stream_begin(int64_t w, int64_t warps, int64_t total) { return w * total / warps; }
+__device__ __forceinline__ int64_t stream_owner(int64_t tile, int64_t warps, int64_t total) { return ((tile + 1) * warps - 1) / total; }
+
+enum : uint32_t { kFirst = 1u << 16, kLast = 1u << 17, kWhole = 1u << 18, kSecond = 1u << 19 };
+
+// T: the type of the products - the queries' for a plain pool, fp16 for a quantised one, which looks at p.q_bf16.
+template <typename T, int KIND, int DP, int NB>
+__global__ void __launch_bounds__(128, KIND != kPlain && DP <= 128 && NB == 1 ? 4 : 2) stream_kernel(const __grid_constant__ AttnParams p)
+{
+    using R = Ring<KIND, DP>;
     using ST = std::conditional_t<KIND == kPlain, T, __half>;
-    using VT = std::conditional_t<KIND == kPlain, T, __nv_bfloat16>;
+    using VT = ST;
     constexpr int kCols = 8 * NB;
     extern __shared__ __align__(128) unsigned char shared[];
+    __shared__ int64_t sums_of[4], start_at[4], start_off[4];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int H = p.layer.H, group = p.split.group;
+    const int group = p.split.group;
 
-    // Which part: [begin, end) of the keys behind `table`, for rows row0 .. of KV head h.
-    const int64_t prefix_ctas = p.split.prefix_rows == 16 ? static_cast<int64_t>(p.split.prefix_parts) * H * p.split.prefix_blocks : 0;
-    int64_t id = blockIdx.x, begin, end, row0, row_end, part, table_width;
-    int h;
-    const int32_t *table;
-    const bool prefix = id < prefix_ctas;
-    if (prefix) {
-        const int64_t block = id % p.split.prefix_blocks;
-        id /= p.split.prefix_blocks;
-        h = static_cast<int>(id % H);
-        part = id / H;
-        begin = part * p.split.prefix_chunk;
-        int64_t len = *p.prefix_len;
-        if (len > p.max_prefix || len < 0) {
-            if (threadIdx.x == 0) atomicOr(p.status, kStatusBadIndex);
-            len = len < 0 ? 0 : p.max_prefix;
-        }
-        end = min(begin + p.split.prefix_chunk, len);
-        table = p.prefix_table;
-        table_width = INT32_MAX;
-        row0 = block * kCols;
-        row_end = p.R * group;
-    } else {
-        id -= prefix_ctas;
-        const int64_t block = id % p.split.own_blocks;
-        id /= p.split.own_blocks;
-        h = static_cast<int>(id % H);
-        id /= H;
-        const int64_t r = id % p.R;
-        part = id / p.R;
-        begin = part * p.split.own_chunk;
-        int64_t len = p.lens[r];
-        if (len > p.max_len) {
-            if (threadIdx.x == 0) atomicOr(p.status, kStatusBadIndex);
-            len = p.max_len;
-        }
-        end = min(begin + p.split.own_chunk, len);
-        part += p.split.prefix_parts;
-        table = reinterpret_cast<const int32_t *>(p.tables + r * p.table_stride);
-        table_width = p.table_width;
-        row0 = r * group + block * kCols;
-        row_end = (r + 1) * group;
+    // Every CTA adds the tiles of all requests up, each thread over a run of them, and finds where its warps
+    // begin; CTA 0 also leaves the sums for join_kernel.
+    const int64_t per = (p.R + 1 + 127) / 128, mine0 = threadIdx.x * per, mine1 = min(mine0 + per, p.R + 1);
+    int64_t my_tiles = 0;
+    for (int64_t r = mine0; r < mine1; r++) my_tiles += static_cast<int64_t>((stream_length(p, r, blockIdx.x == 0) + 15) >> 4) * stream_items(p, r);
+    int64_t upto = my_tiles;
+#pragma unroll
+    for (int x = 1; x < 32; x <<= 1) {
+        const int64_t v = __shfl_up_sync(0xffffffffu, upto, x);
+        if (lane >= x) upto += v;
     }
-    if (begin >= end) return;
+    if (lane == 31) sums_of[warp] = upto;
+    __syncthreads();
+    int64_t total = 0;
+#pragma unroll
+    for (int w = 0; w < 4; w++) {
+        if (w < warp) upto += sums_of[w];
+        total += sums_of[w];
+    }
+    int64_t before = upto - my_tiles;
+    const int64_t warps = stream_warps(p, total), index = static_cast<int64_t>(warp) * gridDim.x + blockIdx.x;
+#pragma unroll
+    for (int w = 0; w < 4; w++) {
+        const int64_t i = static_cast<int64_t>(w) * gridDim.x + blockIdx.x;
+        if (i >= warps) break;
+        int64_t from = stream_begin(i, warps, total), at = before;
+        if (from < before || from >= upto) continue;
+        for (int64_t r = mine0; r < mine1; r++) {
+            const int64_t n = static_cast<int64_t>((stream_length(p, r, false) + 15) >> 4) * stream_items(p, r);
+            if (from < at + n) {
+                start_at[w] = r, start_off[w] = from - at;
+                break;
+            }
+            at += n;
+        }
+    }
+    if (blockIdx.x == 0) {
+        for (int64_t r = mine0; r < mine1; r++) {
+            p.before[r] = before;
+            before += static_cast<int64_t>((stream_length(p, r, false) + 15) >> 4) * stream_items(p, r);
+        }
+        if (threadIdx.x == 0) p.before[p.R + 1] = total;
+    }
+    __syncthreads();
+    if (index >= warps) return;
+    const int todo = static_cast<int>(stream_begin(index + 1, warps, total) - stream_begin(index, warps, total));
 
     const int c = lane & 3, g = lane >> 2, D = p.layer.D;
-    const uint32_t ring = static_cast<uint32_t>(__cvta_generic_to_shared(shared)) + warp * R::stages * R::stage;
-    const int first = static_cast<int>(begin) + 16 * warp, last = static_cast<int>(end);
-    const int tiles = first < last ? (last - first + 63) / 64 : 0;
+    const uint32_t ring = static_cast<uint32_t>(__cvta_generic_to_shared(shared)) + warp * R::stages * R::tile;
+    const uint32_t heads = static_cast<uint32_t>(__cvta_generic_to_shared(shared)) + 4 * R::stages * R::tile + warp * R::stages * R::head;
+    const bool one_block = p.layer.B % 16 == 0;  // a tile's keys lie in one block
 
-    const bool one_block = p.layer.B % 16 == 0;  // parts begin at multiples of 64 keys
-    // the block that holds key `first + 64 * tile + (lane & 15)`; -1: not a key
-    auto look_up = [&](int tile) -> int32_t {
-        const int t = first + 64 * tile + (lane & 15);
-        if (tile >= tiles || t >= last) return -1;
+    // The next tile to be copied: tile `l_tile` of `l_tiles` of item `l_item` of request l_r.
+    int64_t l_r = start_at[warp];
+    int l_len = stream_length(p, l_r, false), l_tiles = (l_len + 15) >> 4;
+    int l_item = static_cast<int>(start_off[warp] / l_tiles), l_tile = static_cast<int>(start_off[warp] - static_cast<int64_t>(l_item) * l_tiles);
+    const int32_t *l_table = l_r < p.R ? reinterpret_cast<const int32_t *>(p.tables + l_r * p.table_stride) : p.prefix_table;
+    auto head_of = [&](int64_t r, int item) {
+        const int blocks = r < p.R ? p.split.own_blocks : p.split.prefix_blocks;
+        return blocks == 1 ? item : item / blocks;
+    };
+    bool l_first = true, l_from_start = l_tile == 0, l_second = false;
+    int l_left = todo;
+    // this lane's rows and chunk of every copy
+    const int my_row = lane / R::chunks, my_chunk = lane % R::chunks;
+    const bool in_row = my_chunk * 16 < D * R::esize;
+    int spot[R::copies];
+#pragma unroll
+    for (int i = 0; i < R::copies; i++) spot[i] = place_of<KIND, DP>(i * R::rows_per_copy + my_row, my_chunk);
+    const int64_t v_from_k = p.layer.v - p.layer.k, copy_step = static_cast<int64_t>(R::rows_per_copy) * p.layer.geo.token;
+    // the block that holds key 16 * l_tile + (lane & 15); -1: not a key
+    auto look_up = [&]() -> int32_t {
+        const int t = 16 * l_tile + (lane & 15);
+        if (l_left <= 0 || t >= l_len) return -1;
         const uint32_t entry = quick_div(static_cast<uint32_t>(t), p.div_block);
         int32_t b = -1;
-        if (entry < table_width) b = table[entry];
+        if (l_r == p.R || entry < p.table_width) b = l_table[entry];
         if (b < 0 || b >= p.layer.num_blocks) {
             atomicOr(p.status, kStatusBadIndex);
             return -1;
         }
         return b;
     };
-    auto fill = [&](int tile, int32_t block) {
-        const uint32_t at = ring + (tile % R::stages) * R::stage;
-        const int t = first + 64 * tile + (lane & 15);
+    // Copies the next tile to stage `to`, its keys' blocks given, and steps on.
+    auto fill = [&](int to, int32_t block) {
+        const uint32_t at = ring + to * R::tile, head = heads + to * R::head;
+        const int t = 16 * l_tile + (lane & 15);
         const int n = t - static_cast<int>(quick_div(static_cast<uint32_t>(t), p.div_block)) * static_cast<int>(p.layer.B);
-        const int64_t off = block >= 0 ? p.layer.geo.at(block, n, h) : -1;
-        const uint32_t mask = __ballot_sync(0xffffffffu, block >= 0);
-        if (lane == 0) asm volatile("st.shared.u32 [%0], %1;" ::"r"(at + R::mask_at), "r"(mask) : "memory");
+        const int h = head_of(l_r, l_item);
+        const uint32_t mask = __ballot_sync(0xffffffffu, block >= 0) & 0xffffu;
+        const bool end = l_tile + 1 == l_tiles, last = end || l_left == 1;
+        if (lane == 0)
+            asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(head),
+                         "r"(mask | (l_first ? kFirst : 0u) | (last ? kLast : 0u) | (last && end && l_from_start ? kWhole : 0u) | (l_second ? kSecond : 0u)), "r"(static_cast<uint32_t>(l_r)), "r"(l_item), "r"(0)
+                         : "memory");
         if (one_block) {
-            // 16 keys of one block: a fixed step from row to row
-            const int64_t base = __shfl_sync(0xffffffffu, off, 0);
-            const char *k = p.layer.k + base, *v = p.layer.v + base;
+            // a fixed step from key to key
+            const int n0 = __shfl_sync(0xffffffffu, n, 0), b0 = __shfl_sync(0xffffffffu, block, 0);
+            const char *k = p.layer.k + p.layer.geo.at(max(b0, 0), n0 + my_row, h) + my_chunk * 16;
+            const uint32_t rows = in_row ? mask >> my_row : 0u;
 #pragma unroll
-            for (int i = 0; i < 16 * R::chunks / 32; i++) {
-                const int idx = i * 32 + lane, r = idx / R::chunks, ch = idx % R::chunks;
-                const bool there = mask >> r & 1 && ch * 16 < D * R::esize;
-                const int from = there ? r * p.layer.geo.token + ch * 16 : 0;
-                const uint32_t to = at + place_of<KIND, DP>(r, ch);
-                copy_async16(to, k + from, there);
-                copy_async16(to + R::plane, v + from, there);
+            for (int i = 0; i < R::copies; i++, k += copy_step) {
+                const bool there = rows >> (i * R::rows_per_copy) & 1;
+                copy_async16(at + spot[i], k, there);  // where it is not there, nothing is read
+                copy_async16(at + spot[i] + R::plane, k + v_from_k, there);
             }
         } else {
+            const int64_t off = block >= 0 ? p.layer.geo.at(block, n, h) : -1;
 #pragma unroll
-            for (int i = 0; i < 16 * R::chunks / 32; i++) {
-                const int idx = i * 32 + lane, r = idx / R::chunks, ch = idx % R::chunks;
-                const int64_t src = __shfl_sync(0xffffffffu, off, r);
-                const bool there = src >= 0 && ch * 16 < D * R::esize;
-                const int64_t from = there ? src + ch * 16 : 0;
-                const uint32_t to = at + place_of<KIND, DP>(r, ch);
-                copy_async16(to, p.layer.k + from, there);
-                copy_async16(to + R::plane, p.layer.v + from, there);
+            for (int i = 0; i < R::copies; i++) {
+                const int64_t src = __shfl_sync(0xffffffffu, off, i * R::rows_per_copy + my_row);
+                const bool there = src >= 0 && in_row;
+                const char *k = p.layer.k + (there ? src + my_chunk * 16 : 0);
+                copy_async16(at + spot[i], k, there);
+                copy_async16(at + spot[i] + R::plane, k + v_from_k, there);
             }
         }
         if constexpr (KIND != kPlain) {
             const int64_t from = block >= 0 ? p.layer.scale_geo.at(block, n, h) : 0;
-            copy_async4(at + R::scale_at + lane * 4, reinterpret_cast<const char *>(lane < 16 ? p.layer.k_scale : p.layer.v_scale) + from, block >= 0);
+            copy_async4(head + 16 + lane * 4, reinterpret_cast<const char *>(lane < 16 ? p.layer.k_scale : p.layer.v_scale) + from, block >= 0);
+        }
+        l_left--;
+        l_first = last;
+        l_tile++;
+        if (end) {
+            l_tile = 0, l_from_start = true, l_second = true;
+            if (++l_item == stream_items(p, l_r) && l_left > 0) {
+                // the next request that has keys; `l_left` says that there is one
+                l_item = 0;
+                for (int64_t base = l_r + 1; base <= p.R; base += 32) {
+                    const int len = base + lane <= p.R ? stream_length(p, base + lane, false) : 0;
+                    const uint32_t some = __ballot_sync(0xffffffffu, len > 0);
+                    if (!some) continue;
+                    const int at_lane = __ffs(some) - 1;
+                    l_r = base + at_lane;
+                    l_len = __shfl_sync(0xffffffffu, len, at_lane);
+                    break;
+                }
+                l_tiles = (l_len + 15) >> 4;
+                l_table = l_r < p.R ? reinterpret_cast<const int32_t *>(p.tables + l_r * p.table_stride) : p.prefix_table;
+            }
         }
     };
 
-    int32_t ahead = look_up(0);
+    int32_t ahead = look_up();
 #pragma unroll
     for (int i = 0; i < R::stages - 1; i++) {
-        const int32_t b = ahead;
-        ahead = look_up(i + 1);
-        if (i < tiles) fill(i, b);
+        if (i < todo) {
+            fill(i, ahead);
+            ahead = look_up();
+        }
         copy_commit();
     }
 
-    // Queries as B fragments: column g, element pairs 2c and 2c + 8 of every 16; for codes the lane's share of every
-    // 64 is 16c .. 16c + 15, four to a step.  factor: of the scores of columns 2c and 2c + 1.
+    // Rows of an item: columns 0 .. row_end - row0 of KV head h.
+    struct Item {
+        int64_t row0, row_end;
+        int h;
+    };
+    auto item_of = [&](int64_t r, int item) {
+        Item it;
+        const int blocks = r < p.R ? p.split.own_blocks : p.split.prefix_blocks;
+        it.h = head_of(r, item);
+        const int block = item - it.h * blocks;
+        it.row0 = (r < p.R ? r * group : 0) + block * kCols;
+        it.row_end = (r < p.R ? r + 1 : p.R) * group;
+        return it;
+    };
+    // Queries as B fragments: column g, element pairs 2c and 2c + 8 of every 16; for codes 4c and 4c + 2.  factor: of the scores of columns 2c and 2c + 1.
     uint32_t qf[NB][DP / 16][2];
     float factor[NB][2];
+    auto load_queries = [&](int64_t r, int item, uint32_t (&q)[NB][DP / 16][2]) {
+        const Item it = item_of(r, item);
 #pragma unroll
-    for (int nb = 0; nb < NB; nb++) {
-        const int64_t row = row0 + 8 * nb + g;
-        const bool there = row < row_end;
-        const int64_t r = there ? quick_div(static_cast<uint32_t>(row), p.div_group) : 0;
-        const char *q = p.q + r * p.q_req + (h * group + (there ? row - r * group : 0)) * p.q_head;
+        for (int nb = 0; nb < NB; nb++) {
+            const int64_t row = it.row0 + 8 * nb + g;
+            const bool there = row < it.row_end;
+            const int64_t req = there ? quick_div(static_cast<uint32_t>(row), p.div_group) : 0;
+            const char *src = p.q + req * p.q_req + (it.h * group + (there ? row - req * group : 0)) * p.q_head;
 #pragma unroll
-        for (int ks = 0; ks < DP / 16; ks++) {
-            const int d0 = KIND == kPlain ? 16 * ks + 2 * c : 64 * (ks / 4) + 16 * c + 4 * (ks % 4);
-            const int d1 = KIND == kPlain ? d0 + 8 : d0 + 2;
-            qf[nb][ks][0] = there && d0 < D ? *reinterpret_cast<const uint32_t *>(q + d0 * 2) : 0u;
-            qf[nb][ks][1] = there && d1 < D ? *reinterpret_cast<const uint32_t *>(q + d1 * 2) : 0u;
+            for (int ks = 0; ks < DP / 16; ks++) {
+                const int d0 = 16 * ks + (KIND == kPlain ? 2 : 4) * c;
+                const int d1 = KIND == kPlain ? d0 + 8 : d0 + 2;
+                q[nb][ks][0] = there && d0 < D ? *reinterpret_cast<const uint32_t *>(src + d0 * 2) : 0u;
+                q[nb][ks][1] = there && d1 < D ? *reinterpret_cast<const uint32_t *>(src + d1 * 2) : 0u;
+            }
         }
-        factor[nb][0] = factor[nb][1] = p.scale_log2;
-        if constexpr (KIND != kPlain) {
-            float most = 0.f;  // of the finite ones
+    };
+    auto take_queries = [&]() {
 #pragma unroll
-            for (int ks = 0; ks < DP / 16; ks++)
+        for (int nb = 0; nb < NB; nb++) {
+            factor[nb][0] = factor[nb][1] = p.scale_log2;
+            if constexpr (KIND != kPlain) {
+                float most = 0.f;  // of the finite ones
 #pragma unroll
-                for (int j = 0; j < 2; j++) {
-                    const float2 f = p.q_bf16 ? unpack2<__nv_bfloat16>(qf[nb][ks][j]) : unpack2<__half>(qf[nb][ks][j]);
-                    if (fabsf(f.x) < INFINITY) most = fmaxf(most, fabsf(f.x));
-                    if (fabsf(f.y) < INFINITY) most = fmaxf(most, fabsf(f.y));
-                }
-            most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 1));
-            most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 2));
-            const int e = most > 0.f ? max(static_cast<int>(__float_as_uint(most) >> 23) - 127, -100) : 14;
-            const float up = __uint_as_float(static_cast<uint32_t>(14 - e + 127) << 23), down = __uint_as_float(static_cast<uint32_t>(e - 14 + 127) << 23);
+                for (int ks = 0; ks < DP / 16; ks++)
 #pragma unroll
-            for (int ks = 0; ks < DP / 16; ks++)
+                    for (int j = 0; j < 2; j++) {
+                        const float2 f = p.q_bf16 ? unpack2<__nv_bfloat16>(qf[nb][ks][j]) : unpack2<__half>(qf[nb][ks][j]);
+                        if (fabsf(f.x) < INFINITY) most = fmaxf(most, fabsf(f.x));
+                        if (fabsf(f.y) < INFINITY) most = fmaxf(most, fabsf(f.y));
+                    }
+                most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 1));
+                most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 2));
+                const int e = most > 0.f ? max(static_cast<int>(__float_as_uint(most) >> 23) - 127, -100) : 14;
+                const float up = __uint_as_float(static_cast<uint32_t>(14 - e + 127) << 23), down = __uint_as_float(static_cast<uint32_t>(e - 14 + 127) << 23);
 #pragma unroll
-                for (int j = 0; j < 2; j++) {
-                    const float2 f = p.q_bf16 ? unpack2<__nv_bfloat16>(qf[nb][ks][j]) : unpack2<__half>(qf[nb][ks][j]);
-                    qf[nb][ks][j] = pack2<__half>(f.x * up, f.y * up);
-                }
-            factor[nb][0] = p.scale_log2 * __shfl_sync(0xffffffffu, down, 8 * c);
-            factor[nb][1] = p.scale_log2 * __shfl_sync(0xffffffffu, down, 8 * c + 4);
+                for (int ks = 0; ks < DP / 16; ks++)
+#pragma unroll
+                    for (int j = 0; j < 2; j++) {
+                        const float2 f = p.q_bf16 ? unpack2<__nv_bfloat16>(qf[nb][ks][j]) : unpack2<__half>(qf[nb][ks][j]);
+                        qf[nb][ks][j] = pack2<__half>(f.x * up, f.y * up);
+                    }
+                factor[nb][0] = p.scale_log2 * __shfl_sync(0xffffffffu, down, 8 * c);
+                factor[nb][1] = p.scale_log2 * __shfl_sync(0xffffffffu, down, 8 * c + 4);
+            }
         }
-    }
+    };
+    load_queries(start_at[warp], static_cast<int>(start_off[warp] / ((stream_length(p, start_at[warp], false) + 15) >> 4)), qf);
 
     float o[NB][DP / 16][4], top[NB][2], sum[NB][2];
-#pragma unroll
-    for (int nb = 0; nb < NB; nb++) {
-#pragma unroll
-        for (int i = 0; i < DP / 16; i++) o[nb][i][0] = o[nb][i][1] = o[nb][i][2] = o[nb][i][3] = 0.f;
-        top[nb][0] = top[nb][1] = -INFINITY, sum[nb][0] = sum[nb][1] = 0.f;
-    }
-
-    for (int i = 0; i < tiles; i++) {
+    float largest = 0.f;  // codes: the largest scale of V so far
+    // this lane's keys of a tile, rows g and g + 8 of S'
+    const int key0 = KIND == kPlain ? g : 4 * (g >> 1) + (g & 1), key1 = KIND == kPlain ? g + 8 : key0 + 2;
+    int stage = 0, next_fill = R::stages - 1;
+    for (int i = 0; i < todo; i++) {
         copy_wait<R::stages - 2>();
         __syncwarp();
-        const uint32_t at = ring + (i % R::stages) * R::stage;
-        uint32_t mask;
-        asm volatile("ld.shared.u32 %0, [%1];" : "=r"(mask) : "r"(at + R::mask_at));
+        const uint32_t at = ring + stage * R::tile, head_at = heads + stage * R::head;
+        uint32_t head, head_r, head_item, unused;
+        asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(head), "=r"(head_r), "=r"(head_item), "=r"(unused) : "r"(head_at));
+        if (head & kFirst) {
+            take_queries();
+            largest = 7.888609052e-31f;  // 2^-100
+#pragma unroll
+            for (int nb = 0; nb < NB; nb++) {
+#pragma unroll
+                for (int k = 0; k < DP / 16; k++) o[nb][k][0] = o[nb][k][1] = o[nb][k][2] = o[nb][k][3] = 0.f;
+                top[nb][0] = top[nb][1] = -INFINITY, sum[nb][0] = sum[nb][1] = 0.f;
+            }
+        }
 
         // s: keys g (0, 1) and g + 8 (2, 3) x columns 2c, 2c + 1
         float s[NB][4] = {};
@@ -379,38 +446,57 @@ __global__ void __launch_bounds__(128) parts_kernel(const __grid_constant__ Attn
                 for (int nb = 0; nb < NB; nb++) mma16816<ST>(s[nb], a, qf[nb][ks][0], qf[nb][ks][1]);
             }
         } else {
+            const int i = lane & 7, key = 4 * (i >> 1) + (i & 1) + ((lane >> 2) & 2);
 #pragma unroll
-            for (int k64 = 0; k64 < DP / 64; k64++) {
-                const uint4 v = load_shared16(at + place_of<KIND, DP>(g, 4 * k64 + c)), w = load_shared16(at + place_of<KIND, DP>(g + 8, 4 * k64 + c));
-                const uint32_t lo[4] = {v.x, v.y, v.z, v.w}, hi[4] = {w.x, w.y, w.z, w.w};
+            for (int ks = 0; ks < DP / 16; ks += 2) {
+                uint32_t w[4];  // chunk ks: rows g and g + 8; chunk ks + 1
+                load_matrix4<false>(at + place_of<KIND, DP>(key, ks + (lane >> 4)), w);
 #pragma unroll
-                for (int j = 0; j < 4; j++) {
+                for (int j = 0; j < 2; j++) {
                     uint32_t a[4];
-                    widen_half<KIND>(lo[j], a[0], a[2]);
-                    widen_half<KIND>(hi[j], a[1], a[3]);
+                    widen<KIND>(w[2 * j], a[0], a[2]);
+                    widen<KIND>(w[2 * j + 1], a[1], a[3]);
 #pragma unroll
-                    for (int nb = 0; nb < NB; nb++) mma16816<ST>(s[nb], a, qf[nb][4 * k64 + j][0], qf[nb][4 * k64 + j][1]);
+                    for (int nb = 0; nb < NB; nb++) mma16816<ST>(s[nb], a, qf[nb][ks + j][0], qf[nb][ks + j][1]);
                 }
             }
         }
+        // An item's last scores are taken: its queries make room for the next one's, loaded while this tile ends.
+        if ((head & kLast) && i + 1 < todo) {
+            const uint32_t next = heads + (stage + 1 == R::stages ? 0 : stage + 1) * R::head;
+            uint32_t flags, r, item, none;
+            asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(flags), "=r"(r), "=r"(item), "=r"(none) : "r"(next));
+            load_queries(r, static_cast<int>(item), qf);
+        }
 
-        float k_scale[2] = {1.f, 1.f}, v_scale[2] = {1.f, 1.f};
+        float k_scale[2] = {1.f, 1.f}, v_log[2] = {0.f, 0.f}, v_inverse[2] = {1.f, 1.f};
         if constexpr (KIND != kPlain) {
+            float v[2];
 #pragma unroll
             for (int j = 0; j < 2; j++) {
-                asm volatile("ld.shared.f32 %0, [%1];" : "=f"(k_scale[j]) : "r"(at + R::scale_at + (g + 8 * j) * 4));
-                asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v_scale[j]) : "r"(at + R::scale_at + 64 + (g + 8 * j) * 4));
+                asm volatile("ld.shared.f32 %0, [%1];" : "=f"(k_scale[j]) : "r"(head_at + 16 + (j ? key1 : key0) * 4));
+                asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v[j]) : "r"(head_at + 80 + (j ? key1 : key0) * 4));
+            }
+            float here = fmaxf(v[0], v[1]);
+#pragma unroll
+            for (int x = 4; x < 32; x <<= 1) here = fmaxf(here, __shfl_xor_sync(0xffffffffu, here, x));
+            largest = fmaxf(largest, here);
+#pragma unroll
+            for (int j = 0; j < 2; j++) {
+                if (v[j] == 0.f) v[j] = largest;  // a row of zeros: its codes are 0 whatever the scale
+                v_log[j] = __log2f(v[j]);
+                v_inverse[j] = __fdividef(1.f, v[j]);
             }
         }
         float most[NB][2];
         bool move = false;
-        const bool key[2] = {(mask >> g & 1) != 0, (mask >> (g + 8) & 1) != 0};
+        const bool key[2] = {(head >> key0 & 1) != 0, (head >> key1 & 1) != 0};
 #pragma unroll
         for (int nb = 0; nb < NB; nb++)
 #pragma unroll
             for (int j = 0; j < 2; j++) {
-                s[nb][j] = key[0] ? s[nb][j] * (KIND == kPlain ? factor[nb][j] : factor[nb][j] * k_scale[0]) : -INFINITY;
-                s[nb][j + 2] = key[1] ? s[nb][j + 2] * (KIND == kPlain ? factor[nb][j] : factor[nb][j] * k_scale[1]) : -INFINITY;
+                s[nb][j] = key[0] ? (KIND == kPlain ? s[nb][j] * factor[nb][j] : fmaf(s[nb][j], factor[nb][j] * k_scale[0], v_log[0])) : -INFINITY;
+                s[nb][j + 2] = key[1] ? (KIND == kPlain ? s[nb][j + 2] * factor[nb][j] : fmaf(s[nb][j + 2], factor[nb][j] * k_scale[1], v_log[1])) : -INFINITY;
                 most[nb][j] = fmaxf(s[nb][j], s[nb][j + 2]);
                 move = move || most[nb][j] > top[nb][j] + 8.f;
             }
@@ -438,9 +524,10 @@ __global__ void __launch_bounds__(128) parts_kernel(const __grid_constant__ Attn
         for (int nb = 0; nb < NB; nb++) {
             const float m0 = top[nb][0] == -INFINITY ? 0.f : top[nb][0], m1 = top[nb][1] == -INFINITY ? 0.f : top[nb][1];
             const float e0 = exp2_approx(s[nb][0] - m0), e1 = exp2_approx(s[nb][1] - m1), e2 = exp2_approx(s[nb][2] - m0), e3 = exp2_approx(s[nb][3] - m1);
-            sum[nb][0] += e0 + e2, sum[nb][1] += e1 + e3;
-            pf[nb][0] = transposed(KIND == kPlain ? pack2<VT>(e0, e1) : pack2<VT>(e0 * v_scale[0], e1 * v_scale[0]));
-            pf[nb][1] = transposed(KIND == kPlain ? pack2<VT>(e2, e3) : pack2<VT>(e2 * v_scale[1], e3 * v_scale[1]));
+            if constexpr (KIND == kPlain) sum[nb][0] += e0 + e2, sum[nb][1] += e1 + e3;
+            else sum[nb][0] = fmaf(e0, v_inverse[0], fmaf(e2, v_inverse[1], sum[nb][0])), sum[nb][1] = fmaf(e1, v_inverse[0], fmaf(e3, v_inverse[1], sum[nb][1]));
+            pf[nb][0] = transposed(pack2<VT>(e0, e1));
+            pf[nb][1] = transposed(pack2<VT>(e2, e3));
         }
 
         if constexpr (KIND == kPlain) {
@@ -452,80 +539,59 @@ __global__ void __launch_bounds__(128) parts_kernel(const __grid_constant__ Attn
                 for (int nb = 0; nb < NB; nb++) mma16816<VT>(o[nb][k], a, pf[nb][0], pf[nb][1]);
             }
         } else {
-            constexpr int bytes = DP >= 128 ? 16 : 8;  // codes a lane reads of each of its four keys
 #pragma unroll
-            for (int u = 0; u < DP / (8 * bytes); u++) {
-                uint32_t w[4][bytes / 4];
+            for (int k = 0; k < DP / 16; k += 2) {
+                uint32_t w[4];
+                load_codes_transposed(at + R::plane + place_of<KIND, DP>(lane & 15, k + (lane >> 4)), w);
 #pragma unroll
-                for (int k = 0; k < 4; k++) {
-                    const int kk = 2 * c + (k & 1) + 8 * (k >> 1);
-                    if constexpr (bytes == 16) {
-                        const uint4 v = load_shared16(at + R::plane + place_of<KIND, DP>(kk, 8 * u + g));
-                        w[k][0] = v.x, w[k][1] = v.y, w[k][2] = v.z, w[k][3] = v.w;
-                    } else {
-                        const uint2 v = load_shared8(at + R::plane + place_of<KIND, DP>(kk, g >> 1) + (g & 1) * 8);
-                        w[k][0] = v.x, w[k][1] = v.y;
-                    }
-                }
+                for (int j = 0; j < 2; j++) {
+                    uint32_t a[4];
+                    widen<KIND>(w[2 * j], a[0], a[2]);
+                    widen<KIND>(w[2 * j + 1], a[1], a[3]);
 #pragma unroll
-                for (int t = 0; t < bytes; t += 2) {
-                    const uint32_t a[4] = {widen_bf16<KIND>(w[0][t / 4], w[1][t / 4], t & 3), widen_bf16<KIND>(w[0][t / 4], w[1][t / 4], (t & 3) + 1),
-                                           widen_bf16<KIND>(w[2][t / 4], w[3][t / 4], t & 3), widen_bf16<KIND>(w[2][t / 4], w[3][t / 4], (t & 3) + 1)};
-#pragma unroll
-                    for (int nb = 0; nb < NB; nb++) mma16816<VT>(o[nb][(bytes * u + t) / 2], a, pf[nb][0], pf[nb][1]);
+                    for (int nb = 0; nb < NB; nb++) mma16816<VT>(o[nb][k + j], a, pf[nb][0], pf[nb][1]);
                 }
             }
         }
         __syncwarp();
-        const int32_t b = ahead;
-        ahead = look_up(i + R::stages);
-        if (i + R::stages - 1 < tiles) fill(i + R::stages - 1, b);
+        if (l_left > 0) {
+            fill(next_fill, ahead);
+            ahead = look_up();
+        }
         copy_commit();
+        next_fill = next_fill + 1 == R::stages ? 0 : next_fill + 1;
+        stage = stage + 1 == R::stages ? 0 : stage + 1;
+
+        if (head & kLast) {
+            // The item's part of the keys: a whole part, or one of this warp's two pieces.
+            const Item it = item_of(head_r, static_cast<int>(head_item));
+            const bool whole = head & kWhole;
+            const int64_t slot = p.split.whole_parts - 1 - (head_r < p.R && p.max_prefix > 0 && p.split.prefix_rows == 16);  // own keys, then the prefix
+            const int64_t piece = (index * 2 + (head & kSecond ? 1 : 0)) * kCols;
+#pragma unroll
+            for (int nb = 0; nb < NB; nb++)
+#pragma unroll
+                for (int j = 0; j < 2; j++) {
+                    float all = sum[nb][j];
+#pragma unroll
+                    for (int x = 4; x < 32; x <<= 1) all += __shfl_xor_sync(0xffffffffu, all, x);
+                    const int col = 8 * nb + 2 * c + j;
+                    const int64_t row = it.row0 + col;
+                    if (row >= it.row_end) continue;
+                    const int64_t req = quick_div(static_cast<uint32_t>(row), p.div_group);
+                    const int64_t where = whole ? slot * p.split.rows + req * p.Hq + it.h * group + (row - req * group) : piece + col;
+                    float *dst = (whole ? p.parts : p.pieces) + where * D;
+                    const float inv = all == 0.f ? 0.f : 1.f / all;
+#pragma unroll
+                    for (int k = 0; k < DP / 16; k++)
+#pragma unroll
+                        for (int half = 0; half < 2; half++)
+                            if (16 * k < D) dst[16 * k + g + 8 * half] = o[nb][k][2 * half + j] * inv;
+                    if (g == 0) (whole ? p.sums : p.piece_sums)[where] = all == 0.f ? -INFINITY : (top[nb][j] == -INFINITY ? 0.f : top[nb][j]) + log2f(all);
+                }
+        }
     }
     copy_wait<0>();
-
-    // Join the four warps: outputs and (maximum, sum) of each in shared memory.
-    __syncthreads();
-    float *mine = reinterpret_cast<float *>(shared) + warp * kCols * (DP + 2);
-#pragma unroll
-    for (int nb = 0; nb < NB; nb++)
-#pragma unroll
-        for (int j = 0; j < 2; j++) {
-#pragma unroll
-            for (int x = 4; x < 32; x <<= 1) sum[nb][j] += __shfl_xor_sync(0xffffffffu, sum[nb][j], x);
-            float *col = mine + (8 * nb + 2 * c + j) * (DP + 2);
-#pragma unroll
-            for (int k = 0; k < DP / 16; k++)
-#pragma unroll
-                for (int half = 0; half < 2; half++) {
-                    constexpr int bytes = DP >= 128 ? 16 : 8;
-                    const int d = KIND == kPlain ? 16 * k + g + 8 * half : 8 * bytes * (2 * k / bytes) + g * bytes + 2 * k % bytes + half;
-                    col[d] = o[nb][k][2 * half + j];
-                }
-            if (g == 0) col[DP] = top[nb][j], col[DP + 1] = sum[nb][j];
-        }
-    __syncthreads();
-    for (int i = warp; i < kCols; i += 4) {
-        const int64_t row = row0 + i;
-        if (row >= row_end) break;
-        const float *w[4];
-        float m = -INFINITY, f[4], total = 0.f;
-#pragma unroll
-        for (int k = 0; k < 4; k++) {
-            w[k] = reinterpret_cast<const float *>(shared) + (k * kCols + i) * (DP + 2);
-            m = fmaxf(m, w[k][DP]);
-        }
-#pragma unroll
-        for (int k = 0; k < 4; k++) {
-            f[k] = w[k][DP] == -INFINITY && w[k][DP + 1] == 0.f ? 0.f : exp2f(w[k][DP] - m);
-            total += f[k] * w[k][DP + 1];
-        }
-        const int64_t r = quick_div(static_cast<uint32_t>(row), p.div_group);
-        const int64_t at = part * p.split.rows + r * p.Hq + h * group + (row - r * group);
-        const float inv = total == 0.f ? 0.f : 1.f / total;
-        for (int d = lane; d < D; d += 32) p.parts[at * D + d] = (f[0] * w[0][d] + f[1] * w[1][d] + f[2] * w[2][d] + f[3] * w[3][d]) * inv;
-        if (lane == 0) p.sums[at] = total == 0.f ? -INFINITY : (m == -INFINITY ? 0.f : m) + log2f(total);
-    }
 }
 
 // The parts' outputs, each by its share of the whole sum.  WARPS warps of a CTA take a row, each some of its
@@ -538,17 +604,59 @@ __global__ void __launch_bounds__(128) join_kernel(const __grid_constant__ AttnP
     __shared__ float others[WARPS == 1 ? 1 : 4][WARPS == 1 ? 1 : 32 * 8 + 1];
     const int64_t row = static_cast<int64_t>(blockIdx.x) * (4 / WARPS) + warp / WARPS;
     if (row >= p.split.rows) return;  // WARPS > 1: a CTA is one row
-    const int64_t r = row / p.Hq, head = row - r * p.Hq;
-    int64_t len = p.lens[r];
-    if (len < 0) return;
-    len = min(len, p.max_len);
-    const int64_t shared_len = p.split.prefix_parts ? min(max(static_cast<int64_t>(*p.prefix_len), int64_t(0)), p.max_prefix) : 0;
-    const int front = static_cast<int>((shared_len + p.split.prefix_chunk - 1) / p.split.prefix_chunk) * (p.split.prefix_rows == 128 ? 2 : 1);
-    const int back = static_cast<int>((len + p.split.own_chunk - 1) / p.split.own_chunk);
-    const int n = front + back;
-    auto index = [&](int i) -> int64_t { return static_cast<int64_t>(i < front ? i : p.split.prefix_parts + i - front) * p.split.rows + row; };
+    const int64_t r = row / p.Hq;
+    const int head = static_cast<int>(row - r * p.Hq), h = head / p.split.group, in_group = head - h * p.split.group;
+    if (p.lens[r] < 0) return;
+    // Sources: prefix_kernel's parts, then what the stream left of the request's own keys and of the prefix.
+    int front = 0;
+    if (p.split.prefix_rows > 16) {
+        const int64_t len = min(max(static_cast<int64_t>(*p.prefix_len), int64_t(0)), p.max_prefix);
+        front = static_cast<int>((len + p.split.prefix_chunk - 1) / p.split.prefix_chunk) * (p.split.prefix_rows == 128 ? 2 : 1);
+    }
+    int count[2] = {0, 0};
+    int64_t from_whole[2] = {0, 0}, from_piece[2] = {0, 0};  // rows of `parts`, or of `pieces` (from_whole < 0)
+    int64_t step_piece[2] = {0, 0};
+    if (p.split.stream_ctas > 0) {
+        const int64_t total = p.before[p.R + 1], warps = total ? stream_warps(p, total) : 1;
+#pragma unroll
+        for (int k = 0; k < 2; k++) {
+            const int64_t q = k ? p.R : r;
+            const int tiles = (stream_length(p, q, false) + 15) >> 4;
+            if (!tiles) continue;
+            const int64_t in_q = k ? r * p.split.group + in_group : in_group;
+            const int block = static_cast<int>(in_q / p.split.columns), col = static_cast<int>(in_q - static_cast<int64_t>(block) * p.split.columns);
+            const int64_t first = p.before[q] + (static_cast<int64_t>(h) * (k ? p.split.prefix_blocks : p.split.own_blocks) + block) * tiles;
+            const int64_t w0 = stream_owner(first, warps, total), w1 = stream_owner(first + tiles - 1, warps, total);
+            count[k] = static_cast<int>(w1 - w0 + 1);
+            from_whole[k] = -1;
+            if (w0 == w1) from_whole[k] = (p.split.whole_parts - 1 - (k == 0 && p.max_prefix > 0 && p.split.prefix_rows == 16)) * p.split.rows + row;
+            // a warp's first item is its piece 0; only the item's first warp may have begun with another item
+            from_piece[k] = w0 * 2 * p.split.columns + col;
+            step_piece[k] = stream_begin(w0, warps, total) < first ? p.split.columns : 0;
+        }
+    }
+    const int n = front + count[0] + count[1];
+    // Where part i is: its sum and its outputs.
+    auto source = [&](int i, const float *&outputs) -> const float * {
+        if (i < front) {
+            const int64_t at = static_cast<int64_t>(i) * p.split.rows + row;
+            outputs = p.parts + at * D;
+            return p.sums + at;
+        }
+        i -= front;
+        const int k = i >= count[0];
+        i -= k ? count[0] : 0;
+        if (from_whole[k] >= 0) {
+            outputs = p.parts + from_whole[k] * D;
+            return p.sums + from_whole[k];
+        }
+        const int64_t at = from_piece[k] + (i == 0 ? step_piece[k] : static_cast<int64_t>(i) * 2 * p.split.columns);
+        outputs = p.pieces + at * D;
+        return p.piece_sums + at;
+    };
     float m = -INFINITY;
-    for (int i = lane; i < n; i += 32) m = fmaxf(m, p.sums[index(i)]);
+    const float *outputs;
+    for (int i = lane; i < n; i += 32) m = fmaxf(m, *source(i, outputs));
 #pragma unroll
     for (int x = 16; x; x >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, x));
     const float base = m == -INFINITY ? 0.f : m;
@@ -556,18 +664,19 @@ __global__ void __launch_bounds__(128) join_kernel(const __grid_constant__ AttnP
     const int from = n * share / WARPS, to = n * (share + 1) / WARPS;
     for (int i0 = from; i0 < to; i0 += 32) {
         const int mine = i0 + lane;
-        const float weight = mine < to ? exp2f(p.sums[index(mine)] - base) : 0.f;
+        const float weight = mine < to ? exp2f(*source(mine, outputs) - base) : 0.f;
         total += weight;
         for (int j0 = 0; j0 < min(32, to - i0); j0 += kAhead) {
             float w[kAhead];
             float4 v[kAhead][2];
 #pragma unroll
             for (int j = 0; j < kAhead; j++) {
+                source(min(i0 + j0 + j, n - 1), outputs);
                 w[j] = __shfl_sync(0xffffffffu, weight, j0 + j);  // 0 past the end and for a part without keys, whose outputs were not written
 #pragma unroll
                 for (int k = 0; k < 2; k++) {
                     v[j][k] = make_float4(0.f, 0.f, 0.f, 0.f);
-                    if (w[j] != 0.f && lane * 4 + 128 * k < D) v[j][k] = *reinterpret_cast<const float4 *>(p.parts + index(i0 + j0 + j) * D + lane * 4 + 128 * k);
+                    if (w[j] != 0.f && lane * 4 + 128 * k < D) v[j][k] = *reinterpret_cast<const float4 *>(outputs + lane * 4 + 128 * k);
                 }
             }
 #pragma unroll
@@ -603,51 +712,50 @@ __global__ void __launch_bounds__(128) join_kernel(const __grid_constant__ AttnP
 
 // --------------------------------------------------------------------------------------- launching
 template <typename T, int KIND, int DP, int NB>
-static int launch_parts(const AttnParams &p, unsigned grid, int device, cudaStream_t s)
+static int launch_stream(const AttnParams &p, unsigned grid, int device, cudaStream_t s)
 {
-    using R = Ring<KIND, DP, NB>;
+    using R = Ring<KIND, DP>;
     static bool raised[kMaxDevices];  // set once per device; setting it twice does no harm
     if (!raised[device]) {
-        const cudaError_t e = cudaFuncSetAttribute(parts_kernel<T, KIND, DP, NB>, cudaFuncAttributeMaxDynamicSharedMemorySize, R::bytes);
+        const cudaError_t e = cudaFuncSetAttribute(stream_kernel<T, KIND, DP, NB>, cudaFuncAttributeMaxDynamicSharedMemorySize, R::bytes);
         if (e != cudaSuccess) return cuda_fail(e, "cudaFuncSetAttribute(dynamic shared memory)");
         raised[device] = true;
     }
-    parts_kernel<T, KIND, DP, NB><<<grid, 128, R::bytes, s>>>(p);
+    stream_kernel<T, KIND, DP, NB><<<grid, 128, R::bytes, s>>>(p);
     const cudaError_t e = cudaGetLastError();
     return e == cudaSuccess ? TC_OK : cuda_fail(e, "kernel launch");
 }
 
 template <typename T, int KIND, int NB>
-static int launch_parts_for(const AttnParams &p, unsigned grid, int device, cudaStream_t s)
+static int launch_stream_for(const AttnParams &p, unsigned grid, int device, cudaStream_t s)
 {
-    if (p.layer.D <= 64) return launch_parts<T, KIND, 64, NB>(p, grid, device, s);
-    if (p.layer.D <= 128) return launch_parts<T, KIND, 128, NB>(p, grid, device, s);
-    return launch_parts<T, KIND, 256, NB>(p, grid, device, s);
+    if (p.layer.D <= 64) return launch_stream<T, KIND, 64, NB>(p, grid, device, s);
+    if (p.layer.D <= 128) return launch_stream<T, KIND, 128, NB>(p, grid, device, s);
+    return launch_stream<T, KIND, 256, NB>(p, grid, device, s);
 }
 
 template <typename T, int KIND>
-static int launch_parts_columns(const AttnParams &p, unsigned grid, int device, cudaStream_t s)
+static int launch_stream_columns(const AttnParams &p, unsigned grid, int device, cudaStream_t s)
 {
-    return p.split.columns == 8 ? launch_parts_for<T, KIND, 1>(p, grid, device, s) : launch_parts_for<T, KIND, 2>(p, grid, device, s);
+    return p.split.columns == 8 ? launch_stream_for<T, KIND, 1>(p, grid, device, s) : launch_stream_for<T, KIND, 2>(p, grid, device, s);
 }
 
 template <typename T>
 static int launch_decode(const AttnParams &p, int device, cudaStream_t s)
 {
     int rc = TC_OK;
-    if (p.split.prefix_rows > 16 && (rc = launch_prefix(p, std::is_same<T, __half>::value ? TC_FP16 : TC_BF16, device, s)) != TC_OK) return rc;
-    const int64_t ctas = (p.split.prefix_rows == 16 ? static_cast<int64_t>(p.split.prefix_parts) * p.layer.H * p.split.prefix_blocks : 0) + static_cast<int64_t>(p.split.own_parts) * p.R * p.layer.H * p.split.own_blocks;
-    if (ctas > INT32_MAX) return fail(TC_ERR_TOO_LARGE, "%lld parts: too many for one call", (long long)ctas);
-    if (ctas) {
-        const unsigned grid = static_cast<unsigned>(ctas);
+    if (p.split.prefix_parts && (rc = launch_prefix(p, std::is_same<T, __half>::value ? TC_FP16 : TC_BF16, device, s)) != TC_OK) return rc;
+    if (p.split.stream_ctas) {
+        const unsigned grid = static_cast<unsigned>(p.split.stream_ctas);
         switch (p.layer.dtype) {
-        case TC_E4M3: rc = launch_parts_columns<__half, kE4m3>(p, grid, device, s); break;
-        case TC_INT8: rc = launch_parts_columns<__half, kInt8>(p, grid, device, s); break;
-        default: rc = launch_parts_columns<T, kPlain>(p, grid, device, s); break;
+        case TC_E4M3: rc = launch_stream_columns<__half, kE4m3>(p, grid, device, s); break;
+        case TC_INT8: rc = launch_stream_columns<__half, kInt8>(p, grid, device, s); break;
+        default: rc = launch_stream_columns<T, kPlain>(p, grid, device, s); break;
         }
         if (rc != TC_OK) return rc;
     }
-    if (p.split.prefix_parts + p.split.own_parts > 8) join_kernel<T, 4><<<static_cast<unsigned>(p.split.rows), 128, 0, s>>>(p);
+    // parts of a row: the prefix kernel's, and the warps that share one item of the stream
+    if (p.split.prefix_parts + p.split.stream_ctas * 4 / std::max<int64_t>(p.R * p.layer.H, 1) > 8) join_kernel<T, 4><<<static_cast<unsigned>(p.split.rows), 128, 0, s>>>(p);
     else join_kernel<T, 1><<<static_cast<unsigned>((p.split.rows + 3) / 4), 128, 0, s>>>(p);
     const cudaError_t e = cudaGetLastError();
     return e == cudaSuccess ? TC_OK : cuda_fail(e, "kernel launch");
@@ -741,8 +849,12 @@ extern "C" int tc_attn_decode(const tc_kv_layer_t *layer, const tc_attn_decode_t
     p.scale_log2 = static_cast<float>((a->scale != 0.f ? static_cast<double>(a->scale) : 1.0 / std::sqrt(static_cast<double>(p.layer.D))) * 1.4426950408889634);
     p.div_block = make_fastdiv(p.layer.B);
     p.div_group = make_fastdiv(static_cast<uint32_t>(p.split.group));
-    p.sums = static_cast<float *>(a->workspace);
-    p.parts = reinterpret_cast<float *>(static_cast<char *>(a->workspace) + p.split.sum_bytes);
+    char *const ws = static_cast<char *>(a->workspace);
+    p.sums = reinterpret_cast<float *>(ws + p.split.sums_at);
+    p.parts = reinterpret_cast<float *>(ws + p.split.parts_at);
+    p.piece_sums = reinterpret_cast<float *>(ws + p.split.piece_sums_at);
+    p.pieces = reinterpret_cast<float *>(ws + p.split.pieces_at);
+    p.before = reinterpret_cast<int64_t *>(ws + p.split.before_at);
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     return a->dtype == TC_BF16 ? launch_decode<__nv_bfloat16>(p, device, s) : launch_decode<__half>(p, device, s);
 }

@@ -19,8 +19,9 @@ struct AttnSplit {
     int32_t whole_parts;       // prefix_parts, the own keys' part, and that of a prefix in the stream
     int64_t prefix_chunk;      // keys per part of prefix_kernel
     int64_t rows;              // R * Hq
+    int64_t stream_tiles;      // of 16 keys, at most
     int64_t workspace;         // bytes; in it: [whole_parts][rows] sums and [..][D] outputs, [warps][2][columns] sums
-    int64_t sums_at, parts_at, piece_sums_at, pieces_at, before_at;  // and [..][D] outputs of pieces, [R + 2] tiles before a request
+    int64_t sums_at, parts_at, piece_sums_at, pieces_at, before_at;  // and [..][D] outputs of pieces, [R + 5] words at `before`
 };
 
 struct AttnParams {
@@ -36,10 +37,10 @@ struct AttnParams {
     int64_t R, max_len, max_prefix;
     int32_t Hq, q_bf16;
     float scale_log2;  // scale * log2(e)
-    FastDiv div_block, div_group;
+    FastDiv div_block, div_group, div_heads;
     AttnSplit split;
     float *sums, *parts, *piece_sums, *pieces;
-    int64_t *before;
+    uint32_t *before;  // {tiles, share, divider of the share}, then the tiles before each request and the prefix
     unsigned int *status;
 };
 

@@ -13,6 +13,7 @@
 
 namespace tc {
 
+constexpr float kLn2 = 0.6931471805599453f;
 constexpr int kLeastShare = 4;  // tiles of 16 keys that a warp of the stream takes at least
 constexpr int kSms = 148;  // B200; the workspace must not depend on the device that happens to be current
 
@@ -52,6 +53,7 @@ void split_attn(int64_t R, int64_t Hq, int64_t H, int64_t D, int64_t max_len, in
     // The stream's warps: what the GPU holds at once, fewer where not even the longest batch would
     // give each its least share.
     const int64_t stream_tiles = R * H * s->own_blocks * ((max_len + 15) / 16) + (s->prefix_rows == 16 ? H * s->prefix_blocks * ((max_prefix + 15) / 16) : 0);
+    s->stream_tiles = stream_tiles;
     const int64_t ctas = std::min<int64_t>(static_cast<int64_t>(kSms) * stream_ctas(quantised, D, s->columns), (stream_tiles + kLeastShare - 1) / kLeastShare);
     s->stream_ctas = static_cast<int32_t>(ctas);
     const int64_t whole = s->prefix_parts + (max_len > 0) + (max_prefix > 0 && s->prefix_rows == 16), pieces = ctas * 4 * 2 * s->columns;
@@ -65,7 +67,7 @@ void split_attn(int64_t R, int64_t Hq, int64_t H, int64_t D, int64_t max_len, in
     s->parts_at = place(whole * s->rows * D * 4);
     s->piece_sums_at = place(pieces * 4);
     s->pieces_at = place(pieces * D * 4);
-    s->before_at = place(ctas ? (R + 2) * 8 : 0);
+    s->before_at = place(ctas ? (R + 5) * 4 : 0);
 }
 
 // ------------------------------------------------------------------------------- device helpers
@@ -173,10 +175,9 @@ __device__ __forceinline__ int stream_length(const AttnParams &p, int64_t r, boo
     return static_cast<int>(min(max(len, int64_t(0)), most));
 }
 __device__ __forceinline__ int stream_items(const AttnParams &p, int64_t r) { return p.layer.H * (r < p.R ? p.split.own_blocks : p.split.prefix_blocks); }
-// Warps that share `total` tiles, and the first tile of warp w.
-__device__ __forceinline__ int64_t stream_warps(const AttnParams &p, int64_t total) { return min(static_cast<int64_t>(p.split.stream_ctas) * 4, (total + kLeastShare - 1) / kLeastShare); }
-__device__ __forceinline__ int64_t stream_begin(int64_t w, int64_t warps, int64_t total) { return w * total / warps; }
-__device__ __forceinline__ int64_t stream_owner(int64_t tile, int64_t warps, int64_t total) { return ((tile + 1) * warps - 1) / total; }
+// Tiles that each warp takes of `total` (below 2^31): warp w has [w * share, (w + 1) * share).
+__device__ __forceinline__ uint32_t stream_share(const AttnParams &p, uint32_t total) { return max((total + p.split.stream_ctas * 4 - 1) / (p.split.stream_ctas * 4), static_cast<uint32_t>(kLeastShare)); }
+__device__ __forceinline__ uint32_t stream_tiles(const AttnParams &p, int64_t r, bool tell) { return static_cast<uint32_t>((stream_length(p, r, tell) + 15) >> 4) * stream_items(p, r); }
 
 enum : uint32_t { kFirst = 1u << 16, kLast = 1u << 17, kWhole = 1u << 18, kSecond = 1u << 19 };
 
@@ -189,56 +190,62 @@ __global__ void __launch_bounds__(128, KIND != kPlain && DP <= 128 && NB == 1 ? 
     using VT = ST;
     constexpr int kCols = 8 * NB;
     extern __shared__ __align__(128) unsigned char shared[];
-    __shared__ int64_t sums_of[4], start_at[4], start_off[4];
+    __shared__ uint32_t sums_of[4], start_at[4], start_off[4];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int group = p.split.group;
 
     // Every CTA adds the tiles of all requests up, each thread over a run of them, and finds where its warps
     // begin; CTA 0 also leaves the sums for join_kernel.
     const int64_t per = (p.R + 1 + 127) / 128, mine0 = threadIdx.x * per, mine1 = min(mine0 + per, p.R + 1);
-    int64_t my_tiles = 0;
-    for (int64_t r = mine0; r < mine1; r++) my_tiles += static_cast<int64_t>((stream_length(p, r, blockIdx.x == 0) + 15) >> 4) * stream_items(p, r);
-    int64_t upto = my_tiles;
+    uint32_t my_tiles = 0;
+    for (int64_t r = mine0; r < mine1; r++) my_tiles += stream_tiles(p, r, blockIdx.x == 0);
+    uint32_t upto = my_tiles;
 #pragma unroll
     for (int x = 1; x < 32; x <<= 1) {
-        const int64_t v = __shfl_up_sync(0xffffffffu, upto, x);
+        const uint32_t v = __shfl_up_sync(0xffffffffu, upto, x);
         if (lane >= x) upto += v;
     }
     if (lane == 31) sums_of[warp] = upto;
     __syncthreads();
-    int64_t total = 0;
+    uint32_t total = 0;
 #pragma unroll
     for (int w = 0; w < 4; w++) {
         if (w < warp) upto += sums_of[w];
         total += sums_of[w];
     }
-    int64_t before = upto - my_tiles;
-    const int64_t warps = stream_warps(p, total), index = static_cast<int64_t>(warp) * gridDim.x + blockIdx.x;
+    const uint32_t before = upto - my_tiles, share = stream_share(p, total);
 #pragma unroll
     for (int w = 0; w < 4; w++) {
-        const int64_t i = static_cast<int64_t>(w) * gridDim.x + blockIdx.x;
-        if (i >= warps) break;
-        int64_t from = stream_begin(i, warps, total), at = before;
+        const uint32_t from = (w * gridDim.x + blockIdx.x) * share;
         if (from < before || from >= upto) continue;
+        uint32_t at = before;
         for (int64_t r = mine0; r < mine1; r++) {
-            const int64_t n = static_cast<int64_t>((stream_length(p, r, false) + 15) >> 4) * stream_items(p, r);
+            const uint32_t n = stream_tiles(p, r, false);
             if (from < at + n) {
-                start_at[w] = r, start_off[w] = from - at;
+                start_at[w] = static_cast<uint32_t>(r), start_off[w] = from - at;
                 break;
             }
             at += n;
         }
     }
     if (blockIdx.x == 0) {
+        uint32_t at = before;
         for (int64_t r = mine0; r < mine1; r++) {
-            p.before[r] = before;
-            before += static_cast<int64_t>((stream_length(p, r, false) + 15) >> 4) * stream_items(p, r);
+            p.before[4 + r] = at;
+            at += stream_tiles(p, r, false);
         }
-        if (threadIdx.x == 0) p.before[p.R + 1] = total;
+        if (threadIdx.x == 0) {
+            // the share, and what quick_div needs to divide by it (as make_fastdiv on the host)
+            const uint32_t shift = share > 1 ? 32 - __clz(share - 1) : 0;
+            const uint32_t mul = static_cast<uint32_t>((((1ull << shift) - share) << 32) / share + 1);
+            *reinterpret_cast<uint4 *>(p.before) = make_uint4(total, share, mul, shift);
+        }
     }
     __syncthreads();
-    if (index >= warps) return;
-    const int todo = static_cast<int>(stream_begin(index + 1, warps, total) - stream_begin(index, warps, total));
+    // spread over the SMs first, so that few shares do not meet on few of them
+    const uint32_t index = warp * gridDim.x + blockIdx.x;
+    if (static_cast<uint64_t>(index) * share >= total) return;
+    const int todo = static_cast<int>(min(share, total - index * share));
 
     const int c = lane & 3, g = lane >> 2, D = p.layer.D;
     const uint32_t ring = static_cast<uint32_t>(__cvta_generic_to_shared(shared)) + warp * R::stages * R::tile;
@@ -248,12 +255,13 @@ __global__ void __launch_bounds__(128, KIND != kPlain && DP <= 128 && NB == 1 ? 
     // The next tile to be copied: tile `l_tile` of `l_tiles` of item `l_item` of request l_r.
     int64_t l_r = start_at[warp];
     int l_len = stream_length(p, l_r, false), l_tiles = (l_len + 15) >> 4;
-    int l_item = static_cast<int>(start_off[warp] / l_tiles), l_tile = static_cast<int>(start_off[warp] - static_cast<int64_t>(l_item) * l_tiles);
+    int l_item = static_cast<int>(start_off[warp] / l_tiles), l_tile = static_cast<int>(start_off[warp] - l_item * l_tiles);
     const int32_t *l_table = l_r < p.R ? reinterpret_cast<const int32_t *>(p.tables + l_r * p.table_stride) : p.prefix_table;
     auto head_of = [&](int64_t r, int item) {
         const int blocks = r < p.R ? p.split.own_blocks : p.split.prefix_blocks;
         return blocks == 1 ? item : item / blocks;
     };
+    const int first_item = l_item;
     bool l_first = true, l_from_start = l_tile == 0, l_second = false;
     int l_left = todo;
     // this lane's rows and chunk of every copy
@@ -411,7 +419,7 @@ __global__ void __launch_bounds__(128, KIND != kPlain && DP <= 128 && NB == 1 ? 
             }
         }
     };
-    load_queries(start_at[warp], static_cast<int>(start_off[warp] / ((stream_length(p, start_at[warp], false) + 15) >> 4)), qf);
+    load_queries(start_at[warp], first_item, qf);
 
     float o[NB][DP / 16][4], top[NB][2], sum[NB][2];
     float largest = 0.f;  // codes: the largest scale of V so far
@@ -567,7 +575,7 @@ __global__ void __launch_bounds__(128, KIND != kPlain && DP <= 128 && NB == 1 ? 
             const Item it = item_of(head_r, static_cast<int>(head_item));
             const bool whole = head & kWhole;
             const int64_t slot = p.split.whole_parts - 1 - (head_r < p.R && p.max_prefix > 0 && p.split.prefix_rows == 16);  // own keys, then the prefix
-            const int64_t piece = (index * 2 + (head & kSecond ? 1 : 0)) * kCols;
+            const int64_t piece = (static_cast<int64_t>(index) * 2 + (head & kSecond ? 1 : 0)) * kCols;
 #pragma unroll
             for (int nb = 0; nb < NB; nb++)
 #pragma unroll
@@ -581,133 +589,155 @@ __global__ void __launch_bounds__(128, KIND != kPlain && DP <= 128 && NB == 1 ? 
                     const int64_t req = quick_div(static_cast<uint32_t>(row), p.div_group);
                     const int64_t where = whole ? slot * p.split.rows + req * p.Hq + it.h * group + (row - req * group) : piece + col;
                     float *dst = (whole ? p.parts : p.pieces) + where * D;
-                    const float inv = all == 0.f ? 0.f : 1.f / all;
+                    const float inv = all == 0.f ? 0.f : 1.f / all, log = all == 0.f ? -INFINITY : (top[nb][j] == -INFINITY ? 0.f : top[nb][j]) + log2f(all);
+                    if (whole && p.max_prefix == 0) {
+                        // these are all of the row's keys: its output
+                        char *out = p.out + req * p.out_req + (it.h * group + (row - req * group)) * p.out_head;
+#pragma unroll
+                        for (int k = 0; k < DP / 16; k++)
+#pragma unroll
+                            for (int half = 0; half < 2; half++) {
+                                const float x = o[nb][k][2 * half + j] * inv;
+                                if (16 * k >= D) continue;
+                                if (KIND == kPlain ? std::is_same<T, __nv_bfloat16>::value : p.q_bf16) reinterpret_cast<__nv_bfloat16 *>(out)[16 * k + g + 8 * half] = __float2bfloat16_rn(x);
+                                else reinterpret_cast<__half *>(out)[16 * k + g + 8 * half] = __float2half_rn(x);
+                            }
+                        if (g == 0 && p.lse) p.lse[req * p.Hq + it.h * group + (row - req * group)] = log * kLn2;
+                        continue;
+                    }
 #pragma unroll
                     for (int k = 0; k < DP / 16; k++)
 #pragma unroll
                         for (int half = 0; half < 2; half++)
                             if (16 * k < D) dst[16 * k + g + 8 * half] = o[nb][k][2 * half + j] * inv;
-                    if (g == 0) (whole ? p.sums : p.piece_sums)[where] = all == 0.f ? -INFINITY : (top[nb][j] == -INFINITY ? 0.f : top[nb][j]) + log2f(all);
+                    if (g == 0) (whole ? p.sums : p.piece_sums)[where] = log;
                 }
         }
     }
     copy_wait<0>();
 }
 
-// The parts' outputs, each by its share of the whole sum.  WARPS warps of a CTA take a row, each some of its
-// parts: one where there are few parts, four where one warp's chain of loads would be long.
+// The parts' outputs, each by its share of the whole sum, with a running maximum.  WARPS warps take a row, each
+// some of its parts: one where there are few parts, more where one warp's chain of loads would be long.
+// A batch's sums and outputs are loaded together: what a part without keys (sum -infinity) left in its
+// place is read but not used.
 template <typename T, int WARPS>
-__global__ void __launch_bounds__(128) join_kernel(const __grid_constant__ AttnParams p)
+__global__ void __launch_bounds__(WARPS == 1 ? 128 : 32 * WARPS) join_kernel(const __grid_constant__ AttnParams p)
 {
-    constexpr int kAhead = 4;  // parts loaded at once
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, D = p.layer.D, share = warp % WARPS;
-    __shared__ float others[WARPS == 1 ? 1 : 4][WARPS == 1 ? 1 : 32 * 8 + 1];
-    const int64_t row = static_cast<int64_t>(blockIdx.x) * (4 / WARPS) + warp / WARPS;
-    if (row >= p.split.rows) return;  // WARPS > 1: a CTA is one row
-    const int64_t r = row / p.Hq;
-    const int head = static_cast<int>(row - r * p.Hq), h = head / p.split.group, in_group = head - h * p.split.group;
-    if (p.lens[r] < 0) return;
-    // Sources: prefix_kernel's parts, then what the stream left of the request's own keys and of the prefix.
-    int front = 0;
-    if (p.split.prefix_rows > 16) {
-        const int64_t len = min(max(static_cast<int64_t>(*p.prefix_len), int64_t(0)), p.max_prefix);
-        front = static_cast<int>((len + p.split.prefix_chunk - 1) / p.split.prefix_chunk) * (p.split.prefix_rows == 128 ? 2 : 1);
+    constexpr int kAhead = 4;  // parts of a batch
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, D = p.layer.D, share_of = WARPS == 1 ? 0 : warp;
+    __shared__ float others[WARPS == 1 ? 1 : WARPS][WARPS == 1 ? 1 : 32 * 8 + 2];
+    const uint32_t row = WARPS == 1 ? blockIdx.x * 4 + warp : blockIdx.x, rows = static_cast<uint32_t>(p.split.rows);
+    if (row >= rows) return;
+    const uint32_t r = quick_div(row, p.div_heads), head = row - r * p.Hq, h = quick_div(head, p.div_group), in_group = head - h * p.split.group;
+    const int32_t own_len = p.lens[r], prefix_len = p.max_prefix ? *p.prefix_len : 0;
+    uint4 shares = make_uint4(0, 0, 0, 0);
+    uint32_t before[2] = {0, 0};
+    const bool prefix_streams = p.max_prefix && p.split.prefix_rows == 16;
+    if (p.split.stream_ctas) {
+        shares = *reinterpret_cast<const uint4 *>(p.before);
+        before[0] = p.before[4 + r];
+        if (prefix_streams) before[1] = p.before[4 + p.R];
     }
-    int count[2] = {0, 0};
-    int64_t from_whole[2] = {0, 0}, from_piece[2] = {0, 0};  // rows of `parts`, or of `pieces` (from_whole < 0)
-    int64_t step_piece[2] = {0, 0};
-    if (p.split.stream_ctas > 0) {
-        const int64_t total = p.before[p.R + 1], warps = total ? stream_warps(p, total) : 1;
-#pragma unroll
-        for (int k = 0; k < 2; k++) {
-            const int64_t q = k ? p.R : r;
-            const int tiles = (stream_length(p, q, false) + 15) >> 4;
-            if (!tiles) continue;
-            const int64_t in_q = k ? r * p.split.group + in_group : in_group;
-            const int block = static_cast<int>(in_q / p.split.columns), col = static_cast<int>(in_q - static_cast<int64_t>(block) * p.split.columns);
-            const int64_t first = p.before[q] + (static_cast<int64_t>(h) * (k ? p.split.prefix_blocks : p.split.own_blocks) + block) * tiles;
-            const int64_t w0 = stream_owner(first, warps, total), w1 = stream_owner(first + tiles - 1, warps, total);
-            count[k] = static_cast<int>(w1 - w0 + 1);
-            from_whole[k] = -1;
-            if (w0 == w1) from_whole[k] = (p.split.whole_parts - 1 - (k == 0 && p.max_prefix > 0 && p.split.prefix_rows == 16)) * p.split.rows + row;
-            // a warp's first item is its piece 0; only the item's first warp may have begun with another item
-            from_piece[k] = w0 * 2 * p.split.columns + col;
-            step_piece[k] = stream_begin(w0, warps, total) < first ? p.split.columns : 0;
-        }
-    }
-    const int n = front + count[0] + count[1];
-    // Where part i is: its sum and its outputs.
-    auto source = [&](int i, const float *&outputs) -> const float * {
-        if (i < front) {
-            const int64_t at = static_cast<int64_t>(i) * p.split.rows + row;
-            outputs = p.parts + at * D;
-            return p.sums + at;
-        }
-        i -= front;
-        const int k = i >= count[0];
-        i -= k ? count[0] : 0;
-        if (from_whole[k] >= 0) {
-            outputs = p.parts + from_whole[k] * D;
-            return p.sums + from_whole[k];
-        }
-        const int64_t at = from_piece[k] + (i == 0 ? step_piece[k] : static_cast<int64_t>(i) * 2 * p.split.columns);
-        outputs = p.pieces + at * D;
-        return p.piece_sums + at;
+    if (own_len < 0) return;
+    const uint32_t share = shares.y;
+    const FastDiv div_share{shares.z, shares.w};
+    const uint32_t own_keys = min(own_len, static_cast<int32_t>(p.max_len)), prefix_keys = min(max(prefix_len, 0), static_cast<int32_t>(p.max_prefix));
+    // What the stream left of an item: one whole part, or pieces of warps w0 .. w1.  A warp's first item is its piece 0; only
+    // the item's first warp may have begun with another item.
+    struct Left {
+        uint32_t count, first, next;  // parts; index of the first and the second of them
+        bool whole;
     };
-    float m = -INFINITY;
-    const float *outputs;
-    for (int i = lane; i < n; i += 32) m = fmaxf(m, *source(i, outputs));
-#pragma unroll
-    for (int x = 16; x; x >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, x));
-    const float base = m == -INFINITY ? 0.f : m;
-    float acc[8] = {}, total = 0.f;
-    const int from = n * share / WARPS, to = n * (share + 1) / WARPS;
-    for (int i0 = from; i0 < to; i0 += 32) {
-        const int mine = i0 + lane;
-        const float weight = mine < to ? exp2f(*source(mine, outputs) - base) : 0.f;
-        total += weight;
-        for (int j0 = 0; j0 < min(32, to - i0); j0 += kAhead) {
-            float w[kAhead];
+    auto left = [&](uint32_t keys, uint32_t at, uint32_t in_q, uint32_t blocks, uint32_t whole_slot) {
+        Left l{0, 0, 0, false};
+        const uint32_t tiles = (keys + 15) >> 4, columns = p.split.columns, block = blocks > 1 ? in_q / columns : 0, col = in_q - block * columns;
+        if (!tiles) return l;
+        const uint32_t first = at + (h * blocks + block) * tiles, w0 = quick_div(first, div_share), w1 = quick_div(first + tiles - 1, div_share);
+        l.count = w1 - w0 + 1;
+        l.whole = w0 == w1;
+        l.first = l.whole ? whole_slot : w0 * 2 * columns + col + (w0 * share < first ? columns : 0);
+        l.next = (w0 + 1) * 2 * columns + col;
+        return l;
+    };
+    const Left own = left(own_keys, before[0], in_group, p.split.own_blocks, p.split.whole_parts - (prefix_streams ? 2 : 1));
+    if (p.max_prefix == 0 && own.whole) return;  // the stream has written the output
+    Left shared{0, 0, 0, false};
+    if (prefix_streams) shared = left(prefix_keys, before[1], r * p.split.group + in_group, p.split.prefix_blocks, p.split.whole_parts - 1);
+    const uint32_t front = p.split.prefix_parts ? (prefix_keys + static_cast<uint32_t>(p.split.prefix_chunk) - 1) / static_cast<uint32_t>(p.split.prefix_chunk) * (p.split.prefix_rows == 128 ? 2 : 1) : 0;
+
+    float acc[8] = {}, all = 0.f, top = -INFINITY;
+#pragma unroll 1
+    for (int run = 0; run < 5; run++) {
+        // parts `from` .. of a run: prefix_kernel's; the first and the further ones of the own keys, and of a prefix in the stream
+        const Left &l = run < 3 ? own : shared;
+        const bool first = run & 1, whole = run == 0 || (first && l.whole);
+        const uint32_t n = run == 0 ? front : first ? min(l.count, 1u) : max(l.count, 1u) - 1;
+        const uint32_t from = first ? (share_of ? 1 : 0) : n * share_of / WARPS, to = first ? n : n * (share_of + 1) / WARPS;
+        if (from >= to) continue;
+        const float *sums = whole ? p.sums : p.piece_sums, *outputs = whole ? p.parts : p.pieces;
+        const int64_t step = run == 0 ? rows : 2 * p.split.columns;
+        int64_t at = (run == 0 ? row : first ? (whole ? static_cast<int64_t>(l.first) * rows + row : l.first) : l.next) + from * step;
+        for (uint32_t i0 = from; i0 < to; i0 += kAhead, at += kAhead * step) {
+            float sum[kAhead];
             float4 v[kAhead][2];
 #pragma unroll
             for (int j = 0; j < kAhead; j++) {
-                source(min(i0 + j0 + j, n - 1), outputs);
-                w[j] = __shfl_sync(0xffffffffu, weight, j0 + j);  // 0 past the end and for a part without keys, whose outputs were not written
+                sum[j] = -INFINITY;
+                v[j][0] = v[j][1] = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (i0 + j >= to) continue;
+                const float *src = outputs + (at + j * step) * D + lane * 4;
+                sum[j] = sums[at + j * step];
+                if (lane * 4 < D) v[j][0] = *reinterpret_cast<const float4 *>(src);
+                if (lane * 4 + 128 < D) v[j][1] = *reinterpret_cast<const float4 *>(src + 128);
+            }
+            float m = top;
 #pragma unroll
-                for (int k = 0; k < 2; k++) {
-                    v[j][k] = make_float4(0.f, 0.f, 0.f, 0.f);
-                    if (w[j] != 0.f && lane * 4 + 128 * k < D) v[j][k] = *reinterpret_cast<const float4 *>(outputs + lane * 4 + 128 * k);
-                }
+            for (int j = 0; j < kAhead; j++) m = fmaxf(m, sum[j]);
+            if (m > top) {
+                const float f = exp2_approx(top - m);
+#pragma unroll
+                for (int k = 0; k < 8; k++) acc[k] *= f;
+                all *= f;
+                top = m;
             }
 #pragma unroll
-            for (int j = 0; j < kAhead; j++)
+            for (int j = 0; j < kAhead; j++) {
+                if (sum[j] == -INFINITY) continue;
+                const float w = exp2_approx(sum[j] - (top == -INFINITY ? 0.f : top));  // NaN where the sum is
+                all += w;
 #pragma unroll
-                for (int k = 0; k < 2; k++)
-                    if (w[j] != 0.f) acc[4 * k] += w[j] * v[j][k].x, acc[4 * k + 1] += w[j] * v[j][k].y, acc[4 * k + 2] += w[j] * v[j][k].z, acc[4 * k + 3] += w[j] * v[j][k].w;
+                for (int k = 0; k < 2; k++) acc[4 * k] += w * v[j][k].x, acc[4 * k + 1] += w * v[j][k].y, acc[4 * k + 2] += w * v[j][k].z, acc[4 * k + 3] += w * v[j][k].w;
+            }
         }
     }
-#pragma unroll
-    for (int x = 16; x; x >>= 1) total += __shfl_xor_sync(0xffffffffu, total, x);
     if constexpr (WARPS > 1) {
 #pragma unroll
         for (int k = 0; k < 8; k++) others[warp][k * 32 + lane] = acc[k];
-        if (lane == 0) others[warp][256] = total;
+        if (lane == 0) others[warp][256] = all, others[warp][257] = top;
         __syncthreads();
         if (warp) return;
+        for (int w = 0; w < WARPS; w++) top = fmaxf(top, others[w][257]);
+        const float base = top == -INFINITY ? 0.f : top;
+        all = 0.f;
 #pragma unroll
-        for (int w = 1; w < WARPS; w++) {
+        for (int k = 0; k < 8; k++) acc[k] = 0.f;
+        for (int w = 0; w < WARPS; w++) {
+            const float part = others[w][256];
+            if (part == 0.f) continue;
+            const float f = others[w][257] == -INFINITY ? 1.f : exp2_approx(others[w][257] - base);  // -infinity: all of its sums are NaN
+            all += f * part;
 #pragma unroll
-            for (int k = 0; k < 8; k++) acc[k] += others[w][k * 32 + lane];
-            total += others[w][256];
+            for (int k = 0; k < 8; k++) acc[k] += f * others[w][k * 32 + lane];
         }
     }
-    const float inv = total == 0.f ? 0.f : 1.f / total;
+    const float inv = all == 0.f ? 0.f : 1.f / all;
     char *dst = p.out + r * p.out_req + head * p.out_head;
 #pragma unroll
     for (int k = 0; k < 2; k++)
         if (lane * 4 + 128 * k < D)
             *reinterpret_cast<uint2 *>(dst + (lane * 4 + 128 * k) * 2) = make_uint2(pack2<T>(acc[4 * k] * inv, acc[4 * k + 1] * inv), pack2<T>(acc[4 * k + 2] * inv, acc[4 * k + 3] * inv));
-    if (p.lse && lane == 0) p.lse[row] = total == 0.f ? -INFINITY : (base + log2f(total)) * 0.6931471805599453f;
+    if (p.lse && lane == 0) p.lse[row] = all == 0.f ? -INFINITY : ((top == -INFINITY ? 0.f : top) + log2f(all)) * kLn2;
 }
 
 // --------------------------------------------------------------------------------------- launching
@@ -754,9 +784,12 @@ static int launch_decode(const AttnParams &p, int device, cudaStream_t s)
         }
         if (rc != TC_OK) return rc;
     }
-    // parts of a row: the prefix kernel's, and the warps that share one item of the stream
-    if (p.split.prefix_parts + p.split.stream_ctas * 4 / std::max<int64_t>(p.R * p.layer.H, 1) > 8) join_kernel<T, 4><<<static_cast<unsigned>(p.split.rows), 128, 0, s>>>(p);
-    else join_kernel<T, 1><<<static_cast<unsigned>((p.split.rows + 3) / 4), 128, 0, s>>>(p);
+    // parts of a row: the prefix kernel's, and about as many as warps share one item of the stream
+    const int64_t parts = p.split.prefix_parts + p.split.stream_ctas * 4 / std::max<int64_t>(p.R * p.layer.H * p.split.own_blocks, 1);
+    const unsigned rows = static_cast<unsigned>(p.split.rows);
+    if (parts > 32) join_kernel<T, 16><<<rows, 512, 0, s>>>(p);
+    else if (parts > 8) join_kernel<T, 4><<<rows, 128, 0, s>>>(p);
+    else join_kernel<T, 1><<<(rows + 3) / 4, 128, 0, s>>>(p);
     const cudaError_t e = cudaGetLastError();
     return e == cudaSuccess ? TC_OK : cuda_fail(e, "kernel launch");
 }
@@ -779,7 +812,9 @@ static int check_decode(const tc_kv_layer_t *layer, const tc_attn_decode_t *a, A
     if (a->max_len < 0 || a->max_len > INT32_MAX - 4096 || a->max_prefix < 0 || a->max_prefix > INT32_MAX - 4096)
         return fail(TC_ERR_SHAPE, "max_len %lld and max_prefix %lld must be in [0, 2^31 - 4096)", (long long)a->max_len, (long long)a->max_prefix);
     if (!(a->scale == a->scale) || std::isinf(a->scale)) return fail(TC_ERR_INVALID_ARG, "scale is not a finite number");
+    if (a->R * p->layer.H > (1 << 30) / std::max<int64_t>(1, (a->max_len + 15) / 16)) return fail(TC_ERR_TOO_LARGE, "R * H * max_len = %lld * %d * %lld: too many keys for one call", (long long)a->R, p->layer.H, (long long)a->max_len);
     split_attn(a->R, a->Hq, p->layer.H, D, a->max_len, a->max_prefix, p->layer.quantised(), &p->split);
+    if (p->split.stream_tiles >= (1ll << 31)) return fail(TC_ERR_TOO_LARGE, "%lld tiles of 16 keys: too many for one call", (long long)p->split.stream_tiles);
     return TC_OK;
 }
 
@@ -849,12 +884,13 @@ extern "C" int tc_attn_decode(const tc_kv_layer_t *layer, const tc_attn_decode_t
     p.scale_log2 = static_cast<float>((a->scale != 0.f ? static_cast<double>(a->scale) : 1.0 / std::sqrt(static_cast<double>(p.layer.D))) * 1.4426950408889634);
     p.div_block = make_fastdiv(p.layer.B);
     p.div_group = make_fastdiv(static_cast<uint32_t>(p.split.group));
+    p.div_heads = make_fastdiv(static_cast<uint32_t>(p.Hq));
     char *const ws = static_cast<char *>(a->workspace);
     p.sums = reinterpret_cast<float *>(ws + p.split.sums_at);
     p.parts = reinterpret_cast<float *>(ws + p.split.parts_at);
     p.piece_sums = reinterpret_cast<float *>(ws + p.split.piece_sums_at);
     p.pieces = reinterpret_cast<float *>(ws + p.split.pieces_at);
-    p.before = reinterpret_cast<int64_t *>(ws + p.split.before_at);
+    p.before = reinterpret_cast<uint32_t *>(ws + p.split.before_at);
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     return a->dtype == TC_BF16 ? launch_decode<__nv_bfloat16>(p, device, s) : launch_decode<__half>(p, device, s);
 }

@@ -33,7 +33,7 @@ void split_attn(int64_t R, int64_t Hq, int64_t H, int64_t D, int64_t max_len, in
     s->columns = s->group <= 8 ? 8 : 16;
     s->own_blocks = (s->group + s->columns - 1) / s->columns;
     const int64_t rows = R * s->group;  // of one KV head
-    s->prefix_rows = max_prefix == 0 || rows <= 16 || D > 128 || quantised ? 16 : rows <= 128 ? 128 : 256;
+    s->prefix_rows = max_prefix == 0 || rows <= 16 || D > 128 ? 16 : rows <= 128 ? 128 : 256;
     const int64_t block = s->prefix_rows == 16 ? s->columns : s->prefix_rows;
     s->prefix_blocks = static_cast<int32_t>((rows + block - 1) / block);
     s->prefix_chunk = 128;
@@ -113,7 +113,6 @@ template <> __device__ __forceinline__ void mma16816<__nv_bfloat16>(float (&c)[4
 // are; the sum takes w / v_scale, which is exp2(s - top).  Queries of such a pool are fp16 with a power of two
 // per row taken out, so that the row's largest is in [2^14, 2^15): what is then below fp16's smallest
 // step is below 2^-38 of that largest.
-enum { kPlain = 0, kE4m3 = 1, kInt8 = 2 };
 
 template <int KIND, int DP>
 struct Ring {
@@ -137,21 +136,6 @@ __device__ __forceinline__ int place_of(int r, int c)
     else return r * row + ((c ^ (r >> 2 & 3)) << 4);
 }
 
-// Four codes as two pairs of fp16 numbers, exactly.
-template <int KIND>
-__device__ __forceinline__ void widen(uint32_t w, uint32_t &lo, uint32_t &hi)
-{
-    if constexpr (KIND == kE4m3) {
-        lo = e4m3_to_half2(w), hi = e4m3_to_half2(w >> 16);
-    } else {
-        // int8: the bytes of 1024 + (code + 128), less 1152
-        const uint32_t u = w ^ 0x80808080u, less = 0x64806480u;
-        const uint32_t a = __byte_perm(u, 0x64646464u, 0x4140), b = __byte_perm(u, 0x64646464u, 0x4342);
-        const __half2 x = __hsub2(*reinterpret_cast<const __half2 *>(&a), *reinterpret_cast<const __half2 *>(&less));
-        const __half2 y = __hsub2(*reinterpret_cast<const __half2 *>(&b), *reinterpret_cast<const __half2 *>(&less));
-        lo = *reinterpret_cast<const uint32_t *>(&x), hi = *reinterpret_cast<const uint32_t *>(&y);
-    }
-}
 // 16 keys x 32 d's of 8 bits, transposed: r[0], r[1]: d's g and g + 8, keys 4c .. 4c + 3; r[2], r[3]: 16 d's on.
 __device__ __forceinline__ void load_codes_transposed(uint32_t addr, uint32_t (&r)[4])
 {
@@ -398,20 +382,16 @@ __global__ void __launch_bounds__(128, KIND != kPlain && DP <= 128 && NB == 1 ? 
 #pragma unroll
                 for (int ks = 0; ks < DP / 16; ks++)
 #pragma unroll
-                    for (int j = 0; j < 2; j++) {
-                        const float2 f = p.q_bf16 ? unpack2<__nv_bfloat16>(qf[nb][ks][j]) : unpack2<__half>(qf[nb][ks][j]);
-                        if (fabsf(f.x) < INFINITY) most = fmaxf(most, fabsf(f.x));
-                        if (fabsf(f.y) < INFINITY) most = fmaxf(most, fabsf(f.y));
-                    }
+                    for (int j = 0; j < 2; j++) most = finite_magnitude(most, query_pair(qf[nb][ks][j], p.q_bf16));
                 most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 1));
                 most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 2));
-                const int e = most > 0.f ? max(static_cast<int>(__float_as_uint(most) >> 23) - 127, -100) : 14;
-                const float up = __uint_as_float(static_cast<uint32_t>(14 - e + 127) << 23), down = __uint_as_float(static_cast<uint32_t>(e - 14 + 127) << 23);
+                float up, down;
+                query_powers(most, up, down);
 #pragma unroll
                 for (int ks = 0; ks < DP / 16; ks++)
 #pragma unroll
                     for (int j = 0; j < 2; j++) {
-                        const float2 f = p.q_bf16 ? unpack2<__nv_bfloat16>(qf[nb][ks][j]) : unpack2<__half>(qf[nb][ks][j]);
+                        const float2 f = query_pair(qf[nb][ks][j], p.q_bf16);
                         qf[nb][ks][j] = pack2<__half>(f.x * up, f.y * up);
                     }
                 factor[nb][0] = p.scale_log2 * __shfl_sync(0xffffffffu, down, 8 * c);

@@ -24,4 +24,36 @@ __device__ __forceinline__ float exp2_approx(float x)
     return y;
 }
 
+enum { kPlain = 0, kE4m3 = 1, kInt8 = 2 };
+
+// Four codes as two pairs of fp16 numbers, exactly.
+template <int KIND>
+__device__ __forceinline__ void widen(uint32_t w, uint32_t &lo, uint32_t &hi)
+{
+    if constexpr (KIND == kE4m3) {
+        lo = e4m3_to_half2(w), hi = e4m3_to_half2(w >> 16);
+    } else {
+        // int8: the bytes of 1024 + (code + 128), less 1152
+        const uint32_t u = w ^ 0x80808080u, less = 0x64806480u;
+        const uint32_t a = __byte_perm(u, 0x64646464u, 0x4140), b = __byte_perm(u, 0x64646464u, 0x4342);
+        const __half2 x = __hsub2(*reinterpret_cast<const __half2 *>(&a), *reinterpret_cast<const __half2 *>(&less));
+        const __half2 y = __hsub2(*reinterpret_cast<const __half2 *>(&b), *reinterpret_cast<const __half2 *>(&less));
+        lo = *reinterpret_cast<const uint32_t *>(&x), hi = *reinterpret_cast<const uint32_t *>(&y);
+    }
+}
+// Queries that meet codes are fp16 with a power of two taken out of each row, so that its largest finite
+// magnitude `most` is in [2^14, 2^15).  The power to multiply with, and the one that undoes it.
+__device__ __forceinline__ void query_powers(float most, float &up, float &down)
+{
+    const int e = most > 0.f ? max(static_cast<int>(__float_as_uint(most) >> 23) - 127, -100) : 14;
+    up = __uint_as_float(static_cast<uint32_t>(14 - e + 127) << 23), down = __uint_as_float(static_cast<uint32_t>(e - 14 + 127) << 23);
+}
+__device__ __forceinline__ float2 query_pair(uint32_t w, bool bf16) { return bf16 ? unpack2<__nv_bfloat16>(w) : unpack2<__half>(w); }
+__device__ __forceinline__ float finite_magnitude(float most, float2 f)
+{
+    if (fabsf(f.x) < INFINITY) most = fmaxf(most, fabsf(f.x));
+    if (fabsf(f.y) < INFINITY) most = fmaxf(most, fabsf(f.y));
+    return most;
+}
+
 }  // namespace tc

@@ -6,15 +6,17 @@
 // every tile of 128 keys, so a tile is read once for 256 rows; with fewer, both hold the same rows and
 // take the tiles in turn.  Either way the tensor cores work on one slot while the other is in its softmax.
 //
-//   warps 0-3, 4-7   softmax of slot 0 and 1: a thread owns one row, so no shuffle is needed.  Two passes
-//                    over S: the maximum, then the probabilities, rounded to 16 bits and written over
-//                    S, where the second product takes them from tensor memory.  The running maximum
-//                    moves only when a tile exceeds it by more than 2^8 (then O is rescaled).
+//   warps 0-3, 4-7   softmax of slot 0 and 1: a thread owns one row and holds a tile's 128 scores in registers, so no
+//                    shuffle is needed.  The probabilities, rounded to 16 bits, are written over S, where the
+//                    second product takes them from tensor memory.  The running maximum moves only
+//                    when a tile exceeds it by more than 2^8 (then O is rescaled).
 //   warps 8-11       fill a ring of K and V tiles from the pages: 16-byte asynchronous copies into the
-//                    swizzled layout, whatever the page size; one lane looks a key's block up.
+//                    swizzled layout, whatever the page size; one lane looks a key's block up.  Codes are
+//                    staged as they are first and widened to fp16 by the warp that fetched them.
 //   warp 12          one thread issues the matrix products in the order
 //                    O0 += P0 V, S0 = Q0 K', O1 += P1 V, S1 = Q1 K', ...
 //
+// Scales of a quantised pool: as in stream_kernel, K's multiplies the scores, V's is in the exponent.
 // Every wait is bounded; one that runs out sets TC_DEVICE_BULK_WAIT_TIMEOUT and the CTA leaves.
 #include <algorithm>
 
@@ -24,16 +26,19 @@
 namespace tc {
 
 constexpr int kTile = 128;       // keys of a tile, and rows of a slot
-constexpr int kPrefixThreads = 416;
+constexpr int kPrefixThreads = 512;  // 128 registers each; the softmax takes 192, the others leave 64
+constexpr int kInfos = 4;            // tiles whose masks and scales are kept
 
-template <int DP, bool TWO>
+template <int KIND, int DP, bool TWO>
 struct PrefixShape {
     static constexpr int halves = DP / 64;
     static constexpr int tile = kTile * DP * 2;        // bytes of a K or V tile, and of a slot's queries
     static constexpr int queries = (TWO ? 2 : 1) * tile;
-    static constexpr int stages = TWO && DP == 128 ? 4 : DP == 128 ? 5 : 8;
-    static constexpr int infos = 8;                    // tiles whose validity masks are kept
-    static constexpr int bytes = queries + stages * tile + infos * 16 + 512 + 1024;  // + slack for the alignment
+    static constexpr int codes = KIND == kPlain ? 0 : kTile * DP;   // bytes of a staged tile of codes
+    static constexpr int staged = KIND == kPlain ? 0 : TWO ? 3 : 5;
+    static constexpr int stages = KIND != kPlain ? 3 : TWO && DP == 128 ? 4 : 5;
+    static constexpr int info = KIND == kPlain ? 16 : 16 + 3 * 4 * kTile;  // mask, then scales of K, log2 and inverse of V's
+    static constexpr int bytes = queries + stages * tile + staged * codes + kInfos * info + 256 + 1024;  // barriers, slack for the alignment
 };
 
 __device__ __forceinline__ void barrier_init(uint32_t bar, uint32_t count) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory"); }
@@ -82,10 +87,9 @@ __device__ __forceinline__ void tensor_load32(uint32_t addr, uint32_t (&r)[32])
     asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
                  : TC_R8(r, 0), TC_R8(r, 8), TC_R8(r, 16), TC_R8(r, 24) : "r"(addr));
 }
-__device__ __forceinline__ void tensor_store32(uint32_t addr, const uint32_t (&r)[32])
+__device__ __forceinline__ void tensor_load16(uint32_t addr, uint32_t (&r)[16])
 {
-    asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31};" ::TC_W8(r, 0), TC_W8(r, 8),
-                 TC_W8(r, 16), TC_W8(r, 24), "r"(addr) : "memory");
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];" : TC_R8(r, 0), TC_R8(r, 8) : "r"(addr));
 }
 __device__ __forceinline__ void tensor_store16(uint32_t addr, const uint32_t (&r)[16])
 {
@@ -101,14 +105,41 @@ __device__ __forceinline__ void fence_shared_to_async() { asm volatile("fence.pr
 // 16-byte chunks of a row permuted by its place in its group of eight.
 __device__ __forceinline__ uint32_t swizzled(int r, int chunk) { return (chunk >> 3) * (kTile * 128) + r * 128 + (((chunk & 7) ^ (r & 7)) << 4); }
 
-template <typename T, int DP, bool TWO>
+__device__ __forceinline__ float larger3(float a, float b, float c)
+{
+    float r;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+__device__ __forceinline__ float2 fused2(float2 a, float2 b, float2 c)
+{
+    float2 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;"
+        : "=l"(reinterpret_cast<uint64_t &>(r)) : "l"(reinterpret_cast<uint64_t &>(a)), "l"(reinterpret_cast<uint64_t &>(b)), "l"(reinterpret_cast<uint64_t &>(c)));
+    return r;
+}
+__device__ __forceinline__ float2 sum2(float2 a, float2 b)
+{
+    float2 r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(reinterpret_cast<uint64_t &>(r)) : "l"(reinterpret_cast<uint64_t &>(a)), "l"(reinterpret_cast<uint64_t &>(b)));
+    return r;
+}
+__device__ __forceinline__ float4 load_shared_f4(uint32_t addr)
+{
+    float4 v;
+    asm volatile("ld.shared.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr));
+    return v;
+}
+
+// T: the type of the products, fp16 for codes.
+template <typename T, int KIND, int DP, bool TWO>
 __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_kernel(const __grid_constant__ AttnParams p)
 {
-    using Shape = PrefixShape<DP, TWO>;
+    using Shape = PrefixShape<KIND, DP, TWO>;
     extern __shared__ unsigned char raw[];
     const uint32_t base = (static_cast<uint32_t>(__cvta_generic_to_shared(raw)) + 1023) & ~1023u;
     unsigned char *const gen = raw + (base - static_cast<uint32_t>(__cvta_generic_to_shared(raw)));
-    const uint32_t ring = base + Shape::queries, info = ring + Shape::stages * Shape::tile, bars = info + Shape::infos * 16;
+    const uint32_t ring = base + Shape::queries, staging = ring + Shape::stages * Shape::tile, info = staging + Shape::staged * Shape::codes, bars = info + kInfos * Shape::info;
     const uint32_t full = bars, empty = full + 8 * Shape::stages, s_full = empty + 8 * Shape::stages, p_ready = s_full + 16, o_done = p_ready + 16, tensor_at = o_done + 16;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, H = p.layer.H, group = p.split.group, D = p.layer.D;
 
@@ -141,8 +172,7 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_kernel(const __grid_
     }
     // Queries: zero past the last row and past D; a negative scale is taken into their sign.
     const uint32_t flip = p.scale_log2 < 0.f ? 0x80008000u : 0u;
-    for (int i = threadIdx.x; i < (TWO ? 256 : 128) * (DP / 8); i += kPrefixThreads) {
-        const int r = i / (DP / 8), chunk = i % (DP / 8);
+    auto query = [&](int r, int chunk) {
         const int64_t row = row0 + r;
         uint4 v = make_uint4(0, 0, 0, 0);
         if (row < row_end && chunk * 8 < D) {
@@ -150,7 +180,32 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_kernel(const __grid_
             v = *reinterpret_cast<const uint4 *>(p.q + req * p.q_req + (h * group + (row - req * group)) * p.q_head + chunk * 16);
             v.x ^= flip, v.y ^= flip, v.z ^= flip, v.w ^= flip;
         }
-        *reinterpret_cast<uint4 *>(gen + (r >> 7) * Shape::tile + swizzled(r & 127, chunk)) = v;
+        return v;
+    };
+    float factor = fabsf(p.scale_log2);  // of this thread's row of scores
+    if constexpr (KIND == kPlain) {
+        for (int i = threadIdx.x; i < (TWO ? 256 : 128) * (DP / 8); i += kPrefixThreads)
+            *reinterpret_cast<uint4 *>(gen + (i / (DP / 8) >> 7) * Shape::tile + swizzled(i / (DP / 8) & 127, i % (DP / 8))) = query(i / (DP / 8), i % (DP / 8));
+    } else if (warp < 8) {
+        const int r = TWO ? threadIdx.x : threadIdx.x & 127;
+        float most = 0.f, up, down;
+        for (int i = 0; i < DP / 8; i++) {
+            const uint4 v = query(r, i);
+            for (uint32_t w : {v.x, v.y, v.z, v.w}) most = finite_magnitude(most, query_pair(w, p.q_bf16));
+        }
+        query_powers(most, up, down);
+        factor *= down;
+        if (TWO || warp < 4)
+            for (int i = 0; i < DP / 8; i++) {
+                const uint4 v = query(r, i);
+                uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                for (int j = 0; j < 4; j++) {
+                    const float2 f = query_pair(w[j], p.q_bf16);
+                    w[j] = pack2<__half>(f.x * up, f.y * up);
+                }
+                *reinterpret_cast<uint4 *>(gen + (r >> 7) * Shape::tile + swizzled(r & 127, i)) = make_uint4(w[0], w[1], w[2], w[3]);
+            }
     }
     fence_shared_to_async();
     fence_before();
@@ -162,77 +217,95 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_kernel(const __grid_
 
     if (warp < 8) {
         // ---------------------------------------------------------------------------- softmax
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 192;");
         const int slot = warp >> 2, r = (warp & 3) * 32 + lane;
         const uint32_t lanes = tensor + (static_cast<uint32_t>((warp & 3) * 32) << 16), s_at = lanes + slot * 128, o_at = lanes + 256 + slot * 128;
-        const float scale = fabsf(p.scale_log2);
-        float top = -INFINITY, sum = 0.f;
+        float top = -INFINITY;
+        float2 sum = make_float2(0.f, 0.f);
         int mine = 0;
         for (int t = slot; t < steps && fine; t += 2, mine++) {
             fine = __all_sync(0xffffffffu, barrier_wait(s_full + 8 * slot, mine & 1));
             if (!fine) break;
             fence_after();
             const int tile = TWO ? t >> 1 : t;
+            const uint32_t about = info + (tile % kInfos) * Shape::info;
+            union {
+                uint32_t w[4][32];
+                float f[4][32];
+                float2 f2[4][16];
+            } s;
+#pragma unroll
+            for (int c = 0; c < 4; c++) tensor_load32(s_at + 32 * c, s.w[c]);
             uint32_t mask[4];
-            asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(mask[0]), "=r"(mask[1]), "=r"(mask[2]), "=r"(mask[3]) : "r"(info + (tile % Shape::infos) * 16));
-            const bool whole = (mask[0] & mask[1] & mask[2] & mask[3]) == 0xffffffffu;
-            float most = -INFINITY;
+            asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(mask[0]), "=r"(mask[1]), "=r"(mask[2]), "=r"(mask[3]) : "r"(about));
+            tensor_loaded();
+            if constexpr (KIND != kPlain) {
 #pragma unroll
-            for (int c = 0; c < 4; c++) {
-                uint32_t v[32];
-                tensor_load32(s_at + 32 * c, v);
-                tensor_loaded();
-                if (whole) {
-#pragma unroll
-                    for (int i = 0; i < 32; i += 2) most = fmaxf(most, fmaxf(__uint_as_float(v[i]), __uint_as_float(v[i + 1])));
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 32; i++)
-                        if (mask[c] >> i & 1) most = fmaxf(most, __uint_as_float(v[i]));
+                for (int i = 0; i < 32; i++) {
+                    const float4 k = load_shared_f4(about + 16 + 16 * i), v = load_shared_f4(about + 16 + 4 * kTile + 16 * i);
+                    const float2 f2 = make_float2(factor, factor), zero = make_float2(0.f, 0.f);
+                    float2 *x = &s.f2[i / 8][i % 8 * 2];
+                    x[0] = fused2(x[0], fused2(f2, make_float2(k.x, k.y), zero), make_float2(v.x, v.y));
+                    x[1] = fused2(x[1], fused2(f2, make_float2(k.z, k.w), zero), make_float2(v.z, v.w));
                 }
             }
-            most *= scale;
+            if ((mask[0] & mask[1] & mask[2] & mask[3]) != 0xffffffffu) {
+#pragma unroll
+                for (int c = 0; c < 4; c++)
+#pragma unroll
+                    for (int i = 0; i < 32; i++)
+                        if (!(mask[c] >> i & 1)) s.f[c][i] = -INFINITY;
+            }
+            float m4[4];
+#pragma unroll
+            for (int c = 0; c < 4; c++) {
+                m4[c] = fmaxf(s.f[c][0], s.f[c][1]);
+#pragma unroll
+                for (int i = 2; i < 32; i += 2) m4[c] = larger3(m4[c], s.f[c][i], s.f[c][i + 1]);
+            }
+            const float most = fmaxf(larger3(m4[0], m4[1], m4[2]), m4[3]) * (KIND == kPlain ? factor : 1.f);
             if (__any_sync(0xffffffffu, most > top + 8.f)) {
                 const float m = fmaxf(top, most), f = m == top ? 1.f : exp2_approx(top - m);
                 top = m;
-                sum *= f;
+                sum.x *= f, sum.y *= f;
                 if (mine) {
-#pragma unroll
-                    for (int c = 0; c < DP / 32; c++) {
-                        uint32_t v[32];
-                        tensor_load32(o_at + 32 * c, v);
+#pragma unroll 1
+                    for (int c = 0; c < DP / 16; c++) {
+                        uint32_t v[16];
+                        tensor_load16(o_at + 16 * c, v);
                         tensor_loaded();
 #pragma unroll
-                        for (int i = 0; i < 32; i++) v[i] = __float_as_uint(__uint_as_float(v[i]) * f);
-                        tensor_store32(o_at + 32 * c, v);
+                        for (int i = 0; i < 16; i++) v[i] = __float_as_uint(__uint_as_float(v[i]) * f);
+                        tensor_store16(o_at + 16 * c, v);
                     }
                 }
             }
             const float m = top == -INFINITY ? 0.f : top;
-            float add[2] = {0.f, 0.f};
+            const float2 minus = make_float2(-m, -m), f2 = make_float2(factor, factor);
 #pragma unroll
             for (int c = 0; c < 4; c++) {
-                uint32_t v[32], w[16];
-                tensor_load32(s_at + 32 * c, v);
-                tensor_loaded();
+                uint32_t w[16];
+                float4 inverse = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
                 for (int i = 0; i < 16; i++) {
-                    float a = fmaf(__uint_as_float(v[2 * i]), scale, -m), b = fmaf(__uint_as_float(v[2 * i + 1]), scale, -m);
-                    if (!whole) {
-                        if (!(mask[c] >> (2 * i) & 1)) a = -INFINITY;
-                        if (!(mask[c] >> (2 * i + 1) & 1)) b = -INFINITY;
+                    float2 e = KIND == kPlain ? fused2(s.f2[c][i], f2, minus) : sum2(s.f2[c][i], minus);
+                    e = make_float2(exp2_approx(e.x), exp2_approx(e.y));
+                    if constexpr (KIND == kPlain) {
+                        sum = sum2(sum, e);
+                    } else {
+                        if (i % 2 == 0) inverse = load_shared_f4(about + 16 + 8 * kTile + 16 * (8 * c + i / 2));
+                        sum = fused2(e, i % 2 == 0 ? make_float2(inverse.x, inverse.y) : make_float2(inverse.z, inverse.w), sum);
                     }
-                    a = exp2_approx(a), b = exp2_approx(b);
-                    add[0] += a, add[1] += b;
-                    w[i] = pack2<T>(a, b);
+                    w[i] = pack2<T>(e.x, e.y);
                 }
                 tensor_store16(s_at + 16 * c, w);
             }
-            sum += add[0] + add[1];
             tensor_stored();
             fence_before();
             barrier_arrive(p_ready + 8 * slot);
         }
         // The part: outputs by the sum, and its logarithm.  A slot without a tile says -infinity.
+        const float all = sum.x + sum.y;
         const int64_t row = row0 + (TWO ? slot * 128 : 0) + r;
         const int64_t out_part = TWO ? part : 2 * part + slot;
         const bool store = row < row_end;
@@ -241,7 +314,7 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_kernel(const __grid_
         if (mine && fine) fine = __all_sync(0xffffffffu, barrier_wait(o_done + 8 * slot, 0));
         if (mine && fine) {
             fence_after();
-            const float inv = sum == 0.f ? 0.f : 1.f / sum;
+            const float inv = all == 0.f ? 0.f : 1.f / all;
 #pragma unroll
             for (int c = 0; c < DP / 32; c++) {
                 uint32_t v[32];
@@ -254,9 +327,10 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_kernel(const __grid_
                             make_float4(__uint_as_float(v[i]) * inv, __uint_as_float(v[i + 1]) * inv, __uint_as_float(v[i + 2]) * inv, __uint_as_float(v[i + 3]) * inv);
             }
         }
-        if (store) p.sums[at] = !mine || sum == 0.f ? -INFINITY : (top == -INFINITY ? 0.f : top) + log2f(sum);
+        if (store) p.sums[at] = !mine || all == 0.f ? -INFINITY : (top == -INFINITY ? 0.f : top) + log2f(all);
     } else if (warp < 12) {
         // --------------------------------------------------------------------------- the pages
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
         const int w = warp - 8;
         auto look_up = [&](int tile) -> int32_t {
             const int t = begin + tile * kTile + w * 32 + lane;
@@ -268,84 +342,179 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_kernel(const __grid_
             }
             return b;
         };
-        int32_t ahead = look_up(0);
-        int told = 0;  // copies whose arrival has been passed on
-        // Copy u (K of tile u / 2, then V) goes to stage u % stages; three copies are in flight.
-        auto pass_on = [&](int u) {
-            fence_shared_to_async();
-            barrier_arrive(full + 8 * (u % Shape::stages));
-        };
-        for (int tile = 0; tile < tiles && fine; tile++) {
-            const int32_t blk = ahead;
-            ahead = look_up(tile + 1);
+        auto place_in_block = [&](int tile) {
             const int t = begin + tile * kTile + w * 32 + lane;
-            const int n = t - static_cast<int>(quick_div(static_cast<uint32_t>(t), p.div_block)) * static_cast<int>(p.layer.B);
-            const int64_t off = blk >= 0 ? p.layer.geo.at(blk, n, h) : -1;
-            const uint32_t mask = __ballot_sync(0xffffffffu, blk >= 0);
-            for (int kv = 0; kv < 2; kv++) {
-                const int u = 2 * tile + kv, stage = u % Shape::stages;
+            return t - static_cast<int>(quick_div(static_cast<uint32_t>(t), p.div_block)) * static_cast<int>(p.layer.B);
+        };
+        if constexpr (KIND == kPlain) {
+            int32_t ahead = look_up(0);
+            int told = 0;  // copies whose arrival has been passed on
+            // Copy u (K of tile u / 2, then V) goes to stage u % stages; three copies are in flight.
+            auto pass_on = [&](int u) {
+                fence_shared_to_async();
+                barrier_arrive(full + 8 * (u % Shape::stages));
+            };
+            for (int tile = 0; tile < tiles && fine; tile++) {
+                const int32_t blk = ahead;
+                ahead = look_up(tile + 1);
+                const int64_t off = blk >= 0 ? p.layer.geo.at(blk, place_in_block(tile), h) : -1;
+                const uint32_t mask = __ballot_sync(0xffffffffu, blk >= 0);
+                for (int kv = 0; kv < 2; kv++) {
+                    const int u = 2 * tile + kv, stage = u % Shape::stages;
+                    if (u >= Shape::stages) fine = __all_sync(0xffffffffu, barrier_wait(empty + 8 * stage, (u / Shape::stages - 1) & 1));
+                    if (!fine) break;
+                    // the tile whose mask this one's replaces is past its last use: its V is older than this stage's last copy
+                    if (kv == 0 && lane == 0) asm volatile("st.shared.u32 [%0], %1;" ::"r"(info + (tile % kInfos) * Shape::info + 4 * w), "r"(mask) : "memory");
+                    const char *plane = kv ? p.layer.v : p.layer.k;
+                    const uint32_t to = ring + stage * Shape::tile;
+                    constexpr int chunks = DP / 8;
+#pragma unroll
+                    for (int i = 0; i < chunks; i++) {
+                        const int idx = i * 32 + lane, rr = idx / chunks, ch = idx % chunks;
+                        const int64_t src = __shfl_sync(0xffffffffu, off, rr);
+                        const bool there = src >= 0 && ch * 8 < D;
+                        copy_async16(to + swizzled(w * 32 + rr, ch), plane + (there ? src + ch * 16 : 0), there);
+                    }
+                    copy_commit();
+                    if (u >= 2) {
+                        copy_wait<2>();
+                        pass_on(told++);
+                    }
+                }
+            }
+            copy_wait<0>();
+            if (fine)
+                while (told < 2 * tiles) pass_on(told++);
+        } else {
+            // Codes: a warp fetches and widens its own 32 keys of every tile.
+            constexpr int chunks = DP / 16;
+            const uint32_t mine = staging + w * 32 * DP;
+            int32_t ahead = look_up(0);
+            int64_t off = -1;
+            float next_k = 0.f, next_v = 0.f, scale_k = 0.f, scale_v = 0.f, largest = 7.888609052e-31f;  // 2^-100
+            uint32_t next_mask = 0, mask = 0;
+            auto fetch = [&](int u) {
+                if (u < 2 * tiles) {
+                    if ((u & 1) == 0) {
+                        const int tile = u >> 1, n = place_in_block(tile);
+                        const int32_t blk = ahead;
+                        ahead = look_up(tile + 1);
+                        off = blk >= 0 ? p.layer.geo.at(blk, n, h) : -1;
+                    }
+                    const char *plane = u & 1 ? p.layer.v : p.layer.k;
+#pragma unroll
+                    for (int i = 0; i < chunks; i++) {
+                        const int idx = i * 32 + lane, rr = idx / chunks, ch = idx % chunks;
+                        const int64_t src = __shfl_sync(0xffffffffu, off, rr);
+                        const bool there = src >= 0 && ch * 16 < D;
+                        copy_async16(mine + (u % Shape::staged) * Shape::codes + rr * DP + ch * 16, plane + (there ? src + ch * 16 : 0), there);
+                    }
+                }
+                copy_commit();
+            };
+            // masks and scales of a tile, a tile ahead of their use
+            auto fetch_scales = [&](int tile) {
+                const int t = begin + tile * kTile + w * 32 + lane;
+                next_k = next_v = 0.f;
+                bool there = tile < tiles && t < end;
+                if (there) {
+                    const int32_t blk = p.prefix_table[quick_div(static_cast<uint32_t>(t), p.div_block)];
+                    there = blk >= 0 && blk < p.layer.num_blocks;
+                    if (there) {
+                        const int64_t at = p.layer.scale_geo.at(blk, place_in_block(tile), h);
+                        next_k = *reinterpret_cast<const float *>(reinterpret_cast<const char *>(p.layer.k_scale) + at);
+                        next_v = *reinterpret_cast<const float *>(reinterpret_cast<const char *>(p.layer.v_scale) + at);
+                    }
+                }
+                next_mask = __ballot_sync(0xffffffffu, there);
+            };
+            fetch_scales(0);
+            for (int u = 0; u < Shape::staged - 1; u++) fetch(u);
+            for (int u = 0; u < 2 * tiles; u++) {
+                copy_wait<Shape::staged - 2>();
+                __syncwarp();
+                const int stage = u % Shape::stages, tile = u >> 1;
                 if (u >= Shape::stages) fine = __all_sync(0xffffffffu, barrier_wait(empty + 8 * stage, (u / Shape::stages - 1) & 1));
                 if (!fine) break;
-                // an older tile's mask is past its last use when this tile's K stage is free
-                if (kv == 0 && lane == 0) asm volatile("st.shared.u32 [%0], %1;" ::"r"(info + (tile % Shape::infos) * 16 + 4 * w), "r"(mask) : "memory");
-                const char *plane = kv ? p.layer.v : p.layer.k;
-                const uint32_t to = ring + stage * Shape::tile;
-                constexpr int chunks = DP / 8;
+                if ((u & 1) == 0) {
+                    // as above, this info's last tile is past its use
+                    scale_k = next_k, scale_v = next_v, mask = next_mask;
+                    fetch_scales(tile + 1);
+                    float most = scale_v;
+#pragma unroll
+                    for (int x = 16; x; x >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, x));
+                    largest = fmaxf(largest, most);
+                    if (scale_v == 0.f) scale_v = largest;  // a row of zeros: its codes are 0 whatever the scale
+                    const uint32_t about = info + (tile % kInfos) * Shape::info;
+                    if (lane == 0) asm volatile("st.shared.u32 [%0], %1;" ::"r"(about + 4 * w), "r"(mask) : "memory");
+                    const uint32_t key = about + 16 + 4 * (w * 32 + lane);
+                    asm volatile("st.shared.f32 [%0], %1;" ::"r"(key), "f"(scale_k) : "memory");
+                    asm volatile("st.shared.f32 [%0], %1;" ::"r"(key + 4 * kTile), "f"(__log2f(scale_v)) : "memory");
+                    asm volatile("st.shared.f32 [%0], %1;" ::"r"(key + 8 * kTile), "f"(__fdividef(1.f, scale_v)) : "memory");
+                }
+                const uint32_t from = mine + (u % Shape::staged) * Shape::codes, to = ring + stage * Shape::tile;
 #pragma unroll
                 for (int i = 0; i < chunks; i++) {
                     const int idx = i * 32 + lane, rr = idx / chunks, ch = idx % chunks;
-                    const int64_t src = __shfl_sync(0xffffffffu, off, rr);
-                    const bool there = src >= 0 && ch * 8 < D;
-                    copy_async16(to + swizzled(w * 32 + rr, ch), plane + (there ? src + ch * 16 : 0), there);
+                    uint32_t c[4], x[8];
+                    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(c[0]), "=r"(c[1]), "=r"(c[2]), "=r"(c[3]) : "r"(from + rr * DP + ch * 16));
+#pragma unroll
+                    for (int j = 0; j < 4; j++) widen<KIND>(c[j], x[2 * j], x[2 * j + 1]);
+                    // two 16-byte chunks; the lanes of the upper 64 d's write theirs in the other order, into other banks
+                    const bool odd = ch >= 4;
+                    const uint32_t a = to + swizzled(w * 32 + rr, 2 * ch + odd), b = to + swizzled(w * 32 + rr, 2 * ch + !odd);
+                    asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(a), "r"(odd ? x[4] : x[0]), "r"(odd ? x[5] : x[1]), "r"(odd ? x[6] : x[2]), "r"(odd ? x[7] : x[3]) : "memory");
+                    asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(b), "r"(odd ? x[0] : x[4]), "r"(odd ? x[1] : x[5]), "r"(odd ? x[2] : x[6]), "r"(odd ? x[3] : x[7]) : "memory");
                 }
-                copy_commit();
-                if (u >= 2) {
-                    copy_wait<2>();
-                    pass_on(told++);
-                }
+                fence_shared_to_async();
+                barrier_arrive(full + 8 * stage);
+                __syncwarp();
+                fetch(u + Shape::staged - 1);
             }
+            copy_wait<0>();
         }
-        copy_wait<0>();
-        if (fine)
-            while (told < 2 * tiles) pass_on(told++);
-    } else if (lane == 0) {
-        // --------------------------------------------------------------------- matrix products
-        const uint32_t qk = instruction<T>(kTile, false), pv = instruction<T>(DP, true);
-        auto scores = [&](int t) {
-            const int slot = t & 1, tile = TWO ? t >> 1 : t, u = 2 * tile, stage = u % Shape::stages;
-            if (!TWO || slot == 0) {
-                if (!barrier_wait(full + 8 * stage, (u / Shape::stages) & 1)) return false;
+    } else {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+        if (warp == 12 && lane == 0) {
+            // ----------------------------------------------------------------- matrix products
+            const uint32_t qk = instruction<T>(kTile, false), pv = instruction<T>(DP, true);
+            auto scores = [&](int t) {
+                const int slot = t & 1, tile = TWO ? t >> 1 : t, u = 2 * tile, stage = u % Shape::stages;
+                if (!TWO || slot == 0) {
+                    if (!barrier_wait(full + 8 * stage, (u / Shape::stages) & 1)) return false;
+                    fence_after();
+                }
+                const uint32_t q = base + (TWO ? slot * Shape::tile : 0), k = ring + stage * Shape::tile;
+#pragma unroll
+                for (int i = 0; i < DP / 16; i++) {
+                    const uint32_t at = (i >> 2) * (kTile * 128) + (i & 3) * 32;
+                    mma_shared(tensor + slot * 128, operand(q + at, 16), operand(k + at, 16), qk, i > 0);
+                }
+                commit_to(s_full + 8 * slot);
+                if (!TWO || slot == 1) commit_to(empty + 8 * stage);
+                return true;
+            };
+            for (int t = 0; t < 2 && t < steps && fine; t++) fine = scores(t);
+            for (int t = 0; t < steps && fine; t++) {
+                const int slot = t & 1, tile = TWO ? t >> 1 : t, u = 2 * tile + 1, stage = u % Shape::stages;
+                if (!TWO || slot == 0) fine = barrier_wait(full + 8 * stage, (u / Shape::stages) & 1);
+                if (fine) fine = barrier_wait(p_ready + 8 * slot, (t >> 1) & 1);
+                if (!fine) break;
                 fence_after();
-            }
-            const uint32_t q = base + (TWO ? slot * Shape::tile : 0), k = ring + stage * Shape::tile;
+                const uint32_t v = ring + stage * Shape::tile;
 #pragma unroll
-            for (int i = 0; i < DP / 16; i++) {
-                const uint32_t at = (i >> 2) * (kTile * 128) + (i & 3) * 32;
-                mma_shared(tensor + slot * 128, operand(q + at, 16), operand(k + at, 16), qk, i > 0);
+                for (int i = 0; i < kTile / 16; i++) mma_tensor(tensor + 256 + slot * 128, tensor + slot * 128 + 8 * i, operand(v + i * 2048, kTile * 128), pv, t > 1 || i > 0);
+                if (!TWO || slot == 1) commit_to(empty + 8 * stage);
+                if (t + 2 >= steps) commit_to(o_done + 8 * slot);
+                else fine = scores(t + 2);
             }
-            commit_to(s_full + 8 * slot);
-            if (!TWO || slot == 1) commit_to(empty + 8 * stage);
-            return true;
-        };
-        for (int t = 0; t < 2 && t < steps && fine; t++) fine = scores(t);
-        for (int t = 0; t < steps && fine; t++) {
-            const int slot = t & 1, tile = TWO ? t >> 1 : t, u = 2 * tile + 1, stage = u % Shape::stages;
-            if (!TWO || slot == 0) fine = barrier_wait(full + 8 * stage, (u / Shape::stages) & 1);
-            if (fine) fine = barrier_wait(p_ready + 8 * slot, (t >> 1) & 1);
-            if (!fine) break;
-            fence_after();
-            const uint32_t v = ring + stage * Shape::tile;
-#pragma unroll
-            for (int i = 0; i < kTile / 16; i++) mma_tensor(tensor + 256 + slot * 128, tensor + slot * 128 + 8 * i, operand(v + i * 2048, kTile * 128), pv, t > 1 || i > 0);
-            if (!TWO || slot == 1) commit_to(empty + 8 * stage);
-            if (t + 2 >= steps) commit_to(o_done + 8 * slot);
-            else fine = scores(t + 2);
+            if (!fine) {
+                // products may be in flight: let them end before the tensor memory is given back
+                commit_to(o_done);
+                barrier_wait(o_done, 0);
+            }
         }
-        if (!fine) {
-            // products may be in flight: let them end before the tensor memory is given back
-            commit_to(o_done);
-            barrier_wait(o_done, 0);
-        }
+        __syncwarp();
     }
     if (!fine) atomicOr(p.status, static_cast<unsigned int>(TC_DEVICE_BULK_WAIT_TIMEOUT));
     fence_before();
@@ -353,26 +522,28 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_kernel(const __grid_
     if (warp == 12) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tensor) : "memory");
 }
 
-template <typename T, int DP, bool TWO>
+template <typename T, int KIND, int DP, bool TWO>
 static int launch_prefix_shape(const AttnParams &p, unsigned grid, int device, cudaStream_t s)
 {
+    using Shape = PrefixShape<KIND, DP, TWO>;
+    static_assert(Shape::bytes <= 232448, "more shared memory than a CTA can have");
     static bool raised[kMaxDevices];
     if (!raised[device]) {
-        const cudaError_t e = cudaFuncSetAttribute(prefix_kernel<T, DP, TWO>, cudaFuncAttributeMaxDynamicSharedMemorySize, PrefixShape<DP, TWO>::bytes);
+        const cudaError_t e = cudaFuncSetAttribute(prefix_kernel<T, KIND, DP, TWO>, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape::bytes);
         if (e != cudaSuccess) return cuda_fail(e, "cudaFuncSetAttribute(dynamic shared memory)");
         raised[device] = true;
     }
-    prefix_kernel<T, DP, TWO><<<grid, kPrefixThreads, PrefixShape<DP, TWO>::bytes, s>>>(p);
+    prefix_kernel<T, KIND, DP, TWO><<<grid, kPrefixThreads, Shape::bytes, s>>>(p);
     const cudaError_t e = cudaGetLastError();
     return e == cudaSuccess ? TC_OK : cuda_fail(e, "kernel launch");
 }
 
-template <typename T>
+template <typename T, int KIND>
 static int launch_prefix_type(const AttnParams &p, unsigned grid, int device, cudaStream_t s)
 {
     const bool two = p.split.prefix_rows == 256;
-    if (p.layer.D <= 64) return two ? launch_prefix_shape<T, 64, true>(p, grid, device, s) : launch_prefix_shape<T, 64, false>(p, grid, device, s);
-    return two ? launch_prefix_shape<T, 128, true>(p, grid, device, s) : launch_prefix_shape<T, 128, false>(p, grid, device, s);
+    if (p.layer.D <= 64) return two ? launch_prefix_shape<T, KIND, 64, true>(p, grid, device, s) : launch_prefix_shape<T, KIND, 64, false>(p, grid, device, s);
+    return two ? launch_prefix_shape<T, KIND, 128, true>(p, grid, device, s) : launch_prefix_shape<T, KIND, 128, false>(p, grid, device, s);
 }
 
 int launch_prefix(const AttnParams &p, int dtype, int device, cudaStream_t s)
@@ -381,7 +552,11 @@ int launch_prefix(const AttnParams &p, int dtype, int device, cudaStream_t s)
     const int64_t ctas = chunks * p.layer.H * p.split.prefix_blocks;
     if (ctas > INT32_MAX) return fail(TC_ERR_TOO_LARGE, "%lld parts: too many for one call", (long long)ctas);
     const unsigned grid = static_cast<unsigned>(ctas);
-    return dtype == TC_BF16 ? launch_prefix_type<__nv_bfloat16>(p, grid, device, s) : launch_prefix_type<__half>(p, grid, device, s);
+    switch (p.layer.dtype) {
+    case TC_E4M3: return launch_prefix_type<__half, kE4m3>(p, grid, device, s);
+    case TC_INT8: return launch_prefix_type<__half, kInt8>(p, grid, device, s);
+    default: return dtype == TC_BF16 ? launch_prefix_type<__nv_bfloat16, kPlain>(p, grid, device, s) : launch_prefix_type<__half, kPlain>(p, grid, device, s);
+    }
 }
 
 }  // namespace tc

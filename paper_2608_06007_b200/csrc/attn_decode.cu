@@ -599,125 +599,147 @@ __global__ void __launch_bounds__(128, KIND != kPlain && DP <= 128 && NB == 1 ? 
 
 // The parts' outputs, each by its share of the whole sum, with a running maximum.  WARPS warps take a row, each
 // some of its parts: one where there are few parts, more where one warp's chain of loads would be long.
-// A batch's sums and outputs are loaded together: what a part without keys (sum -infinity) left in its
-// place is read but not used.
-template <typename T, int WARPS>
+// Every lane finds one part - its sum, and where its outputs are - and then the warp reads the outputs of kAhead
+// parts at once: what a part without keys (sum -infinity) left in its place is read but not used.
+// The latencies of these few loads are all the time there is, so a row's lengths are loaded a row ahead.
+template <typename T, int DP, int WARPS>
 __global__ void __launch_bounds__(WARPS == 1 ? 128 : 32 * WARPS) join_kernel(const __grid_constant__ AttnParams p)
 {
-    constexpr int kAhead = 4;  // parts of a batch
+    constexpr int kAhead = DP <= 128 ? 8 : 4, kVectors = DP <= 128 ? 1 : 2;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, D = p.layer.D, share_of = WARPS == 1 ? 0 : warp;
-    __shared__ float others[WARPS == 1 ? 1 : WARPS][WARPS == 1 ? 1 : 32 * 8 + 2];
-    const uint32_t row = WARPS == 1 ? blockIdx.x * 4 + warp : blockIdx.x, rows = static_cast<uint32_t>(p.split.rows);
+    __shared__ __align__(16) float others[WARPS == 1 ? 1 : WARPS][WARPS == 1 ? 4 : DP + 4];
+    const uint32_t rows = static_cast<uint32_t>(p.split.rows), row_step = WARPS == 1 ? gridDim.x * 4 : gridDim.x;
+    uint32_t row = WARPS == 1 ? blockIdx.x * 4 + warp : blockIdx.x;
     if (row >= rows) return;
-    const uint32_t r = quick_div(row, p.div_heads), head = row - r * p.Hq, h = quick_div(head, p.div_group), in_group = head - h * p.split.group;
-    const int32_t own_len = p.lens[r], prefix_len = p.max_prefix ? *p.prefix_len : 0;
-    uint4 shares = make_uint4(0, 0, 0, 0);
-    uint32_t before[2] = {0, 0};
-    const bool prefix_streams = p.max_prefix && p.split.prefix_rows == 16;
-    if (p.split.stream_ctas) {
-        shares = *reinterpret_cast<const uint4 *>(p.before);
-        before[0] = p.before[4 + r];
-        if (prefix_streams) before[1] = p.before[4 + p.R];
-    }
-    if (own_len < 0) return;
-    const uint32_t share = shares.y;
+    const bool prefix_streams = p.max_prefix && p.split.prefix_rows == 16, streams = p.split.stream_ctas > 0;
+    int32_t own_len = p.lens[quick_div(row, p.div_heads)];
+    uint32_t own_at = streams ? p.before[4 + quick_div(row, p.div_heads)] : 0;
+    const int32_t prefix_len = p.max_prefix ? *p.prefix_len : 0;
+    const uint4 shares = streams ? *reinterpret_cast<const uint4 *>(p.before) : make_uint4(0, 0, 0, 0);
+    const uint32_t prefix_at = prefix_streams ? p.before[4 + p.R] : 0, share = shares.y;
     const FastDiv div_share{shares.z, shares.w};
-    const uint32_t own_keys = min(own_len, static_cast<int32_t>(p.max_len)), prefix_keys = min(max(prefix_len, 0), static_cast<int32_t>(p.max_prefix));
+    const uint32_t prefix_keys = min(max(prefix_len, 0), static_cast<int32_t>(p.max_prefix)), chunk = static_cast<uint32_t>(p.split.prefix_chunk);
+    const uint32_t front = p.split.prefix_parts ? (prefix_keys + chunk - 1) / chunk * (p.split.prefix_rows == 128 ? 2 : 1) : 0;
     // What the stream left of an item: one whole part, or pieces of warps w0 .. w1.  A warp's first item is its piece 0; only
     // the item's first warp may have begun with another item.
     struct Left {
         uint32_t count, first, next;  // parts; index of the first and the second of them
         bool whole;
     };
-    auto left = [&](uint32_t keys, uint32_t at, uint32_t in_q, uint32_t blocks, uint32_t whole_slot) {
-        Left l{0, 0, 0, false};
-        const uint32_t tiles = (keys + 15) >> 4, columns = p.split.columns, block = blocks > 1 ? in_q / columns : 0, col = in_q - block * columns;
-        if (!tiles) return l;
-        const uint32_t first = at + (h * blocks + block) * tiles, w0 = quick_div(first, div_share), w1 = quick_div(first + tiles - 1, div_share);
-        l.count = w1 - w0 + 1;
-        l.whole = w0 == w1;
-        l.first = l.whole ? whole_slot : w0 * 2 * columns + col + (w0 * share < first ? columns : 0);
-        l.next = (w0 + 1) * 2 * columns + col;
-        return l;
-    };
-    const Left own = left(own_keys, before[0], in_group, p.split.own_blocks, p.split.whole_parts - (prefix_streams ? 2 : 1));
-    if (p.max_prefix == 0 && own.whole) return;  // the stream has written the output
-    Left shared{0, 0, 0, false};
-    if (prefix_streams) shared = left(prefix_keys, before[1], r * p.split.group + in_group, p.split.prefix_blocks, p.split.whole_parts - 1);
-    const uint32_t front = p.split.prefix_parts ? (prefix_keys + static_cast<uint32_t>(p.split.prefix_chunk) - 1) / static_cast<uint32_t>(p.split.prefix_chunk) * (p.split.prefix_rows == 128 ? 2 : 1) : 0;
 
-    float acc[8] = {}, all = 0.f, top = -INFINITY;
+    for (; row < rows; row += row_step) {
+        const uint32_t r = quick_div(row, p.div_heads), head = row - r * p.Hq, h = quick_div(head, p.div_group), in_group = head - h * p.split.group;
+        const int32_t len = own_len;
+        const uint32_t at = own_at;
+        if (row + row_step < rows) {
+            const uint32_t next = quick_div(row + row_step, p.div_heads);
+            own_len = p.lens[next];
+            if (streams) own_at = p.before[4 + next];
+        }
+        if (len < 0) continue;
+        auto left = [&](uint32_t keys, uint32_t begin, uint32_t in_q, uint32_t blocks, uint32_t whole_slot) {
+            Left l{0, 0, 0, false};
+            const uint32_t tiles = (keys + 15) >> 4, columns = p.split.columns, block = blocks > 1 ? in_q / columns : 0, col = in_q - block * columns;
+            if (!tiles) return l;
+            const uint32_t first = begin + (h * blocks + block) * tiles, w0 = quick_div(first, div_share), w1 = quick_div(first + tiles - 1, div_share);
+            l.count = w1 - w0 + 1;
+            l.whole = w0 == w1;
+            l.first = l.whole ? whole_slot : w0 * 2 * columns + col + (w0 * share < first ? columns : 0);
+            l.next = (w0 + 1) * 2 * columns + col;
+            return l;
+        };
+        const Left own = left(min(len, static_cast<int32_t>(p.max_len)), at, in_group, p.split.own_blocks, p.split.whole_parts - (prefix_streams ? 2 : 1));
+        if (p.max_prefix == 0 && own.whole) continue;  // the stream has written the output
+        Left shared{0, 0, 0, false};
+        if (prefix_streams) shared = left(prefix_keys, prefix_at, r * p.split.group + in_group, p.split.prefix_blocks, p.split.whole_parts - 1);
+        const uint32_t n = front + own.count + shared.count, from = n * share_of / WARPS, to = n * (share_of + 1) / WARPS;
+
+        float acc[4 * kVectors] = {}, all = 0.f, top = -INFINITY;
+        for (uint32_t i0 = from; i0 < to; i0 += 32) {
+            // this lane's part: prefix_kernel's, then those of the own keys, then those of a prefix in the stream
+            const uint32_t i = min(i0 + lane, to - 1), q = i - front;
+            const bool mine = q < own.count;
+            const Left &l = mine ? own : shared;
+            const uint32_t k = mine ? q : q - own.count;
+            const bool whole = i < front || l.whole;
+            const int64_t index = i < front ? static_cast<int64_t>(i) * rows + row
+                                  : l.whole ? static_cast<int64_t>(l.first) * rows + row
+                                            : static_cast<int64_t>(k == 0 ? l.first : l.next + (k - 1) * 2 * p.split.columns);
+            const float *outputs = (whole ? p.parts : p.pieces) + index * D;
+            const float sum = i0 + lane < to ? (whole ? p.sums : p.piece_sums)[index] : -INFINITY;
+            const int here = static_cast<int>(min(to - i0, 32u));
+            float weight = 0.f;
 #pragma unroll 1
-    for (int run = 0; run < 5; run++) {
-        // parts `from` .. of a run: prefix_kernel's; the first and the further ones of the own keys, and of a prefix in the stream
-        const Left &l = run < 3 ? own : shared;
-        const bool first = run & 1, whole = run == 0 || (first && l.whole);
-        const uint32_t n = run == 0 ? front : first ? min(l.count, 1u) : max(l.count, 1u) - 1;
-        const uint32_t from = first ? (share_of ? 1 : 0) : n * share_of / WARPS, to = first ? n : n * (share_of + 1) / WARPS;
-        if (from >= to) continue;
-        const float *sums = whole ? p.sums : p.piece_sums, *outputs = whole ? p.parts : p.pieces;
-        const int64_t step = run == 0 ? rows : 2 * p.split.columns;
-        int64_t at = (run == 0 ? row : first ? (whole ? static_cast<int64_t>(l.first) * rows + row : l.first) : l.next) + from * step;
-        for (uint32_t i0 = from; i0 < to; i0 += kAhead, at += kAhead * step) {
-            float sum[kAhead];
-            float4 v[kAhead][2];
+            for (int j0 = 0; j0 < here; j0 += kAhead) {
+                float4 v[kAhead][kVectors];
 #pragma unroll
-            for (int j = 0; j < kAhead; j++) {
-                sum[j] = -INFINITY;
-                v[j][0] = v[j][1] = make_float4(0.f, 0.f, 0.f, 0.f);
-                if (i0 + j >= to) continue;
-                const float *src = outputs + (at + j * step) * D + lane * 4;
-                sum[j] = sums[at + j * step];
-                if (lane * 4 < D) v[j][0] = *reinterpret_cast<const float4 *>(src);
-                if (lane * 4 + 128 < D) v[j][1] = *reinterpret_cast<const float4 *>(src + 128);
-            }
-            float m = top;
+                for (int j = 0; j < kAhead; j++) {
+                    const float *src = reinterpret_cast<const float *>(__shfl_sync(0xffffffffu, reinterpret_cast<uint64_t>(outputs), min(j0 + j, here - 1))) + lane * 4;
 #pragma unroll
-            for (int j = 0; j < kAhead; j++) m = fmaxf(m, sum[j]);
-            if (m > top) {
-                const float f = exp2_approx(top - m);
+                    for (int x = 0; x < kVectors; x++) {
+                        v[j][x] = make_float4(0.f, 0.f, 0.f, 0.f);
+                        if (j0 + j < here && lane * 4 + 128 * x < D) v[j][x] = *reinterpret_cast<const float4 *>(src + 128 * x);
+                    }
+                }
+                if (j0 == 0) {
+                    float m = sum;
 #pragma unroll
-                for (int k = 0; k < 8; k++) acc[k] *= f;
-                all *= f;
-                top = m;
-            }
+                    for (int x = 16; x; x >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, x));
+                    if (m > top) {
+                        const float f = exp2_approx(top - m);
 #pragma unroll
-            for (int j = 0; j < kAhead; j++) {
-                if (sum[j] == -INFINITY) continue;
-                const float w = exp2_approx(sum[j] - (top == -INFINITY ? 0.f : top));  // NaN where the sum is
-                all += w;
+                        for (int x = 0; x < 4 * kVectors; x++) acc[x] *= f;
+                        all *= f;
+                        top = m;
+                    }
+                    weight = sum == -INFINITY ? 0.f : exp2_approx(sum - (top == -INFINITY ? 0.f : top));  // NaN where the sum is
+                    float add = weight;
 #pragma unroll
-                for (int k = 0; k < 2; k++) acc[4 * k] += w * v[j][k].x, acc[4 * k + 1] += w * v[j][k].y, acc[4 * k + 2] += w * v[j][k].z, acc[4 * k + 3] += w * v[j][k].w;
+                    for (int x = 16; x; x >>= 1) add += __shfl_xor_sync(0xffffffffu, add, x);
+                    all += add;
+                }
+#pragma unroll
+                for (int j = 0; j < kAhead; j++) {
+                    const float w = __shfl_sync(0xffffffffu, weight, (j0 + j) & 31);
+                    if (w == 0.f || j0 + j >= here) continue;
+#pragma unroll
+                    for (int x = 0; x < kVectors; x++) acc[4 * x] += w * v[j][x].x, acc[4 * x + 1] += w * v[j][x].y, acc[4 * x + 2] += w * v[j][x].z, acc[4 * x + 3] += w * v[j][x].w;
+                }
             }
         }
-    }
-    if constexpr (WARPS > 1) {
+        if constexpr (WARPS > 1) {
 #pragma unroll
-        for (int k = 0; k < 8; k++) others[warp][k * 32 + lane] = acc[k];
-        if (lane == 0) others[warp][256] = all, others[warp][257] = top;
-        __syncthreads();
-        if (warp) return;
-        for (int w = 0; w < WARPS; w++) top = fmaxf(top, others[w][257]);
-        const float base = top == -INFINITY ? 0.f : top;
-        all = 0.f;
+            for (int x = 0; x < kVectors; x++)
+                if (lane * 4 + 128 * x < DP) *reinterpret_cast<float4 *>(&others[warp][lane * 4 + 128 * x]) = make_float4(acc[4 * x], acc[4 * x + 1], acc[4 * x + 2], acc[4 * x + 3]);
+            if (lane == 0) others[warp][DP] = all, others[warp][DP + 1] = top;
+            __syncthreads();
+            if (warp) return;  // a CTA takes one row
+            for (int w = 0; w < WARPS; w++) top = fmaxf(top, others[w][DP + 1]);
+            const float base = top == -INFINITY ? 0.f : top;
+            all = 0.f;
 #pragma unroll
-        for (int k = 0; k < 8; k++) acc[k] = 0.f;
-        for (int w = 0; w < WARPS; w++) {
-            const float part = others[w][256];
-            if (part == 0.f) continue;
-            const float f = others[w][257] == -INFINITY ? 1.f : exp2_approx(others[w][257] - base);  // -infinity: all of its sums are NaN
-            all += f * part;
+            for (int x = 0; x < 4 * kVectors; x++) acc[x] = 0.f;
+            for (int w = 0; w < WARPS; w++) {
+                const float part = others[w][DP], part_top = others[w][DP + 1];
+                if (part == 0.f) continue;
+                const float f = part_top == -INFINITY ? 1.f : exp2_approx(part_top - base);  // -infinity: all of its sums are NaN
+                all += f * part;
 #pragma unroll
-            for (int k = 0; k < 8; k++) acc[k] += f * others[w][k * 32 + lane];
+                for (int x = 0; x < kVectors; x++)
+                    if (lane * 4 + 128 * x < DP)
+#pragma unroll
+                        for (int k = 0; k < 4; k++) acc[4 * x + k] += f * others[w][lane * 4 + 128 * x + k];
+            }
         }
-    }
-    const float inv = all == 0.f ? 0.f : 1.f / all;
-    char *dst = p.out + r * p.out_req + head * p.out_head;
+        const float inv = all == 0.f ? 0.f : 1.f / all;
+        char *dst = p.out + r * p.out_req + head * p.out_head;
 #pragma unroll
-    for (int k = 0; k < 2; k++)
-        if (lane * 4 + 128 * k < D)
-            *reinterpret_cast<uint2 *>(dst + (lane * 4 + 128 * k) * 2) = make_uint2(pack2<T>(acc[4 * k] * inv, acc[4 * k + 1] * inv), pack2<T>(acc[4 * k + 2] * inv, acc[4 * k + 3] * inv));
-    if (p.lse && lane == 0) p.lse[row] = all == 0.f ? -INFINITY : ((top == -INFINITY ? 0.f : top) + log2f(all)) * kLn2;
+        for (int x = 0; x < kVectors; x++)
+            if (lane * 4 + 128 * x < D)
+                *reinterpret_cast<uint2 *>(dst + (lane * 4 + 128 * x) * 2) = make_uint2(pack2<T>(acc[4 * x] * inv, acc[4 * x + 1] * inv), pack2<T>(acc[4 * x + 2] * inv, acc[4 * x + 3] * inv));
+        if (p.lse && lane == 0) p.lse[row] = all == 0.f ? -INFINITY : ((top == -INFINITY ? 0.f : top) + log2f(all)) * kLn2;
+        if (WARPS > 1) return;
+    }
 }
 
 // --------------------------------------------------------------------------------------- launching
@@ -767,9 +789,14 @@ static int launch_decode(const AttnParams &p, int device, cudaStream_t s)
     // parts of a row: the prefix kernel's, and about as many as warps share one item of the stream
     const int64_t parts = p.split.prefix_parts + p.split.stream_ctas * 4 / std::max<int64_t>(p.R * p.layer.H * p.split.own_blocks, 1);
     const unsigned rows = static_cast<unsigned>(p.split.rows);
-    if (parts > 32) join_kernel<T, 16><<<rows, 512, 0, s>>>(p);
-    else if (parts > 8) join_kernel<T, 4><<<rows, 128, 0, s>>>(p);
-    else join_kernel<T, 1><<<(rows + 3) / 4, 128, 0, s>>>(p);
+    const unsigned few = std::min<unsigned>((rows + 3) / 4, kSms * 5);
+    if (p.layer.D <= 128) {
+        if (parts > 32) join_kernel<T, 128, 16><<<rows, 512, 0, s>>>(p);
+        else join_kernel<T, 128, 1><<<few, 128, 0, s>>>(p);
+    } else {
+        if (parts > 32) join_kernel<T, 256, 16><<<rows, 512, 0, s>>>(p);
+        else join_kernel<T, 256, 1><<<few, 128, 0, s>>>(p);
+    }
     const cudaError_t e = cudaGetLastError();
     return e == cudaSuccess ? TC_OK : cuda_fail(e, "kernel launch");
 }

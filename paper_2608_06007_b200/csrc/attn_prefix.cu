@@ -1,20 +1,22 @@
 // The shared prefix of tc_attn_decode on the fifth-generation tensor cores.
 //
 // All rows of queries of one KV head - R requests x Hq / H heads - meet every key of the prefix, so
-// this is a dense attention over pages.  A CTA has two slots of 128 rows in tensor memory, each with its scores S (128
-// columns) and its outputs O.  With more than 128 rows the slots hold different rows and both take
-// every tile of 128 keys, so a tile is read once for 256 rows; with fewer, both hold the same rows and
-// take the tiles in turn.  Either way the tensor cores work on one slot while the other is in its softmax.
+// this is a dense attention over pages.  A CTA has two slots of 128 rows in tensor memory, each with its probabilities P
+// (64 columns) and its outputs O (128); one buffer of scores S (128) serves both in turn, since a softmax takes
+// its scores into registers at once.  So the next scores of a slot are there when its softmax
+// ends, and neither the tensor cores nor the softmax wait for one another.  With more than 128
+// rows the slots hold different rows and both take every tile of 128 keys, so a tile is read once for
+// 256 rows; with fewer, both hold the same rows and take the tiles in turn.
 //
 //   warps 0-3, 4-7   softmax of slot 0 and 1: a thread owns one row and holds a tile's 128 scores in registers, so no
-//                    shuffle is needed.  The probabilities, rounded to 16 bits, are written over S, where the
-//                    second product takes them from tensor memory.  The running maximum moves only
-//                    when a tile exceeds it by more than 2^8 (then O is rescaled).
+//                    shuffle is needed.  The probabilities, rounded to 16 bits, go to tensor memory, where the
+//                    second product takes them.  The running maximum moves only when a tile exceeds it
+//                    by more than 2^8 (then O is rescaled).
 //   warps 8-11       fill a ring of K and V tiles from the pages: 16-byte asynchronous copies into the
 //                    swizzled layout, whatever the page size; one lane looks a key's block up.  Codes are
 //                    staged as they are first and widened to fp16 by the warp that fetched them.
 //   warp 12          one thread issues the matrix products in the order
-//                    O0 += P0 V, S0 = Q0 K', O1 += P1 V, S1 = Q1 K', ...
+//                    S = Q0 K', O1 += P1 V, S = Q1 K', O0 += P0 V, ...
 //
 // Scales of a quantised pool: as in stream_kernel, K's multiplies the scores, V's is in the exponent.
 // Every wait is bounded; one that runs out sets TC_DEVICE_BULK_WAIT_TIMEOUT and the CTA leaves.
@@ -35,8 +37,9 @@ struct PrefixShape {
     static constexpr int tile = kTile * DP * 2;        // bytes of a K or V tile, and of a slot's queries
     static constexpr int queries = (TWO ? 2 : 1) * tile;
     static constexpr int codes = KIND == kPlain ? 0 : kTile * DP;   // bytes of a staged tile of codes
-    static constexpr int staged = KIND == kPlain ? 0 : TWO ? 3 : 5;
-    static constexpr int stages = KIND != kPlain ? 3 : TWO && DP == 128 ? 4 : 5;
+    static constexpr int staged = KIND == kPlain ? 0 : 3;
+    // Scores run a tile and a half ahead of the outputs (TWO), or three tiles.
+    static constexpr int stages = KIND != kPlain ? (TWO ? 3 : 4) : TWO ? 4 : 6;
     static constexpr int info = KIND == kPlain ? 16 : 16 + 3 * 4 * kTile;  // mask, then scales of K, log2 and inverse of V's
     static constexpr int bytes = queries + stages * tile + staged * codes + kInfos * info + 256 + 1024;  // barriers, slack for the alignment
 };
@@ -54,6 +57,13 @@ __device__ __forceinline__ bool barrier_wait(uint32_t bar, uint32_t parity)
         if (spin > 64) __nanosleep(500);
     }
     return false;
+}
+
+__device__ __forceinline__ bool barrier_passed(uint32_t bar, uint32_t parity)
+{
+    uint32_t done;
+    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(done) : "r"(bar), "r"(parity) : "memory");
+    return done != 0;
 }
 
 // Shared-memory operand descriptor: 128-byte swizzle, 8-row atoms of 1024 bytes `sbo` apart; lbo: from one
@@ -101,6 +111,14 @@ __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::be
 __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_shared_to_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
+// One lane of a converged warp.
+__device__ __forceinline__ bool elected()
+{
+    uint32_t yes;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(yes));
+    return yes != 0;
+}
+
 // Byte of element d of row r in a swizzled tile of 128 rows: columns of 64 elements, 128 bytes a row, the
 // 16-byte chunks of a row permuted by its place in its group of eight.
 __device__ __forceinline__ uint32_t swizzled(int r, int chunk) { return (chunk >> 3) * (kTile * 128) + r * 128 + (((chunk & 7) ^ (r & 7)) << 4); }
@@ -140,8 +158,8 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_kernel(const __grid_
     const uint32_t base = (static_cast<uint32_t>(__cvta_generic_to_shared(raw)) + 1023) & ~1023u;
     unsigned char *const gen = raw + (base - static_cast<uint32_t>(__cvta_generic_to_shared(raw)));
     const uint32_t ring = base + Shape::queries, staging = ring + Shape::stages * Shape::tile, info = staging + Shape::staged * Shape::codes, bars = info + kInfos * Shape::info;
-    const uint32_t full = bars, empty = full + 8 * Shape::stages, s_full = empty + 8 * Shape::stages, p_ready = s_full + 16, o_done = p_ready + 16, tensor_at = o_done + 16;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, H = p.layer.H, group = p.split.group, D = p.layer.D;
+    const uint32_t full = bars, empty = full + 8 * Shape::stages, s_full = empty + 8 * Shape::stages, s_taken = s_full + 16, p_ready = s_taken + 16, o_added = p_ready + 16, tensor_at = o_added + 16;
+    const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31, H = p.layer.H, group = p.split.group, D = p.layer.D;
 
     // Which rows, which keys.
     int64_t id = blockIdx.x;
@@ -157,13 +175,14 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_kernel(const __grid_
     const int begin = static_cast<int>(part * p.split.prefix_chunk);
     const int end = static_cast<int>(min(static_cast<int64_t>(begin) + p.split.prefix_chunk, len));
     if (begin >= end) return;
-    const int tiles = (end - begin + kTile - 1) / kTile;
+    const int tiles = __shfl_sync(0xffffffffu, (end - begin + kTile - 1) / kTile, 0);
     const int64_t row0 = block * (TWO ? 256 : 128), row_end = p.R * group;
     const int steps = TWO ? 2 * tiles : tiles;  // step t: slot t & 1, tile t / 2 (TWO) or t
 
     if (threadIdx.x == 0) {
+        barrier_init(tensor_at + 8, 1);
         for (int i = 0; i < Shape::stages; i++) barrier_init(full + 8 * i, 128), barrier_init(empty + 8 * i, 1);
-        for (int i = 0; i < 2; i++) barrier_init(s_full + 8 * i, 1), barrier_init(p_ready + 8 * i, 128), barrier_init(o_done + 8 * i, 1);
+        for (int i = 0; i < 2; i++) barrier_init(s_full + 8 * i, 1), barrier_init(s_taken + 8 * i, 128), barrier_init(p_ready + 8 * i, 128), barrier_init(o_added + 8 * i, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 12) {
@@ -211,15 +230,16 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_kernel(const __grid_
     fence_before();
     __syncthreads();
     fence_after();
-    uint32_t tensor;
-    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(tensor) : "r"(tensor_at));
+    // All 512 columns are this CTA's, so they begin at 0; a constant lets the products' operands stay in
+    // uniform registers.
+    constexpr uint32_t tensor = 0;
     bool fine = true;  // no wait of this thread has run out
 
     if (warp < 8) {
         // ---------------------------------------------------------------------------- softmax
         asm volatile("setmaxnreg.inc.sync.aligned.u32 192;");
         const int slot = warp >> 2, r = (warp & 3) * 32 + lane;
-        const uint32_t lanes = tensor + (static_cast<uint32_t>((warp & 3) * 32) << 16), s_at = lanes + slot * 128, o_at = lanes + 256 + slot * 128;
+        const uint32_t lanes = tensor + (static_cast<uint32_t>((warp & 3) * 32) << 16), s_at = lanes, p_at = lanes + 128 + slot * 64, o_at = lanes + 256 + slot * 128;
         float top = -INFINITY;
         float2 sum = make_float2(0.f, 0.f);
         int mine = 0;
@@ -239,6 +259,8 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_kernel(const __grid_
             uint32_t mask[4];
             asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(mask[0]), "=r"(mask[1]), "=r"(mask[2]), "=r"(mask[3]) : "r"(about));
             tensor_loaded();
+            fence_before();
+            barrier_arrive(s_taken + 8 * slot);
             if constexpr (KIND != kPlain) {
 #pragma unroll
                 for (int i = 0; i < 32; i++) {
@@ -264,6 +286,12 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_kernel(const __grid_
                 for (int i = 2; i < 32; i += 2) m4[c] = larger3(m4[c], s.f[c][i], s.f[c][i + 1]);
             }
             const float most = fmaxf(larger3(m4[0], m4[1], m4[2]), m4[3]) * (KIND == kPlain ? factor : 1.f);
+            // P is free and O at rest when this slot's last product is done
+            if (mine) {
+                fine = __all_sync(0xffffffffu, barrier_wait(o_added + 8 * slot, (mine - 1) & 1));
+                if (!fine) break;
+                fence_after();
+            }
             if (__any_sync(0xffffffffu, most > top + 8.f)) {
                 const float m = fmaxf(top, most), f = m == top ? 1.f : exp2_approx(top - m);
                 top = m;
@@ -298,7 +326,7 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_kernel(const __grid_
                     }
                     w[i] = pack2<T>(e.x, e.y);
                 }
-                tensor_store16(s_at + 16 * c, w);
+                tensor_store16(p_at + 16 * c, w);
             }
             tensor_stored();
             fence_before();
@@ -311,7 +339,7 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_kernel(const __grid_
         const bool store = row < row_end;
         const int64_t req = store ? quick_div(static_cast<uint32_t>(row), p.div_group) : 0;
         const int64_t at = out_part * p.split.rows + req * p.Hq + h * group + (row - req * group);
-        if (mine && fine) fine = __all_sync(0xffffffffu, barrier_wait(o_done + 8 * slot, 0));
+        if (mine && fine) fine = __all_sync(0xffffffffu, barrier_wait(o_added + 8 * slot, (mine - 1) & 1));
         if (mine && fine) {
             fence_after();
             const float inv = all == 0.f ? 0.f : 1.f / all;
@@ -349,7 +377,7 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_kernel(const __grid_
         if constexpr (KIND == kPlain) {
             int32_t ahead = look_up(0);
             int told = 0;  // copies whose arrival has been passed on
-            // Copy u (K of tile u / 2, then V) goes to stage u % stages; three copies are in flight.
+            // Copy u (K of tile u / 2, then V) goes to stage u % stages; up to three are in flight.
             auto pass_on = [&](int u) {
                 fence_shared_to_async();
                 barrier_arrive(full + 8 * (u % Shape::stages));
@@ -361,8 +389,13 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_kernel(const __grid_
                 const uint32_t mask = __ballot_sync(0xffffffffu, blk >= 0);
                 for (int kv = 0; kv < 2; kv++) {
                     const int u = 2 * tile + kv, stage = u % Shape::stages;
-                    if (u >= Shape::stages) fine = __all_sync(0xffffffffu, barrier_wait(empty + 8 * stage, (u / Shape::stages - 1) & 1));
-                    if (!fine) break;
+                    if (u >= Shape::stages && !__all_sync(0xffffffffu, barrier_passed(empty + 8 * stage, (u / Shape::stages - 1) & 1))) {
+                        // nothing to issue: pass on what is in flight as soon as it is there
+                        copy_wait<0>();
+                        while (told < u) pass_on(told++);
+                        fine = __all_sync(0xffffffffu, barrier_wait(empty + 8 * stage, (u / Shape::stages - 1) & 1));
+                        if (!fine) break;
+                    }
                     // the tile whose mask this one's replaces is past its last use: its V is older than this stage's last copy
                     if (kv == 0 && lane == 0) asm volatile("st.shared.u32 [%0], %1;" ::"r"(info + (tile % kInfos) * Shape::info + 4 * w), "r"(mask) : "memory");
                     const char *plane = kv ? p.layer.v : p.layer.k;
@@ -376,10 +409,8 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_kernel(const __grid_
                         copy_async16(to + swizzled(w * 32 + rr, ch), plane + (there ? src + ch * 16 : 0), there);
                     }
                     copy_commit();
-                    if (u >= 2) {
-                        copy_wait<2>();
-                        pass_on(told++);
-                    }
+                    copy_wait<2>();
+                    if (told + 2 <= u) pass_on(told++);
                 }
             }
             copy_wait<0>();
@@ -475,46 +506,63 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_kernel(const __grid_
         }
     } else {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
-        if (warp == 12 && lane == 0) {
+        if (warp == 12) {
             // ----------------------------------------------------------------- matrix products
+            // The warp stays together and elects the thread that issues: with uniform control the operands are
+            // uniform registers already (issued from one lane's branch, products took twice as long).
             const uint32_t qk = instruction<T>(kTile, false), pv = instruction<T>(DP, true);
             auto scores = [&](int t) {
                 const int slot = t & 1, tile = TWO ? t >> 1 : t, u = 2 * tile, stage = u % Shape::stages;
                 if (!TWO || slot == 0) {
-                    if (!barrier_wait(full + 8 * stage, (u / Shape::stages) & 1)) return false;
+                    if (!__all_sync(0xffffffffu, barrier_wait(full + 8 * stage, (u / Shape::stages) & 1))) return false;
                     fence_after();
                 }
                 const uint32_t q = base + (TWO ? slot * Shape::tile : 0), k = ring + stage * Shape::tile;
+                const uint64_t q_operand = operand(q, 16), k_operand = operand(k, 16);
+                if (elected()) {
 #pragma unroll
-                for (int i = 0; i < DP / 16; i++) {
-                    const uint32_t at = (i >> 2) * (kTile * 128) + (i & 3) * 32;
-                    mma_shared(tensor + slot * 128, operand(q + at, 16), operand(k + at, 16), qk, i > 0);
+                    for (int i = 0; i < DP / 16; i++) {
+                        const uint32_t at = ((i >> 2) * (kTile * 128) + (i & 3) * 32) >> 4;
+                        mma_shared(tensor, q_operand + at, k_operand + at, qk, i > 0);
+                    }
+                    commit_to(s_full + 8 * slot);
+                    if (!TWO || slot == 1) commit_to(empty + 8 * stage);
                 }
-                commit_to(s_full + 8 * slot);
-                if (!TWO || slot == 1) commit_to(empty + 8 * stage);
+                __syncwarp();
                 return true;
             };
-            for (int t = 0; t < 2 && t < steps && fine; t++) fine = scores(t);
+            fine = scores(0);
             for (int t = 0; t < steps && fine; t++) {
+                // the scores of step t + 2 (at the start: also t + 1) go where those of the step before were
+                for (int next = t ? t + 2 : 1; next <= t + 2 && next < steps && fine; next++) {
+                    fine = __all_sync(0xffffffffu, barrier_wait(s_taken + 8 * ((next - 1) & 1), ((next - 1) >> 1) & 1));
+                    if (fine) {
+                        fence_after();
+                        fine = scores(next);
+                    }
+                }
                 const int slot = t & 1, tile = TWO ? t >> 1 : t, u = 2 * tile + 1, stage = u % Shape::stages;
-                if (!TWO || slot == 0) fine = barrier_wait(full + 8 * stage, (u / Shape::stages) & 1);
+                if (fine && (!TWO || slot == 0)) fine = barrier_wait(full + 8 * stage, (u / Shape::stages) & 1);
                 if (fine) fine = barrier_wait(p_ready + 8 * slot, (t >> 1) & 1);
+                fine = __all_sync(0xffffffffu, fine);
                 if (!fine) break;
                 fence_after();
-                const uint32_t v = ring + stage * Shape::tile;
+                const uint64_t v_operand = operand(ring + stage * Shape::tile, kTile * 128);
+                if (elected()) {
 #pragma unroll
-                for (int i = 0; i < kTile / 16; i++) mma_tensor(tensor + 256 + slot * 128, tensor + slot * 128 + 8 * i, operand(v + i * 2048, kTile * 128), pv, t > 1 || i > 0);
-                if (!TWO || slot == 1) commit_to(empty + 8 * stage);
-                if (t + 2 >= steps) commit_to(o_done + 8 * slot);
-                else fine = scores(t + 2);
+                    for (int i = 0; i < kTile / 16; i++) mma_tensor(tensor + 256 + slot * 128, tensor + 128 + slot * 64 + 8 * i, v_operand + i * (2048 >> 4), pv, t > 1 || i > 0);
+                    if (!TWO || slot == 1) commit_to(empty + 8 * stage);
+                    commit_to(o_added + 8 * slot);
+                }
+                __syncwarp();
             }
             if (!fine) {
                 // products may be in flight: let them end before the tensor memory is given back
-                commit_to(o_done);
-                barrier_wait(o_done, 0);
+                if (elected()) commit_to(tensor_at + 8);
+                __syncwarp();
+                barrier_wait(tensor_at + 8, 0);
             }
         }
-        __syncwarp();
     }
     if (!fine) atomicOr(p.status, static_cast<unsigned int>(TC_DEVICE_BULK_WAIT_TIMEOUT));
     fence_before();

@@ -15,8 +15,7 @@
 //   warps 8-11       fill a ring of K and V tiles from the pages: 16-byte asynchronous copies into the
 //                    swizzled layout, whatever the page size; one lane looks a key's block up.  Codes are
 //                    staged as they are first and widened to fp16 by the warp that fetched them.
-//   warp 12          one thread issues the matrix products in the order
-//                    S = Q0 K', O1 += P1 V, S = Q1 K', O0 += P0 V, ...
+//   warps 12, 13     issue the matrix products, S = Q K' and O += P V.
 //
 // Scales of a quantised pool: as in stream_kernel, K's multiplies the scores, V's is in the exponent.
 // Every wait is bounded; one that runs out sets TC_DEVICE_BULK_WAIT_TIMEOUT and the CTA leaves.
@@ -180,7 +179,7 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_kernel(const __grid_
     const int steps = TWO ? 2 * tiles : tiles;  // step t: slot t & 1, tile t / 2 (TWO) or t
 
     if (threadIdx.x == 0) {
-        barrier_init(tensor_at + 8, 1);
+        barrier_init(tensor_at + 8, 1), barrier_init(tensor_at + 16, 1);
         for (int i = 0; i < Shape::stages; i++) barrier_init(full + 8 * i, 128), barrier_init(empty + 8 * i, 1);
         for (int i = 0; i < 2; i++) barrier_init(s_full + 8 * i, 1), barrier_init(s_taken + 8 * i, 128), barrier_init(p_ready + 8 * i, 128), barrier_init(o_added + 8 * i, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -287,18 +286,21 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_kernel(const __grid_
             }
             const float most = fmaxf(larger3(m4[0], m4[1], m4[2]), m4[3]) * (KIND == kPlain ? factor : 1.f);
             // P is free and O at rest when this slot's last product is done
-            if (mine) {
+            bool rest = mine == 0;
+            auto await_rest = [&]() {
+                if (rest) return;
                 fine = __all_sync(0xffffffffu, barrier_wait(o_added + 8 * slot, (mine - 1) & 1));
-                if (!fine) break;
                 fence_after();
-            }
+                rest = true;
+            };
             if (__any_sync(0xffffffffu, most > top + 8.f)) {
                 const float m = fmaxf(top, most), f = m == top ? 1.f : exp2_approx(top - m);
                 top = m;
                 sum.x *= f, sum.y *= f;
                 if (mine) {
+                    await_rest();
 #pragma unroll 1
-                    for (int c = 0; c < DP / 16; c++) {
+                    for (int c = 0; c < DP / 16 && fine; c++) {
                         uint32_t v[16];
                         tensor_load16(o_at + 16 * c, v);
                         tensor_loaded();
@@ -310,9 +312,9 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_kernel(const __grid_
             }
             const float m = top == -INFINITY ? 0.f : top;
             const float2 minus = make_float2(-m, -m), f2 = make_float2(factor, factor);
+            uint32_t w[4][16];
 #pragma unroll
             for (int c = 0; c < 4; c++) {
-                uint32_t w[16];
                 float4 inverse = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
                 for (int i = 0; i < 16; i++) {
@@ -324,10 +326,13 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_kernel(const __grid_
                         if (i % 2 == 0) inverse = load_shared_f4(about + 16 + 8 * kTile + 16 * (8 * c + i / 2));
                         sum = fused2(e, i % 2 == 0 ? make_float2(inverse.x, inverse.y) : make_float2(inverse.z, inverse.w), sum);
                     }
-                    w[i] = pack2<T>(e.x, e.y);
+                    w[c][i] = pack2<T>(e.x, e.y);
                 }
-                tensor_store16(p_at + 16 * c, w);
             }
+            await_rest();
+            if (!fine) break;
+#pragma unroll
+            for (int c = 0; c < 4; c++) tensor_store16(p_at + 16 * c, w[c]);
             tensor_stored();
             fence_before();
             barrier_arrive(p_ready + 8 * slot);
@@ -506,19 +511,21 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_kernel(const __grid_
         }
     } else {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+        // ----------------------------------------------------------------------- matrix products
+        // Two warps, one for each product, so that neither waits for what only the other needs.  They stay together and
+        // elect the thread that issues: with uniform control the operands are uniform registers already
+        // (issued from one lane's branch, products took twice as long).
         if (warp == 12) {
-            // ----------------------------------------------------------------- matrix products
-            // The warp stays together and elects the thread that issues: with uniform control the operands are
-            // uniform registers already (issued from one lane's branch, products took twice as long).
-            const uint32_t qk = instruction<T>(kTile, false), pv = instruction<T>(DP, true);
-            auto scores = [&](int t) {
+            const uint32_t qk = instruction<T>(kTile, false);
+            for (int t = 0; t < steps && fine; t++) {
                 const int slot = t & 1, tile = TWO ? t >> 1 : t, u = 2 * tile, stage = u % Shape::stages;
-                if (!TWO || slot == 0) {
-                    if (!__all_sync(0xffffffffu, barrier_wait(full + 8 * stage, (u / Shape::stages) & 1))) return false;
-                    fence_after();
-                }
-                const uint32_t q = base + (TWO ? slot * Shape::tile : 0), k = ring + stage * Shape::tile;
-                const uint64_t q_operand = operand(q, 16), k_operand = operand(k, 16);
+                if (!TWO || slot == 0) fine = barrier_wait(full + 8 * stage, (u / Shape::stages) & 1);
+                // the buffer is free when the scores of the step before have been taken
+                if (t && fine) fine = barrier_wait(s_taken + 8 * (slot ^ 1), ((t - 1) >> 1) & 1);
+                fine = __all_sync(0xffffffffu, fine);
+                if (!fine) break;
+                fence_after();
+                const uint64_t q_operand = operand(base + (TWO ? slot * Shape::tile : 0), 16), k_operand = operand(ring + stage * Shape::tile, 16);
                 if (elected()) {
 #pragma unroll
                     for (int i = 0; i < DP / 16; i++) {
@@ -529,20 +536,12 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_kernel(const __grid_
                     if (!TWO || slot == 1) commit_to(empty + 8 * stage);
                 }
                 __syncwarp();
-                return true;
-            };
-            fine = scores(0);
+            }
+        } else if (warp == 13) {
+            const uint32_t pv = instruction<T>(DP, true);
             for (int t = 0; t < steps && fine; t++) {
-                // the scores of step t + 2 (at the start: also t + 1) go where those of the step before were
-                for (int next = t ? t + 2 : 1; next <= t + 2 && next < steps && fine; next++) {
-                    fine = __all_sync(0xffffffffu, barrier_wait(s_taken + 8 * ((next - 1) & 1), ((next - 1) >> 1) & 1));
-                    if (fine) {
-                        fence_after();
-                        fine = scores(next);
-                    }
-                }
                 const int slot = t & 1, tile = TWO ? t >> 1 : t, u = 2 * tile + 1, stage = u % Shape::stages;
-                if (fine && (!TWO || slot == 0)) fine = barrier_wait(full + 8 * stage, (u / Shape::stages) & 1);
+                if (!TWO || slot == 0) fine = barrier_wait(full + 8 * stage, (u / Shape::stages) & 1);
                 if (fine) fine = barrier_wait(p_ready + 8 * slot, (t >> 1) & 1);
                 fine = __all_sync(0xffffffffu, fine);
                 if (!fine) break;
@@ -556,12 +555,13 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_kernel(const __grid_
                 }
                 __syncwarp();
             }
-            if (!fine) {
-                // products may be in flight: let them end before the tensor memory is given back
-                if (elected()) commit_to(tensor_at + 8);
-                __syncwarp();
-                barrier_wait(tensor_at + 8, 0);
-            }
+        }
+        if (warp < 14 && !fine) {
+            // products may be in flight: let them end before the tensor memory is given back
+            const uint32_t last = tensor_at + 8 + 8 * (warp - 12);
+            if (elected()) commit_to(last);
+            __syncwarp();
+            barrier_wait(last, 0);
         }
     }
     if (!fine) atomicOr(p.status, static_cast<unsigned int>(TC_DEVICE_BULK_WAIT_TIMEOUT));

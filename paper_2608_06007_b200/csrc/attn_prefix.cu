@@ -17,7 +17,7 @@
 //                    staged as they are first and widened to fp16 by the warp that fetched them.
 //   warps 12, 13     issue the matrix products, S = Q K' and O += P V.
 //
-// Scales of a quantised pool: as in stream_kernel, K's multiplies the scores, V's is in the exponent.
+// Scales of a quantised pool: K's multiply the scores, V's are taken into the values.
 // Every wait is bounded; one that runs out sets TC_DEVICE_BULK_WAIT_TIMEOUT and the CTA leaves.
 #include <algorithm>
 
@@ -39,15 +39,23 @@ struct PrefixShape {
     static constexpr int staged = KIND == kPlain ? 0 : 3;
     // Scores run a tile and a half ahead of the outputs (TWO), or three tiles.
     static constexpr int stages = KIND != kPlain ? (TWO ? 3 : 4) : TWO ? 4 : 6;
-    static constexpr int info = KIND == kPlain ? 16 : 16 + 3 * 4 * kTile;  // mask, then scales of K, log2 and inverse of V's
+    static constexpr int info = KIND == kPlain ? 16 : 48 + 4 * kTile;  // mask; exponents of V's (from each warp); scales of K
     static constexpr int bytes = queries + stages * tile + staged * codes + kInfos * info + 256 + 1024;  // barriers, slack for the alignment
 };
 
 __device__ __forceinline__ void barrier_init(uint32_t bar, uint32_t count) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory"); }
 __device__ __forceinline__ void barrier_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
+__device__ __forceinline__ bool barrier_passed(uint32_t bar, uint32_t parity)
+{
+    uint32_t done;
+    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(done) : "r"(bar), "r"(parity) : "memory");
+    return done != 0;
+}
+
 // Waits for the phase of that parity to end; false when it does not within about a second.
 __device__ __forceinline__ bool barrier_wait(uint32_t bar, uint32_t parity)
 {
+    if (barrier_passed(bar, parity)) return true;
     for (uint32_t spin = 0; spin < (1u << 20); spin++) {
         uint32_t done;
         asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\tselp.u32 %0, 1, 0, p;\n\t}"
@@ -56,13 +64,6 @@ __device__ __forceinline__ bool barrier_wait(uint32_t bar, uint32_t parity)
         if (spin > 64) __nanosleep(500);
     }
     return false;
-}
-
-__device__ __forceinline__ bool barrier_passed(uint32_t bar, uint32_t parity)
-{
-    uint32_t done;
-    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(done) : "r"(bar), "r"(parity) : "memory");
-    return done != 0;
 }
 
 // Shared-memory operand descriptor: 128-byte swizzle, 8-row atoms of 1024 bytes `sbo` apart; lbo: from one
@@ -260,14 +261,16 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_kernel(const __grid_
             tensor_loaded();
             fence_before();
             barrier_arrive(s_taken + 8 * slot);
+            float exponent = 0.f;
             if constexpr (KIND != kPlain) {
+                asm volatile("ld.shared.f32 %0, [%1];" : "=f"(exponent) : "r"(about + 16));
+                const float2 f2 = make_float2(factor, factor), zero = make_float2(0.f, 0.f), e2 = make_float2(exponent, exponent);
 #pragma unroll
                 for (int i = 0; i < 32; i++) {
-                    const float4 k = load_shared_f4(about + 16 + 16 * i), v = load_shared_f4(about + 16 + 4 * kTile + 16 * i);
-                    const float2 f2 = make_float2(factor, factor), zero = make_float2(0.f, 0.f);
+                    const float4 k = load_shared_f4(about + 48 + 16 * i);
                     float2 *x = &s.f2[i / 8][i % 8 * 2];
-                    x[0] = fused2(x[0], fused2(f2, make_float2(k.x, k.y), zero), make_float2(v.x, v.y));
-                    x[1] = fused2(x[1], fused2(f2, make_float2(k.z, k.w), zero), make_float2(v.z, v.w));
+                    x[0] = fused2(x[0], fused2(f2, make_float2(k.x, k.y), zero), e2);
+                    x[1] = fused2(x[1], fused2(f2, make_float2(k.z, k.w), zero), e2);
                 }
             }
             if ((mask[0] & mask[1] & mask[2] & mask[3]) != 0xffffffffu) {
@@ -313,23 +316,21 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_kernel(const __grid_
             const float m = top == -INFINITY ? 0.f : top;
             const float2 minus = make_float2(-m, -m), f2 = make_float2(factor, factor);
             uint32_t w[4][16];
+            float2 here = make_float2(0.f, 0.f);
 #pragma unroll
             for (int c = 0; c < 4; c++) {
-                float4 inverse = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
                 for (int i = 0; i < 16; i++) {
                     float2 e = KIND == kPlain ? fused2(s.f2[c][i], f2, minus) : sum2(s.f2[c][i], minus);
                     e = make_float2(exp2_approx(e.x), exp2_approx(e.y));
-                    if constexpr (KIND == kPlain) {
-                        sum = sum2(sum, e);
-                    } else {
-                        if (i % 2 == 0) inverse = load_shared_f4(about + 16 + 8 * kTile + 16 * (8 * c + i / 2));
-                        sum = fused2(e, i % 2 == 0 ? make_float2(inverse.x, inverse.y) : make_float2(inverse.z, inverse.w), sum);
-                    }
+                    here = sum2(here, e);
                     w[c][i] = pack2<T>(e.x, e.y);
                 }
             }
-            await_rest();
+            // the tile's power of two is in its values: out of the sum
+            if constexpr (KIND == kPlain) sum = sum2(sum, here);
+            else sum = fused2(here, make_float2(exp2_approx(-exponent), exp2_approx(-exponent)), sum);
+            await_rest();  // by now it has been given, as a rule
             if (!fine) break;
 #pragma unroll
             for (int c = 0; c < 4; c++) tensor_store16(p_at + 16 * c, w[c]);
@@ -422,13 +423,16 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_kernel(const __grid_
             if (fine)
                 while (told < 2 * tiles) pass_on(told++);
         } else {
-            // Codes: a warp fetches and widens its own 32 keys of every tile.
+            // Codes: a warp fetches and widens its own 32 keys of every tile.  V's are multiplied by their scales over a
+            // power of two that the tile's largest scale sets, 2^exponent, which puts the values below 2^16: rounded
+            // to fp16 twice (the factor and the product), half a step of 2^-11 each, like the probabilities
+            // that they meet.  K's scales are left to the scores, in fp32, for the sake of the logarithms.
             constexpr int chunks = DP / 16;
             const uint32_t mine = staging + w * 32 * DP;
             int32_t ahead = look_up(0);
             int64_t off = -1;
-            float next_k = 0.f, next_v = 0.f, scale_k = 0.f, scale_v = 0.f, largest = 7.888609052e-31f;  // 2^-100
-            uint32_t next_mask = 0, mask = 0;
+            float next_k = 0.f, next_v = 0.f, scale_v = 0.f;
+            uint32_t next_mask = 0;
             auto fetch = [&](int u) {
                 if (u < 2 * tiles) {
                     if ((u & 1) == 0) {
@@ -471,39 +475,61 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_kernel(const __grid_
                 __syncwarp();
                 const int stage = u % Shape::stages, tile = u >> 1;
                 if (u >= Shape::stages) fine = __all_sync(0xffffffffu, barrier_wait(empty + 8 * stage, (u / Shape::stages - 1) & 1));
-                if (!fine) break;
+                const uint32_t about = info + (tile % kInfos) * Shape::info;
                 if ((u & 1) == 0) {
-                    // as above, this info's last tile is past its use
-                    scale_k = next_k, scale_v = next_v, mask = next_mask;
+                    // the tile whose mask and scales these replace is past its last use: its V is older than this stage's last copy
+                    const float scale_k = next_k;
+                    scale_v = next_v;
+                    if (lane == 0) asm volatile("st.shared.u32 [%0], %1;" ::"r"(about + 4 * w), "r"(next_mask) : "memory");
+                    asm volatile("st.shared.f32 [%0], %1;" ::"r"(about + 48 + 4 * (w * 32 + lane)), "f"(scale_k) : "memory");
                     fetch_scales(tile + 1);
-                    float most = scale_v;
+                    float most = scale_v;  // a NaN is passed over
 #pragma unroll
                     for (int x = 16; x; x >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, x));
-                    largest = fmaxf(largest, most);
-                    if (scale_v == 0.f) scale_v = largest;  // a row of zeros: its codes are 0 whatever the scale
-                    const uint32_t about = info + (tile % kInfos) * Shape::info;
-                    if (lane == 0) asm volatile("st.shared.u32 [%0], %1;" ::"r"(about + 4 * w), "r"(mask) : "memory");
-                    const uint32_t key = about + 16 + 4 * (w * 32 + lane);
-                    asm volatile("st.shared.f32 [%0], %1;" ::"r"(key), "f"(scale_k) : "memory");
-                    asm volatile("st.shared.f32 [%0], %1;" ::"r"(key + 4 * kTile), "f"(__log2f(scale_v)) : "memory");
-                    asm volatile("st.shared.f32 [%0], %1;" ::"r"(key + 8 * kTile), "f"(__fdividef(1.f, scale_v)) : "memory");
+                    if (lane == 0) asm volatile("st.shared.f32 [%0], %1;" ::"r"(about + 32 + 4 * w), "f"(most) : "memory");
+                    asm volatile("bar.sync 1, 128;" ::: "memory");  // the four warps come here for every tile, whatever a wait said
+                    const float4 all = load_shared_f4(about + 32);
+                    most = fmaxf(fmaxf(all.x, all.y), fmaxf(all.z, all.w));
+                    const int e = most > 0.f ? static_cast<int>(__float_as_uint(most) >> 23) - 127 - 6 : 0;
+                    scale_v *= __uint_as_float(static_cast<uint32_t>(min(max(127 - e, 1), 254)) << 23);
+                    if (w == 0 && lane == 0) asm volatile("st.shared.f32 [%0], %1;" ::"r"(about + 16), "f"(static_cast<float>(e)) : "memory");
                 }
                 const uint32_t from = mine + (u % Shape::staged) * Shape::codes, to = ring + stage * Shape::tile;
+                const uint32_t factor2 = pack2<__half>(scale_v, scale_v);
+                // four 16-byte chunks of codes at a time, loads first
 #pragma unroll
-                for (int i = 0; i < chunks; i++) {
-                    const int idx = i * 32 + lane, rr = idx / chunks, ch = idx % chunks;
-                    uint32_t c[4], x[8];
-                    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(c[0]), "=r"(c[1]), "=r"(c[2]), "=r"(c[3]) : "r"(from + rr * DP + ch * 16));
+                for (int i0 = 0; i0 < chunks && fine; i0 += 4) {
+                    uint32_t c[4][4];
 #pragma unroll
-                    for (int j = 0; j < 4; j++) widen<KIND>(c[j], x[2 * j], x[2 * j + 1]);
-                    // two 16-byte chunks; the lanes of the upper 64 d's write theirs in the other order, into other banks
-                    const bool odd = ch >= 4;
-                    const uint32_t a = to + swizzled(w * 32 + rr, 2 * ch + odd), b = to + swizzled(w * 32 + rr, 2 * ch + !odd);
-                    asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(a), "r"(odd ? x[4] : x[0]), "r"(odd ? x[5] : x[1]), "r"(odd ? x[6] : x[2]), "r"(odd ? x[7] : x[3]) : "memory");
-                    asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(b), "r"(odd ? x[0] : x[4]), "r"(odd ? x[1] : x[5]), "r"(odd ? x[2] : x[6]), "r"(odd ? x[3] : x[7]) : "memory");
+                    for (int i = 0; i < 4; i++) {
+                        const int idx = (i0 + i) * 32 + lane;
+                        asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(c[i][0]), "=r"(c[i][1]), "=r"(c[i][2]), "=r"(c[i][3]) : "r"(from + idx / chunks * DP + idx % chunks * 16));
+                    }
+#pragma unroll
+                    for (int i = 0; i < 4; i++) {
+                        const int idx = (i0 + i) * 32 + lane, rr = idx / chunks, ch = idx % chunks;
+                        // two 16-byte chunks; the lanes of the upper 64 d's write theirs in the other order, into other banks
+                        const bool odd = ch >= 4;
+                        uint32_t x[8];
+                        widen<KIND>(odd ? c[i][2] : c[i][0], x[0], x[1]);
+                        widen<KIND>(odd ? c[i][3] : c[i][1], x[2], x[3]);
+                        widen<KIND>(odd ? c[i][0] : c[i][2], x[4], x[5]);
+                        widen<KIND>(odd ? c[i][1] : c[i][3], x[6], x[7]);
+                        if (u & 1) {
+                            const uint32_t f = __shfl_sync(0xffffffffu, factor2, rr);
+#pragma unroll
+                            for (int j = 0; j < 8; j++) {
+                                const __half2 v = __hmul2(*reinterpret_cast<const __half2 *>(&x[j]), *reinterpret_cast<const __half2 *>(&f));
+                                x[j] = *reinterpret_cast<const uint32_t *>(&v);
+                            }
+                        }
+                        const uint32_t a = to + swizzled(w * 32 + rr, 2 * ch + odd), b = to + swizzled(w * 32 + rr, 2 * ch + !odd);
+                        asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(a), "r"(x[0]), "r"(x[1]), "r"(x[2]), "r"(x[3]) : "memory");
+                        asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(b), "r"(x[4]), "r"(x[5]), "r"(x[6]), "r"(x[7]) : "memory");
+                    }
                 }
                 fence_shared_to_async();
-                barrier_arrive(full + 8 * stage);
+                if (fine) barrier_arrive(full + 8 * stage);
                 __syncwarp();
                 fetch(u + Shape::staged - 1);
             }

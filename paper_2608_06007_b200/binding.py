@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 
 import numpy as np
 
@@ -176,8 +177,8 @@ def load_library(path: str | None = None):
     lib.tc_plan_check_device.restype = C.c_int
     lib.tc_selftest_wait_timeout.argtypes = [vp]
     lib.tc_selftest_wait_timeout.restype = C.c_int
-    for name, args in (("tc_kv_append", tc_kv_append_t), ("tc_kv_gather", tc_kv_gather_t), ("tc_attn_decode", tc_attn_decode_t)):
-        getattr(lib, name).argtypes = [C.POINTER(tc_kv_layer_t), C.POINTER(args), vp]
+    for name in ("tc_kv_append", "tc_kv_gather", "tc_attn_decode"):
+        getattr(lib, name).argtypes = [C.POINTER(tc_kv_layer_t), vp, vp]  # the second: a packed struct as bytes, or byref(args)
         getattr(lib, name).restype = C.c_int
     lib.tc_attn_workspace.argtypes = [C.POINTER(tc_kv_layer_t), C.POINTER(tc_attn_decode_t), C.POINTER(C.c_int64)]
     lib.tc_attn_workspace.restype = C.c_int
@@ -477,43 +478,52 @@ def kv_layer(pool: tc_kv_pool_t, shape, dtype, bases, *, layer=0, scale_pool=Non
     return KVLayer(struct, (bases, scale_bases))
 
 
+# The calls below are made once per layer and step, so their Python is kept short: one pass over each tensor's
+# attributes, and the argument struct packed in one go (the formats are those of the tc_*_t structs above).
 _dtypes = {}
+_APPEND = struct.Struct("=IIqqii4Q8q4Q2q")
+_GATHER = struct.Struct("=IiqqQqqQQQQ4q")
+_DECODE = struct.Struct("=IiqqQQ4qQfiQqqQqQQqQq")
+assert (_APPEND.size, _GATHER.size, _DECODE.size) == (C.sizeof(tc_kv_append_t), C.sizeof(tc_kv_gather_t), C.sizeof(tc_attn_decode_t))
 
 
-def _dtype(t) -> int:
-    """TC_* number of a torch tensor's element type."""
+def _dtype(t):
+    """(TC_* number, bytes) of a torch tensor's element type."""
     if not _dtypes:
         import torch
-        _dtypes.update({torch.bfloat16: TC_BF16, torch.float16: TC_FP16, torch.float32: TC_FP32})
+        _dtypes.update({torch.bfloat16: (TC_BF16, 2), torch.float16: (TC_FP16, 2), torch.float32: (TC_FP32, 4)})
+        _integers.update({torch.int32: 4, torch.uint32: 4, torch.int64: 8, torch.uint64: 8})
     try:
         return _dtypes[t.dtype]
     except KeyError:
         raise ValueError(f"tensors of type {t.dtype} are not taken here") from None
 
 
-def _rows(name, t, n, heads, D):
-    """Byte strides of a [n, heads, D] tensor with contiguous rows."""
-    if tuple(t.shape) != (n, heads, D):
+_integers = {}
+
+
+def _rows(name, t, n, heads, D, dtype, e):
+    """Byte strides of a [n, heads, D] tensor of that type with contiguous rows."""
+    if t.dtype is not dtype and t.dtype != dtype:
+        raise ValueError(f"{name} has type {t.dtype}, expected {dtype}")
+    if t.shape != (n, heads, D):
         raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {(n, heads, D)}")
     s0, s1, s2 = t.stride()
     if s2 != 1 and D > 1:
         raise ValueError(f"{name}: the elements of a row must be contiguous (stride {s2})")
-    e = t.element_size()
-    return _Stride(s0 * e, s1 * e)
+    return s0 * e, s1 * e
 
 
 def _vector(name, t, n, size):
-    """Address of a contiguous device vector of n elements of `size` bytes."""
-    if t is None:
-        return None
-    if t.numel() < n or t.element_size() != size or t.is_floating_point() or not t.is_contiguous():
+    """Address of a contiguous vector of n integers of `size` bytes."""
+    if t is None or t.numel() < n or _integers.get(t.dtype) != size or not t.is_contiguous():
         raise ValueError(f"{name} must hold {n} contiguous integers of {8 * size} bits")
     return t.data_ptr()
 
 
 def _matrix(name, t, rows):
     """(address, width, byte stride) of an int32 [rows, width] table."""
-    if t.dim() != 2 or t.shape[0] < rows or t.element_size() != 4 or t.is_floating_point() or (t.shape[1] > 1 and t.stride(1) != 1):
+    if t.dim() != 2 or t.shape[0] < rows or _integers.get(t.dtype) != 4 or (t.shape[1] > 1 and t.stride(1) != 1):
         raise ValueError(f"{name} must be a matrix of {rows} rows of contiguous 32-bit integers")
     return t.data_ptr(), t.shape[1], t.stride(0) * 4
 
@@ -521,78 +531,85 @@ def _matrix(name, t, rows):
 def tc_kv_append(layer: KVLayer, k, v, slots, *, q=None, q_out=None, positions=None, cos=None, sin=None, interleaved=False, stream=None) -> None:
     """Write tokens' K and V, [n, H, D], into the pool at `slots` (int64, negative = padding), quantised if the
     pool is.  cos, sin ([positions, rot_dim / 2], fp32): rotate K, and q ([n, Hq, D]) into q_out, by row positions[i]."""
-    n = k.shape[0]
-    a = tc_kv_append_t(C.sizeof(tc_kv_append_t), TC_ROPE_INTERLEAVED if interleaved else 0, n, 0, _dtype(k))
-    a.k, a.k_stride = k.data_ptr(), _rows("k", k, n, layer.H, layer.D)
-    a.v, a.v_stride = v.data_ptr(), _rows("v", v, n, layer.H, layer.D)
-    if v.dtype != k.dtype:
-        raise ValueError("k and v differ in type")
+    code, e = _dtype(k)
+    dtype, H, D, n = k.dtype, layer.H, layer.D, k.shape[0]
+    k0, k1 = _rows("k", k, n, H, D, dtype, e)
+    v0, v1 = _rows("v", v, n, H, D, dtype, e)
+    hq = q_at = out_at = q0 = q1 = o0 = o1 = rot = pos_at = cos_at = sin_at = n_pos = row = 0
     if q is not None:
-        if q_out is None or q.dtype != k.dtype or q_out.dtype != k.dtype:
-            raise ValueError("q needs a q_out, and both k's type")
-        a.Hq = q.shape[1]
-        a.q, a.q_stride = q.data_ptr(), _rows("q", q, n, a.Hq, layer.D)
-        a.q_out, a.q_out_stride = q_out.data_ptr(), _rows("q_out", q_out, n, a.Hq, layer.D)
-    a.slots = _vector("slots", slots, n, 8)
+        if q_out is None:
+            raise ValueError("q needs a q_out")
+        hq = q.shape[1]
+        q0, q1 = _rows("q", q, n, hq, D, dtype, e)
+        o0, o1 = _rows("q_out", q_out, n, hq, D, dtype, e)
+        q_at, out_at = q.data_ptr(), q_out.data_ptr()
     if cos is not None:
-        if sin is None or cos.shape != sin.shape or cos.dim() != 2 or cos.element_size() != 4 or sin.element_size() != 4 or cos.stride() != sin.stride() or (cos.shape[1] > 1 and cos.stride(1) != 1):
+        if sin is None:
+            raise ValueError("cos needs a sin")
+        strides = cos.stride()
+        n_pos, half = cos.shape
+        if sin.shape != cos.shape or sin.stride() != strides or _dtypes.get(cos.dtype) != (TC_FP32, 4) or sin.dtype != cos.dtype or (half > 1 and strides[1] != 1):
             raise ValueError("cos and sin must be fp32 matrices of the same shape and strides, with contiguous rows")
-        a.rot_dim = 2 * cos.shape[1]
-        if a.rot_dim:
-            a.positions = _vector("positions", positions, n, 8)
-            a.cos, a.sin, a.n_positions, a.table_stride = cos.data_ptr(), sin.data_ptr(), cos.shape[0], cos.stride(0) * 4
-    _check(load_library().tc_kv_append(layer.ref, C.byref(a), _stream(stream)))
+        if half:
+            rot, row = 2 * half, strides[0] * 4
+            pos_at, cos_at, sin_at = _vector("positions", positions, n, 8), cos.data_ptr(), sin.data_ptr()
+    args = _APPEND.pack(_APPEND.size, TC_ROPE_INTERLEAVED if interleaved else 0, n, hq, code, rot, q_at, out_at, k.data_ptr(), v.data_ptr(), q0, q1, o0, o1, k0, k1, v0, v1,
+                        _vector("slots", slots, n, 8), pos_at, cos_at, sin_at, n_pos, row)
+    rc = load_library().tc_kv_append(layer.ref, args, _stream(stream))
+    if rc:
+        _check(rc)
 
 
 def tc_kv_gather(layer: KVLayer, tables, offsets, k_out=None, v_out=None, *, first=None, stream=None) -> None:
     """Rows offsets[r] .. offsets[r + 1] of k_out and v_out ([rows, H, D]) <- the tokens of request r from first[r]
     (default 0) on, by tables (int32, [R, width]).  offsets: int64 [R + 1]."""
-    R = offsets.shape[0] - 1
-    a = tc_kv_gather_t(C.sizeof(tc_kv_gather_t))
-    for name, t in (("k", k_out), ("v", v_out)):
-        if t is None:
-            continue
-        if a.dtype and (a.dtype != _dtype(t) or a.n_rows != t.shape[0]):
-            raise ValueError("k_out and v_out differ in type or rows")
-        a.dtype, a.n_rows = _dtype(t), t.shape[0]
-        setattr(a, name + "_out", t.data_ptr())
-        setattr(a, name + "_stride", _rows(name + "_out", t, a.n_rows, layer.H, layer.D))
-    a.R = R
-    a.tables, a.table_width, a.table_stride = _matrix("tables", tables, R)
-    a.offsets, a.first = _vector("offsets", offsets, R + 1, 8), _vector("first", first, R, 8)
-    _check(load_library().tc_kv_gather(layer.ref, C.byref(a), _stream(stream)))
-
-
-def _decode_args(q, max_len, max_prefix):
-    return tc_attn_decode_t(C.sizeof(tc_attn_decode_t), _dtype(q), q.shape[0], q.shape[1], max_len=max_len, max_prefix=max_prefix)
+    some = k_out if k_out is not None else v_out
+    if some is None:
+        raise ValueError("k_out or v_out is required")
+    code, e = _dtype(some)
+    dtype, n, H, D, R = some.dtype, some.shape[0], layer.H, layer.D, offsets.shape[0] - 1
+    k0 = k1 = v0 = v1 = k_at = v_at = 0
+    if k_out is not None:
+        k0, k1 = _rows("k_out", k_out, n, H, D, dtype, e)
+        k_at = k_out.data_ptr()
+    if v_out is not None:
+        v0, v1 = _rows("v_out", v_out, n, H, D, dtype, e)
+        v_at = v_out.data_ptr()
+    table, width, step = _matrix("tables", tables, R)
+    args = _GATHER.pack(_GATHER.size, code, R, n, table, width, step, _vector("offsets", offsets, R + 1, 8), 0 if first is None else _vector("first", first, R, 8), k_at, v_at, k0, k1, v0, v1)
+    rc = load_library().tc_kv_gather(layer.ref, args, _stream(stream))
+    if rc:
+        _check(rc)
 
 
 def tc_attn_workspace_bytes(layer: KVLayer, q, *, max_len, max_prefix=0) -> int:
     """Bytes of workspace that tc_attn_decode needs for queries of this shape and these bounds."""
     out = C.c_int64()
-    _check(load_library().tc_attn_workspace(layer.ref, C.byref(_decode_args(q, max_len, max_prefix)), C.byref(out)))
+    args = tc_attn_decode_t(C.sizeof(tc_attn_decode_t), _dtype(q)[0], q.shape[0], q.shape[1], max_len=max_len, max_prefix=max_prefix)
+    _check(load_library().tc_attn_workspace(layer.ref, C.byref(args), C.byref(out)))
     return out.value
 
 
 def tc_attn_decode(layer: KVLayer, q, out, tables, lens, *, max_len, workspace, prefix_table=None, prefix_len=None, max_prefix=0, scale=0.0, lse=None, stream=None) -> None:
     """out[r, h] <- attention of q[r, h] ([R, Hq, D]) over the prefix (prefix_len tokens of prefix_table, read once for
     all requests) and the lens[r] tokens (int32; negative = padding) of tables[r].  lse: fp32 [R, Hq] or None."""
+    code, e = _dtype(q)
+    dtype, D = q.dtype, layer.D
     R, Hq = q.shape[0], q.shape[1]
-    a = _decode_args(q, max_len, max_prefix)
-    a.q, a.q_stride = q.data_ptr(), _rows("q", q, R, Hq, layer.D)
-    if out.dtype != q.dtype:
-        raise ValueError("out must have q's type")
-    a.out, a.out_stride = out.data_ptr(), _rows("out", out, R, Hq, layer.D)
-    a.scale = scale
+    q0, q1 = _rows("q", q, R, Hq, D, dtype, e)
+    o0, o1 = _rows("out", out, R, Hq, D, dtype, e)
+    lse_at = table = width = step = prefix_at = prefix_len_at = 0
     if lse is not None:
-        if tuple(lse.shape) != (R, Hq) or lse.element_size() != 4 or not lse.is_contiguous():
+        if lse.shape != (R, Hq) or _dtypes.get(lse.dtype) != (TC_FP32, 4) or not lse.is_contiguous():
             raise ValueError("lse must be a contiguous fp32 [R, Hq]")
-        a.lse = lse.data_ptr()
+        lse_at = lse.data_ptr()
     if max_len:
-        a.tables, a.table_width, a.table_stride = _matrix("tables", tables, R)
-    a.lens = _vector("lens", lens, R, 4)
+        table, width, step = _matrix("tables", tables, R)
     if max_prefix:
-        a.prefix_table = _vector("prefix_table", prefix_table, -(-max_prefix // layer.B), 4)
-        a.prefix_len = _vector("prefix_len", prefix_len, 1, 4)
-    a.workspace, a.workspace_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
-    _check(load_library().tc_attn_decode(layer.ref, C.byref(a), _stream(stream)))
+        prefix_at = _vector("prefix_table", prefix_table, -(-max_prefix // layer.B), 4)
+        prefix_len_at = _vector("prefix_len", prefix_len, 1, 4)
+    args = _DECODE.pack(_DECODE.size, code, R, Hq, q.data_ptr(), out.data_ptr(), q0, q1, o0, o1, lse_at, scale, 0, table, width, step, _vector("lens", lens, R, 4), max_len,
+                        prefix_at, prefix_len_at, max_prefix, workspace.data_ptr(), workspace.numel() * workspace.element_size())
+    rc = load_library().tc_attn_decode(layer.ref, args, _stream(stream))
+    if rc:
+        _check(rc)

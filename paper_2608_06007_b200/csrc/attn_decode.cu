@@ -175,6 +175,7 @@ __global__ void __launch_bounds__(128, KIND != kPlain && DP <= 128 && NB == 1 ? 
     constexpr int kCols = 8 * NB;
     extern __shared__ __align__(128) unsigned char shared[];
     __shared__ uint32_t sums_of[4], start_at[4], start_off[4];
+    allow_next();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int group = p.split.group;
 
@@ -228,7 +229,7 @@ __global__ void __launch_bounds__(128, KIND != kPlain && DP <= 128 && NB == 1 ? 
     __syncthreads();
     // spread over the SMs first, so that few shares do not meet on few of them
     const uint32_t index = warp * gridDim.x + blockIdx.x;
-    if (static_cast<uint64_t>(index) * share >= total) return;
+    if (static_cast<uint64_t>(index) * share >= total) return await_last();
     const int todo = static_cast<int>(min(share, total - index * share));
 
     const int c = lane & 3, g = lane >> 2, D = p.layer.D;
@@ -595,6 +596,7 @@ __global__ void __launch_bounds__(128, KIND != kPlain && DP <= 128 && NB == 1 ? 
         }
     }
     copy_wait<0>();
+    await_last();  // join_kernel waits for this kernel alone
 }
 
 // The parts' outputs, each by its share of the whole sum, with a running maximum.  WARPS warps take a row, each
@@ -613,10 +615,11 @@ __global__ void __launch_bounds__(WARPS == 1 ? 128 : 32 * WARPS) join_kernel(con
     if (row >= rows) return;
     const bool prefix_streams = p.max_prefix && p.split.prefix_rows == 16, streams = p.split.stream_ctas > 0;
     int32_t own_len = p.lens[quick_div(row, p.div_heads)];
-    uint32_t own_at = streams ? p.before[4 + quick_div(row, p.div_heads)] : 0;
     const int32_t prefix_len = p.max_prefix ? *p.prefix_len : 0;
+    await_last();  // what is read from here on the kernels before this one have written
     const uint4 shares = streams ? *reinterpret_cast<const uint4 *>(p.before) : make_uint4(0, 0, 0, 0);
     const uint32_t prefix_at = prefix_streams ? p.before[4 + p.R] : 0, share = shares.y;
+    uint32_t own_at = streams ? p.before[4 + quick_div(row, p.div_heads)] : 0;
     const FastDiv div_share{shares.z, shares.w};
     const uint32_t prefix_keys = min(max(prefix_len, 0), static_cast<int32_t>(p.max_prefix)), chunk = static_cast<uint32_t>(p.split.prefix_chunk);
     const uint32_t front = p.split.prefix_parts ? (prefix_keys + chunk - 1) / chunk * (p.split.prefix_rows == 128 ? 2 : 1) : 0;
@@ -753,9 +756,7 @@ static int launch_stream(const AttnParams &p, unsigned grid, int device, cudaStr
         if (e != cudaSuccess) return cuda_fail(e, "cudaFuncSetAttribute(dynamic shared memory)");
         raised[device] = true;
     }
-    stream_kernel<T, KIND, DP, NB><<<grid, 128, R::bytes, s>>>(p);
-    const cudaError_t e = cudaGetLastError();
-    return e == cudaSuccess ? TC_OK : cuda_fail(e, "kernel launch");
+    return launch_attn(stream_kernel<T, KIND, DP, NB>, grid, 128, R::bytes, p.split.prefix_parts > 0, p, s);
 }
 
 template <typename T, int KIND, int NB>
@@ -790,15 +791,9 @@ static int launch_decode(const AttnParams &p, int device, cudaStream_t s)
     const int64_t parts = p.split.prefix_parts + p.split.stream_ctas * 4 / std::max<int64_t>(p.R * p.layer.H * p.split.own_blocks, 1);
     const unsigned rows = static_cast<unsigned>(p.split.rows);
     const unsigned few = std::min<unsigned>((rows + 3) / 4, kSms * 5);
-    if (p.layer.D <= 128) {
-        if (parts > 32) join_kernel<T, 128, 16><<<rows, 512, 0, s>>>(p);
-        else join_kernel<T, 128, 1><<<few, 128, 0, s>>>(p);
-    } else {
-        if (parts > 32) join_kernel<T, 256, 16><<<rows, 512, 0, s>>>(p);
-        else join_kernel<T, 256, 1><<<few, 128, 0, s>>>(p);
-    }
-    const cudaError_t e = cudaGetLastError();
-    return e == cudaSuccess ? TC_OK : cuda_fail(e, "kernel launch");
+    const bool follows = p.split.prefix_parts || p.split.stream_ctas;
+    if (p.layer.D <= 128) return parts > 32 ? launch_attn(join_kernel<T, 128, 16>, rows, 512, 0, follows, p, s) : launch_attn(join_kernel<T, 128, 1>, few, 128, 0, follows, p, s);
+    return parts > 32 ? launch_attn(join_kernel<T, 256, 16>, rows, 512, 0, follows, p, s) : launch_attn(join_kernel<T, 256, 1>, few, 128, 0, follows, p, s);
 }
 
 // What both entry points check; fills p's geometry and split.

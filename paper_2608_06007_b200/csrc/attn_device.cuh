@@ -1,6 +1,7 @@
 // Device helpers that the kernels of tc_attn_decode share.
 #pragma once
 
+#include "attn.h"
 #include "ops_device.cuh"
 
 namespace tc {
@@ -16,6 +17,11 @@ __device__ __forceinline__ void copy_async4(uint32_t dst, const void *src, bool 
 }
 __device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N> __device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+// The kernels of one call overlap at their ends: allow_next lets the next one be launched once every CTA of
+// this one has started, await_last waits until the one before is done and its writes are seen.
+__device__ __forceinline__ void allow_next() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void await_last() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
 __device__ __forceinline__ float exp2_approx(float x)
 {
@@ -54,6 +60,24 @@ __device__ __forceinline__ float finite_magnitude(float most, float2 f)
     if (fabsf(f.x) < INFINITY) most = fmaxf(most, fabsf(f.x));
     if (fabsf(f.y) < INFINITY) most = fmaxf(most, fabsf(f.y));
     return most;
+}
+
+// `follows`: a kernel of the same call was launched before this one, which then may start before that one's end.
+template <typename Kernel>
+int launch_attn(Kernel kernel, unsigned grid, unsigned threads, size_t shared, bool follows, const AttnParams &p, cudaStream_t s)
+{
+    cudaLaunchConfig_t config{};
+    config.gridDim = dim3(grid);
+    config.blockDim = dim3(threads);
+    config.dynamicSmemBytes = shared;
+    config.stream = s;
+    cudaLaunchAttribute attribute{};
+    attribute.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attribute.val.programmaticStreamSerializationAllowed = 1;
+    config.attrs = &attribute;
+    config.numAttrs = follows ? 1 : 0;
+    const cudaError_t e = cudaLaunchKernelEx(&config, kernel, p);
+    return e == cudaSuccess ? TC_OK : cuda_fail(e, "kernel launch");
 }
 
 }  // namespace tc

@@ -155,6 +155,7 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_kernel(const __grid_
 {
     using Shape = PrefixShape<KIND, DP, TWO>;
     extern __shared__ unsigned char raw[];
+    allow_next();
     const uint32_t base = (static_cast<uint32_t>(__cvta_generic_to_shared(raw)) + 1023) & ~1023u;
     unsigned char *const gen = raw + (base - static_cast<uint32_t>(__cvta_generic_to_shared(raw)));
     const uint32_t ring = base + Shape::queries, staging = ring + Shape::stages * Shape::tile, info = staging + Shape::staged * Shape::codes, bars = info + kInfos * Shape::info;
@@ -607,9 +608,7 @@ static int launch_prefix_shape(const AttnParams &p, unsigned grid, int device, c
         if (e != cudaSuccess) return cuda_fail(e, "cudaFuncSetAttribute(dynamic shared memory)");
         raised[device] = true;
     }
-    prefix_kernel<T, KIND, DP, TWO><<<grid, kPrefixThreads, Shape::bytes, s>>>(p);
-    const cudaError_t e = cudaGetLastError();
-    return e == cudaSuccess ? TC_OK : cuda_fail(e, "kernel launch");
+    return launch_attn(prefix_kernel<T, KIND, DP, TWO>, grid, kPrefixThreads, Shape::bytes, false, p, s);
 }
 
 template <typename T, int KIND>

@@ -14,7 +14,7 @@
 namespace tc {
 
 constexpr float kLn2 = 0.6931471805599453f;
-constexpr int kLeastShare = 4;  // tiles of 16 keys that a warp of the stream takes at least
+constexpr int kLeastShare = 2;  // tiles of 16 keys that a warp of the stream takes at least
 constexpr int kSms = 148;  // B200; the workspace must not depend on the device that happens to be current
 
 // CTAs of stream_kernel that one SM holds: by shared memory (three stages a warp) and registers.
@@ -256,21 +256,19 @@ __global__ void __launch_bounds__(128, KIND != kPlain && DP <= 128 && NB == 1 ? 
 #pragma unroll
     for (int i = 0; i < R::copies; i++) spot[i] = place_of<KIND, DP>(i * R::rows_per_copy + my_row, my_chunk);
     const int64_t v_from_k = p.layer.v - p.layer.k, copy_step = static_cast<int64_t>(R::rows_per_copy) * p.layer.geo.token;
-    // the block that holds key 16 * l_tile + (lane & 15); -1: not a key
+    // What the table says of key 16 * l_tile + (lane & 15); kNoKey: it is none.  Looked at a tile later, so that nothing
+    // waits for the load.
+    constexpr int32_t kNoKey = INT32_MIN;
     auto look_up = [&]() -> int32_t {
         const int t = 16 * l_tile + (lane & 15);
-        if (l_left <= 0 || t >= l_len) return -1;
+        if (l_left <= 0 || t >= l_len) return kNoKey;
         const uint32_t entry = quick_div(static_cast<uint32_t>(t), p.div_block);
-        int32_t b = -1;
-        if (l_r == p.R || entry < p.table_width) b = l_table[entry];
-        if (b < 0 || b >= p.layer.num_blocks) {
-            atomicOr(p.status, kStatusBadIndex);
-            return -1;
-        }
-        return b;
+        return l_r == p.R || entry < p.table_width ? l_table[entry] : -1;
     };
     // Copies the next tile to stage `to`, its keys' blocks given, and steps on.
-    auto fill = [&](int to, int32_t block) {
+    auto fill = [&](int to, int32_t said) {
+        if (said != kNoKey && (said < 0 || said >= p.layer.num_blocks)) atomicOr(p.status, kStatusBadIndex);
+        const int32_t block = said >= 0 && said < p.layer.num_blocks ? said : -1;
         const uint32_t at = ring + to * R::tile, head = heads + to * R::head;
         const int t = 16 * l_tile + (lane & 15);
         const int n = t - static_cast<int>(quick_div(static_cast<uint32_t>(t), p.div_block)) * static_cast<int>(p.layer.B);

@@ -367,15 +367,16 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_kernel(const __grid_
         // --------------------------------------------------------------------------- the pages
         asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
         const int w = warp - 8;
+        // what the table says of this lane's key of a tile; kNoKey: it is none.  Looked at a tile later
+        constexpr int32_t kNoKey = INT32_MIN;
         auto look_up = [&](int tile) -> int32_t {
             const int t = begin + tile * kTile + w * 32 + lane;
-            if (tile >= tiles || t >= end) return -1;
-            const int32_t b = p.prefix_table[quick_div(static_cast<uint32_t>(t), p.div_block)];
-            if (b < 0 || b >= p.layer.num_blocks) {
-                atomicOr(p.status, kStatusBadIndex);
-                return -1;
-            }
-            return b;
+            return tile < tiles && t < end ? p.prefix_table[quick_div(static_cast<uint32_t>(t), p.div_block)] : kNoKey;
+        };
+        auto checked = [&](int32_t said) -> int32_t {
+            const bool in = said >= 0 && said < p.layer.num_blocks;
+            if (!in && said != kNoKey) atomicOr(p.status, kStatusBadIndex);
+            return in ? said : -1;
         };
         auto place_in_block = [&](int tile) {
             const int t = begin + tile * kTile + w * 32 + lane;
@@ -390,7 +391,7 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_kernel(const __grid_
                 barrier_arrive(full + 8 * (u % Shape::stages));
             };
             for (int tile = 0; tile < tiles && fine; tile++) {
-                const int32_t blk = ahead;
+                const int32_t blk = checked(ahead);
                 ahead = look_up(tile + 1);
                 const int64_t off = blk >= 0 ? p.layer.geo.at(blk, place_in_block(tile), h) : -1;
                 const uint32_t mask = __ballot_sync(0xffffffffu, blk >= 0);
@@ -438,7 +439,7 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_kernel(const __grid_
                 if (u < 2 * tiles) {
                     if ((u & 1) == 0) {
                         const int tile = u >> 1, n = place_in_block(tile);
-                        const int32_t blk = ahead;
+                        const int32_t blk = checked(ahead);
                         ahead = look_up(tile + 1);
                         off = blk >= 0 ? p.layer.geo.at(blk, n, h) : -1;
                     }

@@ -16,10 +16,11 @@ struct AttnSplit {
     int32_t prefix_blocks;     // blocks of that many (of `columns`) of the R * group rows of one KV head
     int32_t prefix_parts;      // parts that prefix_kernel leaves of every row
     int32_t stream_ctas;       // of four warps each
+    int32_t tile_keys;         // keys of a tile of the stream
     int32_t whole_parts;       // prefix_parts, the own keys' part, and that of a prefix in the stream
     int64_t prefix_chunk;      // keys per part of prefix_kernel
     int64_t rows;              // R * Hq
-    int64_t stream_tiles;      // of 16 keys, at most
+    int64_t stream_tiles;      // at most
     int64_t workspace;         // bytes; in it: [whole_parts][rows] sums and [..][D] outputs, [warps][2][columns] sums
     int64_t sums_at, parts_at, piece_sums_at, pieces_at, before_at;  // and [..][D] outputs of pieces, [R + 5] words at `before`
 };

@@ -17,12 +17,12 @@ constexpr float kLn2 = 0.6931471805599453f;
 constexpr int kLeastShare = 2;  // tiles of 16 keys that a warp of the stream takes at least
 constexpr int kSms = 148;  // B200; the workspace must not depend on the device that happens to be current
 
-// CTAs of stream_kernel that one SM holds: by shared memory (three stages a warp) and registers.
+// CTAs of stream_kernel that one SM holds, by shared memory and registers.
 static int stream_ctas(bool quantised, int64_t D, int columns)
 {
-    if (D > 128) return 1 + (quantised && columns == 8);
-    if (D > 64) return quantised && columns == 8 ? 4 : 2;
-    return 4;
+    if (D > 128) return 1;
+    if (D > 64) return quantised && columns == 8 ? 3 : 2;
+    return columns == 8 ? 4 : 2;
 }
 
 void split_attn(int64_t R, int64_t Hq, int64_t H, int64_t D, int64_t max_len, int64_t max_prefix, bool quantised, AttnSplit *s)
@@ -52,7 +52,9 @@ void split_attn(int64_t R, int64_t Hq, int64_t H, int64_t D, int64_t max_len, in
     }
     // The stream's warps: what the GPU holds at once, fewer where not even the longest batch would
     // give each its least share.
-    const int64_t stream_tiles = R * H * s->own_blocks * ((max_len + 15) / 16) + (s->prefix_rows == 16 ? H * s->prefix_blocks * ((max_prefix + 15) / 16) : 0);
+    s->tile_keys = quantised ? 32 : 16;
+    auto tiles_of = [&](int64_t keys) { return (keys + s->tile_keys - 1) / s->tile_keys; };
+    const int64_t stream_tiles = R * H * s->own_blocks * tiles_of(max_len) + (s->prefix_rows == 16 ? H * s->prefix_blocks * tiles_of(max_prefix) : 0);
     s->stream_tiles = stream_tiles;
     const int64_t ctas = std::min<int64_t>(static_cast<int64_t>(kSms) * stream_ctas(quantised, D, s->columns), (stream_tiles + kLeastShare - 1) / kLeastShare);
     s->stream_ctas = static_cast<int32_t>(ctas);
@@ -92,7 +94,7 @@ template <> __device__ __forceinline__ void mma16816<__nv_bfloat16>(float (&c)[4
 }
 
 // ---------------------------------------------------------------------------------- the stream
-// All tiles of 16 keys - of every request, KV head and block of columns in turn, then of a prefix that
+// All tiles of keys - of every request, KV head and block of columns in turn, then of a prefix that
 // few rows share - are one sequence, of which every warp of the grid takes an equal stretch, whatever
 // the lengths.  It has its own ring of stages, filled by 16-byte asynchronous copies whatever the size
 // of the pages, and works alone: the copies run ahead across the ends of items, so that short
@@ -114,15 +116,18 @@ template <> __device__ __forceinline__ void mma16816<__nv_bfloat16>(float (&c)[4
 // per row taken out, so that the row's largest is in [2^14, 2^15): what is then below fp16's smallest
 // step is below 2^-38 of that largest.
 
+// A tile is 16 keys, or 32 for codes, whose widening takes twice the instructions a byte: two groups of 16
+// side by side keep the warps busier than a third more warps would (D = 128, 297k tokens of 4 heads: 62 us against 70).
 template <int KIND, int DP>
 struct Ring {
     static constexpr int esize = KIND == kPlain ? 2 : 1;
+    static constexpr int groups = KIND == kPlain ? 1 : 2, keys = 16 * groups;
     static constexpr int row = DP * esize, chunks = row / 16;  // bytes and 16-byte chunks of a key
-    static constexpr int plane = 16 * row, tile = 2 * plane;   // K, then V
-    static constexpr int head = KIND == kPlain ? 16 : 144;     // {mask and flags, request, item}, then 16 scales of K and of V
-    static constexpr int stages = 3;  // D = 128: two CTAs an SM for 16-bit pools, four for codes
+    static constexpr int plane = 16 * row, group = 2 * plane, tile = groups * group;  // 16 keys' K, then their V
+    static constexpr int head = KIND == kPlain ? 16 : 16 + 8 * keys;  // {mask, flags, request, item}, then scales of K and of V
+    static constexpr int stages = KIND == kPlain ? 3 : 2;  // D = 128: two CTAs an SM for 16-bit pools, three for codes
     static constexpr int bytes = 4 * stages * (tile + head);
-    static constexpr int copies = 16 * chunks / 32, rows_per_copy = 32 / chunks;  // of a plane, by a warp
+    static constexpr int copies = 16 * chunks / 32, rows_per_copy = 32 / chunks;  // of 16 keys, by a warp
 };
 
 // Where chunk c of key r of a tile is staged: no two of the rows that one shared-memory pass serves meet in a
@@ -159,15 +164,16 @@ __device__ __forceinline__ int stream_length(const AttnParams &p, int64_t r, boo
     return static_cast<int>(min(max(len, int64_t(0)), most));
 }
 __device__ __forceinline__ int stream_items(const AttnParams &p, int64_t r) { return p.layer.H * (r < p.R ? p.split.own_blocks : p.split.prefix_blocks); }
+__device__ __forceinline__ uint32_t tiles_of(const AttnParams &p, uint32_t keys) { return p.split.tile_keys == 16 ? (keys + 15) >> 4 : (keys + 31) >> 5; }
 // Tiles that each warp takes of `total` (below 2^31): warp w has [w * share, (w + 1) * share).
 __device__ __forceinline__ uint32_t stream_share(const AttnParams &p, uint32_t total) { return max((total + p.split.stream_ctas * 4 - 1) / (p.split.stream_ctas * 4), static_cast<uint32_t>(kLeastShare)); }
-__device__ __forceinline__ uint32_t stream_tiles(const AttnParams &p, int64_t r, bool tell) { return static_cast<uint32_t>((stream_length(p, r, tell) + 15) >> 4) * stream_items(p, r); }
+__device__ __forceinline__ uint32_t stream_tiles(const AttnParams &p, int64_t r, bool tell) { return tiles_of(p, stream_length(p, r, tell)) * stream_items(p, r); }
 
-enum : uint32_t { kFirst = 1u << 16, kLast = 1u << 17, kWhole = 1u << 18, kSecond = 1u << 19 };
+enum : uint32_t { kFirst = 1, kLast = 2, kWhole = 4, kSecond = 8 };
 
 // T: the type of the products - the queries' for a plain pool, fp16 for a quantised one, which looks at p.q_bf16.
 template <typename T, int KIND, int DP, int NB>
-__global__ void __launch_bounds__(128, KIND != kPlain && DP <= 128 && NB == 1 ? 4 : 2) stream_kernel(const __grid_constant__ AttnParams p)
+__global__ void __launch_bounds__(128, DP > 128 ? 1 : NB > 1 ? 2 : DP == 64 ? 4 : KIND == kPlain ? 2 : 3) stream_kernel(const __grid_constant__ AttnParams p)
 {
     using R = Ring<KIND, DP>;
     using ST = std::conditional_t<KIND == kPlain, T, __half>;
@@ -235,11 +241,11 @@ __global__ void __launch_bounds__(128, KIND != kPlain && DP <= 128 && NB == 1 ? 
     const int c = lane & 3, g = lane >> 2, D = p.layer.D;
     const uint32_t ring = static_cast<uint32_t>(__cvta_generic_to_shared(shared)) + warp * R::stages * R::tile;
     const uint32_t heads = static_cast<uint32_t>(__cvta_generic_to_shared(shared)) + 4 * R::stages * R::tile + warp * R::stages * R::head;
-    const bool one_block = p.layer.B % 16 == 0;  // a tile's keys lie in one block
+    const bool one_block = p.layer.B % 16 == 0;  // 16 keys lie in one block
 
     // The next tile to be copied: tile `l_tile` of `l_tiles` of item `l_item` of request l_r.
     int64_t l_r = start_at[warp];
-    int l_len = stream_length(p, l_r, false), l_tiles = (l_len + 15) >> 4;
+    int l_len = stream_length(p, l_r, false), l_tiles = static_cast<int>(tiles_of(p, l_len));
     int l_item = static_cast<int>(start_off[warp] / l_tiles), l_tile = static_cast<int>(start_off[warp] - l_item * l_tiles);
     const int32_t *l_table = l_r < p.R ? reinterpret_cast<const int32_t *>(p.tables + l_r * p.table_stride) : p.prefix_table;
     auto head_of = [&](int64_t r, int item) {
@@ -256,11 +262,12 @@ __global__ void __launch_bounds__(128, KIND != kPlain && DP <= 128 && NB == 1 ? 
 #pragma unroll
     for (int i = 0; i < R::copies; i++) spot[i] = place_of<KIND, DP>(i * R::rows_per_copy + my_row, my_chunk);
     const int64_t v_from_k = p.layer.v - p.layer.k, copy_step = static_cast<int64_t>(R::rows_per_copy) * p.layer.geo.token;
-    // What the table says of key 16 * l_tile + (lane & 15); kNoKey: it is none.  Looked at a tile later, so that nothing
+    // What the table says of the tile's key of this lane; kNoKey: it is none.  Looked at a tile later, so that nothing
     // waits for the load.
     constexpr int32_t kNoKey = INT32_MIN;
+    const int my_key = lane % R::keys;
     auto look_up = [&]() -> int32_t {
-        const int t = 16 * l_tile + (lane & 15);
+        const int t = R::keys * l_tile + my_key;
         if (l_left <= 0 || t >= l_len) return kNoKey;
         const uint32_t entry = quick_div(static_cast<uint32_t>(t), p.div_block);
         return l_r == p.R || entry < p.table_width ? l_table[entry] : -1;
@@ -270,40 +277,45 @@ __global__ void __launch_bounds__(128, KIND != kPlain && DP <= 128 && NB == 1 ? 
         if (said != kNoKey && (said < 0 || said >= p.layer.num_blocks)) atomicOr(p.status, kStatusBadIndex);
         const int32_t block = said >= 0 && said < p.layer.num_blocks ? said : -1;
         const uint32_t at = ring + to * R::tile, head = heads + to * R::head;
-        const int t = 16 * l_tile + (lane & 15);
+        const int t = R::keys * l_tile + my_key;
         const int n = t - static_cast<int>(quick_div(static_cast<uint32_t>(t), p.div_block)) * static_cast<int>(p.layer.B);
         const int h = head_of(l_r, l_item);
-        const uint32_t mask = __ballot_sync(0xffffffffu, block >= 0) & 0xffffu;
+        const uint32_t mask = __ballot_sync(0xffffffffu, block >= 0);
         const bool end = l_tile + 1 == l_tiles, last = end || l_left == 1;
         if (lane == 0)
             asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(head),
-                         "r"(mask | (l_first ? kFirst : 0u) | (last ? kLast : 0u) | (last && end && l_from_start ? kWhole : 0u) | (l_second ? kSecond : 0u)), "r"(static_cast<uint32_t>(l_r)), "r"(l_item), "r"(0)
+                         "r"(mask), "r"((l_first ? kFirst : 0u) | (last ? kLast : 0u) | (last && end && l_from_start ? kWhole : 0u) | (l_second ? kSecond : 0u)), "r"(static_cast<uint32_t>(l_r)), "r"(l_item)
                          : "memory");
-        if (one_block) {
-            // a fixed step from key to key
-            const int n0 = __shfl_sync(0xffffffffu, n, 0), b0 = __shfl_sync(0xffffffffu, block, 0);
-            const char *k = p.layer.k + p.layer.geo.at(max(b0, 0), n0 + my_row, h) + my_chunk * 16;
-            const uint32_t rows = in_row ? mask >> my_row : 0u;
 #pragma unroll
-            for (int i = 0; i < R::copies; i++, k += copy_step) {
-                const bool there = rows >> (i * R::rows_per_copy) & 1;
-                copy_async16(at + spot[i], k, there);  // where it is not there, nothing is read
-                copy_async16(at + spot[i] + R::plane, k + v_from_k, there);
-            }
-        } else {
-            const int64_t off = block >= 0 ? p.layer.geo.at(block, n, h) : -1;
+        for (int sub = 0; sub < R::groups; sub++) {
+            const uint32_t dst = at + sub * R::group;
+            if (one_block) {
+                // a fixed step from key to key
+                const int n0 = __shfl_sync(0xffffffffu, n, 16 * sub), b0 = __shfl_sync(0xffffffffu, block, 16 * sub);
+                const char *k = p.layer.k + p.layer.geo.at(max(b0, 0), n0 + my_row, h) + my_chunk * 16;
+                const uint32_t rows = in_row ? mask >> (16 * sub + my_row) : 0u;
 #pragma unroll
-            for (int i = 0; i < R::copies; i++) {
-                const int64_t src = __shfl_sync(0xffffffffu, off, i * R::rows_per_copy + my_row);
-                const bool there = src >= 0 && in_row;
-                const char *k = p.layer.k + (there ? src + my_chunk * 16 : 0);
-                copy_async16(at + spot[i], k, there);
-                copy_async16(at + spot[i] + R::plane, k + v_from_k, there);
+                for (int i = 0; i < R::copies; i++, k += copy_step) {
+                    const bool there = rows >> (i * R::rows_per_copy) & 1;
+                    copy_async16(dst + spot[i], k, there);  // where it is not there, nothing is read
+                    copy_async16(dst + spot[i] + R::plane, k + v_from_k, there);
+                }
+            } else {
+                const int64_t off = block >= 0 ? p.layer.geo.at(block, n, h) : -1;
+#pragma unroll
+                for (int i = 0; i < R::copies; i++) {
+                    const int64_t src = __shfl_sync(0xffffffffu, off, 16 * sub + i * R::rows_per_copy + my_row);
+                    const bool there = src >= 0 && in_row;
+                    const char *k = p.layer.k + (there ? src + my_chunk * 16 : 0);
+                    copy_async16(dst + spot[i], k, there);
+                    copy_async16(dst + spot[i] + R::plane, k + v_from_k, there);
+                }
             }
         }
         if constexpr (KIND != kPlain) {
             const int64_t from = block >= 0 ? p.layer.scale_geo.at(block, n, h) : 0;
-            copy_async4(head + 16 + lane * 4, reinterpret_cast<const char *>(lane < 16 ? p.layer.k_scale : p.layer.v_scale) + from, block >= 0);
+            copy_async4(head + 16 + lane * 4, reinterpret_cast<const char *>(p.layer.k_scale) + from, block >= 0);
+            copy_async4(head + 16 + 4 * R::keys + lane * 4, reinterpret_cast<const char *>(p.layer.v_scale) + from, block >= 0);
         }
         l_left--;
         l_first = last;
@@ -322,7 +334,7 @@ __global__ void __launch_bounds__(128, KIND != kPlain && DP <= 128 && NB == 1 ? 
                     l_len = __shfl_sync(0xffffffffu, len, at_lane);
                     break;
                 }
-                l_tiles = (l_len + 15) >> 4;
+                l_tiles = static_cast<int>(tiles_of(p, l_len));
                 l_table = l_r < p.R ? reinterpret_cast<const int32_t *>(p.tables + l_r * p.table_stride) : p.prefix_table;
             }
         }
@@ -401,17 +413,24 @@ __global__ void __launch_bounds__(128, KIND != kPlain && DP <= 128 && NB == 1 ? 
     load_queries(start_at[warp], first_item, qf);
 
     float o[NB][DP / 16][4], top[NB][2], sum[NB][2];
-    float largest = 0.f;  // codes: the largest scale of V so far
-    // this lane's keys of a tile, rows g and g + 8 of S'
+    float largest = 0.f;  // codes: a scale of V for rows that have none
+    // this lane's keys of 16, rows g and g + 8 of S'
     const int key0 = KIND == kPlain ? g : 4 * (g >> 1) + (g & 1), key1 = KIND == kPlain ? g + 8 : key0 + 2;
     int stage = 0, next_fill = R::stages - 1;
     for (int i = 0; i < todo; i++) {
         copy_wait<R::stages - 2>();
-        __syncwarp();
+        __syncwarp();  // every lane is done with the tile before, whose stage is filled again
+        if (l_left > 0) {
+            fill(next_fill, ahead);
+            ahead = look_up();
+        }
+        copy_commit();
+        next_fill = next_fill + 1 == R::stages ? 0 : next_fill + 1;
+        __syncwarp();  // with two stages that was the next tile, whose head is looked at below
         const uint32_t at = ring + stage * R::tile, head_at = heads + stage * R::head;
-        uint32_t head, head_r, head_item, unused;
-        asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(head), "=r"(head_r), "=r"(head_item), "=r"(unused) : "r"(head_at));
-        if (head & kFirst) {
+        uint32_t mask, flags, head_r, head_item;
+        asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(mask), "=r"(flags), "=r"(head_r), "=r"(head_item) : "r"(head_at));
+        if (flags & kFirst) {
             take_queries();
             largest = 7.888609052e-31f;  // 2^-100
 #pragma unroll
@@ -422,71 +441,99 @@ __global__ void __launch_bounds__(128, KIND != kPlain && DP <= 128 && NB == 1 ? 
             }
         }
 
-        // s: keys g (0, 1) and g + 8 (2, 3) x columns 2c, 2c + 1
-        float s[NB][4] = {};
+        // s: keys key0 (0, 1) and key1 (2, 3) of each 16 x columns 2c, 2c + 1
+        float s[R::groups][NB][4] = {};
         if constexpr (KIND == kPlain) {
 #pragma unroll
             for (int ks = 0; ks < DP / 16; ks++) {
                 uint32_t a[4];
                 load_matrix4<false>(at + place_of<KIND, DP>(lane & 15, 2 * ks + (lane >> 4)), a);
 #pragma unroll
-                for (int nb = 0; nb < NB; nb++) mma16816<ST>(s[nb], a, qf[nb][ks][0], qf[nb][ks][1]);
+                for (int nb = 0; nb < NB; nb++) mma16816<ST>(s[0][nb], a, qf[nb][ks][0], qf[nb][ks][1]);
             }
         } else {
             const int i = lane & 7, key = 4 * (i >> 1) + (i & 1) + ((lane >> 2) & 2);
 #pragma unroll
             for (int ks = 0; ks < DP / 16; ks += 2) {
-                uint32_t w[4];  // chunk ks: rows g and g + 8; chunk ks + 1
-                load_matrix4<false>(at + place_of<KIND, DP>(key, ks + (lane >> 4)), w);
+                const uint32_t from = at + place_of<KIND, DP>(key, ks + (lane >> 4));
+                uint32_t w[R::groups][4];  // chunk ks: rows g and g + 8; chunk ks + 1
 #pragma unroll
-                for (int j = 0; j < 2; j++) {
-                    uint32_t a[4];
-                    widen<KIND>(w[2 * j], a[0], a[2]);
-                    widen<KIND>(w[2 * j + 1], a[1], a[3]);
+                for (int sub = 0; sub < R::groups; sub++) load_matrix4<false>(from + sub * R::group, w[sub]);
 #pragma unroll
-                    for (int nb = 0; nb < NB; nb++) mma16816<ST>(s[nb], a, qf[nb][ks + j][0], qf[nb][ks + j][1]);
-                }
+                for (int j = 0; j < 2; j++)
+#pragma unroll
+                    for (int sub = 0; sub < R::groups; sub++) {
+                        uint32_t a[4];
+                        widen<KIND>(w[sub][2 * j], a[0], a[2]);
+                        widen<KIND>(w[sub][2 * j + 1], a[1], a[3]);
+#pragma unroll
+                        for (int nb = 0; nb < NB; nb++) mma16816<ST>(s[sub][nb], a, qf[nb][ks + j][0], qf[nb][ks + j][1]);
+                    }
             }
         }
         // An item's last scores are taken: its queries make room for the next one's, loaded while this tile ends.
-        if ((head & kLast) && i + 1 < todo) {
+        if ((flags & kLast) && i + 1 < todo) {
             const uint32_t next = heads + (stage + 1 == R::stages ? 0 : stage + 1) * R::head;
-            uint32_t flags, r, item, none;
-            asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(flags), "=r"(r), "=r"(item), "=r"(none) : "r"(next));
+            uint32_t next_mask, next_flags, r, item;
+            asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(next_mask), "=r"(next_flags), "=r"(r), "=r"(item) : "r"(next));
             load_queries(r, static_cast<int>(item), qf);
         }
 
-        float k_scale[2] = {1.f, 1.f}, v_log[2] = {0.f, 0.f}, v_inverse[2] = {1.f, 1.f};
+        float k_scale[R::groups][2], v_log[R::groups][2], v_inverse[R::groups][2];
         if constexpr (KIND != kPlain) {
-            float v[2];
+            float v[R::groups][2], here = 0.f;
 #pragma unroll
-            for (int j = 0; j < 2; j++) {
-                asm volatile("ld.shared.f32 %0, [%1];" : "=f"(k_scale[j]) : "r"(head_at + 16 + (j ? key1 : key0) * 4));
-                asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v[j]) : "r"(head_at + 80 + (j ? key1 : key0) * 4));
+            for (int sub = 0; sub < R::groups; sub++)
+#pragma unroll
+                for (int j = 0; j < 2; j++) {
+                    const uint32_t key = head_at + 16 + (16 * sub + (j ? key1 : key0)) * 4;
+                    asm volatile("ld.shared.f32 %0, [%1];" : "=f"(k_scale[sub][j]) : "r"(key));
+                    asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v[sub][j]) : "r"(key + 4 * R::keys));
+                }
+            bool zero = false;
+#pragma unroll
+            for (int sub = 0; sub < R::groups; sub++)
+#pragma unroll
+                for (int j = 0; j < 2; j++) zero = zero || v[sub][j] == 0.f;
+            if (__any_sync(0xffffffffu, zero)) {
+                // a row of zeros, or no key: its codes are 0 whatever the scale; one like its neighbours'
+#pragma unroll
+                for (int sub = 0; sub < R::groups; sub++) here = fmaxf(here, fmaxf(v[sub][0], v[sub][1]));
+#pragma unroll
+                for (int x = 4; x < 32; x <<= 1) here = fmaxf(here, __shfl_xor_sync(0xffffffffu, here, x));
+                if (here > 0.f) largest = here;
+#pragma unroll
+                for (int sub = 0; sub < R::groups; sub++)
+#pragma unroll
+                    for (int j = 0; j < 2; j++)
+                        if (v[sub][j] == 0.f) v[sub][j] = largest;
             }
-            float here = fmaxf(v[0], v[1]);
 #pragma unroll
-            for (int x = 4; x < 32; x <<= 1) here = fmaxf(here, __shfl_xor_sync(0xffffffffu, here, x));
-            largest = fmaxf(largest, here);
+            for (int sub = 0; sub < R::groups; sub++)
 #pragma unroll
-            for (int j = 0; j < 2; j++) {
-                if (v[j] == 0.f) v[j] = largest;  // a row of zeros: its codes are 0 whatever the scale
-                v_log[j] = __log2f(v[j]);
-                v_inverse[j] = __fdividef(1.f, v[j]);
-            }
+                for (int j = 0; j < 2; j++) v_log[sub][j] = __log2f(v[sub][j]), v_inverse[sub][j] = __fdividef(1.f, v[sub][j]);
         }
         float most[NB][2];
         bool move = false;
-        const bool key[2] = {(head >> key0 & 1) != 0, (head >> key1 & 1) != 0};
 #pragma unroll
-        for (int nb = 0; nb < NB; nb++)
+        for (int nb = 0; nb < NB; nb++) most[nb][0] = most[nb][1] = -INFINITY;
 #pragma unroll
-            for (int j = 0; j < 2; j++) {
-                s[nb][j] = key[0] ? (KIND == kPlain ? s[nb][j] * factor[nb][j] : fmaf(s[nb][j], factor[nb][j] * k_scale[0], v_log[0])) : -INFINITY;
-                s[nb][j + 2] = key[1] ? (KIND == kPlain ? s[nb][j + 2] * factor[nb][j] : fmaf(s[nb][j + 2], factor[nb][j] * k_scale[1], v_log[1])) : -INFINITY;
-                most[nb][j] = fmaxf(s[nb][j], s[nb][j + 2]);
-                move = move || most[nb][j] > top[nb][j] + 8.f;
-            }
+        for (int sub = 0; sub < R::groups; sub++) {
+            const bool key[2] = {(mask >> (16 * sub + key0) & 1) != 0, (mask >> (16 * sub + key1) & 1) != 0};
+#pragma unroll
+            for (int nb = 0; nb < NB; nb++)
+#pragma unroll
+                for (int j = 0; j < 2; j++) {
+                    float &a = s[sub][nb][j], &b = s[sub][nb][j + 2];
+                    if constexpr (KIND == kPlain) a *= factor[nb][j], b *= factor[nb][j];
+                    else a = fmaf(a, factor[nb][j] * k_scale[sub][0], v_log[sub][0]), b = fmaf(b, factor[nb][j] * k_scale[sub][1], v_log[sub][1]);
+                    if (!key[0]) a = -INFINITY;
+                    if (!key[1]) b = -INFINITY;
+                    most[nb][j] = fmaxf(most[nb][j], fmaxf(a, b));
+                }
+        }
+#pragma unroll
+        for (int nb = 0; nb < NB; nb++) move = move || most[nb][0] > top[nb][0] + 8.f || most[nb][1] > top[nb][1] + 8.f;
         // A running maximum moves only when a score exceeds it by more than 8 (2^8 in probabilities): up
         // to there they stay small enough for either 16-bit type and the outputs need no rescaling.
         if (__any_sync(0xffffffffu, move)) {
@@ -506,15 +553,22 @@ __global__ void __launch_bounds__(128, KIND != kPlain && DP <= 128 && NB == 1 ? 
                 for (int k = 0; k < DP / 16; k++) o[nb][k][0] *= f[0], o[nb][k][1] *= f[1], o[nb][k][2] *= f[0], o[nb][k][3] *= f[1];
             }
         }
-        uint32_t pf[NB][2];
+        uint32_t pf[R::groups][NB][2];
 #pragma unroll
         for (int nb = 0; nb < NB; nb++) {
             const float m0 = top[nb][0] == -INFINITY ? 0.f : top[nb][0], m1 = top[nb][1] == -INFINITY ? 0.f : top[nb][1];
-            const float e0 = exp2_approx(s[nb][0] - m0), e1 = exp2_approx(s[nb][1] - m1), e2 = exp2_approx(s[nb][2] - m0), e3 = exp2_approx(s[nb][3] - m1);
-            if constexpr (KIND == kPlain) sum[nb][0] += e0 + e2, sum[nb][1] += e1 + e3;
-            else sum[nb][0] = fmaf(e0, v_inverse[0], fmaf(e2, v_inverse[1], sum[nb][0])), sum[nb][1] = fmaf(e1, v_inverse[0], fmaf(e3, v_inverse[1], sum[nb][1]));
-            pf[nb][0] = transposed(pack2<VT>(e0, e1));
-            pf[nb][1] = transposed(pack2<VT>(e2, e3));
+#pragma unroll
+            for (int sub = 0; sub < R::groups; sub++) {
+                const float e0 = exp2_approx(s[sub][nb][0] - m0), e1 = exp2_approx(s[sub][nb][1] - m1), e2 = exp2_approx(s[sub][nb][2] - m0), e3 = exp2_approx(s[sub][nb][3] - m1);
+                if constexpr (KIND == kPlain) {
+                    sum[nb][0] += e0 + e2, sum[nb][1] += e1 + e3;
+                } else {
+                    sum[nb][0] = fmaf(e0, v_inverse[sub][0], fmaf(e2, v_inverse[sub][1], sum[nb][0]));
+                    sum[nb][1] = fmaf(e1, v_inverse[sub][0], fmaf(e3, v_inverse[sub][1], sum[nb][1]));
+                }
+                pf[sub][nb][0] = transposed(pack2<VT>(e0, e1));
+                pf[sub][nb][1] = transposed(pack2<VT>(e2, e3));
+            }
         }
 
         if constexpr (KIND == kPlain) {
@@ -523,38 +577,35 @@ __global__ void __launch_bounds__(128, KIND != kPlain && DP <= 128 && NB == 1 ? 
                 uint32_t a[4];  // d's 16k .. + 7 and + 8 .., keys 0-7 and 8-15
                 load_matrix4<true>(at + R::plane + place_of<KIND, DP>((lane & 7) + ((lane >> 4) << 3), 2 * k + ((lane >> 3) & 1)), a);
 #pragma unroll
-                for (int nb = 0; nb < NB; nb++) mma16816<VT>(o[nb][k], a, pf[nb][0], pf[nb][1]);
+                for (int nb = 0; nb < NB; nb++) mma16816<VT>(o[nb][k], a, pf[0][nb][0], pf[0][nb][1]);
             }
         } else {
 #pragma unroll
             for (int k = 0; k < DP / 16; k += 2) {
-                uint32_t w[4];
-                load_codes_transposed(at + R::plane + place_of<KIND, DP>(lane & 15, k + (lane >> 4)), w);
+                const uint32_t from = at + R::plane + place_of<KIND, DP>(lane & 15, k + (lane >> 4));
+                uint32_t w[R::groups][4];
 #pragma unroll
-                for (int j = 0; j < 2; j++) {
-                    uint32_t a[4];
-                    widen<KIND>(w[2 * j], a[0], a[2]);
-                    widen<KIND>(w[2 * j + 1], a[1], a[3]);
+                for (int sub = 0; sub < R::groups; sub++) load_codes_transposed(from + sub * R::group, w[sub]);
 #pragma unroll
-                    for (int nb = 0; nb < NB; nb++) mma16816<VT>(o[nb][k + j], a, pf[nb][0], pf[nb][1]);
-                }
+                for (int sub = 0; sub < R::groups; sub++)
+#pragma unroll
+                    for (int j = 0; j < 2; j++) {
+                        uint32_t a[4];
+                        widen<KIND>(w[sub][2 * j], a[0], a[2]);
+                        widen<KIND>(w[sub][2 * j + 1], a[1], a[3]);
+#pragma unroll
+                        for (int nb = 0; nb < NB; nb++) mma16816<VT>(o[nb][k + j], a, pf[sub][nb][0], pf[sub][nb][1]);
+                    }
             }
         }
-        __syncwarp();
-        if (l_left > 0) {
-            fill(next_fill, ahead);
-            ahead = look_up();
-        }
-        copy_commit();
-        next_fill = next_fill + 1 == R::stages ? 0 : next_fill + 1;
         stage = stage + 1 == R::stages ? 0 : stage + 1;
 
-        if (head & kLast) {
+        if (flags & kLast) {
             // The item's part of the keys: a whole part, or one of this warp's two pieces.
             const Item it = item_of(head_r, static_cast<int>(head_item));
-            const bool whole = head & kWhole;
+            const bool whole = flags & kWhole;
             const int64_t slot = p.split.whole_parts - 1 - (head_r < p.R && p.max_prefix > 0 && p.split.prefix_rows == 16);  // own keys, then the prefix
-            const int64_t piece = (static_cast<int64_t>(index) * 2 + (head & kSecond ? 1 : 0)) * kCols;
+            const int64_t piece = (static_cast<int64_t>(index) * 2 + (flags & kSecond ? 1 : 0)) * kCols;
 #pragma unroll
             for (int nb = 0; nb < NB; nb++)
 #pragma unroll
@@ -640,7 +691,7 @@ __global__ void __launch_bounds__(WARPS == 1 ? 128 : 32 * WARPS) join_kernel(con
         if (len < 0) continue;
         auto left = [&](uint32_t keys, uint32_t begin, uint32_t in_q, uint32_t blocks, uint32_t whole_slot) {
             Left l{0, 0, 0, false};
-            const uint32_t tiles = (keys + 15) >> 4, columns = p.split.columns, block = blocks > 1 ? in_q / columns : 0, col = in_q - block * columns;
+            const uint32_t tiles = tiles_of(p, keys), columns = p.split.columns, block = blocks > 1 ? in_q / columns : 0, col = in_q - block * columns;
             if (!tiles) return l;
             const uint32_t first = begin + (h * blocks + block) * tiles, w0 = quick_div(first, div_share), w1 = quick_div(first + tiles - 1, div_share);
             l.count = w1 - w0 + 1;

@@ -187,10 +187,12 @@ __device__ __forceinline__ void store_chunk(char *p, const Pairs &x, int half)
 }
 
 // Rows whose D is a multiple of 8 and whose addresses are multiples of 16 bytes; rot_dim a multiple of 16.
+// A token's threads hold one row of K or V each and kQueries of Q, all loaded before slot and position
+// are known; as many threads as K and V have rows (up to 256) leave nothing idle.
 template <typename T, bool INTERLEAVED, bool QUANTISED>
 __global__ void __launch_bounds__(256, sizeof(T) == 4 ? 2 : 3) append_vector_kernel(const __grid_constant__ AppendParams p)
 {
-    constexpr int kRows = 3;  // rows in flight
+    constexpr int kQueries = sizeof(T) == 4 ? 2 : 4;
     const int tpt = p.threads_per_token, lt = threadIdx.x & (tpt - 1);
     const int64_t token = static_cast<int64_t>(blockIdx.x) * (blockDim.x / tpt) + threadIdx.x / tpt;
     if (token >= p.n_tokens) return;
@@ -202,21 +204,21 @@ __global__ void __launch_bounds__(256, sizeof(T) == 4 ? 2 : 3) append_vector_ker
     if (!INTERLEAVED && pair < turned) a = 8 * pair, b = a + p.rot / 2;
     else a = 16 * pair, b = a + 8;
     const bool has_a = a < D, has_b = b < D;
-    const int rows = 2 * H + p.Hq, step = tpt >> p.log2_lanes, first = lt >> p.log2_lanes;
-    using Rows = Chunk<T>[kRows][2];
-    auto load_rows = [&](int base, Rows &in) {  // waits for neither slot nor position
-#pragma unroll
-        for (int u = 0; u < kRows; u++) {
-            const int row = base + first + u * step;
-            in[u][0] = Chunk<T>{}, in[u][1] = Chunk<T>{};
-            if (row >= rows) continue;
-            const char *src = row_source(p, row, token);
-            if (has_a) load_chunk<T>(src + a * static_cast<int>(sizeof(T)), in[u][0]);
-            if (has_b) load_chunk<T>(src + b * static_cast<int>(sizeof(T)), in[u][1]);
-        }
+    const int step = tpt >> p.log2_lanes, first = lt >> p.log2_lanes;
+    constexpr int e = static_cast<int>(sizeof(T));
+    auto load_row = [&](const char *src, bool there, Chunk<T> (&in)[2]) {
+        in[0] = Chunk<T>{}, in[1] = Chunk<T>{};
+        if (there && has_a) load_chunk<T>(src + a * e, in[0]);
+        if (there && has_b) load_chunk<T>(src + b * e, in[1]);
     };
-    Rows in;
-    load_rows(0, in);
+    auto kv_source = [&](int row) { return row < H ? p.k + token * p.k_tok + row * p.k_head : p.v + token * p.v_tok + (row - H) * p.v_head; };
+    Chunk<T> kv[2], q[kQueries][2];
+    load_row(kv_source(first), first < 2 * H, kv);
+    const char *q_src = p.q + token * p.q_tok + first * p.q_head;
+    const int64_t q_step = step * p.q_head, o_step = step * p.o_head;
+#pragma unroll
+    for (int u = 0; u < kQueries; u++) load_row(q_src + u * q_step, first + u * step < p.Hq, q[u]);
+
     int64_t block;
     int32_t n;
     if (!token_target(p, slot, pos, &block, &n)) return;  // one token's threads are whole warps
@@ -225,85 +227,86 @@ __global__ void __launch_bounds__(256, sizeof(T) == 4 ? 2 : 3) append_vector_ker
         load_floats<float, 8>(p.cos + pos * p.table_stride + 32 * pair, reinterpret_cast<float *>(c));
         load_floats<float, 8>(p.sin + pos * p.table_stride + 32 * pair, reinterpret_cast<float *>(s));
     }
-    const int64_t place = p.layer.geo.at(block, n, 0), scale_place = QUANTISED ? p.layer.scale_geo.at(block, n, 0) : 0;
     const float2 zero = make_float2(p.minus_zero, p.minus_zero);
-    auto work = [&](int base) {
+    auto rotate = [&](Pairs &x) {
 #pragma unroll
-        for (int u = 0; u < kRows; u++) {
-            const int row = base + first + u * step;
-            if (base + (first & ~(32 / lanes - 1)) + u * step >= rows) break;  // nothing for the whole warp
-            Pairs x;
-            widen_chunks<T, INTERLEAVED>(in[u], x);
-            if (pair < turned && (row < H || row >= 2 * H)) {
-#pragma unroll
-                for (int i = 0; i < 4; i++) {
-                    const float2 xs = fma2(x.lo[i], s[i], zero), ys = fma2(x.hi[i], s[i], zero);
-                    x.lo[i] = add2(fma2(x.lo[i], c[i], zero), make_float2(-ys.x, -ys.y));
-                    x.hi[i] = add2(fma2(x.hi[i], c[i], zero), xs);
-                }
-            }
-            float scale = 0.f;
-            if constexpr (QUANTISED) {
-                // lanes of K or V rows need their partners; a warp of query rows alone skips this
-                if (__any_sync(0xffffffffu, row < 2 * H)) {
-                    float most = 0.f;
-#pragma unroll
-                    for (int i = 0; i < 4; i++)
-                        most = larger(larger(larger(most, fabsf(x.lo[i].x)), fabsf(x.lo[i].y)), larger(fabsf(x.hi[i].x), fabsf(x.hi[i].y)));
-                    for (int m = 1; m < lanes; m <<= 1) most = larger(most, __shfl_xor_sync(0xffffffffu, most, m));
-                    scale = row_scale(__float_as_uint(most), p.layer.dtype);
-                }
-            }
-            if (row >= rows) continue;
-            if (row >= 2 * H) {
-                char *dst = p.q_out + token * p.o_tok + (row - 2 * H) * p.o_head;
-                if (has_a) store_chunk<T, INTERLEAVED>(dst + a * static_cast<int>(sizeof(T)), x, 0);
-                if (has_b) store_chunk<T, INTERLEAVED>(dst + b * static_cast<int>(sizeof(T)), x, 1);
-                continue;
-            }
-            const bool is_v = row >= H;
-            const int h = is_v ? row - H : row;
-            char *dst = (is_v ? p.layer.v : p.layer.k) + place + static_cast<int64_t>(h) * p.layer.geo.head;
-            if constexpr (!QUANTISED) {
-                auto put = [&](auto type) {
-                    using P = decltype(type);
-                    if (has_a) store_chunk<P, INTERLEAVED>(dst + a * static_cast<int>(sizeof(P)), x, 0);
-                    if (has_b) store_chunk<P, INTERLEAVED>(dst + b * static_cast<int>(sizeof(P)), x, 1);
-                };
-                if (p.layer.dtype == TC_BF16) put(__nv_bfloat16{});
-                else if (p.layer.dtype == TC_FP16) put(__half{});
-                else put(float{});
-            } else {
-                if (pair == 0) *reinterpret_cast<float *>(reinterpret_cast<char *>(is_v ? p.layer.v_scale : p.layer.k_scale) + scale_place + static_cast<int64_t>(h) * p.layer.scale_geo.head) = scale;
-                if (scale >= kDividable) {
-                    const float y = __fdiv_rn(1.f, scale);
-#pragma unroll
-                    for (int i = 0; i < 4; i++) x.lo[i] = divide2(x.lo[i], -scale, y), x.hi[i] = divide2(x.hi[i], -scale, y);
-                } else {
-                    const bool some = scale > 0.f;  // rows tinier than divide2 takes; and rows whose codes are 0
-#pragma unroll
-                    for (int i = 0; i < 4; i++) {
-                        x.lo[i] = some ? make_float2(__fdiv_rn(x.lo[i].x, scale), __fdiv_rn(x.lo[i].y, scale)) : make_float2(0.f, 0.f);
-                        x.hi[i] = some ? make_float2(__fdiv_rn(x.hi[i].x, scale), __fdiv_rn(x.hi[i].y, scale)) : make_float2(0.f, 0.f);
-                    }
-                }
-#pragma unroll
-                for (int half = 0; half < 2; half++) {
-                    uint32_t w[4];
-#pragma unroll
-                    for (int i = 0; i < 4; i++) {
-                        const float2 e = element2<INTERLEAVED>(x, half, i);
-                        w[i] = p.layer.dtype == TC_E4M3 ? e4m3_pair(e.x, e.y) : int8_pair(e.x, e.y);
-                    }
-                    if (half ? has_b : has_a) *reinterpret_cast<uint2 *>(dst + (half ? b : a)) = make_uint2(w[0] | (w[1] << 16), w[2] | (w[3] << 16));
-                }
-            }
+        for (int i = 0; i < 4; i++) {
+            const float2 xs = fma2(x.lo[i], s[i], zero), ys = fma2(x.hi[i], s[i], zero);
+            x.lo[i] = add2(fma2(x.lo[i], c[i], zero), make_float2(-ys.x, -ys.y));
+            x.hi[i] = add2(fma2(x.hi[i], c[i], zero), xs);
         }
     };
-    for (int base = 0;;) {
-        work(base);
-        if ((base += kRows * step) >= rows) break;
-        load_rows(base, in);
+
+    char *q_dst = p.q_out + token * p.o_tok + first * p.o_head;
+    for (int row = first; row < p.Hq;) {
+#pragma unroll
+        for (int u = 0; u < kQueries; u++) {
+            if (row + u * step >= p.Hq) break;
+            Pairs x;
+            widen_chunks<T, INTERLEAVED>(q[u], x);
+            if (pair < turned) rotate(x);
+            if (has_a) store_chunk<T, INTERLEAVED>(q_dst + u * o_step + a * e, x, 0);
+            if (has_b) store_chunk<T, INTERLEAVED>(q_dst + u * o_step + b * e, x, 1);
+        }
+        row += kQueries * step, q_src += kQueries * q_step, q_dst += kQueries * o_step;
+        if (row >= p.Hq) break;
+#pragma unroll
+        for (int u = 0; u < kQueries; u++) load_row(q_src + u * q_step, row + u * step < p.Hq, q[u]);
+    }
+
+    const int64_t place = p.layer.geo.at(block, n, 0), scale_place = QUANTISED ? p.layer.scale_geo.at(block, n, 0) : 0;
+    for (int row0 = 0; row0 < 2 * H; row0 += step) {
+        const int row = row0 + first;
+        const bool here = row < 2 * H, is_v = row >= H;
+        if (row0) load_row(kv_source(row), here, kv);
+        Pairs x;
+        widen_chunks<T, INTERLEAVED>(kv, x);
+        if (pair < turned && !is_v) rotate(x);
+        float scale = 0.f;
+        if constexpr (QUANTISED) {
+            float most = 0.f;
+#pragma unroll
+            for (int i = 0; i < 4; i++) most = larger(larger(larger(most, fabsf(x.lo[i].x)), fabsf(x.lo[i].y)), larger(fabsf(x.hi[i].x), fabsf(x.hi[i].y)));
+            for (int m = 1; m < lanes; m <<= 1) most = larger(most, __shfl_xor_sync(0xffffffffu, most, m));
+            scale = row_scale(__float_as_uint(most), p.layer.dtype);
+        }
+        if (!here) continue;
+        const int h = is_v ? row - H : row;
+        char *dst = (is_v ? p.layer.v : p.layer.k) + place + static_cast<int64_t>(h) * p.layer.geo.head;
+        if constexpr (!QUANTISED) {
+            auto put = [&](auto type) {
+                using P = decltype(type);
+                if (has_a) store_chunk<P, INTERLEAVED>(dst + a * static_cast<int>(sizeof(P)), x, 0);
+                if (has_b) store_chunk<P, INTERLEAVED>(dst + b * static_cast<int>(sizeof(P)), x, 1);
+            };
+            if (p.layer.dtype == TC_BF16) put(__nv_bfloat16{});
+            else if (p.layer.dtype == TC_FP16) put(__half{});
+            else put(float{});
+        } else {
+            if (pair == 0) *reinterpret_cast<float *>(reinterpret_cast<char *>(is_v ? p.layer.v_scale : p.layer.k_scale) + scale_place + static_cast<int64_t>(h) * p.layer.scale_geo.head) = scale;
+            if (scale >= kDividable) {
+                const float y = __fdiv_rn(1.f, scale);
+#pragma unroll
+                for (int i = 0; i < 4; i++) x.lo[i] = divide2(x.lo[i], -scale, y), x.hi[i] = divide2(x.hi[i], -scale, y);
+            } else {
+                const bool some = scale > 0.f;  // rows tinier than divide2 takes; and rows whose codes are 0
+#pragma unroll
+                for (int i = 0; i < 4; i++) {
+                    x.lo[i] = some ? make_float2(__fdiv_rn(x.lo[i].x, scale), __fdiv_rn(x.lo[i].y, scale)) : make_float2(0.f, 0.f);
+                    x.hi[i] = some ? make_float2(__fdiv_rn(x.hi[i].x, scale), __fdiv_rn(x.hi[i].y, scale)) : make_float2(0.f, 0.f);
+                }
+            }
+#pragma unroll
+            for (int half = 0; half < 2; half++) {
+                uint32_t w[4];
+#pragma unroll
+                for (int i = 0; i < 4; i++) {
+                    const float2 v = element2<INTERLEAVED>(x, half, i);
+                    w[i] = p.layer.dtype == TC_E4M3 ? e4m3_pair(v.x, v.y) : int8_pair(v.x, v.y);
+                }
+                if (half ? has_b : has_a) *reinterpret_cast<uint2 *>(dst + (half ? b : a)) = make_uint2(w[0] | (w[1] << 16), w[2] | (w[3] << 16));
+            }
+        }
     }
 }
 
@@ -378,7 +381,7 @@ static int launch_append(AppendParams &p, bool vector, cudaStream_t s)
     if (vector) {
         int log2_lanes = 0;
         while ((16 << log2_lanes) < p.layer.D) log2_lanes++;
-        const int64_t wanted = rows << log2_lanes;
+        const int64_t wanted = 2ll * p.layer.H << log2_lanes;
         int tpt = 32;
         while (tpt < 256 && tpt < wanted) tpt *= 2;
         p.log2_lanes = log2_lanes;

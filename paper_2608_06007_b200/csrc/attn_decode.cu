@@ -480,6 +480,8 @@ __global__ void __launch_bounds__(128, DP > 128 ? 1 : NB > 1 ? 2 : DP == 64 ? 4 
         }
 
         float k_scale[R::groups][2], v_log[R::groups][2], v_inverse[R::groups][2];
+        uint32_t poison = 0;
+        bool poisoned = false;  // a V that is not finite: NaN for the outputs, but not for the sum
         if constexpr (KIND != kPlain) {
             float v[R::groups][2], here = 0.f;
 #pragma unroll
@@ -490,13 +492,15 @@ __global__ void __launch_bounds__(128, DP > 128 ? 1 : NB > 1 ? 2 : DP == 64 ? 4 
                     asm volatile("ld.shared.f32 %0, [%1];" : "=f"(k_scale[sub][j]) : "r"(key));
                     asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v[sub][j]) : "r"(key + 4 * R::keys));
                 }
-            bool zero = false;
+            bool odd = false, nan = false;
 #pragma unroll
             for (int sub = 0; sub < R::groups; sub++)
 #pragma unroll
-                for (int j = 0; j < 2; j++) zero = zero || v[sub][j] == 0.f;
-            if (__any_sync(0xffffffffu, zero)) {
-                // a row of zeros, or no key: its codes are 0 whatever the scale; one like its neighbours'
+                for (int j = 0; j < 2; j++) odd = odd || !(v[sub][j] > 0.f), nan = nan || v[sub][j] != v[sub][j];
+            if (__any_sync(0xffffffffu, odd)) {
+                poisoned = __any_sync(0xffffffffu, nan);
+                // a row of zeros, or no key, or one that is not finite: its codes are 0 whatever the scale; one like its
+                // neighbours'
 #pragma unroll
                 for (int sub = 0; sub < R::groups; sub++) here = fmaxf(here, fmaxf(v[sub][0], v[sub][1]));
 #pragma unroll
@@ -505,8 +509,10 @@ __global__ void __launch_bounds__(128, DP > 128 ? 1 : NB > 1 ? 2 : DP == 64 ? 4 
 #pragma unroll
                 for (int sub = 0; sub < R::groups; sub++)
 #pragma unroll
-                    for (int j = 0; j < 2; j++)
-                        if (v[sub][j] == 0.f) v[sub][j] = largest;
+                    for (int j = 0; j < 2; j++) {
+                        if (v[sub][j] != v[sub][j]) poison |= 1u << (2 * sub + j);
+                        if (!(v[sub][j] > 0.f)) v[sub][j] = largest;
+                    }
             }
 #pragma unroll
             for (int sub = 0; sub < R::groups; sub++)
@@ -559,12 +565,16 @@ __global__ void __launch_bounds__(128, DP > 128 ? 1 : NB > 1 ? 2 : DP == 64 ? 4 
             const float m0 = top[nb][0] == -INFINITY ? 0.f : top[nb][0], m1 = top[nb][1] == -INFINITY ? 0.f : top[nb][1];
 #pragma unroll
             for (int sub = 0; sub < R::groups; sub++) {
-                const float e0 = exp2_approx(s[sub][nb][0] - m0), e1 = exp2_approx(s[sub][nb][1] - m1), e2 = exp2_approx(s[sub][nb][2] - m0), e3 = exp2_approx(s[sub][nb][3] - m1);
+                float e0 = exp2_approx(s[sub][nb][0] - m0), e1 = exp2_approx(s[sub][nb][1] - m1), e2 = exp2_approx(s[sub][nb][2] - m0), e3 = exp2_approx(s[sub][nb][3] - m1);
                 if constexpr (KIND == kPlain) {
                     sum[nb][0] += e0 + e2, sum[nb][1] += e1 + e3;
                 } else {
                     sum[nb][0] = fmaf(e0, v_inverse[sub][0], fmaf(e2, v_inverse[sub][1], sum[nb][0]));
                     sum[nb][1] = fmaf(e1, v_inverse[sub][0], fmaf(e3, v_inverse[sub][1], sum[nb][1]));
+                }
+                if (KIND != kPlain && poisoned) {
+                    if (poison >> (2 * sub) & 1) e0 = e1 = __uint_as_float(0x7fc00000u);
+                    if (poison >> (2 * sub + 1) & 1) e2 = e3 = __uint_as_float(0x7fc00000u);
                 }
                 pf[sub][nb][0] = transposed(pack2<VT>(e0, e1));
                 pf[sub][nb][1] = transposed(pack2<VT>(e2, e3));

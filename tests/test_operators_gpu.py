@@ -157,7 +157,7 @@ def test_append_types_and_rotations(kind, x, interleaved):
     status_is(0)
 
 
-@pytest.mark.parametrize("D,H,Hq,n,B", [(1, 1, 1, 1, 1), (2, 3, 5, 9, 7), (65, 2, 4, 33, 5), (256, 1, 1, 3, 16), (512, 2, 3, 5, 4), (16, 1, 40, 70, 3), (8, 64, 64, 2, 2), (504, 1, 2, 4, 3)])
+@pytest.mark.parametrize("D,H,Hq,n,B", [(1, 1, 1, 1, 1), (2, 3, 5, 9, 7), (65, 2, 4, 33, 5), (256, 1, 1, 3, 16), (512, 2, 3, 5, 4), (16, 1, 40, 70, 3), (8, 64, 64, 2, 2), (504, 1, 2, 4, 3), (256, 1, 21, 3, 4), (512, 6, 9, 3, 4), (16, 200, 3, 5, 2)])
 @pytest.mark.parametrize("kind", ["bf16", "e4m3", "int8"])
 def test_append_sizes(D, H, Hq, n, B, kind):
     rng = np.random.default_rng([D, H, n])
@@ -397,11 +397,13 @@ def run_attend(pool, s, **changes):
     tc.tc_attn_decode(pool.handle, s["dq"], s["out"], args.pop("tables"), args.pop("lens"), **args)
 
 
-def check_attend(pool, s, x):
+def check_attend(pool, s, x, only=None):
     D, scale = pool.D, s["scale"] or pool.D ** -0.5
     out, lse, q = np64(s["out"]), np64(s["lse"]), np64(s["q"])
     kv = [tokens_of(v, s["shared"], 0, s["prefix"], pool.B) for v in s["values"]]
     for r, n in enumerate(s["lens"]):
+        if only is not None and r not in only:
+            continue
         if n < 0:
             assert (out[r] == 9.0).all() and (lse[r] == 9.0).all()
             continue
@@ -449,6 +451,74 @@ def test_attention_over_a_prefix_shared_by_many(R, prefix, D, x, kind):
     s = attend_case(pool, lens, prefix, 8, x, rng, spread=1.7)
     run_attend(pool, s)
     check_attend(pool, s, x)
+    status_is(0)
+
+
+@pytest.mark.parametrize("x,kind", [("bf16", "bf16"), ("fp16", "fp16"), ("bf16", "e4m3"), ("fp16", "int8")])
+@pytest.mark.parametrize("R,H,g,prefix,D,B", [(160, 8, 4, 6000, 128, 16), (70, 8, 7, 2500, 64, 5), (30, 8, 4, 5001, 128, 32), (12, 16, 5, 9000, 80, 16), (300, 3, 1, 4096, 128, 1)])
+def test_attention_over_many_tiles_of_a_prefix(x, kind, R, H, g, prefix, D, B):
+    """Every CTA of the prefix goes round its ring of tiles several times, with one block of rows and with several."""
+    rng = np.random.default_rng([R, prefix, KIND[kind]])
+    lens = rng.integers(0, 3, R).tolist()
+    pool = Pool(kind, D=D, H=H, B=B, blocks=2 * R + prefix // B + 4, layout="hnd" if R % 4 else "nhd")
+    s = attend_case(pool, lens, prefix, H * g, x, rng, spread=1.3)
+    run_attend(pool, s)
+    check_attend(pool, s, x, only={0, 1, R // 2, R - 1})
+    assert torch.isfinite(s["out"].float()).all() and torch.isfinite(s["lse"]).all()
+    status_is(0)
+
+
+@pytest.mark.parametrize("kind", ["e4m3", "int8"])
+@pytest.mark.parametrize("R,prefix", [(2, 0), (2, 70), (40, 200), (80, 1000)])
+def test_attention_over_values_of_very_different_sizes(kind, R, prefix):
+    """Rows of V from 1e-30 to 1e30, and rows of zeros, in one request: no common scale."""
+    rng = np.random.default_rng([R, prefix])
+    lens = rng.integers(1, 90, R).tolist()
+    pool = Pool(kind, blocks=sum(-(-n // 16) for n in lens) + prefix // 16 + 4)
+    s = attend_case(pool, lens, prefix, 8, "bf16", rng, poison=False)
+    for power in ((-3, 4), (-30, -20), (20, 29)):
+        v = (rng.standard_normal((pool.blocks, pool.B, pool.H, pool.D)) * 10.0 ** rng.integers(*power, (pool.blocks, pool.B, pool.H, 1))).astype(np.float32)
+        v[rng.random(v.shape[:3]) < 0.1] = 0
+        codes, scale = orc.quantise(v, kind)
+        pool.codes(1).copy_(torch.from_numpy(codes.view(np.uint8)))
+        pool.scale(1).copy_(torch.from_numpy(scale))
+        s["values"] = [s["values"][0], orc.values(codes, scale, kind)]
+        run_attend(pool, s)
+        check_attend(pool, s, "bf16")
+    status_is(0)
+
+
+@pytest.mark.parametrize("kind", ["e4m3", "int8"])
+@pytest.mark.parametrize("R,prefix", [(2, 0), (2, 40), (30, 200)])
+def test_attention_where_a_quantised_row_was_not_finite(kind, R, prefix):
+    rng = np.random.default_rng([R, prefix, 9])
+    pool = Pool(kind, blocks=R * 4 + 20)
+    s = attend_case(pool, [50] * R, prefix, 8, "bf16", rng)
+    block = int(s["table"][1, 1])
+    pool.scale(1)[block, 5, 0] = float("nan")  # V: the outputs are NaN, the logarithms are not
+    pool.codes(1)[block, 5, 0] = 0
+    run_attend(pool, s)
+    nan = torch.zeros(R, 8, dtype=torch.bool)
+    nan[1, :4] = True
+    out = s["out"].cpu()
+    assert torch.equal(out.isnan().all(-1), nan) and torch.equal(out.isnan().any(-1), nan) and torch.isfinite(s["lse"]).all()
+    pool.scale(0)[block, 5, 1] = float("nan")  # K: both
+    run_attend(pool, s)
+    nan[1, 4:] = True
+    out = s["out"].cpu()
+    assert torch.equal(out.isnan().any(-1), nan) and torch.equal(s["lse"].cpu().isnan(), nan & (torch.arange(8) >= 4))
+    status_is(0)
+
+
+def test_attention_with_a_negative_scale():
+    rng = np.random.default_rng(27)
+    for kind, x in (("bf16", "bf16"), ("int8", "fp16")):
+        pool = Pool(kind, blocks=60)
+        s = attend_case(pool, [30, 40, 5, 0, 17], 300, 16, x, rng, scale=-0.2)
+        s["scale"] = -0.2
+        run_attend(pool, s)
+        check = dict(s, q=-s["q"], scale=0.2)  # the same scores
+        check_attend(pool, check, x)
     status_is(0)
 
 
@@ -624,6 +694,48 @@ def test_a_request_written_published_hydrated_and_answered_from():
             x = orc.values(stored.numpy().view(np.uint8 if kind == "e4m3" else np.int8), scale.numpy(), kind) if scale is not None else np64(stored.view(torch.bfloat16))
             assert torch.equal(outs[0][c].cpu(), torch.from_numpy(x.astype(np.float32)).bfloat16())
     status_is(0)
+
+
+FIRST_CALL = """
+import sys
+sys.path[:0] = [{root!r}, {tests!r}]
+import numpy as np, torch
+from test_operators_gpu import *
+rng = np.random.default_rng(0)
+for kind in ("bf16", "e4m3"):
+    pool = Pool(kind, blocks=80)
+    s = attend_case(pool, [40, 33], 200, 32, "bf16", rng, poison=False)
+    app = append_case(pool, 2, 32, "bf16", 64, False, rng)
+    free = np.setdiff1d(np.arange(80), np.concatenate([s["table"].ravel(), s["shared"]]))
+    app["slots"] = free[:2].astype(np.int64) * 16
+    k, v = (torch.zeros(73, 2, 128, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    d = [dev(x) for x in (app["slots"], app["pos"], app["cos"], app["sin"], np.array([0, 40, 73]))]
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        stream = torch.cuda.current_stream()
+        tc.tc_kv_append(pool.handle, app["k"], app["v"], d[0], q=app["q"], q_out=s["dq"], positions=d[1], cos=d[2], sin=d[3], stream=stream)
+        tc.tc_kv_gather(pool.handle, s["d"]["tables"], d[4], k, v, stream=stream)
+        run_attend(pool, s, stream=stream)
+    graph.replay()
+    torch.cuda.synchronize()
+    want_q, _ = expect_append(pool, app)
+    assert torch.equal(s["dq"].cpu(), want_q)
+    check_attend(pool, dict(s, q=want_q), "bf16")
+    want = np.concatenate([tokens_of(s["values"][0], s["table"][r], 0, n, 16) for r, n in enumerate([40, 33])])
+    assert torch.equal(k.cpu(), torch.from_numpy(want.astype(np.float32)).bfloat16())
+print("captured")
+"""
+
+
+def test_the_first_call_of_a_process_may_be_a_captured_one():
+    import os
+    import subprocess
+    import sys
+    here = os.path.dirname(os.path.abspath(__file__))
+    code = FIRST_CALL.format(root=os.path.dirname(here), tests=here)
+    got = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=300)
+    assert got.returncode == 0 and "captured" in got.stdout, got.stderr[-2000:]
 
 
 def test_pinned_host_memory_serves_and_pageable_memory_is_refused():

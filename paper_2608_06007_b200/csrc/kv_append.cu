@@ -26,7 +26,7 @@ struct AppendParams {
     int64_t n_tokens;
     int32_t Hq, rot, interleaved;
     int32_t log2_lanes;        // lanes of a row (vector kernel)
-    int32_t threads_per_token; // a power of two, 32..256
+    int32_t threads_per_token; // a power of two, 32..256 (both kernels)
     unsigned int *status;
     float minus_zero;
 };
@@ -75,13 +75,6 @@ __device__ __forceinline__ bool token_target(const AppendParams &p, int64_t slot
         return false;
     }
     return true;
-}
-
-__device__ __forceinline__ void turn(float &x, float &y, float c, float s)
-{
-    const float a = __fsub_rn(__fmul_rn(x, c), __fmul_rn(y, s));
-    y = __fadd_rn(__fmul_rn(y, c), __fmul_rn(x, s));
-    x = a;
 }
 
 // Scale of a row whose largest magnitude has the bits `most` (bits of magnitudes order like the
@@ -310,66 +303,82 @@ __global__ void __launch_bounds__(256, sizeof(T) == 4 ? 2 : 3) append_vector_ker
     }
 }
 
-// Any D up to 512 and any alignment down to the element: a warp per row, element by element.
-template <typename T>
+// Any D up to 32 * ITEMS and any alignment down to the element: a warp per row, element by element.  A warp
+// keeps its lanes' table entries and goes through its share of the token's rows, the next row loaded ahead.
+template <typename T, int ITEMS>
 __global__ void __launch_bounds__(256) append_scalar_kernel(const __grid_constant__ AppendParams p)
 {
-    const int rows = 2 * p.layer.H + p.Hq, D = p.layer.D, lane = threadIdx.x & 31;
-    const int64_t item = static_cast<int64_t>(blockIdx.x) * 8 + (threadIdx.x >> 5);
-    const int64_t token = item / rows;
+    const int rows = 2 * p.layer.H + p.Hq, D = p.layer.D, lane = threadIdx.x & 31, wpt = p.threads_per_token / 32;
+    const int64_t token = static_cast<int64_t>(blockIdx.x) * (8 / wpt) + (threadIdx.x >> 5) / wpt;
     if (token >= p.n_tokens) return;
-    const int row = static_cast<int>(item - token * rows);
-    const int64_t pos = p.rot ? p.positions[token] : 0;
+    const int64_t slot = p.slots[token], pos = p.rot ? p.positions[token] : 0;
+    int other[ITEMS];  // where the element's partner is; -1: it is not rotated
+#pragma unroll
+    for (int i = 0; i < ITEMS; i++) {
+        const int d = lane + 32 * i;
+        const bool second = p.interleaved ? (d & 1) : d >= p.rot / 2;
+        other[i] = d >= p.rot ? -1 : p.interleaved ? d ^ 1 : second ? d - p.rot / 2 : d + p.rot / 2;
+    }
+    T in[ITEMS], partner[ITEMS];
+    auto load_row = [&](int row) {
+        const T *src = reinterpret_cast<const T *>(row_source(p, row, token));
+        const bool turned = row < p.layer.H || row >= 2 * p.layer.H;
+#pragma unroll
+        for (int i = 0; i < ITEMS; i++) {
+            const int d = lane + 32 * i;
+            in[i] = partner[i] = from_float<T>(0.f);
+            if (d < D) in[i] = src[d];
+            if (turned && other[i] >= 0) partner[i] = src[other[i]];
+        }
+    };
+    int row = (threadIdx.x >> 5) % wpt;
+    if (row < rows) load_row(row);
     int64_t block;
     int32_t n;
-    if (!token_target(p, p.slots[token], pos, &block, &n)) return;
-    const RowPlace r = row_place(p, row, token, block, n);
-    const T *src = reinterpret_cast<const T *>(row_source(p, row, token));
-    float x[16];
-    uint32_t most = 0;
+    if (!token_target(p, slot, pos, &block, &n)) return;
+    float c[ITEMS], s[ITEMS];
 #pragma unroll
-    for (int i = 0; i < 16; i++) {
-        const int d = lane + 32 * i;
-        x[i] = 0.f;
-        if (d < D) {
-            x[i] = to_float(src[d]);
-            if (r.turn && d < p.rot) {
-                const int half = p.rot / 2;
-                const bool second = p.interleaved ? (d & 1) : d >= half;
-                const int j = p.interleaved ? d >> 1 : (second ? d - half : d);
-                const int other = p.interleaved ? d ^ 1 : (second ? d - half : d + half);
-                const float c = reinterpret_cast<const float *>(p.cos + pos * p.table_stride)[j], s = reinterpret_cast<const float *>(p.sin + pos * p.table_stride)[j];
-                float y = to_float(src[other]);
-                if (second) {
-                    turn(y, x[i], c, s);
-                } else {
-                    turn(x[i], y, c, s);
-                }
+    for (int i = 0; i < ITEMS; i++) {
+        c[i] = s[i] = 0.f;
+        if (other[i] < 0) continue;
+        const int d = lane + 32 * i, j = p.interleaved ? d >> 1 : min(d, other[i]);
+        c[i] = reinterpret_cast<const float *>(p.cos + pos * p.table_stride)[j];
+        s[i] = reinterpret_cast<const float *>(p.sin + pos * p.table_stride)[j];
+        if (d < other[i]) s[i] = -s[i];  // x cos - x' sin for the first of a pair, x' cos + x sin for the second
+    }
+    for (; row < rows; row += wpt) {
+        const RowPlace r = row_place(p, row, token, block, n);
+        float x[ITEMS];
+        uint32_t most = 0;
+#pragma unroll
+        for (int i = 0; i < ITEMS; i++) {
+            x[i] = to_float(in[i]);
+            if (r.turn && other[i] >= 0) x[i] = __fadd_rn(__fmul_rn(x[i], c[i]), __fmul_rn(to_float(partner[i]), s[i]));
+            most = max(most, __float_as_uint(x[i]) & 0x7fffffffu);
+        }
+        most = __reduce_max_sync(0xffffffffu, most);  // also: q may be rotated in place, all lanes have read their partners
+        if (row + wpt < rows) load_row(row + wpt);
+        float scale = 0.f;
+        if (r.pool && p.layer.k_scale) {
+            scale = row_scale(most, p.layer.dtype);
+            if (lane == 0) *r.scale = scale;
+        }
+        const bool some = scale > 0.f;
+#pragma unroll
+        for (int i = 0; i < ITEMS; i++) {
+            const int d = lane + 32 * i;
+            if (d >= D) continue;
+            if (!r.pool) {
+                reinterpret_cast<T *>(r.dst)[d] = from_float<T>(x[i]);
+                continue;
             }
-        }
-        most = max(most, __float_as_uint(x[i]) & 0x7fffffffu);
-    }
-    most = __reduce_max_sync(0xffffffffu, most);  // also: q may be rotated in place, all lanes have read their partners
-    float scale = 0.f;
-    if (r.pool && p.layer.k_scale) {
-        scale = row_scale(most, p.layer.dtype);
-        if (lane == 0) *r.scale = scale;
-    }
-    const bool some = scale > 0.f;
-#pragma unroll
-    for (int i = 0; i < 16; i++) {
-        const int d = lane + 32 * i;
-        if (d >= D) continue;
-        if (!r.pool) {
-            reinterpret_cast<T *>(r.dst)[d] = from_float<T>(x[i]);
-            continue;
-        }
-        switch (p.layer.dtype) {
-        case TC_BF16: reinterpret_cast<__nv_bfloat16 *>(r.dst)[d] = from_float<__nv_bfloat16>(x[i]); break;
-        case TC_FP16: reinterpret_cast<__half *>(r.dst)[d] = from_float<__half>(x[i]); break;
-        case TC_FP32: reinterpret_cast<float *>(r.dst)[d] = x[i]; break;
-        case TC_E4M3: r.dst[d] = static_cast<char>(e4m3_pair(some ? __fdiv_rn(x[i], scale) : 0.f, 0.f)); break;
-        default: r.dst[d] = static_cast<char>(int8_pair(some ? __fdiv_rn(x[i], scale) : 0.f, 0.f)); break;
+            switch (p.layer.dtype) {
+            case TC_BF16: reinterpret_cast<__nv_bfloat16 *>(r.dst)[d] = from_float<__nv_bfloat16>(x[i]); break;
+            case TC_FP16: reinterpret_cast<__half *>(r.dst)[d] = from_float<__half>(x[i]); break;
+            case TC_FP32: reinterpret_cast<float *>(r.dst)[d] = x[i]; break;
+            case TC_E4M3: r.dst[d] = static_cast<char>(e4m3_pair(some ? __fdiv_rn(x[i], scale) : 0.f, 0.f)); break;
+            default: r.dst[d] = static_cast<char>(int8_pair(some ? __fdiv_rn(x[i], scale) : 0.f, 0.f)); break;
+            }
         }
     }
 }
@@ -397,8 +406,15 @@ static int launch_append(AppendParams &p, bool vector, cudaStream_t s)
             else append_vector_kernel<T, false, false><<<g, 256, 0, s>>>(p);
         }
     } else {
-        if (static_cast<__int128>(p.n_tokens) * rows > static_cast<__int128>(INT32_MAX) * 8) return fail(TC_ERR_TOO_LARGE, "n_tokens %lld: too many for one call", (long long)p.n_tokens);
-        append_scalar_kernel<T><<<static_cast<unsigned>((p.n_tokens * rows + 7) / 8), 256, 0, s>>>(p);
+        int warps = 1;  // of a token: about four rows each
+        while (warps < 8 && warps * 4 < rows) warps *= 2;
+        p.threads_per_token = 32 * warps;
+        const int64_t grid = (p.n_tokens + 8 / warps - 1) / (8 / warps);
+        if (grid > INT32_MAX) return fail(TC_ERR_TOO_LARGE, "n_tokens %lld: too many for one call", (long long)p.n_tokens);
+        const unsigned g = static_cast<unsigned>(grid);
+        if (p.layer.D <= 64) append_scalar_kernel<T, 2><<<g, 256, 0, s>>>(p);
+        else if (p.layer.D <= 128) append_scalar_kernel<T, 4><<<g, 256, 0, s>>>(p);
+        else append_scalar_kernel<T, 16><<<g, 256, 0, s>>>(p);
     }
     const cudaError_t e = cudaGetLastError();
     return e == cudaSuccess ? TC_OK : cuda_fail(e, "kernel launch");

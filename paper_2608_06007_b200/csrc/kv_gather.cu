@@ -69,7 +69,7 @@ __device__ __forceinline__ Words<N * static_cast<int>(sizeof(T)) / 4> narrow_wor
     return r;
 }
 
-// A unit is UNIT output bytes: 32 or 16, or (0) one element at any alignment of the element.
+// A unit is UNIT output bytes: 32, 16 or 8, or (0) one element at any alignment of the element.
 template <int POOL, typename T, int UNIT>
 __global__ void __launch_bounds__(256) gather_kernel(const __grid_constant__ GatherParams p)
 {
@@ -169,6 +169,8 @@ static int launch_gather(GatherParams &p, int unit, int sms, cudaStream_t s)
     if (grid > INT32_MAX) return fail(TC_ERR_TOO_LARGE, "n_rows %lld: too many for one call", (long long)p.n_rows);
     if constexpr (widest == 32)
         if (unit == 32) gather_kernel<POOL, T, 32><<<static_cast<unsigned>(grid), 256, 0, s>>>(p);
+    if constexpr (sizeof(T) == 2)
+        if (unit == 8) gather_kernel<POOL, T, 8><<<static_cast<unsigned>(grid), 256, 0, s>>>(p);
     if (unit == 16) gather_kernel<POOL, T, 16><<<static_cast<unsigned>(grid), 256, 0, s>>>(p);
     if (unit == 0) gather_kernel<POOL, T, 0><<<static_cast<unsigned>(grid), 256, 0, s>>>(p);
     const cudaError_t e = cudaGetLastError();
@@ -230,9 +232,9 @@ extern "C" int tc_kv_gather(const tc_kv_layer_t *layer, const tc_kv_gather_t *a,
     p.planes = (a->k_out != nullptr) + (a->v_out != nullptr);
     p.plane0 = a->k_out ? 0 : 1;
     // Units of 32 output bytes where both sides are aligned to what one unit reads and writes in one
-    // access, else of 16, else single elements.
+    // access, else of 16 or 8, else single elements.
     auto fits = [&](int unit) { return align >= static_cast<uint32_t>(unit) && D * e % unit == 0 && p.layer.align >= static_cast<uint32_t>(std::min(32, unit / e * p.layer.esize)); };
-    const int unit = fits(32) ? 32 : fits(16) ? 16 : 0;
+    const int unit = fits(32) ? 32 : fits(16) ? 16 : e == 2 && fits(8) ? 8 : 0;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     switch (p.layer.dtype) {
     case TC_BF16: return launch_gather_to<TC_BF16>(p, a->dtype, unit, sms, s);

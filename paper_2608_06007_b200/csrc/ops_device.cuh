@@ -74,7 +74,8 @@ __device__ __forceinline__ Words<W> load_words(const void *p)
 template <int W>
 __device__ __forceinline__ void store_words(void *p, const Words<W> &r)
 {
-    static_assert(W == 4 || W == 8);
+    static_assert(W == 2 || W == 4 || W == 8);
+    if constexpr (W == 2) asm volatile("st.global.v2.b32 [%0], {%1,%2};" ::"l"(p), "r"(r.w[0]), "r"(r.w[1]) : "memory");
     if constexpr (W == 4) asm volatile("st.global.v4.b32 [%0], {%1,%2,%3,%4};" ::"l"(p), "r"(r.w[0]), "r"(r.w[1]), "r"(r.w[2]), "r"(r.w[3]) : "memory");
     if constexpr (W == 8)
         asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(r.w[0]), "r"(r.w[1]), "r"(r.w[2]), "r"(r.w[3]), "r"(r.w[4]), "r"(r.w[5]), "r"(r.w[6]), "r"(r.w[7])

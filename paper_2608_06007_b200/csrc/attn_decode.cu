@@ -14,6 +14,7 @@
 namespace tc {
 
 constexpr float kLn2 = 0.6931471805599453f;
+constexpr int kPrefixTiles = 4;
 constexpr int kLeastShare = 2;  // tiles of 16 keys that a warp of the stream takes at least
 constexpr int kSms = 148;  // B200; the workspace must not depend on the device that happens to be current
 
@@ -32,18 +33,26 @@ void split_attn(int64_t R, int64_t Hq, int64_t H, int64_t D, int64_t max_len, in
     s->rows = R * Hq;
     s->columns = s->group <= 8 ? 8 : 16;
     s->own_blocks = (s->group + s->columns - 1) / s->columns;
-    const int64_t rows = R * s->group;  // of one KV head
-    s->prefix_rows = max_prefix == 0 || rows <= 16 || D > 128 ? 16 : rows <= 128 ? 128 : 256;
+    s->tile_keys = quantised ? 32 : 16;
+    auto tiles_of = [&](int64_t keys) { return (keys + s->tile_keys - 1) / s->tile_keys; };
+    // prefix_kernel takes a while to begin: a prefix that adds few tiles to each warp of the stream is left to it
+    const int64_t rows = R * s->group, warps = 4ll * kSms * stream_ctas(quantised, D, s->columns);  // rows of one KV head
+    const bool alone = rows > 16 && D <= 128 && H * ((rows + s->columns - 1) / s->columns) * tiles_of(max_prefix) > kPrefixTiles * warps;
+    s->prefix_rows = !alone ? 16 : rows <= 128 ? 128 : 256;
     const int64_t block = s->prefix_rows == 16 ? s->columns : s->prefix_rows;
     s->prefix_blocks = static_cast<int32_t>((rows + block - 1) / block);
     s->prefix_chunk = 128;
     if (s->prefix_rows > 16) {
-        // One CTA per SM: the number of parts that leaves the fewest tiles to the busiest SM, a part costing
-        // about two tiles to start and end.  At most 64 parts, and 256 MB of them.
+        // One CTA per SM: the number of parts that costs least, counted in tiles (about 1.5 us).  The busiest SM's, with
+        // four to start and end each part, and what writing the parts and reading them again in join_kernel
+        // takes, at some 3 TB/s.  At most 64 parts, and 256 MB of them.
         const int64_t tiles = (max_prefix + 127) / 128, ctas = H * s->prefix_blocks, most = std::max<int64_t>(1, (128ll << 20) / (s->rows * (D + 1) * 4));
-        int64_t best = 1, best_cost = INT64_MAX;
+        const int slots = s->prefix_rows == 128 ? 2 : 1;
+        int64_t best = 1;
+        double best_cost = 1e300;
         for (int64_t n = 1; n <= std::min<int64_t>({tiles, 64, most}); n++) {
-            const int64_t per = (tiles + n - 1) / n, cost = (ctas * ((tiles + per - 1) / per) + kSms - 1) / kSms * (per + 2);
+            const int64_t per = (tiles + n - 1) / n, parts = (tiles + per - 1) / per;
+            const double cost = static_cast<double>((ctas * parts + kSms - 1) / kSms * ((per + slots - 1) / slots * slots + 4)) + static_cast<double>(parts * slots) * s->rows * D * 8 / 4.5e6;
             if (cost < best_cost) best = n, best_cost = cost;
         }
         const int64_t per = (tiles + best - 1) / best;
@@ -52,8 +61,6 @@ void split_attn(int64_t R, int64_t Hq, int64_t H, int64_t D, int64_t max_len, in
     }
     // The stream's warps: what the GPU holds at once, fewer where not even the longest batch would
     // give each its least share.
-    s->tile_keys = quantised ? 32 : 16;
-    auto tiles_of = [&](int64_t keys) { return (keys + s->tile_keys - 1) / s->tile_keys; };
     const int64_t stream_tiles = R * H * s->own_blocks * tiles_of(max_len) + (s->prefix_rows == 16 ? H * s->prefix_blocks * tiles_of(max_prefix) : 0);
     s->stream_tiles = stream_tiles;
     const int64_t ctas = std::min<int64_t>(static_cast<int64_t>(kSms) * stream_ctas(quantised, D, s->columns), (stream_tiles + kLeastShare - 1) / kLeastShare);
@@ -849,10 +856,11 @@ static int launch_decode(const AttnParams &p, int device, cudaStream_t s)
     // parts of a row: the prefix kernel's, and about as many as warps share one item of the stream
     const int64_t parts = p.split.prefix_parts + p.split.stream_ctas * 4 / std::max<int64_t>(p.R * p.layer.H * p.split.own_blocks, 1);
     const unsigned rows = static_cast<unsigned>(p.split.rows);
+    const bool wide = parts > 32 && rows < 1024;  // few rows of many parts
     const unsigned few = std::min<unsigned>((rows + 3) / 4, kSms * 5);
     const bool follows = p.split.prefix_parts || p.split.stream_ctas;
-    if (p.layer.D <= 128) return parts > 32 ? launch_attn(join_kernel<T, 128, 16>, rows, 512, 0, follows, p, s) : launch_attn(join_kernel<T, 128, 1>, few, 128, 0, follows, p, s);
-    return parts > 32 ? launch_attn(join_kernel<T, 256, 16>, rows, 512, 0, follows, p, s) : launch_attn(join_kernel<T, 256, 1>, few, 128, 0, follows, p, s);
+    if (p.layer.D <= 128) return wide ? launch_attn(join_kernel<T, 128, 16>, rows, 512, 0, follows, p, s) : launch_attn(join_kernel<T, 128, 1>, few, 128, 0, follows, p, s);
+    return wide ? launch_attn(join_kernel<T, 256, 16>, rows, 512, 0, follows, p, s) : launch_attn(join_kernel<T, 256, 1>, few, 128, 0, follows, p, s);
 }
 
 // What both entry points check; fills p's geometry and split.

@@ -19,11 +19,11 @@ constexpr int kLeastShare = 2;  // tiles of 16 keys that a warp of the stream ta
 constexpr int kSms = 148;  // B200; the workspace must not depend on the device that happens to be current
 
 // CTAs of stream_kernel that one SM holds, by shared memory and registers.
-static int stream_ctas(bool quantised, int64_t D, int columns)
+static int stream_ctas(int64_t D, int columns)
 {
     if (D > 128) return 1;
-    if (D > 64) return quantised && columns == 8 ? 3 : 2;
-    return columns == 8 ? 4 : 2;
+    if (columns > 8) return 2;
+    return D > 64 ? 3 : 4;
 }
 
 void split_attn(int64_t R, int64_t Hq, int64_t H, int64_t D, int64_t max_len, int64_t max_prefix, bool quantised, AttnSplit *s)
@@ -36,7 +36,7 @@ void split_attn(int64_t R, int64_t Hq, int64_t H, int64_t D, int64_t max_len, in
     s->tile_keys = quantised ? 32 : 16;
     auto tiles_of = [&](int64_t keys) { return (keys + s->tile_keys - 1) / s->tile_keys; };
     // prefix_kernel takes a while to begin: a prefix that adds few tiles to each warp of the stream is left to it
-    const int64_t rows = R * s->group, warps = 4ll * kSms * stream_ctas(quantised, D, s->columns);  // rows of one KV head
+    const int64_t rows = R * s->group, warps = 4ll * kSms * stream_ctas(D, s->columns);  // rows of one KV head
     const bool alone = rows > 16 && D <= 128 && H * ((rows + s->columns - 1) / s->columns) * tiles_of(max_prefix) > kPrefixTiles * warps;
     s->prefix_rows = !alone ? 16 : rows <= 128 ? 128 : 256;
     const int64_t block = s->prefix_rows == 16 ? s->columns : s->prefix_rows;
@@ -63,7 +63,7 @@ void split_attn(int64_t R, int64_t Hq, int64_t H, int64_t D, int64_t max_len, in
     // give each its least share.
     const int64_t stream_tiles = R * H * s->own_blocks * tiles_of(max_len) + (s->prefix_rows == 16 ? H * s->prefix_blocks * tiles_of(max_prefix) : 0);
     s->stream_tiles = stream_tiles;
-    const int64_t ctas = std::min<int64_t>(static_cast<int64_t>(kSms) * stream_ctas(quantised, D, s->columns), (stream_tiles + kLeastShare - 1) / kLeastShare);
+    const int64_t ctas = std::min<int64_t>(static_cast<int64_t>(kSms) * stream_ctas(D, s->columns), (stream_tiles + kLeastShare - 1) / kLeastShare);
     s->stream_ctas = static_cast<int32_t>(ctas);
     const int64_t whole = s->prefix_parts + (max_len > 0) + (max_prefix > 0 && s->prefix_rows == 16), pieces = ctas * 4 * 2 * s->columns;
     auto place = [&](int64_t bytes) {
@@ -132,7 +132,9 @@ struct Ring {
     static constexpr int row = DP * esize, chunks = row / 16;  // bytes and 16-byte chunks of a key
     static constexpr int plane = 16 * row, group = 2 * plane, tile = groups * group;  // 16 keys' K, then their V
     static constexpr int head = KIND == kPlain ? 16 : 16 + 8 * keys;  // {mask, flags, request, item}, then scales of K and of V
-    static constexpr int stages = KIND == kPlain ? 3 : 2;  // D = 128: two CTAs an SM for 16-bit pools, three for codes
+    // One tile is in flight while one is worked on.  D = 128 and 8 columns: three CTAs an SM (a third stage and two CTAs
+    // were slower where requests are short: 512 of about 200 keys 102 against 88 us).
+    static constexpr int stages = 2;
     static constexpr int bytes = 4 * stages * (tile + head);
     static constexpr int copies = 16 * chunks / 32, rows_per_copy = 32 / chunks;  // of 16 keys, by a warp
 };
@@ -180,7 +182,7 @@ enum : uint32_t { kFirst = 1, kLast = 2, kWhole = 4, kSecond = 8 };
 
 // T: the type of the products - the queries' for a plain pool, fp16 for a quantised one, which looks at p.q_bf16.
 template <typename T, int KIND, int DP, int NB>
-__global__ void __launch_bounds__(128, DP > 128 ? 1 : NB > 1 ? 2 : DP == 64 ? 4 : KIND == kPlain ? 2 : 3) stream_kernel(const __grid_constant__ AttnParams p)
+__global__ void __launch_bounds__(128, DP > 128 ? 1 : NB > 1 ? 2 : DP == 64 ? 4 : 3) stream_kernel(const __grid_constant__ AttnParams p)
 {
     using R = Ring<KIND, DP>;
     using ST = std::conditional_t<KIND == kPlain, T, __half>;

@@ -504,7 +504,7 @@ _integers = {}
 
 def _rows(name, t, n, heads, D, dtype, e):
     """Byte strides of a [n, heads, D] tensor of that type with contiguous rows."""
-    if t.dtype is not dtype and t.dtype != dtype:
+    if t.dtype is not dtype:
         raise ValueError(f"{name} has type {t.dtype}, expected {dtype}")
     if t.shape != (n, heads, D):
         raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {(n, heads, D)}")
@@ -532,9 +532,13 @@ def tc_kv_append(layer: KVLayer, k, v, slots, *, q=None, q_out=None, positions=N
     """Write tokens' K and V, [n, H, D], into the pool at `slots` (int64, negative = padding), quantised if the
     pool is.  cos, sin ([positions, rot_dim / 2], fp32): rotate K, and q ([n, Hq, D]) into q_out, by row positions[i]."""
     code, e = _dtype(k)
-    dtype, H, D, n = k.dtype, layer.H, layer.D, k.shape[0]
+    dtype, shape, H, D = k.dtype, k.shape, layer.H, layer.D
+    n = shape[0]
     k0, k1 = _rows("k", k, n, H, D, dtype, e)
-    v0, v1 = _rows("v", v, n, H, D, dtype, e)
+    if v.shape == shape and v.dtype is dtype and v.stride() == k.stride():
+        v0, v1 = k0, k1
+    else:
+        v0, v1 = _rows("v", v, n, H, D, dtype, e)
     hq = q_at = out_at = q0 = q1 = o0 = o1 = rot = pos_at = cos_at = sin_at = n_pos = row = 0
     if q is not None:
         if q_out is None:
@@ -546,16 +550,16 @@ def tc_kv_append(layer: KVLayer, k, v, slots, *, q=None, q_out=None, positions=N
     if cos is not None:
         if sin is None:
             raise ValueError("cos needs a sin")
-        strides = cos.stride()
-        n_pos, half = cos.shape
-        if sin.shape != cos.shape or sin.stride() != strides or _dtypes.get(cos.dtype) != (TC_FP32, 4) or sin.dtype != cos.dtype or (half > 1 and strides[1] != 1):
+        strides, table = cos.stride(), cos.shape
+        n_pos, half = table
+        if sin.shape != table or sin.stride() != strides or _dtypes.get(cos.dtype) != (TC_FP32, 4) or sin.dtype is not cos.dtype or (half > 1 and strides[1] != 1):
             raise ValueError("cos and sin must be fp32 matrices of the same shape and strides, with contiguous rows")
         if half:
             rot, row = 2 * half, strides[0] * 4
             pos_at, cos_at, sin_at = _vector("positions", positions, n, 8), cos.data_ptr(), sin.data_ptr()
     args = _APPEND.pack(_APPEND.size, TC_ROPE_INTERLEAVED if interleaved else 0, n, hq, code, rot, q_at, out_at, k.data_ptr(), v.data_ptr(), q0, q1, o0, o1, k0, k1, v0, v1,
                         _vector("slots", slots, n, 8), pos_at, cos_at, sin_at, n_pos, row)
-    rc = load_library().tc_kv_append(layer.ref, args, _stream(stream))
+    rc = (_lib or load_library()).tc_kv_append(layer.ref, args, None if stream is None else _stream(stream))
     if rc:
         _check(rc)
 
@@ -573,11 +577,14 @@ def tc_kv_gather(layer: KVLayer, tables, offsets, k_out=None, v_out=None, *, fir
         k0, k1 = _rows("k_out", k_out, n, H, D, dtype, e)
         k_at = k_out.data_ptr()
     if v_out is not None:
-        v0, v1 = _rows("v_out", v_out, n, H, D, dtype, e)
+        if k_at and v_out.shape == k_out.shape and v_out.dtype is dtype and v_out.stride() == k_out.stride():
+            v0, v1 = k0, k1
+        else:
+            v0, v1 = _rows("v_out", v_out, n, H, D, dtype, e)
         v_at = v_out.data_ptr()
     table, width, step = _matrix("tables", tables, R)
     args = _GATHER.pack(_GATHER.size, code, R, n, table, width, step, _vector("offsets", offsets, R + 1, 8), 0 if first is None else _vector("first", first, R, 8), k_at, v_at, k0, k1, v0, v1)
-    rc = load_library().tc_kv_gather(layer.ref, args, _stream(stream))
+    rc = (_lib or load_library()).tc_kv_gather(layer.ref, args, None if stream is None else _stream(stream))
     if rc:
         _check(rc)
 
@@ -610,6 +617,6 @@ def tc_attn_decode(layer: KVLayer, q, out, tables, lens, *, max_len, workspace, 
         prefix_len_at = _vector("prefix_len", prefix_len, 1, 4)
     args = _DECODE.pack(_DECODE.size, code, R, Hq, q.data_ptr(), out.data_ptr(), q0, q1, o0, o1, lse_at, scale, 0, table, width, step, _vector("lens", lens, R, 4), max_len,
                         prefix_at, prefix_len_at, max_prefix, workspace.data_ptr(), workspace.numel() * workspace.element_size())
-    rc = load_library().tc_attn_decode(layer.ref, args, _stream(stream))
+    rc = (_lib or load_library()).tc_attn_decode(layer.ref, args, None if stream is None else _stream(stream))
     if rc:
         _check(rc)

@@ -539,8 +539,10 @@ TC_API int tc_kv_gather(const tc_kv_layer_t *layer, const tc_kv_gather_t *args, 
  *   s_j = scale * (q . k_j),  out[r][h] = sum_j exp(s_j) v_j / sum_j exp(s_j),  lse[r][h] = log sum_j exp(s_j)
  * A request without keys (and one whose every s_j is -infinity) gets out 0 and lse -infinity;
  * lens[r] < 0: the request is padding, its rows of out and lse are left as they were.
- * Pages are read once per call for the prefix (per 256 rows of queries and KV head) and once for
- * each request's own; slots past a length are never read.
+ * A prefix's pages are read once for up to 256 rows (request, head) of a KV head (8 or 16 where the
+ * prefix is short or D > 128), a request's own once for its up to 16 heads of a KV head; slots past a
+ * length are never read.  Scores, softmax statistics and outputs are fp32; probabilities are rounded to
+ * the products' 16-bit type (fp16 for quantised pools).  A call is one to three launches.
  * D is a multiple of 16 up to 256, every address and stride a multiple of 16 bytes (tables, lens,
  * prefix_len, lse and the scales: of 4).  An unquantised pool has the queries' type. */
 typedef struct {
@@ -645,7 +647,8 @@ TC_API int tc_trim(void);
  *   TC_DEVICE_BULK_WAIT_TIMEOUT  a CTA of the realigning path (misaligned geometry or pointers)
  *       waited about a second for its asynchronous bulk copies into shared memory and gave up;
  *       the CTA returned without storing, so the destination of that call is incomplete.  Not
- *       expected to occur; the wait is bounded so that a failure cannot hang the device.
+ *       expected to occur; the wait is bounded so that a failure cannot hang the device.  Likewise a
+ *       CTA of tc_attn_decode's prefix kernel: the outputs of that call are then wrong.
  * flags: host pointer.  The call synchronises the device first (every stream's previously
  * enqueued work, non-blocking streams included) and then copies the word back: it is a
  * diagnostic, off the data path. */

@@ -2,7 +2,10 @@
 //
 // A CTA takes a few consecutive output rows: one thread per row finds its request (bisection of
 // the offsets) and its block, then every thread keeps one place (plane, head, unit of 32 output
-// bytes) and steps from token to token, eight loads in flight.  Bound by HBM.
+// bytes) and steps from token to token, 128 bytes of loads in flight.  Bound by HBM: 98k tokens of 8 heads x
+// 128 e4m3 to bf16 (554 MB) take 96 us, 5.8 TB/s, 0.88 of a plain copy; 149k tokens int8 to fp16 (900 MB)
+// 147 us, 0.93.  (Two CTAs an SM instead of three: 102 and 156 us.  Units of 16 bytes stored from 8 codes,
+// four loads in flight: 178 and 304 us.)
 #include "ops_device.cuh"
 
 #include <algorithm>
@@ -71,7 +74,7 @@ __device__ __forceinline__ Words<N * static_cast<int>(sizeof(T)) / 4> narrow_wor
 
 // A unit is UNIT output bytes: 32, 16 or 8, or (0) one element at any alignment of the element.
 template <int POOL, typename T, int UNIT>
-__global__ void __launch_bounds__(256) gather_kernel(const __grid_constant__ GatherParams p)
+__global__ void __launch_bounds__(256, 3) gather_kernel(const __grid_constant__ GatherParams p)
 {
     constexpr bool quantised = POOL == TC_E4M3 || POOL == TC_INT8;
     constexpr int esize = POOL == TC_FP32 ? 4 : quantised ? 1 : 2;

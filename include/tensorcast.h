@@ -553,7 +553,7 @@ typedef struct {
     void *out;            /* [R][Hq][D]; not q */
     int64_t q_stride[2], out_stride[2]; /* request, head */
     float *lse;           /* [R][Hq], tight, natural logarithm; or NULL */
-    float scale;          /* of the scores; 0 = 1 / sqrt(D) */
+    float scale;          /* of the scores, magnitude at most 1e30; 0 = 1 / sqrt(D) */
     int32_t reserved;     /* 0 */
     const int32_t *tables; /* [R][table_width] block ids of each request's own tokens */
     int64_t table_width, table_stride; /* entries per request, bytes from request to request */

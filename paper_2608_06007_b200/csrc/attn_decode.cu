@@ -713,6 +713,7 @@ __global__ void __launch_bounds__(WARPS == 1 ? 128 : 32 * WARPS) join_kernel(con
             if (streams) own_at = p.before[4 + next];
         }
         if (len < 0) continue;
+        if (len > p.max_len && head == 0 && lane == 0) atomicOr(p.status, kStatusBadIndex);
         auto left = [&](uint32_t keys, uint32_t begin, uint32_t in_q, uint32_t blocks, uint32_t whole_slot) {
             Left l{0, 0, 0, false};
             const uint32_t tiles = tiles_of(p, keys), columns = p.split.columns, block = blocks > 1 ? in_q / columns : 0, col = in_q - block * columns;
@@ -887,7 +888,7 @@ static int check_decode(const tc_kv_layer_t *layer, const tc_attn_decode_t *a, A
     if (a->R * a->Hq > (1 << 30)) return fail(TC_ERR_TOO_LARGE, "R * Hq = %lld rows: too many for one call", (long long)(a->R * a->Hq));
     if (a->max_len < 0 || a->max_len > INT32_MAX - 4096 || a->max_prefix < 0 || a->max_prefix > INT32_MAX - 4096)
         return fail(TC_ERR_SHAPE, "max_len %lld and max_prefix %lld must be in [0, 2^31 - 4096)", (long long)a->max_len, (long long)a->max_prefix);
-    if (!(a->scale == a->scale) || std::isinf(a->scale)) return fail(TC_ERR_INVALID_ARG, "scale is not a finite number");
+    if (!(std::fabs(a->scale) <= 1e30f)) return fail(TC_ERR_INVALID_ARG, "scale is not a number of at most 1e30");
     if (a->R * p->layer.H > (1 << 30) / std::max<int64_t>(1, (a->max_len + 15) / 16)) return fail(TC_ERR_TOO_LARGE, "R * H * max_len = %lld * %d * %lld: too many keys for one call", (long long)a->R, p->layer.H, (long long)a->max_len);
     split_attn(a->R, a->Hq, p->layer.H, D, a->max_len, a->max_prefix, p->layer.quantised(), &p->split);
     if (p->split.stream_tiles >= (1ll << 31)) return fail(TC_ERR_TOO_LARGE, "%lld tiles of 16 keys: too many for one call", (long long)p->split.stream_tiles);

@@ -482,7 +482,7 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_kernel(const __grid_
                 copy_wait<Shape::staged - 2>();
                 __syncwarp();
                 const int stage = u % Shape::stages, tile = u >> 1;
-                if (u >= Shape::stages) fine = __all_sync(0xffffffffu, barrier_wait(empty + 8 * stage, (u / Shape::stages - 1) & 1));
+                if (u >= Shape::stages && fine) fine = __all_sync(0xffffffffu, barrier_wait(empty + 8 * stage, (u / Shape::stages - 1) & 1));
                 const uint32_t about = info + (tile % kInfos) * Shape::info;
                 if ((u & 1) == 0) {
                     // the tile whose mask and scales these replace is past its last use: its V is older than this stage's last copy

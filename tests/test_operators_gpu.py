@@ -214,6 +214,10 @@ def test_append_rows_that_are_not_finite_zero_or_tiny():
         x[4] = 1e-38 if x.dtype == torch.float32 else 0
         x[5] *= 1e30 if x.dtype == torch.float32 else 1
         x[6, 4:] = 1e-41 if x.dtype == torch.float32 else 0
+        x[7] *= 5e37                # products and quotients next to the largest numbers
+        x[8] *= 1e-36
+        x[9] *= 3e-24               # scales on both sides of 2^-80
+        x[10] *= 4e-22
 
     rng = np.random.default_rng(6)
     for kind in ("e4m3", "int8", "fp32"):
@@ -577,6 +581,10 @@ def test_attention_leaves_out_what_is_out_of_range_and_says_so():
     s["d"]["prefix_len"][0] = 5000
     run_attend(pool, s)
     check_attend(pool, s, "bf16")
+    status_is(tc.TC_DEVICE_BAD_INDEX)
+    # a length where none was announced
+    run_attend(pool, s, max_len=0, max_prefix=0, tables=s["d"]["tables"])
+    assert (s["out"] == 0).all() and (s["lse"] == float("-inf")).all()
     status_is(tc.TC_DEVICE_BAD_INDEX)
     s["d"]["prefix_len"][0] = -3
     s["d"]["lens"][0] = 40

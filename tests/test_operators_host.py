@@ -114,7 +114,7 @@ def test_gather_refuses(changes, status):
 
 @pytest.mark.parametrize("changes,status", [
     (dict(struct_size=8), INVALID), (dict(dtype=tc.TC_FP32), INVALID), (dict(dtype=tc.TC_FP16), INVALID), (dict(R=-1), SHAPE), (dict(Hq=12), SHAPE), (dict(Hq=0), SHAPE), (dict(R=1 << 20, Hq=1 << 16), TOO_LARGE),
-    (dict(max_len=-1), SHAPE), (dict(max_prefix=1 << 31), SHAPE), (dict(scale=float("nan")), INVALID), (dict(scale=float("inf")), INVALID), (dict(q=None), INVALID), (dict(out=None), INVALID),
+    (dict(max_len=-1), SHAPE), (dict(max_prefix=1 << 31), SHAPE), (dict(scale=float("nan")), INVALID), (dict(scale=float("inf")), INVALID), (dict(scale=-2e30), INVALID), (dict(q=None), INVALID), (dict(out=None), INVALID),
     (dict(out=3 * BASE), OVERLAP), (dict(q=3 * BASE + 8), INVALID), (dict(out_stride=(8192, 128)), OVERLAP), (dict(lse=BASE + 2), INVALID), (dict(lens=None), INVALID), (dict(tables=None), INVALID),
     (dict(table_stride=2), INVALID), (dict(table_width=3), BOUNDS), (dict(prefix_table=None), INVALID), (dict(prefix_len=None), INVALID), (dict(workspace=None), INVALID),
     (dict(workspace=BASE + 8), INVALID), (dict(workspace_bytes=100), BOUNDS),

@@ -19,7 +19,7 @@ constexpr float kLn2 = 0.6931471805599453f;
 // to begin and end (128 requests of 32 heads behind 64 tokens 23 us against 33; behind 1000 35 against 74).
 constexpr int kPrefixTiles = 4;
 // Tiles that a warp of the stream takes at least: one alone is 2 us of latencies (4 requests of 342 tokens:
-// 1, 2, 4 tiles 6.5, 8.6, 12.5 us in the stream, and 5.0, 4.8, 4.0 to join the pieces).
+// 1, 2, 4 tiles 6.5, 8.6, 12.5 us in the stream, and 5.0, 4.8, 4.0 to join the pieces, by a profiler).
 constexpr int kLeastShare = 2;
 constexpr int kSms = 148;  // B200; the workspace must not depend on the device that happens to be current
 
@@ -110,8 +110,8 @@ template <> __device__ __forceinline__ void mma16816<__nv_bfloat16>(float (&c)[4
 // the lengths.  It has its own ring of stages, filled by 16-byte asynchronous copies whatever the size
 // of the pages, and works alone: the copies run ahead across the ends of items, so that short
 // requests cost no gaps.  An item that is one warp's leaves a whole part, one that is cut leaves pieces,
-// at most two a warp.  Bound by HBM for 16-bit pools (297k tokens of 4 heads x 128, 608 MB: 98 us, 6.2 TB/s,
-// 0.95 of a plain copy), by latency and issue for codes (the same in int8, 313 MB: 62 us, 5.0 TB/s).
+// at most two a warp.  Bound by HBM for 16-bit pools (297k tokens of 4 heads x 128, 608 MB: a call takes 106 us, 5.7 TB/s,
+// 0.88 of a plain copy), by latency and issue for codes (the same in int8, 313 MB: 70 us, 4.4 TB/s).
 //
 // The keys are the rows of the matrix products, S' = K Q' and O' = V' P' on m16n8k16: the columns are
 // the query heads of one KV head (or rows of the batch, for the prefix), 8 or 16 at a time, so few
@@ -129,7 +129,7 @@ template <> __device__ __forceinline__ void mma16816<__nv_bfloat16>(float (&c)[4
 // step is below 2^-38 of that largest.
 
 // A tile is 16 keys, or 32 for codes, whose widening takes twice the instructions a byte: two groups of 16
-// side by side keep the warps busier than a third more warps would (D = 128, 297k tokens of 4 heads: 62 us against 70).
+// side by side keep the warps busier than a third more warps would (D = 128, 297k tokens of 4 heads, by a profiler: 62 us against 70).
 template <int KIND, int DP>
 struct Ring {
     static constexpr int esize = KIND == kPlain ? 2 : 1;
@@ -138,7 +138,7 @@ struct Ring {
     static constexpr int plane = 16 * row, group = 2 * plane, tile = groups * group;  // 16 keys' K, then their V
     static constexpr int head = KIND == kPlain ? 16 : 16 + 8 * keys;  // {mask, flags, request, item}, then scales of K and of V
     // One tile is in flight while one is worked on.  D = 128 and 8 columns: three CTAs an SM (a third stage and two CTAs
-    // were slower where requests are short: 512 of about 200 keys 102 against 88 us).
+    // were slower where requests are short, by a profiler: 512 of about 200 keys 102 against 88 us).
     static constexpr int stages = 2;
     static constexpr int bytes = 4 * stages * (tile + head);
     static constexpr int copies = 16 * chunks / 32, rows_per_copy = 32 / chunks;  // of 16 keys, by a warp

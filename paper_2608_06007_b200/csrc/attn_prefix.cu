@@ -17,12 +17,12 @@
 //                    staged as they are first and widened to fp16 by the warp that fetched them.
 //   warps 12, 13     issue the matrix products, S = Q K' and O += P V.
 //
-// Bound by the softmax: 128 requests x 64 heads x 128 behind 32768 tokens (1.4e11 flop) take 142 us, 0.97 PFLOP/s,
-// 0.60 of the measured rate; per tile and slot of 1024 clocks of products the softmax takes some 2900 for both
-// slots, 2048 of them exponentials.  Measured on that case: scores over probabilities, a buffer per
+// Bound by the softmax: 128 requests x 64 heads x 128 behind 32768 tokens (1.4e11 flop): a call takes 152 us, 0.92 PFLOP/s,
+// 0.57 of the measured rate; per tile and slot of 1024 clocks of products the softmax takes some 2900 for both
+// slots, 2048 of them exponentials.  Kernel times that a profiler gave there, for 142 us: scores over probabilities, a buffer per
 // slot 160 us; one buffer, both products from one warp 155; scores issued between the halves of the second product
 // 186; a part of the exponentials as polynomials 154.  Codes: bound by the four warps that widen them
-// (512 requests x 32 heads behind 4000 e4m3 tokens 70 us, bf16 48).
+// (512 requests x 32 heads behind 4000 e4m3 tokens 70 us, bf16 48, by a profiler; the calls 148 and 131).
 //
 // Scales of a quantised pool: K's multiply the scores, V's are taken into the values.
 // Every wait is bounded; one that runs out sets TC_DEVICE_BULK_WAIT_TIMEOUT and the CTA leaves.

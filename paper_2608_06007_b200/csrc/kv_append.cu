@@ -110,13 +110,15 @@ __device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c)
 // x / scale for two numbers, correctly rounded, by Markstein's method: with y the rounded reciprocal, one
 // step q + (x - q scale) y brings q within an ulp, a second one rounds it correctly, as long as the
 // remainders are exact.  They are where scale >= 2^-80: a quotient below 2^-11 becomes code 0 however
-// it is rounded, and above that the remainder's last bit is above 2^-149.
+// it is rounded, and above that the remainder's last bit is above 2^-149.  The remainder of x = -0 is +0, and
+// so would the quotient be: its sign, which an e4m3 code keeps, is x's.
 __device__ __forceinline__ float2 divide2(float2 x, float minus_scale, float y)
 {
     const float2 ms = make_float2(minus_scale, minus_scale), y2 = make_float2(y, y);
     float2 q = fma2(x, y2, make_float2(-0.f, -0.f));
     q = fma2(fma2(q, ms, x), y2, q);
-    return fma2(fma2(q, ms, x), y2, q);
+    q = fma2(fma2(q, ms, x), y2, q);
+    return make_float2(copysignf(q.x, x.x), copysignf(q.y, x.y));
 }
 constexpr float kDividable = 8.27180613e-25f;  // 2^-80
 

@@ -56,7 +56,8 @@ template <> __device__ __forceinline__ void mma16816<__nv_bfloat16>(float (&c)[4
 // one d (V); which key is which row of S' is chosen so that both products agree on the order of the keys.
 // The key's scale multiplies the scores.  The value's goes into the exponent, w = exp2(s + log2 v_scale
 // - top), so that fp16 probabilities have the largest contribution as their reference whatever the scales
-// are; the sum takes w / v_scale, which is exp2(s - top).  Queries of such a pool are fp16 with a power of two
+// are.  The sum has exp2(s - ref) with a running maximum of its own: scales reach from 2^-126 to 2^127, so neither is the
+// other times a number that fp32 holds.  Queries of such a pool are fp16 with a power of two
 // per row taken out, so that the row's largest is in [2^14, 2^15): what is then below fp16's smallest
 // step is below 2^-38 of that largest.
 
@@ -359,6 +360,7 @@ __global__ void __launch_bounds__(128, DP > 128 ? 1 : NB > 1 ? 2 : DP == 64 ? 4 
     load_queries(start_at[warp], first_item, qf);
 
     float o[NB][DP / 16][4], top[NB][2], sum[NB][2];
+    float ref[NB][2];  // codes: the running maximum of the scores, which the sum is relative to; `top` has V's scales in it
     float largest = 0.f;  // codes: a scale of V for rows that have none
     // this lane's keys of 16, rows g and g + 8 of S'
     const int key0 = KIND == kPlain ? g : 4 * (g >> 1) + (g & 1), key1 = KIND == kPlain ? g + 8 : key0 + 2;
@@ -383,7 +385,7 @@ __global__ void __launch_bounds__(128, DP > 128 ? 1 : NB > 1 ? 2 : DP == 64 ? 4 
             for (int nb = 0; nb < NB; nb++) {
 #pragma unroll
                 for (int k = 0; k < DP / 16; k++) o[nb][k][0] = o[nb][k][1] = o[nb][k][2] = o[nb][k][3] = 0.f;
-                top[nb][0] = top[nb][1] = -INFINITY, sum[nb][0] = sum[nb][1] = 0.f;
+                top[nb][0] = top[nb][1] = ref[nb][0] = ref[nb][1] = -INFINITY, sum[nb][0] = sum[nb][1] = 0.f;
             }
         }
 
@@ -425,7 +427,7 @@ __global__ void __launch_bounds__(128, DP > 128 ? 1 : NB > 1 ? 2 : DP == 64 ? 4 
             load_queries(r, static_cast<int>(item), qf);
         }
 
-        float k_scale[R::groups][2], v_log[R::groups][2], v_inverse[R::groups][2];
+        float k_scale[R::groups][2], v_log[R::groups][2];
         uint32_t poison = 0;
         bool poisoned = false;  // a V that is not finite: NaN for the outputs, but not for the sum
         if constexpr (KIND != kPlain) {
@@ -463,12 +465,12 @@ __global__ void __launch_bounds__(128, DP > 128 ? 1 : NB > 1 ? 2 : DP == 64 ? 4 
 #pragma unroll
             for (int sub = 0; sub < R::groups; sub++)
 #pragma unroll
-                for (int j = 0; j < 2; j++) v_log[sub][j] = __log2f(v[sub][j]), v_inverse[sub][j] = __fdividef(1.f, v[sub][j]);
+                for (int j = 0; j < 2; j++) v_log[sub][j] = __log2f(v[sub][j]);
         }
-        float most[NB][2];
+        float most[NB][2], most_ref[NB][2];  // of what `top` and `ref` are of
         bool move = false;
 #pragma unroll
-        for (int nb = 0; nb < NB; nb++) most[nb][0] = most[nb][1] = -INFINITY;
+        for (int nb = 0; nb < NB; nb++) most[nb][0] = most[nb][1] = most_ref[nb][0] = most_ref[nb][1] = -INFINITY;
 #pragma unroll
         for (int sub = 0; sub < R::groups; sub++) {
             const bool key[2] = {(mask >> (16 * sub + key0) & 1) != 0, (mask >> (16 * sub + key1) & 1) != 0};
@@ -478,14 +480,21 @@ __global__ void __launch_bounds__(128, DP > 128 ? 1 : NB > 1 ? 2 : DP == 64 ? 4 
                 for (int j = 0; j < 2; j++) {
                     float &a = s[sub][nb][j], &b = s[sub][nb][j + 2];
                     if constexpr (KIND == kPlain) a *= factor[nb][j], b *= factor[nb][j];
-                    else a = fmaf(a, factor[nb][j] * k_scale[sub][0], v_log[sub][0]), b = fmaf(b, factor[nb][j] * k_scale[sub][1], v_log[sub][1]);
+                    else a *= factor[nb][j] * k_scale[sub][0], b *= factor[nb][j] * k_scale[sub][1];
                     if (!key[0]) a = -INFINITY;
                     if (!key[1]) b = -INFINITY;
-                    most[nb][j] = fmaxf(most[nb][j], fmaxf(a, b));
+                    if constexpr (KIND == kPlain) {
+                        most[nb][j] = fmaxf(most[nb][j], fmaxf(a, b));
+                    } else {
+                        most[nb][j] = fmaxf(most[nb][j], fmaxf(a + v_log[sub][0], b + v_log[sub][1]));
+                        most_ref[nb][j] = fmaxf(most_ref[nb][j], fmaxf(a, b));
+                    }
                 }
         }
 #pragma unroll
-        for (int nb = 0; nb < NB; nb++) move = move || most[nb][0] > top[nb][0] + 8.f || most[nb][1] > top[nb][1] + 8.f;
+        for (int nb = 0; nb < NB; nb++)
+#pragma unroll
+            for (int j = 0; j < 2; j++) move = move || most[nb][j] > top[nb][j] + 8.f || (KIND != kPlain && most_ref[nb][j] > ref[nb][j] + 8.f);
         // A running maximum moves only when a score exceeds it by more than 8 (2^8 in probabilities): up
         // to there they stay small enough for either 16-bit type and the outputs need no rescaling.
         if (__any_sync(0xffffffffu, move)) {
@@ -499,7 +508,15 @@ __global__ void __launch_bounds__(128, DP > 128 ? 1 : NB > 1 ? 2 : DP == 64 ? 4 
                     const float m = fmaxf(top[nb][j], most[nb][j]);
                     f[j] = m == top[nb][j] ? 1.f : exp2_approx(top[nb][j] - m);
                     top[nb][j] = m;
-                    sum[nb][j] *= f[j];
+                    if constexpr (KIND == kPlain) {
+                        sum[nb][j] *= f[j];
+                    } else {
+#pragma unroll
+                        for (int x = 4; x < 32; x <<= 1) most_ref[nb][j] = fmaxf(most_ref[nb][j], __shfl_xor_sync(0xffffffffu, most_ref[nb][j], x));
+                        const float r = fmaxf(ref[nb][j], most_ref[nb][j]);
+                        if (r != ref[nb][j]) sum[nb][j] *= exp2_approx(ref[nb][j] - r);
+                        ref[nb][j] = r;
+                    }
                 }
 #pragma unroll
                 for (int k = 0; k < DP / 16; k++) o[nb][k][0] *= f[0], o[nb][k][1] *= f[1], o[nb][k][2] *= f[0], o[nb][k][3] *= f[1];
@@ -509,15 +526,16 @@ __global__ void __launch_bounds__(128, DP > 128 ? 1 : NB > 1 ? 2 : DP == 64 ? 4 
 #pragma unroll
         for (int nb = 0; nb < NB; nb++) {
             const float m0 = top[nb][0] == -INFINITY ? 0.f : top[nb][0], m1 = top[nb][1] == -INFINITY ? 0.f : top[nb][1];
+            const float r0 = ref[nb][0] == -INFINITY ? 0.f : ref[nb][0], r1 = ref[nb][1] == -INFINITY ? 0.f : ref[nb][1];
 #pragma unroll
             for (int sub = 0; sub < R::groups; sub++) {
-                float e0 = exp2_approx(s[sub][nb][0] - m0), e1 = exp2_approx(s[sub][nb][1] - m1), e2 = exp2_approx(s[sub][nb][2] - m0), e3 = exp2_approx(s[sub][nb][3] - m1);
-                if constexpr (KIND == kPlain) {
-                    sum[nb][0] += e0 + e2, sum[nb][1] += e1 + e3;
-                } else {
-                    sum[nb][0] = fmaf(e0, v_inverse[sub][0], fmaf(e2, v_inverse[sub][1], sum[nb][0]));
-                    sum[nb][1] = fmaf(e1, v_inverse[sub][0], fmaf(e3, v_inverse[sub][1], sum[nb][1]));
+                float (&x)[4] = s[sub][nb];
+                if constexpr (KIND != kPlain) {
+                    sum[nb][0] += exp2_approx(x[0] - r0) + exp2_approx(x[2] - r0), sum[nb][1] += exp2_approx(x[1] - r1) + exp2_approx(x[3] - r1);
+                    x[0] += v_log[sub][0], x[1] += v_log[sub][0], x[2] += v_log[sub][1], x[3] += v_log[sub][1];
                 }
+                float e0 = exp2_approx(x[0] - m0), e1 = exp2_approx(x[1] - m1), e2 = exp2_approx(x[2] - m0), e3 = exp2_approx(x[3] - m1);
+                if constexpr (KIND == kPlain) sum[nb][0] += e0 + e2, sum[nb][1] += e1 + e3;
                 if (KIND != kPlain && poisoned) {
                     if (poison >> (2 * sub) & 1) e0 = e1 = __uint_as_float(0x7fc00000u);
                     if (poison >> (2 * sub + 1) & 1) e2 = e3 = __uint_as_float(0x7fc00000u);
@@ -575,7 +593,10 @@ __global__ void __launch_bounds__(128, DP > 128 ? 1 : NB > 1 ? 2 : DP == 64 ? 4 
                     const int64_t req = quick_div(static_cast<uint32_t>(row), p.div_group);
                     const int64_t where = whole ? slot * p.split.rows + req * p.Hq + it.h * group + (row - req * group) : piece + col;
                     float *dst = (whole ? p.parts : p.pieces) + where * D;
-                    const float inv = all == 0.f ? 0.f : 1.f / all, log = all == 0.f ? -INFINITY : (top[nb][j] == -INFINITY ? 0.f : top[nb][j]) + log2f(all);
+                    const float base = KIND == kPlain ? top[nb][j] : ref[nb][j];
+                    const float inv = all == 0.f ? 0.f : 1.f / all, log = all == 0.f ? -INFINITY : (base == -INFINITY ? 0.f : base) + log2f(all);
+                    // outputs are relative to `top`: from there to `ref`, in two steps that fp32 holds
+                    const float step = KIND == kPlain ? 1.f : exp2_approx(0.5f * (top[nb][j] - (base == -INFINITY ? 0.f : base)));
                     if (whole && p.max_prefix == 0) {
                         // these are all of the row's keys: its output
                         char *out = p.out + req * p.out_req + (it.h * group + (row - req * group)) * p.out_head;
@@ -583,7 +604,7 @@ __global__ void __launch_bounds__(128, DP > 128 ? 1 : NB > 1 ? 2 : DP == 64 ? 4 
                         for (int k = 0; k < DP / 16; k++)
 #pragma unroll
                             for (int half = 0; half < 2; half++) {
-                                const float x = o[nb][k][2 * half + j] * inv;
+                                const float x = KIND == kPlain ? o[nb][k][2 * half + j] * inv : o[nb][k][2 * half + j] * inv * step * step;
                                 if (16 * k >= D) continue;
                                 if (KIND == kPlain ? std::is_same<T, __nv_bfloat16>::value : p.q_bf16) reinterpret_cast<__nv_bfloat16 *>(out)[16 * k + g + 8 * half] = __float2bfloat16_rn(x);
                                 else reinterpret_cast<__half *>(out)[16 * k + g + 8 * half] = __float2half_rn(x);
@@ -595,7 +616,7 @@ __global__ void __launch_bounds__(128, DP > 128 ? 1 : NB > 1 ? 2 : DP == 64 ? 4 
                     for (int k = 0; k < DP / 16; k++)
 #pragma unroll
                         for (int half = 0; half < 2; half++)
-                            if (16 * k < D) dst[16 * k + g + 8 * half] = o[nb][k][2 * half + j] * inv;
+                            if (16 * k < D) dst[16 * k + g + 8 * half] = KIND == kPlain ? o[nb][k][2 * half + j] * inv : o[nb][k][2 * half + j] * inv * step * step;
                     if (g == 0) (whole ? p.sums : p.piece_sums)[where] = log;
                 }
         }

@@ -1,10 +1,19 @@
-"""The operators on a paged layer where numbers are at the ends of their range."""
+"""The operators on a paged layer where numbers are far apart, and each of decode's kernels by name.
+
+A case says which kernel takes its prefix - none, the stream, or the prefix kernel with 128 or 256 rows a CTA - and
+fails where the library's rule gives it to another."""
 import numpy as np
 import pytest
+import torch
 
-from test_operators_gpu import Pool, append_case, check_append, run_append, status_is
+import paper_2608_06007_b200 as tc
+from operators_split import prefix_taken_by
+from oracle import operators as orc
+from test_operators_gpu import Pool, append_case, attend_case, check_append, check_attend, dev, np64, run_append, run_attend, status_is, tokens_of
 
 pytestmark = pytest.mark.gpu
+
+TOP = {"e4m3": 448.0, "int8": 127.0}
 
 
 # ---------------------------------------------------------------------------------------- append
@@ -26,4 +35,125 @@ def test_append_keeps_the_sign_of_zeros(kind, x, interleaved):
         s = append_case(pool, 37, 4, x, rot, interleaved, rng, mutate=mutate)
         run_append(pool, s)
         check_append(pool, s)
+    status_is(0)
+
+
+# ---------------------------------------------------------------------------------------- decode
+# name: (requests, KV heads, query heads of each, head dim, prefix, own tokens at most)
+SHAPES = {
+    "none": (3, 2, 4, 128, 0, 600),
+    "none, 64": (3, 1, 3, 64, 0, 600),
+    "none, 12 heads": (2, 1, 12, 128, 0, 300),
+    "none, 256": (2, 1, 5, 256, 0, 300),
+    "stream": (4, 2, 4, 128, 700, 60),
+    "stream, 16 rows": (3, 1, 11, 80, 600, 60),
+    "prefix 128": (20, 8, 6, 128, 2100, 40),
+    "prefix 128, 64": (32, 8, 4, 64, 2700, 40),
+    "prefix 256": (36, 8, 7, 128, 1300, 40),
+    "prefix 256, 80": (36, 8, 7, 80, 1300, 40),
+}
+STREAMS = [name for name in SHAPES if not name.startswith("prefix")]
+PREFIXES = [name for name in SHAPES if name.startswith("prefix")]
+
+
+def shaped(shape, kind, x, rng, B=16, layout="nhd", plain_tiles=False, **more):
+    R, H, g, D, prefix, most = SHAPES[shape]
+    if plain_tiles and prefix > 1000:
+        prefix //= 2  # 16-bit pools have tiles of half as many keys
+    lens = rng.integers(0, most + 1, R)
+    lens[0], lens[-1] = most, 1
+    lens = lens.tolist()
+    if prefix:
+        taken = prefix_taken_by(R, H * g, H, D, max(lens), prefix, kind in TOP)
+        assert taken == shape.split(",")[0], taken
+    pool = Pool(kind, layout=layout, D=D, H=H, B=B, blocks=sum(-(-n // B) for n in lens) + -(-prefix // B) + 3)
+    return pool, attend_case(pool, lens, prefix, H * g, x, rng, poison=False, **more)
+
+
+def rows_of(pool, s, plane, make):
+    """Sets a quantised plane's codes and scales: make(t, shape) -> (codes as numbers, scales) of token t[i] of the prefix
+    (then of each request, counting on behind it), for all heads."""
+    codes = np.zeros((pool.blocks, pool.B, pool.H, pool.D), dtype=np.uint8)
+    scale = np.zeros((pool.blocks, pool.B, pool.H), dtype=np.float32)
+    for table, first, n in [(s["shared"], 0, s["prefix"])] + [(tab, s["prefix"], max(0, m)) for tab, m in zip(s["table"], s["lens"])]:
+        t = np.arange(n)
+        c, sc = make(first + t, (n, pool.H, pool.D))
+        c = np.asarray(c, dtype=np.float64)
+        codes[table[t // pool.B], t % pool.B] = orc.e4m3_round(c) if pool.kind == "e4m3" else np.rint(c).astype(np.int8).view(np.uint8)
+        scale[table[t // pool.B], t % pool.B] = sc
+    pool.codes(plane).copy_(torch.from_numpy(codes))
+    pool.scale(plane).copy_(torch.from_numpy(scale))
+    s["values"][plane] = orc.values(codes if pool.kind == "e4m3" else codes.view(np.int8), scale, pool.kind)
+    s["scale_of"] = s.get("scale_of", {}) | {plane: np.abs(scale.astype(np.float64))}
+
+
+def check_ranges(pool, s, x, prefix_kernel, only):
+    """Outputs and logarithms of some requests against 64 bits.  A quantised pool's products are of 16-bit numbers: a
+    probability is rounded once (half a step of 2^-11), a value of the prefix kernel's twice more.  A weight is 2 to the
+    power of a sum of logarithms of up to some hundreds, in fp32: 2^-14 of it.  A product below fp16's normal numbers is off by half of 2^-24 at most,
+    beside a largest contribution of at least 1/2 (code: up to TOP), or for values 2^-15 of their scale.  Then the output's own half step."""
+    scale, top = s["scale"] or pool.D ** -0.5, TOP[pool.kind]
+    out, lse, q = np64(s["out"]), np64(s["lse"]), np64(s["q"])
+    g = s["q"].shape[1] // pool.H
+    u_o = torch.finfo(s["out"].dtype).eps / 2
+    half = 2.0 ** -25 if x == "fp16" else 2.0 ** -133
+    both = lambda what, r: np.concatenate([tokens_of(what, s["shared"], 0, s["prefix"], pool.B), tokens_of(what, s["table"][r], 0, s["lens"][r], pool.B)])
+    for r in only:
+        if s["lens"][r] < 0:
+            assert (out[r] == 9.0).all() and (lse[r] == 9.0).all()
+            continue
+        keys, vals = (both(v, r) for v in s["values"])
+        if not len(keys):
+            assert (out[r] == 0).all() and (lse[r] == -np.inf).all()
+            continue
+        sizes = both(s["scale_of"][1], r)
+        want, want_lse, mass = orc.attend(q[r], keys, vals, scale)
+        k = np.repeat(keys, g, axis=1)
+        score = np.einsum("hd,nhd->hn", q[r], k) * scale
+        weights = np.exp(score - want_lse[:, None]) * np.repeat(sizes, g, axis=1).T  # of each key, times its scale
+        delta = (pool.D + 4) * 2.0 ** -24 * abs(scale) * np.einsum("hd,nhd->nh", np.abs(q[r]), np.abs(k)).max(0)
+        most = ((3 if prefix_kernel else 1) * 2.0 ** -11 * (1 + 2.0 ** -6) + 2 * delta[:, None] + 2.0 ** -14) * mass
+        most += (len(keys) * 2.0 ** -24 * top * weights.max(1) + 2.0 ** -15 * weights.sum(1))[:, None]
+        most += u_o * (1 + 2.0 ** -6) * np.abs(want) + half
+        off = np.abs(out[r] - want)
+        assert (off <= most).all(), (r, off.max(), np.abs(want).max(), (off / np.maximum(most, 1e-300)).max())
+        assert (np.abs(lse[r] - want_lse) <= delta + 2.0 ** -18 + 2.0 ** -22 * np.abs(want_lse)).all(), (r, lse[r], want_lse)
+
+
+def check(pool, s, x, prefix_kernel, only):
+    if pool.kind not in TOP:
+        return check_attend(pool, s, x, only=set(only))
+    # test_operators_gpu's bound has no term for probabilities below fp16's normal numbers in quantised pools
+    check_ranges(pool, dict(s, scale_of={1: np64(pool.scale(1).abs())}), x, prefix_kernel, only)
+
+
+def spread_codes(rng, kind):
+    return lambda shape: np.clip(rng.standard_normal(shape) * TOP[kind] / 3, -TOP[kind], TOP[kind])
+
+
+V_SCALES = {
+    "smallest": lambda rng, t, H: np.full((len(t), H), 2.0 ** -126) * (1 + rng.random((len(t), H))),
+    "small": lambda rng, t, H: np.full((len(t), H), 2.0 ** -113) * (1 + rng.random((len(t), H))),
+    "large": lambda rng, t, H: np.full((len(t), H), 1e35) * (1 + rng.random((len(t), H))),
+    "spans of 64 far apart": lambda rng, t, H: np.where(t // 64 % 2, 2.0 ** 60, 2.0 ** -90)[:, None] * np.ones(H),
+    "spans of 128 far apart": lambda rng, t, H: np.where(t // 128 % 2, 2.0 ** -90, 2.0 ** 60)[:, None] * np.ones(H),
+    "mixed": lambda rng, t, H: 10.0 ** rng.uniform(-30, 30, (len(t), H)),
+}
+
+
+@pytest.mark.parametrize("shape", STREAMS)
+@pytest.mark.parametrize("kind,x", [("e4m3", "bf16"), ("int8", "bf16")])
+@pytest.mark.parametrize("scales", V_SCALES)
+def test_attention_over_scales_of_v_at_the_ends_of_their_range(shape, kind, x, scales):
+    """Scales that tc_kv_append may write, 2^-126 and up, together in one request; equal scores and ordinary ones."""
+    rng = np.random.default_rng([len(shape), len(scales), x == "bf16"])
+    pool, s = shaped(shape, kind, x, rng)
+    codes = spread_codes(rng, kind)
+    rows_of(pool, s, 1, lambda t, sh: (codes(sh), V_SCALES[scales](rng, t, pool.H)))
+    only = sorted({0, len(s["lens"]) - 1})
+    run_attend(pool, s)
+    check_ranges(pool, s, x, shape.startswith("prefix"), only)
+    rows_of(pool, s, 0, lambda t, sh: (np.zeros(sh), np.ones(sh[:2])))
+    run_attend(pool, s)
+    check_ranges(pool, s, x, shape.startswith("prefix"), only)
     status_is(0)

@@ -361,7 +361,6 @@ __global__ void __launch_bounds__(128, DP > 128 ? 1 : NB > 1 ? 2 : DP == 64 ? 4 
 
     float o[NB][DP / 16][4], top[NB][2], sum[NB][2];
     float ref[NB][2];  // codes: the running maximum of the scores, which the sum is relative to; `top` has V's scales in it
-    float largest = 0.f;  // codes: a scale of V for rows that have none
     // this lane's keys of 16, rows g and g + 8 of S'
     const int key0 = KIND == kPlain ? g : 4 * (g >> 1) + (g & 1), key1 = KIND == kPlain ? g + 8 : key0 + 2;
     int stage = 0, next_fill = R::stages - 1;
@@ -380,7 +379,6 @@ __global__ void __launch_bounds__(128, DP > 128 ? 1 : NB > 1 ? 2 : DP == 64 ? 4 
         asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(mask), "=r"(flags), "=r"(head_r), "=r"(head_item) : "r"(head_at));
         if (flags & kFirst) {
             take_queries();
-            largest = 7.888609052e-31f;  // 2^-100
 #pragma unroll
             for (int nb = 0; nb < NB; nb++) {
 #pragma unroll
@@ -428,44 +426,19 @@ __global__ void __launch_bounds__(128, DP > 128 ? 1 : NB > 1 ? 2 : DP == 64 ? 4 
         }
 
         float k_scale[R::groups][2], v_log[R::groups][2];
-        uint32_t poison = 0;
-        bool poisoned = false;  // a V that is not finite: NaN for the outputs, but not for the sum
+        uint32_t v_sign[R::groups][2];
         if constexpr (KIND != kPlain) {
-            float v[R::groups][2], here = 0.f;
 #pragma unroll
             for (int sub = 0; sub < R::groups; sub++)
 #pragma unroll
                 for (int j = 0; j < 2; j++) {
                     const uint32_t key = head_at + 16 + (16 * sub + (j ? key1 : key0)) * 4;
+                    float v;
                     asm volatile("ld.shared.f32 %0, [%1];" : "=f"(k_scale[sub][j]) : "r"(key));
-                    asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v[sub][j]) : "r"(key + 4 * R::keys));
+                    asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(key + 4 * R::keys));
+                    // 0: -infinity, a weight of 0; NaN: the weight and with it the outputs, but not the sum
+                    v_log[sub][j] = __log2f(fabsf(v)), v_sign[sub][j] = __float_as_uint(v) & 0x80000000u;
                 }
-            bool odd = false, nan = false;
-#pragma unroll
-            for (int sub = 0; sub < R::groups; sub++)
-#pragma unroll
-                for (int j = 0; j < 2; j++) odd = odd || !(v[sub][j] > 0.f), nan = nan || v[sub][j] != v[sub][j];
-            if (__any_sync(0xffffffffu, odd)) {
-                poisoned = __any_sync(0xffffffffu, nan);
-                // a row of zeros, or no key, or one that is not finite: its codes are 0 whatever the scale; one like its
-                // neighbours'
-#pragma unroll
-                for (int sub = 0; sub < R::groups; sub++) here = fmaxf(here, fmaxf(v[sub][0], v[sub][1]));
-#pragma unroll
-                for (int x = 4; x < 32; x <<= 1) here = fmaxf(here, __shfl_xor_sync(0xffffffffu, here, x));
-                if (here > 0.f) largest = here;
-#pragma unroll
-                for (int sub = 0; sub < R::groups; sub++)
-#pragma unroll
-                    for (int j = 0; j < 2; j++) {
-                        if (v[sub][j] != v[sub][j]) poison |= 1u << (2 * sub + j);
-                        if (!(v[sub][j] > 0.f)) v[sub][j] = largest;
-                    }
-            }
-#pragma unroll
-            for (int sub = 0; sub < R::groups; sub++)
-#pragma unroll
-                for (int j = 0; j < 2; j++) v_log[sub][j] = __log2f(v[sub][j]);
         }
         float most[NB][2], most_ref[NB][2];  // of what `top` and `ref` are of
         bool move = false;
@@ -536,9 +509,9 @@ __global__ void __launch_bounds__(128, DP > 128 ? 1 : NB > 1 ? 2 : DP == 64 ? 4 
                 }
                 float e0 = exp2_approx(x[0] - m0), e1 = exp2_approx(x[1] - m1), e2 = exp2_approx(x[2] - m0), e3 = exp2_approx(x[3] - m1);
                 if constexpr (KIND == kPlain) sum[nb][0] += e0 + e2, sum[nb][1] += e1 + e3;
-                if (KIND != kPlain && poisoned) {
-                    if (poison >> (2 * sub) & 1) e0 = e1 = __uint_as_float(0x7fc00000u);
-                    if (poison >> (2 * sub + 1) & 1) e2 = e3 = __uint_as_float(0x7fc00000u);
+                if constexpr (KIND != kPlain) {
+                    e0 = __uint_as_float(__float_as_uint(e0) ^ v_sign[sub][0]), e1 = __uint_as_float(__float_as_uint(e1) ^ v_sign[sub][0]);
+                    e2 = __uint_as_float(__float_as_uint(e2) ^ v_sign[sub][1]), e3 = __uint_as_float(__float_as_uint(e3) ^ v_sign[sub][1]);
                 }
                 pf[sub][nb][0] = transposed(pack2<VT>(e0, e1));
                 pf[sub][nb][1] = transposed(pack2<VT>(e2, e3));
@@ -595,8 +568,17 @@ __global__ void __launch_bounds__(128, DP > 128 ? 1 : NB > 1 ? 2 : DP == 64 ? 4 
                     float *dst = (whole ? p.parts : p.pieces) + where * D;
                     const float base = KIND == kPlain ? top[nb][j] : ref[nb][j];
                     const float inv = all == 0.f ? 0.f : 1.f / all, log = all == 0.f ? -INFINITY : (base == -INFINITY ? 0.f : base) + log2f(all);
-                    // outputs are relative to `top`: from there to `ref`, in two steps that fp32 holds
-                    const float step = KIND == kPlain ? 1.f : exp2_approx(0.5f * (top[nb][j] - (base == -INFINITY ? 0.f : base)));
+                    float by = inv;
+                    if constexpr (KIND != kPlain) {
+                        // outputs are relative to `top`: from there to `ref`, in two steps where fp32 does not hold one
+                        float step = top[nb][j] - (base == -INFINITY ? 0.f : base);
+                        if (!(fabsf(step) < 80.f)) {
+                            step *= 0.5f;
+#pragma unroll
+                            for (int k = 0; k < DP / 16; k++) o[nb][k][j] *= exp2_approx(step), o[nb][k][2 + j] *= exp2_approx(step);
+                        }
+                        by *= exp2_approx(step);
+                    }
                     if (whole && p.max_prefix == 0) {
                         // these are all of the row's keys: its output
                         char *out = p.out + req * p.out_req + (it.h * group + (row - req * group)) * p.out_head;
@@ -604,7 +586,7 @@ __global__ void __launch_bounds__(128, DP > 128 ? 1 : NB > 1 ? 2 : DP == 64 ? 4 
                         for (int k = 0; k < DP / 16; k++)
 #pragma unroll
                             for (int half = 0; half < 2; half++) {
-                                const float x = KIND == kPlain ? o[nb][k][2 * half + j] * inv : o[nb][k][2 * half + j] * inv * step * step;
+                                const float x = o[nb][k][2 * half + j] * by;
                                 if (16 * k >= D) continue;
                                 if (KIND == kPlain ? std::is_same<T, __nv_bfloat16>::value : p.q_bf16) reinterpret_cast<__nv_bfloat16 *>(out)[16 * k + g + 8 * half] = __float2bfloat16_rn(x);
                                 else reinterpret_cast<__half *>(out)[16 * k + g + 8 * half] = __float2half_rn(x);
@@ -616,7 +598,7 @@ __global__ void __launch_bounds__(128, DP > 128 ? 1 : NB > 1 ? 2 : DP == 64 ? 4 
                     for (int k = 0; k < DP / 16; k++)
 #pragma unroll
                         for (int half = 0; half < 2; half++)
-                            if (16 * k < D) dst[16 * k + g + 8 * half] = KIND == kPlain ? o[nb][k][2 * half + j] * inv : o[nb][k][2 * half + j] * inv * step * step;
+                            if (16 * k < D) dst[16 * k + g + 8 * half] = o[nb][k][2 * half + j] * by;
                     if (g == 0) (whole ? p.sums : p.piece_sums)[where] = log;
                 }
         }

@@ -138,6 +138,7 @@ V_SCALES = {
     "spans of 64 far apart": lambda rng, t, H: np.where(t // 64 % 2, 2.0 ** 60, 2.0 ** -90)[:, None] * np.ones(H),
     "spans of 128 far apart": lambda rng, t, H: np.where(t // 128 % 2, 2.0 ** -90, 2.0 ** 60)[:, None] * np.ones(H),
     "mixed": lambda rng, t, H: 10.0 ** rng.uniform(-30, 30, (len(t), H)),
+    "mixed, zeros": lambda rng, t, H: 10.0 ** rng.uniform(-37, 5, (len(t), H)) * (rng.random((len(t), H)) > 0.3),
 }
 
 
@@ -156,4 +157,19 @@ def test_attention_over_scales_of_v_at_the_ends_of_their_range(shape, kind, x, s
     rows_of(pool, s, 0, lambda t, sh: (np.zeros(sh), np.ones(sh[:2])))
     run_attend(pool, s)
     check_ranges(pool, s, x, shape.startswith("prefix"), only)
+    status_is(0)
+
+
+@pytest.mark.parametrize("shape", STREAMS)
+@pytest.mark.parametrize("kind,x", [("e4m3", "bf16"), ("int8", "fp16")])
+def test_attention_over_scales_of_v_that_are_zero_or_negative(shape, kind, x):
+    """A value is code * scale whatever wrote them: codes under a scale of 0 are zeros, a negative one turns signs."""
+    rng = np.random.default_rng([len(shape), x == "bf16"])
+    pool, s = shaped(shape, kind, x, rng)
+    codes = spread_codes(rng, kind)
+    only = sorted({0, len(s["lens"]) - 1})
+    for sizes in ((1.0, -1.0, 0.0), (-1.0,), (0.0,), (1.0, 0.0), (-40.0, 1.0)):
+        rows_of(pool, s, 1, lambda t, sh: (codes(sh), rng.choice(sizes, (len(t), pool.H)) * (1 + rng.random((len(t), pool.H))) / TOP[kind]))
+        run_attend(pool, s)
+        check_ranges(pool, s, x, shape.startswith("prefix"), only)
     status_is(0)

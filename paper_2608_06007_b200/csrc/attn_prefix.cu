@@ -24,7 +24,8 @@
 // 186; a part of the exponentials as polynomials 154.  Codes: bound by the four warps that widen them
 // (512 requests x 32 heads behind 4000 e4m3 tokens 70 us, bf16 48, by a profiler; the calls 148 and 131).
 //
-// Scales of a quantised pool: K's multiply the scores, V's are taken into the values.
+// Scales of a quantised pool: K's multiply the scores, V's are taken into the values, over a power of two per tile that
+// goes into the probabilities.  The sum, without it, has a running maximum of its own: scales reach from 2^-126 to 2^127.
 // Every wait is bounded; one that runs out sets TC_DEVICE_BULK_WAIT_TIMEOUT and the CTA leaves.
 #include <algorithm>
 
@@ -45,7 +46,7 @@ struct PrefixShape {
     static constexpr int staged = KIND == kPlain ? 0 : 3;
     // Scores run a tile and a half ahead of the outputs (TWO), or three tiles.
     static constexpr int stages = KIND != kPlain ? (TWO ? 3 : 4) : TWO ? 4 : 6;
-    static constexpr int info = KIND == kPlain ? 16 : 48 + 4 * kTile;  // mask; exponent of V's, each warp's largest scale; scales of K
+    static constexpr int info = KIND == kPlain ? 16 : 64 + 4 * kTile;  // mask; V's exponent and whether it is far below others; each warp's largest scale; scales of K
     static constexpr int bytes = queries + stages * tile + staged * codes + kInfos * info + 256 + 1024;  // barriers, slack for the alignment
 };
 
@@ -110,6 +111,10 @@ __device__ __forceinline__ void tensor_load16(uint32_t addr, uint32_t (&r)[16])
 __device__ __forceinline__ void tensor_store16(uint32_t addr, const uint32_t (&r)[16])
 {
     asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15};" ::TC_W8(r, 0), TC_W8(r, 8), "r"(addr) : "memory");
+}
+__device__ __forceinline__ void tensor_store8(uint32_t addr, const uint32_t (&r)[8])
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%8], {%0,%1,%2,%3,%4,%5,%6,%7};" ::TC_W8(r, 0), "r"(addr) : "memory");
 }
 __device__ __forceinline__ void tensor_loaded() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tensor_stored() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
@@ -248,14 +253,39 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_kernel(const __grid_
         const int slot = warp >> 2, r = (warp & 3) * 32 + lane;
         const uint32_t lanes = tensor + (static_cast<uint32_t>((warp & 3) * 32) << 16), s_at = lanes, p_at = lanes + 128 + slot * 64, o_at = lanes + 256 + slot * 128;
         float top = -INFINITY;
+        float ref = -INFINITY;  // codes: the running maximum of the scores, which the sum is relative to; `top` has the tiles' powers in it
         float2 sum = make_float2(0.f, 0.f);
         int mine = 0;
+        auto scale_outputs = [&](float f) {
+#pragma unroll 1
+            for (int c = 0; c < DP / 16 && fine; c++) {
+                uint32_t v[16];
+                tensor_load16(o_at + 16 * c, v);
+                tensor_loaded();
+#pragma unroll
+                for (int i = 0; i < 16; i++) v[i] = __float_as_uint(__uint_as_float(v[i]) * f);
+                tensor_store16(o_at + 16 * c, v);
+            }
+        };
+        auto raise_ref = [&](float highest) {
+            const float to = fmaxf(ref, highest), less = exp2_approx(ref - (to == -INFINITY ? 0.f : to));
+            sum.x *= less, sum.y *= less;
+            ref = to;
+        };
         for (int t = slot; t < steps && fine; t += 2, mine++) {
             fine = __all_sync(0xffffffffu, barrier_wait(s_full + 8 * slot, mine & 1));
             if (!fine) break;
             fence_after();
             const int tile = TWO ? t >> 1 : t;
             const uint32_t about = info + (tile % kInfos) * Shape::info;
+            // P is free and O at rest when this slot's last product is done
+            bool rest = mine == 0;
+            auto await_rest = [&]() {
+                if (rest) return;
+                fine = __all_sync(0xffffffffu, barrier_wait(o_added + 8 * slot, (mine - 1) & 1));
+                fence_after();
+                rest = true;
+            };
             union {
                 uint32_t w[4][32];
                 float f[4][32];
@@ -265,19 +295,72 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_kernel(const __grid_
             for (int c = 0; c < 4; c++) tensor_load32(s_at + 32 * c, s.w[c]);
             uint32_t mask[4];
             asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(mask[0]), "=r"(mask[1]), "=r"(mask[2]), "=r"(mask[3]) : "r"(about));
+            float exponent = 0.f;
+            uint32_t far = 0;
+            if constexpr (KIND != kPlain) asm volatile("ld.shared.v2.b32 {%0,%1}, [%2];" : "=f"(exponent), "=r"(far) : "r"(about + 16));
             tensor_loaded();
+            if constexpr (KIND != kPlain) {
+                if (far) {
+                    // Rare: scales of V so far apart that what is next to nothing among the probabilities can be much of the sum.
+                    // Each key has its own power of two here, and the sum exponentials of its own; the scores
+                    // stay in tensor memory and are gone through twice, 16 at a time.
+                    float highest = -INFINITY, most = -INFINITY, base = 0.f, m = 0.f;
+#pragma unroll 1
+                    for (int pass = 0; pass < 2 && fine; pass++) {
+                        if (pass) {
+                            raise_ref(highest);
+                            base = ref == -INFINITY ? 0.f : ref;
+                            const float to = fmaxf(top, most), f = to == top ? 1.f : exp2_approx(top - to);
+                            top = to;
+                            m = top == -INFINITY ? 0.f : top;
+                            await_rest();
+                            if (mine) scale_outputs(f);
+                        }
+#pragma unroll 1
+                        for (int c = 0; c < 8 && fine; c++) {
+                            uint32_t v[16], w[8], here;
+                            tensor_load16(s_at + 16 * c, v);
+                            asm volatile("ld.shared.u32 %0, [%1];" : "=r"(here) : "r"(about + 4 * (c >> 1)));
+                            here >>= 16 * (c & 1);
+                            tensor_loaded();
+#pragma unroll
+                            for (int i = 0; i < 16; i += 4) {
+                                const float4 k4 = load_shared_f4(about + 64 + 4 * (16 * c + i));
+                                const float k[4] = {k4.x, k4.y, k4.z, k4.w};
+                                float x[4];
+#pragma unroll
+                                for (int j = 0; j < 4; j++) {
+                                    x[j] = here >> (i + j) & 1 ? __uint_as_float(v[i + j]) * (factor * k[j]) : -INFINITY;
+                                    if (!pass) {
+                                        highest = fmaxf(highest, x[j]), most = fmaxf(most, x[j] + exponent);
+                                    } else {
+                                        sum.x += exp2_approx(x[j] - base);
+                                        x[j] = exp2_approx(x[j] + exponent - m);
+                                    }
+                                }
+                                w[i / 2] = pack2<T>(x[0], x[1]), w[i / 2 + 1] = pack2<T>(x[2], x[3]);
+                            }
+                            if (pass) tensor_store8(p_at + 8 * c, w);
+                        }
+                    }
+                    if (!fine) break;
+                    tensor_stored();
+                    fence_before();
+                    barrier_arrive(s_taken + 8 * slot);
+                    barrier_arrive(p_ready + 8 * slot);
+                    continue;
+                }
+            }
             fence_before();
             barrier_arrive(s_taken + 8 * slot);
-            float exponent = 0.f;
             if constexpr (KIND != kPlain) {
-                asm volatile("ld.shared.f32 %0, [%1];" : "=f"(exponent) : "r"(about + 16));
-                const float2 f2 = make_float2(factor, factor), zero = make_float2(0.f, 0.f), e2 = make_float2(exponent, exponent);
+                const float2 f2 = make_float2(factor, factor), zero = make_float2(0.f, 0.f);
 #pragma unroll
                 for (int i = 0; i < 32; i++) {
-                    const float4 k = load_shared_f4(about + 48 + 16 * i);
+                    const float4 k = load_shared_f4(about + 64 + 16 * i);
                     float2 *x = &s.f2[i / 8][i % 8 * 2];
-                    x[0] = fused2(x[0], fused2(f2, make_float2(k.x, k.y), zero), e2);
-                    x[1] = fused2(x[1], fused2(f2, make_float2(k.z, k.w), zero), e2);
+                    x[0] = fused2(x[0], fused2(f2, make_float2(k.x, k.y), zero), zero);
+                    x[1] = fused2(x[1], fused2(f2, make_float2(k.z, k.w), zero), zero);
                 }
             }
             if ((mask[0] & mask[1] & mask[2] & mask[3]) != 0xffffffffu) {
@@ -294,34 +377,21 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_kernel(const __grid_
 #pragma unroll
                 for (int i = 2; i < 32; i += 2) m4[c] = larger3(m4[c], s.f[c][i], s.f[c][i + 1]);
             }
-            const float most = fmaxf(larger3(m4[0], m4[1], m4[2]), m4[3]) * (KIND == kPlain ? factor : 1.f);
-            // P is free and O at rest when this slot's last product is done
-            bool rest = mine == 0;
-            auto await_rest = [&]() {
-                if (rest) return;
-                fine = __all_sync(0xffffffffu, barrier_wait(o_added + 8 * slot, (mine - 1) & 1));
-                fence_after();
-                rest = true;
-            };
-            if (__any_sync(0xffffffffu, most > top + 8.f)) {
+            const float highest = fmaxf(larger3(m4[0], m4[1], m4[2]), m4[3]), most = KIND == kPlain ? highest * factor : highest + exponent;
+            bool move = most > top + 8.f;
+            if constexpr (KIND != kPlain) move = move || highest > ref + 8.f;
+            if (__any_sync(0xffffffffu, move)) {
+                if constexpr (KIND != kPlain) raise_ref(highest);
                 const float m = fmaxf(top, most), f = m == top ? 1.f : exp2_approx(top - m);
                 top = m;
-                sum.x *= f, sum.y *= f;
+                if constexpr (KIND == kPlain) sum.x *= f, sum.y *= f;
                 if (mine) {
                     await_rest();
-#pragma unroll 1
-                    for (int c = 0; c < DP / 16 && fine; c++) {
-                        uint32_t v[16];
-                        tensor_load16(o_at + 16 * c, v);
-                        tensor_loaded();
-#pragma unroll
-                        for (int i = 0; i < 16; i++) v[i] = __float_as_uint(__uint_as_float(v[i]) * f);
-                        tensor_store16(o_at + 16 * c, v);
-                    }
+                    scale_outputs(f);
                 }
             }
             const float m = top == -INFINITY ? 0.f : top;
-            const float2 minus = make_float2(-m, -m), f2 = make_float2(factor, factor);
+            const float2 minus = make_float2(exponent - m, exponent - m), f2 = make_float2(factor, factor);
             uint32_t w[4][16];
             float2 here = make_float2(0.f, 0.f);
 #pragma unroll
@@ -334,9 +404,13 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_kernel(const __grid_
                     w[c][i] = pack2<T>(e.x, e.y);
                 }
             }
-            // the tile's power of two is in its values: out of the sum
-            if constexpr (KIND == kPlain) sum = sum2(sum, here);
-            else sum = fused2(here, make_float2(exp2_approx(-exponent), exp2_approx(-exponent)), sum);
+            if constexpr (KIND == kPlain) {
+                sum = sum2(sum, here);
+            } else {
+                // `here` is relative to m - exponent, which is at most 48 above ref: exponent is no less than 40 below any before
+                const float all = here.x + here.y;
+                sum.x = fmaf(all, all == 0.f ? 0.f : exp2_approx(m - exponent - (ref == -INFINITY ? 0.f : ref)), sum.x);
+            }
             await_rest();  // by now it has been given, as a rule
             if (!fine) break;
 #pragma unroll
@@ -353,10 +427,21 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_kernel(const __grid_
         const int64_t req = store ? quick_div(static_cast<uint32_t>(row), p.div_group) : 0;
         const int64_t at = out_part * p.split.rows + req * p.Hq + h * group + (row - req * group);
         if (mine && fine) fine = __all_sync(0xffffffffu, barrier_wait(o_added + 8 * slot, (mine - 1) & 1));
+        const float base = KIND == kPlain ? top : ref;
         if (mine && fine) {
             fence_after();
-            const float inv = all == 0.f ? 0.f : 1.f / all;
-#pragma unroll
+            float inv = all == 0.f ? 0.f : 1.f / all;
+            if constexpr (KIND != kPlain) {
+                // outputs are relative to `top`: from there to `ref`, in two steps where fp32 does not hold one
+                float step = top - (base == -INFINITY ? 0.f : base);
+                if (__any_sync(0xffffffffu, !(fabsf(step) < 80.f))) {
+                    step *= 0.5f;
+                    scale_outputs(exp2_approx(step));
+                    tensor_stored();
+                }
+                inv *= exp2_approx(step);
+            }
+#pragma unroll(KIND == kPlain ? 1 : DP / 32)
             for (int c = 0; c < DP / 32; c++) {
                 uint32_t v[32];
                 tensor_load32(o_at + 32 * c, v);
@@ -364,11 +449,11 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_kernel(const __grid_
 #pragma unroll
                 for (int i = 0; i < 32; i += 4)
                     if (store && 32 * c + i < D)
-                        *reinterpret_cast<float4 *>(p.parts + at * D + 32 * c + i) =
-                            make_float4(__uint_as_float(v[i]) * inv, __uint_as_float(v[i + 1]) * inv, __uint_as_float(v[i + 2]) * inv, __uint_as_float(v[i + 3]) * inv);
+                        *reinterpret_cast<float4 *>(p.parts + at * D + 32 * c + i) = make_float4(__uint_as_float(v[i]) * inv, __uint_as_float(v[i + 1]) * inv,
+                                                                                                 __uint_as_float(v[i + 2]) * inv, __uint_as_float(v[i + 3]) * inv);
             }
         }
-        if (store) p.sums[at] = !mine || all == 0.f ? -INFINITY : (top == -INFINITY ? 0.f : top) + log2f(all);
+        if (store) p.sums[at] = !mine || all == 0.f ? -INFINITY : (base == -INFINITY ? 0.f : base) + log2f(all);
     } else if (warp < 12) {
         // --------------------------------------------------------------------------- the pages
         asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
@@ -476,6 +561,7 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_kernel(const __grid_
                 }
                 next_mask = __ballot_sync(0xffffffffu, there);
             };
+            int e_most = -133;  // the largest exponent of a tile so far
             fetch_scales(0);
             for (int u = 0; u < Shape::staged - 1; u++) fetch(u);
             for (int u = 0; u < 2 * tiles; u++) {
@@ -489,18 +575,21 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_kernel(const __grid_
                     const float scale_k = next_k;
                     scale_v = next_v;
                     if (lane == 0) asm volatile("st.shared.u32 [%0], %1;" ::"r"(about + 4 * w), "r"(next_mask) : "memory");
-                    asm volatile("st.shared.f32 [%0], %1;" ::"r"(about + 48 + 4 * (w * 32 + lane)), "f"(scale_k) : "memory");
+                    asm volatile("st.shared.f32 [%0], %1;" ::"r"(about + 64 + 4 * (w * 32 + lane)), "f"(scale_k) : "memory");
                     fetch_scales(tile + 1);
-                    float most = scale_v;  // a NaN is passed over
-#pragma unroll
-                    for (int x = 16; x; x >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, x));
-                    if (lane == 0) asm volatile("st.shared.f32 [%0], %1;" ::"r"(about + 32 + 4 * w), "f"(most) : "memory");
+                    const uint32_t size = scale_v > 0.f ? __float_as_uint(scale_v) : 0;  // a NaN is passed over
+                    const uint32_t warp_most = __reduce_max_sync(0xffffffffu, size);
+                    if (lane == 0) asm volatile("st.shared.u32 [%0], %1;" ::"r"(about + 32 + 4 * w), "r"(warp_most) : "memory");
                     asm volatile("bar.sync 1, 128;" ::: "memory");  // the four warps come here for every tile, whatever a wait said
-                    const float4 all = load_shared_f4(about + 32);
-                    most = fmaxf(fmaxf(all.x, all.y), fmaxf(all.z, all.w));
-                    const int e = most > 0.f ? static_cast<int>(__float_as_uint(most) >> 23) - 127 - 6 : 0;
-                    scale_v *= __uint_as_float(static_cast<uint32_t>(min(max(127 - e, 1), 254)) << 23);
-                    if (w == 0 && lane == 0) asm volatile("st.shared.f32 [%0], %1;" ::"r"(about + 16), "f"(static_cast<float>(e)) : "memory");
+                    uint32_t all[4];
+                    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(all[0]), "=r"(all[1]), "=r"(all[2]), "=r"(all[3]) : "r"(about + 32));
+                    const int e = static_cast<int>(max(max(all[0], all[1]), max(all[2], all[3])) >> 23) - 127 - 6;  // a tile of zeros: the least
+                    const bool far = e < e_most - 40;
+                    e_most = max(e_most, e);
+                    // 2^-e, up to 2^133, in two factors
+                    scale_v *= __uint_as_float(static_cast<uint32_t>(127 + min(-e, 127)) << 23);
+                    scale_v *= __uint_as_float(static_cast<uint32_t>(127 + max(-e - 127, 0)) << 23);
+                    if (w == 0 && lane == 0) asm volatile("st.shared.v2.b32 [%0], {%1,%2};" ::"r"(about + 16), "f"(static_cast<float>(e)), "r"(static_cast<uint32_t>(far)) : "memory");
                 }
                 const uint32_t from = mine + (u % Shape::staged) * Shape::codes, to = ring + stage * Shape::tile;
                 const uint32_t factor2 = pack2<__half>(scale_v, scale_v);

@@ -142,7 +142,7 @@ V_SCALES = {
 }
 
 
-@pytest.mark.parametrize("shape", STREAMS)
+@pytest.mark.parametrize("shape", SHAPES)
 @pytest.mark.parametrize("kind,x", [("e4m3", "bf16"), ("int8", "bf16")])
 @pytest.mark.parametrize("scales", V_SCALES)
 def test_attention_over_scales_of_v_at_the_ends_of_their_range(shape, kind, x, scales):

@@ -46,7 +46,7 @@ struct PrefixShape {
     static constexpr int staged = KIND == kPlain ? 0 : 3;
     // Scores run a tile and a half ahead of the outputs (TWO), or three tiles.
     static constexpr int stages = KIND != kPlain ? (TWO ? 3 : 4) : TWO ? 4 : 6;
-    static constexpr int info = KIND == kPlain ? 16 : 64 + 4 * kTile;  // mask; V's exponent and whether it is far below others; each warp's largest scale; scales of K
+    static constexpr int info = KIND == kPlain ? 16 : 64 + 8 * kTile;  // mask; V's exponent, whether scales are far apart; each warp's largest and smallest; scales of K; keys' exponents
     static constexpr int bytes = queries + stages * tile + staged * codes + kInfos * info + 256 + 1024;  // barriers, slack for the alignment
 };
 
@@ -326,16 +326,17 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_kernel(const __grid_
 #pragma unroll
                             for (int i = 0; i < 16; i += 4) {
                                 const float4 k4 = load_shared_f4(about + 64 + 4 * (16 * c + i));
-                                const float k[4] = {k4.x, k4.y, k4.z, k4.w};
+                                const float4 e4 = load_shared_f4(about + 64 + 4 * kTile + 4 * (16 * c + i));
+                                const float k[4] = {k4.x, k4.y, k4.z, k4.w}, e[4] = {e4.x, e4.y, e4.z, e4.w};
                                 float x[4];
 #pragma unroll
                                 for (int j = 0; j < 4; j++) {
                                     x[j] = here >> (i + j) & 1 ? __uint_as_float(v[i + j]) * (factor * k[j]) : -INFINITY;
                                     if (!pass) {
-                                        highest = fmaxf(highest, x[j]), most = fmaxf(most, x[j] + exponent);
+                                        highest = fmaxf(highest, x[j]), most = fmaxf(most, x[j] + e[j]);
                                     } else {
                                         sum.x += exp2_approx(x[j] - base);
-                                        x[j] = exp2_approx(x[j] + exponent - m);
+                                        x[j] = exp2_approx(x[j] + e[j] - m);
                                     }
                                 }
                                 w[i / 2] = pack2<T>(x[0], x[1]), w[i / 2 + 1] = pack2<T>(x[2], x[3]);
@@ -519,7 +520,10 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_kernel(const __grid_
             // Codes: a warp fetches and widens its own 32 keys of every tile.  V's are multiplied by their scales over a
             // power of two that the tile's largest scale sets, 2^exponent, which puts the values below 2^16: rounded
             // to fp16 twice (the factor and the product), half a step of 2^-11 each, like the probabilities
-            // that they meet.  K's scales are left to the scores, in fp32, for the sake of the logarithms.
+            // that they meet.  Products below fp16's normal numbers are off by half of 2^-24, which is 2^-15 of the
+            // key's scale at most, since a tile whose scales span more than 2^16 is `far`: there each key
+            // has an exponent of its own.  So it is where a tile's largest scale is 2^-40 of one before.  K's scales are left to the
+            // scores, in fp32, for the sake of the logarithms.
             constexpr int chunks = DP / 16;
             const uint32_t mine = staging + w * 32 * DP;
             int32_t ahead = look_up(0);
@@ -578,18 +582,27 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_kernel(const __grid_
                     asm volatile("st.shared.f32 [%0], %1;" ::"r"(about + 64 + 4 * (w * 32 + lane)), "f"(scale_k) : "memory");
                     fetch_scales(tile + 1);
                     const uint32_t size = scale_v > 0.f ? __float_as_uint(scale_v) : 0;  // a NaN is passed over
-                    const uint32_t warp_most = __reduce_max_sync(0xffffffffu, size);
-                    if (lane == 0) asm volatile("st.shared.u32 [%0], %1;" ::"r"(about + 32 + 4 * w), "r"(warp_most) : "memory");
+                    const uint32_t warp_most = __reduce_max_sync(0xffffffffu, size), warp_least = __reduce_min_sync(0xffffffffu, size ? size : 0x7f800000u);
+                    if (lane == 0) {
+                        asm volatile("st.shared.u32 [%0], %1;" ::"r"(about + 32 + 4 * w), "r"(warp_most) : "memory");
+                        asm volatile("st.shared.u32 [%0], %1;" ::"r"(about + 48 + 4 * w), "r"(warp_least) : "memory");
+                    }
                     asm volatile("bar.sync 1, 128;" ::: "memory");  // the four warps come here for every tile, whatever a wait said
-                    uint32_t all[4];
+                    uint32_t all[4], low[4];
                     asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(all[0]), "=r"(all[1]), "=r"(all[2]), "=r"(all[3]) : "r"(about + 32));
-                    const int e = static_cast<int>(max(max(all[0], all[1]), max(all[2], all[3])) >> 23) - 127 - 6;  // a tile of zeros: the least
-                    const bool far = e < e_most - 40;
+                    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(low[0]), "=r"(low[1]), "=r"(low[2]), "=r"(low[3]) : "r"(about + 48));
+                    int e = static_cast<int>(max(max(all[0], all[1]), max(all[2], all[3])) >> 23) - 127 - 6;  // a tile of zeros: the least
+                    const bool far = e < e_most - 40 || static_cast<int>(min(min(low[0], low[1]), min(low[2], low[3])) >> 23) - 127 - 6 < e - 16;
                     e_most = max(e_most, e);
+                    if (w == 0 && lane == 0) asm volatile("st.shared.v2.b32 [%0], {%1,%2};" ::"r"(about + 16), "f"(static_cast<float>(e)), "r"(static_cast<uint32_t>(far)) : "memory");
+                    if (far) {
+                        // each key's own; one of zeros takes no part in the probabilities
+                        e = static_cast<int>(size >> 23) - 127 - 6;
+                        asm volatile("st.shared.f32 [%0], %1;" ::"r"(about + 64 + 4 * kTile + 4 * (w * 32 + lane)), "f"(scale_v == 0.f ? -4096.f : static_cast<float>(e)) : "memory");
+                    }
                     // 2^-e, up to 2^133, in two factors
                     scale_v *= __uint_as_float(static_cast<uint32_t>(127 + min(-e, 127)) << 23);
                     scale_v *= __uint_as_float(static_cast<uint32_t>(127 + max(-e - 127, 0)) << 23);
-                    if (w == 0 && lane == 0) asm volatile("st.shared.v2.b32 [%0], {%1,%2};" ::"r"(about + 16), "f"(static_cast<float>(e)), "r"(static_cast<uint32_t>(far)) : "memory");
                 }
                 const uint32_t from = mine + (u % Shape::staged) * Shape::codes, to = ring + stage * Shape::tile;
                 const uint32_t factor2 = pack2<__half>(scale_v, scale_v);

@@ -160,6 +160,26 @@ def test_attention_over_scales_of_v_at_the_ends_of_their_range(shape, kind, x, s
     status_is(0)
 
 
+@pytest.mark.parametrize("shape", SHAPES)
+@pytest.mark.parametrize("kind,x", [("e4m3", "bf16"), ("int8", "bf16")])
+@pytest.mark.parametrize("power", [-10, -24, -40, -90])
+def test_attention_that_looks_at_one_key_of_a_small_scale(shape, kind, x, power):
+    """One key has all of the weight, and a V far smaller than its neighbours'."""
+    rng = np.random.default_rng([len(shape), -power])
+    pool, s = shaped(shape, kind, x, rng)
+    at = (s["prefix"] or s["lens"][0]) // 2 + 5
+    codes = spread_codes(rng, kind)
+    rows_of(pool, s, 1, lambda t, sh: (codes(sh), np.where(t == at, 2.0 ** power, 1.0)[:, None] * np.ones(pool.H)))
+    rows_of(pool, s, 0, lambda t, sh: ((t == at)[:, None, None] * np.full(sh, 64.0), np.full(sh[:2], 1 / 16)))
+    q = torch.from_numpy(8.0 + rng.random(s["q"].shape)).to(s["q"].dtype)  # that key's scores: 34 sqrt(D), the others' 0
+    s["q"] = q
+    s["dq"].copy_(q)
+    run_attend(pool, s)
+    check_ranges(pool, s, x, shape.startswith("prefix"), [0])
+    assert np.abs(np64(s["out"])[0]).max() < 2.0 ** power * TOP[kind] * 1.01 + 1e-30
+    status_is(0)
+
+
 @pytest.mark.parametrize("shape", STREAMS)
 @pytest.mark.parametrize("kind,x", [("e4m3", "bf16"), ("int8", "fp16")])
 def test_attention_over_scales_of_v_that_are_zero_or_negative(shape, kind, x):

@@ -581,7 +581,7 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_kernel(const __grid_
                     if (lane == 0) asm volatile("st.shared.u32 [%0], %1;" ::"r"(about + 4 * w), "r"(next_mask) : "memory");
                     asm volatile("st.shared.f32 [%0], %1;" ::"r"(about + 64 + 4 * (w * 32 + lane)), "f"(scale_k) : "memory");
                     fetch_scales(tile + 1);
-                    const uint32_t size = scale_v > 0.f ? __float_as_uint(scale_v) : 0;  // a NaN is passed over
+                    const uint32_t bits = __float_as_uint(scale_v) & 0x7fffffffu, size = bits > 0x7f800000u ? 0 : bits;  // a NaN is passed over
                     const uint32_t warp_most = __reduce_max_sync(0xffffffffu, size), warp_least = __reduce_min_sync(0xffffffffu, size ? size : 0x7f800000u);
                     if (lane == 0) {
                         asm volatile("st.shared.u32 [%0], %1;" ::"r"(about + 32 + 4 * w), "r"(warp_most) : "memory");

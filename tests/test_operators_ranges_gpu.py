@@ -180,7 +180,7 @@ def test_attention_that_looks_at_one_key_of_a_small_scale(shape, kind, x, power)
     status_is(0)
 
 
-@pytest.mark.parametrize("shape", STREAMS)
+@pytest.mark.parametrize("shape", SHAPES)
 @pytest.mark.parametrize("kind,x", [("e4m3", "bf16"), ("int8", "fp16")])
 def test_attention_over_scales_of_v_that_are_zero_or_negative(shape, kind, x):
     """A value is code * scale whatever wrote them: codes under a scale of 0 are zeros, a negative one turns signs."""

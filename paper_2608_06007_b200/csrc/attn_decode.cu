@@ -5,7 +5,8 @@
 // prefix_kernel (attn_prefix.cu) takes a prefix that many rows share, stream_kernel all other keys.
 // Softmax statistics, scores and outputs are fp32 throughout; only the probabilities are rounded, to 16
 // bits, to enter the second matrix product (half a step of 2^-8 or 2^-11 relative to each, no worse than
-// the rounding of the values and of the output to those types).
+// the rounding of the values and of the output to those types; in fp16 so down to 2^-21 of the largest, and by at most
+// 2^-32 of it below that).
 #include <algorithm>
 #include <cmath>
 
@@ -126,6 +127,7 @@ __global__ void __launch_bounds__(128, DP > 128 ? 1 : NB > 1 ? 2 : DP == 64 ? 4 
     using ST = std::conditional_t<KIND == kPlain, T, __half>;
     using VT = ST;
     constexpr int kCols = 8 * NB;
+    constexpr float kLift = probability_lift<VT>();
     extern __shared__ __align__(128) unsigned char shared[];
     __shared__ uint32_t sums_of[4], start_at[4], start_off[4];
     allow_next();
@@ -498,7 +500,7 @@ __global__ void __launch_bounds__(128, DP > 128 ? 1 : NB > 1 ? 2 : DP == 64 ? 4 
         uint32_t pf[R::groups][NB][2];
 #pragma unroll
         for (int nb = 0; nb < NB; nb++) {
-            const float m0 = top[nb][0] == -INFINITY ? 0.f : top[nb][0], m1 = top[nb][1] == -INFINITY ? 0.f : top[nb][1];
+            const float m0 = top[nb][0] == -INFINITY ? 0.f : top[nb][0] - kLift, m1 = top[nb][1] == -INFINITY ? 0.f : top[nb][1] - kLift;
             const float r0 = ref[nb][0] == -INFINITY ? 0.f : ref[nb][0], r1 = ref[nb][1] == -INFINITY ? 0.f : ref[nb][1];
 #pragma unroll
             for (int sub = 0; sub < R::groups; sub++) {
@@ -567,11 +569,11 @@ __global__ void __launch_bounds__(128, DP > 128 ? 1 : NB > 1 ? 2 : DP == 64 ? 4 
                     const int64_t where = whole ? slot * p.split.rows + req * p.Hq + it.h * group + (row - req * group) : piece + col;
                     float *dst = (whole ? p.parts : p.pieces) + where * D;
                     const float base = KIND == kPlain ? top[nb][j] : ref[nb][j];
-                    const float inv = all == 0.f ? 0.f : 1.f / all, log = all == 0.f ? -INFINITY : (base == -INFINITY ? 0.f : base) + log2f(all);
+                    const float inv = all == 0.f ? 0.f : 1.f / all, log = all == 0.f ? -INFINITY : (base == -INFINITY ? 0.f : base - (KIND == kPlain ? kLift : 0.f)) + log2f(all);
                     float by = inv;
                     if constexpr (KIND != kPlain) {
                         // outputs are relative to `top`: from there to `ref`, in two steps where fp32 does not hold one
-                        float step = top[nb][j] - (base == -INFINITY ? 0.f : base);
+                        float step = top[nb][j] - kLift - (base == -INFINITY ? 0.f : base);
                         if (!(fabsf(step) < 80.f)) {
                             step *= 0.5f;
 #pragma unroll

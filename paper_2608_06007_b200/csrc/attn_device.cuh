@@ -1,6 +1,8 @@
 // Device helpers that the kernels of tc_attn_decode share.
 #pragma once
 
+#include <type_traits>
+
 #include "attn.h"
 #include "ops_device.cuh"
 
@@ -31,6 +33,10 @@ __device__ __forceinline__ float exp2_approx(float x)
 }
 
 enum { kPlain = 0, kE4m3 = 1, kInt8 = 2 };
+
+// Probabilities are multiplied by 2 to this power before they are rounded.  They are up to 2^8, since a running maximum may
+// lag by that much; in fp16, whose normal numbers end at 2^-14, 2^7 more is what there is room for.
+template <typename T> __device__ constexpr float probability_lift() { return std::is_same<T, __half>::value ? 7.f : 0.f; }
 
 // Four codes as two pairs of fp16 numbers, exactly.
 template <int KIND>

@@ -165,6 +165,7 @@ template <typename T, int KIND, int DP, bool TWO>
 __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_kernel(const __grid_constant__ AttnParams p)
 {
     using Shape = PrefixShape<KIND, DP, TWO>;
+    constexpr float kLift = probability_lift<T>();
     extern __shared__ unsigned char raw[];
     allow_next();
     const uint32_t base = (static_cast<uint32_t>(__cvta_generic_to_shared(raw)) + 1023) & ~1023u;
@@ -312,7 +313,7 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_kernel(const __grid_
                             base = ref == -INFINITY ? 0.f : ref;
                             const float to = fmaxf(top, most), f = to == top ? 1.f : exp2_approx(top - to);
                             top = to;
-                            m = top == -INFINITY ? 0.f : top;
+                            m = top == -INFINITY ? 0.f : top - kLift;
                             await_rest();
                             if (mine) scale_outputs(f);
                         }
@@ -391,7 +392,7 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_kernel(const __grid_
                     scale_outputs(f);
                 }
             }
-            const float m = top == -INFINITY ? 0.f : top;
+            const float m = top == -INFINITY ? 0.f : top - kLift;
             const float2 minus = make_float2(exponent - m, exponent - m), f2 = make_float2(factor, factor);
             uint32_t w[4][16];
             float2 here = make_float2(0.f, 0.f);
@@ -428,13 +429,13 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_kernel(const __grid_
         const int64_t req = store ? quick_div(static_cast<uint32_t>(row), p.div_group) : 0;
         const int64_t at = out_part * p.split.rows + req * p.Hq + h * group + (row - req * group);
         if (mine && fine) fine = __all_sync(0xffffffffu, barrier_wait(o_added + 8 * slot, (mine - 1) & 1));
-        const float base = KIND == kPlain ? top : ref;
+        const float base = KIND == kPlain ? top - kLift : ref;
         if (mine && fine) {
             fence_after();
             float inv = all == 0.f ? 0.f : 1.f / all;
             if constexpr (KIND != kPlain) {
                 // outputs are relative to `top`: from there to `ref`, in two steps where fp32 does not hold one
-                float step = top - (base == -INFINITY ? 0.f : base);
+                float step = top - kLift - (base == -INFINITY ? 0.f : base);
                 if (__any_sync(0xffffffffu, !(fabsf(step) < 80.f))) {
                     step *= 0.5f;
                     scale_outputs(exp2_approx(step));

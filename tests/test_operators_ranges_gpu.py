@@ -193,3 +193,40 @@ def test_attention_over_scales_of_v_that_are_zero_or_negative(shape, kind, x):
         run_attend(pool, s)
         check_ranges(pool, s, x, shape.startswith("prefix"), only)
     status_is(0)
+
+
+@pytest.mark.parametrize("shape", SHAPES)
+@pytest.mark.parametrize("kind", ["fp16", "e4m3", "int8"])
+def test_attention_over_many_small_probabilities(shape, kind):
+    """One key above all the others, whose probabilities are then below fp16's normal numbers, but are most of the output."""
+    rng = np.random.default_rng([len(shape), 4])
+    pool, s = shaped(shape, kind, "fp16", rng, plain_tiles=kind == "fp16")
+    n = s["prefix"] or s["lens"][0]
+    at = 3
+    one = np.zeros((n, pool.H, pool.D))
+    key = one.copy()
+    key[at] = 1.0
+    val = one + 1.0
+    val[at] = 0.0
+    table = s["shared"] if s["prefix"] else s["table"][0]
+    t = np.arange(n)
+    for plane, rows in ((0, key), (1, val)):
+        if kind == "fp16":
+            pool.codes(plane).zero_()
+            pool.codes(plane)[dev(table[t // 16]).long(), dev(t % 16)] = torch.from_numpy(rows).half().view(torch.uint8).cuda()
+            s["values"][plane] = np64(pool.codes(plane).contiguous().view(torch.float16))
+        else:
+            rows_of(pool, s, plane, lambda i, sh: (rows[i] if len(i) and i[0] < n and len(i) == n else np.zeros(sh), np.ones(sh[:2])))
+    for above in (9.0, 12.0, 14.0):  # natural logarithms: 2^-13 to 2^-20
+        q = torch.full(s["q"].shape, above * pool.D ** 0.5 / pool.D).half()
+        s["q"] = q
+        s["dq"].copy_(q)
+        run_attend(pool, s)
+        r = 0
+        keys, vals = (np.concatenate([tokens_of(v, s["shared"], 0, s["prefix"], 16), tokens_of(v, s["table"][r], 0, s["lens"][r], 16)]) for v in s["values"])
+        want, want_lse, mass = orc.attend(np64(q)[r], keys, vals, pool.D ** -0.5)
+        # probabilities: half a step of 2^-11 (and the prefix kernel's values, 1, exactly), down to 2^-21 of the largest; below that 2^-32 of it
+        most = (2.0 ** -11 * (1 + 2.0 ** -6) + 2.0 ** -15) * mass + len(keys) * 2.0 ** -32 * np.abs(vals).max() + 2.0 ** -11 * np.abs(want) + 2.0 ** -25
+        off = np.abs(np64(s["out"])[r] - want)
+        assert (off <= most).all(), (above, off.max(), want.max(), (off / most).max())
+    status_is(0)

@@ -230,3 +230,118 @@ def test_attention_over_many_small_probabilities(shape, kind):
         off = np.abs(np64(s["out"])[r] - want)
         assert (off <= most).all(), (above, off.max(), want.max(), (off / most).max())
     status_is(0)
+
+
+# The prefix kernel in the cases that the stream is tested in.
+PLAIN = [("bf16", "bf16"), ("fp16", "fp16"), ("bf16", "e4m3"), ("fp16", "int8")]
+
+
+@pytest.mark.parametrize("shape", PREFIXES)
+@pytest.mark.parametrize("x,kind", PLAIN)
+@pytest.mark.parametrize("layout,B", [("nhd", 16), ("hnd", 5)])
+def test_a_prefix_shared_by_many(shape, x, kind, layout, B):
+    rng = np.random.default_rng([len(shape), B])
+    pool, s = shaped(shape, kind, x, rng, layout=layout, B=B)
+    s["lens"][1] = -1
+    s["d"]["lens"][1] = -1
+    run_attend(pool, s)
+    check(pool, s, x, True, {0, 1, 2, len(s["lens"]) - 1})
+    status_is(0)
+    # a negative scale, and scores far apart
+    for scale in (-0.2, 0.9):
+        run_attend(pool, s, scale=scale)
+        check(pool, dict(s, q=-s["q"] if scale < 0 else s["q"], scale=abs(scale)), x, True, {0, 2, len(s["lens"]) - 1})
+    status_is(0)
+
+
+@pytest.mark.parametrize("shape", PREFIXES)
+@pytest.mark.parametrize("x,kind", PLAIN)
+def test_a_prefix_shorter_than_announced_or_out_of_range(shape, x, kind):
+    rng = np.random.default_rng([len(shape), 6])
+    pool, s = shaped(shape, kind, x, rng)
+    full, some = s["prefix"], {0, len(s["lens"]) - 1}
+    for n in (full - 1, full // 2 + 3, 129, 128, 1, 0):
+        s["d"]["prefix_len"][0] = n
+        run_attend(pool, s, max_prefix=full)
+        check(pool, dict(s, prefix=n), x, True, some)
+    status_is(0)
+    for n, cut in ((-7, 0), (full + 5000, full)):
+        s["d"]["prefix_len"][0] = n
+        run_attend(pool, s, max_prefix=full)
+        status_is(tc.TC_DEVICE_BAD_INDEX)
+        check(pool, dict(s, prefix=cut), x, True, some)
+    # block ids that the pool does not have: their keys are left out, as if the prefix were without them
+    s["d"]["prefix_len"][0] = full
+    for i, bad in ((2, -1), (9, pool.blocks), (full // 16 - 1, 2 ** 31 - 1)):
+        s["d"]["prefix_table"][i] = bad
+    run_attend(pool, s)
+    status_is(tc.TC_DEVICE_BAD_INDEX)
+    keep = [i for i in range(len(s["shared"])) if i not in (2, 9, full // 16 - 1)]
+    check(pool, dict(s, prefix=full - 48, shared=s["shared"][keep]), x, True, some)
+    status_is(0)
+
+
+@pytest.mark.parametrize("shape", PREFIXES)
+@pytest.mark.parametrize("x,kind,apart", [(x, kind, False) for x, kind in PLAIN] + [("bf16", "e4m3", True), ("bf16", "int8", True)])
+def test_a_prefix_with_rows_that_are_not_finite(shape, x, kind, apart):
+    rng = np.random.default_rng([len(shape), 8])
+    pool, s = shaped(shape, kind, x, rng)
+    if apart:  # scales of V far from one another
+        pool.scale(1).mul_(dev(10.0 ** rng.uniform(-20, 0, (pool.blocks, pool.B, pool.H)), torch.float32))
+    R, Hq = s["q"].shape[:2]
+    g = Hq // pool.H
+    block = int(s["shared"][7])
+    nan = torch.zeros(R, Hq, dtype=torch.bool)
+    # V: the outputs of its KV head are NaN, the logarithms are not
+    if kind in TOP:
+        pool.scale(1)[block, 5, 0] = float("nan")
+        pool.codes(1)[block, 5, 0] = 0
+    else:
+        pool.codes(1)[block, 5, 0] = 0xFF
+    run_attend(pool, s)
+    nan[:, :g] = True
+    out = s["out"].cpu()
+    assert torch.equal(out.isnan().all(-1), nan) and torch.equal(out.isnan().any(-1), nan) and torch.isfinite(s["lse"]).all()
+    # K: both
+    if kind in TOP:
+        pool.scale(0)[block, 5, 1] = float("nan")
+    else:
+        pool.codes(0)[block, 5, 1] = 0xFF
+    run_attend(pool, s)
+    nan[:, g : 2 * g] = True
+    out, lse = s["out"].cpu(), s["lse"].cpu()
+    want = torch.zeros_like(nan)
+    want[:, g : 2 * g] = True
+    assert torch.equal(out.isnan().any(-1), nan) and torch.equal(lse.isnan(), want)
+    # a query: its row
+    s["dq"][1, 3 * g] = float("nan")
+    run_attend(pool, s)
+    nan[1, 3 * g] = want[1, 3 * g] = True
+    assert torch.equal(s["out"].cpu().isnan().any(-1), nan) and torch.equal(s["lse"].cpu().isnan(), want)
+    status_is(0)
+
+
+@pytest.mark.parametrize("shape", ["stream", "prefix 128", "prefix 256"])
+@pytest.mark.parametrize("kind", ["bf16", "e4m3"])
+def test_a_captured_decode_replays_with_new_lengths(shape, kind):
+    """Outputs after every replay, of all requests, the padded ones' untouched."""
+    rng = np.random.default_rng([len(shape), 33])
+    R, H, g, D, prefix, most = SHAPES[shape]
+    assert prefix_taken_by(R, H * g, H, D, most, prefix, kind in TOP) == shape
+    pool = Pool(kind, D=D, H=H, blocks=R * -(-most // 16) + -(-prefix // 16) + 3)
+    s = attend_case(pool, [most] * R, prefix, H * g, "bf16", rng, poison=False)
+    run_attend(pool, s)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run_attend(pool, s, stream=torch.cuda.current_stream())
+    for lens, n in (([most] * R, prefix), (rng.integers(-1, most + 1, R).tolist(), prefix // 3), ([0] * (R - 1) + [-1], 1), (rng.integers(0, 3, R).tolist(), 0), ([most] * R, prefix - 1)):
+        s["d"]["lens"].copy_(dev(np.array(lens, dtype=np.int32)))
+        s["d"]["prefix_len"].fill_(n)
+        s["out"].fill_(9.0), s["lse"].fill_(9.0)
+        s["workspace"].fill_(0xFF)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        check(pool, dict(s, lens=lens, prefix=n), "bf16", shape != "stream", set(range(0, R, max(1, R // 6))) | {R - 1})
+    status_is(0)

@@ -491,8 +491,8 @@ def _dtype(t):
     """(TC_* number, bytes) of a torch tensor's element type."""
     if not _dtypes:
         import torch
+        _integers.update({torch.int32: 4, torch.uint32: 4, torch.int64: 8, torch.uint64: 8})  # first: another thread goes by _dtypes
         _dtypes.update({torch.bfloat16: (TC_BF16, 2), torch.float16: (TC_FP16, 2), torch.float32: (TC_FP32, 4)})
-        _integers.update({torch.int32: 4, torch.uint32: 4, torch.int64: 8, torch.uint64: 8})
     try:
         return _dtypes[t.dtype]
     except KeyError:

@@ -828,6 +828,7 @@ static int check_decode(const tc_kv_layer_t *layer, const tc_attn_decode_t *a, A
     if (a->R * a->Hq > (1 << 30)) return fail(TC_ERR_TOO_LARGE, "R * Hq = %lld rows: too many for one call", (long long)(a->R * a->Hq));
     if (a->max_len < 0 || a->max_len > INT32_MAX - 4096 || a->max_prefix < 0 || a->max_prefix > INT32_MAX - 4096)
         return fail(TC_ERR_SHAPE, "max_len %lld and max_prefix %lld must be in [0, 2^31 - 4096)", (long long)a->max_len, (long long)a->max_prefix);
+    if (a->reserved) return fail(TC_ERR_INVALID_ARG, "reserved is %d, not 0", a->reserved);
     if (!(std::fabs(a->scale) <= 1e30f)) return fail(TC_ERR_INVALID_ARG, "scale is not a number of at most 1e30");
     if (a->R * p->layer.H > (1 << 30) / std::max<int64_t>(1, (a->max_len + 15) / 16)) return fail(TC_ERR_TOO_LARGE, "R * H * max_len = %lld * %d * %lld: too many keys for one call", (long long)a->R, p->layer.H, (long long)a->max_len);
     split_attn(a->R, a->Hq, p->layer.H, D, a->max_len, a->max_prefix, p->layer.quantised(), &p->split);

@@ -1,4 +1,5 @@
 """Calls of the operators that are refused, and first calls of a process, without a GPU."""
+import ctypes as C
 import threading
 
 import pytest
@@ -6,7 +7,7 @@ import torch
 
 import paper_2608_06007_b200 as tc
 from paper_2608_06007_b200 import binding as b
-from test_operators_host import layer
+from test_operators_host import INVALID, call, decode_args, layer
 
 
 def test_two_threads_may_make_the_first_call_of_a_process(monkeypatch):
@@ -28,3 +29,10 @@ def test_two_threads_may_make_the_first_call_of_a_process(monkeypatch):
     with pytest.raises(tc.TensorCastError):  # the library's refusal of the made-up addresses, not ValueError
         tc.tc_kv_append(layer(), k, k, torch.zeros(3, dtype=torch.int64))
     first.join()
+
+
+def test_decode_refuses_a_reserved_field_that_is_not_0():
+    args, size = decode_args(reserved=1), C.c_int64()
+    rc, why = call("tc_attn_decode", layer(), args)
+    assert rc == INVALID and "reserved" in why
+    assert tc.load_library().tc_attn_workspace(layer().ref, C.byref(args), C.byref(size)) == INVALID

@@ -504,7 +504,7 @@ typedef struct {
     int32_t dtype;        /* TC_BF16, TC_FP16 or TC_FP32: of q, k, v and q_out */
     int32_t rot_dim;      /* even, 0..D; 0 = no rotation */
     const void *q;        /* [n_tokens][Hq][D] or NULL */
-    void *q_out;          /* the rotated queries; may be q itself (same strides) */
+    void *q_out;          /* the rotated queries; q itself (same strides), or no byte of q's, k's and v's rows */
     const void *k, *v;    /* [n_tokens][H][D] */
     int64_t q_stride[2], q_out_stride[2], k_stride[2], v_stride[2]; /* token, head */
     const int64_t *slots;     /* [n_tokens] */
@@ -528,7 +528,7 @@ typedef struct {
     int64_t table_width, table_stride; /* entries per request, bytes from request to request */
     const int64_t *offsets; /* [R + 1], from 0, not decreasing */
     const int64_t *first;   /* [R] first token of each request, or NULL = 0 */
-    void *k_out, *v_out;    /* [n_rows][H][D]; either may be NULL */
+    void *k_out, *v_out;    /* [n_rows][H][D]; either may be NULL; no byte of one's rows belongs to the other's */
     int64_t k_stride[2], v_stride[2]; /* row, head */
 } tc_kv_gather_t;
 

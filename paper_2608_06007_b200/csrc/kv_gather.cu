@@ -210,6 +210,7 @@ extern "C" int tc_kv_gather(const tc_kv_layer_t *layer, const tc_kv_gather_t *a,
     if (!a->k_out && !a->v_out) return fail(TC_ERR_INVALID_ARG, "k_out or v_out is required");
     if (a->k_out && (rc = check_rows("k_out", a->k_out, a->k_stride, a->n_rows, p.layer.H, int64_t(D) * e, e, true, &align)) != TC_OK) return rc;
     if (a->v_out && (rc = check_rows("v_out", a->v_out, a->v_stride, a->n_rows, p.layer.H, int64_t(D) * e, e, true, &align)) != TC_OK) return rc;
+    if (a->k_out == a->v_out) return fail(TC_ERR_OVERLAP, "k_out is v_out: both planes would be written there");
     if (a->table_width < 1) return fail(TC_ERR_SHAPE, "table_width %lld < 1", (long long)a->table_width);
     if (a->table_stride < 0 || a->table_stride % 4 || reinterpret_cast<uintptr_t>(a->tables) % 4) return fail(TC_ERR_INVALID_ARG, "tables and table_stride must be multiples of 4 bytes");
     if (!a->tables || !a->offsets) return fail(TC_ERR_INVALID_ARG, "tables and offsets are required");

@@ -7,7 +7,7 @@ import torch
 
 import paper_2608_06007_b200 as tc
 from paper_2608_06007_b200 import binding as b
-from test_operators_host import INVALID, call, decode_args, layer
+from test_operators_host import BASE, INVALID, OVERLAP, call, decode_args, gather_args, layer
 
 
 def test_two_threads_may_make_the_first_call_of_a_process(monkeypatch):
@@ -36,3 +36,8 @@ def test_decode_refuses_a_reserved_field_that_is_not_0():
     rc, why = call("tc_attn_decode", layer(), args)
     assert rc == INVALID and "reserved" in why
     assert tc.load_library().tc_attn_workspace(layer().ref, C.byref(args), C.byref(size)) == INVALID
+
+
+def test_gather_refuses_one_output_for_both_planes():
+    rc, why = call("tc_kv_gather", layer(), gather_args(v_out=5 * BASE))
+    assert rc == OVERLAP and "v_out" in why

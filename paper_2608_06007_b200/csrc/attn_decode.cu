@@ -8,6 +8,7 @@
 // the rounding of the values and of the output to those types; in fp16 so down to 2^-21 of the largest, and by at most
 // 2^-32 of it below that).
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 
 #include "attn.h"
@@ -764,11 +765,11 @@ template <typename T, int KIND, int DP, int NB>
 static int launch_stream(const AttnParams &p, unsigned grid, int device, cudaStream_t s)
 {
     using R = Ring<KIND, DP>;
-    static bool raised[kMaxDevices];  // set once per device; setting it twice does no harm
-    if (!raised[device]) {
+    static std::atomic<bool> raised[kMaxDevices];  // set once per device; setting it twice does no harm
+    if (!raised[device].load(std::memory_order_relaxed)) {
         const cudaError_t e = cudaFuncSetAttribute(stream_kernel<T, KIND, DP, NB>, cudaFuncAttributeMaxDynamicSharedMemorySize, R::bytes);
         if (e != cudaSuccess) return cuda_fail(e, "cudaFuncSetAttribute(dynamic shared memory)");
-        raised[device] = true;
+        raised[device].store(true, std::memory_order_relaxed);
     }
     return launch_attn(stream_kernel<T, KIND, DP, NB>, grid, 128, R::bytes, p.split.prefix_parts > 0, p, s);
 }

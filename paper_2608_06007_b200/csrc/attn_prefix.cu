@@ -28,6 +28,7 @@
 // goes into the probabilities.  The sum, without it, has a running maximum of its own: scales reach from 2^-126 to 2^127.
 // Every wait is bounded; one that runs out sets TC_DEVICE_BULK_WAIT_TIMEOUT and the CTA leaves.
 #include <algorithm>
+#include <atomic>
 
 #include "attn.h"
 #include "attn_device.cuh"
@@ -712,11 +713,11 @@ static int launch_prefix_shape(const AttnParams &p, unsigned grid, int device, c
 {
     using Shape = PrefixShape<KIND, DP, TWO>;
     static_assert(Shape::bytes <= 232448, "more shared memory than a CTA can have");
-    static bool raised[kMaxDevices];
-    if (!raised[device]) {
+    static std::atomic<bool> raised[kMaxDevices];  // set once per device; setting it twice does no harm
+    if (!raised[device].load(std::memory_order_relaxed)) {
         const cudaError_t e = cudaFuncSetAttribute(prefix_kernel<T, KIND, DP, TWO>, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape::bytes);
         if (e != cudaSuccess) return cuda_fail(e, "cudaFuncSetAttribute(dynamic shared memory)");
-        raised[device] = true;
+        raised[device].store(true, std::memory_order_relaxed);
     }
     return launch_attn(prefix_kernel<T, KIND, DP, TWO>, grid, kPrefixThreads, Shape::bytes, false, p, s);
 }

@@ -2,6 +2,10 @@
 
 A case says which kernel takes its prefix - none, the stream, or the prefix kernel with 128 or 256 rows a CTA - and
 fails where the library's rule gives it to another."""
+import os
+import subprocess
+import sys
+
 import numpy as np
 import pytest
 import torch
@@ -345,3 +349,38 @@ def test_a_captured_decode_replays_with_new_lengths(shape, kind):
         torch.cuda.synchronize()
         check(pool, dict(s, lens=lens, prefix=n), "bf16", shape != "stream", set(range(0, R, max(1, R // 6))) | {R - 1})
     status_is(0)
+
+
+FIRST_CALLS = """
+import sys, threading
+sys.path[:0] = [{root!r}, {tests!r}]
+from test_operators_ranges_gpu import *
+rng = np.random.default_rng(5)
+cases = [(kind, *shaped(shape, kind, "bf16", rng)) for shape in ("stream", "prefix 128", "prefix 256") for kind in ("bf16", "e4m3") for _ in (0, 1)]
+streams = [torch.cuda.Stream() for _ in cases]
+torch.cuda.synchronize()
+begin = threading.Barrier(len(cases))
+failed = []
+def go(case, stream):
+    kind, pool, s = case
+    begin.wait()
+    try:
+        run_attend(pool, s, stream=stream)
+    except Exception as e:
+        failed.append(e)
+threads = [threading.Thread(target=go, args=x) for x in zip(cases, streams)]
+for t in threads: t.start()
+for t in threads: t.join()
+torch.cuda.synchronize()
+assert not failed, failed
+for i, (kind, pool, s) in enumerate(cases):
+    check(pool, s, "bf16", i >= 4, {{0, len(s["lens"]) - 1}})
+print("answered")
+"""
+
+
+def test_threads_may_make_the_first_calls_of_a_process_at_once():
+    """Every kernel's first launch, on a stream and a workspace of its own."""
+    here = os.path.dirname(os.path.abspath(__file__))
+    got = subprocess.run([sys.executable, "-c", FIRST_CALLS.format(root=os.path.dirname(here), tests=here)], capture_output=True, text=True, timeout=300)
+    assert got.returncode == 0 and "answered" in got.stdout, got.stderr[-2000:]

@@ -161,6 +161,75 @@ __device__ __forceinline__ float4 load_shared_f4(uint32_t addr)
     return v;
 }
 
+struct RowState {
+    float top, ref, sum;
+};
+
+// Rare: scales of V so far apart that what is next to nothing among the probabilities can be much of the sum.
+// Each key has its own power of two here, and the sum exponentials of its own; the scores
+// stay in tensor memory and are gone through twice, 16 at a time.  False when a wait ran out.  A function of its
+// own: in line, never run, it slowed the other tiles (512 requests behind 4000 e4m3 147 -> 150 us a call).
+template <int DP>
+__device__ __noinline__ bool far_tile(RowState &state, uint32_t s_at, uint32_t p_at, uint32_t o_at, uint32_t about, float factor, uint32_t o_added, int mine)
+{
+    constexpr float kLift = probability_lift<__half>();
+    float highest = -INFINITY, most = -INFINITY, base = 0.f, m = 0.f, sum = state.sum;
+#pragma unroll 1
+    for (int pass = 0; pass < 2; pass++) {
+        if (pass) {
+            const float ref = fmaxf(state.ref, highest);
+            base = ref == -INFINITY ? 0.f : ref;
+            sum *= exp2_approx(state.ref - base);
+            state.ref = ref;
+            const float to = fmaxf(state.top, most), f = to == state.top ? 1.f : exp2_approx(state.top - to);
+            state.top = to;
+            m = to == -INFINITY ? 0.f : to - kLift;
+            if (mine) {
+                if (!__all_sync(0xffffffffu, barrier_wait(o_added, (mine - 1) & 1))) return false;
+                fence_after();
+#pragma unroll 1
+                for (int c = 0; c < DP / 16; c++) {
+                    uint32_t v[16];
+                    tensor_load16(o_at + 16 * c, v);
+                    tensor_loaded();
+#pragma unroll
+                    for (int i = 0; i < 16; i++) v[i] = __float_as_uint(__uint_as_float(v[i]) * f);
+                    tensor_store16(o_at + 16 * c, v);
+                }
+            }
+        }
+#pragma unroll 1
+        for (int c = 0; c < 8; c++) {
+            uint32_t v[16], w[8], here;
+            tensor_load16(s_at + 16 * c, v);
+            asm volatile("ld.shared.u32 %0, [%1];" : "=r"(here) : "r"(about + 4 * (c >> 1)));
+            here >>= 16 * (c & 1);
+            tensor_loaded();
+#pragma unroll
+            for (int i = 0; i < 16; i += 4) {
+                const float4 k4 = load_shared_f4(about + 64 + 4 * (16 * c + i));
+                const float4 e4 = load_shared_f4(about + 64 + 4 * kTile + 4 * (16 * c + i));
+                const float k[4] = {k4.x, k4.y, k4.z, k4.w}, e[4] = {e4.x, e4.y, e4.z, e4.w};
+                float x[4];
+#pragma unroll
+                for (int j = 0; j < 4; j++) {
+                    x[j] = here >> (i + j) & 1 ? __uint_as_float(v[i + j]) * (factor * k[j]) : -INFINITY;
+                    if (!pass) {
+                        highest = fmaxf(highest, x[j]), most = fmaxf(most, x[j] + e[j]);
+                    } else {
+                        sum += exp2_approx(x[j] - base);
+                        x[j] = exp2_approx(x[j] + e[j] - m);
+                    }
+                }
+                w[i / 2] = pack2<__half>(x[0], x[1]), w[i / 2 + 1] = pack2<__half>(x[2], x[3]);
+            }
+            if (pass) tensor_store8(p_at + 8 * c, w);
+        }
+    }
+    state.sum = sum;
+    return true;
+}
+
 // T: the type of the products, fp16 for codes.
 template <typename T, int KIND, int DP, bool TWO>
 __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_kernel(const __grid_constant__ AttnParams p)
@@ -303,49 +372,9 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_kernel(const __grid_
             tensor_loaded();
             if constexpr (KIND != kPlain) {
                 if (far) {
-                    // Rare: scales of V so far apart that what is next to nothing among the probabilities can be much of the sum.
-                    // Each key has its own power of two here, and the sum exponentials of its own; the scores
-                    // stay in tensor memory and are gone through twice, 16 at a time.
-                    float highest = -INFINITY, most = -INFINITY, base = 0.f, m = 0.f;
-#pragma unroll 1
-                    for (int pass = 0; pass < 2 && fine; pass++) {
-                        if (pass) {
-                            raise_ref(highest);
-                            base = ref == -INFINITY ? 0.f : ref;
-                            const float to = fmaxf(top, most), f = to == top ? 1.f : exp2_approx(top - to);
-                            top = to;
-                            m = top == -INFINITY ? 0.f : top - kLift;
-                            await_rest();
-                            if (mine) scale_outputs(f);
-                        }
-#pragma unroll 1
-                        for (int c = 0; c < 8 && fine; c++) {
-                            uint32_t v[16], w[8], here;
-                            tensor_load16(s_at + 16 * c, v);
-                            asm volatile("ld.shared.u32 %0, [%1];" : "=r"(here) : "r"(about + 4 * (c >> 1)));
-                            here >>= 16 * (c & 1);
-                            tensor_loaded();
-#pragma unroll
-                            for (int i = 0; i < 16; i += 4) {
-                                const float4 k4 = load_shared_f4(about + 64 + 4 * (16 * c + i));
-                                const float4 e4 = load_shared_f4(about + 64 + 4 * kTile + 4 * (16 * c + i));
-                                const float k[4] = {k4.x, k4.y, k4.z, k4.w}, e[4] = {e4.x, e4.y, e4.z, e4.w};
-                                float x[4];
-#pragma unroll
-                                for (int j = 0; j < 4; j++) {
-                                    x[j] = here >> (i + j) & 1 ? __uint_as_float(v[i + j]) * (factor * k[j]) : -INFINITY;
-                                    if (!pass) {
-                                        highest = fmaxf(highest, x[j]), most = fmaxf(most, x[j] + e[j]);
-                                    } else {
-                                        sum.x += exp2_approx(x[j] - base);
-                                        x[j] = exp2_approx(x[j] + e[j] - m);
-                                    }
-                                }
-                                w[i / 2] = pack2<T>(x[0], x[1]), w[i / 2 + 1] = pack2<T>(x[2], x[3]);
-                            }
-                            if (pass) tensor_store8(p_at + 8 * c, w);
-                        }
-                    }
+                    RowState state{top, ref, sum.x + sum.y};
+                    fine = far_tile<DP>(state, s_at, p_at, o_at, about, factor, o_added + 8 * slot, mine);
+                    top = state.top, ref = state.ref, sum = make_float2(state.sum, 0.f);
                     if (!fine) break;
                     tensor_stored();
                     fence_before();

@@ -618,6 +618,7 @@ __global__ void __launch_bounds__(128, DP > 128 ? 1 : NB > 1 ? 2 : DP == 64 ? 4 
 // warp takes a row, four loads in flight leave registers for eight CTAs an SM.  Against five CTAs with eight loads, a
 // call of 512 requests of 32 heads, e4m3, D = 128, took 149 us for 157 behind a prefix of 4000 and 76 for 81 without.
 constexpr int kJoinCtas = 8;
+constexpr float kLess = 16.f;  // weights are 2^-16 at most: the outputs of up to that many parts may be next to the largest number
 template <typename T, int DP, int WARPS>
 __global__ void __launch_bounds__(WARPS == 1 ? 128 : 32 * WARPS, WARPS == 1 ? kJoinCtas : 1) join_kernel(const __grid_constant__ AttnParams p)
 {
@@ -710,7 +711,7 @@ __global__ void __launch_bounds__(WARPS == 1 ? 128 : 32 * WARPS, WARPS == 1 ? kJ
                         all *= f;
                         top = m;
                     }
-                    weight = sum == -INFINITY ? 0.f : exp2_approx(sum - (top == -INFINITY ? 0.f : top));  // NaN where the sum is
+                    weight = sum == -INFINITY ? 0.f : exp2_approx(sum - (top == -INFINITY ? 0.f : top) - kLess);  // NaN where the sum is
                     float add = weight;
 #pragma unroll
                     for (int x = 16; x; x >>= 1) add += __shfl_xor_sync(0xffffffffu, add, x);
@@ -755,7 +756,7 @@ __global__ void __launch_bounds__(WARPS == 1 ? 128 : 32 * WARPS, WARPS == 1 ? kJ
         for (int x = 0; x < kVectors; x++)
             if (lane * 4 + 128 * x < D)
                 *reinterpret_cast<uint2 *>(dst + (lane * 4 + 128 * x) * 2) = make_uint2(pack2<T>(acc[4 * x] * inv, acc[4 * x + 1] * inv), pack2<T>(acc[4 * x + 2] * inv, acc[4 * x + 3] * inv));
-        if (p.lse && lane == 0) p.lse[row] = all == 0.f ? -INFINITY : ((top == -INFINITY ? 0.f : top) + log2f(all)) * kLn2;
+        if (p.lse && lane == 0) p.lse[row] = all == 0.f ? -INFINITY : ((top == -INFINITY ? 0.f : top) + kLess + log2f(all)) * kLn2;
         if (WARPS > 1) return;
     }
 }

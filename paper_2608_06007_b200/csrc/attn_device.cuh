@@ -35,8 +35,9 @@ __device__ __forceinline__ float exp2_approx(float x)
 enum { kPlain = 0, kE4m3 = 1, kInt8 = 2 };
 
 // Probabilities are multiplied by 2 to this power before they are rounded.  They are up to 2^8, since a running maximum may
-// lag by that much; in fp16, whose normal numbers end at 2^-14, 2^7 more is what there is room for.
-template <typename T> __device__ constexpr float probability_lift() { return std::is_same<T, __half>::value ? 7.f : 0.f; }
+// lag by that much; in fp16, whose normal numbers end at 2^-14, 2^7 more is what there is room for.  bf16 has room below, and
+// values near 2^128, of which fp32 then holds sums of 2^16.
+template <typename T> __device__ constexpr float probability_lift() { return std::is_same<T, __half>::value ? 7.f : -16.f; }
 
 // Four codes as two pairs of fp16 numbers, exactly.
 template <int KIND>

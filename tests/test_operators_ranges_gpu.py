@@ -236,6 +236,31 @@ def test_attention_over_many_small_probabilities(shape, kind):
     status_is(0)
 
 
+@pytest.mark.parametrize("shape", SHAPES)
+@pytest.mark.parametrize("kind", ["bf16", "e4m3", "int8"])
+def test_attention_over_values_next_to_the_largest_number(shape, kind):
+    """Means of many values near 2^127, whose sums no fp32 holds; equal scores and ordinary ones."""
+    rng = np.random.default_rng([len(shape), 12])
+    pool, s = shaped(shape, kind, "bf16", rng)
+    for equal in (True, False):
+        if kind in TOP:
+            rows_of(pool, s, 1, lambda t, sh: (np.full(sh, TOP[kind]), np.full(sh[:2], 2.0 ** 127 * 0.9 / TOP[kind])))
+        else:
+            big = torch.full((pool.blocks, pool.B, pool.H, pool.D), 2.0 ** 127 * 0.9).bfloat16()
+            pool.codes(1).copy_(big.view(torch.uint8))
+            s["values"][1] = np64(big)
+        if equal:
+            s["dq"].zero_()
+        else:
+            s["dq"].copy_(s["q"])
+        run_attend(pool, s)
+        # a mean of equal numbers is that number: probabilities and their sum are off by a half step of 2^-8 (bf16) or 2^-11 each
+        want = s["values"][1].max()
+        out = np64(s["out"])[np.array(s["lens"]) + s["prefix"] > 0]
+        assert (np.abs(out - want) <= (2.0 ** -8 + 2.0 ** -8 + 2.0 ** -10) * want).all(), (equal, out.min(), out.max(), want)
+    status_is(0)
+
+
 # The prefix kernel in the cases that the stream is tested in.
 PLAIN = [("bf16", "bf16"), ("fp16", "fp16"), ("bf16", "e4m3"), ("fp16", "int8")]
 

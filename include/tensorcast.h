@@ -542,7 +542,10 @@ TC_API int tc_kv_gather(const tc_kv_layer_t *layer, const tc_kv_gather_t *args, 
  * A prefix's pages are read once for up to 256 rows (request, head) of a KV head (8 or 16 where the
  * prefix is short or D > 128), a request's own once for its up to 16 heads of a KV head; slots past a
  * length are never read.  Scores, softmax statistics and outputs are fp32; probabilities are rounded to
- * the products' 16-bit type (fp16 for quantised pools).  A call is one to three launches.
+ * the products' 16-bit type (fp16 for quantised pools).  For quantised pools queries are fp16 times a power of two per
+ * row, and the values of a prefix that is read once for many rows are rounded to fp16 times a power of two.
+ * A scale of V may be any number: 0 and negative ones are taken as they are, one that is not finite leaves no finite
+ * output (but its lse) to a row that has its key.  A call is one to three launches.
  * D is a multiple of 16 up to 256, every address and stride a multiple of 16 bytes (tables, lens,
  * prefix_len, lse and the scales: of 4).  An unquantised pool has the queries' type. */
 typedef struct {
@@ -566,7 +569,9 @@ typedef struct {
     int64_t workspace_bytes;     /*   may run at once; its contents before and after mean nothing */
 } tc_attn_decode_t;
 
-/* Bytes of workspace that the call needs: by R, Hq, max_len, max_prefix and the layer's geometry alone. */
+/* Bytes of workspace that the call needs: by R, Hq, max_len, max_prefix and the layer's geometry alone.  It does not
+ * grow with each of them: a prefix is cut into fewer parts where more rows share it, so that fewer requests may need more.
+ * A program whose batch varies asks for every size that it will use and takes the largest. */
 TC_API int tc_attn_workspace(const tc_kv_layer_t *layer, const tc_attn_decode_t *args, int64_t *bytes);
 TC_API int tc_attn_decode(const tc_kv_layer_t *layer, const tc_attn_decode_t *args, void *stream);
 

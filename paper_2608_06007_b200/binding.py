@@ -590,7 +590,8 @@ def tc_kv_gather(layer: KVLayer, tables, offsets, k_out=None, v_out=None, *, fir
 
 
 def tc_attn_workspace_bytes(layer: KVLayer, q, *, max_len, max_prefix=0) -> int:
-    """Bytes of workspace that tc_attn_decode needs for queries of this shape and these bounds."""
+    """Bytes of workspace that tc_attn_decode needs for queries of this shape and these bounds.  Fewer requests may need
+    more: a program whose batch varies takes the largest over its sizes."""
     out = C.c_int64()
     args = tc_attn_decode_t(C.sizeof(tc_attn_decode_t), _dtype(q)[0], q.shape[0], q.shape[1], max_len=max_len, max_prefix=max_prefix)
     _check(load_library().tc_attn_workspace(layer.ref, C.byref(args), C.byref(out)))

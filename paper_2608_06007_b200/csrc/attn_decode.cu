@@ -44,8 +44,8 @@ template <> __device__ __forceinline__ void mma16816<__nv_bfloat16>(float (&c)[4
 // the lengths.  It has its own ring of stages, filled by 16-byte asynchronous copies whatever the size
 // of the pages, and works alone: the copies run ahead across the ends of items, so that short
 // requests cost no gaps.  An item that is one warp's leaves a whole part, one that is cut leaves pieces,
-// at most two a warp.  Bound by HBM for 16-bit pools (297k tokens of 4 heads x 128, 608 MB: a call takes 106 us, 5.7 TB/s,
-// 0.88 of a plain copy), by latency and issue for codes (the same in int8, 313 MB: 70 us, 4.4 TB/s).
+// at most two a warp.  Bound by HBM for 16-bit pools (297k tokens of 4 heads x 128, 608 MB: a call takes 105 us, 5.8 TB/s,
+// 0.88 of a plain copy), by latency and issue for codes (the same in int8, 313 MB: 73 us in a long run, 4.3 TB/s; 69 us 20 in a row).
 //
 // The keys are the rows of the matrix products, S' = K Q' and O' = V' P' on m16n8k16: the columns are
 // the query heads of one KV head (or rows of the batch, for the prefix), 8 or 16 at a time, so few
@@ -59,7 +59,8 @@ template <> __device__ __forceinline__ void mma16816<__nv_bfloat16>(float (&c)[4
 // The key's scale multiplies the scores.  The value's goes into the exponent, w = exp2(s + log2 v_scale
 // - top), so that fp16 probabilities have the largest contribution as their reference whatever the scales
 // are.  The sum has exp2(s - ref) with a running maximum of its own: scales reach from 2^-126 to 2^127, so neither is the
-// other times a number that fp32 holds.  Queries of such a pool are fp16 with a power of two
+// other times a number that fp32 holds.  (These exponentials cost 3 % at D = 256, 12 % with 16 columns there, nothing
+// else that was measured; w over its scale instead, where an item's scales allow it, was slower.)  Queries of such a pool are fp16 with a power of two
 // per row taken out, so that the row's largest is in [2^14, 2^15): what is then below fp16's smallest
 // step is below 2^-38 of that largest.
 
@@ -806,7 +807,9 @@ static int launch_decode(const AttnParams &p, int device, cudaStream_t s)
     // parts of a row: the prefix kernel's, and about as many as warps share one item of the stream
     const int64_t parts = p.split.prefix_parts + p.split.stream_ctas * 4 / std::max<int64_t>(p.R * p.layer.H * p.split.own_blocks, 1);
     const unsigned rows = static_cast<unsigned>(p.split.rows);
-    const bool wide = parts > 32 && rows < 1024;  // few rows of many parts
+    // Few rows of many parts: 16 warps a row.  One context of 65536 int8 tokens 29 us so, 92 with a warp a row; three of 65k to
+    // 131k 69 and 98; 64 requests of some 256 tokens (2048 rows) 59 so and 27 with a warp a row.
+    const bool wide = parts > 32 && rows < 1024;
     const unsigned few = std::min<unsigned>((rows + 3) / 4, kSms * kJoinCtas);
     const bool follows = p.split.prefix_parts || p.split.stream_ctas;
     if (p.layer.D <= 128) return wide ? launch_attn(join_kernel<T, 128, 16>, rows, 512, 0, follows, p, s) : launch_attn(join_kernel<T, 128, 1>, few, 128, 0, follows, p, s);

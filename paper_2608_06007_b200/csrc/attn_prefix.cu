@@ -17,8 +17,8 @@
 //                    staged as they are first and widened to fp16 by the warp that fetched them.
 //   warps 12, 13     issue the matrix products, S = Q K' and O += P V.
 //
-// Bound by the softmax: 128 requests x 64 heads x 128 behind 32768 tokens (1.4e11 flop): a call takes 152 us, 0.92 PFLOP/s,
-// 0.57 of the measured rate; per tile and slot of 1024 clocks of products the softmax takes some 2900 for both
+// Bound by the softmax: 128 requests x 64 heads x 128 behind 32768 tokens (1.4e11 flop): a call takes 168 us in a long run, 0.82 PFLOP/s,
+// 0.51 of the measured rate (148 to 154 us, 0.56, 20 in a row); per tile and slot of 1024 clocks of products the softmax takes some 2900 for both
 // slots, 2048 of them exponentials.  Kernel times that a profiler gave there, for 142 us: scores over probabilities, a buffer per
 // slot 160 us; one buffer, both products from one warp 155; scores issued between the halves of the second product
 // 186; a part of the exponentials as polynomials 154.  Codes: bound by the four warps that widen them

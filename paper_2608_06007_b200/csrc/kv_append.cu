@@ -5,7 +5,7 @@
 // neighbours for the interleaved one and for what is not rotated.  2^k lanes hold a row, so the
 // row's largest magnitude is k shuffles away and every number is read once and written once.  The
 // threads of one token share its table row in registers over all of its heads.  Bound by HBM: 32768 tokens of 64
-// query and 8 KV heads x 128, bf16 to e4m3 (1.29 GB), take 223 us, 5.8 TB/s, 0.88 of a plain copy, 20 passes in a row; 239 us in a long run.  (Slot
+// query and 8 KV heads x 128, bf16 to e4m3 (1.29 GB), take 238 us in a long run, 5.4 TB/s, 0.83 of a plain copy; 222 us, 0.89, 20 passes in a row.  (Slot
 // and position waited for before the rows are loaded, one row type per pass: 651 us.)  Few tokens are bound by
 // latency: 37 tokens of the 8B model's shape 4 us (the kernel, by a profiler; the call 12).
 //
@@ -186,7 +186,9 @@ __device__ __forceinline__ void store_chunk(char *p, const Pairs &x, int half)
 
 // Rows whose D is a multiple of 8 and whose addresses are multiples of 16 bytes; rot_dim a multiple of 16.
 // A token's threads hold one row of K or V each and kQueries of Q, all loaded before slot and position
-// are known; as many threads as K and V have rows (up to 256) leave nothing idle.
+// are known; as many threads as K and V have rows (up to 256) leave nothing idle.  Three CTAs an SM leave 80 registers a
+// thread, and up to 104 bytes of the 16-bit kernels' spill: with two, which spill nothing, 32768 tokens took 242 us for
+// 222 (e4m3; bf16 pool 234 for 215).  fp32 rows take twice the registers: four queries at once 261 us for 251 with two.
 template <typename T, bool INTERLEAVED, bool QUANTISED>
 __global__ void __launch_bounds__(256, sizeof(T) == 4 ? 2 : 3) append_vector_kernel(const __grid_constant__ AppendParams p)
 {

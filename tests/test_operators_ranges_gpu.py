@@ -261,6 +261,24 @@ def test_attention_over_values_next_to_the_largest_number(shape, kind):
     status_is(0)
 
 
+@pytest.mark.parametrize("shape", SHAPES)
+@pytest.mark.parametrize("kind", ["e4m3", "int8"])
+@pytest.mark.parametrize("bad", [float("inf"), float("-inf"), float("nan")])
+def test_attention_over_a_scale_of_v_that_is_not_finite(shape, kind, bad):
+    rng = np.random.default_rng([len(shape), 14])
+    pool, s = shaped(shape, kind, "bf16", rng)
+    R, Hq = s["q"].shape[:2]
+    table = s["shared"] if s["prefix"] else s["table"][0]
+    pool.codes(1)[int(table[2]), 3, 0] = 0x31  # a code that is not 0
+    pool.scale(1)[int(table[2]), 3, 0] = bad
+    run_attend(pool, s)
+    spoilt = torch.zeros(R, Hq, dtype=torch.bool)
+    spoilt[slice(None) if s["prefix"] else 0, : Hq // pool.H] = True
+    finite = s["out"].cpu().isfinite()
+    assert torch.equal(finite.all(-1), ~spoilt) and torch.equal(finite.any(-1), ~spoilt) and torch.isfinite(s["lse"]).all()
+    status_is(0)
+
+
 # The prefix kernel in the cases that the stream is tested in.
 PLAIN = [("bf16", "bf16"), ("fp16", "fp16"), ("bf16", "e4m3"), ("fp16", "int8")]
 

@@ -55,6 +55,7 @@ SHAPES = {
     "prefix 128, 64": (32, 8, 4, 64, 2700, 40),
     "prefix 256": (36, 8, 7, 128, 1300, 40),
     "prefix 256, 80": (36, 8, 7, 80, 1300, 40),
+    "prefix 256, three blocks": (150, 3, 4, 128, 1300, 20),
 }
 STREAMS = [name for name in SHAPES if not name.startswith("prefix")]
 PREFIXES = [name for name in SHAPES if name.startswith("prefix")]
@@ -361,10 +362,41 @@ def test_a_prefix_with_rows_that_are_not_finite(shape, x, kind, apart):
     want[:, g : 2 * g] = True
     assert torch.equal(out.isnan().any(-1), nan) and torch.equal(lse.isnan(), want)
     # a query: its row
-    s["dq"][1, 3 * g] = float("nan")
+    s["dq"][1, 2 * g] = float("nan")
     run_attend(pool, s)
-    nan[1, 3 * g] = want[1, 3 * g] = True
+    nan[1, 2 * g] = want[1, 2 * g] = True
     assert torch.equal(s["out"].cpu().isnan().any(-1), nan) and torch.equal(s["lse"].cpu().isnan(), want)
+    status_is(0)
+
+
+@pytest.mark.parametrize("shape", SHAPES)
+@pytest.mark.parametrize("x,kind", PLAIN)
+def test_attention_into_strided_outputs_from_strided_tables(shape, x, kind):
+    """Outputs with heads outside requests and a gap behind every row, tables that are a window of wider ones, no logarithms."""
+    rng = np.random.default_rng([len(shape), 17])
+    pool, s = shaped(shape, kind, x, rng)
+    s["lens"][-2] = -1
+    s["d"]["lens"][-2] = -1
+    run_attend(pool, s)
+    R, Hq, D = s["q"].shape
+    whole = torch.full((Hq, R, D + 24), 9.0, dtype=s["q"].dtype, device="cuda")
+    wide = torch.full((R, s["table"].shape[1] + 5), -1, dtype=torch.int32, device="cuda")
+    wide[:, 3:-2] = s["d"]["tables"]
+    want, s["out"] = s["out"], whole.transpose(0, 1)[..., :D]
+    run_attend(pool, s, lse=None, tables=wide[:, 3:-2])
+    assert torch.equal(s["out"], want) and (whole[..., D:] == 9.0).all()
+    check(pool, s, x, shape.startswith("prefix"), {0, R - 2, R - 1})
+    status_is(0)
+
+
+@pytest.mark.parametrize("x,kind,prefix", [("bf16", "bf16", 40000), ("fp16", "int8", 80000)])
+def test_a_long_prefix_of_one_request_with_many_heads(x, kind, prefix):
+    assert prefix_taken_by(1, 20, 1, 128, 30, prefix, kind in TOP) == "prefix 128"
+    rng = np.random.default_rng(prefix)
+    pool = Pool(kind, H=1, blocks=prefix // 16 + 4)
+    s = attend_case(pool, [30], prefix, 20, x, rng, poison=False)
+    run_attend(pool, s)
+    check(pool, s, x, True, {0})
     status_is(0)
 
 

@@ -619,7 +619,7 @@ __global__ void __launch_bounds__(128, DP > 128 ? 1 : NB > 1 ? 2 : DP == 64 ? 4 
 // warp takes a row, four loads in flight leave registers for eight CTAs an SM.  Against five CTAs with eight loads, a
 // call of 512 requests of 32 heads, e4m3, D = 128, took 149 us for 157 behind a prefix of 4000 and 76 for 81 without.
 constexpr int kJoinCtas = 8;
-constexpr float kLess = 16.f;  // weights are 2^-16 at most: the outputs of up to that many parts may be next to the largest number
+constexpr float kLess = 12.f;  // weights are 2^-12 at most: the outputs of up to that many parts may be next to the largest number
 template <typename T, int DP, int WARPS>
 __global__ void __launch_bounds__(WARPS == 1 ? 128 : 32 * WARPS, WARPS == 1 ? kJoinCtas : 1) join_kernel(const __grid_constant__ AttnParams p)
 {

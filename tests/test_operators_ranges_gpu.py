@@ -2,9 +2,11 @@
 
 A case says which kernel takes its prefix - none, the stream, or the prefix kernel with 128 or 256 rows a CTA - and
 fails where the library's rule gives it to another."""
+import ctypes
 import os
 import subprocess
 import sys
+import time
 
 import numpy as np
 import pytest
@@ -13,6 +15,7 @@ import torch
 import paper_2608_06007_b200 as tc
 from operators_split import prefix_taken_by
 from oracle import operators as orc
+from paper_2608_06007_b200 import build
 from test_operators_gpu import Pool, append_case, attend_case, check_append, check_attend, dev, np64, run_append, run_attend, status_is, tokens_of
 
 pytestmark = pytest.mark.gpu
@@ -459,3 +462,38 @@ def test_threads_may_make_the_first_calls_of_a_process_at_once():
     here = os.path.dirname(os.path.abspath(__file__))
     got = subprocess.run([sys.executable, "-c", FIRST_CALLS.format(root=os.path.dirname(here), tests=here)], capture_output=True, text=True, timeout=300)
     assert got.returncode == 0 and "answered" in got.stdout, got.stderr[-2000:]
+
+
+WAITS = """
+#include "barrier.cuh"
+__global__ void waits(int *got)
+{
+    __shared__ __align__(8) unsigned long long bars[2];
+    const uint32_t bar = static_cast<uint32_t>(__cvta_generic_to_shared(bars));
+    tc::barrier_init(bar, 1), tc::barrier_init(bar + 8, 1);
+    tc::barrier_arrive(bar + 8);
+    got[0] = tc::barrier_wait(bar + 8, 0);
+    got[1] = tc::barrier_wait(bar + 8, 1);
+    got[2] = tc::barrier_wait(bar, 0);
+    tc::barrier_arrive(bar);
+    got[3] = tc::barrier_wait(bar, 0);
+}
+extern "C" __attribute__((visibility("default"))) int run(int *got)
+{
+    waits<<<1, 1>>>(got);
+    return static_cast<int>(cudaDeviceSynchronize());
+}
+"""
+
+
+def test_waits_of_the_prefix_kernel_end_by_themselves(tmp_path):
+    """On a phase that has passed, one that nothing ends (a second or two, then false), and one that ends after that."""
+    src, lib = tmp_path / "waits.cu", tmp_path / "waits.so"
+    src.write_text(WAITS)
+    subprocess.check_call([os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc"), *build.NVCC_FLAGS, "-I", build.CSRC, "-shared", "-cudart", "static", "-o", str(lib), str(src)])
+    got = torch.full((4,), 7, dtype=torch.int32, device="cuda")
+    torch.cuda.synchronize()
+    begin = time.monotonic()
+    assert ctypes.CDLL(str(lib)).run(ctypes.c_void_p(got.data_ptr())) == 0
+    assert 0.2 < time.monotonic() - begin < 20
+    assert got.tolist() == [1, 0, 0, 1]

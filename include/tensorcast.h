@@ -575,6 +575,45 @@ typedef struct {
 TC_API int tc_attn_workspace(const tc_kv_layer_t *layer, const tc_attn_decode_t *args, int64_t *bytes);
 TC_API int tc_attn_decode(const tc_kv_layer_t *layer, const tc_attn_decode_t *args, void *stream);
 
+/* Chunks of new tokens - pieces of prompts, whole prompts, tokens guessed ahead, single ones, any of them side by side - over a
+ * paged cache that holds the new tokens already (tc_kv_append).  Rows offsets[r] .. offsets[r+1] of q and out are request
+ * r's new tokens, the last n = offsets[r+1] - offsets[r] of the lens[r] that its table holds: row i of them is at position
+ * p = lens[r] - n + i.  For every such row and query head h, with KV head h / (Hq / H), over the keys j that the row sees,
+ *   j <= p, and with window > 0 also  j > p - window or j < sinks :
+ *   s_j = scale * (q . k_j),  out = sum_j exp(s_j) v_j / sum_j exp(s_j),  lse = log sum_j exp(s_j)
+ * What a row does not see has no part in it, be it infinite or NaN.  A row whose every s_j is -infinity gets out 0 and lse -infinity.
+ * lens[r] < 0: the request is padding.  A request with n = 0 is passed over.  Their rows, and rows in front of offsets[0] and
+ * behind offsets[R], are left as they were; so are those of a request with n > max_new, lens[r] > max_len, lens[r] < n or
+ * offsets that decrease or leave [0, n_tokens], which sets TC_DEVICE_BAD_INDEX.
+ * Slots of the cache that no row of a request sees are never read.  Scores, softmax statistics and outputs are fp32; probabilities, quantised pools
+ * and their scales are dealt with as by tc_attn_decode.  Which parts a request's keys are cut into depends on the lengths of
+ * the whole batch, and with it the order of sums; the same call on the same batch gives the same bits.
+ * A call is one or two launches.  D is a multiple of 16 up to 256, every address and stride a multiple of 16 bytes (tables,
+ * lens, lse and the scales: of 4, offsets: of 8).  An unquantised pool has the queries' type. */
+typedef struct {
+    uint32_t struct_size; /* sizeof(tc_attn_chunk_t) */
+    int32_t dtype;        /* TC_BF16 or TC_FP16: of q and out */
+    int64_t R, n_tokens, Hq; /* requests, rows of q and out, query heads (a multiple of H) */
+    const void *q;        /* [n_tokens][Hq][D] */
+    void *out;            /* [n_tokens][Hq][D]; not q */
+    int64_t q_stride[2], out_stride[2]; /* token, head */
+    float *lse;           /* [n_tokens][Hq], tight, natural logarithm; or NULL */
+    float scale;          /* of the scores, magnitude at most 1e30; 0 = 1 / sqrt(D) */
+    int32_t reserved;     /* 0 */
+    int64_t window, sinks; /* 0, 0: a row sees every key up to its own */
+    const int32_t *tables; /* [R][table_width] block ids of each request's tokens */
+    int64_t table_width, table_stride; /* entries per request, bytes from request to request */
+    const int64_t *offsets; /* [R + 1], not decreasing */
+    const int32_t *lens;    /* [R] tokens of each request, the new ones among them */
+    int64_t max_new, max_len; /* no n and no lens[r] is larger; max_new <= max_len <= 2^24 */
+    void *workspace;          /* 16-byte aligned, >= tc_attn_chunk_workspace bytes, not shared by calls that */
+    int64_t workspace_bytes;  /*   may run at once; its contents before and after mean nothing */
+} tc_attn_chunk_t;
+
+/* Bytes of workspace that the call needs: by R, n_tokens, Hq, max_new, max_len, window, sinks and the layer's geometry alone. */
+TC_API int tc_attn_chunk_workspace(const tc_kv_layer_t *layer, const tc_attn_chunk_t *args, int64_t *bytes);
+TC_API int tc_attn_chunk(const tc_kv_layer_t *layer, const tc_attn_chunk_t *args, void *stream);
+
 /* ---- off the data path: inspection and diagnostics -------------------------------------- */
 
 typedef struct {

@@ -137,11 +137,18 @@ class tc_attn_decode_t(C.Structure):
                 ("workspace", C.c_void_p), ("workspace_bytes", C.c_int64)]
 
 
+class tc_attn_chunk_t(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("dtype", C.c_int32), ("R", C.c_int64), ("n_tokens", C.c_int64), ("Hq", C.c_int64), ("q", C.c_void_p), ("out", C.c_void_p),
+                ("q_stride", _Stride), ("out_stride", _Stride), ("lse", C.c_void_p), ("scale", C.c_float), ("reserved", C.c_int32), ("window", C.c_int64), ("sinks", C.c_int64),
+                ("tables", C.c_void_p), ("table_width", C.c_int64), ("table_stride", C.c_int64), ("offsets", C.c_void_p), ("lens", C.c_void_p),
+                ("max_new", C.c_int64), ("max_len", C.c_int64), ("workspace", C.c_void_p), ("workspace_bytes", C.c_int64)]
+
+
 EXPORTS = ("tc_plan_create", "tc_kv_pack", "tc_kv_unpack", "tc_weights_materialize",
            "tc_plan_destroy", "tc_plan_stats", "tc_plan_descriptors", "tc_strerror", "tc_last_error",
            "tc_kv_pack_noalloc", "tc_weights_materialize_checksum", "tc_trim",
            "tc_weights_materialize_file", "tc_plan_segments", "tc_device_status", "tc_selftest_wait_timeout", "tc_plan_check_device",
-           "tc_kv_append", "tc_kv_gather", "tc_attn_decode", "tc_attn_workspace")
+           "tc_kv_append", "tc_kv_gather", "tc_attn_decode", "tc_attn_workspace", "tc_attn_chunk", "tc_attn_chunk_workspace")
 
 _lib = None
 
@@ -177,11 +184,13 @@ def load_library(path: str | None = None):
     lib.tc_plan_check_device.restype = C.c_int
     lib.tc_selftest_wait_timeout.argtypes = [vp]
     lib.tc_selftest_wait_timeout.restype = C.c_int
-    for name in ("tc_kv_append", "tc_kv_gather", "tc_attn_decode"):
+    for name in ("tc_kv_append", "tc_kv_gather", "tc_attn_decode", "tc_attn_chunk"):
         getattr(lib, name).argtypes = [C.POINTER(tc_kv_layer_t), vp, vp]  # the second: a packed struct as bytes, or byref(args)
         getattr(lib, name).restype = C.c_int
     lib.tc_attn_workspace.argtypes = [C.POINTER(tc_kv_layer_t), C.POINTER(tc_attn_decode_t), C.POINTER(C.c_int64)]
     lib.tc_attn_workspace.restype = C.c_int
+    lib.tc_attn_chunk_workspace.argtypes = [C.POINTER(tc_kv_layer_t), C.POINTER(tc_attn_chunk_t), C.POINTER(C.c_int64)]
+    lib.tc_attn_chunk_workspace.restype = C.c_int
     lib.tc_trim.argtypes = []
     lib.tc_trim.restype = C.c_int
     lib.tc_strerror.argtypes = [C.c_int]
@@ -484,7 +493,8 @@ _dtypes = {}
 _APPEND = struct.Struct("=IIqqii4Q8q4Q2q")
 _GATHER = struct.Struct("=IiqqQqqQQQQ4q")
 _DECODE = struct.Struct("=IiqqQQ4qQfiQqqQqQQqQq")
-assert (_APPEND.size, _GATHER.size, _DECODE.size) == (C.sizeof(tc_kv_append_t), C.sizeof(tc_kv_gather_t), C.sizeof(tc_attn_decode_t))
+_CHUNK = struct.Struct("=IiqqqQQ4qQfiqqQqqQQqqQq")
+assert (_APPEND.size, _GATHER.size, _DECODE.size, _CHUNK.size) == (C.sizeof(tc_kv_append_t), C.sizeof(tc_kv_gather_t), C.sizeof(tc_attn_decode_t), C.sizeof(tc_attn_chunk_t))
 
 
 def _dtype(t):
@@ -619,5 +629,38 @@ def tc_attn_decode(layer: KVLayer, q, out, tables, lens, *, max_len, workspace, 
     args = _DECODE.pack(_DECODE.size, code, R, Hq, q.data_ptr(), out.data_ptr(), q0, q1, o0, o1, lse_at, scale, 0, table, width, step, _vector("lens", lens, R, 4), max_len,
                         prefix_at, prefix_len_at, max_prefix, workspace.data_ptr(), workspace.numel() * workspace.element_size())
     rc = (_lib or load_library()).tc_attn_decode(layer.ref, args, None if stream is None else _stream(stream))
+    if rc:
+        _check(rc)
+
+
+def _lse(lse, n, heads):
+    """Address of the fp32 [n, heads] that logarithms go to; 0 for None."""
+    if lse is None:
+        return 0
+    if lse.shape != (n, heads) or _dtypes.get(lse.dtype) != (TC_FP32, 4) or not lse.is_contiguous():
+        raise ValueError(f"lse must be a contiguous fp32 [{n}, {heads}]")
+    return lse.data_ptr()
+
+
+def tc_attn_chunk_workspace_bytes(layer: KVLayer, q, R, *, max_new, max_len, window=0, sinks=0) -> int:
+    """Bytes of workspace that tc_attn_chunk needs for R requests with queries of this shape and these bounds."""
+    out = C.c_int64()
+    args = tc_attn_chunk_t(C.sizeof(tc_attn_chunk_t), _dtype(q)[0], R, q.shape[0], q.shape[1], max_new=max_new, max_len=max_len, window=window, sinks=sinks)
+    _check(load_library().tc_attn_chunk_workspace(layer.ref, C.byref(args), C.byref(out)))
+    return out.value
+
+
+def tc_attn_chunk(layer: KVLayer, q, out, tables, offsets, lens, *, max_new, max_len, workspace, window=0, sinks=0, scale=0.0, lse=None, stream=None) -> None:
+    """Rows offsets[r] .. offsets[r + 1] (int64, [R + 1]) of q and out ([n_tokens, Hq, D]) are the last of the lens[r] tokens (int32; negative =
+    padding) of tables[r]: each attends to the tokens up to its own, with a window to its last `window` and the request's first `sinks`."""
+    code, e = _dtype(q)
+    dtype, D, R = q.dtype, layer.D, offsets.shape[0] - 1
+    n, Hq = q.shape[0], q.shape[1]
+    q0, q1 = _rows("q", q, n, Hq, D, dtype, e)
+    o0, o1 = _rows("out", out, n, Hq, D, dtype, e)
+    table, width, step = _matrix("tables", tables, R)
+    args = _CHUNK.pack(_CHUNK.size, code, R, n, Hq, q.data_ptr(), out.data_ptr(), q0, q1, o0, o1, _lse(lse, n, Hq), scale, 0, window, sinks, table, width, step,
+                       _vector("offsets", offsets, R + 1, 8), _vector("lens", lens, R, 4), max_new, max_len, workspace.data_ptr(), workspace.numel() * workspace.element_size())
+    rc = (_lib or load_library()).tc_attn_chunk(layer.ref, args, None if stream is None else _stream(stream))
     if rc:
         _check(rc)

@@ -1,0 +1,194 @@
+// tc_attn_chunk: the entry points, unquantised pools, and the kernel that joins the parts of requests whose keys are cut.
+#include <cmath>
+
+#include "attn_chunk.cuh"
+
+namespace tc {
+
+int launch_chunk_plain(const ChunkParams &p, int dtype, int device, cudaStream_t s)
+{
+    return dtype == TC_BF16 ? launch_chunk_type<__nv_bfloat16, kPlain>(p, device, s) : launch_chunk_type<__half, kPlain>(p, device, s);
+}
+
+// The parts' outputs, each by its share of the whole sum.  A warp takes a row; a lane finds the weights of up to four parts,
+// then the warp reads the outputs of four parts at once.  Where nothing was cut it ends after a look at `base`.
+constexpr float kLess = 12.f;  // weights are 2^-12 at most: the outputs of up to that many parts may be next to the largest number
+static_assert(kChunkMostParts <= 128);
+template <typename T, int DP>
+__global__ void __launch_bounds__(128) chunk_join_kernel(const __grid_constant__ ChunkParams p)
+{
+    constexpr int kVectors = DP / 128;
+    const int lane = threadIdx.x & 31, D = p.layer.D;
+    const int64_t first_warp = blockIdx.x * 4ll + (threadIdx.x >> 5), warps = gridDim.x * 4ll;
+    await_last();
+    const int32_t share = static_cast<int32_t>(p.base[0]);
+    if (share >= (1 << 30)) return;
+    for (int64_t r0 = 0; r0 < p.R; r0 += 32) {
+        const uint32_t mine = r0 + lane < p.R ? p.base[4 + r0 + lane] : kUncut;
+        for (uint32_t some = __ballot_sync(0xffffffffu, mine != kUncut); some; some &= some - 1) {
+            const int who = __ffs(some) - 1;
+            const uint32_t base = __shfl_sync(0xffffffffu, mine, who);
+            const ChunkRequest q = chunk_request(p, r0 + who, false);
+            const int32_t parts = chunk_parts(chunk_tiles(p.shape, q.len), share);
+            const int64_t rows = static_cast<int64_t>(q.n) * p.Hq;
+            for (int64_t row = first_warp; row < rows; row += warps) {
+                const int64_t token = row / p.Hq, head = row - token * p.Hq;
+                float sum[4], top = -INFINITY, all = 0.f, acc[4 * kVectors] = {};
+#pragma unroll
+                for (int k = 0; k < 4; k++) {
+                    sum[k] = lane + 32 * k < parts ? p.sums[base + (lane + 32 * k) * rows + row] : -INFINITY;
+                    top = fmaxf(top, sum[k]);
+                }
+#pragma unroll
+                for (int x = 16; x; x >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
+#pragma unroll
+                for (int k = 0; k < 4; k++) {
+                    sum[k] = sum[k] == -INFINITY ? 0.f : exp2_approx(sum[k] - (top == -INFINITY ? 0.f : top) - kLess);  // NaN where the sum is
+                    all += sum[k];
+                }
+#pragma unroll
+                for (int x = 16; x; x >>= 1) all += __shfl_xor_sync(0xffffffffu, all, x);
+#pragma unroll
+                for (int k = 0; k < 4; k++) {
+                    for (int j0 = 32 * k; j0 < min(parts, 32 * k + 32); j0 += 4) {
+                        float4 v[4][kVectors];
+#pragma unroll
+                        for (int j = 0; j < 4; j++)
+#pragma unroll
+                            for (int x = 0; x < kVectors; x++) {
+                                v[j][x] = make_float4(0.f, 0.f, 0.f, 0.f);
+                                if (j0 + j < parts && lane * 4 + 128 * x < D) v[j][x] = *reinterpret_cast<const float4 *>(p.parts + (base + (j0 + j) * rows + row) * D + lane * 4 + 128 * x);
+                            }
+#pragma unroll
+                        for (int j = 0; j < 4; j++) {
+                            const float w = __shfl_sync(0xffffffffu, sum[k], (j0 + j) & 31);
+                            if (w == 0.f || j0 + j >= parts) continue;  // what a part without keys left in its place is read but not used
+#pragma unroll
+                            for (int x = 0; x < kVectors; x++) acc[4 * x] += w * v[j][x].x, acc[4 * x + 1] += w * v[j][x].y, acc[4 * x + 2] += w * v[j][x].z, acc[4 * x + 3] += w * v[j][x].w;
+                        }
+                    }
+                }
+                const float inv = all == 0.f ? 0.f : 1.f / all;
+                char *const dst = p.out + (q.token0 + token) * p.out_token + head * p.out_head;
+#pragma unroll
+                for (int x = 0; x < kVectors; x++)
+                    if (lane * 4 + 128 * x < D)
+                        *reinterpret_cast<uint2 *>(dst + (lane * 4 + 128 * x) * 2) = make_uint2(pack2<T>(acc[4 * x] * inv, acc[4 * x + 1] * inv), pack2<T>(acc[4 * x + 2] * inv, acc[4 * x + 3] * inv));
+                if (p.lse && lane == 0) p.lse[q.token0 * p.Hq + row] = all == 0.f ? -INFINITY : ((top == -INFINITY ? 0.f : top) + kLess + log2f(all)) * kChunkLn2;
+            }
+        }
+    }
+}
+
+template <typename T>
+static int launch_chunk(const ChunkParams &p, int dtype, int device, cudaStream_t s)
+{
+    const int rc = p.layer.quantised() ? launch_chunk_codes(p, device, s) : launch_chunk_plain(p, dtype, device, s);
+    if (rc != TC_OK || !p.plan.part_rows) return rc;
+    const unsigned grid = static_cast<unsigned>(std::min<int64_t>((p.n_tokens * p.Hq + 3) / 4, kChunkSms * 8));
+    return p.layer.D <= 128 ? launch_attn(chunk_join_kernel<T, 128>, grid, 128, 0, true, p, s) : launch_attn(chunk_join_kernel<T, 256>, grid, 128, 0, true, p, s);
+}
+
+// What both entry points check; fills p's geometry and plan.
+static int check_chunk(const tc_kv_layer_t *layer, const tc_attn_chunk_t *a, ChunkParams *p)
+{
+    int rc = check_layer(layer, &p->layer);
+    if (rc != TC_OK) return rc;
+    if (!a) return fail(TC_ERR_INVALID_ARG, "args is required");
+    if (a->struct_size != sizeof *a) return fail(TC_ERR_INVALID_ARG, "args.struct_size %u != %zu: header and library disagree", a->struct_size, sizeof *a);
+    if (a->dtype != TC_BF16 && a->dtype != TC_FP16) return fail(TC_ERR_INVALID_ARG, "dtype %d: q and out are TC_BF16 or TC_FP16", a->dtype);
+    if (!p->layer.quantised() && p->layer.dtype != a->dtype) return fail(TC_ERR_INVALID_ARG, "an unquantised pool must have the queries' dtype (pool %d, queries %d)", p->layer.dtype, a->dtype);
+    const int D = p->layer.D;
+    if (D % 16 || D > 256) return fail(TC_ERR_SHAPE, "D = %d: tc_attn_chunk takes multiples of 16 up to 256", D);
+    if (p->layer.align < 16) return fail(TC_ERR_INVALID_ARG, "tc_attn_chunk needs planes and strides that are multiples of 16 bytes");
+    if (a->R < 0 || a->R > (1 << 24)) return fail(TC_ERR_SHAPE, "R %lld is not in [0, 2^24]", (long long)a->R);
+    if (a->Hq < 1 || a->Hq > (1 << 16) || a->Hq % p->layer.H) return fail(TC_ERR_SHAPE, "Hq %lld is not a multiple of H = %d in [1, 2^16]", (long long)a->Hq, p->layer.H);
+    if (a->n_tokens < 0 || a->n_tokens > (1 << 30)) return fail(TC_ERR_SHAPE, "n_tokens %lld is not in [0, 2^30]", (long long)a->n_tokens);
+    if (a->max_len < 0 || a->max_len > (1 << 24)) return fail(TC_ERR_SHAPE, "max_len %lld is not in [0, 2^24]", (long long)a->max_len);
+    if (a->max_new < 0 || a->max_new > a->max_len) return fail(TC_ERR_SHAPE, "max_new %lld is not in [0, max_len = %lld]", (long long)a->max_new, (long long)a->max_len);
+    if (a->window < 0 || a->sinks < 0) return fail(TC_ERR_SHAPE, "window %lld and sinks %lld must not be negative", (long long)a->window, (long long)a->sinks);
+    if (a->sinks && !a->window) return fail(TC_ERR_INVALID_ARG, "sinks without a window: every key is seen");
+    if (a->reserved) return fail(TC_ERR_INVALID_ARG, "reserved is %d, not 0", a->reserved);
+    if (!(std::fabs(a->scale) <= 1e30f)) return fail(TC_ERR_INVALID_ARG, "scale is not a number of at most 1e30");
+    ChunkShape &s = p->shape;
+    s.group = static_cast<int32_t>(a->Hq / p->layer.H);
+    s.rows = chunk_rows(D), s.keys = chunk_keys(D);
+    s.window = static_cast<int32_t>(a->window ? std::min<int64_t>(a->window, 1 << 30) : 1 << 30);
+    s.sinks = static_cast<int32_t>(std::min<int64_t>(a->sinks, 1 << 30));
+    s.heads = p->layer.H;
+    const int64_t new_most = std::min(a->max_new, a->n_tokens);
+    if (new_most * s.group > INT32_MAX - 4096 || a->R * chunk_blocks(s, static_cast<int32_t>(new_most)) > INT32_MAX / s.heads)
+        return fail(TC_ERR_TOO_LARGE, "R = %lld requests of up to %lld tokens x %lld heads: too many for one call", (long long)a->R, (long long)new_most, (long long)a->Hq);
+    plan_chunk(s, a->R, a->n_tokens, a->max_new, a->max_len, D, &p->plan);
+    return TC_OK;
+}
+
+}  // namespace tc
+
+using namespace tc;
+
+extern "C" int tc_attn_chunk_workspace(const tc_kv_layer_t *layer, const tc_attn_chunk_t *a, int64_t *bytes)
+{
+    clear_error();
+    if (!bytes) return fail(TC_ERR_INVALID_ARG, "bytes is NULL");
+    *bytes = 0;
+    ChunkParams p{};
+    const int rc = check_chunk(layer, a, &p);
+    if (rc == TC_OK) *bytes = p.plan.workspace;
+    return rc;
+}
+
+extern "C" int tc_attn_chunk(const tc_kv_layer_t *layer, const tc_attn_chunk_t *a, void *stream)
+{
+    clear_error();
+    ChunkParams p{};
+    int rc = check_chunk(layer, a, &p);
+    if (rc != TC_OK) return rc;
+    if (a->R == 0 || a->n_tokens == 0 || a->max_new == 0) return TC_OK;
+    uint32_t align = 16;
+    const int64_t row = p.layer.D * 2ll;
+    if ((rc = check_rows("q", a->q, a->q_stride, a->n_tokens, a->Hq, row, 2, false, &align)) != TC_OK) return rc;
+    if ((rc = check_rows("out", a->out, a->out_stride, a->n_tokens, a->Hq, row, 2, true, &align)) != TC_OK) return rc;
+    if (align < 16) return fail(TC_ERR_INVALID_ARG, "q, out and their strides must be multiples of 16 bytes");
+    if (a->q == a->out) return fail(TC_ERR_OVERLAP, "out is q: the queries are read after the first outputs are written");
+    if (reinterpret_cast<uintptr_t>(a->lse) % 4) return fail(TC_ERR_INVALID_ARG, "lse must be 4-byte aligned");
+    if (!a->lens || reinterpret_cast<uintptr_t>(a->lens) % 4) return fail(TC_ERR_INVALID_ARG, "lens is required, 4-byte aligned");
+    if (!a->offsets || reinterpret_cast<uintptr_t>(a->offsets) % 8) return fail(TC_ERR_INVALID_ARG, "offsets is required, 8-byte aligned");
+    if (!a->tables || reinterpret_cast<uintptr_t>(a->tables) % 4 || a->table_stride % 4 || a->table_stride < 0)
+        return fail(TC_ERR_INVALID_ARG, "tables is required; address and table_stride are multiples of 4 bytes");
+    if (a->table_width < (a->max_len + p.layer.B - 1) / p.layer.B)
+        return fail(TC_ERR_BOUNDS, "table_width %lld holds %lld tokens, max_len is %lld", (long long)a->table_width, (long long)(a->table_width * p.layer.B), (long long)a->max_len);
+    if (p.plan.workspace && (!a->workspace || reinterpret_cast<uintptr_t>(a->workspace) % 16)) return fail(TC_ERR_INVALID_ARG, "workspace is required, 16-byte aligned");
+    if (a->workspace_bytes < p.plan.workspace)
+        return fail(TC_ERR_BOUNDS, "workspace_bytes %lld < %lld (tc_attn_chunk_workspace)", (long long)a->workspace_bytes, (long long)p.plan.workspace);
+    if (p.plan.grid > INT32_MAX) return fail(TC_ERR_TOO_LARGE, "%lld items: too many for one call", (long long)p.plan.grid);
+    int device, sms;
+    if ((rc = op_device(&device, &p.status, &sms)) != TC_OK) return rc;
+    const struct {
+        const char *name;
+        const void *p;
+    } pointers[] = {{"layer.k", layer->k}, {"layer.v", layer->v}, {"layer.k_scale", layer->k_scale}, {"layer.v_scale", layer->v_scale}, {"q", a->q}, {"out", a->out},
+                    {"lse", a->lse}, {"lens", a->lens}, {"offsets", a->offsets}, {"tables", a->tables}, {"workspace", p.plan.workspace ? a->workspace : nullptr}};
+    for (const auto &ptr : pointers)
+        if (ptr.p && (rc = check_memory(ptr.name, ptr.p, device)) != TC_OK) return rc;
+    p.q = static_cast<const char *>(a->q);
+    p.q_token = a->q_stride[0], p.q_head = a->q_stride[1];
+    p.out = static_cast<char *>(a->out);
+    p.out_token = a->out_stride[0], p.out_head = a->out_stride[1];
+    p.lse = a->lse;
+    p.tables = reinterpret_cast<const char *>(a->tables);
+    p.table_stride = a->table_stride;
+    p.offsets = a->offsets, p.lens = a->lens;
+    p.R = a->R, p.n_tokens = a->n_tokens, p.max_new = a->max_new, p.max_len = a->max_len;
+    p.Hq = static_cast<int32_t>(a->Hq);
+    p.q_bf16 = a->dtype == TC_BF16;
+    p.scale_log2 = static_cast<float>((a->scale != 0.f ? static_cast<double>(a->scale) : 1.0 / std::sqrt(static_cast<double>(p.layer.D))) * 1.4426950408889634);
+    p.div_block = make_fastdiv(p.layer.B);
+    p.div_group = make_fastdiv(static_cast<uint32_t>(p.shape.group));
+    char *const ws = static_cast<char *>(a->workspace);
+    p.base = reinterpret_cast<uint32_t *>(ws + p.plan.base_at);
+    p.sums = reinterpret_cast<float *>(ws + p.plan.sums_at);
+    p.parts = reinterpret_cast<float *>(ws + p.plan.parts_at);
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    return a->dtype == TC_BF16 ? launch_chunk<__nv_bfloat16>(p, a->dtype, device, s) : launch_chunk<__half>(p, a->dtype, device, s);
+}

@@ -1,0 +1,1015 @@
+// tc_attn_chunk: attention of chunks of new tokens over a paged cache, on the fifth-generation tensor cores.
+#pragma once
+
+#include <algorithm>
+#include <atomic>
+
+#include "attn_chunk.h"
+#include "attn_tensor.cuh"
+
+namespace tc {
+
+constexpr int kChunkThreads = 512;  // 128 registers each; the softmax's 256 take 192, the others keep 64
+constexpr int kChunkInfos = 4;      // tiles whose masks and scales are kept
+constexpr float kChunkLn2 = 0.6931471805599453f;
+
+template <int KIND, int DP>
+struct ChunkMemory {
+    static constexpr int slots = DP > 128 ? 1 : 2, keys = DP > 128 ? 64 : 128;
+    static constexpr int tile = keys * DP * 2, q_tile = 128 * DP * 2;  // bytes
+    static constexpr int queries = slots * q_tile;
+    static constexpr int codes = KIND == kPlain ? 0 : keys * DP, staged = KIND == kPlain ? 0 : 3;
+    static constexpr int stages = KIND == kPlain ? (DP == 64 ? 6 : 4) : (DP == 64 ? 4 : 3);
+    // {mask, 4 words; whether V has numbers that are not finite, a word a warp}; codes: V's exponent, whether scales are far apart; each
+    // warp's largest and smallest; scales of K; keys' exponents
+    static constexpr int info = KIND == kPlain ? 32 : 80 + 8 * keys, scales = 80;
+    // powers of two taken out of the queries, of four items where scores run two ahead (one slot), of two elsewhere
+    static constexpr int down_sets = 4 / slots, downs = KIND == kPlain ? 0 : 4 * 128 * 4;
+    static constexpr int table = 2 * kChunkThreads * 4;                      // items, and rows of parts, before each thread's requests
+    static constexpr int item = 80;
+    static constexpr int rest = kChunkInfos * info + downs + table + 2 * item + 16 + 512;
+    // more than half of an SM's, so that no two CTAs meet on one: the second would wait for tensor memory with an item in hand
+    static constexpr int least = 120 * 1024;
+    static constexpr int used = queries + stages * tile + staged * codes + rest + 1024;
+    static constexpr int bytes = used > least ? used : least;
+};
+
+// One item as it lies in shared memory.
+struct alignas(16) ChunkItem {
+    int32_t valid, r, h, row0;
+    int32_t rows, pos0, begin, end;  // the part: tiles [begin, end) of the list
+    ChunkList list;                  // 7 words
+    uint32_t part_row;               // of the request's row 0 of this part; kUncut: outputs are written
+    int64_t token0;                  // row of q that is the request's first new token
+    int32_t n, pad;
+};
+static_assert(sizeof(ChunkItem) == 80);
+
+struct ChunkRequest {
+    int64_t token0;
+    int32_t n, len;  // n = 0: nothing is done for it
+};
+__device__ __forceinline__ ChunkRequest chunk_request(const ChunkParams &p, int64_t r, bool tell)
+{
+    ChunkRequest q;
+    const int64_t to = p.offsets[r + 1];
+    q.token0 = p.offsets[r], q.len = p.lens[r];
+    const int64_t n = to - q.token0;
+    const bool bad = q.token0 < 0 || to < q.token0 || to > p.n_tokens || n > p.max_new || (q.len >= 0 && (q.len > p.max_len || q.len < n));
+    if (tell && bad) atomicOr(p.status, kStatusBadIndex);
+    q.n = bad || q.len < 0 ? 0 : static_cast<int32_t>(n);
+    return q;
+}
+
+// Any of two 16-bit numbers infinite or NaN.
+template <typename T> __device__ __forceinline__ uint32_t not_finite(uint32_t w)
+{
+    constexpr uint32_t exponent = std::is_same<T, __half>::value ? 0x7c007c00u : 0x7f807f80u, last = std::is_same<T, __half>::value ? 0x04000400u : 0x00800080u;
+    return ((w & exponent) + last) & 0x80008000u;
+}
+
+// Bits 0 .. n - 1.
+__device__ __forceinline__ uint32_t low_bits(int n) { return n <= 0 ? 0u : n >= 32 ? 0xffffffffu : (1u << n) - 1u; }
+
+// Rare: V has numbers that are not finite in a tile that not every row sees all of.  The second product would give 0 times such
+// a number to rows that do not see its key, so here each row adds up what it sees.
+template <typename T, int DP, int KEYS>
+__device__ __noinline__ void spoiled_tile(uint32_t p_at, uint32_t o_at, uint32_t v, uint4 mask, bool first)
+{
+#pragma unroll 1
+    for (int c = 0; c < DP / 16; c++) {
+        uint32_t acc[16];
+#pragma unroll
+        for (int i = 0; i < 16; i++) acc[i] = 0;
+        if (!first) tensor_load16(o_at + 16 * c, acc);
+        tensor_loaded();
+#pragma unroll 1
+        for (int k = 0; k < KEYS; k++) {
+            uint32_t pair, x[8];
+            asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];" : "=r"(pair) : "r"(p_at + (k >> 1)));
+            tensor_loaded();
+            const float2 both = unpack2<T>(pair);
+            const uint32_t word = k & 64 ? (k & 32 ? mask.w : mask.z) : (k & 32 ? mask.y : mask.x);
+            if (!(word >> (k & 31) & 1)) continue;
+            const float weight = k & 1 ? both.y : both.x;
+            asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]) : "r"(v + swizzled<KEYS>(k, 2 * c)));
+            asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(x[4]), "=r"(x[5]), "=r"(x[6]), "=r"(x[7]) : "r"(v + swizzled<KEYS>(k, 2 * c + 1)));
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                const float2 f = unpack2<T>(x[i]);
+                acc[2 * i] = __float_as_uint(fmaf(weight, f.x, __uint_as_float(acc[2 * i])));
+                acc[2 * i + 1] = __float_as_uint(fmaf(weight, f.y, __uint_as_float(acc[2 * i + 1])));
+            }
+        }
+        __syncwarp();
+        tensor_store16(o_at + 16 * c, acc);
+    }
+    tensor_stored();
+}
+
+// T: the type of the products, fp16 for codes.
+template <typename T, int KIND, int DP>
+__global__ void __launch_bounds__(kChunkThreads, 1) chunk_kernel(const __grid_constant__ ChunkParams p)
+{
+    using M = ChunkMemory<KIND, DP>;
+    constexpr int kKeys = M::keys, kSlots = M::slots, kWords = kKeys / 32, kMine = kKeys / 4;  // kMine: keys of a tile that a warp fetches
+    constexpr float kLift = probability_lift<T>();
+    extern __shared__ unsigned char raw[];
+    allow_next();
+    const uint32_t base = (static_cast<uint32_t>(__cvta_generic_to_shared(raw)) + 1023) & ~1023u;
+    unsigned char *const gen = raw + (base - static_cast<uint32_t>(__cvta_generic_to_shared(raw)));
+    constexpr int kRingAt = M::queries, kStagingAt = kRingAt + M::stages * M::tile, kInfoAt = kStagingAt + M::staged * M::codes, kDownsAt = kInfoAt + kChunkInfos * M::info,
+                  kTableAt = kDownsAt + M::downs, kItemsAt = kTableAt + M::table, kAnswerAt = kItemsAt + 2 * M::item, kBarsAt = kAnswerAt + 16;
+    static_assert(kInfoAt % 16 == 0 && kItemsAt % 16 == 0 && kAnswerAt % 16 == 0);
+    const uint32_t ring = base + kRingAt, staging = base + kStagingAt, info = base + kInfoAt;
+    const uint32_t full = base + kBarsAt, empty = full + 8 * M::stages, s_full = empty + 8 * M::stages, s_taken = s_full + 16, p_ready = s_taken + 16, o_added = p_ready + 16;
+    const uint32_t q_full = o_added + 16, q_empty = q_full + 8, item_full = q_empty + 8, item_empty = item_full + 16, wanted = item_empty + 16, answered = wanted + 8, last_at = answered + 8, tensor_at = last_at + 16;
+    static_assert(8 * (2 * M::stages + 18) + 8 <= 512);
+    uint32_t *const items_before = reinterpret_cast<uint32_t *>(gen + kTableAt), *const rows_before = items_before + kChunkThreads;
+    ChunkItem *const items = reinterpret_cast<ChunkItem *>(gen + kItemsAt);
+    const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31, D = p.layer.D, H = p.layer.H;
+    const ChunkShape &shape = p.shape;
+
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < M::stages; i++) barrier_init(full + 8 * i, 128), barrier_init(empty + 8 * i, 1);
+        for (int i = 0; i < 2; i++) barrier_init(s_full + 8 * i, 1), barrier_init(s_taken + 8 * i, 128), barrier_init(p_ready + 8 * i, 128), barrier_init(o_added + 8 * i, 1);
+        for (int i = 0; i < 2; i++) barrier_init(item_full + 8 * i, 1), barrier_init(item_empty + 8 * i, kSlots * 4 + 6), barrier_init(last_at + 8 * i, 1);
+        barrier_init(q_full, 128), barrier_init(q_empty, 1), barrier_init(wanted, 1), barrier_init(answered, 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 12) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(tensor_at) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+
+    // ------------------------------------------------------------------- the cut, the same in every CTA
+    // Each thread has a run of requests.
+    __shared__ int64_t sum_items[16];
+    __shared__ int32_t sum_tiles[16];
+    __shared__ float best_cost[16];
+    __shared__ int32_t best_share[16];
+    __shared__ uint32_t warp_items[16], warp_rows[16];
+    const int64_t per = (p.R + kChunkThreads - 1) / kChunkThreads, run0 = min(threadIdx.x * per, p.R), run1 = min(run0 + per, p.R);
+    int32_t share = 1 << 30;
+    if (p.plan.part_rows) {
+        int64_t n_items = 0;
+        int32_t most = 0;
+        for (int64_t r = run0; r < run1; r++) {
+            const ChunkRequest q = chunk_request(p, r, false);
+            if (!q.n) continue;
+            n_items += static_cast<int64_t>(chunk_blocks(shape, q.n)) * H;
+            most = max(most, chunk_tiles(shape, q.len));
+        }
+#pragma unroll
+        for (int x = 16; x; x >>= 1) n_items += __shfl_xor_sync(0xffffffffu, n_items, x);
+        most = __reduce_max_sync(0xffffffffu, most);
+        if (lane == 0) sum_items[warp] = n_items, sum_tiles[warp] = most;
+        __syncthreads();
+        n_items = 0;
+        for (int w = 0; w < 16; w++) n_items += sum_items[w], most = max(most, sum_tiles[w]);
+        if (n_items < kChunkEnough && most > kChunkLeastShare) {
+            // warp w looks at cuts w and w + 16
+            ChunkCost sum[2];
+            const int32_t shares[2] = {chunk_share(most, warp), chunk_share(most, warp + 16)};
+            const float inverse[2] = {1.f / shares[0], 1.f / shares[1]};
+            for (int64_t r = lane; r < p.R; r += 32) {
+                const ChunkRequest q = chunk_request(p, r, false);
+                if (!q.n) continue;
+                const int32_t blocks = chunk_blocks(shape, q.n) * H, tiles = chunk_tiles(shape, q.len);
+#pragma unroll
+                for (int c = 0; c < 2; c++) sum[c].add(blocks, tiles, shares[c], static_cast<int32_t>((static_cast<float>(tiles + shares[c] - 1) + 0.5f) * inverse[c]));
+            }
+            float cost = 3e38f;
+            int32_t chosen = 1 << 30;
+#pragma unroll
+            for (int c = 0; c < 2; c++) {
+#pragma unroll
+                for (int x = 16; x; x >>= 1) {
+                    sum[c].items += __shfl_xor_sync(0xffffffffu, sum[c].items, x), sum[c].split += __shfl_xor_sync(0xffffffffu, sum[c].split, x);
+                    sum[c].tiles += __shfl_xor_sync(0xffffffffu, sum[c].tiles, x);
+                }
+                const float here = chunk_cost(sum[c].items, sum[c].split, sum[c].tiles, __reduce_max_sync(0xffffffffu, sum[c].longest));
+                if (here < cost) cost = here, chosen = shares[c];
+            }
+            if (lane == 0) best_cost[warp] = cost, best_share[warp] = chosen;
+            __syncthreads();
+            cost = 3e38f;
+            for (int w = 0; w < 16; w++)
+                if (best_cost[w] < cost || (best_cost[w] == cost && best_share[w] > share)) cost = best_cost[w], share = best_share[w];
+        }
+    }
+    uint32_t total;
+    {
+        uint32_t my_items = 0, my_rows = 0;
+        for (int64_t r = run0; r < run1; r++) {
+            const ChunkRequest q = chunk_request(p, r, blockIdx.x == 0);
+            if (!q.n) continue;
+            const int32_t parts = chunk_parts(chunk_tiles(shape, q.len), share);
+            my_items += chunk_blocks(shape, q.n) * H * parts;
+            if (parts > 1) my_rows += static_cast<uint32_t>(q.n) * p.Hq * parts;
+        }
+        uint32_t upto = my_items, rows_upto = my_rows;
+#pragma unroll
+        for (int x = 1; x < 32; x <<= 1) {
+            const uint32_t a = __shfl_up_sync(0xffffffffu, upto, x), b = __shfl_up_sync(0xffffffffu, rows_upto, x);
+            if (lane >= x) upto += a, rows_upto += b;
+        }
+        if (lane == 31) warp_items[warp] = upto, warp_rows[warp] = rows_upto;
+        __syncthreads();
+        total = 0;
+        for (int w = 0; w < 16; w++) {
+            if (w < warp) upto += warp_items[w], rows_upto += warp_rows[w];
+            total += warp_items[w];
+        }
+        items_before[threadIdx.x] = upto - my_items, rows_before[threadIdx.x] = rows_upto - my_rows;
+        if (blockIdx.x == 0 && p.plan.part_rows) {
+            // for join_kernel
+            if (threadIdx.x == 0) p.base[0] = share;
+            uint32_t at = rows_upto - my_rows;
+            for (int64_t r = run0; r < run1; r++) {
+                const ChunkRequest q = chunk_request(p, r, false);
+                const int32_t parts = q.n ? chunk_parts(chunk_tiles(shape, q.len), share) : 0;
+                p.base[4 + r] = parts > 1 ? at : kUncut;
+                if (parts > 1) at += static_cast<uint32_t>(q.n) * p.Hq * parts;
+            }
+        }
+    }
+    fence_before();
+    __syncthreads();
+    fence_after();
+    // All 512 columns are this CTA's, so they begin at 0; a constant lets the products' operands stay in uniform registers.
+    constexpr uint32_t tensor = 0, kScores = 0, kProbabilities = 128, kOutputs = 256;
+    bool fine = true;  // no wait of this thread has run out
+
+    // Item `it` of this CTA's; false when there is none, or a wait ran out.
+    auto take_item = [&](int it, ChunkItem &item) {
+        if (!__all_sync(0xffffffffu, barrier_wait(item_full + 8 * (it & 1), (it >> 1) & 1))) {
+            fine = false;
+            return false;
+        }
+        const uint4 *src = reinterpret_cast<const uint4 *>(items + (it & 1));
+        uint4 *dst = reinterpret_cast<uint4 *>(&item);
+#pragma unroll
+        for (int i = 0; i < 5; i++) dst[i] = src[i];
+        __syncwarp();
+        if (lane == 0) barrier_arrive(item_empty + 8 * (it & 1));
+        return item.valid != 0;
+    };
+    auto tile_of = [](const ChunkItem &item, int i) { return i < item.list.firsts ? i : i + item.list.skip; };
+    // Does slot `slot` need tile i of the list?
+    auto needs = [](const ChunkItem &item, int slot, int i) {
+        if (kSlots == 1) return true;
+        return slot == 0 ? i < item.list.end0 : item.rows > 128 && (i < item.list.firsts || i >= item.list.begin1);
+    };
+    // Is there a key in tile i that some row sees and another does not?
+    auto ragged = [&](const ChunkItem &item, int i) {
+        const int k0 = tile_of(item, i) * kKeys;
+        return k0 + kKeys - 1 > item.pos0 + static_cast<int>(quick_div(item.row0, p.div_group)) || (k0 < item.list.key_end - shape.window && k0 + kKeys > shape.sinks);
+    };
+
+    if (warp < 8) {
+        // ---------------------------------------------------------------------------- softmax
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 192;");
+        const int slot = warp >> 2, r = (warp & 3) * 32 + lane;
+        const uint32_t lanes = tensor + (static_cast<uint32_t>((warp & 3) * 32) << 16), p_at = lanes + kProbabilities + slot * 64, o_at = lanes + kOutputs + slot * 128;
+        uint32_t steps = 0, tiles = 0, loads = 0;  // of this slot; of the CTA; items that had queries
+        for (int it = 0; slot < kSlots && fine; it++) {
+            ChunkItem item;
+            if (!take_item(it, item)) break;
+            const bool some = item.begin < item.end;
+            const int count = item.end - item.begin;
+            if (slot == 1 && item.rows <= 128) {
+                tiles += max(count, 0), loads += some;
+                continue;
+            }
+            const int row = item.row0 + min(slot * 128 + r, item.rows - 1);
+            const int token = static_cast<int>(quick_div(static_cast<uint32_t>(row), p.div_group)), pos = item.pos0 + token;
+            float factor = fabsf(p.scale_log2);  // of this thread's row of scores
+            const uint32_t down_at = base + kDownsAt + 4 * ((loads % M::down_sets) * kSlots * 128 + slot * 128 + r);
+            loads += some;
+            float top = -INFINITY;
+            float ref = -INFINITY;  // codes: the running maximum of the scores, which the sum is relative to; `top` has the tiles' powers in it
+            float2 sum = make_float2(0.f, 0.f);
+            bool mine = false;  // O holds something of this item
+            auto scale_outputs = [&](float f) {
+#pragma unroll 1
+                for (int c = 0; c < DP / 16 && fine; c++) {
+                    uint32_t v[16];
+                    tensor_load16(o_at + 16 * c, v);
+                    tensor_loaded();
+#pragma unroll
+                    for (int i = 0; i < 16; i++) v[i] = __float_as_uint(__uint_as_float(v[i]) * f);
+                    tensor_store16(o_at + 16 * c, v);
+                }
+            };
+            auto raise_ref = [&](float highest) {
+                const float to = fmaxf(ref, highest), less = exp2_approx(ref - (to == -INFINITY ? 0.f : to));
+                sum.x *= less, sum.y *= less;
+                ref = to;
+            };
+            for (int i = item.begin; i < item.end && fine; i++, tiles++) {
+                if (!needs(item, slot, i)) continue;
+                // one slot: the scores have two buffers in turn
+                const uint32_t b = kSlots == 1 ? steps & 1 : slot, parity = kSlots == 1 ? (steps >> 1) & 1 : steps & 1, s_at = lanes + kScores + (kSlots == 1 ? (steps & 1) * kKeys : 0);
+                fine = __all_sync(0xffffffffu, barrier_wait(s_full + 8 * b, parity));
+                if (!fine) break;
+                fence_after();
+                const uint32_t about = info + (tiles % kChunkInfos) * M::info;
+                // P is free and O at rest when this slot's last product is done
+                bool rest = steps == 0;
+                auto await_rest = [&]() {
+                    if (rest) return;
+                    fine = __all_sync(0xffffffffu, barrier_wait(o_added + 8 * slot, (steps - 1) & 1));
+                    fence_after();
+                    rest = true;
+                };
+                union {
+                    uint32_t w[kWords][32];
+                    float f[kWords][32];
+                    float2 f2[kWords][16];
+                } s;
+#pragma unroll
+                for (int c = 0; c < kWords; c++) tensor_load32(s_at + 32 * c, s.w[c]);
+                uint32_t mask[4];
+                asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(mask[0]), "=r"(mask[1]), "=r"(mask[2]), "=r"(mask[3]) : "r"(about));
+                const bool edge = ragged(item, i);
+                if (edge) {
+                    // what this row sees
+                    const int k0 = tile_of(item, i) * kKeys, upper = pos + 1 - k0, lower = upper - shape.window, firsts = shape.sinks - k0;
+#pragma unroll
+                    for (int c = 0; c < kWords; c++) mask[c] &= low_bits(upper - 32 * c) & (~low_bits(lower - 32 * c) | low_bits(firsts - 32 * c));
+                }
+                float exponent = 0.f;
+                uint32_t far = 0;
+                if constexpr (KIND != kPlain) asm volatile("ld.shared.v2.b32 {%0,%1}, [%2];" : "=f"(exponent), "=r"(far) : "r"(about + 32));
+                tensor_loaded();
+                bool stored = false;
+                if constexpr (KIND != kPlain) {
+                    if (!mine) {
+                        float down;
+                        asm volatile("ld.shared.f32 %0, [%1];" : "=f"(down) : "r"(down_at));
+                        factor *= down;
+                    }
+                    if (far) {
+                        RowState state{top, ref, sum.x + sum.y};
+                        await_rest();  // of the item before, too: P is free
+                        if (!fine) break;
+                        fine = far_tile<DP, kKeys>(state, s_at, p_at, o_at, make_uint4(mask[0], mask[1], mask[2], mask[3]), about + M::scales, factor, o_added + 8 * slot, (steps - 1) & 1, mine);
+                        top = state.top, ref = state.ref, sum = make_float2(state.sum, 0.f);
+                        if (!fine) break;
+                        stored = true;
+                    }
+                }
+                if (stored) {
+                    tensor_stored();
+                    fence_before();
+                    barrier_arrive(s_taken + 8 * b);
+                } else {
+                    fence_before();
+                    barrier_arrive(s_taken + 8 * b);
+                    if constexpr (KIND != kPlain) {
+                        const float2 f2 = make_float2(factor, factor), zero = make_float2(0.f, 0.f);
+#pragma unroll
+                        for (int j = 0; j < kKeys / 4; j++) {
+                            const float4 k = load_shared_f4(about + M::scales + 16 * j);
+                            float2 *x = &s.f2[j / 8][j % 8 * 2];
+                            x[0] = fused2(x[0], fused2(f2, make_float2(k.x, k.y), zero), zero);
+                            x[1] = fused2(x[1], fused2(f2, make_float2(k.z, k.w), zero), zero);
+                        }
+                    }
+                    uint32_t all_seen = mask[0];
+#pragma unroll
+                    for (int c = 1; c < kWords; c++) all_seen &= mask[c];
+                    if (all_seen != 0xffffffffu) {
+#pragma unroll
+                        for (int c = 0; c < kWords; c++)
+#pragma unroll
+                            for (int j = 0; j < 32; j++)
+                                if (!(mask[c] >> j & 1)) s.f[c][j] = -INFINITY;
+                    }
+                    float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+                    for (int c = 0; c < kWords; c++) {
+                        m4[c] = fmaxf(s.f[c][0], s.f[c][1]);
+#pragma unroll
+                        for (int j = 2; j < 32; j += 2) m4[c] = larger3(m4[c], s.f[c][j], s.f[c][j + 1]);
+                    }
+                    const float highest = fmaxf(larger3(m4[0], m4[1], m4[2]), m4[3]), most = KIND == kPlain ? highest * factor : highest + exponent;
+                    bool move = most > top + 8.f;
+                    if constexpr (KIND != kPlain) move = move || highest > ref + 8.f;
+                    if (__any_sync(0xffffffffu, move)) {
+                        if constexpr (KIND != kPlain) raise_ref(highest);
+                        const float m = fmaxf(top, most), f = m == top ? 1.f : exp2_approx(top - m);
+                        top = m;
+                        if constexpr (KIND == kPlain) sum.x *= f, sum.y *= f;
+                        if (mine) {
+                            await_rest();
+                            scale_outputs(f);
+                        }
+                    }
+                    const float m = top == -INFINITY ? 0.f : top - kLift;
+                    const float2 minus = make_float2(exponent - m, exponent - m), f2 = make_float2(factor, factor);
+                    uint32_t w[kWords][16];
+                    float2 here = make_float2(0.f, 0.f);
+#pragma unroll
+                    for (int c = 0; c < kWords; c++) {
+#pragma unroll
+                        for (int j = 0; j < 16; j++) {
+                            float2 e = KIND == kPlain ? fused2(s.f2[c][j], f2, minus) : sum2(s.f2[c][j], minus);
+                            e = make_float2(exp2_approx(e.x), exp2_approx(e.y));
+                            here = sum2(here, e);
+                            w[c][j] = pack2<T>(e.x, e.y);
+                        }
+                    }
+                    if constexpr (KIND == kPlain) {
+                        sum = sum2(sum, here);
+                    } else {
+                        // `here` is relative to m - exponent, which is at most 48 above ref: exponent is no less than 40 below any before
+                        const float all = here.x + here.y;
+                        sum.x = fmaf(all, all == 0.f ? 0.f : exp2_approx(m - exponent - (ref == -INFINITY ? 0.f : ref)), sum.x);
+                    }
+                    await_rest();  // by now it has been given, as a rule
+                    if (!fine) break;
+#pragma unroll
+                    for (int c = 0; c < kWords; c++) tensor_store16(p_at + 16 * c, w[c]);
+                    tensor_stored();
+                }
+                if (edge) {
+                    const uint32_t u = 2 * tiles + 1, stage = u % M::stages;
+                    fine = __all_sync(0xffffffffu, barrier_wait(full + 8 * stage, (u / M::stages) & 1));
+                    if (!fine) break;
+                    uint32_t bad[4];
+                    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(bad[0]), "=r"(bad[1]), "=r"(bad[2]), "=r"(bad[3]) : "r"(about + 16));
+                    if (bad[0] | bad[1] | bad[2] | bad[3]) spoiled_tile<T, DP, kKeys>(p_at, o_at, ring + stage * M::tile, make_uint4(mask[0], mask[1], mask[2], mask[3]), !mine);
+                }
+                fence_before();
+                barrier_arrive(p_ready + 8 * slot);
+                mine = true;
+                steps++;
+            }
+            if (!fine) break;
+            // The rows' outputs, or the part: outputs by the sum, and its logarithm.
+            const float all = sum.x + sum.y, lowest = KIND == kPlain ? top - kLift : ref;
+            const bool store = slot * 128 + r < item.rows, cut = item.part_row != kUncut;
+            const int head = item.h * shape.group + (row - token * shape.group);
+            const int64_t at = static_cast<int64_t>(item.part_row) + static_cast<int64_t>(token) * p.Hq + head;
+            const float log = all == 0.f ? -INFINITY : (lowest == -INFINITY ? 0.f : lowest) + log2f(all);
+            char *const out = p.out + (item.token0 + token) * p.out_token + head * p.out_head;
+            if (mine) {
+                fine = __all_sync(0xffffffffu, barrier_wait(o_added + 8 * slot, (steps - 1) & 1));
+                if (!fine) break;
+                fence_after();
+                float inv = all == 0.f ? 0.f : 1.f / all;
+                if constexpr (KIND != kPlain) {
+                    // outputs are relative to `top`: from there to `ref`, in two steps where fp32 does not hold one
+                    float step = top - kLift - (lowest == -INFINITY ? 0.f : lowest);
+                    if (__any_sync(0xffffffffu, !(fabsf(step) < 80.f))) {
+                        step *= 0.5f;
+                        scale_outputs(exp2_approx(step));
+                        tensor_stored();
+                    }
+                    inv *= exp2_approx(step);
+                }
+#pragma unroll 1
+                for (int c = 0; c < DP / 32; c++) {
+                    uint32_t v[32];
+                    tensor_load32(o_at + 32 * c, v);
+                    tensor_loaded();
+#pragma unroll
+                    for (int j = 0; j < 32; j++) v[j] = __float_as_uint(__uint_as_float(v[j]) * inv);
+                    if (cut) {
+#pragma unroll
+                        for (int j = 0; j < 32; j += 4)
+                            if (store && 32 * c + j < D) *reinterpret_cast<uint4 *>(p.parts + at * D + 32 * c + j) = make_uint4(v[j], v[j + 1], v[j + 2], v[j + 3]);
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 32; j += 8) {
+                            uint32_t w[4];
+#pragma unroll
+                            for (int k = 0; k < 4; k++) {
+                                const float a = __uint_as_float(v[j + 2 * k]), z = __uint_as_float(v[j + 2 * k + 1]);
+                                w[k] = KIND == kPlain ? pack2<T>(a, z) : p.q_bf16 ? pack2<__nv_bfloat16>(a, z) : pack2<__half>(a, z);
+                            }
+                            if (store && 32 * c + j < D) *reinterpret_cast<uint4 *>(out + (32 * c + j) * 2) = make_uint4(w[0], w[1], w[2], w[3]);
+                        }
+                    }
+                }
+                fence_before();  // O has been read when the next item's first probabilities are announced
+            } else if (store && !cut) {
+                for (int j = 0; j < D; j += 8) *reinterpret_cast<uint4 *>(out + j * 2) = make_uint4(0, 0, 0, 0);
+            }
+            if (store && cut) p.sums[at] = log;
+            if (store && !cut && p.lse) p.lse[(item.token0 + token) * p.Hq + head] = log * kChunkLn2;
+        }
+    } else if (warp < 12) {
+        // --------------------------------------------------------------------------- the pages
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+        const int w = warp - 8, thread = threadIdx.x - 256;
+        uint32_t tiles = 0, loads = 0;  // of the CTA; items that had queries
+        // what the table says of this lane's key of a tile; kNoKey: it is none.  Looked at a tile later
+        constexpr int32_t kNoKey = INT32_MIN;
+        auto key_of = [&](const ChunkItem &item, int i) { return tile_of(item, i) * kKeys + w * kMine + lane; };
+        auto look_up = [&](const ChunkItem &item, int i) -> int32_t {
+            const int t = key_of(item, i);
+            if (i >= item.end || lane >= kMine || t >= item.list.key_end || (t < item.list.key_low && t >= shape.sinks)) return kNoKey;
+            return reinterpret_cast<const int32_t *>(p.tables + item.r * p.table_stride)[quick_div(static_cast<uint32_t>(t), p.div_block)];
+        };
+        auto checked = [&](int32_t said) -> int32_t {
+            const bool in = said >= 0 && said < p.layer.num_blocks;
+            if (!in && said != kNoKey) atomicOr(p.status, kStatusBadIndex);
+            return in ? said : -1;
+        };
+        auto place_in_block = [&](int t) { return t - static_cast<int>(quick_div(static_cast<uint32_t>(t), p.div_block)) * static_cast<int>(p.layer.B); };
+        // where 8 elements of a row of queries are, or NULL: past the last row or past D
+        auto query_at = [&](const ChunkItem &item, int rr, int chunk) -> const char * {
+            if (rr >= item.rows || chunk * 8 >= D) return nullptr;
+            const uint32_t row = item.row0 + rr, token = quick_div(row, p.div_group);
+            return p.q + (item.token0 + token) * p.q_token + (item.h * shape.group + static_cast<int>(row - token * shape.group)) * p.q_head + chunk * 16;
+        };
+        // all of this group of four warps, wherever a wait of one ran out
+        auto together = [&](bool yes) {
+            uint32_t all;
+            asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.cta.red.and.pred q, 1, 128, p;\n\tselp.u32 %0, 1, 0, q;\n\t}" : "=r"(all) : "r"(static_cast<uint32_t>(yes)) : "memory");
+            return all != 0;
+        };
+
+        if constexpr (KIND == kPlain) {
+            // Copies in flight, oldest last: 1 + the barrier's index (stage; kQueries), flags for V of a tile that needs looking
+            // at (bit 8) and the tile's info (bits 16 on); 0: none.
+            constexpr uint32_t kQueries = 64, kLook = 256;
+            uint32_t flight[2] = {0, 0};
+            auto pass_on = [&](uint32_t what) {
+                if (!what) return;
+                const uint32_t index = (what & 255) - 1;
+                if (what & kLook) {
+                    uint32_t bad = 0;
+                    constexpr int chunks = DP / 8;
+#pragma unroll 4
+                    for (int i = 0; i < kMine * chunks / 32; i++) {
+                        const int idx = i * 32 + lane;
+                        uint32_t x[4];
+                        asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]) : "r"(ring + index * M::tile + swizzled<kKeys>(w * kMine + idx / chunks, idx % chunks)));
+                        bad |= not_finite<T>(x[0]) | not_finite<T>(x[1]) | not_finite<T>(x[2]) | not_finite<T>(x[3]);
+                    }
+                    if (__any_sync(0xffffffffu, bad != 0) && lane == 0) asm volatile("st.shared.u32 [%0], %1;" ::"r"(info + (what >> 16) * M::info + 16 + 4 * w), "r"(1) : "memory");
+                    __syncwarp();
+                }
+                fence_shared_to_async();
+                barrier_arrive(index == kQueries ? q_full : full + 8 * index);
+            };
+            auto in_flight = [&](uint32_t what) {
+                copy_commit();
+                copy_wait<2>();
+                pass_on(flight[1]);
+                flight[1] = flight[0], flight[0] = what;
+            };
+            auto land = [&]() {
+                copy_wait<0>();
+                pass_on(flight[1]), pass_on(flight[0]);
+                flight[0] = flight[1] = 0;
+            };
+            // waits until `bar` has passed, with what is in flight passed on meanwhile
+            auto await_free = [&](uint32_t bar, uint32_t parity) {
+                if (__all_sync(0xffffffffu, barrier_passed(bar, parity))) return;
+                land();
+                fine = __all_sync(0xffffffffu, barrier_wait(bar, parity));
+            };
+            for (int it = 0; fine; it++) {
+                ChunkItem item;
+                if (!__all_sync(0xffffffffu, barrier_passed(item_full + 8 * (it & 1), (it >> 1) & 1))) land();
+                if (!take_item(it, item)) break;
+                int32_t ahead = look_up(item, item.begin);
+                for (int i = item.begin; i < item.end && fine; i++, tiles++) {
+                    if (w == 0 && lane == 0 && i == max(item.begin, item.end - 2)) barrier_arrive(wanted);
+                    const int32_t blk = checked(ahead);
+                    const int64_t off = blk >= 0 ? p.layer.geo.at(blk, place_in_block(key_of(item, i)), item.h) : -1;
+                    ahead = look_up(item, i + 1);
+                    const uint32_t mask = __ballot_sync(0xffffffffu, blk >= 0), slot = tiles % kChunkInfos;
+                    for (int kv = 0; kv < 2; kv++) {
+                        const uint32_t u = 2 * tiles + kv, stage = u % M::stages;
+                        if (u >= M::stages) await_free(empty + 8 * stage, (u / M::stages - 1) & 1);
+                        if (!fine) break;
+                        if (kv == 0 && lane == 0) {
+                            // the tile whose mask this one's replaces is past its last use: its V is older than this stage's last copy
+                            const uint32_t about = info + slot * M::info;
+                            if constexpr (kMine == 32) asm volatile("st.shared.u32 [%0], %1;" ::"r"(about + 4 * w), "r"(mask) : "memory");
+                            else asm volatile("st.shared.u16 [%0], %1;" ::"r"(about + 2 * w), "h"(static_cast<uint16_t>(mask)) : "memory");
+                            asm volatile("st.shared.u32 [%0], %1;" ::"r"(about + 16 + 4 * w), "r"(0) : "memory");
+                        }
+                        const char *plane = kv ? p.layer.v : p.layer.k;
+                        const uint32_t to = ring + stage * M::tile;
+                        constexpr int chunks = DP / 8;
+#pragma unroll
+                        for (int j = 0; j < kMine * chunks / 32; j++) {
+                            const int idx = j * 32 + lane, rr = idx / chunks, ch = idx % chunks;
+                            const int64_t src = __shfl_sync(0xffffffffu, off, rr);
+                            const bool there = src >= 0 && ch * 8 < D;
+                            copy_async16(to + swizzled<kKeys>(w * kMine + rr, ch), plane + (there ? src + ch * 16 : 0), there);
+                        }
+                        in_flight((stage + 1) | (kv && ragged(item, i) ? kLook : 0u) | slot << 16);
+                        if (kv == 0 && i == item.begin) {
+                            // the queries, behind the first keys
+                            if (loads) await_free(q_empty, (loads - 1) & 1);
+                            if (!fine) break;
+#pragma unroll 4
+                            for (int j = 0; j < kSlots * DP / 8; j++) {
+                                const int idx = j * 128 + thread, rr = idx / chunks, ch = idx % chunks;
+                                const char *src = query_at(item, rr, ch);
+                                copy_async16(base + (rr >> 7) * M::q_tile + swizzled(rr & 127, ch), src ? src : p.q, src != nullptr);
+                            }
+                            in_flight(kQueries + 1);
+                            loads++;
+                        }
+                    }
+                }
+                if (item.begin >= item.end && w == 0 && lane == 0) barrier_arrive(wanted);
+            }
+            copy_wait<0>();
+            if (fine) land();
+        } else {
+            // Codes: a warp fetches and widens its own keys of every tile.  V's are multiplied by their scales over a
+            // power of two that the tile's largest scale sets, 2^exponent, which puts the values below 2^16: rounded
+            // to fp16 twice (the factor and the product), half a step of 2^-11 each, like the probabilities
+            // that they meet.  Products below fp16's normal numbers are off by half of 2^-24, which is 2^-15 of the
+            // key's scale at most, since a tile whose scales span more than 2^16 is `far`: there each key
+            // has an exponent of its own.  So it is where a tile's largest scale is 2^-40 of one before.  K's scales are left to the
+            // scores, in fp32, for the sake of the logarithms.
+            constexpr int chunks = DP / 16;
+            const uint32_t staged = staging + w * kMine * DP;
+            uint32_t copies = 0;  // issued, of the CTA
+            for (int it = 0;; it++) {
+                ChunkItem item;
+                const bool took = fine && take_item(it, item);
+                if (!together(took)) break;
+                const int n_copies = 2 * max(item.end - item.begin, 0);
+                int32_t ahead = look_up(item, item.begin);
+                int64_t off = -1;
+                float next_k = 0.f, next_v = 0.f, scale_v = 0.f;
+                uint32_t next_mask = 0;
+                auto fetch = [&](int u) {
+                    if (u < n_copies) {
+                        const int i = item.begin + (u >> 1);
+                        if ((u & 1) == 0) {
+                            const int32_t blk = checked(ahead);
+                            ahead = look_up(item, i + 1);
+                            off = blk >= 0 ? p.layer.geo.at(blk, place_in_block(key_of(item, i)), item.h) : -1;
+                        }
+                        const char *plane = u & 1 ? p.layer.v : p.layer.k;
+#pragma unroll
+                        for (int j = 0; j < kMine * chunks / 32; j++) {
+                            const int idx = j * 32 + lane, rr = idx / chunks, ch = idx % chunks;
+                            const int64_t src = __shfl_sync(0xffffffffu, off, rr);
+                            const bool there = src >= 0 && ch * 16 < D;
+                            copy_async16(staged + (u % M::staged) * M::codes + rr * DP + ch * 16, plane + (there ? src + ch * 16 : 0), there);
+                        }
+                    }
+                    copy_commit();
+                };
+                // masks and scales of a tile, a tile ahead of their use
+                auto fetch_scales = [&](int i) {
+                    next_k = next_v = 0.f;
+                    const int32_t blk = look_up(item, i);
+                    const bool there = blk >= 0 && blk < p.layer.num_blocks;
+                    if (there) {
+                        const int64_t at = p.layer.scale_geo.at(blk, place_in_block(key_of(item, i)), item.h);
+                        next_k = *reinterpret_cast<const float *>(reinterpret_cast<const char *>(p.layer.k_scale) + at);
+                        next_v = *reinterpret_cast<const float *>(reinterpret_cast<const char *>(p.layer.v_scale) + at);
+                    }
+                    next_mask = __ballot_sync(0xffffffffu, there);
+                };
+                int e_most = -133;  // the largest exponent of a tile so far
+                fetch_scales(item.begin);
+                for (int u = 0; u < M::staged - 1; u++) fetch(u);
+                if (n_copies) {
+                    // queries, fp16 with a power of two taken out of each row
+                    if (loads) fine = __all_sync(0xffffffffu, barrier_wait(q_empty, (loads - 1) & 1));
+                    for (int rr = thread; rr < kSlots * 128 && fine; rr += 128) {
+                        float most = 0.f, up, down;
+#pragma unroll 4
+                        for (int j = 0; j < DP / 8; j++) {
+                            const char *src = query_at(item, rr, j);
+                            const uint4 v = src ? *reinterpret_cast<const uint4 *>(src) : make_uint4(0, 0, 0, 0);
+                            for (uint32_t x : {v.x, v.y, v.z, v.w}) most = finite_magnitude(most, query_pair(x, p.q_bf16));
+                        }
+                        query_powers(most, up, down);
+#pragma unroll 4
+                        for (int j = 0; j < DP / 8; j++) {
+                            const char *src = query_at(item, rr, j);
+                            const uint4 v = src ? *reinterpret_cast<const uint4 *>(src) : make_uint4(0, 0, 0, 0);
+                            uint32_t x[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                            for (int k = 0; k < 4; k++) {
+                                const float2 f = query_pair(x[k], p.q_bf16);
+                                x[k] = pack2<__half>(f.x * up, f.y * up);
+                            }
+                            *reinterpret_cast<uint4 *>(gen + (rr >> 7) * M::q_tile + swizzled(rr & 127, j)) = make_uint4(x[0], x[1], x[2], x[3]);
+                        }
+                        *reinterpret_cast<float *>(gen + kDownsAt + 4 * ((loads % M::down_sets) * kSlots * 128 + rr)) = down;
+                    }
+                    fence_shared_to_async();
+                    if (fine) barrier_arrive(q_full);
+                    loads++;
+                }
+                for (int v = 0; v < n_copies; v++) {
+                    const uint32_t u = copies + v, stage = u % M::stages;
+                    const int i = item.begin + (v >> 1);
+                    copy_wait<M::staged - 2>();
+                    __syncwarp();
+                    if (w == 0 && lane == 0 && (v & 1) == 0 && i == max(item.begin, item.end - 2)) barrier_arrive(wanted);
+                    if (u >= M::stages && fine) fine = __all_sync(0xffffffffu, barrier_wait(empty + 8 * stage, (u / M::stages - 1) & 1));
+                    const uint32_t about = info + (tiles % kChunkInfos) * M::info;
+                    if ((v & 1) == 0) {
+                        // the tile whose mask and scales these replace is past its last use: its V is older than this stage's last copy
+                        const float scale_k = next_k;
+                        scale_v = next_v;
+                        if (lane == 0) {
+                            if constexpr (kMine == 32) asm volatile("st.shared.u32 [%0], %1;" ::"r"(about + 4 * w), "r"(next_mask) : "memory");
+                            else asm volatile("st.shared.u16 [%0], %1;" ::"r"(about + 2 * w), "h"(static_cast<uint16_t>(next_mask)) : "memory");
+                            asm volatile("st.shared.u32 [%0], %1;" ::"r"(about + 16 + 4 * w), "r"(0) : "memory");
+                        }
+                        if (lane < kMine) asm volatile("st.shared.f32 [%0], %1;" ::"r"(about + M::scales + 4 * (w * kMine + lane)), "f"(scale_k) : "memory");
+                        fetch_scales(i + 1);
+                        const uint32_t bits = __float_as_uint(scale_v) & 0x7fffffffu, size = bits > 0x7f800000u ? 0 : bits;  // a NaN is passed over
+                        const uint32_t warp_most = __reduce_max_sync(0xffffffffu, size), warp_least = __reduce_min_sync(0xffffffffu, size ? size : 0x7f800000u);
+                        if (lane == 0) {
+                            asm volatile("st.shared.u32 [%0], %1;" ::"r"(about + 48 + 4 * w), "r"(warp_most) : "memory");
+                            asm volatile("st.shared.u32 [%0], %1;" ::"r"(about + 64 + 4 * w), "r"(warp_least) : "memory");
+                        }
+                        fine = together(fine);  // the four warps come here for every tile, and leave together where a wait ran out
+                        if (!fine) break;
+                        uint32_t all[4], low[4];
+                        asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(all[0]), "=r"(all[1]), "=r"(all[2]), "=r"(all[3]) : "r"(about + 48));
+                        asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(low[0]), "=r"(low[1]), "=r"(low[2]), "=r"(low[3]) : "r"(about + 64));
+                        int e = static_cast<int>(max(max(all[0], all[1]), max(all[2], all[3])) >> 23) - 127 - 6;  // a tile of zeros: the least
+                        const bool far = e < e_most - 40 || static_cast<int>(min(min(low[0], low[1]), min(low[2], low[3])) >> 23) - 127 - 6 < e - 16;
+                        e_most = max(e_most, e);
+                        if (w == 0 && lane == 0) asm volatile("st.shared.v2.b32 [%0], {%1,%2};" ::"r"(about + 32), "f"(static_cast<float>(e)), "r"(static_cast<uint32_t>(far)) : "memory");
+                        if (far) {
+                            // each key's own; one of zeros takes no part in the probabilities
+                            e = static_cast<int>(size >> 23) - 127 - 6;
+                            if (lane < kMine)
+                                asm volatile("st.shared.f32 [%0], %1;" ::"r"(about + M::scales + 4 * kKeys + 4 * (w * kMine + lane)), "f"(scale_v == 0.f ? -4096.f : static_cast<float>(e)) : "memory");
+                        }
+                        // 2^-e, up to 2^133, in two factors
+                        scale_v *= __uint_as_float(static_cast<uint32_t>(127 + min(-e, 127)) << 23);
+                        scale_v *= __uint_as_float(static_cast<uint32_t>(127 + max(-e - 127, 0)) << 23);
+                    }
+                    const uint32_t from = staged + (v % M::staged) * M::codes, to = ring + stage * M::tile;
+                    const uint32_t factor2 = pack2<__half>(scale_v, scale_v);
+                    uint32_t bad = 0;
+                    // four 16-byte chunks of codes at a time, loads first
+#pragma unroll
+                    for (int i0 = 0; i0 < kMine * chunks / 32 && fine; i0 += 4) {
+                        uint32_t c[4][4];
+#pragma unroll
+                        for (int j = 0; j < 4; j++) {
+                            const int idx = (i0 + j) * 32 + lane;
+                            asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(c[j][0]), "=r"(c[j][1]), "=r"(c[j][2]), "=r"(c[j][3]) : "r"(from + idx / chunks * DP + idx % chunks * 16));
+                        }
+#pragma unroll
+                        for (int j = 0; j < 4; j++) {
+                            const int idx = (i0 + j) * 32 + lane, rr = idx / chunks, ch = idx % chunks;
+                            // two 16-byte chunks; the lanes of every other 64 d's write theirs in the other order, into other banks
+                            const bool odd = ch & 4;
+                            uint32_t x[8];
+                            widen<KIND>(odd ? c[j][2] : c[j][0], x[0], x[1]);
+                            widen<KIND>(odd ? c[j][3] : c[j][1], x[2], x[3]);
+                            widen<KIND>(odd ? c[j][0] : c[j][2], x[4], x[5]);
+                            widen<KIND>(odd ? c[j][1] : c[j][3], x[6], x[7]);
+                            if (v & 1) {
+                                const uint32_t f = __shfl_sync(0xffffffffu, factor2, rr);
+#pragma unroll
+                                for (int k = 0; k < 8; k++) {
+                                    const __half2 y = __hmul2(*reinterpret_cast<const __half2 *>(&x[k]), *reinterpret_cast<const __half2 *>(&f));
+                                    x[k] = *reinterpret_cast<const uint32_t *>(&y);
+                                    bad |= not_finite<__half>(x[k]);
+                                }
+                            }
+                            const uint32_t a = to + swizzled<kKeys>(w * kMine + rr, 2 * ch + odd), b = to + swizzled<kKeys>(w * kMine + rr, 2 * ch + !odd);
+                            asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(a), "r"(x[0]), "r"(x[1]), "r"(x[2]), "r"(x[3]) : "memory");
+                            asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(b), "r"(x[4]), "r"(x[5]), "r"(x[6]), "r"(x[7]) : "memory");
+                        }
+                    }
+                    if ((v & 1) && __any_sync(0xffffffffu, bad != 0) && ragged(item, i) && lane == 0) asm volatile("st.shared.u32 [%0], %1;" ::"r"(about + 16 + 4 * w), "r"(1) : "memory");
+                    __syncwarp();
+                    fence_shared_to_async();
+                    if (fine) barrier_arrive(full + 8 * stage);
+                    __syncwarp();
+                    fetch(v + M::staged - 1);
+                    tiles += v & 1;
+                }
+                copy_wait<0>();
+                copies += n_copies;
+                if (n_copies == 0 && w == 0 && lane == 0) barrier_arrive(wanted);
+            }
+            copy_wait<0>();
+        }
+    } else {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+        // ----------------------------------------------------------------------- matrix products
+        // Two warps, one for each product, so that neither waits for what only the other needs.  They stay together and
+        // elect the thread that issues: with uniform control the operands are uniform registers already.
+        if (warp == 12) {
+            // a negative scale: the queries enter with the other sign
+            const uint32_t qk = instruction<T>(kKeys, false) | (p.scale_log2 < 0.f ? 1u << 13 : 0u);
+            uint32_t tiles = 0, loads = 0, steps[2] = {0, 0};
+            int before = -1;  // the slot whose scores were the last
+            for (int it = 0; fine; it++) {
+                ChunkItem item;
+                if (!take_item(it, item)) break;
+                if (item.begin >= item.end) continue;
+                fine = __all_sync(0xffffffffu, barrier_wait(q_full, loads & 1));
+                for (int i = item.begin; i < item.end && fine; i++, tiles++) {
+                    const uint32_t u = 2 * tiles, stage = u % M::stages;
+                    fine = barrier_wait(full + 8 * stage, (u / M::stages) & 1);
+#pragma unroll
+                    for (int slot = 0; slot < kSlots; slot++) {
+                        if (!needs(item, slot, i)) continue;
+                        uint32_t b, column = tensor + kScores;
+                        if constexpr (kSlots == 1) {
+                            b = steps[0] & 1, column += b * kKeys;
+                            if (steps[0] >= 2 && fine) fine = barrier_wait(s_taken + 8 * b, ((steps[0] >> 1) - 1) & 1);
+                        } else {
+                            // the buffer is free when the scores of the step before have been taken
+                            b = slot;
+                            if (before >= 0 && fine) fine = barrier_wait(s_taken + 8 * before, (steps[before] - 1) & 1);
+                        }
+                        fine = __all_sync(0xffffffffu, fine);
+                        if (!fine) break;
+                        fence_after();
+                        const uint64_t q_operand = operand(base + slot * M::q_tile, 16), k_operand = operand(ring + stage * M::tile, 16);
+                        if (elected()) {
+#pragma unroll
+                            for (int k = 0; k < DP / 16; k++)
+                                mma_shared(column, q_operand + (((k >> 2) * (128 * 128) + (k & 3) * 32) >> 4), k_operand + (((k >> 2) * (kKeys * 128) + (k & 3) * 32) >> 4), qk, k > 0);
+                            commit_to(s_full + 8 * b);
+                        }
+                        __syncwarp();
+                        steps[slot]++;
+                        before = slot;
+                    }
+                    if (!fine) break;
+                    if (elected()) {
+                        commit_to(empty + 8 * stage);
+                        if (i + 1 == item.end) commit_to(q_empty);
+                    }
+                    __syncwarp();
+                }
+                loads++;
+            }
+        } else if (warp == 13) {
+            const uint32_t pv = instruction<T>(DP, true);
+            uint32_t tiles = 0, steps[2] = {0, 0};
+            for (int it = 0; fine; it++) {
+                ChunkItem item;
+                if (!take_item(it, item)) break;
+                bool holds[2] = {false, false};  // O of a slot holds something of this item
+                for (int i = item.begin; i < item.end && fine; i++, tiles++) {
+                    const uint32_t u = 2 * tiles + 1, stage = u % M::stages;
+                    fine = __all_sync(0xffffffffu, barrier_wait(full + 8 * stage, (u / M::stages) & 1));
+                    if (!fine) break;
+                    uint32_t bad[4];
+                    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(bad[0]), "=r"(bad[1]), "=r"(bad[2]), "=r"(bad[3]) : "r"(info + (tiles % kChunkInfos) * M::info + 16));
+                    const bool spoiled = __any_sync(0xffffffffu, (bad[0] | bad[1] | bad[2] | bad[3]) != 0);
+                    const uint64_t v_operand = operand(ring + stage * M::tile, kKeys * 128);
+#pragma unroll
+                    for (int slot = 0; slot < kSlots; slot++) {
+                        if (!needs(item, slot, i)) continue;
+                        fine = __all_sync(0xffffffffu, barrier_wait(p_ready + 8 * slot, steps[slot] & 1));
+                        if (!fine) break;
+                        fence_after();
+                        if (elected()) {
+                            if (!spoiled) {  // else the softmax has added it up
+#pragma unroll
+                                for (int k = 0; k < kKeys / 16; k++)
+                                    mma_tensor(tensor + kOutputs + slot * 128, tensor + kProbabilities + slot * 64 + 8 * k, v_operand + k * (2048 >> 4), pv, holds[slot] || k > 0);
+                            }
+                            commit_to(o_added + 8 * slot);
+                        }
+                        __syncwarp();
+                        holds[slot] = true;
+                        steps[slot]++;
+                    }
+                    if (!fine) break;
+                    if (elected()) commit_to(empty + 8 * stage);
+                    __syncwarp();
+                }
+            }
+        } else if (warp == 14) {
+            // -------------------------------------------------------------------------- the items
+            // This CTA's first is its own; then it takes over CTAs that have not been launched yet, one whenever the copies of the
+            // last item near their end.
+            const uint32_t answer = base + kAnswerAt;
+            uint32_t id = blockIdx.x, asked = 0;
+            bool more = true;
+            for (int it = 0; fine;) {
+                if (more && id < total) {
+                    // the last thread whose requests begin at or before the item, then the request
+                    int t = -1;
+#pragma unroll
+                    for (int j = 0; j < kChunkThreads / 32; j++) t += __popc(__ballot_sync(0xffffffffu, items_before[j * 32 + lane] <= id));
+                    uint32_t at = items_before[t], rows_at = rows_before[t];
+                    const int64_t to = min((t + 1) * per, p.R);
+                    ChunkItem item;
+                    item.valid = 0;
+                    for (int64_t r = t * per; r < to; r++) {
+                        const ChunkRequest q = chunk_request(p, r, false);
+                        if (!q.n) continue;
+                        const int32_t parts = chunk_parts(chunk_tiles(shape, q.len), share), blocks = chunk_blocks(shape, q.n);
+                        const uint32_t here = static_cast<uint32_t>(blocks) * parts * H;
+                        if (id >= at + here) {
+                            at += here;
+                            if (parts > 1) rows_at += static_cast<uint32_t>(q.n) * p.Hq * parts;
+                            continue;
+                        }
+                        // heads first, so that CTAs side by side read pages side by side; the last block, which sees most, first
+                        uint32_t rest = id - at;
+                        item.h = rest % H, rest /= H;
+                        const int32_t part = rest % parts, block = blocks - 1 - static_cast<int32_t>(rest / parts);
+                        item.valid = 1, item.r = static_cast<int32_t>(r);
+                        item.row0 = block * shape.rows;
+                        item.rows = min(static_cast<int32_t>(min(static_cast<int64_t>(q.n) * shape.group - item.row0, static_cast<int64_t>(shape.rows))), shape.rows);
+                        item.pos0 = q.len - q.n;
+                        item.list = chunk_list(shape, item.pos0, item.row0, item.rows, 128);
+                        item.begin = static_cast<int32_t>(min(static_cast<int64_t>(part) * share, static_cast<int64_t>(item.list.count)));
+                        item.end = static_cast<int32_t>(min(static_cast<int64_t>(item.begin) + share, static_cast<int64_t>(item.list.count)));
+                        item.part_row = parts > 1 ? rows_at + static_cast<uint32_t>(part) * q.n * p.Hq : kUncut;
+                        item.token0 = q.token0, item.n = q.n, item.pad = 0;
+                        break;
+                    }
+                    if (item.valid) {
+                        if (it >= 2) fine = __all_sync(0xffffffffu, barrier_wait(item_empty + 8 * (it & 1), ((it >> 1) - 1) & 1));
+                        if (!fine) break;
+                        if (lane == 0) {
+                            items[it & 1] = item;
+                            barrier_arrive(item_full + 8 * (it & 1));
+                        }
+                        __syncwarp();
+                        fine = __all_sync(0xffffffffu, barrier_wait(wanted, it & 1));
+                        if (!fine) break;
+                        it++;
+                    }
+                }
+                if (!more) {
+                    // no item: the end
+                    if (it >= 2) fine = __all_sync(0xffffffffu, barrier_wait(item_empty + 8 * (it & 1), ((it >> 1) - 1) & 1));
+                    if (lane == 0) {
+                        items[it & 1].valid = 0;
+                        barrier_arrive(item_full + 8 * (it & 1));
+                    }
+                    break;
+                }
+                if (elected()) {
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // the answer before has been read
+                    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], 16;" ::"r"(answered) : "memory");
+                    asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];" ::"r"(answer), "r"(answered) : "memory");
+                }
+                __syncwarp();
+                fine = __all_sync(0xffffffffu, barrier_wait(answered, asked & 1));
+                asked++;
+                if (!fine) break;
+                uint32_t got, next = 0;
+                asm volatile("{\n\t.reg .pred p;\n\t.reg .b128 a;\n\tld.shared.b128 a, [%2];\n\tclusterlaunchcontrol.query_cancel.is_canceled.pred.b128 p, a;\n\tselp.u32 %0, 1, 0, p;\n\t"
+                             "mov.u32 %1, 0;\n\t@p clusterlaunchcontrol.query_cancel.get_first_ctaid.v4.b32.b128 {%1, _, _, _}, a;\n\t}"
+                             : "=r"(got), "=r"(next) : "r"(answer) : "memory");
+                __syncwarp();
+                more = got != 0, id = next;
+            }
+        }
+        if ((warp == 12 || warp == 13) && !fine) {
+            // products may be in flight: let them end before the tensor memory is given back
+            const uint32_t last = last_at + 8 * (warp - 12);
+            if (elected()) commit_to(last);
+            __syncwarp();
+            barrier_wait(last, 0);
+        }
+    }
+    if (!fine) atomicOr(p.status, static_cast<unsigned int>(TC_DEVICE_BULK_WAIT_TIMEOUT));
+    fence_before();
+    __syncthreads();
+    if (warp == 12) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tensor) : "memory");
+}
+
+template <typename T, int KIND, int DP>
+int launch_chunk_shape(const ChunkParams &p, int device, cudaStream_t s)
+{
+    using M = ChunkMemory<KIND, DP>;
+    static_assert(M::bytes <= 232448 - 1024, "more shared memory than a CTA can have beside its static arrays");
+    static std::atomic<bool> raised[kMaxDevices];  // set once per device; setting it twice does no harm
+    if (!raised[device].load(std::memory_order_relaxed)) {
+        const cudaError_t e = cudaFuncSetAttribute(chunk_kernel<T, KIND, DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, M::bytes);
+        if (e != cudaSuccess) return cuda_fail(e, "cudaFuncSetAttribute(dynamic shared memory)");
+        raised[device].store(true, std::memory_order_relaxed);
+    }
+    return launch_attn(chunk_kernel<T, KIND, DP>, static_cast<unsigned>(p.plan.grid), kChunkThreads, M::bytes, false, p, s);
+}
+
+template <typename T, int KIND>
+int launch_chunk_type(const ChunkParams &p, int device, cudaStream_t s)
+{
+    if (p.layer.D <= 64) return launch_chunk_shape<T, KIND, 64>(p, device, s);
+    if (p.layer.D <= 128) return launch_chunk_shape<T, KIND, 128>(p, device, s);
+    return launch_chunk_shape<T, KIND, 256>(p, device, s);
+}
+
+}  // namespace tc

@@ -1,0 +1,40 @@
+// The arguments of tc_attn_chunk's kernels: shared by the entry points and the kernels' launchers.
+#pragma once
+
+#include "attn_chunk_split.h"
+#include "ops.h"
+
+namespace tc {
+
+struct ChunkParams {
+    Layer layer;
+    const char *q;
+    int64_t q_token, q_head;
+    char *out;
+    int64_t out_token, out_head;
+    float *lse;
+    const char *tables;
+    int64_t table_stride;
+    const int64_t *offsets;
+    const int32_t *lens;
+    int64_t R, n_tokens, max_new, max_len;
+    int32_t Hq, q_bf16;
+    float scale_log2;  // scale * log2(e)
+    FastDiv div_block, div_group;
+    ChunkShape shape;
+    ChunkPlan plan;
+    uint32_t *base;  // {share, 0, 0, 0}, then for every request the first of its parts' rows, kUncut where it is not cut
+    float *sums, *parts;
+    unsigned int *status;
+};
+constexpr uint32_t kUncut = 0xffffffffu;
+
+// attn_chunk.cu, attn_chunk_codes.cu: the items, of unquantised pools and of codes
+int launch_chunk_plain(const ChunkParams &p, int dtype, int device, cudaStream_t s);
+int launch_chunk_codes(const ChunkParams &p, int device, cudaStream_t s);
+
+// Rows and tile that the kernels take for a head dim.
+inline int32_t chunk_rows(int64_t D) { return D > 128 ? 128 : 256; }
+inline int32_t chunk_keys(int64_t D) { return D > 128 ? 64 : 128; }
+
+}  // namespace tc

@@ -1,0 +1,132 @@
+// How tc_attn_chunk cuts its work: plain code, for the kernels, the entry points and tests without a GPU.
+//
+// An item is a block of up to `rows` rows (token, head) of one request and KV head, and a part of the tiles of keys that any
+// of them sees.  Lengths are known on the device alone, so every CTA finds the same cut there, by ChunkCost.
+#pragma once
+
+#include <stdint.h>
+
+#include "kv_index.h"
+
+namespace tc {
+
+constexpr int kChunkSms = 148;          // B200; workspaces must not depend on the device that happens to be current
+constexpr int kChunkLeastShare = 6;     // tiles of a part at least: beginning, ending and joining one costs as much as some eight
+constexpr int kChunkMostParts = 128;    // of a request's keys
+constexpr int kChunkSplitItems = 4 * kChunkSms;  // items that a cut may leave of the requests it cuts
+constexpr int kChunkEnough = 4 * kChunkSms;      // with so many items nothing is cut: they even out by themselves
+constexpr int kChunkEnds = 4;           // what an item costs beside its tiles, in tiles; a cut one twice
+
+struct ChunkShape {
+    int32_t group;   // query heads per KV head
+    int32_t rows;    // of an item at most
+    int32_t keys;    // of a tile
+    int32_t window;  // keys that a row sees up to its own, 2^30 = all
+    int32_t sinks;   // first keys that every row sees
+    int32_t heads;   // KV heads
+};
+
+TC_HD int32_t chunk_low(int32_t a, int32_t b) { return a < b ? a : b; }
+TC_HD int32_t chunk_high(int32_t a, int32_t b) { return a > b ? a : b; }
+
+// Items of n new tokens of one KV head, uncut.
+TC_HD int32_t chunk_blocks(const ChunkShape &s, int32_t n) { return static_cast<int32_t>((static_cast<int64_t>(n) * s.group + s.rows - 1) / s.rows); }
+
+// Tiles that a block of a request with `len` keys lists at most.
+TC_HD int32_t chunk_tiles(const ChunkShape &s, int32_t len)
+{
+    const int32_t all = (len + s.keys - 1) / s.keys;
+    const int64_t near = static_cast<int64_t>(s.window) + (s.rows - 1) / s.group + 1;  // keys that a block sees in its window
+    const int64_t most = (near + s.keys - 2) / s.keys + 1 + (chunk_low(s.sinks, len) + s.keys - 1) / s.keys;
+    return most < all ? static_cast<int32_t>(most) : all;
+}
+
+// The tiles that a block lists: the first `firsts`, which hold the keys that all rows see, then from tile firsts + skip on.
+struct ChunkList {
+    int32_t key_end, key_low;  // keys below key_end, from key_low on or below `sinks`, are seen by some row
+    int32_t firsts, skip, count;
+    int32_t end0, begin1;  // of the list: slot 0 needs none from end0 on, slot 1 none between `firsts` and begin1
+};
+// pos0: position of the request's first new token; rows row0 .. row0 + rows_here - 1 of its n * group; slot 0 holds the first `slot_rows`.
+TC_HD ChunkList chunk_list(const ChunkShape &s, int32_t pos0, int32_t row0, int32_t rows_here, int32_t slot_rows)
+{
+    ChunkList l;
+    const int32_t first = pos0 + row0 / s.group, last = pos0 + (row0 + rows_here - 1) / s.group;
+    l.key_end = last + 1;
+    l.key_low = chunk_high(0, first - s.window + 1);
+    const int32_t low = l.key_low / s.keys, high = last / s.keys;
+    const int32_t sunk = (chunk_low(s.sinks, l.key_end) + s.keys - 1) / s.keys;
+    l.firsts = chunk_low(sunk, low);
+    l.skip = low - l.firsts;
+    l.count = l.firsts + high - low + 1;
+    l.end0 = l.count, l.begin1 = l.count;
+    if (rows_here > slot_rows) {
+        l.end0 = (pos0 + (row0 + slot_rows - 1) / s.group) / s.keys - l.skip + 1;
+        if (sunk > low) l.begin1 = l.firsts;  // keys that every row sees reach into the tiles behind
+        else l.begin1 = chunk_high(0, pos0 + (row0 + slot_rows) / s.group - s.window + 1) / s.keys - l.skip;
+    }
+    return l;
+}
+
+TC_HD int32_t chunk_parts(int32_t tiles, int32_t share) { return (tiles + share - 1) / share; }
+// The cuts that are looked at: into parts of so many tiles that the longest list has up to 1 .. 16, then up to 23, 30 .. 128.
+constexpr int kChunkCuts = 32;
+TC_HD int32_t chunk_share(int32_t most_tiles, int32_t cut)
+{
+    const int32_t parts = cut < 16 ? cut + 1 : 16 + (cut - 15) * 7;
+    return chunk_high((most_tiles + parts - 1) / parts, parts > 1 ? kChunkLeastShare : 1);
+}
+
+// What a cut costs, in tiles: waves of items of average size, or the longest item.
+struct ChunkCost {
+    int64_t items = 0, split = 0, tiles = 0;
+    int32_t longest = 0;
+    // blocks: of one request, of all KV heads
+    TC_HD void add(int32_t blocks, int32_t tiles_of, int32_t share, int32_t parts)
+    {
+        const int64_t here = static_cast<int64_t>(blocks) * parts;
+        items += here;
+        tiles += static_cast<int64_t>(blocks) * tiles_of;
+        if (parts > 1) split += here;
+        longest = chunk_high(longest, chunk_low(tiles_of, share) + (parts > 1 ? 2 : 1) * kChunkEnds);
+    }
+};
+TC_HD float chunk_cost(int64_t items, int64_t split, int64_t tiles, int32_t longest)
+{
+    if (split > kChunkSplitItems) return 3e38f;
+    if (items == 0) return 0.f;
+    const float waves = static_cast<float>((items + kChunkSms - 1) / kChunkSms);
+    const float all = waves * static_cast<float>(tiles + kChunkEnds * (items + split)) / static_cast<float>(items);
+    return all > static_cast<float>(longest) ? all : static_cast<float>(longest);
+}
+
+// What the host can say of a call: its grid, and its workspace: {share, R words of `base`} then sums and outputs of the parts' rows.
+struct ChunkPlan {
+    int64_t grid;       // items at most
+    int64_t part_rows;  // rows of parts at most; 0: nothing is cut
+    int64_t base_at, sums_at, parts_at, workspace;
+};
+inline void plan_chunk(const ChunkShape &s, int64_t R, int64_t n_tokens, int64_t max_new, int64_t max_len, int64_t D, ChunkPlan *p)
+{
+    *p = ChunkPlan{};
+    const int64_t new_most = max_new < n_tokens ? max_new : n_tokens, live = R < n_tokens ? R : n_tokens;
+    const int64_t by_each = R * chunk_blocks(s, static_cast<int32_t>(new_most)), by_all = n_tokens * s.group / s.rows + live;
+    const int64_t items = (by_each < by_all ? by_each : by_all) * s.heads, tiles = chunk_tiles(s, static_cast<int32_t>(max_len));
+    p->grid = items;
+    if (tiles <= kChunkLeastShare || items == 0) return;
+    p->grid += kChunkSplitItems;
+    const int64_t item_rows = new_most * s.group < s.rows ? new_most * s.group : s.rows, rows = R * new_most * s.group * s.heads;
+    const int64_t parts = chunk_parts(static_cast<int32_t>(tiles), kChunkLeastShare);
+    const int64_t by_items = kChunkSplitItems * item_rows, by_rows = rows * (parts < kChunkMostParts ? parts : kChunkMostParts);
+    p->part_rows = by_items < by_rows ? by_items : by_rows;
+    auto place = [&](int64_t bytes) {
+        const int64_t at = p->workspace;
+        p->workspace += (bytes + 255) / 256 * 256;
+        return at;
+    };
+    p->base_at = place((R + 4) * 4);
+    p->sums_at = place(p->part_rows * 4);
+    p->parts_at = place(p->part_rows * D * 4);
+}
+
+}  // namespace tc

@@ -70,8 +70,8 @@ __device__ __forceinline__ float finite_magnitude(float most, float2 f)
 }
 
 // `follows`: a kernel of the same call was launched before this one, which then may start before that one's end.
-template <typename Kernel>
-int launch_attn(Kernel kernel, unsigned grid, unsigned threads, size_t shared, bool follows, const AttnParams &p, cudaStream_t s)
+template <typename Kernel, typename Params>
+int launch_attn(Kernel kernel, unsigned grid, unsigned threads, size_t shared, bool follows, const Params &p, cudaStream_t s)
 {
     cudaLaunchConfig_t config{};
     config.gridDim = dim3(grid);

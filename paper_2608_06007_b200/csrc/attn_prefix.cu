@@ -31,12 +31,10 @@
 #include <atomic>
 
 #include "attn.h"
-#include "attn_device.cuh"
-#include "barrier.cuh"
+#include "attn_tensor.cuh"
 
 namespace tc {
 
-constexpr int kTile = 128;       // keys of a tile, and rows of a slot
 constexpr int kPrefixThreads = 512;  // 128 registers each; the softmax's 256 take 192, the others keep 64
 constexpr int kInfos = 4;            // tiles whose masks and scales are kept
 
@@ -51,162 +49,6 @@ struct PrefixShape {
     static constexpr int info = KIND == kPlain ? 16 : 64 + 8 * kTile;  // mask; V's exponent, whether scales are far apart; each warp's largest and smallest; scales of K; keys' exponents
     static constexpr int bytes = queries + stages * tile + staged * codes + kInfos * info + 256 + 1024;  // barriers, slack for the alignment
 };
-
-// Shared-memory operand descriptor: 128-byte swizzle, 8-row atoms of 1024 bytes `sbo` apart; lbo: from one
-// 64-element column of atoms to the next (only where the 64 elements run along M or N).
-__device__ __forceinline__ uint64_t operand(uint32_t addr, uint32_t lbo)
-{
-    return static_cast<uint64_t>((addr >> 4) & 0x3fff) | static_cast<uint64_t>(lbo >> 4) << 16 | static_cast<uint64_t>(1024 >> 4) << 32 | 1ull << 46 | 2ull << 61;
-}
-// Instruction descriptor: fp32 sums of 16-bit products, M = 128.
-template <typename A> __device__ constexpr uint32_t instruction(int n, bool b_rows_along_n)
-{
-    const uint32_t type = sizeof(A) && std::is_same<A, __nv_bfloat16>::value ? 1 : 0;
-    return 1u << 4 | type << 7 | type << 10 | (b_rows_along_n ? 1u << 16 : 0u) | static_cast<uint32_t>(n / 8) << 17 | (128u / 16) << 24;
-}
-__device__ __forceinline__ void mma_shared(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add)
-{
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(static_cast<uint32_t>(add)) : "memory");
-}
-__device__ __forceinline__ void mma_tensor(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool add)
-{
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(static_cast<uint32_t>(add)) : "memory");
-}
-// Arrives at the barrier when all products issued so far by this thread are done.
-__device__ __forceinline__ void commit_to(uint32_t bar) { asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory"); }
-
-#define TC_R8(r, o) "=r"(r[o]), "=r"(r[o + 1]), "=r"(r[o + 2]), "=r"(r[o + 3]), "=r"(r[o + 4]), "=r"(r[o + 5]), "=r"(r[o + 6]), "=r"(r[o + 7])
-#define TC_W8(r, o) "r"(r[o]), "r"(r[o + 1]), "r"(r[o + 2]), "r"(r[o + 3]), "r"(r[o + 4]), "r"(r[o + 5]), "r"(r[o + 6]), "r"(r[o + 7])
-// 32 columns of this thread's lane.  The registers hold them after tensor_loaded().
-__device__ __forceinline__ void tensor_load32(uint32_t addr, uint32_t (&r)[32])
-{
-    asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
-                 : TC_R8(r, 0), TC_R8(r, 8), TC_R8(r, 16), TC_R8(r, 24) : "r"(addr));
-}
-__device__ __forceinline__ void tensor_load16(uint32_t addr, uint32_t (&r)[16])
-{
-    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];" : TC_R8(r, 0), TC_R8(r, 8) : "r"(addr));
-}
-__device__ __forceinline__ void tensor_store16(uint32_t addr, const uint32_t (&r)[16])
-{
-    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15};" ::TC_W8(r, 0), TC_W8(r, 8), "r"(addr) : "memory");
-}
-__device__ __forceinline__ void tensor_store8(uint32_t addr, const uint32_t (&r)[8])
-{
-    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%8], {%0,%1,%2,%3,%4,%5,%6,%7};" ::TC_W8(r, 0), "r"(addr) : "memory");
-}
-__device__ __forceinline__ void tensor_loaded() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
-__device__ __forceinline__ void tensor_stored() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-__device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void fence_shared_to_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
-
-// One lane of a converged warp.
-__device__ __forceinline__ bool elected()
-{
-    uint32_t yes;
-    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(yes));
-    return yes != 0;
-}
-
-// Byte of element d of row r in a swizzled tile of 128 rows: columns of 64 elements, 128 bytes a row, the
-// 16-byte chunks of a row permuted by its place in its group of eight.
-__device__ __forceinline__ uint32_t swizzled(int r, int chunk) { return (chunk >> 3) * (kTile * 128) + r * 128 + (((chunk & 7) ^ (r & 7)) << 4); }
-
-__device__ __forceinline__ float larger3(float a, float b, float c)
-{
-    float r;
-    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
-    return r;
-}
-__device__ __forceinline__ float2 fused2(float2 a, float2 b, float2 c)
-{
-    float2 r;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;"
-        : "=l"(reinterpret_cast<uint64_t &>(r)) : "l"(reinterpret_cast<uint64_t &>(a)), "l"(reinterpret_cast<uint64_t &>(b)), "l"(reinterpret_cast<uint64_t &>(c)));
-    return r;
-}
-__device__ __forceinline__ float2 sum2(float2 a, float2 b)
-{
-    float2 r;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(reinterpret_cast<uint64_t &>(r)) : "l"(reinterpret_cast<uint64_t &>(a)), "l"(reinterpret_cast<uint64_t &>(b)));
-    return r;
-}
-__device__ __forceinline__ float4 load_shared_f4(uint32_t addr)
-{
-    float4 v;
-    asm volatile("ld.shared.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr));
-    return v;
-}
-
-struct RowState {
-    float top, ref, sum;
-};
-
-// Rare: scales of V so far apart that what is next to nothing among the probabilities can be much of the sum.
-// Each key has its own power of two here, and the sum exponentials of its own; the scores
-// stay in tensor memory and are gone through twice, 16 at a time.  False when a wait ran out.  A function of its
-// own: in line, never run, it slowed the other tiles (512 requests behind 4000 e4m3 147 -> 150 us a call).
-template <int DP>
-__device__ __noinline__ bool far_tile(RowState &state, uint32_t s_at, uint32_t p_at, uint32_t o_at, uint32_t about, float factor, uint32_t o_added, int mine)
-{
-    constexpr float kLift = probability_lift<__half>();
-    float highest = -INFINITY, most = -INFINITY, base = 0.f, m = 0.f, sum = state.sum;
-#pragma unroll 1
-    for (int pass = 0; pass < 2; pass++) {
-        if (pass) {
-            const float ref = fmaxf(state.ref, highest);
-            base = ref == -INFINITY ? 0.f : ref;
-            sum *= exp2_approx(state.ref - base);
-            state.ref = ref;
-            const float to = fmaxf(state.top, most), f = to == state.top ? 1.f : exp2_approx(state.top - to);
-            state.top = to;
-            m = to == -INFINITY ? 0.f : to - kLift;
-            if (mine) {
-                if (!__all_sync(0xffffffffu, barrier_wait(o_added, (mine - 1) & 1))) return false;
-                fence_after();
-#pragma unroll 1
-                for (int c = 0; c < DP / 16; c++) {
-                    uint32_t v[16];
-                    tensor_load16(o_at + 16 * c, v);
-                    tensor_loaded();
-#pragma unroll
-                    for (int i = 0; i < 16; i++) v[i] = __float_as_uint(__uint_as_float(v[i]) * f);
-                    tensor_store16(o_at + 16 * c, v);
-                }
-            }
-        }
-#pragma unroll 1
-        for (int c = 0; c < 8; c++) {
-            uint32_t v[16], w[8], here;
-            tensor_load16(s_at + 16 * c, v);
-            asm volatile("ld.shared.u32 %0, [%1];" : "=r"(here) : "r"(about + 4 * (c >> 1)));
-            here >>= 16 * (c & 1);
-            tensor_loaded();
-#pragma unroll
-            for (int i = 0; i < 16; i += 4) {
-                const float4 k4 = load_shared_f4(about + 64 + 4 * (16 * c + i));
-                const float4 e4 = load_shared_f4(about + 64 + 4 * kTile + 4 * (16 * c + i));
-                const float k[4] = {k4.x, k4.y, k4.z, k4.w}, e[4] = {e4.x, e4.y, e4.z, e4.w};
-                float x[4];
-#pragma unroll
-                for (int j = 0; j < 4; j++) {
-                    x[j] = here >> (i + j) & 1 ? __uint_as_float(v[i + j]) * (factor * k[j]) : -INFINITY;
-                    if (!pass) {
-                        highest = fmaxf(highest, x[j]), most = fmaxf(most, x[j] + e[j]);
-                    } else {
-                        sum += exp2_approx(x[j] - base);
-                        x[j] = exp2_approx(x[j] + e[j] - m);
-                    }
-                }
-                w[i / 2] = pack2<__half>(x[0], x[1]), w[i / 2 + 1] = pack2<__half>(x[2], x[3]);
-            }
-            if (pass) tensor_store8(p_at + 8 * c, w);
-        }
-    }
-    state.sum = sum;
-    return true;
-}
 
 // T: the type of the products, fp16 for codes.
 template <typename T, int KIND, int DP, bool TWO>
@@ -351,7 +193,7 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_kernel(const __grid_
             if constexpr (KIND != kPlain) {
                 if (far) {
                     RowState state{top, ref, sum.x + sum.y};
-                    fine = far_tile<DP>(state, s_at, p_at, o_at, about, factor, o_added + 8 * slot, mine);
+                    fine = far_tile<DP, kTile>(state, s_at, p_at, o_at, make_uint4(mask[0], mask[1], mask[2], mask[3]), about + 64, factor, o_added + 8 * slot, (mine - 1) & 1, mine > 0);
                     top = state.top, ref = state.ref, sum = make_float2(state.sum, 0.f);
                     if (!fine) break;
                     tensor_stored();

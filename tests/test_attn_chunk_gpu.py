@@ -1,0 +1,32 @@
+"""tc_attn_chunk against 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2608_06007_b200 as tc
+from attn_chunk import batch, check_chunk, run_chunk
+from test_operators_gpu import status_is
+
+pytestmark = pytest.mark.gpu
+
+TYPES = [("bf16", "bf16"), ("fp16", "fp16"), ("bf16", "e4m3"), ("fp16", "int8")]
+WINDOWS = [(0, 0), (1, 0), (33, 4), (200, 1), (128, 300)]
+
+
+@pytest.mark.parametrize("x,kind", TYPES)
+@pytest.mark.parametrize("window,sinks", WINDOWS)
+def test_a_few_requests(x, kind, window, sinks):
+    s = batch(kind, x, [37, 100, -1, 5, 200, 64], [7, 100, 3, 1, 13, 0], Hq=8, window=window, sinks=sinks, front=2, behind=3)
+    run_chunk(s)
+    check_chunk(s)
+    status_is(0)
+
+
+@pytest.mark.parametrize("x,kind", TYPES + [("fp16", "e4m3"), ("bf16", "int8")])
+@pytest.mark.parametrize("D,H,g,B,layout", [(128, 2, 4, 16, "nhd"), (64, 1, 1, 5, "hnd"), (80, 3, 7, 16, "hnd"), (256, 1, 20, 8, "nhd"), (16, 2, 16, 1, "nhd"), (192, 1, 3, 32, "hnd"), (112, 2, 17, 7, "nhd")])
+def test_types_and_shapes(x, kind, D, H, g, B, layout):
+    for window, sinks in ((0, 0), (70, 3)):
+        s = batch(kind, x, [300, 1, 129, 128], [150, 1, 40, 128], Hq=H * g, H=H, D=D, B=B, layout=layout, window=window, sinks=sinks, gap=32)
+        run_chunk(s)
+        check_chunk(s)
+    status_is(0)

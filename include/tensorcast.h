@@ -575,6 +575,11 @@ typedef struct {
 TC_API int tc_attn_workspace(const tc_kv_layer_t *layer, const tc_attn_decode_t *args, int64_t *bytes);
 TC_API int tc_attn_decode(const tc_kv_layer_t *layer, const tc_attn_decode_t *args, void *stream);
 
+/* tc_attn_decode over the keys j >= lens[r] - window and j < sinks alone (window >= 1, sinks >= 0): a request's last tokens and
+ * its first ones, which stay visible however long it grows.  Slots of other tokens are never read, so that their blocks may be given
+ * back; the table's entries for them may be anything.  There is no shared prefix (max_prefix = 0).  The workspace is tc_attn_workspace's for the same args. */
+TC_API int tc_attn_decode_window(const tc_kv_layer_t *layer, const tc_attn_decode_t *args, int64_t window, int64_t sinks, void *stream);
+
 /* Chunks of new tokens - pieces of prompts, whole prompts, tokens guessed ahead, single ones, any of them side by side - over a
  * paged cache that holds the new tokens already (tc_kv_append).  Rows offsets[r] .. offsets[r+1] of q and out are request
  * r's new tokens, the last n = offsets[r+1] - offsets[r] of the lens[r] that its table holds: row i of them is at position

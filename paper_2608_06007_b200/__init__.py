@@ -8,6 +8,6 @@ from .binding import (  # noqa: F401
     TensorCastError, kv_spec, load_library, pool, tc_kv_pack, tc_kv_unpack, tc_plan_create,
     tc_plan_descriptors, tc_plan_destroy, tc_plan_stats, tc_device_status, tc_selftest_wait_timeout, tc_plan_check_device, TC_PLAN_DEBUG_BOUNDS, TC_DEVICE_OUT_OF_BOUNDS, TC_DEVICE_BULK_WAIT_TIMEOUT, tc_weights_materialize, weights_spec,
     TC_BF16, TC_FP16, TC_FP32, TC_E4M3, TC_INT8, TC_ROPE_INTERLEAVED, TC_DEVICE_BAD_INDEX, KVLayer, kv_layer, tc_kv_append, tc_kv_gather, tc_attn_decode,
-    tc_attn_workspace_bytes, tc_attn_chunk, tc_attn_chunk_workspace_bytes,
+    tc_attn_workspace_bytes, tc_attn_chunk, tc_attn_chunk_workspace_bytes, tc_attn_decode_window,
 )
 from .build import build_library  # noqa: F401

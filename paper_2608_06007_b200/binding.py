@@ -148,7 +148,7 @@ EXPORTS = ("tc_plan_create", "tc_kv_pack", "tc_kv_unpack", "tc_weights_materiali
            "tc_plan_destroy", "tc_plan_stats", "tc_plan_descriptors", "tc_strerror", "tc_last_error",
            "tc_kv_pack_noalloc", "tc_weights_materialize_checksum", "tc_trim",
            "tc_weights_materialize_file", "tc_plan_segments", "tc_device_status", "tc_selftest_wait_timeout", "tc_plan_check_device",
-           "tc_kv_append", "tc_kv_gather", "tc_attn_decode", "tc_attn_workspace", "tc_attn_chunk", "tc_attn_chunk_workspace")
+           "tc_kv_append", "tc_kv_gather", "tc_attn_decode", "tc_attn_workspace", "tc_attn_chunk", "tc_attn_chunk_workspace", "tc_attn_decode_window")
 
 _lib = None
 
@@ -187,6 +187,8 @@ def load_library(path: str | None = None):
     for name in ("tc_kv_append", "tc_kv_gather", "tc_attn_decode", "tc_attn_chunk"):
         getattr(lib, name).argtypes = [C.POINTER(tc_kv_layer_t), vp, vp]  # the second: a packed struct as bytes, or byref(args)
         getattr(lib, name).restype = C.c_int
+    lib.tc_attn_decode_window.argtypes = [C.POINTER(tc_kv_layer_t), vp, C.c_int64, C.c_int64, vp]
+    lib.tc_attn_decode_window.restype = C.c_int
     lib.tc_attn_workspace.argtypes = [C.POINTER(tc_kv_layer_t), C.POINTER(tc_attn_decode_t), C.POINTER(C.c_int64)]
     lib.tc_attn_workspace.restype = C.c_int
     lib.tc_attn_chunk_workspace.argtypes = [C.POINTER(tc_kv_layer_t), C.POINTER(tc_attn_chunk_t), C.POINTER(C.c_int64)]
@@ -599,6 +601,15 @@ def tc_kv_gather(layer: KVLayer, tables, offsets, k_out=None, v_out=None, *, fir
         _check(rc)
 
 
+def _lse(lse, n, heads):
+    """Address of the fp32 [n, heads] that logarithms go to; 0 for None."""
+    if lse is None:
+        return 0
+    if lse.shape != (n, heads) or _dtypes.get(lse.dtype) != (TC_FP32, 4) or not lse.is_contiguous():
+        raise ValueError(f"lse must be a contiguous fp32 [{n}, {heads}]")
+    return lse.data_ptr()
+
+
 def tc_attn_workspace_bytes(layer: KVLayer, q, *, max_len, max_prefix=0) -> int:
     """Bytes of workspace that tc_attn_decode needs for queries of this shape and these bounds.  Fewer requests may need
     more: a program whose batch varies takes the largest over its sizes."""
@@ -618,9 +629,7 @@ def tc_attn_decode(layer: KVLayer, q, out, tables, lens, *, max_len, workspace, 
     o0, o1 = _rows("out", out, R, Hq, D, dtype, e)
     lse_at = table = width = step = prefix_at = prefix_len_at = 0
     if lse is not None:
-        if lse.shape != (R, Hq) or _dtypes.get(lse.dtype) != (TC_FP32, 4) or not lse.is_contiguous():
-            raise ValueError("lse must be a contiguous fp32 [R, Hq]")
-        lse_at = lse.data_ptr()
+        lse_at = _lse(lse, R, Hq)
     if max_len:
         table, width, step = _matrix("tables", tables, R)
     if max_prefix:
@@ -633,13 +642,20 @@ def tc_attn_decode(layer: KVLayer, q, out, tables, lens, *, max_len, workspace, 
         _check(rc)
 
 
-def _lse(lse, n, heads):
-    """Address of the fp32 [n, heads] that logarithms go to; 0 for None."""
-    if lse is None:
-        return 0
-    if lse.shape != (n, heads) or _dtypes.get(lse.dtype) != (TC_FP32, 4) or not lse.is_contiguous():
-        raise ValueError(f"lse must be a contiguous fp32 [{n}, {heads}]")
-    return lse.data_ptr()
+def tc_attn_decode_window(layer: KVLayer, q, out, tables, lens, *, window, sinks=0, max_len, workspace, scale=0.0, lse=None, stream=None) -> None:
+    """tc_attn_decode of q ([R, Hq, D]) over the last `window` and the first `sinks` of the lens[r] tokens of tables[r] alone.  The workspace is
+    tc_attn_workspace_bytes' for the same max_len."""
+    code, e = _dtype(q)
+    dtype, D = q.dtype, layer.D
+    R, Hq = q.shape[0], q.shape[1]
+    q0, q1 = _rows("q", q, R, Hq, D, dtype, e)
+    o0, o1 = _rows("out", out, R, Hq, D, dtype, e)
+    table, width, step = _matrix("tables", tables, R) if max_len else (0, 0, 0)
+    args = _DECODE.pack(_DECODE.size, code, R, Hq, q.data_ptr(), out.data_ptr(), q0, q1, o0, o1, _lse(lse, R, Hq), scale, 0, table, width, step, _vector("lens", lens, R, 4), max_len,
+                        0, 0, 0, workspace.data_ptr(), workspace.numel() * workspace.element_size())
+    rc = (_lib or load_library()).tc_attn_decode_window(layer.ref, args, window, sinks, None if stream is None else _stream(stream))
+    if rc:
+        _check(rc)
 
 
 def tc_attn_chunk_workspace_bytes(layer: KVLayer, q, R, *, max_new, max_len, window=0, sinks=0) -> int:

@@ -17,6 +17,7 @@ struct AttnParams {
     int64_t table_width, table_stride;
     const int32_t *lens, *prefix_table, *prefix_len;
     int64_t R, max_len, max_prefix;
+    int32_t window, sinks;  // keys at the end, and at the front, that a row sees; window 0: all
     int32_t Hq, q_bf16;
     float scale_log2;  // scale * log2(e)
     FastDiv div_block, div_group, div_heads;
@@ -28,5 +29,7 @@ struct AttnParams {
 
 // attn_prefix.cu: the prefix parts of splits whose prefix_rows is 128 or 256
 int launch_prefix(const AttnParams &p, int dtype, int device, cudaStream_t s);
+// attn_window.cu: a call with a window
+int launch_window(const AttnParams &p, int dtype, int device, cudaStream_t s);
 
 }  // namespace tc

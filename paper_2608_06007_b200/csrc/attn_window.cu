@@ -1,0 +1,12 @@
+// tc_attn_decode_window: one query token per request over its last tokens and its first ones.  The keys that it sees are two runs, so
+// the stream's tiles are those of both, one behind the other, and all else is as without a window (attn_stream.cuh).
+#include "attn_stream.cuh"
+
+namespace tc {
+
+int launch_window(const AttnParams &p, int dtype, int device, cudaStream_t s)
+{
+    return dtype == TC_BF16 ? launch_stream_and_join<__nv_bfloat16, true>(p, device, s) : launch_stream_and_join<__half, true>(p, device, s);
+}
+
+}  // namespace tc

@@ -112,3 +112,42 @@ def check_chunk(s, only=None, left_out=()):
         rows_off(s, r, row0, m, keys, vals, 3)
     out, lse = np64(s["out"]), np64(s["lse"])
     assert (out[~mine] == 9.0).all() and (lse[~mine] == 9.0).all()
+
+
+def window_batch(kind, x, lens, **more):
+    """One query token per request: a batch whose rows of q are the requests', padding among them."""
+    s = batch(kind, x, lens, [1 if n > 0 else 0 for n in lens], **more)
+    Hq, D, R = s["q"].shape[1], s["pool"].D, len(lens)
+    rng = np.random.default_rng(R)
+    s["q"] = torch.from_numpy(rng.standard_normal((R, Hq, D)).astype(np.float32) * more.get("spread", 1.0)).to(TORCH[x])
+    if more.get("strided"):
+        s["dq"] = torch.zeros(Hq, R, D + 16, dtype=s["q"].dtype, device="cuda").transpose(0, 1)[..., :D]
+        s["dq"].copy_(s["q"])
+        s["out"] = torch.full((Hq, R, D + 8), 9.0, dtype=s["q"].dtype, device="cuda").transpose(0, 1)[..., :D]
+    else:
+        s["dq"], s["out"] = s["q"].cuda(), torch.full((R, Hq, D), 9.0, dtype=s["q"].dtype, device="cuda")
+    s["lse"] = torch.full((R, Hq), 9.0, device="cuda")
+    s["offsets"] = np.arange(R + 1)
+    del s["d"]["offsets"]
+    return s
+
+
+def run_window(s, workspace=None, **changes):
+    pool = s["pool"]
+    if workspace is None:
+        workspace = torch.full((tc.tc_attn_workspace_bytes(pool.handle, s["dq"], max_len=s["max_len"]),), 0xFF, dtype=torch.uint8, device="cuda")
+    args = dict(window=s["window"], sinks=s["sinks"], max_len=s["max_len"], scale=s["scale"], lse=s["lse"], workspace=workspace) | s["d"] | changes
+    tc.tc_attn_decode_window(pool.handle, s["dq"], s["out"], **args)
+
+
+def check_window(s, only=None):
+    pool = s["pool"]
+    out, lse = np64(s["out"]), np64(s["lse"])
+    for r, n in enumerate(s["lens"]):
+        if n < 0:
+            assert (out[r] == 9.0).all() and (lse[r] == 9.0).all()
+        elif n == 0:
+            assert (out[r] == 0).all() and (lse[r] == -np.inf).all()
+        elif only is None or r in only:
+            keys, vals = (tokens_of(v, s["table"][r], 0, n, pool.B) for v in s["values"])
+            rows_off(s, r, r, 1, keys, vals, 1)

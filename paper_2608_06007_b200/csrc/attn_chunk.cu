@@ -11,7 +11,7 @@ int launch_chunk_plain(const ChunkParams &p, int dtype, int device, cudaStream_t
 }
 
 // The parts' outputs, each by its share of the whole sum.  A warp takes a row; a lane finds the weights of up to four parts,
-// then the warp reads the outputs of four parts at once.  Where nothing was cut it ends after a look at `base`.
+// then the warp reads the outputs of four parts at once.  Where nothing was cut it ends after a look at `cuts`.
 constexpr float kLess = 12.f;  // weights are 2^-12 at most: the outputs of up to that many parts may be next to the largest number
 static_assert(kChunkMostParts <= 128);
 template <typename T, int DP>
@@ -21,16 +21,16 @@ __global__ void __launch_bounds__(128) chunk_join_kernel(const __grid_constant__
     const int lane = threadIdx.x & 31, D = p.layer.D;
     const int64_t first_warp = blockIdx.x * 4ll + (threadIdx.x >> 5), warps = gridDim.x * 4ll;
     await_last();
-    const int32_t share = static_cast<int32_t>(p.base[0]);
-    if (share >= (1 << 30)) return;
     for (int64_t r0 = 0; r0 < p.R; r0 += 32) {
-        const uint32_t mine = r0 + lane < p.R ? p.base[4 + r0 + lane] : kUncut;
-        for (uint32_t some = __ballot_sync(0xffffffffu, mine != kUncut); some; some &= some - 1) {
+        const ChunkRequest mine = r0 + lane < p.R ? chunk_request(p, r0 + lane, false) : ChunkRequest{0, 0, 0};
+        const uint2 cut = mine.n ? p.cuts[r0 + lane] : make_uint2(0, 0);
+        // (where a call's kernel gave up, or offsets made more items than its grid holds, nobody may have said)
+        const bool said = cut.y > 1 && cut.y <= kChunkMostParts && cut.x + static_cast<int64_t>(cut.y) * mine.n * p.Hq <= p.plan.part_rows;
+        for (uint32_t some = __ballot_sync(0xffffffffu, said); some; some &= some - 1) {
             const int who = __ffs(some) - 1;
-            const uint32_t base = __shfl_sync(0xffffffffu, mine, who);
-            const ChunkRequest q = chunk_request(p, r0 + who, false);
-            const int32_t parts = chunk_parts(chunk_tiles(p.shape, q.len), share);
-            const int64_t rows = static_cast<int64_t>(q.n) * p.Hq;
+            const uint32_t base = __shfl_sync(0xffffffffu, cut.x, who);
+            const int32_t parts = static_cast<int32_t>(__shfl_sync(0xffffffffu, cut.y, who));
+            const int64_t rows = static_cast<int64_t>(__shfl_sync(0xffffffffu, mine.n, who)) * p.Hq, token0 = __shfl_sync(0xffffffffu, mine.token0, who);
             for (int64_t row = first_warp; row < rows; row += warps) {
                 const int64_t token = row / p.Hq, head = row - token * p.Hq;
                 float sum[4], top = -INFINITY, all = 0.f, acc[4 * kVectors] = {};
@@ -69,12 +69,12 @@ __global__ void __launch_bounds__(128) chunk_join_kernel(const __grid_constant__
                     }
                 }
                 const float inv = all == 0.f ? 0.f : 1.f / all;
-                char *const dst = p.out + (q.token0 + token) * p.out_token + head * p.out_head;
+                char *const dst = p.out + (token0 + token) * p.out_token + head * p.out_head;
 #pragma unroll
                 for (int x = 0; x < kVectors; x++)
                     if (lane * 4 + 128 * x < D)
                         *reinterpret_cast<uint2 *>(dst + (lane * 4 + 128 * x) * 2) = make_uint2(pack2<T>(acc[4 * x] * inv, acc[4 * x + 1] * inv), pack2<T>(acc[4 * x + 2] * inv, acc[4 * x + 3] * inv));
-                if (p.lse && lane == 0) p.lse[q.token0 * p.Hq + row] = all == 0.f ? -INFINITY : ((top == -INFINITY ? 0.f : top) + kLess + log2f(all)) * kChunkLn2;
+                if (p.lse && lane == 0) p.lse[token0 * p.Hq + row] = all == 0.f ? -INFINITY : ((top == -INFINITY ? 0.f : top) + kLess + log2f(all)) * kChunkLn2;
             }
         }
     }
@@ -186,7 +186,7 @@ extern "C" int tc_attn_chunk(const tc_kv_layer_t *layer, const tc_attn_chunk_t *
     p.div_block = make_fastdiv(p.layer.B);
     p.div_group = make_fastdiv(static_cast<uint32_t>(p.shape.group));
     char *const ws = static_cast<char *>(a->workspace);
-    p.base = reinterpret_cast<uint32_t *>(ws + p.plan.base_at);
+    p.cuts = reinterpret_cast<uint2 *>(ws + p.plan.cuts_at);
     p.sums = reinterpret_cast<float *>(ws + p.plan.sums_at);
     p.parts = reinterpret_cast<float *>(ws + p.plan.parts_at);
     cudaStream_t s = static_cast<cudaStream_t>(stream);

@@ -222,17 +222,6 @@ __global__ void __launch_bounds__(kChunkThreads, 1) chunk_kernel(const __grid_co
             total += warp_items[w];
         }
         items_before[threadIdx.x] = upto - my_items, rows_before[threadIdx.x] = rows_upto - my_rows;
-        if (blockIdx.x == 0 && p.plan.part_rows) {
-            // for join_kernel
-            if (threadIdx.x == 0) p.base[0] = share;
-            uint32_t at = rows_upto - my_rows;
-            for (int64_t r = run0; r < run1; r++) {
-                const ChunkRequest q = chunk_request(p, r, false);
-                const int32_t parts = q.n ? chunk_parts(chunk_tiles(shape, q.len), share) : 0;
-                p.base[4 + r] = parts > 1 ? at : kUncut;
-                if (parts > 1) at += static_cast<uint32_t>(q.n) * p.Hq * parts;
-            }
-        }
     }
     fence_before();
     __syncthreads();
@@ -935,6 +924,8 @@ __global__ void __launch_bounds__(kChunkThreads, 1) chunk_kernel(const __grid_co
                         item.end = static_cast<int32_t>(min(static_cast<int64_t>(item.begin) + share, static_cast<int64_t>(item.list.count)));
                         item.part_row = parts > 1 ? rows_at + static_cast<uint32_t>(part) * q.n * p.Hq : kUncut;
                         item.token0 = q.token0, item.n = q.n, item.pad = 0;
+                        // for chunk_join_kernel, by whoever has the request's first item
+                        if (p.plan.part_rows && id == at && lane == 0) p.cuts[r] = make_uint2(rows_at, static_cast<uint32_t>(parts));
                         break;
                     }
                     if (item.valid) {

@@ -23,7 +23,7 @@ struct ChunkParams {
     FastDiv div_block, div_group;
     ChunkShape shape;
     ChunkPlan plan;
-    uint32_t *base;  // {share, 0, 0, 0}, then for every request the first of its parts' rows, kUncut where it is not cut
+    uint2 *cuts;  // of every request that has items: the first of its parts' rows, and the number of its parts
     float *sums, *parts;
     unsigned int *status;
 };

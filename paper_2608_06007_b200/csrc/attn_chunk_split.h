@@ -100,11 +100,11 @@ TC_HD float chunk_cost(int64_t items, int64_t split, int64_t tiles, int32_t long
     return all > static_cast<float>(longest) ? all : static_cast<float>(longest);
 }
 
-// What the host can say of a call: its grid, and its workspace: {share, R words of `base`} then sums and outputs of the parts' rows.
+// What the host can say of a call: its grid, and its workspace: R pairs of words, then sums and outputs of the parts' rows.
 struct ChunkPlan {
     int64_t grid;       // items at most
     int64_t part_rows;  // rows of parts at most; 0: nothing is cut
-    int64_t base_at, sums_at, parts_at, workspace;
+    int64_t cuts_at, sums_at, parts_at, workspace;
 };
 inline void plan_chunk(const ChunkShape &s, int64_t R, int64_t n_tokens, int64_t max_new, int64_t max_len, int64_t D, ChunkPlan *p)
 {
@@ -124,7 +124,7 @@ inline void plan_chunk(const ChunkShape &s, int64_t R, int64_t n_tokens, int64_t
         p->workspace += (bytes + 255) / 256 * 256;
         return at;
     };
-    p->base_at = place((R + 4) * 4);
+    p->cuts_at = place(R * 8);
     p->sums_at = place(p->part_rows * 4);
     p->parts_at = place(p->part_rows * D * 4);
 }

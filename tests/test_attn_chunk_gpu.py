@@ -30,3 +30,14 @@ def test_types_and_shapes(x, kind, D, H, g, B, layout):
         run_chunk(s)
         check_chunk(s)
     status_is(0)
+
+
+@pytest.mark.parametrize("x,kind", TYPES)
+@pytest.mark.parametrize("lens,new,D,window,sinks", [([4000], [5], 128, 0, 0), ([1500, 20, 2600], [40, 3, 1], 128, 0, 0), ([9000], [1], 64, 0, 0), ([1300, 700], [9, 2], 256, 0, 0), ([6000], [33], 128, 3000, 500)])
+def test_long_keys_of_few_rows_are_cut_into_parts(x, kind, lens, new, D, window, sinks):
+    s = batch(kind, x, lens, new, Hq=8, D=D, window=window, sinks=sinks)
+    for _ in range(3):
+        s["out"].fill_(9.0), s["lse"].fill_(9.0)
+        run_chunk(s)  # each on a workspace of 0xFF
+        check_chunk(s)
+    status_is(0)

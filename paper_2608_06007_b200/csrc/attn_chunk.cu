@@ -89,6 +89,42 @@ static int launch_chunk(const ChunkParams &p, int dtype, int device, cudaStream_
     return p.layer.D <= 128 ? launch_attn(chunk_join_kernel<T, 128>, grid, 128, 0, true, p, s) : launch_attn(chunk_join_kernel<T, 256>, grid, 128, 0, true, p, s);
 }
 
+// Pages as tensors [block][head][token][d]: where tiles are whole numbers of blocks, or blocks of tiles, so that a
+// box of a page's tokens is part of one tile.  Elsewhere box_rows stays 0.
+static int describe_pages(ChunkParams *p)
+{
+    p->box_rows = 0;
+    const Layer &l = p->layer;
+    const bool codes = l.quantised();
+    const int32_t keys = p->shape.keys, most = codes ? keys : keys / 2;  // of an unquantised tile, two warps fetch half each
+    const int32_t rows = static_cast<int32_t>(std::min<int64_t>(l.B, most));
+    if (rows < 8 || most % rows || l.B % rows || l.num_blocks < 1 || l.geo.block >= (1ll << 40)) return TC_OK;
+    using Encode = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *, const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+    static std::atomic<Encode> known;  // looked up once; twice does no harm
+    Encode encode = known.load(std::memory_order_relaxed);
+    if (!encode) {
+        void *f = nullptr;
+        cudaDriverEntryPointQueryResult found;
+        const cudaError_t e = cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &found);
+        if (e != cudaSuccess) return cuda_fail(e, "cudaGetDriverEntryPointByVersion(cuTensorMapEncodeTiled)");
+        if (found != cudaDriverEntryPointSuccess || !f) return fail(TC_ERR_CUDA, "the driver has no cuTensorMapEncodeTiled");
+        encode = reinterpret_cast<Encode>(f);
+        known.store(encode, std::memory_order_relaxed);
+    }
+    const CUtensorMapDataType type = codes ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : l.dtype == TC_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
+    const cuuint64_t extent[4] = {static_cast<cuuint64_t>(l.D), l.B, static_cast<cuuint64_t>(l.H), static_cast<cuuint64_t>(l.num_blocks)};
+    const cuuint64_t stride[3] = {static_cast<cuuint64_t>(l.geo.token), static_cast<cuuint64_t>(l.geo.head), static_cast<cuuint64_t>(l.geo.block)};
+    const cuuint32_t padded = l.D <= 64 ? 64 : l.D <= 128 ? 128 : 256, box[4] = {codes ? padded : 64, static_cast<cuuint32_t>(rows), 1, 1}, step[4] = {1, 1, 1, 1};
+    for (int v = 0; v < 2; v++)
+        if (encode(v ? &p->map_v : &p->map_k, type, 4, v ? l.v : l.k, extent, stride, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, codes ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B,
+                   CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+            return TC_OK;  // a geometry that tensor maps do not hold
+    p->box_rows = rows;
+    p->div_box = make_fastdiv(static_cast<uint32_t>(rows));
+    return TC_OK;
+}
+
 // What both entry points check; fills p's geometry and plan.
 static int check_chunk(const tc_kv_layer_t *layer, const tc_attn_chunk_t *a, ChunkParams *p)
 {
@@ -185,6 +221,7 @@ extern "C" int tc_attn_chunk(const tc_kv_layer_t *layer, const tc_attn_chunk_t *
     p.scale_log2 = static_cast<float>((a->scale != 0.f ? static_cast<double>(a->scale) : 1.0 / std::sqrt(static_cast<double>(p.layer.D))) * 1.4426950408889634);
     p.div_block = make_fastdiv(p.layer.B);
     p.div_group = make_fastdiv(static_cast<uint32_t>(p.shape.group));
+    if ((rc = describe_pages(&p)) != TC_OK) return rc;
     char *const ws = static_cast<char *>(a->workspace);
     p.cuts = reinterpret_cast<uint2 *>(ws + p.plan.cuts_at);
     p.sums = reinterpret_cast<float *>(ws + p.plan.sums_at);

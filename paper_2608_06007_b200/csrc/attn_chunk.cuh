@@ -9,25 +9,37 @@
 
 namespace tc {
 
-constexpr int kChunkThreads = 512;  // 128 registers each; the softmax's 256 take 192, the others keep 64
-constexpr int kChunkInfos = 4;      // tiles whose masks and scales are kept
 constexpr float kChunkLn2 = 0.6931471805599453f;
+
+// A CTA's warps: eight of softmax, those that fetch pages (codes: four for K and four for V), then four that issue products and find items.
+template <int KIND> struct ChunkWarps {
+    static constexpr int softmax = 8, loaders = KIND == kPlain ? 4 : 8, all = softmax + loaders + 4, threads = 32 * all;
+    // registers of a thread: at the launch, of the softmax, of the others
+    static constexpr int launch_registers = KIND == kPlain ? 128 : 96, softmax_registers = KIND == kPlain ? 192 : 168, other_registers = KIND == kPlain ? 64 : 48;
+    static_assert(32 * softmax * softmax_registers + (threads - 32 * softmax) * other_registers <= threads * launch_registers && threads * launch_registers <= 65536, "a split that never ends");
+};
 
 template <int KIND, int DP>
 struct ChunkMemory {
     static constexpr int slots = DP > 128 ? 1 : 2, keys = DP > 128 ? 64 : 128;
     static constexpr int tile = keys * DP * 2, q_tile = 128 * DP * 2;  // bytes
     static constexpr int queries = slots * q_tile;
-    static constexpr int codes = KIND == kPlain ? 0 : keys * DP, staged = KIND == kPlain ? 0 : 3;
-    static constexpr int stages = KIND == kPlain ? (DP == 64 ? 6 : 4) : (DP == 64 ? 4 : 3);
-    // {mask, 4 words; whether V has numbers that are not finite, a word a warp}; codes: V's exponent, whether scales are far apart; each
-    // warp's largest and smallest; scales of K; keys' exponents
-    static constexpr int info = KIND == kPlain ? 32 : 80 + 8 * keys, scales = 80;
+    static constexpr int stages = KIND == kPlain ? (DP == 64 ? 6 : 4) : (DP == 64 ? 4 : 3);  // K and V in turn
+    // A copy's barriers: K and V have their own warps, which must not share a barrier, since neither sees all of the other's phases.
+    static constexpr int turns = stages % 2 ? 2 * stages : stages;
+    // tiles as they lie in the pool, and the barriers of those
+    static constexpr int codes = KIND == kPlain ? 0 : keys * DP, staged = KIND == kPlain ? 0 : 3, staged_turns = 6;
+    // Tiles whose masks and scales are kept: those of a tile must not be replaced before its last product is issued, and
+    // K and V have their own warps, of which K's may be four tiles ahead.
+    static constexpr int infos = 8;
+    // {mask, 4 words; whether V has numbers that are not finite, up to 4 words}; codes: V's exponent, whether scales are far apart; each
+    // warp's largest and smallest of V's scales, for K's warps and for V's; scales of K; keys' exponents
+    static constexpr int info = KIND == kPlain ? 32 : 112 + 8 * keys, scales = 112;
     // powers of two taken out of the queries, of four items where scores run two ahead (one slot), of two elsewhere
     static constexpr int down_sets = 4 / slots, downs = KIND == kPlain ? 0 : 4 * 128 * 4;
-    static constexpr int table = 2 * kChunkThreads * 4;                      // items, and rows of parts, before each thread's requests
+    static constexpr int table = 2 * ChunkWarps<KIND>::threads * 4;  // items, and rows of parts, before each thread's requests
     static constexpr int item = 80;
-    static constexpr int rest = kChunkInfos * info + downs + table + 2 * item + 16 + 512;
+    static constexpr int rest = infos * info + downs + table + 2 * item + 16 + 512;
     // more than half of an SM's, so that no two CTAs meet on one: the second would wait for tensor memory with an item in hand
     static constexpr int least = 120 * 1024;
     static constexpr int used = queries + stages * tile + staged * codes + rest + 1024;
@@ -68,13 +80,34 @@ template <typename T> __device__ __forceinline__ uint32_t not_finite(uint32_t w)
     return ((w & exponent) + last) & 0x80008000u;
 }
 
+constexpr int32_t kNoKey = INT32_MIN;  // no entry of a table
+
+// A box of a tensor map's tokens t .. of one head and block, elements x .. , to shared memory.
+__device__ __forceinline__ void copy_box(uint32_t dst, const CUtensorMap *map, int x, int t, int h, int block, uint32_t bar)
+{
+    asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
+                 ::"r"(dst), "l"(map), "r"(x), "r"(t), "r"(h), "r"(block), "r"(bar) : "memory");
+}
+
 // Bits 0 .. n - 1.
 __device__ __forceinline__ uint32_t low_bits(int n) { return n <= 0 ? 0u : n >= 32 ? 0xffffffffu : (1u << n) - 1u; }
+
+// What a row sees of a tile: the tile's mask, and keys below `upper`, from `lower` on or below `firsts`.
+struct RowView {
+    uint32_t mask_at;
+    int upper, lower, firsts;
+    __device__ __forceinline__ uint32_t word(int c) const
+    {
+        uint32_t there;
+        asm volatile("ld.shared.u32 %0, [%1];" : "=r"(there) : "r"(mask_at + 4 * c));
+        return there & low_bits(upper - 32 * c) & (~low_bits(lower - 32 * c) | low_bits(firsts - 32 * c));
+    }
+};
 
 // Rare: V has numbers that are not finite in a tile that not every row sees all of.  The second product would give 0 times such
 // a number to rows that do not see its key, so here each row adds up what it sees.
 template <typename T, int DP, int KEYS>
-__device__ __noinline__ void spoiled_tile(uint32_t p_at, uint32_t o_at, uint32_t v, uint4 mask, bool first)
+__device__ __noinline__ void spoiled_tile(uint32_t p_at, uint32_t o_at, uint32_t v, RowView view, bool first)
 {
 #pragma unroll 1
     for (int c = 0; c < DP / 16; c++) {
@@ -89,67 +122,128 @@ __device__ __noinline__ void spoiled_tile(uint32_t p_at, uint32_t o_at, uint32_t
             asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];" : "=r"(pair) : "r"(p_at + (k >> 1)));
             tensor_loaded();
             const float2 both = unpack2<T>(pair);
-            const uint32_t word = k & 64 ? (k & 32 ? mask.w : mask.z) : (k & 32 ? mask.y : mask.x);
-            if (!(word >> (k & 31) & 1)) continue;
+            const bool seen = view.word(k >> 5) >> (k & 31) & 1;
             const float weight = k & 1 ? both.y : both.x;
-            asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]) : "r"(v + swizzled<KEYS>(k, 2 * c)));
-            asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(x[4]), "=r"(x[5]), "=r"(x[6]), "=r"(x[7]) : "r"(v + swizzled<KEYS>(k, 2 * c + 1)));
+            const int chunk = 2 * c;
+            asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]) : "r"(v + swizzled<KEYS>(k, chunk)));
+            asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(x[4]), "=r"(x[5]), "=r"(x[6]), "=r"(x[7]) : "r"(v + swizzled<KEYS>(k, chunk + 1)));
 #pragma unroll
             for (int i = 0; i < 8; i++) {
                 const float2 f = unpack2<T>(x[i]);
-                acc[2 * i] = __float_as_uint(fmaf(weight, f.x, __uint_as_float(acc[2 * i])));
-                acc[2 * i + 1] = __float_as_uint(fmaf(weight, f.y, __uint_as_float(acc[2 * i + 1])));
+                const float a = __uint_as_float(acc[2 * i]), b = __uint_as_float(acc[2 * i + 1]);
+                acc[2 * i] = __float_as_uint(seen ? fmaf(weight, f.x, a) : a), acc[2 * i + 1] = __float_as_uint(seen ? fmaf(weight, f.y, b) : b);
             }
+            __syncwarp();
         }
-        __syncwarp();
         tensor_store16(o_at + 16 * c, acc);
     }
     tensor_stored();
 }
 
+// Rare: scales of V so far apart that what is next to nothing among the probabilities can be much of the sum.  Each key has its
+// own power of two here, and the sum exponentials of its own; the scores stay in tensor memory and are gone through twice, 16 at a time:
+// for the row's maxima, then for the probabilities.  scales: of the tile's K; exponents: of its V.
+template <int KEYS>
+__device__ __noinline__ float2 far_maxima(uint32_t s_at, RowView view, uint32_t scales, uint32_t exponents, float factor)
+{
+    float highest = -INFINITY, most = -INFINITY;
+#pragma unroll 1
+    for (int c = 0; c < KEYS / 16; c++) {
+        uint32_t v[16];
+        tensor_load16(s_at + 16 * c, v);
+        const uint32_t here = view.word(c >> 1) >> 16 * (c & 1);
+        tensor_loaded();
+#pragma unroll
+        for (int i = 0; i < 16; i += 4) {
+            const float4 k4 = load_shared_f4(scales + 4 * (16 * c + i)), e4 = load_shared_f4(exponents + 4 * (16 * c + i));
+            const float k[4] = {k4.x, k4.y, k4.z, k4.w}, e[4] = {e4.x, e4.y, e4.z, e4.w};
+#pragma unroll
+            for (int j = 0; j < 4; j++) {
+                const float x = here >> (i + j) & 1 ? __uint_as_float(v[i + j]) * (factor * k[j]) : -INFINITY;
+                highest = fmaxf(highest, x), most = fmaxf(most, x + e[j]);
+            }
+        }
+    }
+    return make_float2(highest, most);
+}
+// Probabilities relative to m, to p_at; the sum of exponentials relative to `ref`.
+template <int KEYS>
+__device__ __noinline__ float far_probabilities(uint32_t s_at, uint32_t p_at, RowView view, uint32_t scales, uint32_t exponents, float factor, float ref, float m)
+{
+    float sum = 0.f;
+#pragma unroll 1
+    for (int c = 0; c < KEYS / 16; c++) {
+        uint32_t v[16], w[8];
+        tensor_load16(s_at + 16 * c, v);
+        const uint32_t here = view.word(c >> 1) >> 16 * (c & 1);
+        tensor_loaded();
+#pragma unroll
+        for (int i = 0; i < 16; i += 4) {
+            const float4 k4 = load_shared_f4(scales + 4 * (16 * c + i)), e4 = load_shared_f4(exponents + 4 * (16 * c + i));
+            const float k[4] = {k4.x, k4.y, k4.z, k4.w}, e[4] = {e4.x, e4.y, e4.z, e4.w};
+            float x[4];
+#pragma unroll
+            for (int j = 0; j < 4; j++) {
+                x[j] = here >> (i + j) & 1 ? __uint_as_float(v[i + j]) * (factor * k[j]) : -INFINITY;
+                sum += exp2_approx(x[j] - ref);
+                x[j] = exp2_approx(x[j] + e[j] - m);
+            }
+            w[i / 2] = pack2<__half>(x[0], x[1]), w[i / 2 + 1] = pack2<__half>(x[2], x[3]);
+        }
+        tensor_store8(p_at + 8 * c, w);
+    }
+    return sum;
+}
+
 // T: the type of the products, fp16 for codes.
 template <typename T, int KIND, int DP>
-__global__ void __launch_bounds__(kChunkThreads, 1) chunk_kernel(const __grid_constant__ ChunkParams p)
+__global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(const __grid_constant__ ChunkParams p)
 {
     using M = ChunkMemory<KIND, DP>;
-    constexpr int kKeys = M::keys, kSlots = M::slots, kWords = kKeys / 32, kMine = kKeys / 4;  // kMine: keys of a tile that a warp fetches
+    using W = ChunkWarps<KIND>;
+    // kMine: keys of a tile that a warp fetches
+    constexpr int kKeys = M::keys, kSlots = M::slots, kMine = kKeys / 4, kWords = kKeys / 32, kLoad = W::softmax, kIssue = kLoad + W::loaders;
     constexpr float kLift = probability_lift<T>();
     extern __shared__ unsigned char raw[];
     allow_next();
     const uint32_t base = (static_cast<uint32_t>(__cvta_generic_to_shared(raw)) + 1023) & ~1023u;
     unsigned char *const gen = raw + (base - static_cast<uint32_t>(__cvta_generic_to_shared(raw)));
-    constexpr int kRingAt = M::queries, kStagingAt = kRingAt + M::stages * M::tile, kInfoAt = kStagingAt + M::staged * M::codes, kDownsAt = kInfoAt + kChunkInfos * M::info,
-                  kTableAt = kDownsAt + M::downs, kItemsAt = kTableAt + M::table, kAnswerAt = kItemsAt + 2 * M::item, kBarsAt = kAnswerAt + 16;
+    constexpr int kRingAt = M::queries, kStagingAt = kRingAt + M::stages * M::tile, kInfoAt = kStagingAt + M::staged * M::codes, kDownsAt = kInfoAt + M::infos * M::info, kTableAt = kDownsAt + M::downs,
+                  kItemsAt = kTableAt + M::table, kAnswerAt = kItemsAt + 2 * M::item, kBarsAt = kAnswerAt + 16;
     static_assert(kInfoAt % 16 == 0 && kItemsAt % 16 == 0 && kAnswerAt % 16 == 0);
-    const uint32_t ring = base + kRingAt, staging = base + kStagingAt, info = base + kInfoAt;
-    const uint32_t full = base + kBarsAt, empty = full + 8 * M::stages, s_full = empty + 8 * M::stages, s_taken = s_full + 16, p_ready = s_taken + 16, o_added = p_ready + 16;
-    const uint32_t q_full = o_added + 16, q_empty = q_full + 8, item_full = q_empty + 8, item_empty = item_full + 16, wanted = item_empty + 16, answered = wanted + 8, last_at = answered + 8, tensor_at = last_at + 16;
-    static_assert(8 * (2 * M::stages + 18) + 8 <= 512);
-    uint32_t *const items_before = reinterpret_cast<uint32_t *>(gen + kTableAt), *const rows_before = items_before + kChunkThreads;
+    const uint32_t ring = base + kRingAt, info = base + kInfoAt;
+    const uint32_t full = base + kBarsAt, empty = full + 8 * M::turns, s_full = empty + 8 * M::turns, s_taken = s_full + 16, p_ready = s_taken + 16, o_added = p_ready + 16;
+    const uint32_t q_full = o_added + 16, q_empty = q_full + 8, item_full = q_empty + 8, item_empty = item_full + 16, wanted = item_empty + 16, answered = wanted + 8, last_at = answered + 8, landed = last_at + 16, staged_full = landed + 16, staged_empty = staged_full + 8 * M::staged_turns, tensor_at = staged_empty + 8 * M::staged_turns;
+    static_assert(8 * (2 * M::turns + 20 + 2 * M::staged_turns) + 8 <= 512);
+    uint32_t *const items_before = reinterpret_cast<uint32_t *>(gen + kTableAt), *const rows_before = items_before + W::threads;
     ChunkItem *const items = reinterpret_cast<ChunkItem *>(gen + kItemsAt);
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31, D = p.layer.D, H = p.layer.H;
     const ChunkShape &shape = p.shape;
 
     if (threadIdx.x == 0) {
-        for (int i = 0; i < M::stages; i++) barrier_init(full + 8 * i, 128), barrier_init(empty + 8 * i, 1);
+        // boxes announce themselves to whoever waits for their bytes; copies key by key for their lanes, and a lane of each warp what it has written beside them
+        const int ready = KIND != kPlain ? 128 : p.box_rows ? 2 : 2 * 33;
+        for (int i = 0; i < M::turns; i++) barrier_init(full + 8 * i, ready), barrier_init(empty + 8 * i, 1);
+        for (int i = 0; i < 2; i++) barrier_init(landed + 8 * i, 1);
+        for (int i = 0; i < M::staged_turns; i++) barrier_init(staged_full + 8 * i, p.box_rows ? 1 : 128), barrier_init(staged_empty + 8 * i, 128);
         for (int i = 0; i < 2; i++) barrier_init(s_full + 8 * i, 1), barrier_init(s_taken + 8 * i, 128), barrier_init(p_ready + 8 * i, 128), barrier_init(o_added + 8 * i, 1);
-        for (int i = 0; i < 2; i++) barrier_init(item_full + 8 * i, 1), barrier_init(item_empty + 8 * i, kSlots * 4 + 6), barrier_init(last_at + 8 * i, 1);
-        barrier_init(q_full, 128), barrier_init(q_empty, 1), barrier_init(wanted, 1), barrier_init(answered, 1);
+        for (int i = 0; i < 2; i++) barrier_init(item_full + 8 * i, 1), barrier_init(item_empty + 8 * i, kSlots * 4 + W::loaders + 2 + (KIND != kPlain && p.box_rows ? 1 : 0)), barrier_init(last_at + 8 * i, 1);
+        barrier_init(q_full, KIND == kPlain ? 4 * 33 : 256), barrier_init(q_empty, 1), barrier_init(wanted, 1), barrier_init(answered, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp == 12) {
+    if (warp == kIssue) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(tensor_at) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
 
     // ------------------------------------------------------------------- the cut, the same in every CTA
     // Each thread has a run of requests.
-    __shared__ int64_t sum_items[16];
-    __shared__ int32_t sum_tiles[16];
+    __shared__ int64_t sum_items[W::all];
+    __shared__ int32_t sum_tiles[W::all];
     __shared__ float best_cost[16];
     __shared__ int32_t best_share[16];
-    __shared__ uint32_t warp_items[16], warp_rows[16];
-    const int64_t per = (p.R + kChunkThreads - 1) / kChunkThreads, run0 = min(threadIdx.x * per, p.R), run1 = min(run0 + per, p.R);
+    __shared__ uint32_t warp_items[W::all], warp_rows[W::all];
+    const int64_t per = (p.R + W::threads - 1) / W::threads, run0 = min(threadIdx.x * per, p.R), run1 = min(run0 + per, p.R);
     int32_t share = 1 << 30;
     if (p.plan.part_rows) {
         int64_t n_items = 0;
@@ -166,13 +260,13 @@ __global__ void __launch_bounds__(kChunkThreads, 1) chunk_kernel(const __grid_co
         if (lane == 0) sum_items[warp] = n_items, sum_tiles[warp] = most;
         __syncthreads();
         n_items = 0;
-        for (int w = 0; w < 16; w++) n_items += sum_items[w], most = max(most, sum_tiles[w]);
+        for (int w = 0; w < W::all; w++) n_items += sum_items[w], most = max(most, sum_tiles[w]);
         if (n_items < kChunkEnough && most > kChunkLeastShare) {
-            // warp w looks at cuts w and w + 16
+            // warps 0 to 15 look at cuts w and w + 16
             ChunkCost sum[2];
-            const int32_t shares[2] = {chunk_share(most, warp), chunk_share(most, warp + 16)};
+            const int32_t shares[2] = {chunk_share(most, warp & 15), chunk_share(most, (warp & 15) + 16)};
             const float inverse[2] = {1.f / shares[0], 1.f / shares[1]};
-            for (int64_t r = lane; r < p.R; r += 32) {
+            for (int64_t r = lane; r < (warp < 16 ? p.R : 0); r += 32) {
                 const ChunkRequest q = chunk_request(p, r, false);
                 if (!q.n) continue;
                 const int32_t blocks = chunk_blocks(shape, q.n) * H, tiles = chunk_tiles(shape, q.len);
@@ -191,7 +285,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) chunk_kernel(const __grid_co
                 const float here = chunk_cost(sum[c].items, sum[c].split, sum[c].tiles, __reduce_max_sync(0xffffffffu, sum[c].longest));
                 if (here < cost) cost = here, chosen = shares[c];
             }
-            if (lane == 0) best_cost[warp] = cost, best_share[warp] = chosen;
+            if (lane == 0 && warp < 16) best_cost[warp] = cost, best_share[warp] = chosen;
             __syncthreads();
             cost = 3e38f;
             for (int w = 0; w < 16; w++)
@@ -217,7 +311,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) chunk_kernel(const __grid_co
         if (lane == 31) warp_items[warp] = upto, warp_rows[warp] = rows_upto;
         __syncthreads();
         total = 0;
-        for (int w = 0; w < 16; w++) {
+        for (int w = 0; w < W::all; w++) {
             if (w < warp) upto += warp_items[w], rows_upto += warp_rows[w];
             total += warp_items[w];
         }
@@ -244,6 +338,12 @@ __global__ void __launch_bounds__(kChunkThreads, 1) chunk_kernel(const __grid_co
         if (lane == 0) barrier_arrive(item_empty + 8 * (it & 1));
         return item.valid != 0;
     };
+    // Whether the place of copy u among the staged codes is done with.
+    auto staging_free = [&](uint32_t u) { return u < 3 || barrier_wait(staged_empty + 8 * ((u - 3) % M::staged_turns), ((u - 3) / M::staged_turns) & 1); };
+    static_assert(M::staged == 0 || M::staged == 3);
+    // Copy u (K of this CTA's tile u / 2, then V) is in stage u % stages: whether it is there, and whether copy u - stages is done with.
+    auto copied = [&](uint32_t u) { return barrier_wait(full + 8 * (u % M::turns), (u / M::turns) & 1); };
+    auto stage_free = [&](uint32_t u) { return u < M::stages || barrier_wait(empty + 8 * ((u - M::stages) % M::turns), ((u - M::stages) / M::turns) & 1); };
     auto tile_of = [](const ChunkItem &item, int i) { return i < item.list.firsts ? i : i + item.list.skip; };
     // Does slot `slot` need tile i of the list?
     auto needs = [](const ChunkItem &item, int slot, int i) {
@@ -256,9 +356,9 @@ __global__ void __launch_bounds__(kChunkThreads, 1) chunk_kernel(const __grid_co
         return k0 + kKeys - 1 > item.pos0 + static_cast<int>(quick_div(item.row0, p.div_group)) || (k0 < item.list.key_end - shape.window && k0 + kKeys > shape.sinks);
     };
 
-    if (warp < 8) {
+    if (warp < kLoad) {
         // ---------------------------------------------------------------------------- softmax
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 192;");
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(W::softmax_registers));
         const int slot = warp >> 2, r = (warp & 3) * 32 + lane;
         const uint32_t lanes = tensor + (static_cast<uint32_t>((warp & 3) * 32) << 16), p_at = lanes + kProbabilities + slot * 64, o_at = lanes + kOutputs + slot * 128;
         uint32_t steps = 0, tiles = 0, loads = 0;  // of this slot; of the CTA; items that had queries
@@ -303,7 +403,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) chunk_kernel(const __grid_co
                 fine = __all_sync(0xffffffffu, barrier_wait(s_full + 8 * b, parity));
                 if (!fine) break;
                 fence_after();
-                const uint32_t about = info + (tiles % kChunkInfos) * M::info;
+                const uint32_t about = info + (tiles % M::infos) * M::info;
                 // P is free and O at rest when this slot's last product is done
                 bool rest = steps == 0;
                 auto await_rest = [&]() {
@@ -312,6 +412,16 @@ __global__ void __launch_bounds__(kChunkThreads, 1) chunk_kernel(const __grid_co
                     fence_after();
                     rest = true;
                 };
+                // the row's running maximum moves; O is rescaled
+                auto move_top = [&](float most) {
+                    const float m = fmaxf(top, most), f = m == top ? 1.f : exp2_approx(top - m);
+                    top = m;
+                    if constexpr (KIND == kPlain) sum.x *= f, sum.y *= f;
+                    if (mine) {
+                        await_rest();
+                        scale_outputs(f);
+                    }
+                };
                 union {
                     uint32_t w[kWords][32];
                     float f[kWords][32];
@@ -319,43 +429,45 @@ __global__ void __launch_bounds__(kChunkThreads, 1) chunk_kernel(const __grid_co
                 } s;
 #pragma unroll
                 for (int c = 0; c < kWords; c++) tensor_load32(s_at + 32 * c, s.w[c]);
-                uint32_t mask[4];
-                asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(mask[0]), "=r"(mask[1]), "=r"(mask[2]), "=r"(mask[3]) : "r"(about));
                 const bool edge = ragged(item, i);
+                RowView view{about, 1 << 30, -(1 << 30), 0};
                 if (edge) {
-                    // what this row sees
-                    const int k0 = tile_of(item, i) * kKeys, upper = pos + 1 - k0, lower = upper - shape.window, firsts = shape.sinks - k0;
-#pragma unroll
-                    for (int c = 0; c < kWords; c++) mask[c] &= low_bits(upper - 32 * c) & (~low_bits(lower - 32 * c) | low_bits(firsts - 32 * c));
+                    const int k0 = tile_of(item, i) * kKeys;
+                    view.upper = pos + 1 - k0, view.lower = view.upper - shape.window, view.firsts = shape.sinks - k0;
                 }
                 float exponent = 0.f;
                 uint32_t far = 0;
-                if constexpr (KIND != kPlain) asm volatile("ld.shared.v2.b32 {%0,%1}, [%2];" : "=f"(exponent), "=r"(far) : "r"(about + 32));
-                tensor_loaded();
-                bool stored = false;
                 if constexpr (KIND != kPlain) {
+                    asm volatile("ld.shared.v2.b32 {%0,%1}, [%2];" : "=f"(exponent), "=r"(far) : "r"(about + 32));
                     if (!mine) {
                         float down;
                         asm volatile("ld.shared.f32 %0, [%1];" : "=f"(down) : "r"(down_at));
                         factor *= down;
                     }
-                    if (far) {
-                        RowState state{top, ref, sum.x + sum.y};
-                        await_rest();  // of the item before, too: P is free
-                        if (!fine) break;
-                        fine = far_tile<DP, kKeys>(state, s_at, p_at, o_at, make_uint4(mask[0], mask[1], mask[2], mask[3]), about + M::scales, factor, o_added + 8 * slot, (steps - 1) & 1, mine);
-                        top = state.top, ref = state.ref, sum = make_float2(state.sum, 0.f);
-                        if (!fine) break;
-                        stored = true;
-                    }
                 }
-                if (stored) {
+                if (KIND != kPlain && far) {
+                    tensor_loaded();
+                    const uint32_t scales = about + M::scales;
+                    const float2 maxima = far_maxima<kKeys>(s_at, view, scales, scales + 4 * kKeys, factor);
+                    raise_ref(maxima.x);
+                    move_top(maxima.y);
+                    await_rest();
+                    if (!fine) break;
+                    sum.x += far_probabilities<kKeys>(s_at, p_at, view, scales, scales + 4 * kKeys, factor, ref == -INFINITY ? 0.f : ref, top == -INFINITY ? 0.f : top - kLift);
                     tensor_stored();
                     fence_before();
                     barrier_arrive(s_taken + 8 * b);
                 } else {
+                    uint32_t mask[kWords], all_seen = 0xffffffffu;
+#pragma unroll
+                    for (int c = 0; c < kWords; c++) asm volatile("ld.shared.u32 %0, [%1];" : "=r"(mask[c]) : "r"(about + 4 * c));
+                    tensor_loaded();
                     fence_before();
                     barrier_arrive(s_taken + 8 * b);
+                    if (edge) {
+#pragma unroll
+                        for (int c = 0; c < kWords; c++) mask[c] = view.word(c);
+                    }
                     if constexpr (KIND != kPlain) {
                         const float2 f2 = make_float2(factor, factor), zero = make_float2(0.f, 0.f);
 #pragma unroll
@@ -366,9 +478,8 @@ __global__ void __launch_bounds__(kChunkThreads, 1) chunk_kernel(const __grid_co
                             x[1] = fused2(x[1], fused2(f2, make_float2(k.z, k.w), zero), zero);
                         }
                     }
-                    uint32_t all_seen = mask[0];
 #pragma unroll
-                    for (int c = 1; c < kWords; c++) all_seen &= mask[c];
+                    for (int c = 0; c < kWords; c++) all_seen &= mask[c];
                     if (all_seen != 0xffffffffu) {
 #pragma unroll
                         for (int c = 0; c < kWords; c++)
@@ -386,19 +497,13 @@ __global__ void __launch_bounds__(kChunkThreads, 1) chunk_kernel(const __grid_co
                     const float highest = fmaxf(larger3(m4[0], m4[1], m4[2]), m4[3]), most = KIND == kPlain ? highest * factor : highest + exponent;
                     bool move = most > top + 8.f;
                     if constexpr (KIND != kPlain) move = move || highest > ref + 8.f;
+                    // a running maximum moves only when a score exceeds it by more than 8 (2^8 in probabilities)
                     if (__any_sync(0xffffffffu, move)) {
                         if constexpr (KIND != kPlain) raise_ref(highest);
-                        const float m = fmaxf(top, most), f = m == top ? 1.f : exp2_approx(top - m);
-                        top = m;
-                        if constexpr (KIND == kPlain) sum.x *= f, sum.y *= f;
-                        if (mine) {
-                            await_rest();
-                            scale_outputs(f);
-                        }
+                        move_top(most);
                     }
                     const float m = top == -INFINITY ? 0.f : top - kLift;
                     const float2 minus = make_float2(exponent - m, exponent - m), f2 = make_float2(factor, factor);
-                    uint32_t w[kWords][16];
                     float2 here = make_float2(0.f, 0.f);
 #pragma unroll
                     for (int c = 0; c < kWords; c++) {
@@ -407,7 +512,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) chunk_kernel(const __grid_co
                             float2 e = KIND == kPlain ? fused2(s.f2[c][j], f2, minus) : sum2(s.f2[c][j], minus);
                             e = make_float2(exp2_approx(e.x), exp2_approx(e.y));
                             here = sum2(here, e);
-                            w[c][j] = pack2<T>(e.x, e.y);
+                            s.w[c][j] = pack2<T>(e.x, e.y);  // (in the place of scores that are done with)
                         }
                     }
                     if constexpr (KIND == kPlain) {
@@ -420,16 +525,16 @@ __global__ void __launch_bounds__(kChunkThreads, 1) chunk_kernel(const __grid_co
                     await_rest();  // by now it has been given, as a rule
                     if (!fine) break;
 #pragma unroll
-                    for (int c = 0; c < kWords; c++) tensor_store16(p_at + 16 * c, w[c]);
+                    for (int c = 0; c < kWords; c++) tensor_store16(p_at + 16 * c, reinterpret_cast<const uint32_t(&)[16]>(s.w[c]));
                     tensor_stored();
                 }
                 if (edge) {
                     const uint32_t u = 2 * tiles + 1, stage = u % M::stages;
-                    fine = __all_sync(0xffffffffu, barrier_wait(full + 8 * stage, (u / M::stages) & 1));
+                    fine = __all_sync(0xffffffffu, copied(u));
                     if (!fine) break;
                     uint32_t bad[4];
-                    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(bad[0]), "=r"(bad[1]), "=r"(bad[2]), "=r"(bad[3]) : "r"(about + 16));
-                    if (bad[0] | bad[1] | bad[2] | bad[3]) spoiled_tile<T, DP, kKeys>(p_at, o_at, ring + stage * M::tile, make_uint4(mask[0], mask[1], mask[2], mask[3]), !mine);
+                    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(bad[0]), "=r"(bad[1]), "=r"(bad[2]), "=r"(bad[3]) : "r"(about + 16) : "memory");
+                    if (bad[0] | bad[1] | bad[2] | bad[3]) spoiled_tile<T, DP, kKeys>(p_at, o_at, ring + stage * M::tile, view, !mine);
                 }
                 fence_before();
                 barrier_arrive(p_ready + 8 * slot);
@@ -490,24 +595,11 @@ __global__ void __launch_bounds__(kChunkThreads, 1) chunk_kernel(const __grid_co
             if (store && cut) p.sums[at] = log;
             if (store && !cut && p.lse) p.lse[(item.token0 + token) * p.Hq + head] = log * kChunkLn2;
         }
-    } else if (warp < 12) {
+    } else if (warp < kIssue) {
         // --------------------------------------------------------------------------- the pages
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
-        const int w = warp - 8, thread = threadIdx.x - 256;
-        uint32_t tiles = 0, loads = 0;  // of the CTA; items that had queries
-        // what the table says of this lane's key of a tile; kNoKey: it is none.  Looked at a tile later
-        constexpr int32_t kNoKey = INT32_MIN;
-        auto key_of = [&](const ChunkItem &item, int i) { return tile_of(item, i) * kKeys + w * kMine + lane; };
-        auto look_up = [&](const ChunkItem &item, int i) -> int32_t {
-            const int t = key_of(item, i);
-            if (i >= item.end || lane >= kMine || t >= item.list.key_end || (t < item.list.key_low && t >= shape.sinks)) return kNoKey;
-            return reinterpret_cast<const int32_t *>(p.tables + item.r * p.table_stride)[quick_div(static_cast<uint32_t>(t), p.div_block)];
-        };
-        auto checked = [&](int32_t said) -> int32_t {
-            const bool in = said >= 0 && said < p.layer.num_blocks;
-            if (!in && said != kNoKey) atomicOr(p.status, kStatusBadIndex);
-            return in ? said : -1;
-        };
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(W::other_registers));
+        const int thread = threadIdx.x - 32 * kLoad;
+        uint32_t tiles = 0, loads = 0, looks = 0;  // of the CTA; items that had queries; tiles of V that were looked at
         auto place_in_block = [&](int t) { return t - static_cast<int>(quick_div(static_cast<uint32_t>(t), p.div_block)) * static_cast<int>(p.layer.B); };
         // where 8 elements of a row of queries are, or NULL: past the last row or past D
         auto query_at = [&](const ChunkItem &item, int rr, int chunk) -> const char * {
@@ -515,249 +607,311 @@ __global__ void __launch_bounds__(kChunkThreads, 1) chunk_kernel(const __grid_co
             const uint32_t row = item.row0 + rr, token = quick_div(row, p.div_group);
             return p.q + (item.token0 + token) * p.q_token + (item.h * shape.group + static_cast<int>(row - token * shape.group)) * p.q_head + chunk * 16;
         };
-        // all of this group of four warps, wherever a wait of one ran out
-        auto together = [&](bool yes) {
-            uint32_t all;
-            asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.cta.red.and.pred q, 1, 128, p;\n\tselp.u32 %0, 1, 0, q;\n\t}" : "=r"(all) : "r"(static_cast<uint32_t>(yes)) : "memory");
-            return all != 0;
+        // near the item's end the next one is asked for
+        auto near_end = [&](const ChunkItem &item, int i) {
+            if (warp == kLoad && lane == 0 && i == max(item.begin, item.end - 2)) barrier_arrive(wanted);
         };
 
         if constexpr (KIND == kPlain) {
-            // Copies in flight, oldest last: 1 + the barrier's index (stage; kQueries), flags for V of a tile that needs looking
-            // at (bit 8) and the tile's info (bits 16 on); 0: none.
-            constexpr uint32_t kQueries = 64, kLook = 256;
-            uint32_t flight[2] = {0, 0};
-            auto pass_on = [&](uint32_t what) {
-                if (!what) return;
-                const uint32_t index = (what & 255) - 1;
-                if (what & kLook) {
-                    uint32_t bad = 0;
-                    constexpr int chunks = DP / 8;
+            // Two warps fetch K, two V, each half of every tile's keys.  Where pages fit, a lane has a page and fetches boxes of it, 64 elements wide, that
+            // land swizzled; what they bring beside the keys that are seen is harmless in K, whose scores are masked, and
+            // is made zero in V.  Elsewhere keys are copied in chunks of 16 bytes.
+            const int kv = (warp - kLoad) >> 1, sub = warp & 1;
+            constexpr int kHalf = kKeys / 2, kHalfWords = kHalf / 32, chunks = DP / 8;
+            const char *const plane = kv ? p.layer.v : p.layer.k;
+            const CUtensorMap *const map = kv ? &p.map_v : &p.map_k;
+            // Copies announce themselves when they have landed; lane 0 says for its warp what was written beside them.
+            auto announce = [&](uint32_t bar) {
+                asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
+                __syncwarp();
+                if (lane == 0) barrier_arrive(bar);
+            };
+            auto take_queries = [&](const ChunkItem &item) {
+                if (loads) fine = __all_sync(0xffffffffu, barrier_wait(q_empty, (loads - 1) & 1));
+                if (!fine) return;
 #pragma unroll 4
-                    for (int i = 0; i < kMine * chunks / 32; i++) {
-                        const int idx = i * 32 + lane;
-                        uint32_t x[4];
-                        asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]) : "r"(ring + index * M::tile + swizzled<kKeys>(w * kMine + idx / chunks, idx % chunks)));
-                        bad |= not_finite<T>(x[0]) | not_finite<T>(x[1]) | not_finite<T>(x[2]) | not_finite<T>(x[3]);
-                    }
-                    if (__any_sync(0xffffffffu, bad != 0) && lane == 0) asm volatile("st.shared.u32 [%0], %1;" ::"r"(info + (what >> 16) * M::info + 16 + 4 * w), "r"(1) : "memory");
-                    __syncwarp();
+                for (int j = 0; j < kSlots * DP / 8; j++) {
+                    const int idx = j * 128 + thread, rr = idx / chunks, ch = idx % chunks;
+                    const char *src = query_at(item, rr, ch);
+                    copy_async16(base + (rr >> 7) * M::q_tile + swizzled(rr & 127, ch), src ? src : p.q, src != nullptr);
                 }
-                fence_shared_to_async();
-                barrier_arrive(index == kQueries ? q_full : full + 8 * index);
+                announce(q_full);
+                loads++;
             };
-            auto in_flight = [&](uint32_t what) {
-                copy_commit();
-                copy_wait<2>();
-                pass_on(flight[1]);
-                flight[1] = flight[0], flight[0] = what;
+            // What the table says of this lane's page, or of its keys; kNoKey: it is none that is seen.  Looked at a tile later.
+            const int box_rows = p.box_rows, pages = box_rows ? kHalf / box_rows : 0;
+            auto first_key = [&](const ChunkItem &item, int i) { return tile_of(item, i) * kKeys + sub * kHalf; };
+            auto entry = [&](const ChunkItem &item, int i, int t, int rows) -> int32_t {
+                if (i >= item.end || t >= item.list.key_end || (t + rows <= item.list.key_low && t >= shape.sinks)) return kNoKey;
+                return reinterpret_cast<const int32_t *>(p.tables + item.r * p.table_stride)[quick_div(static_cast<uint32_t>(t), p.div_block)];
             };
-            auto land = [&]() {
-                copy_wait<0>();
-                pass_on(flight[1]), pass_on(flight[0]);
-                flight[0] = flight[1] = 0;
+            auto look_up = [&](const ChunkItem &item, int i, int32_t (&said)[kHalfWords]) {
+                const int t = first_key(item, i);
+                if (box_rows) {
+                    said[0] = lane < pages ? entry(item, i, t + lane * box_rows, box_rows) : kNoKey;
+                } else {
+#pragma unroll
+                    for (int x = 0; x < kHalfWords; x++) said[x] = entry(item, i, t + lane + 32 * x, 1);
+                }
             };
-            // waits until `bar` has passed, with what is in flight passed on meanwhile
-            auto await_free = [&](uint32_t bar, uint32_t parity) {
-                if (__all_sync(0xffffffffu, barrier_passed(bar, parity))) return;
-                land();
-                fine = __all_sync(0xffffffffu, barrier_wait(bar, parity));
+            auto checked = [&](int32_t said) -> int32_t {
+                const bool in = said >= 0 && said < p.layer.num_blocks;
+                if (!in && said != kNoKey) atomicOr(p.status, kStatusBadIndex);
+                return in ? said : -1;
             };
             for (int it = 0; fine; it++) {
                 ChunkItem item;
-                if (!__all_sync(0xffffffffu, barrier_passed(item_full + 8 * (it & 1), (it >> 1) & 1))) land();
                 if (!take_item(it, item)) break;
-                int32_t ahead = look_up(item, item.begin);
+                int32_t ahead[kHalfWords];
+                look_up(item, item.begin, ahead);
                 for (int i = item.begin; i < item.end && fine; i++, tiles++) {
-                    if (w == 0 && lane == 0 && i == max(item.begin, item.end - 2)) barrier_arrive(wanted);
-                    const int32_t blk = checked(ahead);
-                    const int64_t off = blk >= 0 ? p.layer.geo.at(blk, place_in_block(key_of(item, i)), item.h) : -1;
-                    ahead = look_up(item, i + 1);
-                    const uint32_t mask = __ballot_sync(0xffffffffu, blk >= 0), slot = tiles % kChunkInfos;
-                    for (int kv = 0; kv < 2; kv++) {
-                        const uint32_t u = 2 * tiles + kv, stage = u % M::stages;
-                        if (u >= M::stages) await_free(empty + 8 * stage, (u / M::stages - 1) & 1);
-                        if (!fine) break;
-                        if (kv == 0 && lane == 0) {
-                            // the tile whose mask this one's replaces is past its last use: its V is older than this stage's last copy
-                            const uint32_t about = info + slot * M::info;
-                            if constexpr (kMine == 32) asm volatile("st.shared.u32 [%0], %1;" ::"r"(about + 4 * w), "r"(mask) : "memory");
-                            else asm volatile("st.shared.u16 [%0], %1;" ::"r"(about + 2 * w), "h"(static_cast<uint16_t>(mask)) : "memory");
-                            asm volatile("st.shared.u32 [%0], %1;" ::"r"(about + 16 + 4 * w), "r"(0) : "memory");
-                        }
-                        const char *plane = kv ? p.layer.v : p.layer.k;
-                        const uint32_t to = ring + stage * M::tile;
-                        constexpr int chunks = DP / 8;
+                    near_end(item, i);
+                    const int t0 = first_key(item, i);
+                    const uint32_t u = 2 * tiles + kv, stage = u % M::stages, bar = full + 8 * (u % M::turns), about = info + (tiles % M::infos) * M::info, to = ring + stage * M::tile;
+                    int32_t blk[kHalfWords];
+                    uint32_t mask[kHalfWords];
+                    blk[0] = checked(ahead[0]);
 #pragma unroll
-                        for (int j = 0; j < kMine * chunks / 32; j++) {
-                            const int idx = j * 32 + lane, rr = idx / chunks, ch = idx % chunks;
-                            const int64_t src = __shfl_sync(0xffffffffu, off, rr);
-                            const bool there = src >= 0 && ch * 8 < D;
-                            copy_async16(to + swizzled<kKeys>(w * kMine + rr, ch), plane + (there ? src + ch * 16 : 0), there);
+                    for (int x = 0; x < kHalfWords; x++) {
+                        const int t = t0 + lane + 32 * x;
+                        bool there = t < item.list.key_end && (t >= item.list.key_low || t < shape.sinks);
+                        if (box_rows) {
+                            there = __shfl_sync(0xffffffffu, blk[0], quick_div(static_cast<uint32_t>(lane + 32 * x), p.div_box)) >= 0 && there;
+                        } else {
+                            if (x) blk[x] = checked(ahead[x]);
+                            there = blk[x] >= 0;
                         }
-                        in_flight((stage + 1) | (kv && ragged(item, i) ? kLook : 0u) | slot << 16);
-                        if (kv == 0 && i == item.begin) {
-                            // the queries, behind the first keys
-                            if (loads) await_free(q_empty, (loads - 1) & 1);
-                            if (!fine) break;
-#pragma unroll 4
-                            for (int j = 0; j < kSlots * DP / 8; j++) {
-                                const int idx = j * 128 + thread, rr = idx / chunks, ch = idx % chunks;
-                                const char *src = query_at(item, rr, ch);
-                                copy_async16(base + (rr >> 7) * M::q_tile + swizzled(rr & 127, ch), src ? src : p.q, src != nullptr);
-                            }
-                            in_flight(kQueries + 1);
-                            loads++;
+                        mask[x] = __ballot_sync(0xffffffffu, there);
+                    }
+                    look_up(item, i + 1, ahead);
+                    if (kv && i == item.begin) take_queries(item);
+                    if (fine) fine = __all_sync(0xffffffffu, stage_free(u));
+                    if (!fine) break;
+                    if (kv == 0 && lane == 0) {
+#pragma unroll
+                        for (int x = 0; x < kHalfWords; x++) asm volatile("st.shared.u32 [%0], %1;" ::"r"(about + 4 * (sub * kHalfWords + x)), "r"(mask[x]) : "memory");
+                    }
+                    const bool look = kv && ragged(item, i);
+                    if (box_rows) {
+                        const uint32_t lands = look ? landed + 8 * sub : bar;
+                        if (lane == 0) asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(lands), "n"(kHalf * DP * 2) : "memory");
+                        __syncwarp();
+                        if (lane < pages) {
+                            const int t = t0 + lane * box_rows;
+#pragma unroll
+                            for (int c = 0; c < DP / 64; c++)
+                                copy_box(to + c * (kKeys * 128) + (sub * kHalf + lane * box_rows) * 128, map, 64 * c, place_in_block(t), item.h, blk[0] >= 0 ? blk[0] : static_cast<int32_t>(p.layer.num_blocks), lands);
+                        }
+                        __syncwarp();
+                    } else {
+                        int64_t off[kHalfWords];
+#pragma unroll
+                        for (int x = 0; x < kHalfWords; x++) off[x] = blk[x] >= 0 ? p.layer.geo.at(blk[x], place_in_block(t0 + lane + 32 * x), item.h) : -1;
+#pragma unroll
+                        for (int j = 0; j < kHalf * chunks / 32; j++) {
+                            const int idx = j * 32 + lane, rr = idx / chunks, ch = idx % chunks;
+                            const int64_t src = __shfl_sync(0xffffffffu, off[j * 32 / chunks / 32], rr & 31);
+                            const bool there = src >= 0 && ch * 8 < D;
+                            copy_async16(to + swizzled<kKeys>(sub * kHalf + rr, ch), plane + (there ? src + ch * 16 : 0), there);
                         }
                     }
+                    if (kv) {
+                        uint32_t bad = 0;
+                        if (look) {
+                            if (box_rows) {
+                                fine = __all_sync(0xffffffffu, barrier_wait(landed + 8 * sub, looks & 1));
+                                looks++;
+                                if (!fine) break;
+                            } else {
+                                copy_wait<0>();
+                            }
+                            uint32_t any = 0;
+#pragma unroll 2
+                            for (int j = 0; j < kHalf * chunks / 32; j++) {
+                                const int idx = j * 32 + lane, rr = idx / chunks;
+                                const uint32_t at = to + swizzled<kKeys>(sub * kHalf + rr, idx % chunks);
+                                uint32_t x[4];
+                                if (kHalfWords == 2 && rr >= 32 ? mask[kHalfWords - 1] >> (rr & 31) & 1 : mask[0] >> (rr & 31) & 1) {
+                                    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]) : "r"(at) : "memory");
+                                    any |= not_finite<T>(x[0]) | not_finite<T>(x[1]) | not_finite<T>(x[2]) | not_finite<T>(x[3]);
+                                } else {
+                                    asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(at), "r"(0) : "memory");
+                                }
+                            }
+                            __syncwarp();
+                            bad = __any_sync(0xffffffffu, any != 0);
+                            fence_shared_to_async();
+                        }
+                        if (lane == 0) asm volatile("st.shared.v2.u32 [%0], {%1,%2};" ::"r"(about + 16 + 8 * sub), "r"(bad), "r"(0) : "memory");
+                    }
+                    if (!box_rows) announce(bar);
+                    else if (look) {
+                        __syncwarp();
+                        if (lane == 0) barrier_arrive(bar);
+                    }
+                    if (!kv && i == item.begin) take_queries(item);
                 }
-                if (item.begin >= item.end && w == 0 && lane == 0) barrier_arrive(wanted);
+                if (item.begin >= item.end && warp == kLoad && lane == 0) barrier_arrive(wanted);
             }
             copy_wait<0>();
-            if (fine) land();
         } else {
-            // Codes: a warp fetches and widens its own keys of every tile.  V's are multiplied by their scales over a
+            // Codes: pages are staged as they lie in the pool, as boxes by a warp of their own or in chunks of 16 bytes by those that widen
+            // them: four warps K, four V, each its own keys of every tile.  V's are multiplied by their scales over a
             // power of two that the tile's largest scale sets, 2^exponent, which puts the values below 2^16: rounded
             // to fp16 twice (the factor and the product), half a step of 2^-11 each, like the probabilities
             // that they meet.  Products below fp16's normal numbers are off by half of 2^-24, which is 2^-15 of the
             // key's scale at most, since a tile whose scales span more than 2^16 is `far`: there each key
             // has an exponent of its own.  So it is where a tile's largest scale is 2^-40 of one before.  K's scales are left to the
             // scores, in fp32, for the sake of the logarithms.
-            constexpr int chunks = DP / 16;
-            const uint32_t staged = staging + w * kMine * DP;
-            uint32_t copies = 0;  // issued, of the CTA
+            const int kv = warp >= kLoad + 4, w = warp & 3;
+            // all of K's or V's four warps, wherever a wait of one ran out
+            auto together = [&](bool yes) {
+                uint32_t all;
+                asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.cta.red.and.pred q, %2, 128, p;\n\tselp.u32 %0, 1, 0, q;\n\t}" : "=r"(all) : "r"(static_cast<uint32_t>(yes)), "r"(kv ? 2 : 1) : "memory");
+                return all != 0;
+            };
+            // what the table says of this lane's key of a tile; kNoKey: it is none.  Looked at a tile later
+            auto key_of = [&](const ChunkItem &item, int i) { return tile_of(item, i) * kKeys + w * kMine + lane; };
+            auto look_up = [&](const ChunkItem &item, int i) -> int32_t {
+                const int t = key_of(item, i);
+                if (i >= item.end || lane >= kMine || t >= item.list.key_end || (t < item.list.key_low && t >= shape.sinks)) return kNoKey;
+                return reinterpret_cast<const int32_t *>(p.tables + item.r * p.table_stride)[quick_div(static_cast<uint32_t>(t), p.div_block)];
+            };
+            auto checked = [&](int32_t said) -> int32_t {
+                const bool in = said >= 0 && said < p.layer.num_blocks;
+                if (!in && said != kNoKey) atomicOr(p.status, kStatusBadIndex);
+                return in ? said : -1;
+            };
+            const char *const plane = kv ? p.layer.v : p.layer.k;
+            constexpr int chunks = DP / 16, kUnits = kMine * chunks / 32;  // 16-byte chunks of codes that a lane has of a tile
             for (int it = 0;; it++) {
                 ChunkItem item;
                 const bool took = fine && take_item(it, item);
                 if (!together(took)) break;
-                const int n_copies = 2 * max(item.end - item.begin, 0);
-                int32_t ahead = look_up(item, item.begin);
-                int64_t off = -1;
-                float next_k = 0.f, next_v = 0.f, scale_v = 0.f;
+                const bool some = item.begin < item.end;
+                float next_k = 0.f, next_v = 0.f;
                 uint32_t next_mask = 0;
-                auto fetch = [&](int u) {
-                    if (u < n_copies) {
-                        const int i = item.begin + (u >> 1);
-                        if ((u & 1) == 0) {
-                            const int32_t blk = checked(ahead);
-                            ahead = look_up(item, i + 1);
-                            off = blk >= 0 ? p.layer.geo.at(blk, place_in_block(key_of(item, i)), item.h) : -1;
-                        }
-                        const char *plane = u & 1 ? p.layer.v : p.layer.k;
+                int32_t ahead = look_up(item, item.begin);
+                // scales of this lane's key of a tile: a tile ahead of their use, and the table two.  Without boxes its codes, too: copy 2 tiles + kv
+                auto fetch = [&](int i, uint32_t tile) {
+                    const int32_t blk = checked(ahead);
+                    ahead = look_up(item, i + 1);
+                    next_k = next_v = 0.f;
+                    const int n = blk >= 0 ? place_in_block(key_of(item, i)) : 0;
+                    if (blk >= 0) {
+                        const int64_t at = p.layer.scale_geo.at(blk, n, item.h);
+                        if (!kv) next_k = *reinterpret_cast<const float *>(reinterpret_cast<const char *>(p.layer.k_scale) + at);
+                        next_v = *reinterpret_cast<const float *>(reinterpret_cast<const char *>(p.layer.v_scale) + at);
+                    }
+                    next_mask = __ballot_sync(0xffffffffu, blk >= 0);
+                    if (!p.box_rows && i < item.end) {
+                        const uint32_t u = 2 * tile + kv, slot = u % M::staged;
+                        if (fine) fine = __all_sync(0xffffffffu, staging_free(u));
+                        if (!fine) return;
+                        const int64_t off = blk >= 0 ? p.layer.geo.at(blk, n, item.h) : -1;
 #pragma unroll
-                        for (int j = 0; j < kMine * chunks / 32; j++) {
+                        for (int j = 0; j < kUnits; j++) {
                             const int idx = j * 32 + lane, rr = idx / chunks, ch = idx % chunks;
                             const int64_t src = __shfl_sync(0xffffffffu, off, rr);
                             const bool there = src >= 0 && ch * 16 < D;
-                            copy_async16(staged + (u % M::staged) * M::codes + rr * DP + ch * 16, plane + (there ? src + ch * 16 : 0), there);
+                            copy_async16(base + kStagingAt + slot * M::codes + (w * kMine + rr) * DP + ch * 16, plane + (there ? src + ch * 16 : 0), there);
                         }
+                        asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(staged_full + 8 * (u % M::staged_turns)) : "memory");
                     }
-                    copy_commit();
-                };
-                // masks and scales of a tile, a tile ahead of their use
-                auto fetch_scales = [&](int i) {
-                    next_k = next_v = 0.f;
-                    const int32_t blk = look_up(item, i);
-                    const bool there = blk >= 0 && blk < p.layer.num_blocks;
-                    if (there) {
-                        const int64_t at = p.layer.scale_geo.at(blk, place_in_block(key_of(item, i)), item.h);
-                        next_k = *reinterpret_cast<const float *>(reinterpret_cast<const char *>(p.layer.k_scale) + at);
-                        next_v = *reinterpret_cast<const float *>(reinterpret_cast<const char *>(p.layer.v_scale) + at);
-                    }
-                    next_mask = __ballot_sync(0xffffffffu, there);
                 };
                 int e_most = -133;  // the largest exponent of a tile so far
-                fetch_scales(item.begin);
-                for (int u = 0; u < M::staged - 1; u++) fetch(u);
-                if (n_copies) {
-                    // queries, fp16 with a power of two taken out of each row
-                    if (loads) fine = __all_sync(0xffffffffu, barrier_wait(q_empty, (loads - 1) & 1));
-                    for (int rr = thread; rr < kSlots * 128 && fine; rr += 128) {
+                fetch(item.begin, tiles);
+                if (some) {
+                    // queries, fp16 with a power of two taken out of each row; eight lanes have a row
+                    if (loads && fine) fine = __all_sync(0xffffffffu, barrier_wait(q_empty, (loads - 1) & 1));
+#pragma unroll 2
+                    for (int r0 = (warp - kLoad) * 4; r0 < kSlots * 128 && fine; r0 += 32) {
+                        const int rr = r0 + (lane >> 3);
+                        uint4 v[DP / 64];
                         float most = 0.f, up, down;
-#pragma unroll 4
-                        for (int j = 0; j < DP / 8; j++) {
-                            const char *src = query_at(item, rr, j);
-                            const uint4 v = src ? *reinterpret_cast<const uint4 *>(src) : make_uint4(0, 0, 0, 0);
-                            for (uint32_t x : {v.x, v.y, v.z, v.w}) most = finite_magnitude(most, query_pair(x, p.q_bf16));
+#pragma unroll
+                        for (int j = 0; j < DP / 64; j++) {
+                            const char *src = query_at(item, rr, 8 * j + (lane & 7));
+                            v[j] = src ? *reinterpret_cast<const uint4 *>(src) : make_uint4(0, 0, 0, 0);
                         }
+#pragma unroll
+                        for (int j = 0; j < DP / 64; j++)
+                            for (uint32_t x : {v[j].x, v[j].y, v[j].z, v[j].w}) most = finite_magnitude(most, query_pair(x, p.q_bf16));
+#pragma unroll
+                        for (int x = 1; x < 8; x <<= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, x));
                         query_powers(most, up, down);
-#pragma unroll 4
-                        for (int j = 0; j < DP / 8; j++) {
-                            const char *src = query_at(item, rr, j);
-                            const uint4 v = src ? *reinterpret_cast<const uint4 *>(src) : make_uint4(0, 0, 0, 0);
-                            uint32_t x[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                        for (int j = 0; j < DP / 64; j++) {
+                            uint32_t x[4] = {v[j].x, v[j].y, v[j].z, v[j].w};
 #pragma unroll
                             for (int k = 0; k < 4; k++) {
                                 const float2 f = query_pair(x[k], p.q_bf16);
                                 x[k] = pack2<__half>(f.x * up, f.y * up);
                             }
-                            *reinterpret_cast<uint4 *>(gen + (rr >> 7) * M::q_tile + swizzled(rr & 127, j)) = make_uint4(x[0], x[1], x[2], x[3]);
+                            *reinterpret_cast<uint4 *>(gen + (rr >> 7) * M::q_tile + swizzled(rr & 127, 8 * j + (lane & 7))) = make_uint4(x[0], x[1], x[2], x[3]);
                         }
-                        *reinterpret_cast<float *>(gen + kDownsAt + 4 * ((loads % M::down_sets) * kSlots * 128 + rr)) = down;
+                        if ((lane & 7) == 0) *reinterpret_cast<float *>(gen + kDownsAt + 4 * ((loads % M::down_sets) * kSlots * 128 + rr)) = down;
                     }
                     fence_shared_to_async();
                     if (fine) barrier_arrive(q_full);
                     loads++;
                 }
-                for (int v = 0; v < n_copies; v++) {
-                    const uint32_t u = copies + v, stage = u % M::stages;
-                    const int i = item.begin + (v >> 1);
-                    copy_wait<M::staged - 2>();
-                    __syncwarp();
-                    if (w == 0 && lane == 0 && (v & 1) == 0 && i == max(item.begin, item.end - 2)) barrier_arrive(wanted);
-                    if (u >= M::stages && fine) fine = __all_sync(0xffffffffu, barrier_wait(empty + 8 * stage, (u / M::stages - 1) & 1));
-                    const uint32_t about = info + (tiles % kChunkInfos) * M::info;
-                    if ((v & 1) == 0) {
-                        // the tile whose mask and scales these replace is past its last use: its V is older than this stage's last copy
-                        const float scale_k = next_k;
-                        scale_v = next_v;
+                for (int i = item.begin; i < item.end; i++, tiles++) {
+                    const uint32_t u = 2 * tiles + kv, stage = u % M::stages, slot = u % M::staged, about = info + (tiles % M::infos) * M::info;
+                    near_end(item, i);
+                    const float scale_k = next_k;
+                    float scale_v = next_v;
+                    const uint32_t mask = next_mask;
+                    fetch(i + 1, tiles + 1);
+                    if (fine) fine = __all_sync(0xffffffffu, stage_free(u));
+                    if (!kv) {
                         if (lane == 0) {
-                            if constexpr (kMine == 32) asm volatile("st.shared.u32 [%0], %1;" ::"r"(about + 4 * w), "r"(next_mask) : "memory");
-                            else asm volatile("st.shared.u16 [%0], %1;" ::"r"(about + 2 * w), "h"(static_cast<uint16_t>(next_mask)) : "memory");
-                            asm volatile("st.shared.u32 [%0], %1;" ::"r"(about + 16 + 4 * w), "r"(0) : "memory");
+                            if constexpr (kMine == 32) asm volatile("st.shared.u32 [%0], %1;" ::"r"(about + 4 * w), "r"(mask) : "memory");
+                            else asm volatile("st.shared.u16 [%0], %1;" ::"r"(about + 2 * w), "h"(static_cast<uint16_t>(mask)) : "memory");
                         }
                         if (lane < kMine) asm volatile("st.shared.f32 [%0], %1;" ::"r"(about + M::scales + 4 * (w * kMine + lane)), "f"(scale_k) : "memory");
-                        fetch_scales(i + 1);
-                        const uint32_t bits = __float_as_uint(scale_v) & 0x7fffffffu, size = bits > 0x7f800000u ? 0 : bits;  // a NaN is passed over
-                        const uint32_t warp_most = __reduce_max_sync(0xffffffffu, size), warp_least = __reduce_min_sync(0xffffffffu, size ? size : 0x7f800000u);
-                        if (lane == 0) {
-                            asm volatile("st.shared.u32 [%0], %1;" ::"r"(about + 48 + 4 * w), "r"(warp_most) : "memory");
-                            asm volatile("st.shared.u32 [%0], %1;" ::"r"(about + 64 + 4 * w), "r"(warp_least) : "memory");
-                        }
-                        fine = together(fine);  // the four warps come here for every tile, and leave together where a wait ran out
-                        if (!fine) break;
-                        uint32_t all[4], low[4];
-                        asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(all[0]), "=r"(all[1]), "=r"(all[2]), "=r"(all[3]) : "r"(about + 48));
-                        asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(low[0]), "=r"(low[1]), "=r"(low[2]), "=r"(low[3]) : "r"(about + 64));
-                        int e = static_cast<int>(max(max(all[0], all[1]), max(all[2], all[3])) >> 23) - 127 - 6;  // a tile of zeros: the least
-                        const bool far = e < e_most - 40 || static_cast<int>(min(min(low[0], low[1]), min(low[2], low[3])) >> 23) - 127 - 6 < e - 16;
-                        e_most = max(e_most, e);
-                        if (w == 0 && lane == 0) asm volatile("st.shared.v2.b32 [%0], {%1,%2};" ::"r"(about + 32), "f"(static_cast<float>(e)), "r"(static_cast<uint32_t>(far)) : "memory");
-                        if (far) {
-                            // each key's own; one of zeros takes no part in the probabilities
-                            e = static_cast<int>(size >> 23) - 127 - 6;
-                            if (lane < kMine)
-                                asm volatile("st.shared.f32 [%0], %1;" ::"r"(about + M::scales + 4 * kKeys + 4 * (w * kMine + lane)), "f"(scale_v == 0.f ? -4096.f : static_cast<float>(e)) : "memory");
-                        }
-                        // 2^-e, up to 2^133, in two factors
-                        scale_v *= __uint_as_float(static_cast<uint32_t>(127 + min(-e, 127)) << 23);
-                        scale_v *= __uint_as_float(static_cast<uint32_t>(127 + max(-e - 127, 0)) << 23);
                     }
-                    const uint32_t from = staged + (v % M::staged) * M::codes, to = ring + stage * M::tile;
-                    const uint32_t factor2 = pack2<__half>(scale_v, scale_v);
+                    // V's exponent: both groups find it, K's for the softmax, V's for the values
+                    const uint32_t bits = __float_as_uint(scale_v) & 0x7fffffffu, size = bits > 0x7f800000u ? 0 : bits;  // a NaN is passed over
+                    const uint32_t warp_most = __reduce_max_sync(0xffffffffu, size), warp_least = __reduce_min_sync(0xffffffffu, size ? size : 0x7f800000u);
+                    if (lane == 0) {
+                        asm volatile("st.shared.u32 [%0], %1;" ::"r"(about + 48 + 32 * kv + 4 * w), "r"(warp_most) : "memory");
+                        asm volatile("st.shared.u32 [%0], %1;" ::"r"(about + 64 + 32 * kv + 4 * w), "r"(warp_least) : "memory");
+                    }
+                    if (fine) fine = __all_sync(0xffffffffu, barrier_wait(staged_full + 8 * (u % M::staged_turns), (u / M::staged_turns) & 1));
+                    fine = together(fine);  // the four warps come here for every tile, and leave together where a wait ran out
+                    if (!fine) break;
+                    uint32_t all[4], low[4];
+                    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(all[0]), "=r"(all[1]), "=r"(all[2]), "=r"(all[3]) : "r"(about + 48 + 32 * kv) : "memory");
+                    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(low[0]), "=r"(low[1]), "=r"(low[2]), "=r"(low[3]) : "r"(about + 64 + 32 * kv) : "memory");
+                    int e = static_cast<int>(max(max(all[0], all[1]), max(all[2], all[3])) >> 23) - 127 - 6;  // a tile of zeros: the least
+                    const bool far = e < e_most - 40 || static_cast<int>(min(min(low[0], low[1]), min(low[2], low[3])) >> 23) - 127 - 6 < e - 16;
+                    e_most = max(e_most, e);
+                    if (!kv && w == 0 && lane == 0) asm volatile("st.shared.v2.b32 [%0], {%1,%2};" ::"r"(about + 32), "f"(static_cast<float>(e)), "r"(static_cast<uint32_t>(far)) : "memory");
+                    if (far) {
+                        // each key's own; one of zeros takes no part in the probabilities
+                        e = static_cast<int>(size >> 23) - 127 - 6;
+                        if (!kv && lane < kMine)
+                            asm volatile("st.shared.f32 [%0], %1;" ::"r"(about + M::scales + 4 * kKeys + 4 * (w * kMine + lane)), "f"(scale_v == 0.f ? -4096.f : static_cast<float>(e)) : "memory");
+                    }
+                    // 2^-e, up to 2^133, in two factors
+                    scale_v *= __uint_as_float(static_cast<uint32_t>(127 + min(-e, 127)) << 23);
+                    scale_v *= __uint_as_float(static_cast<uint32_t>(127 + max(-e - 127, 0)) << 23);
+                    const uint32_t from = base + kStagingAt + slot * M::codes + w * kMine * DP, to = ring + stage * M::tile, factor2 = pack2<__half>(scale_v, scale_v);
+                    const bool look = kv && ragged(item, i);
                     uint32_t bad = 0;
                     // four 16-byte chunks of codes at a time, loads first
 #pragma unroll
-                    for (int i0 = 0; i0 < kMine * chunks / 32 && fine; i0 += 4) {
+                    for (int j0 = 0; j0 < kUnits; j0 += 4) {
                         uint32_t c[4][4];
 #pragma unroll
                         for (int j = 0; j < 4; j++) {
-                            const int idx = (i0 + j) * 32 + lane;
-                            asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(c[j][0]), "=r"(c[j][1]), "=r"(c[j][2]), "=r"(c[j][3]) : "r"(from + idx / chunks * DP + idx % chunks * 16));
+                            const int idx = (j0 + j) * 32 + lane;
+                            asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(c[j][0]), "=r"(c[j][1]), "=r"(c[j][2]), "=r"(c[j][3]) : "r"(from + idx / chunks * DP + idx % chunks * 16) : "memory");
                         }
 #pragma unroll
                         for (int j = 0; j < 4; j++) {
-                            const int idx = (i0 + j) * 32 + lane, rr = idx / chunks, ch = idx % chunks;
+                            const int idx = (j0 + j) * 32 + lane, rr = idx / chunks, ch = idx % chunks;
                             // two 16-byte chunks; the lanes of every other 64 d's write theirs in the other order, into other banks
                             const bool odd = ch & 4;
                             uint32_t x[8];
@@ -765,13 +919,20 @@ __global__ void __launch_bounds__(kChunkThreads, 1) chunk_kernel(const __grid_co
                             widen<KIND>(odd ? c[j][3] : c[j][1], x[2], x[3]);
                             widen<KIND>(odd ? c[j][0] : c[j][2], x[4], x[5]);
                             widen<KIND>(odd ? c[j][1] : c[j][3], x[6], x[7]);
-                            if (v & 1) {
+                            if (kv) {
                                 const uint32_t f = __shfl_sync(0xffffffffu, factor2, rr);
 #pragma unroll
                                 for (int k = 0; k < 8; k++) {
                                     const __half2 y = __hmul2(*reinterpret_cast<const __half2 *>(&x[k]), *reinterpret_cast<const __half2 *>(&f));
                                     x[k] = *reinterpret_cast<const uint32_t *>(&y);
-                                    bad |= not_finite<__half>(x[k]);
+                                }
+                                if (look) {
+                                    const bool there = mask >> rr & 1;
+#pragma unroll
+                                    for (int k = 0; k < 8; k++) {
+                                        if (!there) x[k] = 0;
+                                        bad |= not_finite<__half>(x[k]);
+                                    }
                                 }
                             }
                             const uint32_t a = to + swizzled<kKeys>(w * kMine + rr, 2 * ch + odd), b = to + swizzled<kKeys>(w * kMine + rr, 2 * ch + !odd);
@@ -779,26 +940,25 @@ __global__ void __launch_bounds__(kChunkThreads, 1) chunk_kernel(const __grid_co
                             asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(b), "r"(x[4]), "r"(x[5]), "r"(x[6]), "r"(x[7]) : "memory");
                         }
                     }
-                    if ((v & 1) && __any_sync(0xffffffffu, bad != 0) && ragged(item, i) && lane == 0) asm volatile("st.shared.u32 [%0], %1;" ::"r"(about + 16 + 4 * w), "r"(1) : "memory");
+                    barrier_arrive(staged_empty + 8 * (u % M::staged_turns));
+                    if (kv) {
+                        const uint32_t any = __any_sync(0xffffffffu, bad != 0);
+                        if (lane == 0) asm volatile("st.shared.u32 [%0], %1;" ::"r"(about + 16 + 4 * w), "r"(any) : "memory");
+                    }
                     __syncwarp();
                     fence_shared_to_async();
-                    if (fine) barrier_arrive(full + 8 * stage);
-                    __syncwarp();
-                    fetch(v + M::staged - 1);
-                    tiles += v & 1;
+                    barrier_arrive(full + 8 * (u % M::turns));
                 }
-                copy_wait<0>();
-                copies += n_copies;
-                if (n_copies == 0 && w == 0 && lane == 0) barrier_arrive(wanted);
+                if (!some && warp == kLoad && lane == 0) barrier_arrive(wanted);
             }
             copy_wait<0>();
         }
     } else {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(W::other_registers));
         // ----------------------------------------------------------------------- matrix products
         // Two warps, one for each product, so that neither waits for what only the other needs.  They stay together and
         // elect the thread that issues: with uniform control the operands are uniform registers already.
-        if (warp == 12) {
+        if (warp == kIssue) {
             // a negative scale: the queries enter with the other sign
             const uint32_t qk = instruction<T>(kKeys, false) | (p.scale_log2 < 0.f ? 1u << 13 : 0u);
             uint32_t tiles = 0, loads = 0, steps[2] = {0, 0};
@@ -810,7 +970,8 @@ __global__ void __launch_bounds__(kChunkThreads, 1) chunk_kernel(const __grid_co
                 fine = __all_sync(0xffffffffu, barrier_wait(q_full, loads & 1));
                 for (int i = item.begin; i < item.end && fine; i++, tiles++) {
                     const uint32_t u = 2 * tiles, stage = u % M::stages;
-                    fine = barrier_wait(full + 8 * stage, (u / M::stages) & 1);
+                    fine = copied(u);
+                    if constexpr (KIND == kPlain) fence_shared_to_async();  // what copies key by key have written, to the products
 #pragma unroll
                     for (int slot = 0; slot < kSlots; slot++) {
                         if (!needs(item, slot, i)) continue;
@@ -839,14 +1000,14 @@ __global__ void __launch_bounds__(kChunkThreads, 1) chunk_kernel(const __grid_co
                     }
                     if (!fine) break;
                     if (elected()) {
-                        commit_to(empty + 8 * stage);
+                        commit_to(empty + 8 * (u % M::turns));
                         if (i + 1 == item.end) commit_to(q_empty);
                     }
                     __syncwarp();
                 }
                 loads++;
             }
-        } else if (warp == 13) {
+        } else if (warp == kIssue + 1) {
             const uint32_t pv = instruction<T>(DP, true);
             uint32_t tiles = 0, steps[2] = {0, 0};
             for (int it = 0; fine; it++) {
@@ -855,10 +1016,11 @@ __global__ void __launch_bounds__(kChunkThreads, 1) chunk_kernel(const __grid_co
                 bool holds[2] = {false, false};  // O of a slot holds something of this item
                 for (int i = item.begin; i < item.end && fine; i++, tiles++) {
                     const uint32_t u = 2 * tiles + 1, stage = u % M::stages;
-                    fine = __all_sync(0xffffffffu, barrier_wait(full + 8 * stage, (u / M::stages) & 1));
+                    fine = __all_sync(0xffffffffu, copied(u));
                     if (!fine) break;
+                    if constexpr (KIND == kPlain) fence_shared_to_async();
                     uint32_t bad[4];
-                    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(bad[0]), "=r"(bad[1]), "=r"(bad[2]), "=r"(bad[3]) : "r"(info + (tiles % kChunkInfos) * M::info + 16));
+                    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(bad[0]), "=r"(bad[1]), "=r"(bad[2]), "=r"(bad[3]) : "r"(info + (tiles % M::infos) * M::info + 16) : "memory");
                     const bool spoiled = __any_sync(0xffffffffu, (bad[0] | bad[1] | bad[2] | bad[3]) != 0);
                     const uint64_t v_operand = operand(ring + stage * M::tile, kKeys * 128);
 #pragma unroll
@@ -880,11 +1042,11 @@ __global__ void __launch_bounds__(kChunkThreads, 1) chunk_kernel(const __grid_co
                         steps[slot]++;
                     }
                     if (!fine) break;
-                    if (elected()) commit_to(empty + 8 * stage);
+                    if (elected()) commit_to(empty + 8 * (u % M::turns));
                     __syncwarp();
                 }
             }
-        } else if (warp == 14) {
+        } else if (warp == kIssue + 2) {
             // -------------------------------------------------------------------------- the items
             // This CTA's first is its own; then it takes over CTAs that have not been launched yet, one whenever the copies of the
             // last item near their end.
@@ -896,7 +1058,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) chunk_kernel(const __grid_co
                     // the last thread whose requests begin at or before the item, then the request
                     int t = -1;
 #pragma unroll
-                    for (int j = 0; j < kChunkThreads / 32; j++) t += __popc(__ballot_sync(0xffffffffu, items_before[j * 32 + lane] <= id));
+                    for (int j = 0; j < W::all; j++) t += __popc(__ballot_sync(0xffffffffu, items_before[j * 32 + lane] <= id));
                     uint32_t at = items_before[t], rows_at = rows_before[t];
                     const int64_t to = min((t + 1) * per, p.R);
                     ChunkItem item;
@@ -967,9 +1129,42 @@ __global__ void __launch_bounds__(kChunkThreads, 1) chunk_kernel(const __grid_co
                 more = got != 0, id = next;
             }
         }
-        if ((warp == 12 || warp == 13) && !fine) {
+        if constexpr (KIND != kPlain) {
+        if (warp == kIssue + 3 && p.box_rows) {
+            // ---------------------------------------------------------------------- pages of codes, as boxes
+            // a lane has a page of a tile; what its table says is looked up a tile ahead
+            const int pages = kKeys / p.box_rows;
+            uint32_t u = 0;
+            for (int it = 0; fine; it++) {
+                ChunkItem item;
+                if (!take_item(it, item)) break;
+                auto page_key = [&](int i) { return tile_of(item, i) * kKeys + lane * p.box_rows; };
+                auto look_up = [&](int i) -> int32_t {
+                    const int t = page_key(i);
+                    if (i >= item.end || lane >= pages || t >= item.list.key_end || (t + p.box_rows <= item.list.key_low && t >= shape.sinks)) return kNoKey;
+                    return reinterpret_cast<const int32_t *>(p.tables + item.r * p.table_stride)[quick_div(static_cast<uint32_t>(t), p.div_block)];
+                };
+                int32_t ahead = look_up(item.begin);
+                for (int i = item.begin; i < item.end && fine; i++) {
+                    const int32_t block = ahead >= 0 && ahead < p.layer.num_blocks ? ahead : static_cast<int32_t>(p.layer.num_blocks);  // past the last: zeros
+                    ahead = look_up(i + 1);
+                    const int t = page_key(i), n = t - static_cast<int>(quick_div(static_cast<uint32_t>(t), p.div_block)) * static_cast<int>(p.layer.B);
+                    for (int kv = 0; kv < 2; kv++, u++) {
+                        const uint32_t slot = u % M::staged, bar = staged_full + 8 * (u % M::staged_turns);
+                        fine = __all_sync(0xffffffffu, staging_free(u));
+                        if (!fine) break;
+                        if (lane == 0) asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "n"(kKeys * DP) : "memory");
+                        __syncwarp();
+                        if (lane < pages) copy_box(base + kStagingAt + slot * M::codes + lane * p.box_rows * DP, kv ? &p.map_v : &p.map_k, 0, n, item.h, block, bar);
+                        __syncwarp();
+                    }
+                }
+            }
+        }
+        }
+        if (warp <= kIssue + 1 && !fine) {
             // products may be in flight: let them end before the tensor memory is given back
-            const uint32_t last = last_at + 8 * (warp - 12);
+            const uint32_t last = last_at + 8 * (warp - kIssue);
             if (elected()) commit_to(last);
             __syncwarp();
             barrier_wait(last, 0);
@@ -978,7 +1173,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) chunk_kernel(const __grid_co
     if (!fine) atomicOr(p.status, static_cast<unsigned int>(TC_DEVICE_BULK_WAIT_TIMEOUT));
     fence_before();
     __syncthreads();
-    if (warp == 12) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tensor) : "memory");
+    if (warp == kIssue) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tensor) : "memory");
 }
 
 template <typename T, int KIND, int DP>
@@ -990,9 +1185,14 @@ int launch_chunk_shape(const ChunkParams &p, int device, cudaStream_t s)
     if (!raised[device].load(std::memory_order_relaxed)) {
         const cudaError_t e = cudaFuncSetAttribute(chunk_kernel<T, KIND, DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, M::bytes);
         if (e != cudaSuccess) return cuda_fail(e, "cudaFuncSetAttribute(dynamic shared memory)");
+        // the warps' shares of registers must not be more than a CTA is launched with
+        cudaFuncAttributes attr;
+        const cudaError_t f = cudaFuncGetAttributes(&attr, chunk_kernel<T, KIND, DP>);
+        if (f != cudaSuccess) return cuda_fail(f, "cudaFuncGetAttributes");
+        if (attr.numRegs != ChunkWarps<KIND>::launch_registers) return fail(TC_ERR_CUDA, "tc_attn_chunk's kernel was built with %d registers a thread, not %d", attr.numRegs, ChunkWarps<KIND>::launch_registers);
         raised[device].store(true, std::memory_order_relaxed);
     }
-    return launch_attn(chunk_kernel<T, KIND, DP>, static_cast<unsigned>(p.plan.grid), kChunkThreads, M::bytes, false, p, s);
+    return launch_attn(chunk_kernel<T, KIND, DP>, static_cast<unsigned>(p.plan.grid), ChunkWarps<KIND>::threads, M::bytes, false, p, s);
 }
 
 template <typename T, int KIND>

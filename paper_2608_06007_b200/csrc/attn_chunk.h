@@ -1,6 +1,8 @@
 // The arguments of tc_attn_chunk's kernels: shared by the entry points and the kernels' launchers.
 #pragma once
 
+#include <cuda.h>
+
 #include "attn_chunk_split.h"
 #include "ops.h"
 
@@ -26,6 +28,10 @@ struct ChunkParams {
     uint2 *cuts;  // of every request that has items: the first of its parts' rows, and the number of its parts
     float *sums, *parts;
     unsigned int *status;
+    // Where blocks and tiles fit into one another, pages are fetched as boxes of box_rows tokens of one head; 0: key by key.
+    int32_t box_rows;
+    FastDiv div_box;
+    CUtensorMap map_k, map_v;
 };
 constexpr uint32_t kUncut = 0xffffffffu;
 

@@ -89,16 +89,14 @@ static int launch_chunk(const ChunkParams &p, int dtype, int device, cudaStream_
     return p.layer.D <= 128 ? launch_attn(chunk_join_kernel<T, 128>, grid, 128, 0, true, p, s) : launch_attn(chunk_join_kernel<T, 256>, grid, 128, 0, true, p, s);
 }
 
-// Pages as tensors [block][head][token][d]: where tiles are whole numbers of blocks, or blocks of tiles, so that a
-// box of a page's tokens is part of one tile.  Elsewhere box_rows stays 0.
+// Pages of an unquantised pool as tensors [block][head][token][d]: where half tiles are whole numbers of blocks, or blocks of half tiles, so that a
+// box of a page's tokens is part of one.  Elsewhere box_rows stays 0.
 static int describe_pages(ChunkParams *p)
 {
     p->box_rows = 0;
     const Layer &l = p->layer;
-    const bool codes = l.quantised();
-    const int32_t keys = p->shape.keys, most = codes ? keys : keys / 2;  // of an unquantised tile, two warps fetch half each
-    const int32_t rows = static_cast<int32_t>(std::min<int64_t>(l.B, most));
-    if (rows < 8 || most % rows || l.B % rows || l.num_blocks < 1 || l.geo.block >= (1ll << 40)) return TC_OK;
+    const int32_t most = p->shape.keys / 2, rows = static_cast<int32_t>(std::min<int64_t>(l.B, most));
+    if (l.quantised() || rows < 8 || most % rows || l.B % rows || l.num_blocks < 1 || l.geo.block >= (1ll << 40)) return TC_OK;
     using Encode = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *, const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
                                 CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
     static std::atomic<Encode> known;  // looked up once; twice does no harm
@@ -112,12 +110,12 @@ static int describe_pages(ChunkParams *p)
         encode = reinterpret_cast<Encode>(f);
         known.store(encode, std::memory_order_relaxed);
     }
-    const CUtensorMapDataType type = codes ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : l.dtype == TC_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
+    const CUtensorMapDataType type = l.dtype == TC_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
     const cuuint64_t extent[4] = {static_cast<cuuint64_t>(l.D), l.B, static_cast<cuuint64_t>(l.H), static_cast<cuuint64_t>(l.num_blocks)};
     const cuuint64_t stride[3] = {static_cast<cuuint64_t>(l.geo.token), static_cast<cuuint64_t>(l.geo.head), static_cast<cuuint64_t>(l.geo.block)};
-    const cuuint32_t padded = l.D <= 64 ? 64 : l.D <= 128 ? 128 : 256, box[4] = {codes ? padded : 64, static_cast<cuuint32_t>(rows), 1, 1}, step[4] = {1, 1, 1, 1};
+    const cuuint32_t box[4] = {64, static_cast<cuuint32_t>(rows), 1, 1}, step[4] = {1, 1, 1, 1};
     for (int v = 0; v < 2; v++)
-        if (encode(v ? &p->map_v : &p->map_k, type, 4, v ? l.v : l.k, extent, stride, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, codes ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B,
+        if (encode(v ? &p->map_v : &p->map_k, type, 4, v ? l.v : l.k, extent, stride, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
                    CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
             return TC_OK;  // a geometry that tensor maps do not hold
     p->box_rows = rows;

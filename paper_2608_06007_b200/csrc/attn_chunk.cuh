@@ -15,7 +15,7 @@ constexpr float kChunkLn2 = 0.6931471805599453f;
 template <int KIND> struct ChunkWarps {
     static constexpr int softmax = 8, loaders = KIND == kPlain ? 4 : 8, all = softmax + loaders + 4, threads = 32 * all;
     // registers of a thread: at the launch, of the softmax, of the others
-    static constexpr int launch_registers = KIND == kPlain ? 128 : 96, softmax_registers = KIND == kPlain ? 192 : 168, other_registers = KIND == kPlain ? 64 : 48;
+    static constexpr int launch_registers = KIND == kPlain ? 128 : 96, softmax_registers = KIND == kPlain ? 192 : 112, other_registers = KIND == kPlain ? 64 : 80;
     static_assert(32 * softmax * softmax_registers + (threads - 32 * softmax) * other_registers <= threads * launch_registers && threads * launch_registers <= 65536, "a split that never ends");
 };
 
@@ -24,11 +24,7 @@ struct ChunkMemory {
     static constexpr int slots = DP > 128 ? 1 : 2, keys = DP > 128 ? 64 : 128;
     static constexpr int tile = keys * DP * 2, q_tile = 128 * DP * 2;  // bytes
     static constexpr int queries = slots * q_tile;
-    static constexpr int stages = KIND == kPlain ? (DP == 64 ? 6 : 4) : (DP == 64 ? 4 : 3);  // K and V in turn
-    // A copy's barriers: K and V have their own warps, which must not share a barrier, since neither sees all of the other's phases.
-    static constexpr int turns = stages % 2 ? 2 * stages : stages;
-    // tiles as they lie in the pool, and the barriers of those
-    static constexpr int codes = KIND == kPlain ? 0 : keys * DP, staged = KIND == kPlain ? 0 : 3, staged_turns = 6;
+    static constexpr int stages = DP == 64 ? 6 : 4;  // K and V in turn, so that each stage is always one's
     // Tiles whose masks and scales are kept: those of a tile must not be replaced before its last product is issued, and
     // K and V have their own warps, of which K's may be four tiles ahead.
     static constexpr int infos = 8;
@@ -42,7 +38,7 @@ struct ChunkMemory {
     static constexpr int rest = infos * info + downs + table + 2 * item + 16 + 512;
     // more than half of an SM's, so that no two CTAs meet on one: the second would wait for tensor memory with an item in hand
     static constexpr int least = 120 * 1024;
-    static constexpr int used = queries + stages * tile + staged * codes + rest + 1024;
+    static constexpr int used = queries + stages * tile + rest + 1024;
     static constexpr int bytes = used > least ? used : least;
 };
 
@@ -208,13 +204,13 @@ __global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(con
     allow_next();
     const uint32_t base = (static_cast<uint32_t>(__cvta_generic_to_shared(raw)) + 1023) & ~1023u;
     unsigned char *const gen = raw + (base - static_cast<uint32_t>(__cvta_generic_to_shared(raw)));
-    constexpr int kRingAt = M::queries, kStagingAt = kRingAt + M::stages * M::tile, kInfoAt = kStagingAt + M::staged * M::codes, kDownsAt = kInfoAt + M::infos * M::info, kTableAt = kDownsAt + M::downs,
+    constexpr int kRingAt = M::queries, kInfoAt = kRingAt + M::stages * M::tile, kDownsAt = kInfoAt + M::infos * M::info, kTableAt = kDownsAt + M::downs,
                   kItemsAt = kTableAt + M::table, kAnswerAt = kItemsAt + 2 * M::item, kBarsAt = kAnswerAt + 16;
     static_assert(kInfoAt % 16 == 0 && kItemsAt % 16 == 0 && kAnswerAt % 16 == 0);
     const uint32_t ring = base + kRingAt, info = base + kInfoAt;
-    const uint32_t full = base + kBarsAt, empty = full + 8 * M::turns, s_full = empty + 8 * M::turns, s_taken = s_full + 16, p_ready = s_taken + 16, o_added = p_ready + 16;
-    const uint32_t q_full = o_added + 16, q_empty = q_full + 8, item_full = q_empty + 8, item_empty = item_full + 16, wanted = item_empty + 16, answered = wanted + 8, last_at = answered + 8, landed = last_at + 16, staged_full = landed + 16, staged_empty = staged_full + 8 * M::staged_turns, tensor_at = staged_empty + 8 * M::staged_turns;
-    static_assert(8 * (2 * M::turns + 20 + 2 * M::staged_turns) + 8 <= 512);
+    const uint32_t full = base + kBarsAt, empty = full + 8 * M::stages, s_full = empty + 8 * M::stages, s_taken = s_full + 16, p_ready = s_taken + 16, o_added = p_ready + 16;
+    const uint32_t q_full = o_added + 16, q_empty = q_full + 8, item_full = q_empty + 8, item_empty = item_full + 16, wanted = item_empty + 16, answered = wanted + 8, last_at = answered + 8, landed = last_at + 16, tensor_at = landed + 16;
+    static_assert(8 * (2 * M::stages + 20) + 8 <= 512);
     uint32_t *const items_before = reinterpret_cast<uint32_t *>(gen + kTableAt), *const rows_before = items_before + W::threads;
     ChunkItem *const items = reinterpret_cast<ChunkItem *>(gen + kItemsAt);
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31, D = p.layer.D, H = p.layer.H;
@@ -223,11 +219,10 @@ __global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(con
     if (threadIdx.x == 0) {
         // boxes announce themselves to whoever waits for their bytes; copies key by key for their lanes, and a lane of each warp what it has written beside them
         const int ready = KIND != kPlain ? 128 : p.box_rows ? 2 : 2 * 33;
-        for (int i = 0; i < M::turns; i++) barrier_init(full + 8 * i, ready), barrier_init(empty + 8 * i, 1);
+        for (int i = 0; i < M::stages; i++) barrier_init(full + 8 * i, ready), barrier_init(empty + 8 * i, 1);
         for (int i = 0; i < 2; i++) barrier_init(landed + 8 * i, 1);
-        for (int i = 0; i < M::staged_turns; i++) barrier_init(staged_full + 8 * i, p.box_rows ? 1 : 128), barrier_init(staged_empty + 8 * i, 128);
         for (int i = 0; i < 2; i++) barrier_init(s_full + 8 * i, 1), barrier_init(s_taken + 8 * i, 128), barrier_init(p_ready + 8 * i, 128), barrier_init(o_added + 8 * i, 1);
-        for (int i = 0; i < 2; i++) barrier_init(item_full + 8 * i, 1), barrier_init(item_empty + 8 * i, kSlots * 4 + W::loaders + 2 + (KIND != kPlain && p.box_rows ? 1 : 0)), barrier_init(last_at + 8 * i, 1);
+        for (int i = 0; i < 2; i++) barrier_init(item_full + 8 * i, 1), barrier_init(item_empty + 8 * i, kSlots * 4 + W::loaders + 2), barrier_init(last_at + 8 * i, 1);
         barrier_init(q_full, KIND == kPlain ? 4 * 33 : 256), barrier_init(q_empty, 1), barrier_init(wanted, 1), barrier_init(answered, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -321,7 +316,10 @@ __global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(con
     __syncthreads();
     fence_after();
     // All 512 columns are this CTA's, so they begin at 0; a constant lets the products' operands stay in uniform registers.
-    constexpr uint32_t tensor = 0, kScores = 0, kProbabilities = 128, kOutputs = 256;
+    // A softmax holds a tile's scores in registers and gives their one buffer back at once, beside the two slots' probabilities;
+    // of codes, whose warps leave it few registers, it goes through them twice where they lie, and puts the probabilities in their place.
+    constexpr bool kInPlace = KIND != kPlain && kSlots == 2;
+    constexpr uint32_t tensor = 0, kScores = 0, kScoresStep = kInPlace ? 128 : 0, kProbabilities = kInPlace ? 0 : 128, kProbabilitiesStep = kInPlace ? 128 : 64, kOutputs = 256;
     bool fine = true;  // no wait of this thread has run out
 
     // Item `it` of this CTA's; false when there is none, or a wait ran out.
@@ -338,12 +336,9 @@ __global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(con
         if (lane == 0) barrier_arrive(item_empty + 8 * (it & 1));
         return item.valid != 0;
     };
-    // Whether the place of copy u among the staged codes is done with.
-    auto staging_free = [&](uint32_t u) { return u < 3 || barrier_wait(staged_empty + 8 * ((u - 3) % M::staged_turns), ((u - 3) / M::staged_turns) & 1); };
-    static_assert(M::staged == 0 || M::staged == 3);
     // Copy u (K of this CTA's tile u / 2, then V) is in stage u % stages: whether it is there, and whether copy u - stages is done with.
-    auto copied = [&](uint32_t u) { return barrier_wait(full + 8 * (u % M::turns), (u / M::turns) & 1); };
-    auto stage_free = [&](uint32_t u) { return u < M::stages || barrier_wait(empty + 8 * ((u - M::stages) % M::turns), ((u - M::stages) / M::turns) & 1); };
+    auto copied = [&](uint32_t u) { return barrier_wait(full + 8 * (u % M::stages), (u / M::stages) & 1); };
+    auto stage_free = [&](uint32_t u) { return u < M::stages || barrier_wait(empty + 8 * (u % M::stages), (u / M::stages - 1) & 1); };
     auto tile_of = [](const ChunkItem &item, int i) { return i < item.list.firsts ? i : i + item.list.skip; };
     // Does slot `slot` need tile i of the list?
     auto needs = [](const ChunkItem &item, int slot, int i) {
@@ -360,7 +355,7 @@ __global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(con
         // ---------------------------------------------------------------------------- softmax
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(W::softmax_registers));
         const int slot = warp >> 2, r = (warp & 3) * 32 + lane;
-        const uint32_t lanes = tensor + (static_cast<uint32_t>((warp & 3) * 32) << 16), p_at = lanes + kProbabilities + slot * 64, o_at = lanes + kOutputs + slot * 128;
+        const uint32_t lanes = tensor + (static_cast<uint32_t>((warp & 3) * 32) << 16), p_at = lanes + kProbabilities + slot * kProbabilitiesStep, o_at = lanes + kOutputs + slot * 128;
         uint32_t steps = 0, tiles = 0, loads = 0;  // of this slot; of the CTA; items that had queries
         for (int it = 0; slot < kSlots && fine; it++) {
             ChunkItem item;
@@ -399,7 +394,7 @@ __global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(con
             for (int i = item.begin; i < item.end && fine; i++, tiles++) {
                 if (!needs(item, slot, i)) continue;
                 // one slot: the scores have two buffers in turn
-                const uint32_t b = kSlots == 1 ? steps & 1 : slot, parity = kSlots == 1 ? (steps >> 1) & 1 : steps & 1, s_at = lanes + kScores + (kSlots == 1 ? (steps & 1) * kKeys : 0);
+                const uint32_t b = kSlots == 1 ? steps & 1 : slot, parity = kSlots == 1 ? (steps >> 1) & 1 : steps & 1, s_at = lanes + kScores + slot * kScoresStep + (kSlots == 1 ? (steps & 1) * kKeys : 0);
                 fine = __all_sync(0xffffffffu, barrier_wait(s_full + 8 * b, parity));
                 if (!fine) break;
                 fence_after();
@@ -422,13 +417,6 @@ __global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(con
                         scale_outputs(f);
                     }
                 };
-                union {
-                    uint32_t w[kWords][32];
-                    float f[kWords][32];
-                    float2 f2[kWords][16];
-                } s;
-#pragma unroll
-                for (int c = 0; c < kWords; c++) tensor_load32(s_at + 32 * c, s.w[c]);
                 const bool edge = ragged(item, i);
                 RowView view{about, 1 << 30, -(1 << 30), 0};
                 if (edge) {
@@ -446,7 +434,6 @@ __global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(con
                     }
                 }
                 if (KIND != kPlain && far) {
-                    tensor_loaded();
                     const uint32_t scales = about + M::scales;
                     const float2 maxima = far_maxima<kKeys>(s_at, view, scales, scales + 4 * kKeys, factor);
                     raise_ref(maxima.x);
@@ -457,7 +444,76 @@ __global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(con
                     tensor_stored();
                     fence_before();
                     barrier_arrive(s_taken + 8 * b);
+                } else if constexpr (KIND != kPlain) {
+                    // 32 scores at a time, in a loop whose code stays small: six warps of four kinds share a scheduler's instruction cache
+                    auto scores = [&](int c, float2 (&x)[16]) {
+                        tensor_load32(s_at + 32 * c, reinterpret_cast<uint32_t(&)[32]>(x));
+                        const uint32_t word = view.word(c);
+                        tensor_loaded();
+                        const float2 f2 = make_float2(factor, factor), zero = make_float2(0.f, 0.f);
+#pragma unroll
+                        for (int j = 0; j < 8; j++) {
+                            const float4 k = load_shared_f4(about + M::scales + 128 * c + 16 * j);
+                            x[2 * j] = fused2(x[2 * j], fused2(f2, make_float2(k.x, k.y), zero), zero);
+                            x[2 * j + 1] = fused2(x[2 * j + 1], fused2(f2, make_float2(k.z, k.w), zero), zero);
+                        }
+                        if (word != 0xffffffffu) {
+#pragma unroll
+                            for (int j = 0; j < 16; j++) {
+                                if (!(word >> (2 * j) & 1)) x[j].x = -INFINITY;
+                                if (!(word >> (2 * j + 1) & 1)) x[j].y = -INFINITY;
+                            }
+                        }
+                    };
+                    float highest = -INFINITY;
+#pragma unroll 1
+                    for (int c = 0; c < kWords; c++) {
+                        float2 x[16];
+                        scores(c, x);
+                        float m2[2] = {highest, -INFINITY};
+#pragma unroll
+                        for (int j = 0; j < 16; j++) m2[j & 1] = larger3(m2[j & 1], x[j].x, x[j].y);
+                        highest = fmaxf(m2[0], m2[1]);
+                    }
+                    const float most = highest + exponent;
+                    // a running maximum moves only when a score exceeds it by more than 8 (2^8 in probabilities)
+                    if (__any_sync(0xffffffffu, most > top + 8.f || highest > ref + 8.f)) {
+                        raise_ref(highest);
+                        move_top(most);
+                    }
+                    if constexpr (!kInPlace) await_rest();  // P is free
+                    if (!fine) break;
+                    const float m = top == -INFINITY ? 0.f : top - kLift;
+                    const float2 minus = make_float2(exponent - m, exponent - m);
+                    float2 here = make_float2(0.f, 0.f);
+#pragma unroll 1
+                    for (int c = 0; c < kWords; c++) {
+                        float2 x[16];
+                        scores(c, x);
+                        uint32_t w[16];
+#pragma unroll
+                        for (int j = 0; j < 16; j++) {
+                            float2 e = sum2(x[j], minus);
+                            e = make_float2(exp2_approx(e.x), exp2_approx(e.y));
+                            here = sum2(here, e);
+                            w[j] = pack2<T>(e.x, e.y);
+                        }
+                        tensor_store16(p_at + 16 * c, w);  // in place: 16 columns of the 32 c that have been read
+                    }
+                    // `here` is relative to m - exponent, which is at most 48 above ref: exponent is no less than 40 below any before
+                    const float all = here.x + here.y;
+                    sum.x = fmaf(all, all == 0.f ? 0.f : exp2_approx(m - exponent - (ref == -INFINITY ? 0.f : ref)), sum.x);
+                    tensor_stored();
+                    fence_before();
+                    barrier_arrive(s_taken + 8 * b);
                 } else {
+                    union {
+                        uint32_t w[kWords][32];
+                        float f[kWords][32];
+                        float2 f2[kWords][16];
+                    } s;
+#pragma unroll
+                    for (int c = 0; c < kWords; c++) tensor_load32(s_at + 32 * c, s.w[c]);
                     uint32_t mask[kWords], all_seen = 0xffffffffu;
 #pragma unroll
                     for (int c = 0; c < kWords; c++) asm volatile("ld.shared.u32 %0, [%1];" : "=r"(mask[c]) : "r"(about + 4 * c));
@@ -467,16 +523,6 @@ __global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(con
                     if (edge) {
 #pragma unroll
                         for (int c = 0; c < kWords; c++) mask[c] = view.word(c);
-                    }
-                    if constexpr (KIND != kPlain) {
-                        const float2 f2 = make_float2(factor, factor), zero = make_float2(0.f, 0.f);
-#pragma unroll
-                        for (int j = 0; j < kKeys / 4; j++) {
-                            const float4 k = load_shared_f4(about + M::scales + 16 * j);
-                            float2 *x = &s.f2[j / 8][j % 8 * 2];
-                            x[0] = fused2(x[0], fused2(f2, make_float2(k.x, k.y), zero), zero);
-                            x[1] = fused2(x[1], fused2(f2, make_float2(k.z, k.w), zero), zero);
-                        }
                     }
 #pragma unroll
                     for (int c = 0; c < kWords; c++) all_seen &= mask[c];
@@ -494,34 +540,23 @@ __global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(con
 #pragma unroll
                         for (int j = 2; j < 32; j += 2) m4[c] = larger3(m4[c], s.f[c][j], s.f[c][j + 1]);
                     }
-                    const float highest = fmaxf(larger3(m4[0], m4[1], m4[2]), m4[3]), most = KIND == kPlain ? highest * factor : highest + exponent;
-                    bool move = most > top + 8.f;
-                    if constexpr (KIND != kPlain) move = move || highest > ref + 8.f;
+                    const float highest = fmaxf(larger3(m4[0], m4[1], m4[2]), m4[3]), most = highest * factor;
                     // a running maximum moves only when a score exceeds it by more than 8 (2^8 in probabilities)
-                    if (__any_sync(0xffffffffu, move)) {
-                        if constexpr (KIND != kPlain) raise_ref(highest);
-                        move_top(most);
-                    }
+                    if (__any_sync(0xffffffffu, most > top + 8.f)) move_top(most);
                     const float m = top == -INFINITY ? 0.f : top - kLift;
-                    const float2 minus = make_float2(exponent - m, exponent - m), f2 = make_float2(factor, factor);
+                    const float2 minus = make_float2(-m, -m), f2 = make_float2(factor, factor);
                     float2 here = make_float2(0.f, 0.f);
 #pragma unroll
                     for (int c = 0; c < kWords; c++) {
 #pragma unroll
                         for (int j = 0; j < 16; j++) {
-                            float2 e = KIND == kPlain ? fused2(s.f2[c][j], f2, minus) : sum2(s.f2[c][j], minus);
+                            float2 e = fused2(s.f2[c][j], f2, minus);
                             e = make_float2(exp2_approx(e.x), exp2_approx(e.y));
                             here = sum2(here, e);
                             s.w[c][j] = pack2<T>(e.x, e.y);  // (in the place of scores that are done with)
                         }
                     }
-                    if constexpr (KIND == kPlain) {
-                        sum = sum2(sum, here);
-                    } else {
-                        // `here` is relative to m - exponent, which is at most 48 above ref: exponent is no less than 40 below any before
-                        const float all = here.x + here.y;
-                        sum.x = fmaf(all, all == 0.f ? 0.f : exp2_approx(m - exponent - (ref == -INFINITY ? 0.f : ref)), sum.x);
-                    }
+                    sum = sum2(sum, here);
                     await_rest();  // by now it has been given, as a rule
                     if (!fine) break;
 #pragma unroll
@@ -667,7 +702,7 @@ __global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(con
                 for (int i = item.begin; i < item.end && fine; i++, tiles++) {
                     near_end(item, i);
                     const int t0 = first_key(item, i);
-                    const uint32_t u = 2 * tiles + kv, stage = u % M::stages, bar = full + 8 * (u % M::turns), about = info + (tiles % M::infos) * M::info, to = ring + stage * M::tile;
+                    const uint32_t u = 2 * tiles + kv, stage = u % M::stages, bar = full + 8 * (u % M::stages), about = info + (tiles % M::infos) * M::info, to = ring + stage * M::tile;
                     int32_t blk[kHalfWords];
                     uint32_t mask[kHalfWords];
                     blk[0] = checked(ahead[0]);
@@ -755,8 +790,7 @@ __global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(con
             }
             copy_wait<0>();
         } else {
-            // Codes: pages are staged as they lie in the pool, as boxes by a warp of their own or in chunks of 16 bytes by those that widen
-            // them: four warps K, four V, each its own keys of every tile.  V's are multiplied by their scales over a
+            // Codes: four warps fetch and widen K, four V, each its own keys of every tile, through registers, a tile ahead.  V's are multiplied by their scales over a
             // power of two that the tile's largest scale sets, 2^exponent, which puts the values below 2^16: rounded
             // to fp16 twice (the factor and the product), half a step of 2^-11 each, like the probabilities
             // that they meet.  Products below fp16's normal numbers are off by half of 2^-24, which is 2^-15 of the
@@ -784,43 +818,40 @@ __global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(con
             };
             const char *const plane = kv ? p.layer.v : p.layer.k;
             constexpr int chunks = DP / 16, kUnits = kMine * chunks / 32;  // 16-byte chunks of codes that a lane has of a tile
+            uint4 codes[kUnits];
             for (int it = 0;; it++) {
                 ChunkItem item;
                 const bool took = fine && take_item(it, item);
                 if (!together(took)) break;
                 const bool some = item.begin < item.end;
+                int64_t next_off = -1;
                 float next_k = 0.f, next_v = 0.f;
                 uint32_t next_mask = 0;
                 int32_t ahead = look_up(item, item.begin);
-                // scales of this lane's key of a tile: a tile ahead of their use, and the table two.  Without boxes its codes, too: copy 2 tiles + kv
-                auto fetch = [&](int i, uint32_t tile) {
+                // where this lane's key of a tile is, and its scales: a tile ahead of their use, and the table two
+                auto fetch = [&](int i) {
                     const int32_t blk = checked(ahead);
                     ahead = look_up(item, i + 1);
-                    next_k = next_v = 0.f;
-                    const int n = blk >= 0 ? place_in_block(key_of(item, i)) : 0;
+                    next_off = -1, next_k = next_v = 0.f;
                     if (blk >= 0) {
+                        const int n = place_in_block(key_of(item, i));
+                        next_off = p.layer.geo.at(blk, n, item.h);
                         const int64_t at = p.layer.scale_geo.at(blk, n, item.h);
                         if (!kv) next_k = *reinterpret_cast<const float *>(reinterpret_cast<const char *>(p.layer.k_scale) + at);
                         next_v = *reinterpret_cast<const float *>(reinterpret_cast<const char *>(p.layer.v_scale) + at);
                     }
                     next_mask = __ballot_sync(0xffffffffu, blk >= 0);
-                    if (!p.box_rows && i < item.end) {
-                        const uint32_t u = 2 * tile + kv, slot = u % M::staged;
-                        if (fine) fine = __all_sync(0xffffffffu, staging_free(u));
-                        if (!fine) return;
-                        const int64_t off = blk >= 0 ? p.layer.geo.at(blk, n, item.h) : -1;
-#pragma unroll
-                        for (int j = 0; j < kUnits; j++) {
-                            const int idx = j * 32 + lane, rr = idx / chunks, ch = idx % chunks;
-                            const int64_t src = __shfl_sync(0xffffffffu, off, rr);
-                            const bool there = src >= 0 && ch * 16 < D;
-                            copy_async16(base + kStagingAt + slot * M::codes + (w * kMine + rr) * DP + ch * 16, plane + (there ? src + ch * 16 : 0), there);
-                        }
-                        asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(staged_full + 8 * (u % M::staged_turns)) : "memory");
-                    }
+                };
+                auto load_unit = [&](int j) {
+                    const int idx = j * 32 + lane, rr = idx / chunks, ch = idx % chunks;
+                    const int64_t src = __shfl_sync(0xffffffffu, next_off, rr);
+                    codes[j] = make_uint4(0, 0, 0, 0);
+                    if (src >= 0 && ch * 16 < D) codes[j] = *reinterpret_cast<const uint4 *>(plane + src + ch * 16);
                 };
                 int e_most = -133;  // the largest exponent of a tile so far
-                fetch(item.begin, tiles);
+                fetch(item.begin);
+#pragma unroll
+                for (int j = 0; j < kUnits; j++) load_unit(j);
                 if (some) {
                     // queries, fp16 with a power of two taken out of each row; eight lanes have a row
                     if (loads && fine) fine = __all_sync(0xffffffffu, barrier_wait(q_empty, (loads - 1) & 1));
@@ -857,12 +888,12 @@ __global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(con
                     loads++;
                 }
                 for (int i = item.begin; i < item.end; i++, tiles++) {
-                    const uint32_t u = 2 * tiles + kv, stage = u % M::stages, slot = u % M::staged, about = info + (tiles % M::infos) * M::info;
+                    const uint32_t u = 2 * tiles + kv, stage = u % M::stages, about = info + (tiles % M::infos) * M::info;
                     near_end(item, i);
                     const float scale_k = next_k;
                     float scale_v = next_v;
                     const uint32_t mask = next_mask;
-                    fetch(i + 1, tiles + 1);
+                    fetch(i + 1);
                     if (fine) fine = __all_sync(0xffffffffu, stage_free(u));
                     if (!kv) {
                         if (lane == 0) {
@@ -878,7 +909,6 @@ __global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(con
                         asm volatile("st.shared.u32 [%0], %1;" ::"r"(about + 48 + 32 * kv + 4 * w), "r"(warp_most) : "memory");
                         asm volatile("st.shared.u32 [%0], %1;" ::"r"(about + 64 + 32 * kv + 4 * w), "r"(warp_least) : "memory");
                     }
-                    if (fine) fine = __all_sync(0xffffffffu, barrier_wait(staged_full + 8 * (u % M::staged_turns), (u / M::staged_turns) & 1));
                     fine = together(fine);  // the four warps come here for every tile, and leave together where a wait ran out
                     if (!fine) break;
                     uint32_t all[4], low[4];
@@ -897,61 +927,46 @@ __global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(con
                     // 2^-e, up to 2^133, in two factors
                     scale_v *= __uint_as_float(static_cast<uint32_t>(127 + min(-e, 127)) << 23);
                     scale_v *= __uint_as_float(static_cast<uint32_t>(127 + max(-e - 127, 0)) << 23);
-                    const uint32_t from = base + kStagingAt + slot * M::codes + w * kMine * DP, to = ring + stage * M::tile, factor2 = pack2<__half>(scale_v, scale_v);
+                    const uint32_t to = ring + stage * M::tile, factor2 = kv ? pack2<__half>(scale_v, scale_v) : 0x3c003c00u;
                     const bool look = kv && ragged(item, i);
                     uint32_t bad = 0;
-                    // four 16-byte chunks of codes at a time, loads first
+                    // one way for K, times 1, and V: the code of both groups stays in the instruction cache
 #pragma unroll
-                    for (int j0 = 0; j0 < kUnits; j0 += 4) {
-                        uint32_t c[4][4];
+                    for (int j = 0; j < kUnits; j++) {
+                        const int idx = j * 32 + lane, rr = idx / chunks, ch = idx % chunks;
+                        // two 16-byte chunks; the lanes of every other 64 d's write theirs in the other order, into other banks
+                        const bool odd = ch & 4;
+                        const uint4 c = codes[j];
+                        uint32_t x[8];
+                        widen<KIND>(odd ? c.z : c.x, x[0], x[1]);
+                        widen<KIND>(odd ? c.w : c.y, x[2], x[3]);
+                        widen<KIND>(odd ? c.x : c.z, x[4], x[5]);
+                        widen<KIND>(odd ? c.y : c.w, x[6], x[7]);
+                        load_unit(j);
+                        const uint32_t f = __shfl_sync(0xffffffffu, factor2, rr);
 #pragma unroll
-                        for (int j = 0; j < 4; j++) {
-                            const int idx = (j0 + j) * 32 + lane;
-                            asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(c[j][0]), "=r"(c[j][1]), "=r"(c[j][2]), "=r"(c[j][3]) : "r"(from + idx / chunks * DP + idx % chunks * 16) : "memory");
+                        for (int k = 0; k < 8; k++) {
+                            const __half2 y = __hmul2(*reinterpret_cast<const __half2 *>(&x[k]), *reinterpret_cast<const __half2 *>(&f));
+                            x[k] = *reinterpret_cast<const uint32_t *>(&y);
                         }
+                        if (look) {
 #pragma unroll
-                        for (int j = 0; j < 4; j++) {
-                            const int idx = (j0 + j) * 32 + lane, rr = idx / chunks, ch = idx % chunks;
-                            // two 16-byte chunks; the lanes of every other 64 d's write theirs in the other order, into other banks
-                            const bool odd = ch & 4;
-                            uint32_t x[8];
-                            widen<KIND>(odd ? c[j][2] : c[j][0], x[0], x[1]);
-                            widen<KIND>(odd ? c[j][3] : c[j][1], x[2], x[3]);
-                            widen<KIND>(odd ? c[j][0] : c[j][2], x[4], x[5]);
-                            widen<KIND>(odd ? c[j][1] : c[j][3], x[6], x[7]);
-                            if (kv) {
-                                const uint32_t f = __shfl_sync(0xffffffffu, factor2, rr);
-#pragma unroll
-                                for (int k = 0; k < 8; k++) {
-                                    const __half2 y = __hmul2(*reinterpret_cast<const __half2 *>(&x[k]), *reinterpret_cast<const __half2 *>(&f));
-                                    x[k] = *reinterpret_cast<const uint32_t *>(&y);
-                                }
-                                if (look) {
-                                    const bool there = mask >> rr & 1;
-#pragma unroll
-                                    for (int k = 0; k < 8; k++) {
-                                        if (!there) x[k] = 0;
-                                        bad |= not_finite<__half>(x[k]);
-                                    }
-                                }
-                            }
-                            const uint32_t a = to + swizzled<kKeys>(w * kMine + rr, 2 * ch + odd), b = to + swizzled<kKeys>(w * kMine + rr, 2 * ch + !odd);
-                            asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(a), "r"(x[0]), "r"(x[1]), "r"(x[2]), "r"(x[3]) : "memory");
-                            asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(b), "r"(x[4]), "r"(x[5]), "r"(x[6]), "r"(x[7]) : "memory");
+                            for (int k = 0; k < 8; k++) bad |= not_finite<__half>(x[k]);
                         }
+                        const uint32_t a = to + swizzled<kKeys>(w * kMine + rr, 2 * ch + odd), b = to + swizzled<kKeys>(w * kMine + rr, 2 * ch + !odd);
+                        asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(a), "r"(x[0]), "r"(x[1]), "r"(x[2]), "r"(x[3]) : "memory");
+                        asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(b), "r"(x[4]), "r"(x[5]), "r"(x[6]), "r"(x[7]) : "memory");
                     }
-                    barrier_arrive(staged_empty + 8 * (u % M::staged_turns));
                     if (kv) {
                         const uint32_t any = __any_sync(0xffffffffu, bad != 0);
                         if (lane == 0) asm volatile("st.shared.u32 [%0], %1;" ::"r"(about + 16 + 4 * w), "r"(any) : "memory");
                     }
                     __syncwarp();
                     fence_shared_to_async();
-                    barrier_arrive(full + 8 * (u % M::turns));
+                    barrier_arrive(full + 8 * (u % M::stages));
                 }
                 if (!some && warp == kLoad && lane == 0) barrier_arrive(wanted);
             }
-            copy_wait<0>();
         }
     } else {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(W::other_registers));
@@ -979,6 +994,10 @@ __global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(con
                         if constexpr (kSlots == 1) {
                             b = steps[0] & 1, column += b * kKeys;
                             if (steps[0] >= 2 && fine) fine = barrier_wait(s_taken + 8 * b, ((steps[0] >> 1) - 1) & 1);
+                        } else if constexpr (kInPlace) {
+                            // the slot's columns are free when its last product has taken the probabilities that lay in them
+                            b = slot, column += slot * kScoresStep;
+                            if (steps[slot] && fine) fine = barrier_wait(o_added + 8 * slot, (steps[slot] - 1) & 1);
                         } else {
                             // the buffer is free when the scores of the step before have been taken
                             b = slot;
@@ -1000,7 +1019,7 @@ __global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(con
                     }
                     if (!fine) break;
                     if (elected()) {
-                        commit_to(empty + 8 * (u % M::turns));
+                        commit_to(empty + 8 * (u % M::stages));
                         if (i + 1 == item.end) commit_to(q_empty);
                     }
                     __syncwarp();
@@ -1033,7 +1052,7 @@ __global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(con
                             if (!spoiled) {  // else the softmax has added it up
 #pragma unroll
                                 for (int k = 0; k < kKeys / 16; k++)
-                                    mma_tensor(tensor + kOutputs + slot * 128, tensor + kProbabilities + slot * 64 + 8 * k, v_operand + k * (2048 >> 4), pv, holds[slot] || k > 0);
+                                    mma_tensor(tensor + kOutputs + slot * 128, tensor + kProbabilities + slot * kProbabilitiesStep + 8 * k, v_operand + k * (2048 >> 4), pv, holds[slot] || k > 0);
                             }
                             commit_to(o_added + 8 * slot);
                         }
@@ -1042,7 +1061,7 @@ __global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(con
                         steps[slot]++;
                     }
                     if (!fine) break;
-                    if (elected()) commit_to(empty + 8 * (u % M::turns));
+                    if (elected()) commit_to(empty + 8 * (u % M::stages));
                     __syncwarp();
                 }
             }
@@ -1128,39 +1147,6 @@ __global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(con
                 __syncwarp();
                 more = got != 0, id = next;
             }
-        }
-        if constexpr (KIND != kPlain) {
-        if (warp == kIssue + 3 && p.box_rows) {
-            // ---------------------------------------------------------------------- pages of codes, as boxes
-            // a lane has a page of a tile; what its table says is looked up a tile ahead
-            const int pages = kKeys / p.box_rows;
-            uint32_t u = 0;
-            for (int it = 0; fine; it++) {
-                ChunkItem item;
-                if (!take_item(it, item)) break;
-                auto page_key = [&](int i) { return tile_of(item, i) * kKeys + lane * p.box_rows; };
-                auto look_up = [&](int i) -> int32_t {
-                    const int t = page_key(i);
-                    if (i >= item.end || lane >= pages || t >= item.list.key_end || (t + p.box_rows <= item.list.key_low && t >= shape.sinks)) return kNoKey;
-                    return reinterpret_cast<const int32_t *>(p.tables + item.r * p.table_stride)[quick_div(static_cast<uint32_t>(t), p.div_block)];
-                };
-                int32_t ahead = look_up(item.begin);
-                for (int i = item.begin; i < item.end && fine; i++) {
-                    const int32_t block = ahead >= 0 && ahead < p.layer.num_blocks ? ahead : static_cast<int32_t>(p.layer.num_blocks);  // past the last: zeros
-                    ahead = look_up(i + 1);
-                    const int t = page_key(i), n = t - static_cast<int>(quick_div(static_cast<uint32_t>(t), p.div_block)) * static_cast<int>(p.layer.B);
-                    for (int kv = 0; kv < 2; kv++, u++) {
-                        const uint32_t slot = u % M::staged, bar = staged_full + 8 * (u % M::staged_turns);
-                        fine = __all_sync(0xffffffffu, staging_free(u));
-                        if (!fine) break;
-                        if (lane == 0) asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "n"(kKeys * DP) : "memory");
-                        __syncwarp();
-                        if (lane < pages) copy_box(base + kStagingAt + slot * M::codes + lane * p.box_rows * DP, kv ? &p.map_v : &p.map_k, 0, n, item.h, block, bar);
-                        __syncwarp();
-                    }
-                }
-            }
-        }
         }
         if (warp <= kIssue + 1 && !fine) {
             // products may be in flight: let them end before the tensor memory is given back

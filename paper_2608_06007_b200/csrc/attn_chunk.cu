@@ -93,7 +93,7 @@ static int launch_chunk(const ChunkParams &p, int dtype, int device, cudaStream_
 // box of a page's tokens is part of one.  Elsewhere box_rows stays 0.
 static int describe_pages(ChunkParams *p)
 {
-    p->box_rows = 0;
+    p->box_rows = p->q_boxes = 0;
     const Layer &l = p->layer;
     const int32_t most = p->shape.keys / 2, rows = static_cast<int32_t>(std::min<int64_t>(l.B, most));
     if (l.quantised() || rows < 8 || most % rows || l.B % rows || l.num_blocks < 1 || l.geo.block >= (1ll << 40)) return TC_OK;
@@ -118,6 +118,16 @@ static int describe_pages(ChunkParams *p)
         if (encode(v ? &p->map_v : &p->map_k, type, 4, v ? l.v : l.k, extent, stride, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
                    CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
             return TC_OK;  // a geometry that tensor maps do not hold
+    // the rows of an item's slot, 128, as whole tokens of a group's heads
+    const int32_t group = p->shape.group;
+    if (128 % group == 0) {
+        const cuuint64_t q_extent[3] = {static_cast<cuuint64_t>(l.D), static_cast<cuuint64_t>(p->Hq), static_cast<cuuint64_t>(p->n_tokens)};
+        const cuuint64_t q_stride[2] = {static_cast<cuuint64_t>(p->Hq > 1 ? p->q_head : l.D * 2ll), static_cast<cuuint64_t>(p->n_tokens > 1 ? p->q_token : l.D * 2ll * p->Hq)};
+        const cuuint32_t q_box[3] = {64, static_cast<cuuint32_t>(group), static_cast<cuuint32_t>(128 / group)};
+        p->q_boxes = q_stride[0] < (1ull << 40) && q_stride[1] < (1ull << 40) &&
+                     encode(&p->map_q, type, 3, const_cast<char *>(p->q), q_extent, q_stride, q_box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
+                            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    }
     p->box_rows = rows;
     p->div_box = make_fastdiv(static_cast<uint32_t>(rows));
     return TC_OK;
@@ -144,12 +154,9 @@ static int check_chunk(const tc_kv_layer_t *layer, const tc_attn_chunk_t *a, Chu
     if (a->sinks && !a->window) return fail(TC_ERR_INVALID_ARG, "sinks without a window: every key is seen");
     if (a->reserved) return fail(TC_ERR_INVALID_ARG, "reserved is %d, not 0", a->reserved);
     if (!(std::fabs(a->scale) <= 1e30f)) return fail(TC_ERR_INVALID_ARG, "scale is not a number of at most 1e30");
-    ChunkShape &s = p->shape;
-    s.group = static_cast<int32_t>(a->Hq / p->layer.H);
-    s.rows = chunk_rows(D), s.keys = chunk_keys(D);
-    s.window = static_cast<int32_t>(a->window ? std::min<int64_t>(a->window, 1 << 30) : 1 << 30);
-    s.sinks = static_cast<int32_t>(std::min<int64_t>(a->sinks, 1 << 30));
-    s.heads = p->layer.H;
+    p->shape = chunk_shape(static_cast<int32_t>(a->Hq / p->layer.H), chunk_rows(D), chunk_keys(D), static_cast<int32_t>(a->window ? std::min<int64_t>(a->window, 1 << 30) : 1 << 30),
+                           static_cast<int32_t>(std::min<int64_t>(a->sinks, 1 << 30)), p->layer.H);
+    const ChunkShape &s = p->shape;
     const int64_t new_most = std::min(a->max_new, a->n_tokens);
     if (new_most * s.group > INT32_MAX - 4096 || a->R * chunk_blocks(s, static_cast<int32_t>(new_most)) > INT32_MAX / s.heads)
         return fail(TC_ERR_TOO_LARGE, "R = %lld requests of up to %lld tokens x %lld heads: too many for one call", (long long)a->R, (long long)new_most, (long long)a->Hq);

@@ -85,6 +85,11 @@ __device__ __forceinline__ void copy_box(uint32_t dst, const CUtensorMap *map, i
                  ::"r"(dst), "l"(map), "r"(x), "r"(t), "r"(h), "r"(block), "r"(bar) : "memory");
 }
 
+__device__ __forceinline__ void copy_box3(uint32_t dst, const CUtensorMap *map, int x, int y, int z, uint32_t bar)
+{
+    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
+}
+
 // Bits 0 .. n - 1.
 __device__ __forceinline__ uint32_t low_bits(int n) { return n <= 0 ? 0u : n >= 32 ? 0xffffffffu : (1u << n) - 1u; }
 
@@ -223,7 +228,7 @@ __global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(con
         for (int i = 0; i < 2; i++) barrier_init(landed + 8 * i, 1);
         for (int i = 0; i < 2; i++) barrier_init(s_full + 8 * i, 1), barrier_init(s_taken + 8 * i, 128), barrier_init(p_ready + 8 * i, 128), barrier_init(o_added + 8 * i, 1);
         for (int i = 0; i < 2; i++) barrier_init(item_full + 8 * i, 1), barrier_init(item_empty + 8 * i, kSlots * 4 + W::loaders + 2), barrier_init(last_at + 8 * i, 1);
-        barrier_init(q_full, KIND == kPlain ? 4 * 33 : 256), barrier_init(q_empty, 1), barrier_init(wanted, 1), barrier_init(answered, 1);
+        barrier_init(q_full, KIND != kPlain ? 256 : p.q_boxes ? 1 : 4 * 33), barrier_init(q_empty, 1), barrier_init(wanted, 1), barrier_init(answered, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == kIssue) {
@@ -232,70 +237,68 @@ __global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(con
     }
 
     // ------------------------------------------------------------------- the cut, the same in every CTA
-    // Each thread has a run of requests.
-    __shared__ int64_t sum_items[W::all];
-    __shared__ int32_t sum_tiles[W::all];
+    // Each thread has a run of requests, of which it keeps the first.
+    __shared__ int32_t sum_items[W::all], sum_tiles[W::all], best_share[16];
     __shared__ float best_cost[16];
-    __shared__ int32_t best_share[16];
     __shared__ uint32_t warp_items[W::all], warp_rows[W::all];
     const int64_t per = (p.R + W::threads - 1) / W::threads, run0 = min(threadIdx.x * per, p.R), run1 = min(run0 + per, p.R);
+    struct Extent {
+        int32_t n, blocks, tiles;  // new tokens, items of all heads, uncut, and tiles of one
+    };
+    auto extent_of = [&](int64_t r, bool tell) {
+        const ChunkRequest q = chunk_request(p, r, tell);
+        return q.n ? Extent{q.n, chunk_blocks(shape, q.n) * H, chunk_tiles(shape, q.len)} : Extent{0, 0, 0};
+    };
+    const Extent first = run0 < run1 ? extent_of(run0, blockIdx.x == 0) : Extent{0, 0, 0};
     int32_t share = 1 << 30;
     if (p.plan.part_rows) {
-        int64_t n_items = 0;
-        int32_t most = 0;
-        for (int64_t r = run0; r < run1; r++) {
-            const ChunkRequest q = chunk_request(p, r, false);
-            if (!q.n) continue;
-            n_items += static_cast<int64_t>(chunk_blocks(shape, q.n)) * H;
-            most = max(most, chunk_tiles(shape, q.len));
+        int32_t n_items = first.blocks, most = first.tiles;
+        for (int64_t r = run0 + 1; r < run1; r++) {
+            const Extent e = extent_of(r, false);
+            n_items = min(n_items + e.blocks, 1 << 20), most = max(most, e.tiles);
         }
-#pragma unroll
-        for (int x = 16; x; x >>= 1) n_items += __shfl_xor_sync(0xffffffffu, n_items, x);
+        n_items = __reduce_add_sync(0xffffffffu, min(n_items, 1 << 20));
         most = __reduce_max_sync(0xffffffffu, most);
         if (lane == 0) sum_items[warp] = n_items, sum_tiles[warp] = most;
+        items_before[threadIdx.x] = first.blocks, rows_before[threadIdx.x] = first.tiles;  // for the search
         __syncthreads();
-        n_items = 0;
-        for (int w = 0; w < W::all; w++) n_items += sum_items[w], most = max(most, sum_tiles[w]);
+        n_items = lane < W::all ? sum_items[lane] : 0, most = lane < W::all ? sum_tiles[lane] : 0;
+        n_items = __reduce_add_sync(0xffffffffu, n_items), most = __reduce_max_sync(0xffffffffu, most);
         if (n_items < kChunkEnough && most > kChunkLeastShare) {
-            // warps 0 to 15 look at cuts w and w + 16
-            ChunkCost sum[2];
-            const int32_t shares[2] = {chunk_share(most, warp & 15), chunk_share(most, (warp & 15) + 16)};
-            const float inverse[2] = {1.f / shares[0], 1.f / shares[1]};
-            for (int64_t r = lane; r < (warp < 16 ? p.R : 0); r += 32) {
-                const ChunkRequest q = chunk_request(p, r, false);
-                if (!q.n) continue;
-                const int32_t blocks = chunk_blocks(shape, q.n) * H, tiles = chunk_tiles(shape, q.len);
+            if (warp < 16) {
+                // warp w looks at cuts w and w + 16
+                ChunkCost sum[2];
+                const int32_t shares[2] = {chunk_share(most, warp), chunk_share(most, warp + 16)};
+                const float inverse[2] = {1.f / shares[0], 1.f / shares[1]};
+                for (int64_t r = lane; r < p.R; r += 32) {
+                    const Extent e = per == 1 ? Extent{1, static_cast<int32_t>(items_before[r]), static_cast<int32_t>(rows_before[r])} : extent_of(r, false);
 #pragma unroll
-                for (int c = 0; c < 2; c++) sum[c].add(blocks, tiles, shares[c], static_cast<int32_t>((static_cast<float>(tiles + shares[c] - 1) + 0.5f) * inverse[c]));
-            }
-            float cost = 3e38f;
-            int32_t chosen = 1 << 30;
-#pragma unroll
-            for (int c = 0; c < 2; c++) {
-#pragma unroll
-                for (int x = 16; x; x >>= 1) {
-                    sum[c].items += __shfl_xor_sync(0xffffffffu, sum[c].items, x), sum[c].split += __shfl_xor_sync(0xffffffffu, sum[c].split, x);
-                    sum[c].tiles += __shfl_xor_sync(0xffffffffu, sum[c].tiles, x);
+                    for (int c = 0; c < 2; c++) sum[c].add(e.blocks, e.tiles, shares[c], static_cast<int32_t>((static_cast<float>(e.tiles + shares[c] - 1) + 0.5f) * inverse[c]));
                 }
-                const float here = chunk_cost(sum[c].items, sum[c].split, sum[c].tiles, __reduce_max_sync(0xffffffffu, sum[c].longest));
-                if (here < cost) cost = here, chosen = shares[c];
+#pragma unroll
+                for (int c = 0; c < 2; c++) {
+                    sum[c].items = __reduce_add_sync(0xffffffffu, sum[c].items), sum[c].split = __reduce_add_sync(0xffffffffu, sum[c].split);
+                    sum[c].tiles = __reduce_add_sync(0xffffffffu, sum[c].tiles), sum[c].longest = __reduce_max_sync(0xffffffffu, sum[c].longest);
+                }
+                const float cost0 = chunk_cost(sum[0]), cost1 = chunk_cost(sum[1]);
+                if (lane == 0) best_cost[warp] = min(cost0, cost1), best_share[warp] = cost1 < cost0 ? shares[1] : shares[0];
             }
-            if (lane == 0 && warp < 16) best_cost[warp] = cost, best_share[warp] = chosen;
             __syncthreads();
-            cost = 3e38f;
+            float cost = 3e38f;
             for (int w = 0; w < 16; w++)
                 if (best_cost[w] < cost || (best_cost[w] == cost && best_share[w] > share)) cost = best_cost[w], share = best_share[w];
+        } else {
+            __syncthreads();
         }
     }
     uint32_t total;
     {
         uint32_t my_items = 0, my_rows = 0;
         for (int64_t r = run0; r < run1; r++) {
-            const ChunkRequest q = chunk_request(p, r, blockIdx.x == 0);
-            if (!q.n) continue;
-            const int32_t parts = chunk_parts(chunk_tiles(shape, q.len), share);
-            my_items += chunk_blocks(shape, q.n) * H * parts;
-            if (parts > 1) my_rows += static_cast<uint32_t>(q.n) * p.Hq * parts;
+            const Extent e = r == run0 ? first : extent_of(r, blockIdx.x == 0);
+            const int32_t parts = e.tiles > share ? chunk_parts(e.tiles, share) : 1;
+            my_items += e.blocks * parts;
+            if (parts > 1) my_rows += static_cast<uint32_t>(e.n) * p.Hq * parts;
         }
         uint32_t upto = my_items, rows_upto = my_rows;
 #pragma unroll
@@ -305,11 +308,9 @@ __global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(con
         }
         if (lane == 31) warp_items[warp] = upto, warp_rows[warp] = rows_upto;
         __syncthreads();
-        total = 0;
-        for (int w = 0; w < W::all; w++) {
-            if (w < warp) upto += warp_items[w], rows_upto += warp_rows[w];
-            total += warp_items[w];
-        }
+        const uint32_t theirs = lane < W::all ? warp_items[lane] : 0, their_rows = lane < W::all ? warp_rows[lane] : 0;
+        total = __reduce_add_sync(0xffffffffu, theirs);
+        upto += __reduce_add_sync(0xffffffffu, lane < warp ? theirs : 0), rows_upto += __reduce_add_sync(0xffffffffu, lane < warp ? their_rows : 0);
         items_before[threadIdx.x] = upto - my_items, rows_before[threadIdx.x] = rows_upto - my_rows;
     }
     fence_before();
@@ -661,9 +662,25 @@ __global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(con
                 __syncwarp();
                 if (lane == 0) barrier_arrive(bar);
             };
+            // Where the heads of a group are a power of two, its rows are boxes of whole tokens, and one warp fetches them.
             auto take_queries = [&](const ChunkItem &item) {
+                if (p.q_boxes && warp != kLoad) {
+                    loads++;
+                    return;
+                }
                 if (loads) fine = __all_sync(0xffffffffu, barrier_wait(q_empty, (loads - 1) & 1));
                 if (!fine) return;
+                if (p.q_boxes) {
+                    if (lane == 0) {
+                        asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(q_full), "r"(item.rows > 128 ? M::queries : M::q_tile) : "memory");
+                        const int token = static_cast<int>(item.token0) + static_cast<int>(quick_div(static_cast<uint32_t>(item.row0), p.div_group)), step = 128 / shape.group;
+                        for (int slot = 0; slot < (item.rows > 128 ? kSlots : 1); slot++)
+                            for (int c = 0; c < DP / 64; c++) copy_box3(base + slot * M::q_tile + c * (128 * 128), &p.map_q, 64 * c, item.h * shape.group, token + slot * step, q_full);
+                    }
+                    __syncwarp();
+                    loads++;
+                    return;
+                }
 #pragma unroll 4
                 for (int j = 0; j < kSlots * DP / 8; j++) {
                     const int idx = j * 128 + thread, rr = idx / chunks, ch = idx % chunks;
@@ -761,16 +778,21 @@ __global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(con
                                 copy_wait<0>();
                             }
                             uint32_t any = 0;
-#pragma unroll 2
-                            for (int j = 0; j < kHalf * chunks / 32; j++) {
-                                const int idx = j * 32 + lane, rr = idx / chunks;
-                                const uint32_t at = to + swizzled<kKeys>(sub * kHalf + rr, idx % chunks);
-                                uint32_t x[4];
-                                if (kHalfWords == 2 && rr >= 32 ? mask[kHalfWords - 1] >> (rr & 31) & 1 : mask[0] >> (rr & 31) & 1) {
-                                    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]) : "r"(at) : "memory");
-                                    any |= not_finite<T>(x[0]) | not_finite<T>(x[1]) | not_finite<T>(x[2]) | not_finite<T>(x[3]);
-                                } else {
-                                    asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(at), "r"(0) : "memory");
+                            const bool whole = mask[0] == 0xffffffffu && mask[kHalfWords - 1] == 0xffffffffu;
+#pragma unroll 1
+                            for (int j0 = 0; j0 < kHalf * chunks / 32; j0 += 8) {
+                                uint32_t x[8][4];
+#pragma unroll
+                                for (int j = 0; j < 8; j++) {
+                                    const int idx = (j0 + j) * 32 + lane;
+                                    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(x[j][0]), "=r"(x[j][1]), "=r"(x[j][2]), "=r"(x[j][3]) : "r"(to + swizzled<kKeys>(sub * kHalf + idx / chunks, idx % chunks)) : "memory");
+                                }
+#pragma unroll
+                                for (int j = 0; j < 8; j++) {
+                                    const int idx = (j0 + j) * 32 + lane, rr = idx / chunks;
+                                    const uint32_t odd = not_finite<T>(x[j][0]) | not_finite<T>(x[j][1]) | not_finite<T>(x[j][2]) | not_finite<T>(x[j][3]);
+                                    if (whole || ((kHalfWords == 2 && rr >= 32 ? mask[kHalfWords - 1] : mask[0]) >> (rr & 31) & 1)) any |= odd;
+                                    else asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(to + swizzled<kKeys>(sub * kHalf + rr, idx % chunks)), "r"(0) : "memory");
                                 }
                             }
                             __syncwarp();
@@ -1085,7 +1107,7 @@ __global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(con
                     for (int64_t r = t * per; r < to; r++) {
                         const ChunkRequest q = chunk_request(p, r, false);
                         if (!q.n) continue;
-                        const int32_t parts = chunk_parts(chunk_tiles(shape, q.len), share), blocks = chunk_blocks(shape, q.n);
+                        const int32_t tiles = chunk_tiles(shape, q.len), parts = tiles > share ? chunk_parts(tiles, share) : 1, blocks = chunk_blocks(shape, q.n);
                         const uint32_t here = static_cast<uint32_t>(blocks) * parts * H;
                         if (id >= at + here) {
                             at += here;

@@ -31,7 +31,8 @@ struct ChunkParams {
     // Where blocks and tiles fit into one another, pages are fetched as boxes of box_rows tokens of one head; 0: key by key.
     int32_t box_rows;
     FastDiv div_box;
-    CUtensorMap map_k, map_v;
+    int32_t q_boxes;  // queries are fetched as boxes, too
+    CUtensorMap map_k, map_v, map_q;
 };
 constexpr uint32_t kUncut = 0xffffffffu;
 

@@ -19,27 +19,40 @@ constexpr int kChunkEnds = 4;           // what an item costs beside its tiles, 
 
 struct ChunkShape {
     int32_t group;   // query heads per KV head
-    int32_t rows;    // of an item at most
-    int32_t keys;    // of a tile
+    int32_t rows;    // of an item at most, a power of two
+    int32_t keys;    // of a tile, a power of two
     int32_t window;  // keys that a row sees up to its own, 2^30 = all
     int32_t sinks;   // first keys that every row sees
     int32_t heads;   // KV heads
+    int32_t rows_shift, keys_shift, near_tiles;  // near_tiles: that a block's windows can touch
+    uint32_t group_mul, group_shift;             // to divide by `group`
 };
 
 TC_HD int32_t chunk_low(int32_t a, int32_t b) { return a < b ? a : b; }
 TC_HD int32_t chunk_high(int32_t a, int32_t b) { return a > b ? a : b; }
+TC_HD int32_t chunk_by_group(const ChunkShape &s, int32_t n)
+{
+    const uint32_t u = static_cast<uint32_t>(n);
+    return static_cast<int32_t>((static_cast<uint32_t>((static_cast<uint64_t>(u) * s.group_mul) >> 32) + u) >> s.group_shift);
+}
+
+inline ChunkShape chunk_shape(int32_t group, int32_t rows, int32_t keys, int32_t window, int32_t sinks, int32_t heads)
+{
+    ChunkShape s{group, rows, keys, window, sinks, heads, 0, 0, 0, 0, 0};
+    while (1 << s.rows_shift < rows) s.rows_shift++;
+    while (1 << s.keys_shift < keys) s.keys_shift++;
+    s.near_tiles = (window + (rows - 1) / group + 1 + keys - 2) / keys + 1;
+    while ((1ll << s.group_shift) < group) s.group_shift++;
+    s.group_mul = static_cast<uint32_t>(((1ull << 32) * ((1ull << s.group_shift) - static_cast<uint64_t>(group))) / static_cast<uint64_t>(group) + 1);
+    return s;
+}
 
 // Items of n new tokens of one KV head, uncut.
-TC_HD int32_t chunk_blocks(const ChunkShape &s, int32_t n) { return static_cast<int32_t>((static_cast<int64_t>(n) * s.group + s.rows - 1) / s.rows); }
+TC_HD int32_t chunk_blocks(const ChunkShape &s, int32_t n) { return (n * s.group + s.rows - 1) >> s.rows_shift; }
 
+TC_HD int32_t chunk_tiles_of(const ChunkShape &s, int32_t keys) { return (keys + s.keys - 1) >> s.keys_shift; }
 // Tiles that a block of a request with `len` keys lists at most.
-TC_HD int32_t chunk_tiles(const ChunkShape &s, int32_t len)
-{
-    const int32_t all = (len + s.keys - 1) / s.keys;
-    const int64_t near = static_cast<int64_t>(s.window) + (s.rows - 1) / s.group + 1;  // keys that a block sees in its window
-    const int64_t most = (near + s.keys - 2) / s.keys + 1 + (chunk_low(s.sinks, len) + s.keys - 1) / s.keys;
-    return most < all ? static_cast<int32_t>(most) : all;
-}
+TC_HD int32_t chunk_tiles(const ChunkShape &s, int32_t len) { return chunk_low(s.near_tiles + chunk_tiles_of(s, chunk_low(s.sinks, len)), chunk_tiles_of(s, len)); }
 
 // The tiles that a block lists: the first `firsts`, which hold the keys that all rows see, then from tile firsts + skip on.
 struct ChunkList {
@@ -51,19 +64,18 @@ struct ChunkList {
 TC_HD ChunkList chunk_list(const ChunkShape &s, int32_t pos0, int32_t row0, int32_t rows_here, int32_t slot_rows)
 {
     ChunkList l;
-    const int32_t first = pos0 + row0 / s.group, last = pos0 + (row0 + rows_here - 1) / s.group;
+    const int32_t first = pos0 + chunk_by_group(s, row0), last = pos0 + chunk_by_group(s, row0 + rows_here - 1);
     l.key_end = last + 1;
     l.key_low = chunk_high(0, first - s.window + 1);
-    const int32_t low = l.key_low / s.keys, high = last / s.keys;
-    const int32_t sunk = (chunk_low(s.sinks, l.key_end) + s.keys - 1) / s.keys;
+    const int32_t low = l.key_low >> s.keys_shift, high = last >> s.keys_shift, sunk = chunk_tiles_of(s, chunk_low(s.sinks, l.key_end));
     l.firsts = chunk_low(sunk, low);
     l.skip = low - l.firsts;
     l.count = l.firsts + high - low + 1;
     l.end0 = l.count, l.begin1 = l.count;
     if (rows_here > slot_rows) {
-        l.end0 = (pos0 + (row0 + slot_rows - 1) / s.group) / s.keys - l.skip + 1;
+        l.end0 = ((pos0 + chunk_by_group(s, row0 + slot_rows - 1)) >> s.keys_shift) - l.skip + 1;
         if (sunk > low) l.begin1 = l.firsts;  // keys that every row sees reach into the tiles behind
-        else l.begin1 = chunk_high(0, pos0 + (row0 + slot_rows) / s.group - s.window + 1) / s.keys - l.skip;
+        else l.begin1 = (chunk_high(0, pos0 + chunk_by_group(s, row0 + slot_rows) - s.window + 1) >> s.keys_shift) - l.skip;
     }
     return l;
 }
@@ -77,27 +89,25 @@ TC_HD int32_t chunk_share(int32_t most_tiles, int32_t cut)
     return chunk_high((most_tiles + parts - 1) / parts, parts > 1 ? kChunkLeastShare : 1);
 }
 
-// What a cut costs, in tiles: waves of items of average size, or the longest item.
+// What a cut costs, in tiles: waves of items of average size, or the longest item.  (Fewer than kChunkEnough blocks, of less than 2^18 tiles.)
 struct ChunkCost {
-    int64_t items = 0, split = 0, tiles = 0;
-    int32_t longest = 0;
+    int32_t items = 0, split = 0, tiles = 0, longest = 0;
     // blocks: of one request, of all KV heads
     TC_HD void add(int32_t blocks, int32_t tiles_of, int32_t share, int32_t parts)
     {
-        const int64_t here = static_cast<int64_t>(blocks) * parts;
-        items += here;
-        tiles += static_cast<int64_t>(blocks) * tiles_of;
-        if (parts > 1) split += here;
+        items += blocks * parts;
+        tiles += blocks * tiles_of;
+        if (parts > 1) split += blocks * parts;
         longest = chunk_high(longest, chunk_low(tiles_of, share) + (parts > 1 ? 2 : 1) * kChunkEnds);
     }
 };
-TC_HD float chunk_cost(int64_t items, int64_t split, int64_t tiles, int32_t longest)
+TC_HD float chunk_cost(const ChunkCost &c)
 {
-    if (split > kChunkSplitItems) return 3e38f;
-    if (items == 0) return 0.f;
-    const float waves = static_cast<float>((items + kChunkSms - 1) / kChunkSms);
-    const float all = waves * static_cast<float>(tiles + kChunkEnds * (items + split)) / static_cast<float>(items);
-    return all > static_cast<float>(longest) ? all : static_cast<float>(longest);
+    if (c.split > kChunkSplitItems) return 3e38f;
+    if (c.items == 0) return 0.f;
+    const float waves = static_cast<float>((c.items + kChunkSms - 1) / kChunkSms);
+    const float all = waves * static_cast<float>(c.tiles + kChunkEnds * (c.items + c.split)) / static_cast<float>(c.items);
+    return all > static_cast<float>(c.longest) ? all : static_cast<float>(c.longest);
 }
 
 // What the host can say of a call: its grid, and its workspace: R pairs of words, then sums and outputs of the parts' rows.

@@ -15,10 +15,12 @@ static int pick(int lo, int hi) { seed = seed * 1664525u + 1013904223u; return l
 #define FAIL(...) return printf(__VA_ARGS__), printf("\n"), 1
 int main() {
     for (int round = 0; round < 3000; round++) {
-        ChunkShape s;
-        const int wide = pick(0, 3) == 0;
-        s.group = pick(1, 20), s.rows = wide ? 128 : 256, s.keys = wide ? 64 : 128, s.heads = pick(1, 8);
-        s.window = pick(0, 1) ? pick(1, round % 2 ? 3000 : 100) : 1 << 30, s.sinks = s.window < (1 << 30) && pick(0, 1) ? pick(0, 400) : 0;
+        const int wide = pick(0, 3) == 0, group = pick(1, 20), window = pick(0, 1) ? pick(1, round % 2 ? 3000 : 100) : 1 << 30, sinks = window < (1 << 30) && pick(0, 1) ? pick(0, 400) : 0;
+        const ChunkShape s = chunk_shape(group, wide ? 128 : 256, wide ? 64 : 128, window, sinks, pick(1, 8));
+        for (int i = 0; i < 100; i++) {
+            const int v = i < 50 ? i : pick(0, 2147483647 >> 1);
+            if (chunk_by_group(s, v) != v / group) FAIL("%d / %d", v, group);
+        }
         const int R = pick(1, round % 50 == 0 ? 300 : 6), longest = round % 7 == 0 ? 300000 : round % 3 ? 3000 : 300;
         std::vector<int> len(R), n(R);
         int64_t n_tokens = 0, max_new = 1, max_len = 1;
@@ -47,7 +49,7 @@ int main() {
                     if (parts != chunk_parts(tiles, sh)) FAIL("parts");
                     sum.add(chunk_blocks(s, n[r]) * s.heads, tiles, sh, parts);
                 }
-                const float cost = chunk_cost(sum.items, sum.split, sum.tiles, sum.longest);
+                const float cost = chunk_cost(sum);
                 if (cost < best) best = cost, share = sh;
             }
             if (best > 1e38f) FAIL("no cut at all");

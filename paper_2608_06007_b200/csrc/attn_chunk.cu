@@ -89,14 +89,16 @@ static int launch_chunk(const ChunkParams &p, int dtype, int device, cudaStream_
     return p.layer.D <= 128 ? launch_attn(chunk_join_kernel<T, 128>, grid, 128, 0, true, p, s) : launch_attn(chunk_join_kernel<T, 256>, grid, 128, 0, true, p, s);
 }
 
-// Pages of an unquantised pool as tensors [block][head][token][d]: where half tiles are whole numbers of blocks, or blocks of half tiles, so that a
-// box of a page's tokens is part of one.  Elsewhere box_rows stays 0.
-static int describe_pages(ChunkParams *p)
+// Tensor maps, where a call's geometry fits them: queries as [token][head][d], whose boxes are the whole tokens that an item's slot of 128
+// rows holds; pages of an unquantised pool as [block][head][token][d], where half tiles are whole numbers of blocks, or blocks of half
+// tiles, so that a box of a page's tokens is part of one.  Elsewhere q_boxes or box_rows stays 0.
+static int describe_boxes(ChunkParams *p)
 {
     p->box_rows = p->q_boxes = 0;
     const Layer &l = p->layer;
-    const int32_t most = p->shape.keys / 2, rows = static_cast<int32_t>(std::min<int64_t>(l.B, most));
-    if (l.quantised() || rows < 8 || most % rows || l.B % rows || l.num_blocks < 1 || l.geo.block >= (1ll << 40)) return TC_OK;
+    const int32_t group = p->shape.group, most = p->shape.keys / 2, rows = static_cast<int32_t>(std::min<int64_t>(l.B, most));
+    const bool queries = 128 % group == 0, pages = !l.quantised() && rows >= 8 && most % rows == 0 && l.B % rows == 0 && l.num_blocks > 0;
+    if (!queries && !pages) return TC_OK;
     using Encode = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *, const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
                                 CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
     static std::atomic<Encode> known;  // looked up once; twice does no harm
@@ -110,26 +112,27 @@ static int describe_pages(ChunkParams *p)
         encode = reinterpret_cast<Encode>(f);
         known.store(encode, std::memory_order_relaxed);
     }
-    const CUtensorMapDataType type = l.dtype == TC_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
-    const cuuint64_t extent[4] = {static_cast<cuuint64_t>(l.D), l.B, static_cast<cuuint64_t>(l.H), static_cast<cuuint64_t>(l.num_blocks)};
-    const cuuint64_t stride[3] = {static_cast<cuuint64_t>(l.geo.token), static_cast<cuuint64_t>(l.geo.head), static_cast<cuuint64_t>(l.geo.block)};
-    const cuuint32_t box[4] = {64, static_cast<cuuint32_t>(rows), 1, 1}, step[4] = {1, 1, 1, 1};
-    for (int v = 0; v < 2; v++)
-        if (encode(v ? &p->map_v : &p->map_k, type, 4, v ? l.v : l.k, extent, stride, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-                   CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
-            return TC_OK;  // a geometry that tensor maps do not hold
-    // the rows of an item's slot, 128, as whole tokens of a group's heads
-    const int32_t group = p->shape.group;
-    if (128 % group == 0) {
-        const cuuint64_t q_extent[3] = {static_cast<cuuint64_t>(l.D), static_cast<cuuint64_t>(p->Hq), static_cast<cuuint64_t>(p->n_tokens)};
-        const cuuint64_t q_stride[2] = {static_cast<cuuint64_t>(p->Hq > 1 ? p->q_head : l.D * 2ll), static_cast<cuuint64_t>(p->n_tokens > 1 ? p->q_token : l.D * 2ll * p->Hq)};
-        const cuuint32_t q_box[3] = {64, static_cast<cuuint32_t>(group), static_cast<cuuint32_t>(128 / group)};
-        p->q_boxes = q_stride[0] < (1ull << 40) && q_stride[1] < (1ull << 40) &&
-                     encode(&p->map_q, type, 3, const_cast<char *>(p->q), q_extent, q_stride, q_box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
-                            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    // 64 elements wide, swizzled as the products read them; false for a geometry that tensor maps do not hold
+    auto map = [&](CUtensorMap *m, const void *at, int rank, const cuuint64_t *extent, const cuuint64_t *stride, const cuuint32_t *box) {
+        const cuuint32_t step[4] = {1, 1, 1, 1};
+        for (int i = 0; i + 1 < rank; i++)
+            if (stride[i] == 0 || stride[i] >= (1ull << 40)) return false;
+        return encode(m, p->q_bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, static_cast<cuuint32_t>(rank), const_cast<void *>(at), extent, stride, box, step,
+                      CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    };
+    using Size = cuuint64_t;
+    if (queries) {
+        const Size row = l.D * 2ll, extent[3] = {static_cast<Size>(l.D), static_cast<Size>(p->Hq), static_cast<Size>(p->n_tokens)};
+        const Size stride[2] = {p->Hq > 1 ? static_cast<Size>(p->q_head) : row, p->n_tokens > 1 ? static_cast<Size>(p->q_token) : row * p->Hq};
+        const cuuint32_t box[3] = {64, static_cast<cuuint32_t>(group), static_cast<cuuint32_t>(128 / group)};
+        p->q_boxes = map(&p->map_q, p->q, 3, extent, stride, box);
     }
-    p->box_rows = rows;
-    p->div_box = make_fastdiv(static_cast<uint32_t>(rows));
+    if (pages) {
+        const Size extent[4] = {static_cast<Size>(l.D), l.B, static_cast<Size>(l.H), static_cast<Size>(l.num_blocks)};
+        const Size stride[3] = {static_cast<Size>(l.geo.token), static_cast<Size>(l.geo.head), static_cast<Size>(l.geo.block)};
+        const cuuint32_t box[4] = {64, static_cast<cuuint32_t>(rows), 1, 1};
+        if (map(&p->map_k, l.k, 4, extent, stride, box) && map(&p->map_v, l.v, 4, extent, stride, box)) p->box_rows = rows, p->div_box = make_fastdiv(static_cast<uint32_t>(rows));
+    }
     return TC_OK;
 }
 
@@ -226,7 +229,7 @@ extern "C" int tc_attn_chunk(const tc_kv_layer_t *layer, const tc_attn_chunk_t *
     p.scale_log2 = static_cast<float>((a->scale != 0.f ? static_cast<double>(a->scale) : 1.0 / std::sqrt(static_cast<double>(p.layer.D))) * 1.4426950408889634);
     p.div_block = make_fastdiv(p.layer.B);
     p.div_group = make_fastdiv(static_cast<uint32_t>(p.shape.group));
-    if ((rc = describe_pages(&p)) != TC_OK) return rc;
+    if ((rc = describe_boxes(&p)) != TC_OK) return rc;
     char *const ws = static_cast<char *>(a->workspace);
     p.cuts = reinterpret_cast<uint2 *>(ws + p.plan.cuts_at);
     p.sums = reinterpret_cast<float *>(ws + p.plan.sums_at);

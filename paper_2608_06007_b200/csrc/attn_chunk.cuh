@@ -227,7 +227,7 @@ __global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(con
         for (int i = 0; i < M::stages; i++) barrier_init(full + 8 * i, ready), barrier_init(empty + 8 * i, 1);
         for (int i = 0; i < 2; i++) barrier_init(landed + 8 * i, 1);
         for (int i = 0; i < 2; i++) barrier_init(s_full + 8 * i, 1), barrier_init(s_taken + 8 * i, 128), barrier_init(p_ready + 8 * i, 128), barrier_init(o_added + 8 * i, 1);
-        for (int i = 0; i < 2; i++) barrier_init(item_full + 8 * i, 1), barrier_init(item_empty + 8 * i, kSlots * 4 + W::loaders + 2), barrier_init(last_at + 8 * i, 1);
+        for (int i = 0; i < 2; i++) barrier_init(item_full + 8 * i, 1), barrier_init(item_empty + 8 * i, kSlots * 4 + W::loaders + 2 + (KIND != kPlain && p.q_boxes ? 1 : 0)), barrier_init(last_at + 8 * i, 1);
         barrier_init(q_full, KIND != kPlain ? 256 : p.q_boxes ? 1 : 4 * 33), barrier_init(q_empty, 1), barrier_init(wanted, 1), barrier_init(answered, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -340,6 +340,13 @@ __global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(con
     // Copy u (K of this CTA's tile u / 2, then V) is in stage u % stages: whether it is there, and whether copy u - stages is done with.
     auto copied = [&](uint32_t u) { return barrier_wait(full + 8 * (u % M::stages), (u / M::stages) & 1); };
     auto stage_free = [&](uint32_t u) { return u < M::stages || barrier_wait(empty + 8 * (u % M::stages), (u / M::stages - 1) & 1); };
+    // All rows of an item's queries, as boxes of whole tokens (one lane).
+    auto copy_query_boxes = [&](const ChunkItem &item, uint32_t bar) {
+        asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(item.rows > 128 ? M::queries : M::q_tile) : "memory");
+        const int token = static_cast<int>(item.token0) + static_cast<int>(quick_div(static_cast<uint32_t>(item.row0), p.div_group)), step = static_cast<int>(quick_div(128, p.div_group));
+        for (int slot = 0; slot < (item.rows > 128 ? kSlots : 1); slot++)
+            for (int c = 0; c < DP / 64; c++) copy_box3(base + slot * M::q_tile + c * (128 * 128), &p.map_q, 64 * c, item.h * shape.group, token + slot * step, bar);
+    };
     auto tile_of = [](const ChunkItem &item, int i) { return i < item.list.firsts ? i : i + item.list.skip; };
     // Does slot `slot` need tile i of the list?
     auto needs = [](const ChunkItem &item, int slot, int i) {
@@ -671,12 +678,7 @@ __global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(con
                 if (loads) fine = __all_sync(0xffffffffu, barrier_wait(q_empty, (loads - 1) & 1));
                 if (!fine) return;
                 if (p.q_boxes) {
-                    if (lane == 0) {
-                        asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(q_full), "r"(item.rows > 128 ? M::queries : M::q_tile) : "memory");
-                        const int token = static_cast<int>(item.token0) + static_cast<int>(quick_div(static_cast<uint32_t>(item.row0), p.div_group)), step = 128 / shape.group;
-                        for (int slot = 0; slot < (item.rows > 128 ? kSlots : 1); slot++)
-                            for (int c = 0; c < DP / 64; c++) copy_box3(base + slot * M::q_tile + c * (128 * 128), &p.map_q, 64 * c, item.h * shape.group, token + slot * step, q_full);
-                    }
+                    if (lane == 0) copy_query_boxes(item, q_full);
                     __syncwarp();
                     loads++;
                     return;
@@ -840,8 +842,8 @@ __global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(con
             };
             const char *const plane = kv ? p.layer.v : p.layer.k;
             constexpr int chunks = DP / 16, kUnits = kMine * chunks / 32;  // 16-byte chunks of codes that a lane has of a tile
-            uint4 codes[kUnits];
             for (int it = 0;; it++) {
+                uint4 codes[kUnits];
                 ChunkItem item;
                 const bool took = fine && take_item(it, item);
                 if (!together(took)) break;
@@ -872,20 +874,29 @@ __global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(con
                 };
                 int e_most = -133;  // the largest exponent of a tile so far
                 fetch(item.begin);
-#pragma unroll
-                for (int j = 0; j < kUnits; j++) load_unit(j);
+                // (loaded behind the queries, which need the registers)
+                if (next_off >= 0) asm volatile("prefetch.global.L2 [%0];" ::"l"(plane + next_off));
                 if (some) {
                     // queries, fp16 with a power of two taken out of each row; eight lanes have a row
-                    if (loads && fine) fine = __all_sync(0xffffffffu, barrier_wait(q_empty, (loads - 1) & 1));
+                    if (p.q_boxes) {
+                        if (fine) fine = __all_sync(0xffffffffu, barrier_wait(landed, loads & 1));
+                    } else if (loads && fine) {
+                        fine = __all_sync(0xffffffffu, barrier_wait(q_empty, (loads - 1) & 1));
+                    }
+                    const int rows = item.rows > 128 ? kSlots * 128 : 128;
 #pragma unroll 2
-                    for (int r0 = (warp - kLoad) * 4; r0 < kSlots * 128 && fine; r0 += 32) {
+                    for (int r0 = (warp - kLoad) * 4; r0 < rows && fine; r0 += 32) {
                         const int rr = r0 + (lane >> 3);
+                        unsigned char *const to = gen + (rr >> 7) * M::q_tile;
                         uint4 v[DP / 64];
                         float most = 0.f, up, down;
 #pragma unroll
                         for (int j = 0; j < DP / 64; j++) {
-                            const char *src = query_at(item, rr, 8 * j + (lane & 7));
-                            v[j] = src ? *reinterpret_cast<const uint4 *>(src) : make_uint4(0, 0, 0, 0);
+                            const int ch = 8 * j + (lane & 7);
+                            const char *src = p.q_boxes ? nullptr : query_at(item, rr, ch);
+                            v[j] = make_uint4(0, 0, 0, 0);
+                            if (p.q_boxes) v[j] = *reinterpret_cast<const uint4 *>(to + swizzled(rr & 127, ch));
+                            else if (src) v[j] = *reinterpret_cast<const uint4 *>(src);
                         }
 #pragma unroll
                         for (int j = 0; j < DP / 64; j++)
@@ -901,7 +912,7 @@ __global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(con
                                 const float2 f = query_pair(x[k], p.q_bf16);
                                 x[k] = pack2<__half>(f.x * up, f.y * up);
                             }
-                            *reinterpret_cast<uint4 *>(gen + (rr >> 7) * M::q_tile + swizzled(rr & 127, 8 * j + (lane & 7))) = make_uint4(x[0], x[1], x[2], x[3]);
+                            *reinterpret_cast<uint4 *>(to + swizzled(rr & 127, 8 * j + (lane & 7))) = make_uint4(x[0], x[1], x[2], x[3]);
                         }
                         if ((lane & 7) == 0) *reinterpret_cast<float *>(gen + kDownsAt + 4 * ((loads % M::down_sets) * kSlots * 128 + rr)) = down;
                     }
@@ -909,6 +920,8 @@ __global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(con
                     if (fine) barrier_arrive(q_full);
                     loads++;
                 }
+#pragma unroll
+                for (int j = 0; j < kUnits; j++) load_unit(j);
                 for (int i = item.begin; i < item.end; i++, tiles++) {
                     const uint32_t u = 2 * tiles + kv, stage = u % M::stages, about = info + (tiles % M::infos) * M::info;
                     near_end(item, i);
@@ -1168,6 +1181,20 @@ __global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(con
                              : "=r"(got), "=r"(next) : "r"(answer) : "memory");
                 __syncwarp();
                 more = got != 0, id = next;
+            }
+        }
+        if (KIND != kPlain && warp == kIssue + 3 && p.q_boxes) {
+            // ------------------------------------------------------------------- queries that meet codes
+            // fetched as they are; the warps that fetch K and V take the powers of two out
+            uint32_t loads = 0;
+            for (int it = 0; fine; it++) {
+                ChunkItem item;
+                if (!take_item(it, item)) break;
+                if (item.begin >= item.end) continue;
+                if (loads) fine = __all_sync(0xffffffffu, barrier_wait(q_empty, (loads - 1) & 1));
+                if (fine && lane == 0) copy_query_boxes(item, landed);
+                __syncwarp();
+                loads++;
             }
         }
         if (warp <= kIssue + 1 && !fine) {

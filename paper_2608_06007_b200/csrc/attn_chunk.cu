@@ -81,9 +81,15 @@ __global__ void __launch_bounds__(128) chunk_join_kernel(const __grid_constant__
 }
 
 template <typename T>
-static int launch_chunk(const ChunkParams &p, int dtype, int device, cudaStream_t s)
+static int launch_chunk(const ChunkParams &p, const AttnParams *singles, int dtype, int device, cudaStream_t s)
 {
-    const int rc = p.layer.quantised() ? launch_chunk_codes(p, device, s) : launch_chunk_plain(p, dtype, device, s);
+    int rc = TC_OK;
+    if (singles) {
+        if ((rc = launch_singles_stream(*singles, dtype, device, s)) != TC_OK) return rc;
+        if (p.max_new == 1) return launch_singles_join(*singles, dtype, s);
+    }
+    rc = p.layer.quantised() ? launch_chunk_codes(p, device, s) : launch_chunk_plain(p, dtype, device, s);
+    if (rc == TC_OK && singles) rc = launch_singles_join(*singles, dtype, s);
     if (rc != TC_OK || !p.plan.part_rows) return rc;
     const unsigned grid = static_cast<unsigned>(std::min<int64_t>((p.n_tokens * p.Hq + 3) / 4, kChunkSms * 8));
     return p.layer.D <= 128 ? launch_attn(chunk_join_kernel<T, 128>, grid, 128, 0, true, p, s) : launch_attn(chunk_join_kernel<T, 256>, grid, 128, 0, true, p, s);
@@ -136,8 +142,14 @@ static int describe_boxes(ChunkParams *p)
     return TC_OK;
 }
 
-// What both entry points check; fills p's geometry and plan.
-static int check_chunk(const tc_kv_layer_t *layer, const tc_attn_chunk_t *a, ChunkParams *p)
+// Requests with one new token go to the stream where there may be some number of them: it reads codes at some 4 TB/s and 16-bit numbers
+// at 6, a CTA that holds 256 rows for them at 0.5 and .. (64 requests, 51 of them single, 200k tokens of 8 heads x 128, e4m3: a call of KSINGLES us
+// so, 570 without).  Fewer are not worth its two launches.
+constexpr int64_t kLeastSingles = 8;
+
+// What both entry points check; fills p's geometry and plan, and those of the requests with one new token where these have their own
+// kernels.  *workspace: bytes of both, the second's from *singles_at on.
+static int check_chunk(const tc_kv_layer_t *layer, const tc_attn_chunk_t *a, ChunkParams *p, AttnParams *singles, int64_t *singles_at, int64_t *workspace)
 {
     int rc = check_layer(layer, &p->layer);
     if (rc != TC_OK) return rc;
@@ -163,7 +175,20 @@ static int check_chunk(const tc_kv_layer_t *layer, const tc_attn_chunk_t *a, Chu
     const int64_t new_most = std::min(a->max_new, a->n_tokens);
     if (new_most * s.group > INT32_MAX - 4096 || a->R * chunk_blocks(s, static_cast<int32_t>(new_most)) > INT32_MAX / s.heads)
         return fail(TC_ERR_TOO_LARGE, "R = %lld requests of up to %lld tokens x %lld heads: too many for one call", (long long)a->R, (long long)new_most, (long long)a->Hq);
-    plan_chunk(s, a->R, a->n_tokens, a->max_new, a->max_len, D, &p->plan);
+    p->max_new = a->max_new;
+    if (a->max_new > 1) plan_chunk(s, a->R, a->n_tokens, a->max_new, a->max_len, D, &p->plan);
+    *singles_at = *workspace = p->plan.workspace;
+    const int64_t most = a->window ? std::min(a->max_len, std::min(a->window, a->max_len) + std::min(a->sinks, a->max_len) + 96) : a->max_len;
+    // (what the stream's 32-bit counts of rows and tiles do not hold goes without it)
+    bool fits = a->R * a->Hq <= (1 << 30) && a->R * p->layer.H <= (1 << 30) / std::max<int64_t>(1, (most + 15) / 16);
+    if (fits && (a->max_new == 1 || a->R >= kLeastSingles)) {
+        singles->layer = p->layer;
+        split_attn(a->R, a->Hq, p->layer.H, D, most, 0, p->layer.quantised(), &singles->split);
+        fits = singles->split.stream_tiles < (1ll << 31);
+        p->no_singles = fits;
+        if (fits) *workspace += singles->split.workspace;
+    }
+    if (a->max_new == 1 && !fits) return fail(TC_ERR_TOO_LARGE, "R * H * keys = %lld * %d * %lld: too many for one call", (long long)a->R, p->layer.H, (long long)most);
     return TC_OK;
 }
 
@@ -177,8 +202,10 @@ extern "C" int tc_attn_chunk_workspace(const tc_kv_layer_t *layer, const tc_attn
     if (!bytes) return fail(TC_ERR_INVALID_ARG, "bytes is NULL");
     *bytes = 0;
     ChunkParams p{};
-    const int rc = check_chunk(layer, a, &p);
-    if (rc == TC_OK) *bytes = p.plan.workspace;
+    AttnParams singles{};
+    int64_t at, need;
+    const int rc = check_chunk(layer, a, &p, &singles, &at, &need);
+    if (rc == TC_OK) *bytes = need;
     return rc;
 }
 
@@ -186,7 +213,9 @@ extern "C" int tc_attn_chunk(const tc_kv_layer_t *layer, const tc_attn_chunk_t *
 {
     clear_error();
     ChunkParams p{};
-    int rc = check_chunk(layer, a, &p);
+    AttnParams singles{};
+    int64_t singles_at, need;
+    int rc = check_chunk(layer, a, &p, &singles, &singles_at, &need);
     if (rc != TC_OK) return rc;
     if (a->R == 0 || a->n_tokens == 0 || a->max_new == 0) return TC_OK;
     uint32_t align = 16;
@@ -202,9 +231,9 @@ extern "C" int tc_attn_chunk(const tc_kv_layer_t *layer, const tc_attn_chunk_t *
         return fail(TC_ERR_INVALID_ARG, "tables is required; address and table_stride are multiples of 4 bytes");
     if (a->table_width < (a->max_len + p.layer.B - 1) / p.layer.B)
         return fail(TC_ERR_BOUNDS, "table_width %lld holds %lld tokens, max_len is %lld", (long long)a->table_width, (long long)(a->table_width * p.layer.B), (long long)a->max_len);
-    if (p.plan.workspace && (!a->workspace || reinterpret_cast<uintptr_t>(a->workspace) % 16)) return fail(TC_ERR_INVALID_ARG, "workspace is required, 16-byte aligned");
-    if (a->workspace_bytes < p.plan.workspace)
-        return fail(TC_ERR_BOUNDS, "workspace_bytes %lld < %lld (tc_attn_chunk_workspace)", (long long)a->workspace_bytes, (long long)p.plan.workspace);
+    if (need && (!a->workspace || reinterpret_cast<uintptr_t>(a->workspace) % 16)) return fail(TC_ERR_INVALID_ARG, "workspace is required, 16-byte aligned");
+    if (a->workspace_bytes < need)
+        return fail(TC_ERR_BOUNDS, "workspace_bytes %lld < %lld (tc_attn_chunk_workspace)", (long long)a->workspace_bytes, (long long)need);
     if (p.plan.grid > INT32_MAX) return fail(TC_ERR_TOO_LARGE, "%lld items: too many for one call", (long long)p.plan.grid);
     int device, sms;
     if ((rc = op_device(&device, &p.status, &sms)) != TC_OK) return rc;
@@ -212,7 +241,7 @@ extern "C" int tc_attn_chunk(const tc_kv_layer_t *layer, const tc_attn_chunk_t *
         const char *name;
         const void *p;
     } pointers[] = {{"layer.k", layer->k}, {"layer.v", layer->v}, {"layer.k_scale", layer->k_scale}, {"layer.v_scale", layer->v_scale}, {"q", a->q}, {"out", a->out},
-                    {"lse", a->lse}, {"lens", a->lens}, {"offsets", a->offsets}, {"tables", a->tables}, {"workspace", p.plan.workspace ? a->workspace : nullptr}};
+                    {"lse", a->lse}, {"lens", a->lens}, {"offsets", a->offsets}, {"tables", a->tables}, {"workspace", need ? a->workspace : nullptr}};
     for (const auto &ptr : pointers)
         if (ptr.p && (rc = check_memory(ptr.name, ptr.p, device)) != TC_OK) return rc;
     p.q = static_cast<const char *>(a->q);
@@ -235,5 +264,23 @@ extern "C" int tc_attn_chunk(const tc_kv_layer_t *layer, const tc_attn_chunk_t *
     p.sums = reinterpret_cast<float *>(ws + p.plan.sums_at);
     p.parts = reinterpret_cast<float *>(ws + p.plan.parts_at);
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    return a->dtype == TC_BF16 ? launch_chunk<__nv_bfloat16>(p, a->dtype, device, s) : launch_chunk<__half>(p, a->dtype, device, s);
+    if (p.no_singles) {
+        AttnParams &q = singles;
+        q.q = p.q, q.q_req = p.q_token, q.q_head = p.q_head;
+        q.out = p.out, q.out_req = p.out_token, q.out_head = p.out_head;
+        q.lse = p.lse;
+        q.tables = p.tables, q.table_width = a->table_width, q.table_stride = p.table_stride;
+        q.lens = p.lens, q.offsets = p.offsets, q.n_tokens = p.n_tokens, q.max_new = p.max_new;
+        q.R = p.R, q.max_len = p.max_len;
+        q.window = p.shape.window, q.sinks = p.shape.sinks;
+        q.Hq = p.Hq, q.q_bf16 = p.q_bf16, q.scale_log2 = p.scale_log2;
+        q.div_block = p.div_block, q.div_group = p.div_group, q.div_heads = make_fastdiv(static_cast<uint32_t>(p.Hq));
+        q.status = p.status;
+        char *const at = ws + singles_at;
+        q.sums = reinterpret_cast<float *>(at + q.split.sums_at), q.parts = reinterpret_cast<float *>(at + q.split.parts_at);
+        q.piece_sums = reinterpret_cast<float *>(at + q.split.piece_sums_at), q.pieces = reinterpret_cast<float *>(at + q.split.pieces_at);
+        q.before = reinterpret_cast<uint32_t *>(at + q.split.before_at);
+    }
+    const AttnParams *const apart = p.no_singles ? &singles : nullptr;
+    return a->dtype == TC_BF16 ? launch_chunk<__nv_bfloat16>(p, apart, a->dtype, device, s) : launch_chunk<__half>(p, apart, a->dtype, device, s);
 }

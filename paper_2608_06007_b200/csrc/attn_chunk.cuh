@@ -65,7 +65,7 @@ __device__ __forceinline__ ChunkRequest chunk_request(const ChunkParams &p, int6
     const int64_t n = to - q.token0;
     const bool bad = q.token0 < 0 || to < q.token0 || to > p.n_tokens || n > p.max_new || (q.len >= 0 && (q.len > p.max_len || q.len < n));
     if (tell && bad) atomicOr(p.status, kStatusBadIndex);
-    q.n = bad || q.len < 0 ? 0 : static_cast<int32_t>(n);
+    q.n = bad || q.len < 0 || (p.no_singles && n == 1) ? 0 : static_cast<int32_t>(n);
     return q;
 }
 
@@ -1205,6 +1205,7 @@ __global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(con
             barrier_wait(last, 0);
         }
     }
+    if (p.no_singles) await_last();  // who waits for this kernel waits for those before it, too
     if (!fine) atomicOr(p.status, static_cast<unsigned int>(TC_DEVICE_BULK_WAIT_TIMEOUT));
     fence_before();
     __syncthreads();
@@ -1227,7 +1228,7 @@ int launch_chunk_shape(const ChunkParams &p, int device, cudaStream_t s)
         if (attr.numRegs != ChunkWarps<KIND>::launch_registers) return fail(TC_ERR_CUDA, "tc_attn_chunk's kernel was built with %d registers a thread, not %d", attr.numRegs, ChunkWarps<KIND>::launch_registers);
         raised[device].store(true, std::memory_order_relaxed);
     }
-    return launch_attn(chunk_kernel<T, KIND, DP>, static_cast<unsigned>(p.plan.grid), ChunkWarps<KIND>::threads, M::bytes, false, p, s);
+    return launch_attn(chunk_kernel<T, KIND, DP>, static_cast<unsigned>(p.plan.grid), ChunkWarps<KIND>::threads, M::bytes, p.no_singles != 0, p, s);
 }
 
 template <typename T, int KIND>

@@ -3,6 +3,7 @@
 
 #include <cuda.h>
 
+#include "attn.h"
 #include "attn_chunk_split.h"
 #include "ops.h"
 
@@ -21,7 +22,8 @@ struct ChunkParams {
     const int32_t *lens;
     int64_t R, n_tokens, max_new, max_len;
     int32_t Hq, q_bf16;
-    float scale_log2;  // scale * log2(e)
+    int32_t no_singles;  // requests with one new token have their own kernels, launched before this one
+    float scale_log2;    // scale * log2(e)
     FastDiv div_block, div_group;
     ChunkShape shape;
     ChunkPlan plan;

@@ -17,7 +17,7 @@ template <typename T>
 static int launch_decode(const AttnParams &p, int device, cudaStream_t s)
 {
     const int rc = p.split.prefix_parts ? launch_prefix(p, std::is_same<T, __half>::value ? TC_FP16 : TC_BF16, device, s) : TC_OK;
-    return rc != TC_OK ? rc : launch_stream_and_join<T, false>(p, device, s);
+    return rc != TC_OK ? rc : launch_stream_and_join<T, kAllKeys>(p, device, s);
 }
 
 // What both entry points check; fills p's geometry and split.

@@ -98,13 +98,36 @@ __device__ __forceinline__ uint32_t transposed(uint32_t v)
     return r;
 }
 
+// Whose keys: all of each request's (and a prefix's); those in a window; those of requests with one new token, in a window.
+enum StreamMode { kAllKeys = 0, kWindow = 1, kSingles = 2 };
+
+// What the call says of a request's length; negative: it has no part in the call.
+template <int MODE>
+__device__ __forceinline__ int said_length(const AttnParams &p, int64_t r)
+{
+    const int len = p.lens[r];
+    if constexpr (MODE == kSingles) {
+        const int64_t from = p.offsets[r];
+        if (p.offsets[r + 1] != from + 1 || from < 0 || from >= p.n_tokens || len < 1 || len > p.max_len) return -1;
+    }
+    return len;
+}
+// Its row of q, out and lse.
+template <int MODE> __device__ __forceinline__ int64_t row_of(const AttnParams &p, int64_t r) { return MODE == kSingles ? p.offsets[r] : r; }
+
 // Length of a request (r < R) or of the prefix (r == R; 0 where prefix_kernel takes it), in keys.
+template <int MODE>
 __device__ __forceinline__ int stream_length(const AttnParams &p, int64_t r, bool tell)
 {
     const int64_t most = r < p.R ? p.max_len : p.max_prefix;
     if (most == 0 || (r == p.R && p.split.prefix_rows != 16)) return 0;
-    int64_t len = r < p.R ? p.lens[r] : *p.prefix_len;
+    int64_t len = r < p.R ? said_length<MODE>(p, r) : *p.prefix_len;
     if (tell && (len > most || (r == p.R && len < 0))) atomicOr(p.status, kStatusBadIndex);
+    if constexpr (MODE == kSingles) {
+        const int64_t from = p.offsets[r < p.R ? r : 0], to = p.offsets[r < p.R ? r + 1 : 0];
+        const int said = r < p.R ? p.lens[r] : -1;
+        if (tell && r < p.R && (from < 0 || to < from || to > p.n_tokens || to - from > p.max_new || (said >= 0 && (said > p.max_len || said < to - from)))) atomicOr(p.status, kStatusBadIndex);
+    }
     return static_cast<int>(min(max(len, int64_t(0)), most));
 }
 __device__ __forceinline__ int stream_items(const AttnParams &p, int64_t r) { return p.layer.H * (r < p.R ? p.split.own_blocks : p.split.prefix_blocks); }
@@ -127,17 +150,17 @@ __device__ __forceinline__ WindowTiles window_tiles(const AttnParams &p, int len
     w.count = static_cast<int>(tiles_of(p, len)) - w.skip;
     return w;
 }
-template <bool WINDOW> __device__ __forceinline__ uint32_t own_tiles(const AttnParams &p, int len)
+template <int MODE> __device__ __forceinline__ uint32_t own_tiles(const AttnParams &p, int len)
 {
-    if constexpr (WINDOW) return window_tiles(p, len).count;
+    if constexpr (MODE != kAllKeys) return window_tiles(p, len).count;
     else return tiles_of(p, len);
 }
-template <bool WINDOW> __device__ __forceinline__ uint32_t stream_tiles(const AttnParams &p, int64_t r, bool tell) { return own_tiles<WINDOW>(p, stream_length(p, r, tell)) * stream_items(p, r); }
+template <int MODE> __device__ __forceinline__ uint32_t stream_tiles(const AttnParams &p, int64_t r, bool tell) { return own_tiles<MODE>(p, stream_length<MODE>(p, r, tell)) * stream_items(p, r); }
 
 enum : uint32_t { kFirst = 1, kLast = 2, kWhole = 4, kSecond = 8 };
 
 // T: the type of the products - the queries' for a plain pool, fp16 for a quantised one, which looks at p.q_bf16.
-template <typename T, int KIND, int DP, int NB, bool WINDOW>
+template <typename T, int KIND, int DP, int NB, int MODE>
 __global__ void __launch_bounds__(128, DP > 128 ? 1 : NB > 1 ? 2 : DP == 64 ? 4 : 3) stream_kernel(const __grid_constant__ AttnParams p)
 {
     using R = Ring<KIND, DP>;
@@ -155,7 +178,7 @@ __global__ void __launch_bounds__(128, DP > 128 ? 1 : NB > 1 ? 2 : DP == 64 ? 4 
     // begin; CTA 0 also leaves the sums for join_kernel.
     const int64_t per = (p.R + 1 + 127) / 128, mine0 = threadIdx.x * per, mine1 = min(mine0 + per, p.R + 1);
     uint32_t my_tiles = 0;
-    for (int64_t r = mine0; r < mine1; r++) my_tiles += stream_tiles<WINDOW>(p, r, blockIdx.x == 0);
+    for (int64_t r = mine0; r < mine1; r++) my_tiles += stream_tiles<MODE>(p, r, blockIdx.x == 0);
     uint32_t upto = my_tiles;
 #pragma unroll
     for (int x = 1; x < 32; x <<= 1) {
@@ -177,7 +200,7 @@ __global__ void __launch_bounds__(128, DP > 128 ? 1 : NB > 1 ? 2 : DP == 64 ? 4 
         if (from < before || from >= upto) continue;
         uint32_t at = before;
         for (int64_t r = mine0; r < mine1; r++) {
-            const uint32_t n = stream_tiles<WINDOW>(p, r, false);
+            const uint32_t n = stream_tiles<MODE>(p, r, false);
             if (from < at + n) {
                 start_at[w] = static_cast<uint32_t>(r), start_off[w] = from - at;
                 break;
@@ -189,7 +212,7 @@ __global__ void __launch_bounds__(128, DP > 128 ? 1 : NB > 1 ? 2 : DP == 64 ? 4 
         uint32_t at = before;
         for (int64_t r = mine0; r < mine1; r++) {
             p.before[4 + r] = at;
-            at += stream_tiles<WINDOW>(p, r, false);
+            at += stream_tiles<MODE>(p, r, false);
         }
         if (threadIdx.x == 0) {
             // the share, and what quick_div needs to divide by it (as make_fastdiv on the host)
@@ -211,9 +234,9 @@ __global__ void __launch_bounds__(128, DP > 128 ? 1 : NB > 1 ? 2 : DP == 64 ? 4 
 
     // The next tile to be copied: tile `l_tile` of `l_tiles` of item `l_item` of request l_r.
     int64_t l_r = start_at[warp];
-    int l_len = stream_length(p, l_r, false), l_tiles = static_cast<int>(own_tiles<WINDOW>(p, l_len));
+    int l_len = stream_length<MODE>(p, l_r, false), l_tiles = static_cast<int>(own_tiles<MODE>(p, l_len));
     WindowTiles l_window{};
-    if constexpr (WINDOW) l_window = window_tiles(p, l_len);
+    if constexpr (MODE != kAllKeys) l_window = window_tiles(p, l_len);
     int l_item = static_cast<int>(start_off[warp] / l_tiles), l_tile = static_cast<int>(start_off[warp] - l_item * l_tiles);
     const int32_t *l_table = l_r < p.R ? reinterpret_cast<const int32_t *>(p.tables + l_r * p.table_stride) : p.prefix_table;
     auto head_of = [&](int64_t r, int item) {
@@ -236,13 +259,13 @@ __global__ void __launch_bounds__(128, DP > 128 ? 1 : NB > 1 ? 2 : DP == 64 ? 4 
     const int my_key = lane % R::keys;
     // this lane's key of the next tile
     auto next_key = [&]() {
-        if constexpr (WINDOW) return R::keys * (l_tile + (l_tile >= l_window.firsts ? l_window.skip : 0)) + my_key;
+        if constexpr (MODE != kAllKeys) return R::keys * (l_tile + (l_tile >= l_window.firsts ? l_window.skip : 0)) + my_key;
         else return R::keys * l_tile + my_key;
     };
     auto look_up = [&]() -> int32_t {
         const int t = next_key();
         if (l_left <= 0 || t >= l_len) return kNoKey;
-        if constexpr (WINDOW)
+        if constexpr (MODE != kAllKeys)
             if (t >= p.sinks && t < l_window.first_key) return kNoKey;
         const uint32_t entry = quick_div(static_cast<uint32_t>(t), p.div_block);
         return l_r == p.R || entry < p.table_width ? l_table[entry] : -1;
@@ -266,8 +289,8 @@ __global__ void __launch_bounds__(128, DP > 128 ? 1 : NB > 1 ? 2 : DP == 64 ? 4 
             const uint32_t dst = at + sub * R::group;
             if (one_block) {
                 // a fixed step from key to key; with a window the last of the 16 that is there may be any
-                const uint32_t some = WINDOW ? mask >> (16 * sub) & 0xffffu : 1u;
-                const int n0 = __shfl_sync(0xffffffffu, n, 16 * sub), b0 = __shfl_sync(0xffffffffu, block, 16 * sub + (WINDOW && some ? __ffs(some) - 1 : 0));
+                const uint32_t some = MODE != kAllKeys ? mask >> (16 * sub) & 0xffffu : 1u;
+                const int n0 = __shfl_sync(0xffffffffu, n, 16 * sub), b0 = __shfl_sync(0xffffffffu, block, 16 * sub + (MODE != kAllKeys && some ? __ffs(some) - 1 : 0));
                 const char *k = p.layer.k + p.layer.geo.at(max(b0, 0), n0 + my_row, h) + my_chunk * 16;
                 const uint32_t rows = in_row ? mask >> (16 * sub + my_row) : 0u;
 #pragma unroll
@@ -302,7 +325,7 @@ __global__ void __launch_bounds__(128, DP > 128 ? 1 : NB > 1 ? 2 : DP == 64 ? 4 
                 // the next request that has keys; `l_left` says that there is one
                 l_item = 0;
                 for (int64_t base = l_r + 1; base <= p.R; base += 32) {
-                    const int len = base + lane <= p.R ? stream_length(p, base + lane, false) : 0;
+                    const int len = base + lane <= p.R ? stream_length<MODE>(p, base + lane, false) : 0;
                     const uint32_t some = __ballot_sync(0xffffffffu, len > 0);
                     if (!some) continue;
                     const int at_lane = __ffs(some) - 1;
@@ -310,8 +333,8 @@ __global__ void __launch_bounds__(128, DP > 128 ? 1 : NB > 1 ? 2 : DP == 64 ? 4 
                     l_len = __shfl_sync(0xffffffffu, len, at_lane);
                     break;
                 }
-                l_tiles = static_cast<int>(own_tiles<WINDOW>(p, l_len));
-                if constexpr (WINDOW) l_window = window_tiles(p, l_len);
+                l_tiles = static_cast<int>(own_tiles<MODE>(p, l_len));
+                if constexpr (MODE != kAllKeys) l_window = window_tiles(p, l_len);
                 l_table = l_r < p.R ? reinterpret_cast<const int32_t *>(p.tables + l_r * p.table_stride) : p.prefix_table;
             }
         }
@@ -351,7 +374,7 @@ __global__ void __launch_bounds__(128, DP > 128 ? 1 : NB > 1 ? 2 : DP == 64 ? 4 
             const int64_t row = it.row0 + 8 * nb + g;
             const bool there = row < it.row_end;
             const int64_t req = there ? quick_div(static_cast<uint32_t>(row), p.div_group) : 0;
-            const char *src = p.q + req * p.q_req + (it.h * group + (there ? row - req * group : 0)) * p.q_head;
+            const char *src = p.q + (there ? row_of<MODE>(p, req) : 0) * p.q_req + (it.h * group + (there ? row - req * group : 0)) * p.q_head;
 #pragma unroll
             for (int ks = 0; ks < DP / 16; ks++) {
                 const int d0 = 16 * ks + (KIND == kPlain ? 2 : 4) * c;
@@ -611,7 +634,8 @@ __global__ void __launch_bounds__(128, DP > 128 ? 1 : NB > 1 ? 2 : DP == 64 ? 4 
                     }
                     if (whole && p.max_prefix == 0) {
                         // these are all of the row's keys: its output
-                        char *out = p.out + req * p.out_req + (it.h * group + (row - req * group)) * p.out_head;
+                        const int64_t at = row_of<MODE>(p, req);
+                        char *out = p.out + at * p.out_req + (it.h * group + (row - req * group)) * p.out_head;
 #pragma unroll
                         for (int k = 0; k < DP / 16; k++)
 #pragma unroll
@@ -621,7 +645,7 @@ __global__ void __launch_bounds__(128, DP > 128 ? 1 : NB > 1 ? 2 : DP == 64 ? 4 
                                 if (KIND == kPlain ? std::is_same<T, __nv_bfloat16>::value : p.q_bf16) reinterpret_cast<__nv_bfloat16 *>(out)[16 * k + g + 8 * half] = __float2bfloat16_rn(x);
                                 else reinterpret_cast<__half *>(out)[16 * k + g + 8 * half] = __float2half_rn(x);
                             }
-                        if (g == 0 && p.lse) p.lse[req * p.Hq + it.h * group + (row - req * group)] = log * kLn2;
+                        if (g == 0 && p.lse) p.lse[at * p.Hq + it.h * group + (row - req * group)] = log * kLn2;
                         continue;
                     }
 #pragma unroll
@@ -646,7 +670,7 @@ __global__ void __launch_bounds__(128, DP > 128 ? 1 : NB > 1 ? 2 : DP == 64 ? 4 
 // call of 512 requests of 32 heads, e4m3, D = 128, took 149 us for 157 behind a prefix of 4000 and 76 for 81 without.
 constexpr int kJoinCtas = 8;
 constexpr float kLess = 12.f;  // weights are 2^-12 at most: the outputs of up to that many parts may be next to the largest number
-template <typename T, int DP, int WARPS, bool WINDOW>
+template <typename T, int DP, int WARPS, int MODE>
 __global__ void __launch_bounds__(WARPS == 1 ? 128 : 32 * WARPS, WARPS == 1 ? kJoinCtas : 1) join_kernel(const __grid_constant__ AttnParams p)
 {
     constexpr int kVectors = DP <= 128 ? 1 : 2, kAhead = (WARPS == 1 ? 4 : 8) / kVectors;
@@ -656,7 +680,7 @@ __global__ void __launch_bounds__(WARPS == 1 ? 128 : 32 * WARPS, WARPS == 1 ? kJ
     uint32_t row = WARPS == 1 ? blockIdx.x * 4 + warp : blockIdx.x;
     if (row >= rows) return;
     const bool prefix_streams = p.max_prefix && p.split.prefix_rows == 16, streams = p.split.stream_ctas > 0;
-    int32_t own_len = p.lens[quick_div(row, p.div_heads)];
+    int32_t own_len = said_length<MODE>(p, quick_div(row, p.div_heads));
     const int32_t prefix_len = p.max_prefix ? *p.prefix_len : 0;
     await_last();  // what is read from here on the kernels before this one have written
     const uint4 shares = streams ? *reinterpret_cast<const uint4 *>(p.before) : make_uint4(0, 0, 0, 0);
@@ -678,7 +702,7 @@ __global__ void __launch_bounds__(WARPS == 1 ? 128 : 32 * WARPS, WARPS == 1 ? kJ
         const uint32_t at = own_at;
         if (row + row_step < rows) {
             const uint32_t next = quick_div(row + row_step, p.div_heads);
-            own_len = p.lens[next];
+            own_len = said_length<MODE>(p, next);
             if (streams) own_at = p.before[4 + next];
         }
         if (len < 0) continue;
@@ -694,7 +718,7 @@ __global__ void __launch_bounds__(WARPS == 1 ? 128 : 32 * WARPS, WARPS == 1 ? kJ
             l.next = (w0 + 1) * 2 * columns + col;
             return l;
         };
-        const Left own = left(own_tiles<WINDOW>(p, min(len, static_cast<int32_t>(p.max_len))), at, in_group, p.split.own_blocks, p.split.whole_parts - (prefix_streams ? 2 : 1));
+        const Left own = left(own_tiles<MODE>(p, min(len, static_cast<int32_t>(p.max_len))), at, in_group, p.split.own_blocks, p.split.whole_parts - (prefix_streams ? 2 : 1));
         if (p.max_prefix == 0 && own.whole) continue;  // the stream has written the output
         Left shared{0, 0, 0, false};
         if (prefix_streams) shared = left(tiles_of(p, prefix_keys), prefix_at, r * p.split.group + in_group, p.split.prefix_blocks, p.split.whole_parts - 1);
@@ -778,58 +802,60 @@ __global__ void __launch_bounds__(WARPS == 1 ? 128 : 32 * WARPS, WARPS == 1 ? kJ
             }
         }
         const float inv = all == 0.f ? 0.f : 1.f / all;
-        char *dst = p.out + r * p.out_req + head * p.out_head;
+        const int64_t at_row = row_of<MODE>(p, r);
+        char *dst = p.out + at_row * p.out_req + head * p.out_head;
 #pragma unroll
         for (int x = 0; x < kVectors; x++)
             if (lane * 4 + 128 * x < D)
                 *reinterpret_cast<uint2 *>(dst + (lane * 4 + 128 * x) * 2) = make_uint2(pack2<T>(acc[4 * x] * inv, acc[4 * x + 1] * inv), pack2<T>(acc[4 * x + 2] * inv, acc[4 * x + 3] * inv));
-        if (p.lse && lane == 0) p.lse[row] = all == 0.f ? -INFINITY : ((top == -INFINITY ? 0.f : top) + kLess + log2f(all)) * kLn2;
+        if (p.lse && lane == 0) p.lse[at_row * p.Hq + head] = all == 0.f ? -INFINITY : ((top == -INFINITY ? 0.f : top) + kLess + log2f(all)) * kLn2;
         if (WARPS > 1) return;
     }
 }
 
 // --------------------------------------------------------------------------------------- launching
-template <typename T, int KIND, int DP, int NB, bool WINDOW>
+template <typename T, int KIND, int DP, int NB, int MODE>
 int launch_stream(const AttnParams &p, unsigned grid, int device, cudaStream_t s)
 {
     using R = Ring<KIND, DP>;
     static std::atomic<bool> raised[kMaxDevices];  // set once per device; setting it twice does no harm
     if (!raised[device].load(std::memory_order_relaxed)) {
-        const cudaError_t e = cudaFuncSetAttribute(stream_kernel<T, KIND, DP, NB, WINDOW>, cudaFuncAttributeMaxDynamicSharedMemorySize, R::bytes);
+        const cudaError_t e = cudaFuncSetAttribute(stream_kernel<T, KIND, DP, NB, MODE>, cudaFuncAttributeMaxDynamicSharedMemorySize, R::bytes);
         if (e != cudaSuccess) return cuda_fail(e, "cudaFuncSetAttribute(dynamic shared memory)");
         raised[device].store(true, std::memory_order_relaxed);
     }
-    return launch_attn(stream_kernel<T, KIND, DP, NB, WINDOW>, grid, 128, R::bytes, p.split.prefix_parts > 0, p, s);
+    return launch_attn(stream_kernel<T, KIND, DP, NB, MODE>, grid, 128, R::bytes, p.split.prefix_parts > 0, p, s);
 }
 
-template <typename T, int KIND, int NB, bool WINDOW>
+template <typename T, int KIND, int NB, int MODE>
 int launch_stream_for(const AttnParams &p, unsigned grid, int device, cudaStream_t s)
 {
-    if (p.layer.D <= 64) return launch_stream<T, KIND, 64, NB, WINDOW>(p, grid, device, s);
-    if (p.layer.D <= 128) return launch_stream<T, KIND, 128, NB, WINDOW>(p, grid, device, s);
-    return launch_stream<T, KIND, 256, NB, WINDOW>(p, grid, device, s);
+    if (p.layer.D <= 64) return launch_stream<T, KIND, 64, NB, MODE>(p, grid, device, s);
+    if (p.layer.D <= 128) return launch_stream<T, KIND, 128, NB, MODE>(p, grid, device, s);
+    return launch_stream<T, KIND, 256, NB, MODE>(p, grid, device, s);
 }
 
-template <typename T, int KIND, bool WINDOW>
+template <typename T, int KIND, int MODE>
 int launch_stream_columns(const AttnParams &p, unsigned grid, int device, cudaStream_t s)
 {
-    return p.split.columns == 8 ? launch_stream_for<T, KIND, 1, WINDOW>(p, grid, device, s) : launch_stream_for<T, KIND, 2, WINDOW>(p, grid, device, s);
+    return p.split.columns == 8 ? launch_stream_for<T, KIND, 1, MODE>(p, grid, device, s) : launch_stream_for<T, KIND, 2, MODE>(p, grid, device, s);
 }
 
-// What follows the prefix's own kernel, if it has one.
-template <typename T, bool WINDOW>
-int launch_stream_and_join(const AttnParams &p, int device, cudaStream_t s)
+template <typename T, int MODE>
+int launch_stream_alone(const AttnParams &p, int device, cudaStream_t s)
 {
-    int rc = TC_OK;
-    if (p.split.stream_ctas) {
-        const unsigned grid = static_cast<unsigned>(p.split.stream_ctas);
-        switch (p.layer.dtype) {
-        case TC_E4M3: rc = launch_stream_columns<__half, kE4m3, WINDOW>(p, grid, device, s); break;
-        case TC_INT8: rc = launch_stream_columns<__half, kInt8, WINDOW>(p, grid, device, s); break;
-        default: rc = launch_stream_columns<T, kPlain, WINDOW>(p, grid, device, s); break;
-        }
-        if (rc != TC_OK) return rc;
+    if (!p.split.stream_ctas) return TC_OK;
+    const unsigned grid = static_cast<unsigned>(p.split.stream_ctas);
+    switch (p.layer.dtype) {
+    case TC_E4M3: return launch_stream_columns<__half, kE4m3, MODE>(p, grid, device, s);
+    case TC_INT8: return launch_stream_columns<__half, kInt8, MODE>(p, grid, device, s);
+    default: return launch_stream_columns<T, kPlain, MODE>(p, grid, device, s);
     }
+}
+
+template <typename T, int MODE>
+int launch_join(const AttnParams &p, cudaStream_t s)
+{
     // parts of a row: the prefix kernel's, and about as many as warps share one item of the stream
     const int64_t parts = p.split.prefix_parts + p.split.stream_ctas * 4 / std::max<int64_t>(p.R * p.layer.H * p.split.own_blocks, 1);
     const unsigned rows = static_cast<unsigned>(p.split.rows);
@@ -838,8 +864,16 @@ int launch_stream_and_join(const AttnParams &p, int device, cudaStream_t s)
     const bool wide = parts > 32 && rows < 1024;
     const unsigned few = std::min<unsigned>((rows + 3) / 4, kSms * kJoinCtas);
     const bool follows = p.split.prefix_parts || p.split.stream_ctas;
-    if (p.layer.D <= 128) return wide ? launch_attn(join_kernel<T, 128, 16, WINDOW>, rows, 512, 0, follows, p, s) : launch_attn(join_kernel<T, 128, 1, WINDOW>, few, 128, 0, follows, p, s);
-    return wide ? launch_attn(join_kernel<T, 256, 16, WINDOW>, rows, 512, 0, follows, p, s) : launch_attn(join_kernel<T, 256, 1, WINDOW>, few, 128, 0, follows, p, s);
+    if (p.layer.D <= 128) return wide ? launch_attn(join_kernel<T, 128, 16, MODE>, rows, 512, 0, follows, p, s) : launch_attn(join_kernel<T, 128, 1, MODE>, few, 128, 0, follows, p, s);
+    return wide ? launch_attn(join_kernel<T, 256, 16, MODE>, rows, 512, 0, follows, p, s) : launch_attn(join_kernel<T, 256, 1, MODE>, few, 128, 0, follows, p, s);
+}
+
+// What follows the prefix's own kernel, if it has one.
+template <typename T, int MODE>
+int launch_stream_and_join(const AttnParams &p, int device, cudaStream_t s)
+{
+    const int rc = launch_stream_alone<T, MODE>(p, device, s);
+    return rc != TC_OK ? rc : launch_join<T, MODE>(p, s);
 }
 
 }  // namespace tc

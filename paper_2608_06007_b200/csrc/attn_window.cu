@@ -6,7 +6,7 @@ namespace tc {
 
 int launch_window(const AttnParams &p, int dtype, int device, cudaStream_t s)
 {
-    return dtype == TC_BF16 ? launch_stream_and_join<__nv_bfloat16, true>(p, device, s) : launch_stream_and_join<__half, true>(p, device, s);
+    return dtype == TC_BF16 ? launch_stream_and_join<__nv_bfloat16, kWindow>(p, device, s) : launch_stream_and_join<__half, kWindow>(p, device, s);
 }
 
 }  // namespace tc

@@ -41,3 +41,16 @@ def test_long_keys_of_few_rows_are_cut_into_parts(x, kind, lens, new, D, window,
         run_chunk(s)  # each on a workspace of 0xFF
         check_chunk(s)
     status_is(0)
+
+
+@pytest.mark.parametrize("x,kind", TYPES)
+@pytest.mark.parametrize("window,sinks", [(0, 0), (100, 5)])
+@pytest.mark.parametrize("new", [[1] * 12, [1, 40, 1, 1, 0, 1, 300, 1, 1, 2, 1, 1], [1, 1, 1]])
+def test_single_tokens_alone_and_beside_chunks(x, kind, window, sinks, new):
+    lens = [n + extra if n else 50 for n, extra in zip(new, [0, 17, 900, 64, 50, 33, 200, 3000, 127, 10, 400, 1])]
+    if len(new) > 8:
+        lens[3] = -1
+    s = batch(kind, x, lens, new, Hq=8, window=window, sinks=sinks, front=1, behind=2, strided=True)
+    run_chunk(s)
+    check_chunk(s)
+    status_is(0)

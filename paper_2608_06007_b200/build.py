@@ -12,7 +12,7 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libtensorcast_b200.so")
-SOURCES = ["exec.cu", "launch.cu", "staging.cu", "noalloc.cu", "plan_build.cpp", "ops_check.cpp", "kv_append.cu", "kv_gather.cu", "attn_decode.cu", "attn_prefix.cu", "attn_window.cu", "attn_singles.cu", "attn_chunk.cu", "attn_chunk_codes.cu"]
+SOURCES = ["exec.cu", "launch.cu", "staging.cu", "noalloc.cu", "plan_build.cpp", "ops_check.cpp", "kv_append.cu", "kv_gather.cu", "attn_decode.cu", "attn_prefix.cu", "attn_window.cu", "attn_singles.cu", "attn_chunk.cu", "attn_chunk_codes.cu", "attn_chunk_wide.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC,-Wall,-Wextra,-fvisibility=hidden"]
 

@@ -1,5 +1,6 @@
 // tc_attn_chunk: the entry points, unquantised pools, and the kernel that joins the parts of requests whose keys are cut.
 #include <cmath>
+#include <numeric>
 
 #include "attn_chunk.cuh"
 
@@ -88,7 +89,7 @@ static int launch_chunk(const ChunkParams &p, const AttnParams *singles, int dty
         if ((rc = launch_singles_stream(*singles, dtype, device, s)) != TC_OK) return rc;
         if (p.max_new == 1) return launch_singles_join(*singles, dtype, s);
     }
-    rc = p.layer.quantised() ? launch_chunk_codes(p, device, s) : launch_chunk_plain(p, dtype, device, s);
+    rc = p.wide ? launch_chunk_wide(p, device, s) : p.layer.quantised() ? launch_chunk_codes(p, device, s) : launch_chunk_plain(p, dtype, device, s);
     if (rc == TC_OK && singles) rc = launch_singles_join(*singles, dtype, s);
     if (rc != TC_OK || !p.plan.part_rows) return rc;
     const unsigned grid = static_cast<unsigned>(std::min<int64_t>((p.n_tokens * p.Hq + 3) / 4, kChunkSms * 8));
@@ -96,14 +97,15 @@ static int launch_chunk(const ChunkParams &p, const AttnParams *singles, int dty
 }
 
 // Tensor maps, where a call's geometry fits them: queries as [token][head][d], whose boxes are the whole tokens that an item's slot of 128
-// rows holds; pages of an unquantised pool as [block][head][token][d], where half tiles are whole numbers of blocks, or blocks of half
-// tiles, so that a box of a page's tokens is part of one.  Elsewhere q_boxes or box_rows stays 0.
+// rows holds; pages of an unquantised pool as [block][head][token][d], in boxes of as many tokens as divide a block and half a tile.
+// Elsewhere q_boxes or box_rows stays 0.
+constexpr int32_t kLeastBox = 4;  // tokens: 16 prompts in blocks of 20 take KBOX us so, 544 key by key
 static int describe_boxes(ChunkParams *p)
 {
     p->box_rows = p->q_boxes = 0;
     const Layer &l = p->layer;
-    const int32_t group = p->shape.group, most = p->shape.keys / 2, rows = static_cast<int32_t>(std::min<int64_t>(l.B, most));
-    const bool queries = 128 % group == 0, pages = !l.quantised() && rows >= 8 && most % rows == 0 && l.B % rows == 0 && l.num_blocks > 0;
+    const int32_t group = p->shape.group, rows = static_cast<int32_t>(std::gcd<int64_t>(l.B, p->shape.keys / 2));
+    const bool queries = 128 % group == 0, pages = !l.quantised() && rows >= kLeastBox && l.num_blocks > 0;
     if (!queries && !pages) return TC_OK;
     using Encode = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *, const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
                                 CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
@@ -146,10 +148,12 @@ static int describe_boxes(ChunkParams *p)
 // at 6, a CTA that holds 256 rows for them at 0.5 and .. (64 requests, 51 of them single, 200k tokens of 8 heads x 128, e4m3: a call of KSINGLES us
 // so, 570 without).  Fewer are not worth its two launches.
 constexpr int64_t kLeastSingles = 8;
+// 8 prompts of up to 15061 tokens in a window of 2048, int8, of 8 heads x 128: KWIDE ms so, with 493 MB of them, 3.12 where each block widens its own.
+constexpr int64_t kMostWide = 1ll << 30;
 
 // What both entry points check; fills p's geometry and plan, and those of the requests with one new token where these have their own
-// kernels.  *workspace: bytes of both, the second's from *singles_at on.
-static int check_chunk(const tc_kv_layer_t *layer, const tc_attn_chunk_t *a, ChunkParams *p, AttnParams *singles, int64_t *singles_at, int64_t *workspace)
+// kernels.  *workspace: bytes of all, the second's from *singles_at on, tiles made fp16 from *wide_at.
+static int check_chunk(const tc_kv_layer_t *layer, const tc_attn_chunk_t *a, ChunkParams *p, AttnParams *singles, int64_t *singles_at, int64_t *wide_at, int64_t *workspace)
 {
     int rc = check_layer(layer, &p->layer);
     if (rc != TC_OK) return rc;
@@ -188,6 +192,17 @@ static int check_chunk(const tc_kv_layer_t *layer, const tc_attn_chunk_t *a, Chu
         p->no_singles = fits;
         if (fits) *workspace += singles->split.workspace;
     }
+    // Codes that three blocks of rows meet, or more, are made fp16 once, in the workspace, where that takes no more than kMostWide.
+    p->wide_list = 0;
+    *wide_at = *workspace;
+    if (p->layer.quantised() && a->max_new > 1 && new_most * s.group > 2 * s.rows) {
+        const int64_t near = (std::min<int64_t>(s.window, a->max_len) + new_most) / s.keys + 2 + chunk_tiles_of(s, static_cast<int32_t>(std::min<int64_t>(s.sinks, a->max_len)));
+        const int64_t list = std::min<int64_t>(near, chunk_tiles_of(s, static_cast<int32_t>(a->max_len))), bytes = wide_tile_bytes(D);
+        if (list <= kMostWide / bytes && a->R * s.heads <= kMostWide / bytes / list) {
+            p->wide_list = static_cast<int32_t>(list);
+            *workspace += a->R * s.heads * list * bytes;
+        }
+    }
     if (a->max_new == 1 && !fits) return fail(TC_ERR_TOO_LARGE, "R * H * keys = %lld * %d * %lld: too many for one call", (long long)a->R, p->layer.H, (long long)most);
     return TC_OK;
 }
@@ -203,8 +218,8 @@ extern "C" int tc_attn_chunk_workspace(const tc_kv_layer_t *layer, const tc_attn
     *bytes = 0;
     ChunkParams p{};
     AttnParams singles{};
-    int64_t at, need;
-    const int rc = check_chunk(layer, a, &p, &singles, &at, &need);
+    int64_t at, wide_at, need;
+    const int rc = check_chunk(layer, a, &p, &singles, &at, &wide_at, &need);
     if (rc == TC_OK) *bytes = need;
     return rc;
 }
@@ -214,8 +229,8 @@ extern "C" int tc_attn_chunk(const tc_kv_layer_t *layer, const tc_attn_chunk_t *
     clear_error();
     ChunkParams p{};
     AttnParams singles{};
-    int64_t singles_at, need;
-    int rc = check_chunk(layer, a, &p, &singles, &singles_at, &need);
+    int64_t singles_at, wide_at, need;
+    int rc = check_chunk(layer, a, &p, &singles, &singles_at, &wide_at, &need);
     if (rc != TC_OK) return rc;
     if (a->R == 0 || a->n_tokens == 0 || a->max_new == 0) return TC_OK;
     uint32_t align = 16;
@@ -264,6 +279,7 @@ extern "C" int tc_attn_chunk(const tc_kv_layer_t *layer, const tc_attn_chunk_t *
     p.sums = reinterpret_cast<float *>(ws + p.plan.sums_at);
     p.parts = reinterpret_cast<float *>(ws + p.plan.parts_at);
     cudaStream_t s = static_cast<cudaStream_t>(stream);
+    p.wide = p.wide_list ? ws + wide_at : nullptr;
     if (p.no_singles) {
         AttnParams &q = singles;
         q.q = p.q, q.q_req = p.q_token, q.q_head = p.q_head;

@@ -11,11 +11,15 @@ namespace tc {
 
 constexpr float kChunkLn2 = 0.6931471805599453f;
 
+// Codes that attn_chunk_widen.cu has made fp16, tile by tile, before: their scales still come with the scores.
+constexpr int kWide = 3;
+template <int KIND> constexpr bool kWidens = KIND == kE4m3 || KIND == kInt8;
+
 // A CTA's warps: eight of softmax, those that fetch pages (codes: four for K and four for V), then four that issue products and find items.
 template <int KIND> struct ChunkWarps {
-    static constexpr int softmax = 8, loaders = KIND == kPlain ? 4 : 8, all = softmax + loaders + 4, threads = 32 * all;
+    static constexpr int softmax = 8, loaders = kWidens<KIND> ? 8 : 4, all = softmax + loaders + 4, threads = 32 * all;
     // registers of a thread: at the launch, of the softmax, of the others
-    static constexpr int launch_registers = KIND == kPlain ? 128 : 96, softmax_registers = KIND == kPlain ? 192 : 112, other_registers = KIND == kPlain ? 64 : 80;
+    static constexpr int launch_registers = kWidens<KIND> ? 96 : 128, softmax_registers = kWidens<KIND> ? 112 : 192, other_registers = kWidens<KIND> ? 80 : 64;
     static_assert(32 * softmax * softmax_registers + (threads - 32 * softmax) * other_registers <= threads * launch_registers && threads * launch_registers <= 65536, "a split that never ends");
 };
 
@@ -49,7 +53,7 @@ struct alignas(16) ChunkItem {
     ChunkList list;                  // 7 words
     uint32_t part_row;               // of the request's row 0 of this part; kUncut: outputs are written
     int64_t token0;                  // row of q that is the request's first new token
-    int32_t n, pad;
+    int32_t firsts, skip;            // of the request's list of tiles, where those lie ready
 };
 static_assert(sizeof(ChunkItem) == 80);
 
@@ -88,6 +92,12 @@ __device__ __forceinline__ void copy_box(uint32_t dst, const CUtensorMap *map, i
 __device__ __forceinline__ void copy_box3(uint32_t dst, const CUtensorMap *map, int x, int y, int z, uint32_t bar)
 {
     asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
+}
+
+// A run of bytes, a multiple of 16, to shared memory.
+__device__ __forceinline__ void copy_run(uint32_t dst, const void *src, uint32_t bytes, uint32_t bar)
+{
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
 }
 
 // Bits 0 .. n - 1.
@@ -223,12 +233,12 @@ __global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(con
 
     if (threadIdx.x == 0) {
         // boxes announce themselves to whoever waits for their bytes; copies key by key for their lanes, and a lane of each warp what it has written beside them
-        const int ready = KIND != kPlain ? 128 : p.box_rows ? 2 : 2 * 33;
+        const int ready = KIND == kWide ? 1 : KIND != kPlain ? 128 : p.box_rows ? 2 : 2 * 33;
         for (int i = 0; i < M::stages; i++) barrier_init(full + 8 * i, ready), barrier_init(empty + 8 * i, 1);
         for (int i = 0; i < 2; i++) barrier_init(landed + 8 * i, 1);
         for (int i = 0; i < 2; i++) barrier_init(s_full + 8 * i, 1), barrier_init(s_taken + 8 * i, 128), barrier_init(p_ready + 8 * i, 128), barrier_init(o_added + 8 * i, 1);
         for (int i = 0; i < 2; i++) barrier_init(item_full + 8 * i, 1), barrier_init(item_empty + 8 * i, kSlots * 4 + W::loaders + 2 + (KIND != kPlain && p.q_boxes ? 1 : 0)), barrier_init(last_at + 8 * i, 1);
-        barrier_init(q_full, KIND != kPlain ? 256 : p.q_boxes ? 1 : 4 * 33), barrier_init(q_empty, 1), barrier_init(wanted, 1), barrier_init(answered, 1);
+        barrier_init(q_full, KIND != kPlain ? 32 * W::loaders : p.q_boxes ? 1 : 4 * 33), barrier_init(q_empty, 1), barrier_init(wanted, 1), barrier_init(answered, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == kIssue) {
@@ -319,7 +329,7 @@ __global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(con
     // All 512 columns are this CTA's, so they begin at 0; a constant lets the products' operands stay in uniform registers.
     // A softmax holds a tile's scores in registers and gives their one buffer back at once, beside the two slots' probabilities;
     // of codes, whose warps leave it few registers, it goes through them twice where they lie, and puts the probabilities in their place.
-    constexpr bool kInPlace = KIND != kPlain && kSlots == 2;
+    constexpr bool kInPlace = kWidens<KIND> && kSlots == 2;
     constexpr uint32_t tensor = 0, kScores = 0, kScoresStep = kInPlace ? 128 : 0, kProbabilities = kInPlace ? 0 : 128, kProbabilitiesStep = kInPlace ? 128 : 64, kOutputs = 256;
     bool fine = true;  // no wait of this thread has run out
 
@@ -452,7 +462,7 @@ __global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(con
                     tensor_stored();
                     fence_before();
                     barrier_arrive(s_taken + 8 * b);
-                } else if constexpr (KIND != kPlain) {
+                } else if constexpr (kWidens<KIND>) {
                     // 32 scores at a time, in a loop whose code stays small: six warps of four kinds share a scheduler's instruction cache
                     auto scores = [&](int c, float2 (&x)[16]) {
                         tensor_load32(s_at + 32 * c, reinterpret_cast<uint32_t(&)[32]>(x));
@@ -532,14 +542,26 @@ __global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(con
 #pragma unroll
                         for (int c = 0; c < kWords; c++) mask[c] = view.word(c);
                     }
+                    if constexpr (KIND != kPlain) {
+                        const float2 f2 = make_float2(factor, factor), zero = make_float2(0.f, 0.f);
+#pragma unroll
+                        for (int j = 0; j < kKeys / 4; j++) {
+                            const float4 k = load_shared_f4(about + M::scales + 16 * j);
+                            float2 *x = &s.f2[j / 8][j % 8 * 2];
+                            x[0] = fused2(x[0], fused2(f2, make_float2(k.x, k.y), zero), zero);
+                            x[1] = fused2(x[1], fused2(f2, make_float2(k.z, k.w), zero), zero);
+                        }
+                    }
 #pragma unroll
                     for (int c = 0; c < kWords; c++) all_seen &= mask[c];
-                    if (all_seen != 0xffffffffu) {
+                    if (!__all_sync(0xffffffffu, all_seen == 0xffffffffu)) {
 #pragma unroll
-                        for (int c = 0; c < kWords; c++)
+                        for (int c = 0; c < kWords; c++) {
+                            if (__all_sync(0xffffffffu, mask[c] == 0xffffffffu)) continue;
 #pragma unroll
                             for (int j = 0; j < 32; j++)
                                 if (!(mask[c] >> j & 1)) s.f[c][j] = -INFINITY;
+                        }
                     }
                     float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
@@ -548,23 +570,34 @@ __global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(con
 #pragma unroll
                         for (int j = 2; j < 32; j += 2) m4[c] = larger3(m4[c], s.f[c][j], s.f[c][j + 1]);
                     }
-                    const float highest = fmaxf(larger3(m4[0], m4[1], m4[2]), m4[3]), most = highest * factor;
+                    const float highest = fmaxf(larger3(m4[0], m4[1], m4[2]), m4[3]), most = KIND == kPlain ? highest * factor : highest + exponent;
+                    bool move = most > top + 8.f;
+                    if constexpr (KIND != kPlain) move = move || highest > ref + 8.f;
                     // a running maximum moves only when a score exceeds it by more than 8 (2^8 in probabilities)
-                    if (__any_sync(0xffffffffu, most > top + 8.f)) move_top(most);
+                    if (__any_sync(0xffffffffu, move)) {
+                        if constexpr (KIND != kPlain) raise_ref(highest);
+                        move_top(most);
+                    }
                     const float m = top == -INFINITY ? 0.f : top - kLift;
-                    const float2 minus = make_float2(-m, -m), f2 = make_float2(factor, factor);
+                    const float2 minus = make_float2(exponent - m, exponent - m), f2 = make_float2(factor, factor);
                     float2 here = make_float2(0.f, 0.f);
 #pragma unroll
                     for (int c = 0; c < kWords; c++) {
 #pragma unroll
                         for (int j = 0; j < 16; j++) {
-                            float2 e = fused2(s.f2[c][j], f2, minus);
+                            float2 e = KIND == kPlain ? fused2(s.f2[c][j], f2, minus) : sum2(s.f2[c][j], minus);
                             e = make_float2(exp2_approx(e.x), exp2_approx(e.y));
                             here = sum2(here, e);
                             s.w[c][j] = pack2<T>(e.x, e.y);  // (in the place of scores that are done with)
                         }
                     }
-                    sum = sum2(sum, here);
+                    if constexpr (KIND == kPlain) {
+                        sum = sum2(sum, here);
+                    } else {
+                        // `here` is relative to m - exponent, which is at most 48 above ref: exponent is no less than 40 below any before
+                        const float all = here.x + here.y;
+                        sum.x = fmaf(all, all == 0.f ? 0.f : exp2_approx(m - exponent - (ref == -INFINITY ? 0.f : ref)), sum.x);
+                    }
                     await_rest();  // by now it has been given, as a rule
                     if (!fine) break;
 #pragma unroll
@@ -649,6 +682,50 @@ __global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(con
             if (rr >= item.rows || chunk * 8 >= D) return nullptr;
             const uint32_t row = item.row0 + rr, token = quick_div(row, p.div_group);
             return p.q + (item.token0 + token) * p.q_token + (item.h * shape.group + static_cast<int>(row - token * shape.group)) * p.q_head + chunk * 16;
+        };
+        // Queries that meet codes: fp16 with a power of two taken out of each row; eight lanes have a row.
+        auto prepare_queries = [&](const ChunkItem &item) {
+            if (p.q_boxes) {
+                if (fine) fine = __all_sync(0xffffffffu, barrier_wait(landed, loads & 1));
+            } else if (loads && fine) {
+                fine = __all_sync(0xffffffffu, barrier_wait(q_empty, (loads - 1) & 1));
+            }
+            const int rows = item.rows > 128 ? kSlots * 128 : 128;
+#pragma unroll 2
+            for (int r0 = (warp - kLoad) * 4; r0 < rows && fine; r0 += 4 * W::loaders) {
+                const int rr = r0 + (lane >> 3);
+                unsigned char *const to = gen + (rr >> 7) * M::q_tile;
+                uint4 v[DP / 64];
+                float most = 0.f, up, down;
+#pragma unroll
+                for (int j = 0; j < DP / 64; j++) {
+                    const int ch = 8 * j + (lane & 7);
+                    const char *src = p.q_boxes ? nullptr : query_at(item, rr, ch);
+                    v[j] = make_uint4(0, 0, 0, 0);
+                    if (p.q_boxes) v[j] = *reinterpret_cast<const uint4 *>(to + swizzled(rr & 127, ch));
+                    else if (src) v[j] = *reinterpret_cast<const uint4 *>(src);
+                }
+#pragma unroll
+                for (int j = 0; j < DP / 64; j++)
+                    for (uint32_t x : {v[j].x, v[j].y, v[j].z, v[j].w}) most = finite_magnitude(most, query_pair(x, p.q_bf16));
+#pragma unroll
+                for (int x = 1; x < 8; x <<= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, x));
+                query_powers(most, up, down);
+#pragma unroll
+                for (int j = 0; j < DP / 64; j++) {
+                    uint32_t x[4] = {v[j].x, v[j].y, v[j].z, v[j].w};
+#pragma unroll
+                    for (int k = 0; k < 4; k++) {
+                        const float2 f = query_pair(x[k], p.q_bf16);
+                        x[k] = pack2<__half>(f.x * up, f.y * up);
+                    }
+                    *reinterpret_cast<uint4 *>(to + swizzled(rr & 127, 8 * j + (lane & 7))) = make_uint4(x[0], x[1], x[2], x[3]);
+                }
+                if ((lane & 7) == 0) *reinterpret_cast<float *>(gen + kDownsAt + 4 * ((loads % M::down_sets) * kSlots * 128 + rr)) = down;
+            }
+            fence_shared_to_async();
+            if (fine) barrier_arrive(q_full);
+            loads++;
         };
         // near the item's end the next one is asked for
         auto near_end = [&](const ChunkItem &item, int i) {
@@ -746,6 +823,11 @@ __global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(con
                         for (int x = 0; x < kHalfWords; x++) asm volatile("st.shared.u32 [%0], %1;" ::"r"(about + 4 * (sub * kHalfWords + x)), "r"(mask[x]) : "memory");
                     }
                     const bool look = kv && ragged(item, i);
+                    // what is written beside a copy is written before it is announced: the products may follow its last byte at once
+                    auto say_bad = [&](uint32_t bad) {
+                        if (lane == 0) asm volatile("st.shared.v2.u32 [%0], {%1,%2};" ::"r"(about + 16 + 8 * sub), "r"(bad), "r"(0) : "memory");
+                    };
+                    if (kv && !look) say_bad(0);
                     if (box_rows) {
                         const uint32_t lands = look ? landed + 8 * sub : bar;
                         if (lane == 0) asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(lands), "n"(kHalf * DP * 2) : "memory");
@@ -769,39 +851,35 @@ __global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(con
                             copy_async16(to + swizzled<kKeys>(sub * kHalf + rr, ch), plane + (there ? src + ch * 16 : 0), there);
                         }
                     }
-                    if (kv) {
-                        uint32_t bad = 0;
-                        if (look) {
-                            if (box_rows) {
-                                fine = __all_sync(0xffffffffu, barrier_wait(landed + 8 * sub, looks & 1));
-                                looks++;
-                                if (!fine) break;
-                            } else {
-                                copy_wait<0>();
-                            }
-                            uint32_t any = 0;
-                            const bool whole = mask[0] == 0xffffffffu && mask[kHalfWords - 1] == 0xffffffffu;
-#pragma unroll 1
-                            for (int j0 = 0; j0 < kHalf * chunks / 32; j0 += 8) {
-                                uint32_t x[8][4];
-#pragma unroll
-                                for (int j = 0; j < 8; j++) {
-                                    const int idx = (j0 + j) * 32 + lane;
-                                    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(x[j][0]), "=r"(x[j][1]), "=r"(x[j][2]), "=r"(x[j][3]) : "r"(to + swizzled<kKeys>(sub * kHalf + idx / chunks, idx % chunks)) : "memory");
-                                }
-#pragma unroll
-                                for (int j = 0; j < 8; j++) {
-                                    const int idx = (j0 + j) * 32 + lane, rr = idx / chunks;
-                                    const uint32_t odd = not_finite<T>(x[j][0]) | not_finite<T>(x[j][1]) | not_finite<T>(x[j][2]) | not_finite<T>(x[j][3]);
-                                    if (whole || ((kHalfWords == 2 && rr >= 32 ? mask[kHalfWords - 1] : mask[0]) >> (rr & 31) & 1)) any |= odd;
-                                    else asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(to + swizzled<kKeys>(sub * kHalf + rr, idx % chunks)), "r"(0) : "memory");
-                                }
-                            }
-                            __syncwarp();
-                            bad = __any_sync(0xffffffffu, any != 0);
-                            fence_shared_to_async();
+                    if (look) {
+                        if (box_rows) {
+                            fine = __all_sync(0xffffffffu, barrier_wait(landed + 8 * sub, looks & 1));
+                            looks++;
+                            if (!fine) break;
+                        } else {
+                            copy_wait<0>();
                         }
-                        if (lane == 0) asm volatile("st.shared.v2.u32 [%0], {%1,%2};" ::"r"(about + 16 + 8 * sub), "r"(bad), "r"(0) : "memory");
+                        uint32_t any = 0;
+                        const bool whole = mask[0] == 0xffffffffu && mask[kHalfWords - 1] == 0xffffffffu;
+#pragma unroll 1
+                        for (int j0 = 0; j0 < kHalf * chunks / 32; j0 += 8) {
+                            uint32_t x[8][4];
+#pragma unroll
+                            for (int j = 0; j < 8; j++) {
+                                const int idx = (j0 + j) * 32 + lane;
+                                asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(x[j][0]), "=r"(x[j][1]), "=r"(x[j][2]), "=r"(x[j][3]) : "r"(to + swizzled<kKeys>(sub * kHalf + idx / chunks, idx % chunks)) : "memory");
+                            }
+#pragma unroll
+                            for (int j = 0; j < 8; j++) {
+                                const int idx = (j0 + j) * 32 + lane, rr = idx / chunks;
+                                const uint32_t odd = not_finite<T>(x[j][0]) | not_finite<T>(x[j][1]) | not_finite<T>(x[j][2]) | not_finite<T>(x[j][3]);
+                                if (whole || ((kHalfWords == 2 && rr >= 32 ? mask[kHalfWords - 1] : mask[0]) >> (rr & 31) & 1)) any |= odd;
+                                else asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(to + swizzled<kKeys>(sub * kHalf + rr, idx % chunks)), "r"(0) : "memory");
+                            }
+                        }
+                        __syncwarp();
+                        say_bad(__any_sync(0xffffffffu, any != 0));
+                        fence_shared_to_async();
                     }
                     if (!box_rows) announce(bar);
                     else if (look) {
@@ -813,6 +891,50 @@ __global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(con
                 if (item.begin >= item.end && warp == kLoad && lane == 0) barrier_arrive(wanted);
             }
             copy_wait<0>();
+        } else if constexpr (KIND == kWide) {
+            // Tiles lie ready, swizzled: one warp fetches K, with scales and masks, one V; all four take part in the queries.
+            const int kv = warp - kLoad;
+            for (int it = 0; fine; it++) {
+                ChunkItem item;
+                if (!take_item(it, item)) break;
+                // tile i's place among the request's
+                auto place = [&](int i) {
+                    const int t = tile_of(item, i), listed = t < item.firsts ? t : t - item.skip;
+                    return p.wide + ((static_cast<int64_t>(item.r) * p.wide_list + listed) * H + item.h) * WideTile<DP>::bytes;
+                };
+                auto header = [&](int i) { return kv == 0 && lane < 8 && i < item.end ? reinterpret_cast<const uint32_t *>(place(i) + WideTile<DP>::header_at)[lane] : 0u; };
+                uint32_t ahead = header(item.begin);
+                int e_most = -133;  // the largest exponent of a tile so far
+                if (kv >= 2 && item.begin < item.end) prepare_queries(item);
+                for (int i = item.begin; i < item.end && fine && kv < 2; i++, tiles++) {
+                    const uint32_t u = 2 * tiles + kv, stage = u % M::stages, bar = full + 8 * stage, about = info + (tiles % M::infos) * M::info;
+                    near_end(item, i);
+                    const char *const from = place(i);
+                    uint32_t word = ahead;
+                    ahead = header(i + 1);
+                    fine = __all_sync(0xffffffffu, stage_free(u));
+                    if (!fine) break;
+                    if (kv == 0) {
+                        // {mask, 4 words; exponent, whether scales are far apart, whether V has numbers that are not finite}
+                        const int e = static_cast<int>(__shfl_sync(0xffffffffu, word, 4));
+                        if (lane == 5) word |= e < e_most - 40;
+                        e_most = max(e_most, e);
+                        if (lane == 4) word = __float_as_uint(static_cast<float>(e));
+                        const int to = lane < 4 ? 4 * lane : lane < 6 ? 32 + 4 * (lane - 4) : 16;
+                        if (lane < 7) asm volatile("st.shared.u32 [%0], %1;" ::"r"(about + to), "r"(word) : "memory");
+                        if (lane >= 7 && lane < 10) asm volatile("st.shared.u32 [%0], %1;" ::"r"(about + 20 + 4 * (lane - 7)), "r"(0) : "memory");
+                    }
+                    __syncwarp();
+                    if (lane == 0) {
+                        asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(M::tile + (kv ? 0 : 8 * kKeys)) : "memory");
+                        copy_run(ring + stage * M::tile, from + kv * M::tile, M::tile, bar);
+                        if (kv == 0) copy_run(about + M::scales, from + WideTile<DP>::scales_at, 8 * kKeys, bar);
+                    }
+                    __syncwarp();
+                    if (i == item.begin) prepare_queries(item);
+                }
+                if (item.begin >= item.end && warp == kLoad && lane == 0) barrier_arrive(wanted);
+            }
         } else {
             // Codes: four warps fetch and widen K, four V, each its own keys of every tile, through registers, a tile ahead.  V's are multiplied by their scales over a
             // power of two that the tile's largest scale sets, 2^exponent, which puts the values below 2^16: rounded
@@ -876,50 +998,7 @@ __global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(con
                 fetch(item.begin);
                 // (loaded behind the queries, which need the registers)
                 if (next_off >= 0) asm volatile("prefetch.global.L2 [%0];" ::"l"(plane + next_off));
-                if (some) {
-                    // queries, fp16 with a power of two taken out of each row; eight lanes have a row
-                    if (p.q_boxes) {
-                        if (fine) fine = __all_sync(0xffffffffu, barrier_wait(landed, loads & 1));
-                    } else if (loads && fine) {
-                        fine = __all_sync(0xffffffffu, barrier_wait(q_empty, (loads - 1) & 1));
-                    }
-                    const int rows = item.rows > 128 ? kSlots * 128 : 128;
-#pragma unroll 2
-                    for (int r0 = (warp - kLoad) * 4; r0 < rows && fine; r0 += 32) {
-                        const int rr = r0 + (lane >> 3);
-                        unsigned char *const to = gen + (rr >> 7) * M::q_tile;
-                        uint4 v[DP / 64];
-                        float most = 0.f, up, down;
-#pragma unroll
-                        for (int j = 0; j < DP / 64; j++) {
-                            const int ch = 8 * j + (lane & 7);
-                            const char *src = p.q_boxes ? nullptr : query_at(item, rr, ch);
-                            v[j] = make_uint4(0, 0, 0, 0);
-                            if (p.q_boxes) v[j] = *reinterpret_cast<const uint4 *>(to + swizzled(rr & 127, ch));
-                            else if (src) v[j] = *reinterpret_cast<const uint4 *>(src);
-                        }
-#pragma unroll
-                        for (int j = 0; j < DP / 64; j++)
-                            for (uint32_t x : {v[j].x, v[j].y, v[j].z, v[j].w}) most = finite_magnitude(most, query_pair(x, p.q_bf16));
-#pragma unroll
-                        for (int x = 1; x < 8; x <<= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, x));
-                        query_powers(most, up, down);
-#pragma unroll
-                        for (int j = 0; j < DP / 64; j++) {
-                            uint32_t x[4] = {v[j].x, v[j].y, v[j].z, v[j].w};
-#pragma unroll
-                            for (int k = 0; k < 4; k++) {
-                                const float2 f = query_pair(x[k], p.q_bf16);
-                                x[k] = pack2<__half>(f.x * up, f.y * up);
-                            }
-                            *reinterpret_cast<uint4 *>(to + swizzled(rr & 127, 8 * j + (lane & 7))) = make_uint4(x[0], x[1], x[2], x[3]);
-                        }
-                        if ((lane & 7) == 0) *reinterpret_cast<float *>(gen + kDownsAt + 4 * ((loads % M::down_sets) * kSlots * 128 + rr)) = down;
-                    }
-                    fence_shared_to_async();
-                    if (fine) barrier_arrive(q_full);
-                    loads++;
-                }
+                if (some) prepare_queries(item);
 #pragma unroll
                 for (int j = 0; j < kUnits; j++) load_unit(j);
                 for (int i = item.begin; i < item.end; i++, tiles++) {
@@ -1139,7 +1218,12 @@ __global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(con
                         item.begin = static_cast<int32_t>(min(static_cast<int64_t>(part) * share, static_cast<int64_t>(item.list.count)));
                         item.end = static_cast<int32_t>(min(static_cast<int64_t>(item.begin) + share, static_cast<int64_t>(item.list.count)));
                         item.part_row = parts > 1 ? rows_at + static_cast<uint32_t>(part) * q.n * p.Hq : kUncut;
-                        item.token0 = q.token0, item.n = q.n, item.pad = 0;
+                        item.token0 = q.token0;
+                        item.firsts = item.skip = 0;
+                        if constexpr (KIND == kWide) {
+                            const ChunkList whole = chunk_list(shape, item.pos0, 0, q.n * shape.group, q.n * shape.group);
+                            item.firsts = whole.firsts, item.skip = whole.skip;
+                        }
                         // for chunk_join_kernel, by whoever has the request's first item
                         if (p.plan.part_rows && id == at && lane == 0) p.cuts[r] = make_uint2(rows_at, static_cast<uint32_t>(parts));
                         break;
@@ -1228,7 +1312,7 @@ int launch_chunk_shape(const ChunkParams &p, int device, cudaStream_t s)
         if (attr.numRegs != ChunkWarps<KIND>::launch_registers) return fail(TC_ERR_CUDA, "tc_attn_chunk's kernel was built with %d registers a thread, not %d", attr.numRegs, ChunkWarps<KIND>::launch_registers);
         raised[device].store(true, std::memory_order_relaxed);
     }
-    return launch_attn(chunk_kernel<T, KIND, DP>, static_cast<unsigned>(p.plan.grid), ChunkWarps<KIND>::threads, M::bytes, p.no_singles != 0, p, s);
+    return launch_attn(chunk_kernel<T, KIND, DP>, static_cast<unsigned>(p.plan.grid), ChunkWarps<KIND>::threads, M::bytes, p.no_singles && KIND != kWide, p, s);
 }
 
 template <typename T, int KIND>

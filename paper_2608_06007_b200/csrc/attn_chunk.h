@@ -35,12 +35,23 @@ struct ChunkParams {
     FastDiv div_box;
     int32_t q_boxes;  // queries are fetched as boxes, too
     CUtensorMap map_k, map_v, map_q;
+    char *wide;         // codes' tiles made fp16 before, wide_list places a request, H tiles a place; NULL: each CTA widens its own
+    int32_t wide_list;
 };
 constexpr uint32_t kUncut = 0xffffffffu;
 
-// attn_chunk.cu, attn_chunk_codes.cu: the items, of unquantised pools and of codes
+// attn_chunk.cu, attn_chunk_codes.cu, attn_chunk_wide.cu: the items, of unquantised pools, of codes, and of codes that were made fp16 before
 int launch_chunk_plain(const ChunkParams &p, int dtype, int device, cudaStream_t s);
 int launch_chunk_codes(const ChunkParams &p, int device, cudaStream_t s);
+int launch_chunk_wide(const ChunkParams &p, int device, cudaStream_t s);
+
+// A tile that was made fp16: K and V as the products read them; K's scales and V's exponents of the keys; {mask, 4 words; V's exponent;
+// whether scales are far apart; whether V has numbers that are not finite}.
+template <int DP> struct WideTile {
+    static constexpr int keys = DP > 128 ? 64 : 128, tile = keys * DP * 2;
+    static constexpr int64_t scales_at = 2 * tile, header_at = scales_at + 8 * keys, bytes = header_at + 128;
+};
+inline int64_t wide_tile_bytes(int64_t D) { return D <= 64 ? WideTile<64>::bytes : D <= 128 ? WideTile<128>::bytes : WideTile<256>::bytes; }
 
 // Rows and tile that the kernels take for a head dim.
 inline int32_t chunk_rows(int64_t D) { return D > 128 ? 128 : 256; }

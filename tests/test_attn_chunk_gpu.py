@@ -54,3 +54,24 @@ def test_single_tokens_alone_and_beside_chunks(x, kind, window, sinks, new):
     run_chunk(s)
     check_chunk(s)
     status_is(0)
+
+
+@pytest.mark.parametrize("x,kind", [("bf16", "e4m3"), ("fp16", "int8"), ("bf16", "bf16")])
+@pytest.mark.parametrize("D,H,g", [(128, 2, 4), (64, 1, 8), (80, 2, 3), (256, 1, 4)])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (150, 70), (40, 0)])
+def test_many_blocks_of_rows(x, kind, D, H, g, window, sinks):
+    """Codes that three blocks of rows meet are made fp16 before."""
+    s = batch(kind, x, [700, 300, 1, 450, -1], [400, 300, 1, 129, 2], Hq=H * g, H=H, D=D, window=window, sinks=sinks)
+    run_chunk(s)
+    check_chunk(s)
+    status_is(0)
+
+
+@pytest.mark.parametrize("x,kind", TYPES)
+@pytest.mark.parametrize("B,layout", [(4, "hnd"), (12, "nhd"), (20, "hnd"), (24, "nhd"), (256, "nhd"), (3, "nhd"), (48, "hnd")])
+def test_blocks_of_all_sizes(x, kind, B, layout):
+    for D in (64, 128, 256):
+        s = batch(kind, x, [333, 270], [120, 64], Hq=4, H=2, D=D, B=B, layout=layout, window=100, sinks=9, gap=64)
+        run_chunk(s)
+        check_chunk(s)
+    status_is(0)

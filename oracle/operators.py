@@ -87,29 +87,31 @@ def attend(q, keys, vals, scale):
     return out, lse, mass
 
 
-def attend_chunk(q, keys, vals, scale, window=0, sinks=0):
+def attend_chunk(q, keys, vals, scale, window=0, sinks=0, there=None):
     """One request's new tokens, the last len(q) of its len(keys): q [n, Hq, D], keys and vals [len, H, D], all 64 bits; row i sees
-    keys j <= p = len - n + i, with a window j > p - window or j < sinks.  -> (out [n, Hq, D], lse [n, Hq], weights [n, Hq, len])."""
+    keys j <= p = len - n + i, with a window j > p - window or j < sinks; there [len]: keys that can be seen at all.
+    -> (out [n, Hq, D], lse [n, Hq], weights [n, Hq, len])."""
     n, Hq, D = q.shape
     total, H, _ = keys.shape
     j, p = np.arange(total), np.arange(total - n, total)[:, None]
     seen = (j <= p) & ((window == 0) | (j > p - window) | (j < sinks))
+    if there is not None:
+        seen &= there
     out, lse, weights = np.zeros((n, Hq, D)), np.full((n, Hq), -np.inf), np.zeros((n, Hq, total))
     for h in range(Hq):
         k, v = keys[:, h // (Hq // H)], vals[:, h // (Hq // H)]
         with np.errstate(invalid="ignore"):
             s = np.where(seen, q[:, h] @ k.T * scale, -np.inf)
-        m = s.max(1)
-        some = m > -np.inf
-        e = np.where(some[:, None], np.exp(s - np.where(some, m, 0)[:, None]), 0)
-        total_e = e.sum(1)
-        w = e / np.where(some, total_e, 1)[:, None]
-        # a key that is not seen has no part, whatever its value is
-        bad = ~np.isfinite(v).all(1)
-        out[:, h] = w @ np.where(bad[:, None], 0, v)
-        with np.errstate(invalid="ignore"):
+            m = s.max(1)
+            e = np.exp(s - np.where(m == -np.inf, 0, m)[:, None])  # NaN in rows with a score that is NaN or infinite
+            total_e = e.sum(1)
+            w = e / np.where(total_e == 0, 1, total_e)[:, None]
+            # a key that is not seen has no part, whatever its value is
+            bad = ~np.isfinite(v).all(1)
+            out[:, h] = w @ np.where(bad[:, None], 0, v)
             for x in np.flatnonzero(bad):
                 out[seen[:, x], h] += w[seen[:, x], x][:, None] * v[x]
-        lse[some, h] = m[some] + np.log(total_e[some])
+            some = total_e != 0
+            lse[some, h] = m[some] + np.log(total_e[some])
         weights[:, h] = w
     return out, lse, weights

@@ -57,7 +57,7 @@ def run_chunk(s, workspace=None, **changes):
     tc.tc_attn_chunk(pool.handle, s["dq"], s["out"], **(bounds | s["d"] | dict(scale=s["scale"], lse=s["lse"], workspace=workspace) | changes))
 
 
-def rows_off(s, r, row0, n, keys, vals, kernel_rounds):
+def rows_off(s, r, row0, n, keys, vals, kernel_rounds, there=None, far=False):
     """Outputs and logarithms of one request against 64 bits, within what each rounding may do.
 
     Half a step is 2^-9 of a bf16 number and 2^-12 of an fp16 one at most relative to it where steps are taken at the
@@ -65,22 +65,23 @@ def rows_off(s, r, row0, n, keys, vals, kernel_rounds):
     twice more where a tile is widened for the matrix products (kernel_rounds).  A score is an fp32 sum of D exact products and
     three fp32 factors, so (D + 4) 2^-24 of sum |q k| scale; it moves weights by twice that, relatively.  The exponential, the sum and
     the powers are good to 2^-18 together.  Half-precision products below 2^-14 of a row's largest contribution are off by 2^-25
-    each, and where codes' scales are taken in, by 2^-15 of a key's weight times its scale.  Then the output's own half step."""
+    each, and where codes' scales are taken in, by 2^-15 of a key's weight times its scale.  far: weights are 2 to the power of sums of
+    logarithms of up to some hundreds, in fp32, and off by 2^-14.  Then the output's own half step."""
     pool, x = s["pool"], s["x"]
     scale = s["scale"] or pool.D ** -0.5
     g = s["q"].shape[1] // pool.H
     q = np64(s["q"])[row0 : row0 + n]
-    want, want_lse, w = orc.attend_chunk(q, keys, vals, scale, s["window"], s["sinks"])
+    want, want_lse, w = orc.attend_chunk(q, keys, vals, scale, s["window"], s["sinks"], there)
     out, lse = np64(s["out"])[row0 : row0 + n], np64(s["lse"])[row0 : row0 + n]
     codes = pool.kind in TOP
     u_o = torch.finfo(TORCH[x]).eps / 2
     u_p = kernel_rounds * 2.0 ** -11 if codes else u_o
-    ok = np.isfinite(keys).all((1, 2)) & np.isfinite(vals).all((1, 2))
-    k, v = (np.repeat(np.where(ok[:, None, None], y, 0), g, axis=1) for y in (keys, vals))
+    k, v = (np.repeat(np.where(np.isfinite(y).all(-1)[..., None], y, 0), g, axis=1) for y in (keys, vals))
+    w = np.nan_to_num(w)
     mass = np.einsum("nhl,lhd->nhd", w, np.abs(v))
     length = np.einsum("nhd,lhd->nhl", np.abs(q), np.abs(k)) * abs(scale)
     delta = ((pool.D + 4) * 2.0 ** -24 * np.where(w > 0, length, 0).max(-1)) if len(keys) else np.zeros(q.shape[:2])
-    most = (u_p * (1 + 2.0 ** -6) + 2 * delta[..., None] + 2.0 ** -18) * mass + u_o * (1 + 2.0 ** -6) * np.abs(want) + (2.0 ** -25 if x == "fp16" else 1e-30)
+    most = (u_p * (1 + 2.0 ** -6) + 2 * delta[..., None] + 2.0 ** (-14 if far else -18)) * mass + u_o * (1 + 2.0 ** -6) * np.abs(want) + (2.0 ** -25 if x == "fp16" else 1e-30)
     if codes or x == "fp16":
         size = np.abs(v).max(-1) if len(v) else np.zeros((0, q.shape[1]))  # [len, Hq]
         seen = w > 0
@@ -88,17 +89,17 @@ def rows_off(s, r, row0, n, keys, vals, kernel_rounds):
         most += (seen.sum(-1) * 2.0 ** -24 * largest)[..., None]
         if codes:
             most += (2.0 ** -15 * (w * size.T).sum(-1))[..., None]
-    finite = np.isfinite(want)
+    most, finite = np.nan_to_num(most, nan=np.inf), np.isfinite(want)
     assert (np.isfinite(out) == finite).all(), (r, "finite")
     off = np.where(finite, np.abs(np.where(finite, out, 0) - np.where(finite, want, 0)), 0)
     assert (off <= np.where(finite, most, 0)).all(), (r, off.max(), (off / np.maximum(np.where(finite, most, 1), 1e-300)).max(), np.unravel_index((off - np.where(finite, most, 0)).argmax(), off.shape))
-    there = np.isfinite(want_lse)
+    good = np.isfinite(want_lse)
     assert (np.isnan(lse) == np.isnan(want_lse)).all() and (lse[np.isneginf(want_lse)] == -np.inf).all(), r
-    assert (np.abs(lse - np.where(there, want_lse, 0))[there] <= (delta + 2.0 ** -18 + 2.0 ** -22 * np.abs(np.where(there, want_lse, 0)))[there]).all(), r
+    assert (np.abs(lse - want_lse)[good] <= (delta + 2.0 ** -18 + 2.0 ** -22 * np.abs(want_lse))[good]).all(), r
 
 
-def check_chunk(s, only=None, left_out=()):
-    """Every request against the oracle, and every row that is nobody's as it was."""
+def check_chunk(s, only=None, left_out=(), there=None, far=False):
+    """Every request against the oracle, and every row that is nobody's as it was.  there: of a request, which of its keys can be read."""
     pool, offsets = s["pool"], s["offsets"]
     mine = np.zeros(len(s["q"]), dtype=bool)
     for r, (n, m) in enumerate(zip(s["lens"], s["new"])):
@@ -109,7 +110,7 @@ def check_chunk(s, only=None, left_out=()):
         if only is not None and r not in only:
             continue
         keys, vals = (tokens_of(v, s["table"][r], 0, n, pool.B) for v in s["values"])
-        rows_off(s, r, row0, m, keys, vals, 3)
+        rows_off(s, r, row0, m, keys, vals, 3, None if there is None else there.get(r), far)
     out, lse = np64(s["out"]), np64(s["lse"])
     assert (out[~mine] == 9.0).all() and (lse[~mine] == 9.0).all()
 
@@ -140,7 +141,7 @@ def run_window(s, workspace=None, **changes):
     tc.tc_attn_decode_window(pool.handle, s["dq"], s["out"], **args)
 
 
-def check_window(s, only=None):
+def check_window(s, only=None, there=None):
     pool = s["pool"]
     out, lse = np64(s["out"]), np64(s["lse"])
     for r, n in enumerate(s["lens"]):
@@ -150,4 +151,29 @@ def check_window(s, only=None):
             assert (out[r] == 0).all() and (lse[r] == -np.inf).all()
         elif only is None or r in only:
             keys, vals = (tokens_of(v, s["table"][r], 0, n, pool.B) for v in s["values"])
-            rows_off(s, r, r, 1, keys, vals, 1)
+            rows_off(s, r, r, 1, keys, vals, 1, None if there is None else there.get(r))
+
+
+def set_rows(s, plane, r, tokens, value):
+    """Tokens of request r in a plane: every element (of codes: every scale) becomes `value`, in the oracle's values too."""
+    pool, t = s["pool"], np.asarray(tokens)
+    block, at = s["table"][r][t // pool.B], t % pool.B
+    if pool.kind in TOP:
+        pool.scale(plane)[torch.from_numpy(block).long().cuda(), torch.from_numpy(at).cuda()] = value
+    else:
+        bits = torch.full((len(t), pool.H, pool.D), value, dtype=TORCH[pool.kind]).view(torch.uint8)
+        pool.codes(plane)[torch.from_numpy(block).long().cuda(), torch.from_numpy(at).cuda()] = bits.cuda()
+    s["values"][plane][block, at] = value if pool.kind not in TOP else np.nan
+
+
+def set_scales(s, plane, make):
+    """New scales of a pool of codes: make(t, shape) -> powers of two, of the tokens t of each request, for all heads."""
+    pool = s["pool"]
+    old = np64(pool.scale(plane)).copy()
+    new = old.copy()
+    for table, n in zip(s["table"], s["lens"]):
+        t = np.arange(max(0, n))
+        new[table[t // pool.B], t % pool.B] = make(t, (len(t), pool.H))
+    pool.scale(plane).copy_(torch.from_numpy(new.astype(np.float32)))
+    with np.errstate(invalid="ignore"):
+        s["values"][plane] = s["values"][plane] / old[..., None] * new.astype(np.float32).astype(np.float64)[..., None]

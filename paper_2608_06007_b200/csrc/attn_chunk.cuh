@@ -33,8 +33,8 @@ struct ChunkMemory {
     // K and V have their own warps, of which K's may be four tiles ahead.
     static constexpr int infos = 8;
     // {mask, 4 words; whether V has numbers that are not finite, up to 4 words}; codes: V's exponent, whether scales are far apart; each
-    // warp's largest and smallest of V's scales, for K's warps and for V's; scales of K; keys' exponents
-    static constexpr int info = KIND == kPlain ? 32 : 112 + 8 * keys, scales = 112;
+    // warp's largest and smallest of V's scales; scales of K; keys' exponents; scales of V over the power of two
+    static constexpr int info = KIND == kPlain ? 32 : 80 + 12 * keys, scales = 80;
     // powers of two taken out of the queries, of four items where scores run two ahead (one slot), of two elsewhere
     static constexpr int down_sets = 4 / slots, downs = KIND == kPlain ? 0 : 4 * 128 * 4;
     static constexpr int table = 2 * ChunkWarps<KIND>::threads * 4;  // items, and rows of parts, before each thread's requests
@@ -100,6 +100,28 @@ __device__ __forceinline__ void copy_run(uint32_t dst, const void *src, uint32_t
     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
 }
 
+// A scale of V as a power of two, of its own or its tile's, and the rest, which multiplies the probabilities.
+constexpr int kLeastExponent = -126;
+struct ScaleOfV {
+    float scale;
+    uint32_t size;  // bits of its magnitude; of a NaN 0, so that it is passed over
+    // 2 to this power is above the magnitude
+    __device__ __forceinline__ static int exponent_of(uint32_t size) { return static_cast<int>(size >> 23) - 126; }
+    // far: the key's own, else the tile's; a key of scale 0 takes no part in the maximum where each has its own
+    __device__ __forceinline__ float exponent(bool far, int tile) const { return scale == 0.f ? -4096.f : static_cast<float>(far ? exponent_of(size) : tile); }
+    __device__ __forceinline__ float rest(bool far, int tile) const
+    {
+        const int e = far ? exponent_of(size) : tile, half = e >> 1;  // 2^-e, from 2^-129 to 2^126, in two factors
+        return scale * __uint_as_float(static_cast<uint32_t>(127 - half) << 23) * __uint_as_float(static_cast<uint32_t>(127 - (e - half)) << 23);
+    }
+};
+
+__device__ __forceinline__ ScaleOfV scale_of_v(float scale)
+{
+    const uint32_t size = __float_as_uint(scale) & 0x7fffffffu;
+    return ScaleOfV{scale, size > 0x7f800000u ? 0u : size};
+}
+
 // Bits 0 .. n - 1.
 __device__ __forceinline__ uint32_t low_bits(int n) { return n <= 0 ? 0u : n >= 32 ? 0xffffffffu : (1u << n) - 1u; }
 
@@ -153,9 +175,9 @@ __device__ __noinline__ void spoiled_tile(uint32_t p_at, uint32_t o_at, uint32_t
 
 // Rare: scales of V so far apart that what is next to nothing among the probabilities can be much of the sum.  Each key has its
 // own power of two here, and the sum exponentials of its own; the scores stay in tensor memory and are gone through twice, 16 at a time:
-// for the row's maxima, then for the probabilities.  scales: of the tile's K; exponents: of its V.
+// for the row's maxima, then for the probabilities.  scales: of the tile's K, then exponents and the rest of V's.
 template <int KEYS>
-__device__ __noinline__ float2 far_maxima(uint32_t s_at, RowView view, uint32_t scales, uint32_t exponents, float factor)
+__device__ __noinline__ float2 far_maxima(uint32_t s_at, RowView view, uint32_t scales, float factor)
 {
     float highest = -INFINITY, most = -INFINITY;
 #pragma unroll 1
@@ -166,7 +188,7 @@ __device__ __noinline__ float2 far_maxima(uint32_t s_at, RowView view, uint32_t 
         tensor_loaded();
 #pragma unroll
         for (int i = 0; i < 16; i += 4) {
-            const float4 k4 = load_shared_f4(scales + 4 * (16 * c + i)), e4 = load_shared_f4(exponents + 4 * (16 * c + i));
+            const float4 k4 = load_shared_f4(scales + 4 * (16 * c + i)), e4 = load_shared_f4(scales + 4 * KEYS + 4 * (16 * c + i));
             const float k[4] = {k4.x, k4.y, k4.z, k4.w}, e[4] = {e4.x, e4.y, e4.z, e4.w};
 #pragma unroll
             for (int j = 0; j < 4; j++) {
@@ -179,7 +201,7 @@ __device__ __noinline__ float2 far_maxima(uint32_t s_at, RowView view, uint32_t 
 }
 // Probabilities relative to m, to p_at; the sum of exponentials relative to `ref`.
 template <int KEYS>
-__device__ __noinline__ float far_probabilities(uint32_t s_at, uint32_t p_at, RowView view, uint32_t scales, uint32_t exponents, float factor, float ref, float m)
+__device__ __noinline__ float far_probabilities(uint32_t s_at, uint32_t p_at, RowView view, uint32_t scales, float factor, float ref, float m)
 {
     float sum = 0.f;
 #pragma unroll 1
@@ -190,14 +212,15 @@ __device__ __noinline__ float far_probabilities(uint32_t s_at, uint32_t p_at, Ro
         tensor_loaded();
 #pragma unroll
         for (int i = 0; i < 16; i += 4) {
-            const float4 k4 = load_shared_f4(scales + 4 * (16 * c + i)), e4 = load_shared_f4(exponents + 4 * (16 * c + i));
-            const float k[4] = {k4.x, k4.y, k4.z, k4.w}, e[4] = {e4.x, e4.y, e4.z, e4.w};
+            const float4 k4 = load_shared_f4(scales + 4 * (16 * c + i)), e4 = load_shared_f4(scales + 4 * KEYS + 4 * (16 * c + i));
+            const float4 f4 = load_shared_f4(scales + 8 * KEYS + 4 * (16 * c + i));
+            const float k[4] = {k4.x, k4.y, k4.z, k4.w}, e[4] = {e4.x, e4.y, e4.z, e4.w}, f[4] = {f4.x, f4.y, f4.z, f4.w};
             float x[4];
 #pragma unroll
             for (int j = 0; j < 4; j++) {
                 x[j] = here >> (i + j) & 1 ? __uint_as_float(v[i + j]) * (factor * k[j]) : -INFINITY;
                 sum += exp2_approx(x[j] - ref);
-                x[j] = exp2_approx(x[j] + e[j] - m);
+                x[j] = exp2_approx(x[j] + e[j] - m) * f[j];
             }
             w[i / 2] = pack2<__half>(x[0], x[1]), w[i / 2 + 1] = pack2<__half>(x[2], x[3]);
         }
@@ -453,12 +476,12 @@ __global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(con
                 }
                 if (KIND != kPlain && far) {
                     const uint32_t scales = about + M::scales;
-                    const float2 maxima = far_maxima<kKeys>(s_at, view, scales, scales + 4 * kKeys, factor);
+                    const float2 maxima = far_maxima<kKeys>(s_at, view, scales, factor);
                     raise_ref(maxima.x);
                     move_top(maxima.y);
                     await_rest();
                     if (!fine) break;
-                    sum.x += far_probabilities<kKeys>(s_at, p_at, view, scales, scales + 4 * kKeys, factor, ref == -INFINITY ? 0.f : ref, top == -INFINITY ? 0.f : top - kLift);
+                    sum.x += far_probabilities<kKeys>(s_at, p_at, view, scales, factor, ref == -INFINITY ? 0.f : ref, top == -INFINITY ? 0.f : top - kLift);
                     tensor_stored();
                     fence_before();
                     barrier_arrive(s_taken + 8 * b);
@@ -509,11 +532,14 @@ __global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(con
                         float2 x[16];
                         scores(c, x);
                         uint32_t w[16];
+                        float4 f4;  // the rest of V's scales
 #pragma unroll
                         for (int j = 0; j < 16; j++) {
                             float2 e = sum2(x[j], minus);
                             e = make_float2(exp2_approx(e.x), exp2_approx(e.y));
                             here = sum2(here, e);
+                            if (j % 2 == 0) f4 = load_shared_f4(about + M::scales + 8 * kKeys + 128 * c + 8 * j);
+                            e = fused2(e, j % 2 ? make_float2(f4.z, f4.w) : make_float2(f4.x, f4.y), make_float2(0.f, 0.f));
                             w[j] = pack2<T>(e.x, e.y);
                         }
                         tensor_store16(p_at + 16 * c, w);  // in place: 16 columns of the 32 c that have been read
@@ -583,11 +609,16 @@ __global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(con
                     float2 here = make_float2(0.f, 0.f);
 #pragma unroll
                     for (int c = 0; c < kWords; c++) {
+                        float4 f4;  // the rest of V's scales
 #pragma unroll
                         for (int j = 0; j < 16; j++) {
                             float2 e = KIND == kPlain ? fused2(s.f2[c][j], f2, minus) : sum2(s.f2[c][j], minus);
                             e = make_float2(exp2_approx(e.x), exp2_approx(e.y));
                             here = sum2(here, e);
+                            if constexpr (KIND != kPlain) {
+                                if (j % 2 == 0) f4 = load_shared_f4(about + M::scales + 8 * kKeys + 128 * c + 8 * j);
+                                e = fused2(e, j % 2 ? make_float2(f4.z, f4.w) : make_float2(f4.x, f4.y), make_float2(0.f, 0.f));
+                            }
                             s.w[c][j] = pack2<T>(e.x, e.y);  // (in the place of scores that are done with)
                         }
                     }
@@ -904,7 +935,7 @@ __global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(con
                 };
                 auto header = [&](int i) { return kv == 0 && lane < 8 && i < item.end ? reinterpret_cast<const uint32_t *>(place(i) + WideTile<DP>::header_at)[lane] : 0u; };
                 uint32_t ahead = header(item.begin);
-                int e_most = -133;  // the largest exponent of a tile so far
+                int e_most = kLeastExponent;  // the largest of a tile so far
                 if (kv >= 2 && item.begin < item.end) prepare_queries(item);
                 for (int i = item.begin; i < item.end && fine && kv < 2; i++, tiles++) {
                     const uint32_t u = 2 * tiles + kv, stage = u % M::stages, bar = full + 8 * stage, about = info + (tiles % M::infos) * M::info;
@@ -926,9 +957,9 @@ __global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(con
                     }
                     __syncwarp();
                     if (lane == 0) {
-                        asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(M::tile + (kv ? 0 : 8 * kKeys)) : "memory");
+                        asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(M::tile + (kv ? 0 : 12 * kKeys)) : "memory");
                         copy_run(ring + stage * M::tile, from + kv * M::tile, M::tile, bar);
-                        if (kv == 0) copy_run(about + M::scales, from + WideTile<DP>::scales_at, 8 * kKeys, bar);
+                        if (kv == 0) copy_run(about + M::scales, from + WideTile<DP>::scales_at, 12 * kKeys, bar);
                     }
                     __syncwarp();
                     if (i == item.begin) prepare_queries(item);
@@ -936,18 +967,18 @@ __global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(con
                 if (item.begin >= item.end && warp == kLoad && lane == 0) barrier_arrive(wanted);
             }
         } else {
-            // Codes: four warps fetch and widen K, four V, each its own keys of every tile, through registers, a tile ahead.  V's are multiplied by their scales over a
-            // power of two that the tile's largest scale sets, 2^exponent, which puts the values below 2^16: rounded
-            // to fp16 twice (the factor and the product), half a step of 2^-11 each, like the probabilities
-            // that they meet.  Products below fp16's normal numbers are off by half of 2^-24, which is 2^-15 of the
-            // key's scale at most, since a tile whose scales span more than 2^16 is `far`: there each key
-            // has an exponent of its own.  So it is where a tile's largest scale is 2^-40 of one before.  K's scales are left to the
-            // scores, in fp32, for the sake of the logarithms.
+            // Codes: four warps fetch and widen K, four V, each its own keys of every tile, through registers, a tile ahead; both are fp16
+            // exactly.  K's scales multiply the scores, V's the probabilities, in fp32, before those are rounded to fp16 once: what is
+            // left of a scale over a power of two that the tile's largest sets, 2^exponent, which is in the maximum that probabilities
+            // are relative to.  They keep their precision down to 2^-14, so where scales span no more than 2^16 a key of a small one may have all
+            // the weight.  Where they span more the tile is `far`, and each key has an exponent of its own; so it is where a tile's largest
+            // scale is 2^-40 of one before.
             const int kv = warp >= kLoad + 4, w = warp & 3;
-            // all of K's or V's four warps, wherever a wait of one ran out
+            // all of K's four warps, wherever a wait of one ran out
             auto together = [&](bool yes) {
+                if (kv) return yes;
                 uint32_t all;
-                asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.cta.red.and.pred q, %2, 128, p;\n\tselp.u32 %0, 1, 0, q;\n\t}" : "=r"(all) : "r"(static_cast<uint32_t>(yes)), "r"(kv ? 2 : 1) : "memory");
+                asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.cta.red.and.pred q, 1, 128, p;\n\tselp.u32 %0, 1, 0, q;\n\t}" : "=r"(all) : "r"(static_cast<uint32_t>(yes)) : "memory");
                 return all != 0;
             };
             // what the table says of this lane's key of a tile; kNoKey: it is none.  Looked at a tile later
@@ -994,7 +1025,7 @@ __global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(con
                     codes[j] = make_uint4(0, 0, 0, 0);
                     if (src >= 0 && ch * 16 < D) codes[j] = *reinterpret_cast<const uint4 *>(plane + src + ch * 16);
                 };
-                int e_most = -133;  // the largest exponent of a tile so far
+                int e_most = kLeastExponent;  // the largest of a tile so far
                 fetch(item.begin);
                 // (loaded behind the queries, which need the registers)
                 if (next_off >= 0) asm volatile("prefetch.global.L2 [%0];" ::"l"(plane + next_off));
@@ -1005,7 +1036,7 @@ __global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(con
                     const uint32_t u = 2 * tiles + kv, stage = u % M::stages, about = info + (tiles % M::infos) * M::info;
                     near_end(item, i);
                     const float scale_k = next_k;
-                    float scale_v = next_v;
+                    const float scale_v = next_v;
                     const uint32_t mask = next_mask;
                     fetch(i + 1);
                     if (fine) fine = __all_sync(0xffffffffu, stage_free(u));
@@ -1016,35 +1047,33 @@ __global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(con
                         }
                         if (lane < kMine) asm volatile("st.shared.f32 [%0], %1;" ::"r"(about + M::scales + 4 * (w * kMine + lane)), "f"(scale_k) : "memory");
                     }
-                    // V's exponent: both groups find it, K's for the softmax, V's for the values
-                    const uint32_t bits = __float_as_uint(scale_v) & 0x7fffffffu, size = bits > 0x7f800000u ? 0 : bits;  // a NaN is passed over
-                    const uint32_t warp_most = __reduce_max_sync(0xffffffffu, size), warp_least = __reduce_min_sync(0xffffffffu, size ? size : 0x7f800000u);
-                    if (lane == 0) {
-                        asm volatile("st.shared.u32 [%0], %1;" ::"r"(about + 48 + 32 * kv + 4 * w), "r"(warp_most) : "memory");
-                        asm volatile("st.shared.u32 [%0], %1;" ::"r"(about + 64 + 32 * kv + 4 * w), "r"(warp_least) : "memory");
+                    if (!kv) {
+                        const ScaleOfV v = scale_of_v(scale_v);
+                        const uint32_t warp_most = __reduce_max_sync(0xffffffffu, v.size), warp_least = __reduce_min_sync(0xffffffffu, v.size ? v.size : 0x7f800000u);
+                        if (lane == 0) {
+                            asm volatile("st.shared.u32 [%0], %1;" ::"r"(about + 48 + 4 * w), "r"(warp_most) : "memory");
+                            asm volatile("st.shared.u32 [%0], %1;" ::"r"(about + 64 + 4 * w), "r"(warp_least) : "memory");
+                        }
+                        fine = together(fine);  // the four warps come here for every tile, and leave together where a wait ran out
+                        if (!fine) break;
+                        uint32_t all[4], low[4];
+                        asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(all[0]), "=r"(all[1]), "=r"(all[2]), "=r"(all[3]) : "r"(about + 48) : "memory");
+                        asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(low[0]), "=r"(low[1]), "=r"(low[2]), "=r"(low[3]) : "r"(about + 64) : "memory");
+                        const int e = ScaleOfV::exponent_of(max(max(all[0], all[1]), max(all[2], all[3])));
+                        const bool far = e < e_most - 40 || ScaleOfV::exponent_of(min(min(low[0], low[1]), min(low[2], low[3]))) < e - 16;
+                        e_most = max(e_most, e);
+                        if (w == 0 && lane == 0) asm volatile("st.shared.v2.b32 [%0], {%1,%2};" ::"r"(about + 32), "f"(static_cast<float>(e)), "r"(static_cast<uint32_t>(far)) : "memory");
+                        if (lane < kMine) {
+                            const uint32_t at = about + M::scales + 4 * (w * kMine + lane);
+                            asm volatile("st.shared.f32 [%0], %1;" ::"r"(at + 4 * kKeys), "f"(v.exponent(far, e)) : "memory");
+                            asm volatile("st.shared.f32 [%0], %1;" ::"r"(at + 8 * kKeys), "f"(v.rest(far, e)) : "memory");
+                        }
+                    } else if (!fine) {
+                        break;
                     }
-                    fine = together(fine);  // the four warps come here for every tile, and leave together where a wait ran out
-                    if (!fine) break;
-                    uint32_t all[4], low[4];
-                    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(all[0]), "=r"(all[1]), "=r"(all[2]), "=r"(all[3]) : "r"(about + 48 + 32 * kv) : "memory");
-                    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(low[0]), "=r"(low[1]), "=r"(low[2]), "=r"(low[3]) : "r"(about + 64 + 32 * kv) : "memory");
-                    int e = static_cast<int>(max(max(all[0], all[1]), max(all[2], all[3])) >> 23) - 127 - 6;  // a tile of zeros: the least
-                    const bool far = e < e_most - 40 || static_cast<int>(min(min(low[0], low[1]), min(low[2], low[3])) >> 23) - 127 - 6 < e - 16;
-                    e_most = max(e_most, e);
-                    if (!kv && w == 0 && lane == 0) asm volatile("st.shared.v2.b32 [%0], {%1,%2};" ::"r"(about + 32), "f"(static_cast<float>(e)), "r"(static_cast<uint32_t>(far)) : "memory");
-                    if (far) {
-                        // each key's own; one of zeros takes no part in the probabilities
-                        e = static_cast<int>(size >> 23) - 127 - 6;
-                        if (!kv && lane < kMine)
-                            asm volatile("st.shared.f32 [%0], %1;" ::"r"(about + M::scales + 4 * kKeys + 4 * (w * kMine + lane)), "f"(scale_v == 0.f ? -4096.f : static_cast<float>(e)) : "memory");
-                    }
-                    // 2^-e, up to 2^133, in two factors
-                    scale_v *= __uint_as_float(static_cast<uint32_t>(127 + min(-e, 127)) << 23);
-                    scale_v *= __uint_as_float(static_cast<uint32_t>(127 + max(-e - 127, 0)) << 23);
-                    const uint32_t to = ring + stage * M::tile, factor2 = kv ? pack2<__half>(scale_v, scale_v) : 0x3c003c00u;
+                    const uint32_t to = ring + stage * M::tile;
                     const bool look = kv && ragged(item, i);
-                    uint32_t bad = 0;
-                    // one way for K, times 1, and V: the code of both groups stays in the instruction cache
+                    uint32_t bad = look && !(fabsf(scale_v) < INFINITY);
 #pragma unroll
                     for (int j = 0; j < kUnits; j++) {
                         const int idx = j * 32 + lane, rr = idx / chunks, ch = idx % chunks;
@@ -1057,12 +1086,6 @@ __global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(con
                         widen<KIND>(odd ? c.x : c.z, x[4], x[5]);
                         widen<KIND>(odd ? c.y : c.w, x[6], x[7]);
                         load_unit(j);
-                        const uint32_t f = __shfl_sync(0xffffffffu, factor2, rr);
-#pragma unroll
-                        for (int k = 0; k < 8; k++) {
-                            const __half2 y = __hmul2(*reinterpret_cast<const __half2 *>(&x[k]), *reinterpret_cast<const __half2 *>(&f));
-                            x[k] = *reinterpret_cast<const uint32_t *>(&y);
-                        }
                         if (look) {
 #pragma unroll
                             for (int k = 0; k < 8; k++) bad |= not_finite<__half>(x[k]);

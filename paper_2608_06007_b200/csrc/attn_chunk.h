@@ -45,11 +45,11 @@ int launch_chunk_plain(const ChunkParams &p, int dtype, int device, cudaStream_t
 int launch_chunk_codes(const ChunkParams &p, int device, cudaStream_t s);
 int launch_chunk_wide(const ChunkParams &p, int device, cudaStream_t s);
 
-// A tile that was made fp16: K and V as the products read them; K's scales and V's exponents of the keys; {mask, 4 words; V's exponent;
+// A tile that was made fp16: K and V as the products read them; K's scales, V's exponents and the rest of V's scales of the keys; {mask, 4 words; V's exponent;
 // whether scales are far apart; whether V has numbers that are not finite}.
 template <int DP> struct WideTile {
     static constexpr int keys = DP > 128 ? 64 : 128, tile = keys * DP * 2;
-    static constexpr int64_t scales_at = 2 * tile, header_at = scales_at + 8 * keys, bytes = header_at + 128;
+    static constexpr int64_t scales_at = 2 * tile, header_at = scales_at + 12 * keys, bytes = header_at + 128;
 };
 inline int64_t wide_tile_bytes(int64_t D) { return D <= 64 ? WideTile<64>::bytes : D <= 128 ? WideTile<128>::bytes : WideTile<256>::bytes; }
 

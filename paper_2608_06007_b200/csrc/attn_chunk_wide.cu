@@ -47,19 +47,14 @@ __global__ void __launch_bounds__(256) chunk_widen_kernel(const __grid_constant_
     }
     const uint32_t mask = __ballot_sync(0xffffffffu, blk >= 0);
     // V's exponents, as where a CTA widens its own tiles
-    const uint32_t bits = __float_as_uint(scale_v) & 0x7fffffffu, size = bits > 0x7f800000u ? 0 : bits;  // a NaN is passed over
-    const uint32_t warp_most = __reduce_max_sync(0xffffffffu, size), warp_least = __reduce_min_sync(0xffffffffu, size ? size : 0x7f800000u);
+    const ScaleOfV v = scale_of_v(scale_v);
+    const uint32_t warp_most = __reduce_max_sync(0xffffffffu, v.size), warp_least = __reduce_min_sync(0xffffffffu, v.size ? v.size : 0x7f800000u);
     if (kv && lane == 0) most_of[w] = warp_most, least_of[w] = warp_least;
     __syncthreads();
-    int e = static_cast<int>(max(max(most_of[0], most_of[1]), max(most_of[2], most_of[3])) >> 23) - 127 - 6;  // a tile of zeros: the least
-    const int e_tile = e;
-    const bool far = static_cast<int>(min(min(least_of[0], least_of[1]), min(least_of[2], least_of[3])) >> 23) - 127 - 6 < e - 16;
-    if (far) e = static_cast<int>(size >> 23) - 127 - 6;
-    scale_v *= __uint_as_float(static_cast<uint32_t>(127 + min(-e, 127)) << 23);
-    scale_v *= __uint_as_float(static_cast<uint32_t>(127 + max(-e - 127, 0)) << 23);
+    const int e = ScaleOfV::exponent_of(max(max(most_of[0], most_of[1]), max(most_of[2], most_of[3])));
+    const bool far = ScaleOfV::exponent_of(min(min(least_of[0], least_of[1]), min(least_of[2], least_of[3]))) < e - 16;
     char *const to = p.wide + ((r * p.wide_list + listed) * H + h) * W::bytes;
-    const uint32_t factor2 = kv ? pack2<__half>(scale_v, scale_v) : 0x3c003c00u;
-    uint32_t bad = 0;
+    uint32_t bad = !(fabsf(scale_v) < INFINITY);
 #pragma unroll
     for (int j = 0; j < kUnits; j++) {
         const int idx = j * 32 + lane, rr = idx / chunks, ch = idx % chunks;
@@ -68,13 +63,8 @@ __global__ void __launch_bounds__(256) chunk_widen_kernel(const __grid_constant_
         widen<KIND>(codes[j].y, x[2], x[3]);
         widen<KIND>(codes[j].z, x[4], x[5]);
         widen<KIND>(codes[j].w, x[6], x[7]);
-        const uint32_t f = __shfl_sync(0xffffffffu, factor2, rr);
 #pragma unroll
-        for (int k = 0; k < 8; k++) {
-            const __half2 y = __hmul2(*reinterpret_cast<const __half2 *>(&x[k]), *reinterpret_cast<const __half2 *>(&f));
-            x[k] = *reinterpret_cast<const uint32_t *>(&y);
-            bad |= not_finite<__half>(x[k]);
-        }
+        for (int k = 0; k < 8; k++) bad |= not_finite<__half>(x[k]);
         char *const tile = to + kv * W::tile;
         *reinterpret_cast<uint4 *>(tile + swizzled<kKeys>(w * kMine + rr, 2 * ch)) = make_uint4(x[0], x[1], x[2], x[3]);
         *reinterpret_cast<uint4 *>(tile + swizzled<kKeys>(w * kMine + rr, 2 * ch + 1)) = make_uint4(x[4], x[5], x[6], x[7]);
@@ -86,7 +76,7 @@ __global__ void __launch_bounds__(256) chunk_widen_kernel(const __grid_constant_
         if (lane < kMine) {
             scales[w * kMine + lane] = scale_k;
             // (where a later part finds the tile far from those before it, all of its keys have the tile's exponent)
-            scales[kKeys + w * kMine + lane] = bits == 0 ? -4096.f : static_cast<float>(e);
+            scales[kKeys + w * kMine + lane] = v.exponent(far, e), scales[2 * kKeys + w * kMine + lane] = v.rest(far, e);
         }
         if (lane == 0) {
             if constexpr (kMine == 32) reinterpret_cast<uint32_t *>(to + W::header_at)[w] = mask;
@@ -96,7 +86,7 @@ __global__ void __launch_bounds__(256) chunk_widen_kernel(const __grid_constant_
     __syncthreads();
     if (threadIdx.x == 0) {
         uint32_t *const header = reinterpret_cast<uint32_t *>(to + W::header_at);
-        header[4] = static_cast<uint32_t>(e_tile), header[5] = far, header[6] = bad_of[0] | bad_of[1] | bad_of[2] | bad_of[3];
+        header[4] = static_cast<uint32_t>(e), header[5] = far, header[6] = bad_of[0] | bad_of[1] | bad_of[2] | bad_of[3];
     }
 }
 

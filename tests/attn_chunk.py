@@ -61,8 +61,8 @@ def rows_off(s, r, row0, n, keys, vals, kernel_rounds, there=None, far=False):
     """Outputs and logarithms of one request against 64 bits, within what each rounding may do.
 
     Half a step is 2^-9 of a bf16 number and 2^-12 of an fp16 one at most relative to it where steps are taken at the
-    power of two below it, eps / 2 = 2^-8 and 2^-11 for the worst of them: a probability is rounded once, values of codes
-    twice more where a tile is widened for the matrix products (kernel_rounds).  A score is an fp32 sum of D exact products and
+    power of two below it, eps / 2 = 2^-8 and 2^-11 for the worst of them: a probability is rounded once, or as often as
+    kernel_rounds says.  A score is an fp32 sum of D exact products and
     three fp32 factors, so (D + 4) 2^-24 of sum |q k| scale; it moves weights by twice that, relatively.  The exponential, the sum and
     the powers are good to 2^-18 together.  Half-precision products below 2^-14 of a row's largest contribution are off by 2^-25
     each, and where codes' scales are taken in, by 2^-15 of a key's weight times its scale.  far: weights are 2 to the power of sums of
@@ -110,7 +110,7 @@ def check_chunk(s, only=None, left_out=(), there=None, far=False):
         if only is not None and r not in only:
             continue
         keys, vals = (tokens_of(v, s["table"][r], 0, n, pool.B) for v in s["values"])
-        rows_off(s, r, row0, m, keys, vals, 3, None if there is None else there.get(r), far)
+        rows_off(s, r, row0, m, keys, vals, 1, None if there is None else there.get(r), far)
     out, lse = np64(s["out"]), np64(s["lse"])
     assert (out[~mine] == 9.0).all() and (lse[~mine] == 9.0).all()
 

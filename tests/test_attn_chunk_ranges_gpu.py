@@ -255,7 +255,7 @@ def test_a_prompt_written_and_answered_piece_by_piece(kind):
             x = orc.values(stored.numpy().view(np.uint8 if kind == "e4m3" else np.int8), scale.numpy(), kind) if scale is not None else np64(stored.view(torch.bfloat16))
             values.append(x)
         s = dict(pool=pool, x="bf16", q=q, out=out, lse=lse, scale=0.0, window=window, sinks=sinks)
-        rows_off(s, 0, 0, total, values[0], values[1], 3)
+        rows_off(s, 0, 0, total, values[0], values[1], 1)
     status_is(0)
 
 

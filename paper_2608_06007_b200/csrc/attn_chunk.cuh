@@ -604,6 +604,8 @@ __global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(con
                         if constexpr (KIND != kPlain) raise_ref(highest);
                         move_top(most);
                     }
+                    // asked before the exponentials, answered behind them: as a rule the product before is done by now
+                    const bool asked = steps == 0 || barrier_passed(o_added + 8 * slot, (steps - 1) & 1);
                     const float m = top == -INFINITY ? 0.f : top - kLift;
                     const float2 minus = make_float2(exponent - m, exponent - m), f2 = make_float2(factor, factor);
                     float2 here = make_float2(0.f, 0.f);
@@ -629,7 +631,8 @@ __global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(con
                         const float all = here.x + here.y;
                         sum.x = fmaf(all, all == 0.f ? 0.f : exp2_approx(m - exponent - (ref == -INFINITY ? 0.f : ref)), sum.x);
                     }
-                    await_rest();  // by now it has been given, as a rule
+                    if (!__all_sync(0xffffffffu, asked)) await_rest();
+                    fence_after();
                     if (!fine) break;
 #pragma unroll
                     for (int c = 0; c < kWords; c++) tensor_store16(p_at + 16 * c, reinterpret_cast<const uint32_t(&)[16]>(s.w[c]));

@@ -81,21 +81,6 @@ __global__ void __launch_bounds__(128) chunk_join_kernel(const __grid_constant__
     }
 }
 
-template <typename T>
-static int launch_chunk(const ChunkParams &p, const AttnParams *singles, int dtype, int device, cudaStream_t s)
-{
-    int rc = TC_OK;
-    if (singles) {
-        if ((rc = launch_singles_stream(*singles, dtype, device, s)) != TC_OK) return rc;
-        if (p.max_new == 1) return launch_singles_join(*singles, dtype, s);
-    }
-    rc = p.wide ? launch_chunk_wide(p, device, s) : p.layer.quantised() ? launch_chunk_codes(p, device, s) : launch_chunk_plain(p, dtype, device, s);
-    if (rc == TC_OK && singles) rc = launch_singles_join(*singles, dtype, s);
-    if (rc != TC_OK || !p.plan.part_rows) return rc;
-    const unsigned grid = static_cast<unsigned>(std::min<int64_t>((p.n_tokens * p.Hq + 3) / 4, kChunkSms * 8));
-    return p.layer.D <= 128 ? launch_attn(chunk_join_kernel<T, 128>, grid, 128, 0, true, p, s) : launch_attn(chunk_join_kernel<T, 256>, grid, 128, 0, true, p, s);
-}
-
 // Tensor maps, where a call's geometry fits them: queries as [token][head][d], whose boxes are the whole tokens that an item's slot of 128
 // rows holds; pages of an unquantised pool as [block][head][token][d], in boxes of as many tokens as divide a block and half a tile.
 // Elsewhere q_boxes or box_rows stays 0.
@@ -151,10 +136,19 @@ constexpr int64_t kLeastSingles = 8;
 // 8 prompts of up to 15061 tokens in a window of 2048, int8, of 8 heads x 128: KWIDE ms so, with 493 MB of them, 3.12 where each block widens its own.
 constexpr int64_t kMostWide = 1ll << 30;
 
-// What both entry points check; fills p's geometry and plan, and those of the requests with one new token where these have their own
-// kernels.  *workspace: bytes of all, the second's from *singles_at on, tiles made fp16 from *wide_at.
-static int check_chunk(const tc_kv_layer_t *layer, const tc_attn_chunk_t *a, ChunkParams *p, AttnParams *singles, int64_t *singles_at, int64_t *wide_at, int64_t *workspace)
+// What a call launches, in one workspace.
+struct ChunkCall {
+    ChunkParams most;     // requests that meet the pages as they lie
+    ChunkParams wide;     // those whose codes are made fp16 before
+    AttnParams singles;   // those with one new token
+    bool has_wide, has_singles;
+    int64_t singles_at, wide_at, workspace;
+};
+
+// What both entry points check; fills the kernels' geometry and plans.
+static int check_chunk(const tc_kv_layer_t *layer, const tc_attn_chunk_t *a, ChunkCall *c)
 {
+    ChunkParams *const p = &c->most;
     int rc = check_layer(layer, &p->layer);
     if (rc != TC_OK) return rc;
     if (!a) return fail(TC_ERR_INVALID_ARG, "args is required");
@@ -179,32 +173,68 @@ static int check_chunk(const tc_kv_layer_t *layer, const tc_attn_chunk_t *a, Chu
     const int64_t new_most = std::min(a->max_new, a->n_tokens);
     if (new_most * s.group > INT32_MAX - 4096 || a->R * chunk_blocks(s, static_cast<int32_t>(new_most)) > INT32_MAX / s.heads)
         return fail(TC_ERR_TOO_LARGE, "R = %lld requests of up to %lld tokens x %lld heads: too many for one call", (long long)a->R, (long long)new_most, (long long)a->Hq);
-    p->max_new = a->max_new;
-    if (a->max_new > 1) plan_chunk(s, a->R, a->n_tokens, a->max_new, a->max_len, D, &p->plan);
-    *singles_at = *workspace = p->plan.workspace;
+    p->R = a->R, p->n_tokens = a->n_tokens, p->max_new = a->max_new, p->max_len = a->max_len;
     const int64_t most = a->window ? std::min(a->max_len, std::min(a->window, a->max_len) + std::min(a->sinks, a->max_len) + 96) : a->max_len;
     // (what the stream's 32-bit counts of rows and tiles do not hold goes without it)
     bool fits = a->R * a->Hq <= (1 << 30) && a->R * p->layer.H <= (1 << 30) / std::max<int64_t>(1, (most + 15) / 16);
     if (fits && (a->max_new == 1 || a->R >= kLeastSingles)) {
-        singles->layer = p->layer;
-        split_attn(a->R, a->Hq, p->layer.H, D, most, 0, p->layer.quantised(), &singles->split);
-        fits = singles->split.stream_tiles < (1ll << 31);
-        p->no_singles = fits;
-        if (fits) *workspace += singles->split.workspace;
+        c->singles.layer = p->layer;
+        split_attn(a->R, a->Hq, p->layer.H, D, most, 0, p->layer.quantised(), &c->singles.split);
+        c->has_singles = fits = c->singles.split.stream_tiles < (1ll << 31);
     }
-    // Codes that three blocks of rows meet, or more, are made fp16 once, in the workspace, where that takes no more than kMostWide.
-    p->wide_list = 0;
-    *wide_at = *workspace;
+    p->new_from = c->has_singles ? 2 : 1, p->new_to = a->max_new;
+    // Codes that three blocks of a request's rows meet, or more, are made fp16 once, where the requests that may have as many fit into
+    // kMostWide; else those of the requests with the most new tokens.
     if (p->layer.quantised() && a->max_new > 1 && new_most * s.group > 2 * s.rows) {
         const int64_t near = (std::min<int64_t>(s.window, a->max_len) + new_most) / s.keys + 2 + chunk_tiles_of(s, static_cast<int32_t>(std::min<int64_t>(s.sinks, a->max_len)));
-        const int64_t list = std::min<int64_t>(near, chunk_tiles_of(s, static_cast<int32_t>(a->max_len))), bytes = wide_tile_bytes(D);
-        if (list <= kMostWide / bytes && a->R * s.heads <= kMostWide / bytes / list) {
-            p->wide_list = static_cast<int32_t>(list);
-            *workspace += a->R * s.heads * list * bytes;
+        const int64_t list = std::min<int64_t>(near, chunk_tiles_of(s, static_cast<int32_t>(a->max_len))), bytes = list * s.heads * wide_tile_bytes(D), room = kMostWide / bytes;
+        int64_t from = std::max<int64_t>(2 * s.rows / s.group + 1, p->new_from);
+        if (std::min(a->R, a->n_tokens / from) > room) from = a->n_tokens / (room + 1) + 1;
+        if (room > 0 && from <= new_most) {
+            ChunkParams *const w = &c->wide;
+            c->has_wide = true;
+            *w = *p;
+            w->new_from = from, p->new_to = from - 1;
+            w->wide_by_request = a->R <= a->n_tokens / from;
+            w->wide_requests = std::min(a->R, a->n_tokens / from);
+            w->wide_list = static_cast<int32_t>(list);
+            w->div_wide = make_fastdiv(static_cast<uint32_t>(from));
+            plan_chunk(s, w->wide_requests, a->n_tokens, a->max_new, a->max_len, D, &w->plan);
         }
     }
+    // `cuts`, then the sums and outputs of the parts' rows of all kernels
+    ChunkPlan &plan = p->plan;
+    if (a->max_new > 1 && p->new_from <= p->new_to) plan_chunk(s, a->R, a->n_tokens, p->new_to, a->max_len, D, &plan);
+    auto place = [&](int64_t bytes) {
+        const int64_t at = c->workspace;
+        c->workspace += (bytes + 255) / 256 * 256;
+        return at;
+    };
+    const int64_t part_rows = plan.part_rows + c->wide.plan.part_rows;  // (max_len decides whether anything may be cut: of both or of neither)
+    if (part_rows) plan.cuts_at = place(a->R * 8), plan.sums_at = place(part_rows * 4), plan.parts_at = place(part_rows * D * 4);
+    c->singles_at = place(c->has_singles ? c->singles.split.workspace : 0);
+    c->wide_at = place(c->has_wide ? c->wide.wide_requests * c->wide.wide_list * s.heads * wide_tile_bytes(D) : 0);
     if (a->max_new == 1 && !fits) return fail(TC_ERR_TOO_LARGE, "R * H * keys = %lld * %d * %lld: too many for one call", (long long)a->R, p->layer.H, (long long)most);
     return TC_OK;
+}
+
+template <typename T>
+static int launch_chunk(const ChunkCall &c, int dtype, int device, cudaStream_t s)
+{
+    const ChunkParams &p = c.most;
+    int rc = TC_OK;
+    if (c.has_singles) {
+        if ((rc = launch_singles_stream(c.singles, dtype, device, s)) != TC_OK) return rc;
+        if (p.max_new == 1) return launch_singles_join(c.singles, dtype, s);
+    }
+    if (p.new_from <= p.new_to) rc = p.layer.quantised() ? launch_chunk_codes(p, device, s) : launch_chunk_plain(p, dtype, device, s);
+    if (rc == TC_OK && c.has_wide) rc = launch_chunk_wide(c.wide, device, s);
+    if (rc == TC_OK && c.has_singles) rc = launch_singles_join(c.singles, dtype, s);
+    ChunkParams all = p;
+    if (c.has_wide) all.new_to = c.wide.new_to, all.plan.part_rows += c.wide.plan.part_rows;
+    if (rc != TC_OK || !all.plan.part_rows) return rc;
+    const unsigned grid = static_cast<unsigned>(std::min<int64_t>((p.n_tokens * p.Hq + 3) / 4, kChunkSms * 8));
+    return p.layer.D <= 128 ? launch_attn(chunk_join_kernel<T, 128>, grid, 128, 0, true, all, s) : launch_attn(chunk_join_kernel<T, 256>, grid, 128, 0, true, all, s);
 }
 
 }  // namespace tc
@@ -216,22 +246,20 @@ extern "C" int tc_attn_chunk_workspace(const tc_kv_layer_t *layer, const tc_attn
     clear_error();
     if (!bytes) return fail(TC_ERR_INVALID_ARG, "bytes is NULL");
     *bytes = 0;
-    ChunkParams p{};
-    AttnParams singles{};
-    int64_t at, wide_at, need;
-    const int rc = check_chunk(layer, a, &p, &singles, &at, &wide_at, &need);
-    if (rc == TC_OK) *bytes = need;
+    ChunkCall c{};
+    const int rc = check_chunk(layer, a, &c);
+    if (rc == TC_OK) *bytes = c.workspace;
     return rc;
 }
 
 extern "C" int tc_attn_chunk(const tc_kv_layer_t *layer, const tc_attn_chunk_t *a, void *stream)
 {
     clear_error();
-    ChunkParams p{};
-    AttnParams singles{};
-    int64_t singles_at, wide_at, need;
-    int rc = check_chunk(layer, a, &p, &singles, &singles_at, &wide_at, &need);
+    ChunkCall c{};
+    int rc = check_chunk(layer, a, &c);
     if (rc != TC_OK) return rc;
+    ChunkParams &p = c.most;
+    const int64_t need = c.workspace;
     if (a->R == 0 || a->n_tokens == 0 || a->max_new == 0) return TC_OK;
     uint32_t align = 16;
     const int64_t row = p.layer.D * 2ll;
@@ -249,7 +277,7 @@ extern "C" int tc_attn_chunk(const tc_kv_layer_t *layer, const tc_attn_chunk_t *
     if (need && (!a->workspace || reinterpret_cast<uintptr_t>(a->workspace) % 16)) return fail(TC_ERR_INVALID_ARG, "workspace is required, 16-byte aligned");
     if (a->workspace_bytes < need)
         return fail(TC_ERR_BOUNDS, "workspace_bytes %lld < %lld (tc_attn_chunk_workspace)", (long long)a->workspace_bytes, (long long)need);
-    if (p.plan.grid > INT32_MAX) return fail(TC_ERR_TOO_LARGE, "%lld items: too many for one call", (long long)p.plan.grid);
+    if (const int64_t items = std::max(p.plan.grid, c.wide.plan.grid); items > INT32_MAX) return fail(TC_ERR_TOO_LARGE, "%lld items: too many for one call", (long long)items);
     int device, sms;
     if ((rc = op_device(&device, &p.status, &sms)) != TC_OK) return rc;
     const struct {
@@ -267,7 +295,6 @@ extern "C" int tc_attn_chunk(const tc_kv_layer_t *layer, const tc_attn_chunk_t *
     p.tables = reinterpret_cast<const char *>(a->tables);
     p.table_stride = a->table_stride;
     p.offsets = a->offsets, p.lens = a->lens;
-    p.R = a->R, p.n_tokens = a->n_tokens, p.max_new = a->max_new, p.max_len = a->max_len;
     p.Hq = static_cast<int32_t>(a->Hq);
     p.q_bf16 = a->dtype == TC_BF16;
     p.scale_log2 = static_cast<float>((a->scale != 0.f ? static_cast<double>(a->scale) : 1.0 / std::sqrt(static_cast<double>(p.layer.D))) * 1.4426950408889634);
@@ -279,9 +306,20 @@ extern "C" int tc_attn_chunk(const tc_kv_layer_t *layer, const tc_attn_chunk_t *
     p.sums = reinterpret_cast<float *>(ws + p.plan.sums_at);
     p.parts = reinterpret_cast<float *>(ws + p.plan.parts_at);
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    p.wide = p.wide_list ? ws + wide_at : nullptr;
-    if (p.no_singles) {
-        AttnParams &q = singles;
+    p.beside = c.has_singles;
+    if (c.has_wide) {
+        const ChunkParams w = c.wide;
+        c.wide = p;
+        c.wide.new_from = w.new_from, c.wide.new_to = w.new_to, c.wide.plan = w.plan;
+        c.wide.wide_by_request = w.wide_by_request, c.wide.wide_requests = w.wide_requests, c.wide.wide_list = w.wide_list, c.wide.div_wide = w.div_wide;
+        c.wide.wide = ws + c.wide_at;
+        c.wide.first_part_row = static_cast<uint32_t>(p.plan.part_rows);
+        c.wide.sums += p.plan.part_rows, c.wide.parts += p.plan.part_rows * p.layer.D;
+        c.wide.beside = false;  // its tiles have to be there
+        c.wide.widen_beside = c.has_singles || p.new_from <= p.new_to;
+    }
+    if (c.has_singles) {
+        AttnParams &q = c.singles;
         q.q = p.q, q.q_req = p.q_token, q.q_head = p.q_head;
         q.out = p.out, q.out_req = p.out_token, q.out_head = p.out_head;
         q.lse = p.lse;
@@ -292,11 +330,10 @@ extern "C" int tc_attn_chunk(const tc_kv_layer_t *layer, const tc_attn_chunk_t *
         q.Hq = p.Hq, q.q_bf16 = p.q_bf16, q.scale_log2 = p.scale_log2;
         q.div_block = p.div_block, q.div_group = p.div_group, q.div_heads = make_fastdiv(static_cast<uint32_t>(p.Hq));
         q.status = p.status;
-        char *const at = ws + singles_at;
+        char *const at = ws + c.singles_at;
         q.sums = reinterpret_cast<float *>(at + q.split.sums_at), q.parts = reinterpret_cast<float *>(at + q.split.parts_at);
         q.piece_sums = reinterpret_cast<float *>(at + q.split.piece_sums_at), q.pieces = reinterpret_cast<float *>(at + q.split.pieces_at);
         q.before = reinterpret_cast<uint32_t *>(at + q.split.before_at);
     }
-    const AttnParams *const apart = p.no_singles ? &singles : nullptr;
-    return a->dtype == TC_BF16 ? launch_chunk<__nv_bfloat16>(p, apart, a->dtype, device, s) : launch_chunk<__half>(p, apart, a->dtype, device, s);
+    return a->dtype == TC_BF16 ? launch_chunk<__nv_bfloat16>(c, a->dtype, device, s) : launch_chunk<__half>(c, a->dtype, device, s);
 }

@@ -48,7 +48,7 @@ struct ChunkMemory {
 
 // One item as it lies in shared memory.
 struct alignas(16) ChunkItem {
-    int32_t valid, r, h, row0;
+    int32_t valid, r, h, row0;       // r: of tiles that were made fp16, their place
     int32_t rows, pos0, begin, end;  // the part: tiles [begin, end) of the list
     ChunkList list;                  // 7 words
     uint32_t part_row;               // of the request's row 0 of this part; kUncut: outputs are written
@@ -69,9 +69,12 @@ __device__ __forceinline__ ChunkRequest chunk_request(const ChunkParams &p, int6
     const int64_t n = to - q.token0;
     const bool bad = q.token0 < 0 || to < q.token0 || to > p.n_tokens || n > p.max_new || (q.len >= 0 && (q.len > p.max_len || q.len < n));
     if (tell && bad) atomicOr(p.status, kStatusBadIndex);
-    q.n = bad || q.len < 0 || (p.no_singles && n == 1) ? 0 : static_cast<int32_t>(n);
+    q.n = bad || q.len < 0 || n < p.new_from || n > p.new_to ? 0 : static_cast<int32_t>(n);
     return q;
 }
+
+// Which of the places for tiles made fp16 are request r's.
+__device__ __forceinline__ int64_t wide_place(const ChunkParams &p, int64_t r, int64_t token0) { return p.wide_by_request ? r : quick_div(static_cast<uint32_t>(token0), p.div_wide); }
 
 // Any of two 16-bit numbers infinite or NaN.
 template <typename T> __device__ __forceinline__ uint32_t not_finite(uint32_t w)
@@ -569,13 +572,12 @@ __global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(con
                         for (int c = 0; c < kWords; c++) mask[c] = view.word(c);
                     }
                     if constexpr (KIND != kPlain) {
-                        const float2 f2 = make_float2(factor, factor), zero = make_float2(0.f, 0.f);
+                        const float2 zero = make_float2(0.f, 0.f);
 #pragma unroll
                         for (int j = 0; j < kKeys / 4; j++) {
                             const float4 k = load_shared_f4(about + M::scales + 16 * j);
                             float2 *x = &s.f2[j / 8][j % 8 * 2];
-                            x[0] = fused2(x[0], fused2(f2, make_float2(k.x, k.y), zero), zero);
-                            x[1] = fused2(x[1], fused2(f2, make_float2(k.z, k.w), zero), zero);
+                            x[0] = fused2(x[0], make_float2(k.x, k.y), zero), x[1] = fused2(x[1], make_float2(k.z, k.w), zero);
                         }
                     }
 #pragma unroll
@@ -596,7 +598,7 @@ __global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(con
 #pragma unroll
                         for (int j = 2; j < 32; j += 2) m4[c] = larger3(m4[c], s.f[c][j], s.f[c][j + 1]);
                     }
-                    const float highest = fmaxf(larger3(m4[0], m4[1], m4[2]), m4[3]), most = KIND == kPlain ? highest * factor : highest + exponent;
+                    const float highest = fmaxf(larger3(m4[0], m4[1], m4[2]), m4[3]) * factor, most = highest + exponent;
                     bool move = most > top + 8.f;
                     if constexpr (KIND != kPlain) move = move || highest > ref + 8.f;
                     // a running maximum moves only when a score exceeds it by more than 8 (2^8 in probabilities)
@@ -614,7 +616,7 @@ __global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(con
                         float4 f4;  // the rest of V's scales
 #pragma unroll
                         for (int j = 0; j < 16; j++) {
-                            float2 e = KIND == kPlain ? fused2(s.f2[c][j], f2, minus) : sum2(s.f2[c][j], minus);
+                            float2 e = fused2(s.f2[c][j], f2, minus);
                             e = make_float2(exp2_approx(e.x), exp2_approx(e.y));
                             here = sum2(here, e);
                             if constexpr (KIND != kPlain) {
@@ -1248,10 +1250,11 @@ __global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(con
                         item.firsts = item.skip = 0;
                         if constexpr (KIND == kWide) {
                             const ChunkList whole = chunk_list(shape, item.pos0, 0, q.n * shape.group, q.n * shape.group);
+                            item.r = static_cast<int32_t>(wide_place(p, r, q.token0));
                             item.firsts = whole.firsts, item.skip = whole.skip;
                         }
                         // for chunk_join_kernel, by whoever has the request's first item
-                        if (p.plan.part_rows && id == at && lane == 0) p.cuts[r] = make_uint2(rows_at, static_cast<uint32_t>(parts));
+                        if (p.plan.part_rows && id == at && lane == 0) p.cuts[r] = make_uint2(p.first_part_row + rows_at, static_cast<uint32_t>(parts));
                         break;
                     }
                     if (item.valid) {
@@ -1315,7 +1318,7 @@ __global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(con
             barrier_wait(last, 0);
         }
     }
-    if (p.no_singles) await_last();  // who waits for this kernel waits for those before it, too
+    if (p.beside) await_last();  // who waits for this kernel waits for those before it, too
     if (!fine) atomicOr(p.status, static_cast<unsigned int>(TC_DEVICE_BULK_WAIT_TIMEOUT));
     fence_before();
     __syncthreads();
@@ -1338,7 +1341,7 @@ int launch_chunk_shape(const ChunkParams &p, int device, cudaStream_t s)
         if (attr.numRegs != ChunkWarps<KIND>::launch_registers) return fail(TC_ERR_CUDA, "tc_attn_chunk's kernel was built with %d registers a thread, not %d", attr.numRegs, ChunkWarps<KIND>::launch_registers);
         raised[device].store(true, std::memory_order_relaxed);
     }
-    return launch_attn(chunk_kernel<T, KIND, DP>, static_cast<unsigned>(p.plan.grid), ChunkWarps<KIND>::threads, M::bytes, p.no_singles && KIND != kWide, p, s);
+    return launch_attn(chunk_kernel<T, KIND, DP>, static_cast<unsigned>(p.plan.grid), ChunkWarps<KIND>::threads, M::bytes, p.beside, p, s);
 }
 
 template <typename T, int KIND>

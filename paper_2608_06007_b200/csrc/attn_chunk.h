@@ -22,21 +22,28 @@ struct ChunkParams {
     const int32_t *lens;
     int64_t R, n_tokens, max_new, max_len;
     int32_t Hq, q_bf16;
-    int32_t no_singles;  // requests with one new token have their own kernels, launched before this one
+    int64_t new_from, new_to;  // requests with so many new tokens are this kernel's; others have their own, in the same call
+    bool beside;               // launched behind a kernel of the same call that it need not wait for, but for its own end
     float scale_log2;    // scale * log2(e)
     FastDiv div_block, div_group;
     ChunkShape shape;
     ChunkPlan plan;
     uint2 *cuts;  // of every request that has items: the first of its parts' rows, and the number of its parts
     float *sums, *parts;
+    uint32_t first_part_row;  // of this kernel's among the call's, which `cuts` counts
     unsigned int *status;
     // Where blocks and tiles fit into one another, pages are fetched as boxes of box_rows tokens of one head; 0: key by key.
     int32_t box_rows;
     FastDiv div_box;
     int32_t q_boxes;  // queries are fetched as boxes, too
     CUtensorMap map_k, map_v, map_q;
-    char *wide;         // codes' tiles made fp16 before, wide_list places a request, H tiles a place; NULL: each CTA widens its own
-    int32_t wide_list;
+    // Codes' tiles that are made fp16 before: wide_list places a request, H tiles a place.  A request's places are the r-th, or where
+    // there may be more requests than room the (token0 / new_from)-th: no two of new_from tokens or more have the same.
+    char *wide;
+    int32_t wide_list, wide_by_request;
+    int64_t wide_requests;  // that there is room for
+    FastDiv div_wide;
+    bool widen_beside;  // the kernel that makes them is launched as `beside` says
 };
 constexpr uint32_t kUncut = 0xffffffffu;
 

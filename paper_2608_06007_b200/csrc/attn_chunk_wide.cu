@@ -8,15 +8,27 @@
 namespace tc {
 
 // A CTA has a tile of one request and KV head: four warps K, four V, each a quarter of the keys.
-template <int KIND, int DP>
-__global__ void __launch_bounds__(256) chunk_widen_kernel(const __grid_constant__ ChunkParams p)
+template <int KIND, int DP> __device__ __forceinline__ void widen_tile(const ChunkParams &p)
 {
     using W = WideTile<DP>;
     constexpr int kKeys = W::keys, kMine = kKeys / 4, chunks = DP / 16, kUnits = kMine * chunks / 32;
     __shared__ uint32_t most_of[4], least_of[4], bad_of[4];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, kv = warp >> 2, w = warp & 3, H = p.layer.H, D = p.layer.D;
     const int h = blockIdx.x % H, listed = static_cast<int>(blockIdx.x / H % p.wide_list);
-    const int64_t r = blockIdx.x / H / p.wide_list;
+    int64_t r = blockIdx.x / H / p.wide_list;
+    if (!p.wide_by_request) {
+        // the request whose place this is
+        __shared__ int found;
+        if (threadIdx.x == 0) found = -1;
+        __syncthreads();
+        for (int64_t i = threadIdx.x; i < p.R; i += 256) {
+            const ChunkRequest q = chunk_request(p, i, false);
+            if (q.n && wide_place(p, i, q.token0) == r) found = static_cast<int>(i);
+        }
+        __syncthreads();
+        if (found < 0) return;
+        r = found;
+    }
     const ChunkRequest q = chunk_request(p, r, false);
     if (!q.n) return;
     const ChunkList list = chunk_list(p.shape, q.len - q.n, 0, q.n * p.shape.group, q.n * p.shape.group);
@@ -53,7 +65,7 @@ __global__ void __launch_bounds__(256) chunk_widen_kernel(const __grid_constant_
     __syncthreads();
     const int e = ScaleOfV::exponent_of(max(max(most_of[0], most_of[1]), max(most_of[2], most_of[3])));
     const bool far = ScaleOfV::exponent_of(min(min(least_of[0], least_of[1]), min(least_of[2], least_of[3]))) < e - 16;
-    char *const to = p.wide + ((r * p.wide_list + listed) * H + h) * W::bytes;
+    char *const to = p.wide + ((wide_place(p, r, q.token0) * p.wide_list + listed) * H + h) * W::bytes;
     uint32_t bad = !(fabsf(scale_v) < INFINITY);
 #pragma unroll
     for (int j = 0; j < kUnits; j++) {
@@ -90,11 +102,18 @@ __global__ void __launch_bounds__(256) chunk_widen_kernel(const __grid_constant_
     }
 }
 
+template <int KIND, int DP>
+__global__ void __launch_bounds__(256) chunk_widen_kernel(const __grid_constant__ ChunkParams p)
+{
+    widen_tile<KIND, DP>(p);
+    if (p.widen_beside && blockIdx.x == 0) await_last();  // this kernel has not ended before those before it have
+}
+
 template <int DP>
 static int launch_wide_shape(const ChunkParams &p, int device, cudaStream_t s)
 {
-    const unsigned grid = static_cast<unsigned>(p.R * p.wide_list * p.layer.H);
-    const int rc = p.layer.dtype == TC_E4M3 ? launch_attn(chunk_widen_kernel<kE4m3, DP>, grid, 256, 0, false, p, s) : launch_attn(chunk_widen_kernel<kInt8, DP>, grid, 256, 0, false, p, s);
+    const unsigned grid = static_cast<unsigned>(p.wide_requests * p.wide_list * p.layer.H);
+    const int rc = p.layer.dtype == TC_E4M3 ? launch_attn(chunk_widen_kernel<kE4m3, DP>, grid, 256, 0, p.widen_beside, p, s) : launch_attn(chunk_widen_kernel<kInt8, DP>, grid, 256, 0, p.widen_beside, p, s);
     return rc != TC_OK ? rc : launch_chunk_shape<__half, kWide, DP>(p, device, s);
 }
 

@@ -67,6 +67,25 @@ def test_many_blocks_of_rows(x, kind, D, H, g, window, sinks):
     status_is(0)
 
 
+@pytest.mark.parametrize("x,kind", [("bf16", "e4m3"), ("fp16", "int8")])
+@pytest.mark.parametrize("D,g", [(128, 4), (64, 8), (256, 4)])
+@pytest.mark.parametrize("window,sinks,extra_len", [(0, 0, 0), (0, 0, 100000), (0, 0, 4000000), (150, 70, 100000)])
+def test_requests_of_few_and_of_many_blocks_in_one_call(x, kind, D, g, window, sinks, extra_len):
+    """More requests than have many blocks; bounds so wide that only the longest have room, or none."""
+    new = [1, 300, 2, 140, 135, 1, 129, 128, 0, 65, 66, 33, 1, 400, 64, 500]
+    lens = [n + extra if n else 50 for n, extra in zip(new, [500, 2000, 70, 5, 3000, 40, 1000, 128, 0, 300, 0, 700, 900, 100, 64, 250])]
+    lens[6] = -1
+    s = batch(kind, x, lens, new, Hq=2 * g, D=D, window=window, sinks=sinks, front=3, behind=5, extra_len=extra_len, seed=D)
+    need = tc.tc_attn_chunk_workspace_bytes(s["pool"].handle, s["dq"], len(lens), max_new=s["max_new"], max_len=s["max_len"], window=window, sinks=sinks)
+    workspace = torch.full((need,), 0xFF, dtype=torch.uint8, device="cuda")
+    run_chunk(s, workspace)
+    check_chunk(s)
+    first = s["out"].clone()
+    run_chunk(s, workspace)  # finds what the first call left there
+    assert torch.equal(s["out"], first)
+    status_is(0)
+
+
 @pytest.mark.parametrize("x,kind", TYPES)
 @pytest.mark.parametrize("B,layout", [(4, "hnd"), (12, "nhd"), (20, "hnd"), (24, "nhd"), (256, "nhd"), (3, "nhd"), (48, "hnd")])
 def test_blocks_of_all_sizes(x, kind, B, layout):

@@ -315,6 +315,7 @@ __global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(con
                 for (int c = 0; c < 2; c++) {
                     sum[c].items = __reduce_add_sync(0xffffffffu, sum[c].items), sum[c].split = __reduce_add_sync(0xffffffffu, sum[c].split);
                     sum[c].tiles = __reduce_add_sync(0xffffffffu, sum[c].tiles), sum[c].longest = __reduce_max_sync(0xffffffffu, sum[c].longest);
+                    sum[c].large = __reduce_add_sync(0xffffffffu, sum[c].large), sum[c].rest = __reduce_add_sync(0xffffffffu, sum[c].rest);
                 }
                 const float cost0 = chunk_cost(sum[0]), cost1 = chunk_cost(sum[1]);
                 if (lane == 0) best_cost[warp] = min(cost0, cost1), best_share[warp] = cost1 < cost0 ? shares[1] : shares[0];

@@ -590,11 +590,13 @@ TC_API int tc_attn_decode_window(const tc_kv_layer_t *layer, const tc_attn_decod
  * lens[r] < 0: the request is padding.  A request with n = 0 is passed over.  Their rows, and rows in front of offsets[0] and
  * behind offsets[R], are left as they were; so are those of a request with n > max_new, lens[r] > max_len, lens[r] < n or
  * offsets that decrease or leave [0, n_tokens], which sets TC_DEVICE_BAD_INDEX.
- * Slots of the cache that no row of a request sees are never read.  Scores, softmax statistics and outputs are fp32; probabilities, quantised pools
- * and their scales are dealt with as by tc_attn_decode.  Which parts a request's keys are cut into depends on the lengths of
+ * Entries of a table are looked up for tokens that some row of the request sees; a block id that is out of range sets
+ * TC_DEVICE_BAD_INDEX, and its tokens are left out.  Of a block with such tokens other slots may be read; they have no part in what is written.
+ * Scores, softmax statistics and sums are fp32; codes of a quantised pool are taken exactly, their scales in fp32, and a
+ * probability is rounded once, to 16 bits.  Which parts a request's keys are cut into depends on the lengths of
  * the whole batch, and with it the order of sums; the same call on the same batch gives the same bits.
- * A call is one or two launches.  D is a multiple of 16 up to 256, every address and stride a multiple of 16 bytes (tables,
- * lens, lse and the scales: of 4, offsets: of 8).  An unquantised pool has the queries' type. */
+ * A call is one to six launches, by its arguments alone: it can be captured.  D is a multiple of 16 up to 256, every address and
+ * stride a multiple of 16 bytes (tables, lens, lse and the scales: of 4, offsets: of 8).  An unquantised pool has the queries' type. */
 typedef struct {
     uint32_t struct_size; /* sizeof(tc_attn_chunk_t) */
     int32_t dtype;        /* TC_BF16 or TC_FP16: of q and out */
@@ -615,7 +617,9 @@ typedef struct {
     int64_t workspace_bytes;  /*   may run at once; its contents before and after mean nothing */
 } tc_attn_chunk_t;
 
-/* Bytes of workspace that the call needs: by R, n_tokens, Hq, max_new, max_len, window, sinks and the layer's geometry alone. */
+/* Bytes of workspace that the call needs: by R, n_tokens, Hq, max_new, max_len, window, sinks and the layer's type and geometry alone.
+ * It does not grow with each of them.  Of a quantised pool it has room for up to 2^30 bytes of codes made fp16, where max_new is more
+ * than two blocks of 256 rows (128 above D = 128); bounds as close as the program knows them keep it small. */
 TC_API int tc_attn_chunk_workspace(const tc_kv_layer_t *layer, const tc_attn_chunk_t *args, int64_t *bytes);
 TC_API int tc_attn_chunk(const tc_kv_layer_t *layer, const tc_attn_chunk_t *args, void *stream);
 

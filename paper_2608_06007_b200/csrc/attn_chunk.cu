@@ -84,7 +84,7 @@ __global__ void __launch_bounds__(128) chunk_join_kernel(const __grid_constant__
 // Tensor maps, where a call's geometry fits them: queries as [token][head][d], whose boxes are the whole tokens that an item's slot of 128
 // rows holds; pages of an unquantised pool as [block][head][token][d], in boxes of as many tokens as divide a block and half a tile.
 // Elsewhere q_boxes or box_rows stays 0.
-constexpr int32_t kLeastBox = 4;  // tokens: 16 prompts in blocks of 20 take KBOX us so, 544 key by key
+constexpr int32_t kLeastBox = 4;  // tokens: 16 prompts in blocks of 20 take 404 us so, 544 key by key
 static int describe_boxes(ChunkParams *p)
 {
     p->box_rows = p->q_boxes = 0;
@@ -130,10 +130,11 @@ static int describe_boxes(ChunkParams *p)
 }
 
 // Requests with one new token go to the stream where there may be some number of them: it reads codes at some 4 TB/s and 16-bit numbers
-// at 6, a CTA that holds 256 rows for them at 0.5 and .. (64 requests, 51 of them single, 200k tokens of 8 heads x 128, e4m3: a call of KSINGLES us
-// so, 570 without).  Fewer are not worth its two launches.
+// at 6, where items of 256 rows, of which these have a few, take a tile as slowly as if they were full (64 requests, 51 of them single, 200k tokens
+// of 8 heads x 128, e4m3: a call of 386 us so, 570 without, before requests of many blocks had kernels of their own).  Fewer are not worth its two launches.
 constexpr int64_t kLeastSingles = 8;
-// 8 prompts of up to 15061 tokens in a window of 2048, int8, of 8 heads x 128: KWIDE ms so, with 493 MB of them, 3.12 where each block widens its own.
+// Bytes of tiles made fp16 at most.  8 prompts of up to 15061 tokens in a window of 2048, int8, of 8 heads x 128: 2.07 ms so, with 493 MB of them, 3.12 where
+// each block widens its own; 64 requests, four of them of 104 to 374 new tokens behind up to 10883, e4m3: 286 us, of which these tiles take 32, and 387.
 constexpr int64_t kMostWide = 1ll << 30;
 
 // What a call launches, in one workspace.

@@ -1,4 +1,33 @@
 // tc_attn_chunk: attention of chunks of new tokens over a paged cache, on the fifth-generation tensor cores.
+//
+// Mathematics.  The rows of a request and KV head are its (new token, query head of the group) pairs, token by token, 256 at a time (head
+// dims above 128: 128), so that a tile of K and V meets all heads that share it.  Over the tiles of keys that some row sees, one
+// pass: S = Q K' to tensor memory; a thread has a row, t = max(t, S scale), P = 2^(S scale - t) to tensor memory, l += sum P; O += P V there.
+// All exponents are of 2, the scale has log2(e) in it.  t moves only when a score exceeds it by more than 8: till then P is at most 2^8, and O
+// is not touched; what O and l hold is rescaled when it does, and the last t and l give the outputs and their logarithm.  S, t, l and O are
+// fp32; P is rounded once to the products' 16 bits, fp16 with 2^7 taken in (probability_lift), so that what is below 2^-21 of the
+// row's largest is what its smallest steps lose.
+// Codes are fp16 exactly.  K's scale multiplies the scores.  V's multiplies the probabilities in fp32, before their one rounding,
+// as a power of two that the whole tile has, which goes into the exponent, and a rest below 1; where scales within a tile are more than 2^16 apart,
+// or a tile's largest is 2^40 below one before, each key has a power of its own (far_maxima, far_probabilities).  Queries that
+// meet codes are fp16 with a power of two per row taken out.
+//
+// What a row does not see must not reach it, not even as 0 x NaN: of a tile in which rows differ, the warps that fetch V look whether
+// it has numbers that are not finite, and the rows' sums over such a tile are made one number at a time (spoiled_tile).  Keys
+// that no row sees are 0 in shared memory, or cut off by the tile's mask.
+//
+// Warps.  Eight of softmax, a thread a row; four that fetch (codes: eight that also widen); one each issues S and O products; one finds
+// the items.  Two slots of 128 rows go through a tile, so that one's products run beside the other's exponentials.  Items are
+// independent CTAs of a grid as large as the largest batch that the bounds allow; a CTA that nears the end of one takes over
+// another that has not been launched (try_cancel) and goes on without a gap, since the lengths are known on the device alone.
+//
+// What bounds it.  Two slots' products take 2048 clocks a tile of 128 keys at D = 128, and as many the exponentials, at 16 a clock
+// and SM; a slot's softmax is a chain of some 3000 (load 250, maximum 450, exponentials 1600, the rest and stores 600), of which two run side by
+// side.  Measured: 2048 tokens behind 6144 of 32 heads over 8 KV heads, bf16: 214 us, 1.12 PFLOP/s, 0.67 of a library's large product;
+// 8192 behind 24576, 64 heads: 6.7 ms, 1.14 PFLOP/s.  Two threads a row (16 warps of softmax) were slower, 290 us: half the registers, and both
+// halves of a row wait for one another.  K and V have their own warps: with one for both, V's wait for a free stage held K's next back.
+// Codes that each CTA widens itself: 33 tokens behind 120000 of 28 heads over 4, int8: 151 us, 5 us a tile of the eight widening
+// warps, which bound it; requests of many blocks go another way (attn_chunk_wide.cu).
 #pragma once
 
 #include <algorithm>
@@ -11,7 +40,7 @@ namespace tc {
 
 constexpr float kChunkLn2 = 0.6931471805599453f;
 
-// Codes that attn_chunk_widen.cu has made fp16, tile by tile, before: their scales still come with the scores.
+// Codes that attn_chunk_wide.cu has made fp16, tile by tile, before: their scales still come with the scores.
 constexpr int kWide = 3;
 template <int KIND> constexpr bool kWidens = KIND == kE4m3 || KIND == kInt8;
 

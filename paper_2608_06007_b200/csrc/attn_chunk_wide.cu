@@ -2,7 +2,9 @@
 //
 // A block of 256 rows widens what it meets, which costs its CTA more than the products and the softmax do.  Where a request has many
 // blocks, they would widen the same tiles again and again; here one CTA a tile does it for all: bytes to read once, twice as many to write
-// once, and then to read from L2 as often as blocks meet them.
+// once, and then to read from L2 as often as blocks meet them.  Bound by HBM: 3800 tiles of 128 keys x 128 of int8, 125 MB and
+// 250 MB written: 83 us, 4.5 TB/s.  The items behind it take some 5000 clocks a tile, where 16-bit pools take 3600: each thread loads
+// 128 scales of K and as many of V from shared memory a tile, 2000 clocks of its bandwidth for eight warps.
 #include "attn_chunk.cuh"
 
 namespace tc {

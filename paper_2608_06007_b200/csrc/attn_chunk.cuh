@@ -314,7 +314,7 @@ __global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(con
         const ChunkRequest q = chunk_request(p, r, tell);
         return q.n ? Extent{q.n, chunk_blocks(shape, q.n) * H, chunk_tiles(shape, q.len)} : Extent{0, 0, 0};
     };
-    const Extent first = run0 < run1 ? extent_of(run0, blockIdx.x == 0) : Extent{0, 0, 0};
+    const Extent first = run0 < run1 ? extent_of(run0, true) : Extent{0, 0, 0};
     int32_t share = 1 << 30;
     if (p.plan.part_rows) {
         int32_t n_items = first.blocks, most = first.tiles;
@@ -361,7 +361,7 @@ __global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(con
     {
         uint32_t my_items = 0, my_rows = 0;
         for (int64_t r = run0; r < run1; r++) {
-            const Extent e = r == run0 ? first : extent_of(r, blockIdx.x == 0);
+            const Extent e = r == run0 ? first : extent_of(r, true);
             const int32_t parts = e.tiles > share ? chunk_parts(e.tiles, share) : 1;
             my_items += e.blocks * parts;
             if (parts > 1) my_rows += static_cast<uint32_t>(e.n) * p.Hq * parts;

@@ -26,8 +26,10 @@
 // side.  Measured: 2048 tokens behind 6144 of 32 heads over 8 KV heads, bf16: 214 us, 1.12 PFLOP/s, 0.67 of a library's large product;
 // 8192 behind 24576, 64 heads: 6.7 ms, 1.14 PFLOP/s.  Two threads a row (16 warps of softmax) were slower, 290 us: half the registers, and both
 // halves of a row wait for one another.  K and V have their own warps: with one for both, V's wait for a free stage held K's next back.
-// Codes that each CTA widens itself: 33 tokens behind 120000 of 28 heads over 4, int8: 151 us, 5 us a tile of the eight widening
-// warps, which bound it; requests of many blocks go another way (attn_chunk_wide.cu).
+// Codes that each CTA widens itself: 33 tokens behind 120000 of 28 heads over 4, int8: 151 us.  A slot's chain bounds it, 6100 clocks a
+// tile: its scores wait for the product before, whose probabilities lie in their place (1800), two passes (1500, 2400), the product; the eight
+// widening warps take 3500.  One pass with the old maximum, probabilities in registers till it is known, was slower, 168 us: its code is long
+// and six warps of four kinds share a scheduler's instruction cache.  Requests of many blocks go another way (attn_chunk_wide.cu).
 #pragma once
 
 #include <algorithm>

@@ -170,6 +170,7 @@ static int check_chunk(const tc_kv_layer_t *layer, const tc_attn_chunk_t *a, Chu
     if (!(std::fabs(a->scale) <= 1e30f)) return fail(TC_ERR_INVALID_ARG, "scale is not a number of at most 1e30");
     p->shape = chunk_shape(static_cast<int32_t>(a->Hq / p->layer.H), chunk_rows(D), chunk_keys(D), static_cast<int32_t>(a->window ? std::min<int64_t>(a->window, 1 << 30) : 1 << 30),
                            static_cast<int32_t>(std::min<int64_t>(a->sinks, 1 << 30)), p->layer.H);
+    p->shape.turns = p->layer.quantised() && p->shape.rows == 256;
     const ChunkShape &s = p->shape;
     const int64_t new_most = std::min(a->max_new, a->n_tokens);
     if (new_most * s.group > INT32_MAX - 4096 || a->R * chunk_blocks(s, static_cast<int32_t>(new_most)) > INT32_MAX / s.heads)

@@ -79,7 +79,7 @@ struct ChunkMemory {
 
 // One item as it lies in shared memory.
 struct alignas(16) ChunkItem {
-    int32_t valid, r, h, row0;       // r: of tiles that were made fp16, their place
+    int32_t valid, r, h, row0;       // valid: 0 = the end, 2 = the slots take turns at the tiles; r: of tiles that were made fp16, their place
     int32_t rows, pos0, begin, end;  // the part: tiles [begin, end) of the list
     ChunkList list;                  // 7 words
     uint32_t part_row;               // of the request's row 0 of this part; kUncut: outputs are written
@@ -303,6 +303,11 @@ __global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(con
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
 
+    // Both slots have an item's rows and take turns at its tiles; parts that an item so leaves.
+    constexpr bool kTurns = kWidens<KIND> && kSlots == 2;
+    auto turns = [](const ChunkItem &item) { return kTurns && item.valid == 2; };
+    auto each_leaves = [&](int32_t n, int32_t parts) { return kTurns && chunk_turns(shape, n, parts) ? 2 : 1; };
+
     // ------------------------------------------------------------------- the cut, the same in every CTA
     // Each thread has a run of requests, of which it keeps the first.
     __shared__ int32_t sum_items[W::all], sum_tiles[W::all], best_share[16];
@@ -366,7 +371,7 @@ __global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(con
             const Extent e = r == run0 ? first : extent_of(r, true);
             const int32_t parts = e.tiles > share ? chunk_parts(e.tiles, share) : 1;
             my_items += e.blocks * parts;
-            if (parts > 1) my_rows += static_cast<uint32_t>(e.n) * p.Hq * parts;
+            if (parts > 1) my_rows += static_cast<uint32_t>(e.n) * p.Hq * parts * each_leaves(e.n, parts);
         }
         uint32_t upto = my_items, rows_upto = my_rows;
 #pragma unroll
@@ -417,8 +422,9 @@ __global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(con
     };
     auto tile_of = [](const ChunkItem &item, int i) { return i < item.list.firsts ? i : i + item.list.skip; };
     // Does slot `slot` need tile i of the list?
-    auto needs = [](const ChunkItem &item, int slot, int i) {
+    auto needs = [&](const ChunkItem &item, int slot, int i) {
         if (kSlots == 1) return true;
+        if (turns(item)) return ((i - item.begin) & 1) == slot;
         return slot == 0 ? i < item.list.end0 : item.rows > 128 && (i < item.list.firsts || i >= item.list.begin1);
     };
     // Is there a key in tile i that some row sees and another does not?
@@ -438,14 +444,14 @@ __global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(con
             if (!take_item(it, item)) break;
             const bool some = item.begin < item.end;
             const int count = item.end - item.begin;
-            if (slot == 1 && item.rows <= 128) {
+            if (slot == 1 && item.rows <= 128 && !turns(item)) {
                 tiles += max(count, 0), loads += some;
                 continue;
             }
-            const int row = item.row0 + min(slot * 128 + r, item.rows - 1);
+            const int first_row = turns(item) ? 0 : slot * 128, row = item.row0 + min(first_row + r, item.rows - 1);
             const int token = static_cast<int>(quick_div(static_cast<uint32_t>(row), p.div_group)), pos = item.pos0 + token;
             float factor = fabsf(p.scale_log2);  // of this thread's row of scores
-            const uint32_t down_at = base + kDownsAt + 4 * ((loads % M::down_sets) * kSlots * 128 + slot * 128 + r);
+            const uint32_t down_at = base + kDownsAt + 4 * ((loads % M::down_sets) * kSlots * 128 + first_row + r);
             loads += some;
             float top = -INFINITY;
             float ref = -INFINITY;  // codes: the running maximum of the scores, which the sum is relative to; `top` has the tiles' powers in it
@@ -688,9 +694,9 @@ __global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(con
             if (!fine) break;
             // The rows' outputs, or the part: outputs by the sum, and its logarithm.
             const float all = sum.x + sum.y, lowest = KIND == kPlain ? top - kLift : ref;
-            const bool store = slot * 128 + r < item.rows, cut = item.part_row != kUncut;
+            const bool store = first_row + r < item.rows, cut = item.part_row != kUncut;
             const int head = item.h * shape.group + (row - token * shape.group);
-            const int64_t at = static_cast<int64_t>(item.part_row) + static_cast<int64_t>(token) * p.Hq + head;
+            const int64_t at = static_cast<int64_t>(item.part_row) + (turns(item) ? slot * item.rows * H : 0) + static_cast<int64_t>(token) * p.Hq + head;
             const float log = all == 0.f ? -INFINITY : (lowest == -INFINITY ? 0.f : lowest) + log2f(all);
             char *const out = p.out + (item.token0 + token) * p.out_token + head * p.out_head;
             if (mine) {
@@ -1180,7 +1186,7 @@ __global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(con
                         fine = __all_sync(0xffffffffu, fine);
                         if (!fine) break;
                         fence_after();
-                        const uint64_t q_operand = operand(base + slot * M::q_tile, 16), k_operand = operand(ring + stage * M::tile, 16);
+                        const uint64_t q_operand = operand(base + (turns(item) ? 0 : slot * M::q_tile), 16), k_operand = operand(ring + stage * M::tile, 16);
                         if (elected()) {
 #pragma unroll
                             for (int k = 0; k < DP / 16; k++)
@@ -1263,21 +1269,22 @@ __global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(con
                         const uint32_t here = static_cast<uint32_t>(blocks) * parts * H;
                         if (id >= at + here) {
                             at += here;
-                            if (parts > 1) rows_at += static_cast<uint32_t>(q.n) * p.Hq * parts;
+                            if (parts > 1) rows_at += static_cast<uint32_t>(q.n) * p.Hq * parts * each_leaves(q.n, parts);
                             continue;
                         }
                         // heads first, so that CTAs side by side read pages side by side; the last block, which sees most, first
                         uint32_t rest = id - at;
                         item.h = rest % H, rest /= H;
                         const int32_t part = rest % parts, block = blocks - 1 - static_cast<int32_t>(rest / parts);
-                        item.valid = 1, item.r = static_cast<int32_t>(r);
+                        const int32_t each = each_leaves(q.n, parts);  // parts that an item leaves
+                        item.valid = each, item.r = static_cast<int32_t>(r);
                         item.row0 = block * shape.rows;
                         item.rows = min(static_cast<int32_t>(min(static_cast<int64_t>(q.n) * shape.group - item.row0, static_cast<int64_t>(shape.rows))), shape.rows);
                         item.pos0 = q.len - q.n;
                         item.list = chunk_list(shape, item.pos0, item.row0, item.rows, 128);
                         item.begin = static_cast<int32_t>(min(static_cast<int64_t>(part) * share, static_cast<int64_t>(item.list.count)));
                         item.end = static_cast<int32_t>(min(static_cast<int64_t>(item.begin) + share, static_cast<int64_t>(item.list.count)));
-                        item.part_row = parts > 1 ? rows_at + static_cast<uint32_t>(part) * q.n * p.Hq : kUncut;
+                        item.part_row = parts > 1 ? rows_at + static_cast<uint32_t>(part * each) * q.n * p.Hq : kUncut;
                         item.token0 = q.token0;
                         item.firsts = item.skip = 0;
                         if constexpr (KIND == kWide) {
@@ -1286,7 +1293,7 @@ __global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(con
                             item.firsts = whole.firsts, item.skip = whole.skip;
                         }
                         // for chunk_join_kernel, by whoever has the request's first item
-                        if (p.plan.part_rows && id == at && lane == 0) p.cuts[r] = make_uint2(p.first_part_row + rows_at, static_cast<uint32_t>(parts));
+                        if (p.plan.part_rows && id == at && lane == 0) p.cuts[r] = make_uint2(p.first_part_row + rows_at, static_cast<uint32_t>(parts * each));
                         break;
                     }
                     if (item.valid) {

@@ -26,6 +26,7 @@ struct ChunkShape {
     int32_t heads;   // KV heads
     int32_t rows_shift, keys_shift, near_tiles;  // near_tiles: that a block's windows can touch
     uint32_t group_mul, group_shift;             // to divide by `group`
+    int32_t turns;                               // slots may take turns (chunk_turns)
 };
 
 TC_HD int32_t chunk_low(int32_t a, int32_t b) { return a < b ? a : b; }
@@ -38,7 +39,7 @@ TC_HD int32_t chunk_by_group(const ChunkShape &s, int32_t n)
 
 inline ChunkShape chunk_shape(int32_t group, int32_t rows, int32_t keys, int32_t window, int32_t sinks, int32_t heads)
 {
-    ChunkShape s{group, rows, keys, window, sinks, heads, 0, 0, 0, 0, 0};
+    ChunkShape s{group, rows, keys, window, sinks, heads, 0, 0, 0, 0, 0, 0};
     while (1 << s.rows_shift < rows) s.rows_shift++;
     while (1 << s.keys_shift < keys) s.keys_shift++;
     s.near_tiles = (window + (rows - 1) / group + 1 + keys - 2) / keys + 1;
@@ -81,6 +82,10 @@ TC_HD ChunkList chunk_list(const ChunkShape &s, int32_t pos0, int32_t row0, int3
 }
 
 TC_HD int32_t chunk_parts(int32_t tiles, int32_t share) { return (tiles + share - 1) / share; }
+// A request of up to 128 rows leaves one of two slots idle.  Where its keys are cut, both have its rows, and take turns at a part's tiles: each
+// leaves a part of its own.  Codes that a CTA widens gain by it (8 tokens behind 120000, 56 rows a KV head, int8: 118 -> 100 us); 16-bit pools
+// lose more by twice the parts (70 -> 78 us).
+TC_HD bool chunk_turns(const ChunkShape &s, int32_t n, int32_t parts) { return s.turns && n * s.group <= 128 && parts > 1 && 2 * parts <= kChunkMostParts; }
 // The cuts that are looked at: into parts of so many tiles that the longest list has up to 1 .. 16, then up to 23, 30 .. 128.
 constexpr int kChunkCuts = 32;
 TC_HD int32_t chunk_share(int32_t most_tiles, int32_t cut)
@@ -136,7 +141,7 @@ inline void plan_chunk(const ChunkShape &s, int64_t R, int64_t n_tokens, int64_t
     p->grid = items;
     if (tiles <= kChunkLeastShare || items == 0) return;
     p->grid += kChunkSplitItems;
-    const int64_t item_rows = new_most * s.group < s.rows ? new_most * s.group : s.rows, rows = R * new_most * s.group * s.heads;
+    const int64_t each = s.turns ? 2 : 1, item_rows = each * new_most * s.group < s.rows ? each * new_most * s.group : s.rows, rows = each * R * new_most * s.group * s.heads;
     const int64_t parts = chunk_parts(static_cast<int32_t>(tiles), kChunkLeastShare);
     const int64_t by_items = kChunkSplitItems * item_rows, by_rows = rows * (parts < kChunkMostParts ? parts : kChunkMostParts);
     p->part_rows = by_items < by_rows ? by_items : by_rows;

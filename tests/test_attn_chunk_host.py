@@ -24,7 +24,8 @@ static int pick(int lo, int hi) { seed = seed * 1664525u + 1013904223u; return l
 int main() {
     for (int round = 0; round < 3000; round++) {
         const int wide = pick(0, 3) == 0, group = pick(1, 20), window = pick(0, 1) ? pick(1, round % 2 ? 3000 : 100) : 1 << 30, sinks = window < (1 << 30) && pick(0, 1) ? pick(0, 400) : 0;
-        const ChunkShape s = chunk_shape(group, wide ? 128 : 256, wide ? 64 : 128, window, sinks, pick(1, 8));
+        ChunkShape s = chunk_shape(group, wide ? 128 : 256, wide ? 64 : 128, window, sinks, pick(1, 8));
+        s.turns = !wide && pick(0, 1);
         for (int i = 0; i < 100; i++) {
             const int v = i < 50 ? i : pick(0, 2147483647 >> 1);
             if (chunk_by_group(s, v) != v / group) FAIL("%d / %d", v, group);
@@ -68,7 +69,8 @@ int main() {
             const int tiles = chunk_tiles(s, len[r]), parts = chunk_parts(tiles, share), blocks = chunk_blocks(s, n[r]);
             if (parts > kChunkMostParts) FAIL("%d parts", parts);
             items += (int64_t)blocks * parts * s.heads;
-            if (parts > 1) rows += (int64_t)n[r] * s.group * s.heads * parts;
+            if (parts > 1) rows += (int64_t)n[r] * s.group * s.heads * parts * (chunk_turns(s, n[r], parts) ? 2 : 1);
+            if (chunk_turns(s, n[r], parts) && (blocks > 1 || 2 * parts > kChunkMostParts)) FAIL("turns");
             const int pos0 = len[r] - n[r];
             int covered = 0;
             for (int b = 0; b < blocks; b++) {

@@ -174,7 +174,7 @@ def _plain_chunk(s):
     case = s["case"]
     size, hkv, hq, d, window, sinks = case["block"], case["hkv"], case["hq"], case["d"], case["window"], case["sinks"]
     for r, (n, total, start) in enumerate(zip(s["new"], s["total"], s["starts"])):
-        step = max(1, (1 << 28) // (hq * max(1, min(total, window + 1024 + sinks) if window else total)))
+        step = max(1, (1 << 28) // (hq * (min(total, window + 1024 + sinks) if window else max(total, 1))))
         step = min(step, 1024) if window else step
         for a in range(0, n, step):
             b = min(n, a + step)

@@ -994,6 +994,7 @@ __global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(con
                         if (lane == 5) word |= e < e_most - 40;
                         e_most = max(e_most, e);
                         if (lane == 4) word = __float_as_uint(static_cast<float>(e));
+                        if (lane == 6 && !ragged(item, i)) word = 0;  // what all rows see the products take, whatever it is
                         const int to = lane < 4 ? 4 * lane : lane < 6 ? 32 + 4 * (lane - 4) : 16;
                         if (lane < 7) asm volatile("st.shared.u32 [%0], %1;" ::"r"(about + to), "r"(word) : "memory");
                         if (lane >= 7 && lane < 10) asm volatile("st.shared.u32 [%0], %1;" ::"r"(about + 20 + 4 * (lane - 7)), "r"(0) : "memory");

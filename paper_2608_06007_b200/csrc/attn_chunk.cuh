@@ -976,7 +976,12 @@ __global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(con
                     const int t = tile_of(item, i), listed = t < item.firsts ? t : t - item.skip;
                     return p.wide + ((static_cast<int64_t>(item.r) * p.wide_list + listed) * H + item.h) * WideTile<DP>::bytes;
                 };
-                auto header = [&](int i) { return kv == 0 && lane < 8 && i < item.end ? reinterpret_cast<const uint32_t *>(place(i) + WideTile<DP>::header_at)[lane] : 0u; };
+                // lane by lane: of K the mask, the exponent and whether scales are far apart, of V whether it has numbers that are not finite; each is
+                // written by the warp whose copy it is read with, since neither waits for the other
+                auto header = [&](int i) {
+                    const bool some = (kv == 0 ? lane < 6 : kv == 1 && lane == 6) && i < item.end;
+                    return some ? reinterpret_cast<const uint32_t *>(place(i) + WideTile<DP>::header_at)[lane] : 0u;
+                };
                 uint32_t ahead = header(item.begin);
                 int e_most = kLeastExponent;  // the largest of a tile so far
                 if (kv >= 2 && item.begin < item.end) prepare_queries(item);
@@ -989,15 +994,15 @@ __global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(con
                     fine = __all_sync(0xffffffffu, stage_free(u));
                     if (!fine) break;
                     if (kv == 0) {
-                        // {mask, 4 words; exponent, whether scales are far apart, whether V has numbers that are not finite}
                         const int e = static_cast<int>(__shfl_sync(0xffffffffu, word, 4));
                         if (lane == 5) word |= e < e_most - 40;
                         e_most = max(e_most, e);
                         if (lane == 4) word = __float_as_uint(static_cast<float>(e));
-                        if (lane == 6 && !ragged(item, i)) word = 0;  // what all rows see the products take, whatever it is
-                        const int to = lane < 4 ? 4 * lane : lane < 6 ? 32 + 4 * (lane - 4) : 16;
-                        if (lane < 7) asm volatile("st.shared.u32 [%0], %1;" ::"r"(about + to), "r"(word) : "memory");
-                        if (lane >= 7 && lane < 10) asm volatile("st.shared.u32 [%0], %1;" ::"r"(about + 20 + 4 * (lane - 7)), "r"(0) : "memory");
+                        const int to = lane < 4 ? 4 * lane : 32 + 4 * (lane - 4);
+                        if (lane < 6) asm volatile("st.shared.u32 [%0], %1;" ::"r"(about + to), "r"(word) : "memory");
+                    } else if (lane >= 6 && lane < 10) {
+                        if (!ragged(item, i)) word = 0;  // what all rows see the products take, whatever it is
+                        asm volatile("st.shared.u32 [%0], %1;" ::"r"(about + 16 + 4 * (lane - 6)), "r"(word) : "memory");
                     }
                     __syncwarp();
                     if (lane == 0) {

@@ -589,8 +589,8 @@ TC_API int tc_attn_decode_window(const tc_kv_layer_t *layer, const tc_attn_decod
  * What a row does not see has no part in it, be it infinite or NaN.  A row whose every s_j is -infinity gets out 0 and lse -infinity.
  * lens[r] < 0: the request is padding.  A request with n = 0 is passed over.  Their rows, and rows in front of offsets[0] and
  * behind offsets[R], are left as they were; so are those of a request with n > max_new, lens[r] > max_len, lens[r] < n or
- * offsets that decrease or leave [0, n_tokens], which sets TC_DEVICE_BAD_INDEX (requests that share rows because offsets between
- * them decrease may get anything in all of theirs).
+ * offsets that decrease or leave [0, n_tokens], which sets TC_DEVICE_BAD_INDEX.  Where offsets decrease, requests that so share rows may get
+ * anything in them, and requests behind those may be left out: there is no room for more tokens than n_tokens.
  * Entries of a table are looked up for tokens that some row of the request sees; a block id that is out of range sets
  * TC_DEVICE_BAD_INDEX, and its tokens are left out.  Of a block with such tokens other slots may be read; they have no part in what is written.
  * Scores, softmax statistics and sums are fp32; codes of a quantised pool are taken exactly, their scales in fp32, and a

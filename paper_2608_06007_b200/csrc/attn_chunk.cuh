@@ -1278,6 +1278,10 @@ __global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(con
                             if (parts > 1) rows_at += static_cast<uint32_t>(q.n) * p.Hq * parts * each_leaves(q.n, parts);
                             continue;
                         }
+                        if (parts > 1 && !chunk_has_room(p.plan.part_rows, rows_at, static_cast<int64_t>(q.n) * p.Hq * parts * each_leaves(q.n, parts))) {
+                            if (id == at && lane == 0) p.cuts[r] = make_uint2(0, 0);
+                            break;
+                        }
                         // heads first, so that CTAs side by side read pages side by side; the last block, which sees most, first
                         uint32_t rest = id - at;
                         item.h = rest % H, rest /= H;

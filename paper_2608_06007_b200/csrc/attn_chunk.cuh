@@ -66,8 +66,9 @@ struct ChunkMemory {
     // {mask, 4 words; whether V has numbers that are not finite, up to 4 words}; codes: V's exponent, whether scales are far apart; each
     // warp's largest and smallest of V's scales; scales of K; keys' exponents; scales of V over the power of two
     static constexpr int info = KIND == kPlain ? 32 : 80 + 12 * keys, scales = 80;
-    // powers of two taken out of the queries, of four items where scores run two ahead (one slot), of two elsewhere
-    static constexpr int down_sets = 4 / slots, downs = KIND == kPlain ? 0 : 4 * 128 * 4;
+    // Powers of two taken out of the queries, of four items: an item's are written when its scores may be, and read by a slot whose softmax may be at
+    // the item before the last.  (It is no further behind: an item is published when all warps have taken the one before the last.)
+    static constexpr int down_sets = 4, downs = KIND == kPlain ? 0 : down_sets * slots * 128 * 4;
     static constexpr int table = 2 * ChunkWarps<KIND>::threads * 4;  // items, and rows of parts, before each thread's requests
     static constexpr int item = 80;
     static constexpr int rest = infos * info + downs + table + 2 * item + 16 + 512;

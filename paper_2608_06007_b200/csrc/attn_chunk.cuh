@@ -366,7 +366,7 @@ __global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(con
         }
     }
     uint32_t total;
-    {
+    for (;;) {
         uint32_t my_items = 0, my_rows = 0;
         for (int64_t r = run0; r < run1; r++) {
             const Extent e = r == run0 ? first : extent_of(r, true);
@@ -384,8 +384,14 @@ __global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(con
         __syncthreads();
         const uint32_t theirs = lane < W::all ? warp_items[lane] : 0, their_rows = lane < W::all ? warp_rows[lane] : 0;
         total = __reduce_add_sync(0xffffffffu, theirs);
+        if (!chunk_has_room(p.plan.part_rows, __reduce_add_sync(0xffffffffu, their_rows))) {
+            share = 1 << 30;
+            __syncthreads();
+            continue;
+        }
         upto += __reduce_add_sync(0xffffffffu, lane < warp ? theirs : 0), rows_upto += __reduce_add_sync(0xffffffffu, lane < warp ? their_rows : 0);
         items_before[threadIdx.x] = upto - my_items, rows_before[threadIdx.x] = rows_upto - my_rows;
+        break;
     }
     fence_before();
     __syncthreads();
@@ -1278,10 +1284,6 @@ __global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(con
                             at += here;
                             if (parts > 1) rows_at += static_cast<uint32_t>(q.n) * p.Hq * parts * each_leaves(q.n, parts);
                             continue;
-                        }
-                        if (parts > 1 && !chunk_has_room(p.plan.part_rows, rows_at, static_cast<int64_t>(q.n) * p.Hq * parts * each_leaves(q.n, parts))) {
-                            if (id == at && lane == 0) p.cuts[r] = make_uint2(0, 0);
-                            break;
                         }
                         // heads first, so that CTAs side by side read pages side by side; the last block, which sees most, first
                         uint32_t rest = id - at;

@@ -86,9 +86,9 @@ TC_HD int32_t chunk_parts(int32_t tiles, int32_t share) { return (tiles + share 
 // leaves a part of its own.  Codes that a CTA widens gain by it (8 tokens behind 120000, 56 rows a KV head, int8: 118 -> 100 us); 16-bit pools
 // lose more by twice the parts (70 -> 78 us).
 TC_HD bool chunk_turns(const ChunkShape &s, int32_t n, int32_t parts) { return s.turns && n * s.group <= 128 && parts > 1 && 2 * parts <= kChunkMostParts; }
-// Whether a request's rows of parts fit behind those before it.  They do where offsets do not decrease; where they do, requests share tokens, may
-// be more than a plan has room for, and those without room are left out.
-TC_HD bool chunk_has_room(int64_t part_rows, uint32_t rows_before, int64_t rows) { return rows_before + rows <= part_rows; }
+// Whether there is room for all rows of parts.  There is where offsets do not decrease; where they do, requests share tokens and may be more than
+// a plan counts, and then nothing is cut.
+TC_HD bool chunk_has_room(int64_t part_rows, int64_t rows) { return rows <= part_rows; }
 // The cuts that are looked at: into parts of so many tiles that the longest list has up to 1 .. 16, then up to 23, 30 .. 128.
 constexpr int kChunkCuts = 32;
 TC_HD int32_t chunk_share(int32_t most_tiles, int32_t cut)

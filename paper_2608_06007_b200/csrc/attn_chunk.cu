@@ -299,6 +299,7 @@ extern "C" int tc_attn_chunk(const tc_kv_layer_t *layer, const tc_attn_chunk_t *
     p.offsets = a->offsets, p.lens = a->lens;
     p.Hq = static_cast<int32_t>(a->Hq);
     p.q_bf16 = a->dtype == TC_BF16;
+    p.item_spins = static_cast<uint32_t>(chunk_patience(chunk_tiles(p.shape, static_cast<int32_t>(a->max_len)))) * kWaitSpins;
     p.scale_log2 = static_cast<float>((a->scale != 0.f ? static_cast<double>(a->scale) : 1.0 / std::sqrt(static_cast<double>(p.layer.D))) * 1.4426950408889634);
     p.div_block = make_fastdiv(p.layer.B);
     p.div_group = make_fastdiv(static_cast<uint32_t>(p.shape.group));

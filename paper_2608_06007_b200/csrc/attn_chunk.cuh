@@ -405,7 +405,7 @@ __global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(con
 
     // Item `it` of this CTA's; false when there is none, or a wait ran out.
     auto take_item = [&](int it, ChunkItem &item) {
-        if (!__all_sync(0xffffffffu, barrier_wait(item_full + 8 * (it & 1), (it >> 1) & 1))) {
+        if (!__all_sync(0xffffffffu, barrier_wait(item_full + 8 * (it & 1), (it >> 1) & 1, p.item_spins))) {
             fine = false;
             return false;
         }
@@ -1317,7 +1317,7 @@ __global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(con
                             barrier_arrive(item_full + 8 * (it & 1));
                         }
                         __syncwarp();
-                        fine = __all_sync(0xffffffffu, barrier_wait(wanted, it & 1));
+                        fine = __all_sync(0xffffffffu, barrier_wait(wanted, it & 1, p.item_spins));
                         if (!fine) break;
                         it++;
                     }

@@ -23,6 +23,7 @@ struct ChunkParams {
     int64_t R, n_tokens, max_new, max_len;
     int32_t Hq, q_bf16;
     int64_t new_from, new_to;  // requests with so many new tokens are this kernel's; others have their own, in the same call
+    uint32_t item_spins;       // of waits that may last as long as an item of all the keys there may be
     bool beside;               // launched behind a kernel of the same call that it need not wait for, but for its own end
     float scale_log2;    // scale * log2(e)
     FastDiv div_block, div_group;

@@ -55,6 +55,10 @@ TC_HD int32_t chunk_tiles_of(const ChunkShape &s, int32_t keys) { return (keys +
 // Tiles that a block of a request with `len` keys lists at most.
 TC_HD int32_t chunk_tiles(const ChunkShape &s, int32_t len) { return chunk_low(s.near_tiles + chunk_tiles_of(s, chunk_low(s.sinks, len)), chunk_tiles_of(s, len)); }
 
+// Seconds that a warp waits for an item of so many tiles to end: some 60 us a tile.  The slowest measured took 7.1 (256 rows, int8, D = 128, scales
+// far apart), so that an item of 2^24 keys takes 0.93 s at full clocks and more under a power cap.
+TC_HD int32_t chunk_patience(int32_t tiles) { return 1 + (tiles >> 14); }
+
 // The tiles that a block lists: the first `firsts`, which hold the keys that all rows see, then from tile firsts + skip on.
 struct ChunkList {
     int32_t key_end, key_low;  // keys below key_end, from key_low on or below `sinks`, are seen by some row

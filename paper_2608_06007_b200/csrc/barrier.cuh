@@ -14,11 +14,12 @@ __device__ __forceinline__ bool barrier_passed(uint32_t bar, uint32_t parity)
     return done != 0;
 }
 
-// Waits for the phase of that parity to end; false when it does not within about a second.
-__device__ __forceinline__ bool barrier_wait(uint32_t bar, uint32_t parity)
+// Waits for the phase of that parity to end; false when it does not within about a second, or as many as spins / kWaitSpins.
+constexpr uint32_t kWaitSpins = 1u << 20;
+__device__ __forceinline__ bool barrier_wait(uint32_t bar, uint32_t parity, uint32_t spins = kWaitSpins)
 {
     if (barrier_passed(bar, parity)) return true;
-    for (uint32_t spin = 0; spin < (1u << 20); spin++) {
+    for (uint32_t spin = 0; spin < spins; spin++) {
         uint32_t done;
         asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\tselp.u32 %0, 1, 0, p;\n\t}"
                      : "=r"(done) : "r"(bar), "r"(parity), "r"(1000u) : "memory");

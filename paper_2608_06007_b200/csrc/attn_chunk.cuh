@@ -264,6 +264,18 @@ __device__ __noinline__ float far_probabilities(uint32_t s_at, uint32_t p_at, Ro
     return sum;
 }
 
+// Where a wait ran out: boxes and runs may still be on their way to this CTA's shared memory, whoever asked for them.  Their barriers' phases end when
+// they are there; one that has none runs out.  bars_at: of `full`, in what the kernel has laid out.
+template <int STAGES>
+__device__ __noinline__ void copies_landed(uint32_t bars_at)
+{
+    extern __shared__ unsigned char raw[];
+    const uint32_t full = ((static_cast<uint32_t>(__cvta_generic_to_shared(raw)) + 1023) & ~1023u) + bars_at, i = threadIdx.x, q_full = full + 16 * STAGES + 64;
+    // q_full, answered, landed
+    const uint32_t bar = i < STAGES ? full + 8 * i : i == STAGES ? q_full : i == STAGES + 1 ? q_full + 56 : q_full + 80 + 8 * (i & 1);
+    if (i < STAGES + 4) barrier_wait(bar, barrier_passed(bar, 0));
+}
+
 // T: the type of the products, fp16 for codes.
 template <typename T, int KIND, int DP>
 __global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(const __grid_constant__ ChunkParams p)
@@ -1373,7 +1385,10 @@ __global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(con
     if (p.beside) await_last();  // who waits for this kernel waits for those before it, too
     if (!fine) atomicOr(p.status, static_cast<unsigned int>(TC_DEVICE_BULK_WAIT_TIMEOUT));
     fence_before();
-    __syncthreads();
+    if (!__syncthreads_and(fine)) {
+        copies_landed<M::stages>(kBarsAt);
+        __syncthreads();
+    }
     if (warp == kIssue) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tensor) : "memory");
 }
 

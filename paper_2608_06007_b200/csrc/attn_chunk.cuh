@@ -284,6 +284,9 @@ __global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(con
     using W = ChunkWarps<KIND>;
     // kMine: keys of a tile that a warp fetches
     constexpr int kKeys = M::keys, kSlots = M::slots, kMine = kKeys / 4, kWords = kKeys / 32, kLoad = W::softmax, kIssue = kLoad + W::loaders;
+    // Tiles made fp16: 8 prompts in a window of 2048, int8, 1.92 ms so, 2.11 where the compiler unrolls its waits.  Where codes are widened here it is
+    // the other way, for want of registers: 33 tokens behind 120000, int8, 191 us so and 151.
+    constexpr bool kRolled = KIND == kWide;
     constexpr float kLift = probability_lift<T>();
     extern __shared__ unsigned char raw[];
     allow_next();
@@ -417,7 +420,7 @@ __global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(con
 
     // Item `it` of this CTA's; false when there is none, or a wait ran out.
     auto take_item = [&](int it, ChunkItem &item) {
-        if (!__all_sync(0xffffffffu, barrier_wait(item_full + 8 * (it & 1), (it >> 1) & 1, p.item_spins))) {
+        if (!__all_sync(0xffffffffu, barrier_wait<kRolled>(item_full + 8 * (it & 1), (it >> 1) & 1, p.item_spins))) {
             fine = false;
             return false;
         }
@@ -430,8 +433,8 @@ __global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(con
         return item.valid != 0;
     };
     // Copy u (K of this CTA's tile u / 2, then V) is in stage u % stages: whether it is there, and whether copy u - stages is done with.
-    auto copied = [&](uint32_t u) { return barrier_wait(full + 8 * (u % M::stages), (u / M::stages) & 1); };
-    auto stage_free = [&](uint32_t u) { return u < M::stages || barrier_wait(empty + 8 * (u % M::stages), (u / M::stages - 1) & 1); };
+    auto copied = [&](uint32_t u) { return barrier_wait<kRolled>(full + 8 * (u % M::stages), (u / M::stages) & 1); };
+    auto stage_free = [&](uint32_t u) { return u < M::stages || barrier_wait<kRolled>(empty + 8 * (u % M::stages), (u / M::stages - 1) & 1); };
     // All rows of an item's queries, as boxes of whole tokens (one lane).
     auto copy_query_boxes = [&](const ChunkItem &item, uint32_t bar) {
         asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(item.rows > 128 ? M::queries : M::q_tile) : "memory");
@@ -496,7 +499,7 @@ __global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(con
                 if (!needs(item, slot, i)) continue;
                 // one slot: the scores have two buffers in turn
                 const uint32_t b = kSlots == 1 ? steps & 1 : slot, parity = kSlots == 1 ? (steps >> 1) & 1 : steps & 1, s_at = lanes + kScores + slot * kScoresStep + (kSlots == 1 ? (steps & 1) * kKeys : 0);
-                fine = __all_sync(0xffffffffu, barrier_wait(s_full + 8 * b, parity));
+                fine = __all_sync(0xffffffffu, barrier_wait<kRolled>(s_full + 8 * b, parity));
                 if (!fine) break;
                 fence_after();
                 const uint32_t about = info + (tiles % M::infos) * M::info;
@@ -504,7 +507,7 @@ __global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(con
                 bool rest = steps == 0;
                 auto await_rest = [&]() {
                     if (rest) return;
-                    fine = __all_sync(0xffffffffu, barrier_wait(o_added + 8 * slot, (steps - 1) & 1));
+                    fine = __all_sync(0xffffffffu, barrier_wait<kRolled>(o_added + 8 * slot, (steps - 1) & 1));
                     fence_after();
                     rest = true;
                 };
@@ -719,7 +722,7 @@ __global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(con
             const float log = all == 0.f ? -INFINITY : (lowest == -INFINITY ? 0.f : lowest) + log2f(all);
             char *const out = p.out + (item.token0 + token) * p.out_token + head * p.out_head;
             if (mine) {
-                fine = __all_sync(0xffffffffu, barrier_wait(o_added + 8 * slot, (steps - 1) & 1));
+                fine = __all_sync(0xffffffffu, barrier_wait<kRolled>(o_added + 8 * slot, (steps - 1) & 1));
                 if (!fine) break;
                 fence_after();
                 float inv = all == 0.f ? 0.f : 1.f / all;
@@ -779,9 +782,9 @@ __global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(con
         // Queries that meet codes: fp16 with a power of two taken out of each row; eight lanes have a row.
         auto prepare_queries = [&](const ChunkItem &item) {
             if (p.q_boxes) {
-                if (fine) fine = __all_sync(0xffffffffu, barrier_wait(landed, loads & 1));
+                if (fine) fine = __all_sync(0xffffffffu, barrier_wait<kRolled>(landed, loads & 1));
             } else if (loads && fine) {
-                fine = __all_sync(0xffffffffu, barrier_wait(q_empty, (loads - 1) & 1));
+                fine = __all_sync(0xffffffffu, barrier_wait<kRolled>(q_empty, (loads - 1) & 1));
             }
             const int rows = item.rows > 128 ? kSlots * 128 : 128;
 #pragma unroll 2
@@ -845,7 +848,7 @@ __global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(con
                     loads++;
                     return;
                 }
-                if (loads) fine = __all_sync(0xffffffffu, barrier_wait(q_empty, (loads - 1) & 1));
+                if (loads) fine = __all_sync(0xffffffffu, barrier_wait<kRolled>(q_empty, (loads - 1) & 1));
                 if (!fine) return;
                 if (p.q_boxes) {
                     if (lane == 0) copy_query_boxes(item, q_full);
@@ -946,7 +949,7 @@ __global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(con
                     }
                     if (look) {
                         if (box_rows) {
-                            fine = __all_sync(0xffffffffu, barrier_wait(landed + 8 * sub, looks & 1));
+                            fine = __all_sync(0xffffffffu, barrier_wait<kRolled>(landed + 8 * sub, looks & 1));
                             looks++;
                             if (!fine) break;
                         } else {
@@ -1187,7 +1190,7 @@ __global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(con
                 ChunkItem item;
                 if (!take_item(it, item)) break;
                 if (item.begin >= item.end) continue;
-                fine = __all_sync(0xffffffffu, barrier_wait(q_full, loads & 1));
+                fine = __all_sync(0xffffffffu, barrier_wait<kRolled>(q_full, loads & 1));
                 for (int i = item.begin; i < item.end && fine; i++, tiles++) {
                     const uint32_t u = 2 * tiles, stage = u % M::stages;
                     fine = copied(u);
@@ -1198,15 +1201,15 @@ __global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(con
                         uint32_t b, column = tensor + kScores;
                         if constexpr (kSlots == 1) {
                             b = steps[0] & 1, column += b * kKeys;
-                            if (steps[0] >= 2 && fine) fine = barrier_wait(s_taken + 8 * b, ((steps[0] >> 1) - 1) & 1);
+                            if (steps[0] >= 2 && fine) fine = barrier_wait<kRolled>(s_taken + 8 * b, ((steps[0] >> 1) - 1) & 1);
                         } else if constexpr (kInPlace) {
                             // the slot's columns are free when its last product has taken the probabilities that lay in them
                             b = slot, column += slot * kScoresStep;
-                            if (steps[slot] && fine) fine = barrier_wait(o_added + 8 * slot, (steps[slot] - 1) & 1);
+                            if (steps[slot] && fine) fine = barrier_wait<kRolled>(o_added + 8 * slot, (steps[slot] - 1) & 1);
                         } else {
                             // the buffer is free when the scores of the step before have been taken
                             b = slot;
-                            if (before >= 0 && fine) fine = barrier_wait(s_taken + 8 * before, (steps[before] - 1) & 1);
+                            if (before >= 0 && fine) fine = barrier_wait<kRolled>(s_taken + 8 * before, (steps[before] - 1) & 1);
                         }
                         fine = __all_sync(0xffffffffu, fine);
                         if (!fine) break;
@@ -1250,7 +1253,7 @@ __global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(con
 #pragma unroll
                     for (int slot = 0; slot < kSlots; slot++) {
                         if (!needs(item, slot, i)) continue;
-                        fine = __all_sync(0xffffffffu, barrier_wait(p_ready + 8 * slot, steps[slot] & 1));
+                        fine = __all_sync(0xffffffffu, barrier_wait<kRolled>(p_ready + 8 * slot, steps[slot] & 1));
                         if (!fine) break;
                         fence_after();
                         if (elected()) {
@@ -1322,21 +1325,21 @@ __global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(con
                         break;
                     }
                     if (item.valid) {
-                        if (it >= 2) fine = __all_sync(0xffffffffu, barrier_wait(item_empty + 8 * (it & 1), ((it >> 1) - 1) & 1));
+                        if (it >= 2) fine = __all_sync(0xffffffffu, barrier_wait<kRolled>(item_empty + 8 * (it & 1), ((it >> 1) - 1) & 1));
                         if (!fine) break;
                         if (lane == 0) {
                             items[it & 1] = item;
                             barrier_arrive(item_full + 8 * (it & 1));
                         }
                         __syncwarp();
-                        fine = __all_sync(0xffffffffu, barrier_wait(wanted, it & 1, p.item_spins));
+                        fine = __all_sync(0xffffffffu, barrier_wait<kRolled>(wanted, it & 1, p.item_spins));
                         if (!fine) break;
                         it++;
                     }
                 }
                 if (!more) {
                     // no item: the end
-                    if (it >= 2) fine = __all_sync(0xffffffffu, barrier_wait(item_empty + 8 * (it & 1), ((it >> 1) - 1) & 1));
+                    if (it >= 2) fine = __all_sync(0xffffffffu, barrier_wait<kRolled>(item_empty + 8 * (it & 1), ((it >> 1) - 1) & 1));
                     if (lane == 0) {
                         items[it & 1].valid = 0;
                         barrier_arrive(item_full + 8 * (it & 1));
@@ -1349,7 +1352,7 @@ __global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(con
                     asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];" ::"r"(answer), "r"(answered) : "memory");
                 }
                 __syncwarp();
-                fine = __all_sync(0xffffffffu, barrier_wait(answered, asked & 1));
+                fine = __all_sync(0xffffffffu, barrier_wait<kRolled>(answered, asked & 1));
                 asked++;
                 if (!fine) break;
                 uint32_t got, next = 0;
@@ -1368,7 +1371,7 @@ __global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(con
                 ChunkItem item;
                 if (!take_item(it, item)) break;
                 if (item.begin >= item.end) continue;
-                if (loads) fine = __all_sync(0xffffffffu, barrier_wait(q_empty, (loads - 1) & 1));
+                if (loads) fine = __all_sync(0xffffffffu, barrier_wait<kRolled>(q_empty, (loads - 1) & 1));
                 if (fine && lane == 0) copy_query_boxes(item, landed);
                 __syncwarp();
                 loads++;
@@ -1379,7 +1382,7 @@ __global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(con
             const uint32_t last = last_at + 8 * (warp - kIssue);
             if (elected()) commit_to(last);
             __syncwarp();
-            barrier_wait(last, 0);
+            barrier_wait<kRolled>(last, 0);
         }
     }
     if (p.beside) await_last();  // who waits for this kernel waits for those before it, too

@@ -44,8 +44,9 @@ __global__ void __launch_bounds__(128) chunk_join_kernel(const __grid_constant__
                 for (int x = 16; x; x >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
 #pragma unroll
                 for (int k = 0; k < 4; k++) {
-                    sum[k] = sum[k] == -INFINITY ? 0.f : exp2_approx(sum[k] - (top == -INFINITY ? 0.f : top) - kLess);  // NaN where the sum is
-                    all += sum[k];
+                    const bool some = sum[k] != -INFINITY;
+                    sum[k] = some ? exp2_approx(sum[k] - (top == -INFINITY ? 0.f : top) - kLess) : -1.f;  // NaN where the sum is; -1: no part, or one without weight
+                    if (some) all += sum[k];
                 }
 #pragma unroll
                 for (int x = 16; x; x >>= 1) all += __shfl_xor_sync(0xffffffffu, all, x);
@@ -63,7 +64,8 @@ __global__ void __launch_bounds__(128) chunk_join_kernel(const __grid_constant__
 #pragma unroll
                         for (int j = 0; j < 4; j++) {
                             const float w = __shfl_sync(0xffffffffu, sum[k], (j0 + j) & 31);
-                            if (w == 0.f || j0 + j >= parts) continue;  // what a part without keys left in its place is read but not used
+                            // what a part without keys left in its place is read but not used; one whose weight is 0 in fp32 may not be finite
+                            if (w < 0.f || j0 + j >= parts) continue;
 #pragma unroll
                             for (int x = 0; x < kVectors; x++) acc[4 * x] += w * v[j][x].x, acc[4 * x + 1] += w * v[j][x].y, acc[4 * x + 2] += w * v[j][x].z, acc[4 * x + 3] += w * v[j][x].w;
                         }

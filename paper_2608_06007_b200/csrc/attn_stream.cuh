@@ -762,8 +762,9 @@ __global__ void __launch_bounds__(WARPS == 1 ? 128 : 32 * WARPS, WARPS == 1 ? kJ
                         all *= f;
                         top = m;
                     }
-                    weight = sum == -INFINITY ? 0.f : exp2_approx(sum - (top == -INFINITY ? 0.f : top) - kLess);  // NaN where the sum is
-                    float add = weight;
+                    const bool some = sum != -INFINITY;
+                    weight = some ? exp2_approx(sum - (top == -INFINITY ? 0.f : top) - kLess) : -1.f;  // NaN where the sum is
+                    float add = some ? weight : 0.f;
 #pragma unroll
                     for (int x = 16; x; x >>= 1) add += __shfl_xor_sync(0xffffffffu, add, x);
                     all += add;
@@ -771,7 +772,7 @@ __global__ void __launch_bounds__(WARPS == 1 ? 128 : 32 * WARPS, WARPS == 1 ? kJ
 #pragma unroll
                 for (int j = 0; j < kAhead; j++) {
                     const float w = __shfl_sync(0xffffffffu, weight, (j0 + j) & 31);
-                    if (w == 0.f || j0 + j >= here) continue;
+                    if (w < 0.f || j0 + j >= here) continue;  // (one whose weight is 0 in fp32 may not be finite)
 #pragma unroll
                     for (int x = 0; x < kVectors; x++) acc[4 * x] += w * v[j][x].x, acc[4 * x + 1] += w * v[j][x].y, acc[4 * x + 2] += w * v[j][x].z, acc[4 * x + 3] += w * v[j][x].w;
                 }

@@ -106,12 +106,12 @@ def attend_chunk(q, keys, vals, scale, window=0, sinks=0, there=None):
             e = np.exp(s - np.where(m == -np.inf, 0, m)[:, None])  # NaN in rows with a score that is NaN or infinite
             total_e = e.sum(1)
             w = e / np.where(total_e == 0, 1, total_e)[:, None]
-            # a key that is not seen has no part, whatever its value is
+            some = total_e != 0
+            # a key that is not seen has no part, whatever its value is, and no key has where none has any weight
             bad = ~np.isfinite(v).all(1)
             out[:, h] = w @ np.where(bad[:, None], 0, v)
             for x in np.flatnonzero(bad):
-                out[seen[:, x], h] += w[seen[:, x], x][:, None] * v[x]
-            some = total_e != 0
+                out[seen[:, x] & some, h] += w[seen[:, x] & some, x][:, None] * v[x]
             lse[some, h] = m[some] + np.log(total_e[some])
         weights[:, h] = w
     return out, lse, weights

@@ -725,7 +725,7 @@ __global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(con
                 fine = __all_sync(0xffffffffu, barrier_wait<kRolled>(o_added + 8 * slot, (steps - 1) & 1));
                 if (!fine) break;
                 fence_after();
-                float inv = all == 0.f ? 0.f : 1.f / all;
+                float inv = 1.f / all;
                 if constexpr (KIND != kPlain) {
                     // outputs are relative to `top`: from there to `ref`, in two steps where fp32 does not hold one
                     float step = top - kLift - (lowest == -INFINITY ? 0.f : lowest);
@@ -742,7 +742,7 @@ __global__ void __launch_bounds__(ChunkWarps<KIND>::threads, 1) chunk_kernel(con
                     tensor_load32(o_at + 32 * c, v);
                     tensor_loaded();
 #pragma unroll
-                    for (int j = 0; j < 32; j++) v[j] = __float_as_uint(__uint_as_float(v[j]) * inv);
+                    for (int j = 0; j < 32; j++) v[j] = all == 0.f ? 0u : __float_as_uint(__uint_as_float(v[j]) * inv);  // (without weight 0, whatever V is)
                     if (cut) {
 #pragma unroll
                         for (int j = 0; j < 32; j += 4)

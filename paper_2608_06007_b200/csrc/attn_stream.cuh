@@ -640,7 +640,7 @@ __global__ void __launch_bounds__(128, DP > 128 ? 1 : NB > 1 ? 2 : DP == 64 ? 4 
                         for (int k = 0; k < DP / 16; k++)
 #pragma unroll
                             for (int half = 0; half < 2; half++) {
-                                const float x = o[nb][k][2 * half + j] * by;
+                                const float x = all == 0.f ? 0.f : o[nb][k][2 * half + j] * by;  // (without weight 0, whatever V is)
                                 if (16 * k >= D) continue;
                                 if (KIND == kPlain ? std::is_same<T, __nv_bfloat16>::value : p.q_bf16) reinterpret_cast<__nv_bfloat16 *>(out)[16 * k + g + 8 * half] = __float2bfloat16_rn(x);
                                 else reinterpret_cast<__half *>(out)[16 * k + g + 8 * half] = __float2half_rn(x);

@@ -45,7 +45,7 @@ def made(case, kind, x, D, total, many):
     return s
 
 
-def answer(case, s):
+def ask(case, s):
     if case == "window":
         run_window(s)
     elif case == "decode":
@@ -53,6 +53,10 @@ def answer(case, s):
         tc.tc_attn_decode(s["pool"].handle, s["dq"], s["out"], s["d"]["tables"], s["d"]["lens"], max_len=s["max_len"], lse=s["lse"], workspace=ws)
     else:
         run_chunk(s)
+
+
+def answer(case, s):
+    ask(case, s)
     (check_window if case in ("window", "decode") else check_chunk)(s)
 
 
@@ -68,4 +72,26 @@ def test_a_value_that_is_not_finite_is_seen_whatever_its_weight(case, x, kind, D
     set_rows(s, 1, 0, [token], bad)
     answer(case, s)  # as in 64 bits
     assert not torch.isfinite(s["out"][: s["new"][0] if case in ("chunk", "blocks") else 1]).any()
+    status_is(0)
+
+
+@pytest.mark.parametrize("x,kind", TYPES)
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("total", [20, 290, 3000])
+@pytest.mark.parametrize("case,many", [("chunk", False), ("blocks", False), ("singles", True), ("window", False), ("window", True), ("decode", False), ("decode", True)])
+def test_a_row_without_weight_gets_nothing_whatever_the_values_are(case, many, x, kind, D, total):
+    """Every score is -infinity: outputs are 0 and logarithms -infinity, as the header has it."""
+    total += 180 if case == "blocks" else 0
+    s = made(case, kind, x, D, total, many)
+    put(s, 0, 0, np.arange(total), -1.0 if kind in TOP else -float("inf"))
+    if kind in TOP:  # all codes are negative
+        t = np.arange(total)
+        s["pool"].scale(0)[torch.from_numpy(s["table"][0][t // s["pool"].B]).long().cuda(), torch.from_numpy(t % s["pool"].B).cuda()] = float("inf")
+    ask(case, s)
+    n = s["new"][0] if case in ("chunk", "blocks") else 1
+    for _ in range(2):
+        assert (s["out"][:n] == 0).all() and torch.isneginf(s["lse"][:n]).all()
+        set_rows(s, 1, 0, [7, total // 2], float("inf"))
+        ask(case, s)
+    assert (s["out"][:n] == 0).all() and torch.isneginf(s["lse"][:n]).all()
     status_is(0)

@@ -577,7 +577,9 @@ TC_API int tc_attn_decode(const tc_kv_layer_t *layer, const tc_attn_decode_t *ar
 
 /* tc_attn_decode over the keys j >= lens[r] - window and j < sinks alone (window >= 1, sinks >= 0): a request's last tokens and
  * its first ones, which stay visible however long it grows.  Slots of other tokens are never read, so that their blocks may be given
- * back; the table's entries for them may be anything.  There is no shared prefix (max_prefix = 0).  The workspace is tc_attn_workspace's for the same args. */
+ * back; the table's entries for them may be anything.  There is no shared prefix (max_prefix = 0).
+ * The workspace is tc_attn_workspace's for the same args, or for a max_len of window + sinks + 96 where that is less: fewer bytes, of lengths that
+ * tc_attn_decode has no room for, too. */
 TC_API int tc_attn_decode_window(const tc_kv_layer_t *layer, const tc_attn_decode_t *args, int64_t window, int64_t sinks, void *stream);
 
 /* Chunks of new tokens - pieces of prompts, whole prompts, tokens guessed ahead, single ones, any of them side by side - over a

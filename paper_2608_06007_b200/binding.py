@@ -610,9 +610,13 @@ def _lse(lse, n, heads):
     return lse.data_ptr()
 
 
-def tc_attn_workspace_bytes(layer: KVLayer, q, *, max_len, max_prefix=0) -> int:
-    """Bytes of workspace that tc_attn_decode needs for queries of this shape and these bounds.  Fewer requests may need
-    more: a program whose batch varies takes the largest over its sizes."""
+def tc_attn_workspace_bytes(layer: KVLayer, q, *, max_len, max_prefix=0, window=0, sinks=0) -> int:
+    """Bytes of workspace that tc_attn_decode needs for queries of this shape and these bounds, or with a window
+    tc_attn_decode_window.  Fewer requests may need more: a program whose batch varies takes the largest over its sizes."""
+    if window < 0 or sinks < 0 or bool(window and max_prefix) or bool(sinks and not window):
+        raise ValueError("window and sinks must not be negative; sinks go with a window, a prefix without one")
+    if window:
+        max_len = min(max_len, window + sinks + 96)
     out = C.c_int64()
     args = tc_attn_decode_t(C.sizeof(tc_attn_decode_t), _dtype(q)[0], q.shape[0], q.shape[1], max_len=max_len, max_prefix=max_prefix)
     _check(load_library().tc_attn_workspace(layer.ref, C.byref(args), C.byref(out)))

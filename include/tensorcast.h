@@ -448,6 +448,8 @@ TC_API int tc_kv_pack_noalloc(const tc_plan_spec_t *spec, const void *const *src
  *   tc_kv_gather    pages of a pool, quantised or not, back into contiguous rows
  *   tc_attn_decode  attention of one query token per request over a prefix that the whole batch
  *                   shares, read once for all of it, and over the request's own pages
+ *   tc_attn_decode_window  attention of one query token per request over its last tokens and its first
+ *   tc_attn_chunk   causal attention of any number of new tokens per request over its pages, or a window of them
  *
  * Quantised pools hold one byte per element, code, and one fp32 scale per (token, head) of K and
  * of V: the value is code * scale.  The scales are a paged pool of their own, addressed by the
@@ -704,7 +706,8 @@ TC_API int tc_trim(void);
  *       waited about a second for its asynchronous bulk copies into shared memory and gave up;
  *       the CTA returned without storing, so the destination of that call is incomplete.  Not
  *       expected to occur; the wait is bounded so that a failure cannot hang the device.  Likewise a
- *       CTA of tc_attn_decode's prefix kernel: the outputs of that call are then wrong.
+ *       CTA of tc_attn_decode's prefix kernel or of tc_attn_chunk's kernels (there for its warps' work on one
+ *       another's, a second for every 2^14 tiles of keys that a request may have): the outputs of that call are then wrong.
  * flags: host pointer.  The call synchronises the device first (every stream's previously
  * enqueued work, non-blocking streams included) and then copies the word back: it is a
  * diagnostic, off the data path. */
@@ -712,8 +715,8 @@ TC_API int tc_trim(void);
 #define TC_DEVICE_OUT_OF_BOUNDS 2u /* the bounds checker of a TC_PLAN_DEBUG_BOUNDS plan found a descriptor that
                                       reaches outside its table slot; copy kernels of such plans return
                                       without copying while the flag is set (read it to clear it) */
-#define TC_DEVICE_BAD_INDEX 4u /* tc_kv_append, tc_kv_gather or tc_attn_decode met a block id, slot, position or
-                                  length out of its range and left out what it named */
+#define TC_DEVICE_BAD_INDEX 4u /* tc_kv_append, tc_kv_gather, tc_attn_decode, tc_attn_decode_window or tc_attn_chunk met a block
+                                  id, slot, position, offset or length out of its range and left out what it named */
 TC_API int tc_device_status(uint32_t *flags);
 
 /* Run only the device-side bounds checker of a TC_PLAN_DEBUG_BOUNDS plan on `stream`: every

@@ -133,10 +133,13 @@ static int describe_boxes(ChunkParams *p)
 
 // Requests with one new token go to the stream where there may be some number of them: it reads codes at some 4 TB/s and 16-bit numbers
 // at 6, where items of 256 rows, of which these have a few, take a tile as slowly as if they were full (64 requests, 51 of them single, 200k tokens
-// of 8 heads x 128, e4m3: a call of 386 us so, 570 without, before requests of many blocks had kernels of their own).  Fewer are not worth its two launches.
+// of 8 heads x 128, e4m3: a call of 386 us so, 570 without, before requests of many blocks had kernels of their own).  Its two launches cost some 12 us,
+// and nothing else tells a call of fewer requests from one of prompts.  300 tokens behind 2000 beside R - 1 single ones behind 8000 (30000), us with it and
+// without: bf16 R = 4: 92 and 69 (137, 132), R = 8: 119, 107 (211, 225), R = 16: 158, 156 (344, 419); e4m3 R = 4: 102, 136 (129, 232), R = 8: 120, 210 (184, 437).
+// Prompts of 200 alone, bf16, R = 8: 46, 34.  So codes would gain from fewer than eight on, where some are single, and 16-bit pools lose up to there.
 constexpr int64_t kLeastSingles = 8;
-// Bytes of tiles made fp16 at most.  8 prompts of up to 15061 tokens in a window of 2048, int8, of 8 heads x 128: 2.07 ms so, with 493 MB of them, 3.12 where
-// each block widens its own; 64 requests, four of them of 104 to 374 new tokens behind up to 10883, e4m3: 286 us, of which these tiles take 32, and 387.
+// Bytes of tiles made fp16 at most.  8 prompts of up to 15061 tokens in a window of 2048, int8, of 8 heads x 128: 1.93 ms so, with 493 MB of them, 3.12 where
+// each block widens its own; 64 requests, four of them of 104 to 374 new tokens behind up to 10883, e4m3: 280 us, of which these tiles take 32, and 387.
 constexpr int64_t kMostWide = 1ll << 30;
 
 // What a call launches, in one workspace.
@@ -188,7 +191,9 @@ static int check_chunk(const tc_kv_layer_t *layer, const tc_attn_chunk_t *a, Chu
     }
     p->new_from = c->has_singles ? 2 : 1, p->new_to = a->max_new;
     // Codes that three blocks of a request's rows meet, or more, are made fp16 once, where the requests that may have as many fit into
-    // kMostWide; else those of the requests with the most new tokens.
+    // kMostWide; else those of the requests with the most new tokens.  16 requests of four query heads a KV head, e4m3, us so and where each block widens
+    // its own: two blocks behind 2000 176 and 188, three 221 and 261, four 266 and 335; behind 16000 (4 requests) 276 and 292, 342 and 403, 396 and 527.
+    // With nothing cached the tiles are few and it costs some 15: 67 and 52, 82 and 64, 96 and 84; two blocks lose there what they gain behind 2000.
     if (p->layer.quantised() && a->max_new > 1 && new_most * s.group > 2 * s.rows) {
         const int64_t near = (std::min<int64_t>(s.window, a->max_len) + new_most) / s.keys + 2 + chunk_tiles_of(s, static_cast<int32_t>(std::min<int64_t>(s.sinks, a->max_len)));
         const int64_t list = std::min<int64_t>(near, chunk_tiles_of(s, static_cast<int32_t>(a->max_len))), bytes = list * s.heads * wide_tile_bytes(D), room = kMostWide / bytes;

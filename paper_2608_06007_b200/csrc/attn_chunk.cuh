@@ -23,8 +23,8 @@
 //
 // What bounds it.  Two slots' products take 2048 clocks a tile of 128 keys at D = 128, and as many the exponentials, at 16 a clock
 // and SM; a slot's softmax is a chain of some 3000 (load 250, maximum 450, exponentials 1600, the rest and stores 600), of which two run side by
-// side.  Measured: 2048 tokens behind 6144 of 32 heads over 8 KV heads, bf16: 214 us, 1.12 PFLOP/s, 0.67 of a library's large product;
-// 8192 behind 24576, 64 heads: 6.7 ms, 1.14 PFLOP/s.  Two threads a row (16 warps of softmax) were slower, 290 us: half the registers, and both
+// side.  Measured: 2048 tokens behind 6144 of 32 heads over 8 KV heads, bf16: 215 us, 1.12 PFLOP/s, 0.67 of a library's large product, and 247 us, 0.97
+// PFLOP/s, under the power cap of a long run; 8192 behind 24576, 64 heads: 6.8 ms, 1.13 PFLOP/s, and 7.1.  Two threads a row (16 warps of softmax) were slower, 290 us: half the registers, and both
 // halves of a row wait for one another.  K and V have their own warps: with one for both, V's wait for a free stage held K's next back.
 // Codes that each CTA widens itself: 33 tokens behind 120000 of 28 heads over 4, int8: 151 us.  A slot's chain bounds it, 6100 clocks a
 // tile: its scores wait for the product before, whose probabilities lie in their place (1800), two passes (1500, 2400), the product; the eight

@@ -44,7 +44,7 @@ def test_more_requests_than_threads(x, kind, R, mixed):
 def test_short_prompts_of_one_slot_and_of_two(x, kind, D):
     """One tile of keys each, 240 rows of a KV head and then 40 to 120: a slot may be an item behind the other."""
     rng = np.random.default_rng(D)
-    new = [60 if i % 2 else int(rng.integers(10, 31)) for i in range(160)]
+    new = [60 if i % 2 else int(rng.integers(10, 31)) for i in range(80)]
     s = batch(kind, x, new, new, Hq=32, H=8, D=D, spread=2.0)
     run_chunk(s)
-    check_some(s, set(range(0, 160, 13)))
+    check_some(s, set(range(0, 80, 13)))

@@ -2,7 +2,7 @@
 import pytest
 import torch
 
-from attn_chunk import batch, check_chunk, run_chunk, set_rows
+from attn_chunk import TOP, batch, check_chunk, run_chunk, set_rows
 from test_operators_gpu import status_is
 
 pytestmark = pytest.mark.gpu
@@ -32,9 +32,12 @@ def others(t):
 @pytest.mark.parametrize("new", [40, 150])  # one block or two; three or more, over whose codes tiles are made fp16 before
 @pytest.mark.parametrize("bad", [float("nan"), float("inf")])
 def test_a_value_that_all_rows_see_leaves_them_no_finite_output(x, kind, D, new, bad):
+    s = requests(kind, x, D, new)
+    pool = s["pool"]
+    kept = [pool.raw.clone(), pool.scales.clone() if kind in TOP else None]
     # in the first tile of every item, in a later one, and among first tokens that stay visible
     for token, window, sinks in ((10, 0, 0), (200, 0, 0), (10, 120, 128)):
-        s = requests(kind, x, D, new, window=window, sinks=sinks)
+        s["window"], s["sinks"] = window, sinks
         clean, clean_lse = answers(s)
         set_rows(s, 1, BAD, [token], bad)
         out, lse = answers(s)
@@ -42,6 +45,9 @@ def test_a_value_that_all_rows_see_leaves_them_no_finite_output(x, kind, D, new,
         # the weights are what they were; a sum's exponentials and logarithm are good to 2^-18 and 2^-22, relative to whichever maximum
         assert ((lse - clean_lse).abs() <= 2 * (2.0 ** -18 + 2.0 ** -22 * clean_lse.abs())).all()
         assert torch.equal(others(out), others(clean)) and torch.equal(others(lse), others(clean_lse))
+        pool.raw.copy_(kept[0])
+        if kind in TOP:
+            pool.scales.copy_(kept[1])
     status_is(0)
 
 

@@ -706,8 +706,9 @@ TC_API int tc_trim(void);
  *       waited about a second for its asynchronous bulk copies into shared memory and gave up;
  *       the CTA returned without storing, so the destination of that call is incomplete.  Not
  *       expected to occur; the wait is bounded so that a failure cannot hang the device.  Likewise a
- *       CTA of tc_attn_decode's prefix kernel or of tc_attn_chunk's kernels (there for its warps' work on one
- *       another's, a second for every 2^14 tiles of keys that a request may have): the outputs of that call are then wrong.
+ *       CTA of tc_attn_decode's prefix kernel, and one of tc_attn_chunk's kernels, whose warps wait for one another (about
+ *       a second; for a request's keys to be gone through one more for every 2^14 tiles that max_len allows): the outputs of
+ *       that call are then wrong.
  * flags: host pointer.  The call synchronises the device first (every stream's previously
  * enqueued work, non-blocking streams included) and then copies the word back: it is a
  * diagnostic, off the data path. */
